@@ -671,6 +671,142 @@ void swapnet_engine_free(swapnet_engine* eng);
 int swapnet_gemm_noalloc(int32_t dtype, const void* A, const void* W, const void* bias, void* Y, int32_t M,
                          int32_t N, int32_t K, int32_t act, swapnet_stream stream);
 
+/* ------------------------------------------------- cached attention
+ * The attention of a decoder over its key-value cache as calls of their own,
+ * for programs that keep many sequences' caches themselves, and the calls
+ * that keep such a cache within its rows: every pass over swapped weights
+ * costs their whole transfer, so a program verifies a tree of drafted tokens
+ * in one pass (swapnet_attention_tree, swapnet_tree_accept) and bounds the
+ * cache beside the arena (swapnet_attention_weights, swapnet_cache_evict).
+ * The paper has no counterpart to these calls.
+ *
+ * Like swapnet_gemm_noalloc they allocate nothing, are asynchronous on
+ * `stream`, start after the work queued before them on it, and may be
+ * captured into a graph (make a first call on a device before any capture).
+ * They run on the current device, which has to hold the buffers.  Calls share
+ * nothing but what the caller passes: two calls that may run at the same time
+ * need workspaces of their own, and so do graphs that may be replayed at the
+ * same time.  Sizes are checked on the host; what lies in device memory
+ * (lens, counts, parents, rows) is checked there: a sequence with a value out
+ * of range is left alone (a row list's entry out of range adds nothing) and
+ * the next swapnet_engine_sync on the device reports
+ * SWAPNET_ERR_INVALID_ARG.
+ *
+ * Layout: element type F16 or BF16; a cache row holds the kv_heads heads of
+ * one position, head h at element h * head_dim; sequence b's row j is at
+ * element b * seq_stride + j * kv_stride of k and v.  Query t of sequence b is
+ * row b * tokens + t of q (heads * head_dim elements, stride q_stride).
+ * Strides are in elements, 0 = packed; pointers are 16-byte aligned and
+ * strides multiples of 8.  head_dim is 64 or 128; heads is a multiple of
+ * kv_heads (query head h reads key head h / (heads / kv_heads)). */
+typedef struct swapnet_cached_attention {
+  int32_t dtype;      /* SWAPNET_F16 or SWAPNET_BF16                          */
+  int32_t n_seq;      /* sequences                                            */
+  int32_t tokens;     /* queries per sequence (at most; see counts)           */
+  int32_t heads, kv_heads, head_dim;
+  int32_t max_seq;    /* rows of a sequence's cache                           */
+  float scale;        /* of q . k; 0 = 1 / sqrt(head_dim)                     */
+  const void* q;      /* rotated queries                                      */
+  const void* k;      /* key cache (rotated keys)                             */
+  const void* v;      /* value cache                                          */
+  const int32_t* lens;    /* [n_seq] rows of the cache in use                 */
+  const int32_t* counts;  /* [n_seq] queries in use, NULL = tokens            */
+  const int32_t* parents; /* [n_seq][tokens] a drafted node's parent: an earlier
+                             node, or -1 below the cached rows; NULL = a chain */
+  const int32_t* rows;    /* swapnet_attention_weights: [n_seq][tokens] the
+                             queries that count, NULL = 0, 1, 2, ...          */
+  const void* k_new;  /* drafted nodes' keys [n_seq * tokens], stride new_stride; */
+  const void* v_new;  /* and values; NULL = no draft                          */
+  void* out;          /* [n_seq * tokens][heads * head_dim], stride out_stride */
+  float* lse;         /* [n_seq][heads][tokens] natural log of the softmax sum
+                         of scaled scores (nullable for attention)            */
+  const float* weights_in; /* [n_seq][kv_heads][max_seq], NULL = zeros        */
+  float* weights;          /* the same shape, may be weights_in               */
+  int64_t q_stride, kv_stride, seq_stride, new_stride, out_stride;
+} swapnet_cached_attention;
+
+/* out[t] = sum_j softmax_j(scale q_t . k_j) v_j, exact in fp32 over
+ *   - with a draft (k_new): every cached row (j < lens) and, of the drafted
+ *     nodes, the query's own and its ancestors; at most 128 nodes;
+ *   - without: the queries are the cache's last `counts` rows, each sees the
+ *     rows up to its own (one token: a decode step on a cache that already
+ *     holds its row).  A query that sees no row gives 0 and lse = -inf.
+ * With `weights` (no draft): weights[j] = weights_in[j] + the attention that
+ * row j got from these queries, summed over the query heads that share its
+ * key head; more than 32 rows (tokens x heads / kv_heads) need lse.
+ * Queries at and behind counts, and weights at and behind lens, are left as
+ * they were.  Hidden rows may hold anything.  `workspace` is 256-byte aligned
+ * device memory of at least the bytes that _workspace returns (a function of
+ * the sizes alone), with nothing to keep in it between calls.
+ * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA. */
+int swapnet_attention_tree_workspace(const swapnet_cached_attention* args, uint64_t* bytes);
+int swapnet_attention_tree(const swapnet_cached_attention* args, void* workspace, uint64_t workspace_bytes,
+                           swapnet_stream stream);
+
+/* The weights alone, from lse of an earlier attention call: the i-th query is
+ * row rows[b][i] of q and of lse (i < counts[b]) and sits in cache row
+ * lens[b] - counts[b] + i; it adds e^(scale q . k_j - lse) to every row j up to
+ * its own.  After swapnet_tree_accept: rows = path, counts = accepted,
+ * lens = lens_out.  v, out and the workspace are not used. */
+int swapnet_attention_weights(const swapnet_cached_attention* args, swapnet_stream stream);
+
+/* Eviction: per sequence and key head, of lens rows keep min(lens, keep): the
+ * first `sink`, the last `recent` and those of the largest weights (NaN
+ * counts as the largest; among equal ones the lower row), in row order.  kept
+ * gets the rows kept, k_out / v_out / weights_out their contents in rows
+ * 0 .. min(lens, keep) - 1, lens_out their number.  What lies behind is left
+ * as it was.  All three may be the inputs themselves (in place, one layout
+ * for both); otherwise they must not overlap them.  Keys keep the rotation of
+ * the position they were written at.  head_dim: any multiple of 8 up to 512.
+ * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA. */
+typedef struct swapnet_cache_eviction {
+  int32_t dtype, n_seq, kv_heads, head_dim;
+  int32_t max_seq;       /* rows of an input cache, columns of weights          */
+  int32_t keep, recent, sink;
+  int32_t out_capacity;  /* rows of an output cache, columns of weights_out; 0 = max_seq */
+  int32_t reserved;
+  const void* k;
+  const void* v;
+  const float* weights;  /* [n_seq][kv_heads][max_seq]                          */
+  const int32_t* lens;   /* [n_seq]                                             */
+  void* k_out;
+  void* v_out;
+  float* weights_out;    /* [n_seq][kv_heads][out_capacity]                     */
+  int32_t* kept;         /* [n_seq][kv_heads][keep]                             */
+  int32_t* lens_out;     /* [n_seq], not lens itself                            */
+  int64_t kv_stride, seq_stride, out_stride, out_seq_stride;
+} swapnet_cache_eviction;
+int swapnet_cache_evict(const swapnet_cache_eviction* args, swapnet_stream stream);
+
+/* Greedy acceptance of a drafted tree: node 0 is the token that the last pass
+ * chose; from node i the path goes on to its lowest child whose id equals
+ * targets[i] (the model's choice at node i, e.g. ARGMAX), until there is none.
+ * path gets the accepted nodes in order (-1 behind them), accepted their
+ * number, next the model's choice at the last one, lens_out = lens + accepted;
+ * the accepted rows of every draft are appended to its cache at row lens.  A
+ * sequence whose cache has no room for its path, or with counts < 1, is left
+ * alone and reported as above.  At most 128 nodes and 256 caches.
+ * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA. */
+typedef struct swapnet_tree_acceptance {
+  int32_t dtype, n_seq, tokens;
+  int32_t width;          /* elements of a cache row                            */
+  int32_t max_seq, n_caches;
+  const int32_t* ids;     /* [n_seq][tokens] drafted tokens                     */
+  const int32_t* targets; /* [n_seq][tokens]                                    */
+  const int32_t* parents; /* [n_seq][tokens], NULL = a chain                    */
+  const int32_t* counts;  /* [n_seq], NULL = tokens                             */
+  const int32_t* lens;    /* [n_seq]                                            */
+  void* const* caches;       /* host array of n_caches device pointers: keys and
+                                values of every layer, one layout for all       */
+  const void* const* drafts; /* host array: [n_seq * tokens][width], stride new_stride */
+  int32_t* path;          /* [n_seq][tokens]                                    */
+  int32_t* accepted;      /* [n_seq]                                            */
+  int32_t* next;          /* [n_seq]                                            */
+  int32_t* lens_out;      /* [n_seq], not lens itself                           */
+  int64_t cache_stride, seq_stride, new_stride;
+} swapnet_tree_acceptance;
+int swapnet_tree_accept(const swapnet_tree_acceptance* args, swapnet_stream stream);
+
 /* --------------------------------------------------------- host weights */
 /* Page-locked, device-mapped host memory for weight storage (the pinned
  * host copy that Sec. 4.2's swap-in reads): allocated by the CUDA driver in

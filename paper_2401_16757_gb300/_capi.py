@@ -92,6 +92,29 @@ class EngineBlock(C.Structure):
                 ("zerocopy_us", C.c_float)]
 
 
+class CachedAttention(C.Structure):
+    """swapnet_cached_attention; pointers are device addresses as integers."""
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_seq", "tokens", "heads", "kv_heads", "head_dim", "max_seq")] + \
+        [("scale", C.c_float)] + \
+        [(n, C.c_void_p) for n in ("q", "k", "v", "lens", "counts", "parents", "rows", "k_new", "v_new", "out", "lse",
+                                   "weights_in", "weights")] + \
+        [(n, C.c_int64) for n in ("q_stride", "kv_stride", "seq_stride", "new_stride", "out_stride")]
+
+
+class CacheEviction(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_seq", "kv_heads", "head_dim", "max_seq", "keep", "recent", "sink",
+                                         "out_capacity", "reserved")] + \
+        [(n, C.c_void_p) for n in ("k", "v", "weights", "lens", "k_out", "v_out", "weights_out", "kept", "lens_out")] + \
+        [(n, C.c_int64) for n in ("kv_stride", "seq_stride", "out_stride", "out_seq_stride")]
+
+
+class TreeAcceptance(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_seq", "tokens", "width", "max_seq", "n_caches")] + \
+        [(n, C.c_void_p) for n in ("ids", "targets", "parents", "counts", "lens", "caches", "drafts", "path", "accepted",
+                                   "next", "lens_out")] + \
+        [(n, C.c_int64) for n in ("cache_stride", "seq_stride", "new_stride")]
+
+
 EXPORTS = ["swapnet_default_options", "swapnet_partition", "swapnet_plan_from_cuts", "swapnet_plan_resident",
            "swapnet_plan_info_get", "swapnet_plan_cuts", "swapnet_plan_units", "swapnet_plan_blocks",
            "swapnet_plan_output_offsets", "swapnet_plan_free", "swapnet_schedule", "swapnet_load",
@@ -104,7 +127,9 @@ EXPORTS = ["swapnet_default_options", "swapnet_partition", "swapnet_plan_from_cu
            "swapnet_engine_bind_state", "swapnet_strerror", "swapnet_last_error", "swapnet_debug_fail_next", "swapnet_gemm_noalloc",
            "swapnet_weights_file_write", "swapnet_weights_file_open", "swapnet_weights_file_info",
            "swapnet_weights_file_read", "swapnet_weights_file_close", "swapnet_load_file",
-           "swapnet_debug_wait_timeout", "swapnet_pack_bf16"]
+           "swapnet_debug_wait_timeout", "swapnet_pack_bf16",
+           "swapnet_attention_tree_workspace", "swapnet_attention_tree", "swapnet_attention_weights",
+           "swapnet_cache_evict", "swapnet_tree_accept"]
 
 _lib = None
 
@@ -177,6 +202,11 @@ def lib():
         "swapnet_weights_file_close": (None, [P]),
         "swapnet_load_file": (C.c_int, [P, P, P, C.c_uint64, P, C.c_uint64, C.POINTER(P)]),
         "swapnet_debug_wait_timeout": (C.c_int, [P]),
+        "swapnet_attention_tree_workspace": (C.c_int, [C.POINTER(CachedAttention), C.POINTER(C.c_uint64)]),
+        "swapnet_attention_tree": (C.c_int, [C.POINTER(CachedAttention), P, C.c_uint64, P]),
+        "swapnet_attention_weights": (C.c_int, [C.POINTER(CachedAttention), P]),
+        "swapnet_cache_evict": (C.c_int, [C.POINTER(CacheEviction), P]),
+        "swapnet_tree_accept": (C.c_int, [C.POINTER(TreeAcceptance), P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -362,6 +392,60 @@ def gemm_noalloc(dtype, a_ptr, w_ptr, bias_ptr, y_ptr, M, N, K, act=0, stream=0)
     check(lib().swapnet_gemm_noalloc(dtype, C.c_void_p(a_ptr), C.c_void_p(w_ptr), C.c_void_p(bias_ptr),
                                      C.c_void_p(y_ptr), M, N, K, act, C.c_void_p(stream or None)),
           "swapnet_gemm_noalloc")
+
+
+# -------------------------------------------------------- cached attention
+def cached_attention(dtype, n_seq, tokens, heads, kv_heads, head_dim, max_seq, q, k, lens, v=0, out=0, lse=0, counts=0,
+                     parents=0, rows=0, k_new=0, v_new=0, weights_in=0, weights=0, scale=0.0, q_stride=0, kv_stride=0,
+                     seq_stride=0, new_stride=0, out_stride=0):
+    """The arguments of attention_tree and attention_weights: sizes, then
+    device addresses (0: none), then strides in elements (0: packed)."""
+    return CachedAttention(DTYPE.get(dtype, dtype), n_seq, tokens, heads, kv_heads, head_dim, max_seq, scale, q or None,
+                           k or None, v or None, lens or None, counts or None, parents or None, rows or None,
+                           k_new or None, v_new or None, out or None, lse or None, weights_in or None, weights or None,
+                           q_stride, kv_stride, seq_stride, new_stride, out_stride)
+
+
+def attention_tree_workspace(args):
+    """Bytes of device memory that attention_tree needs beside its operands."""
+    n = C.c_uint64()
+    check(lib().swapnet_attention_tree_workspace(C.byref(args), C.byref(n)), "swapnet_attention_tree_workspace")
+    return n.value
+
+
+def attention_tree(args, workspace=0, workspace_bytes=0, stream=0):
+    """Attention of the queries (a drafted tree, or the cache's last rows) over the cache."""
+    check(lib().swapnet_attention_tree(C.byref(args), workspace or None, workspace_bytes, stream or None),
+          "swapnet_attention_tree")
+
+
+def attention_weights(args, stream=0):
+    """The attention that each cached row got, added up from the queries and lse."""
+    check(lib().swapnet_attention_weights(C.byref(args), stream or None), "swapnet_attention_weights")
+
+
+def cache_evict(dtype, n_seq, kv_heads, head_dim, max_seq, keep, recent, sink, k, v, weights, lens, k_out, v_out,
+                weights_out, kept, lens_out, out_capacity=0, kv_stride=0, seq_stride=0, out_stride=0, out_seq_stride=0,
+                stream=0):
+    """Keeps the rows of each sequence and key head that got the most attention."""
+    a = CacheEviction(DTYPE.get(dtype, dtype), n_seq, kv_heads, head_dim, max_seq, keep, recent, sink, out_capacity, 0,
+                      k or None, v or None, weights or None, lens or None, k_out or None, v_out or None,
+                      weights_out or None, kept or None, lens_out or None, kv_stride, seq_stride, out_stride,
+                      out_seq_stride)
+    check(lib().swapnet_cache_evict(C.byref(a), stream or None), "swapnet_cache_evict")
+
+
+def tree_accept(dtype, n_seq, tokens, width, max_seq, ids, targets, lens, caches, drafts, path, accepted, next, lens_out,
+                parents=0, counts=0, cache_stride=0, seq_stride=0, new_stride=0, stream=0):
+    """Greedy acceptance of a drafted tree; caches and drafts are numpy uint64
+    arrays of device addresses (keys and values of every layer)."""
+    caches, drafts = (np.ascontiguousarray(x, dtype=np.uint64) for x in (caches, drafts))
+    if caches.size != drafts.size:
+        raise ValueError("as many drafts as caches")
+    a = TreeAcceptance(DTYPE.get(dtype, dtype), n_seq, tokens, width, max_seq, caches.size, ids or None, targets or None,
+                       parents or None, counts or None, lens or None, caches.ctypes.data, drafts.ctypes.data, path or None,
+                       accepted or None, next or None, lens_out or None, cache_stride, seq_stride, new_stride)
+    check(lib().swapnet_tree_accept(C.byref(a), stream or None), "swapnet_tree_accept")
 
 
 # ------------------------------------------------------------ host weights

@@ -1,0 +1,278 @@
+// Entry points of the cached-attention operators: argument checks, the choice
+// of kernels and the workspace.  Nothing is allocated and nothing waits for
+// the device.
+#include <algorithm>
+#include <atomic>
+#include <cmath>
+#include <cstring>
+
+#include "cached.h"
+#include "internal.h"
+#include "kernels.h"
+
+namespace swapnet {
+
+// Splits of a (sequence, key head)'s keys: enough CTAs for every SM to hold
+// two of them, twice over where the cache is long enough for 256 keys each.
+CachedPlan cached_plan(const CachedArgs& a) {
+  CachedPlan p;
+  std::memset(&p, 0, sizeof(p));
+  const int64_t rows = (int64_t)a.tokens * a.group;
+  const int64_t pairs = (int64_t)a.n_seq * a.kv_heads * ((rows + 31) / 32);
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((4 * 152 + pairs - 1) / pairs, (a.max_seq + 255) / 256));
+  p.spill = a.weights && rows <= 32;
+  p.score_ld = (a.max_seq + 15) / 16 * 16;
+  const uint64_t all = (uint64_t)a.n_seq * a.kv_heads * rows;
+  if (p.splits > 1) p.part_bytes = align_up(all * p.splits * a.dim * 4);
+  if (p.splits > 1 || p.spill) p.ml_bytes = align_up(all * p.splits * 8);
+  if (p.spill) p.score_bytes = align_up(all * p.score_ld * 4);
+  return p;
+}
+
+namespace {
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// What both attention entry points require of their arguments.
+int fill_args(const swapnet_cached_attention* c, CachedArgs* a) {
+  if (!c) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "null arguments");
+  std::memset(a, 0, sizeof(*a));
+  if (c->dtype != SWAPNET_F16 && c->dtype != SWAPNET_BF16) SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "cached attention: fp16 or bf16 only");
+  if (c->n_seq < 1 || c->tokens < 1 || c->heads < 1 || c->kv_heads < 1 || c->max_seq < 1)
+    SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cached attention: empty shape");
+  if (c->heads % c->kv_heads) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cached attention: heads must be a multiple of kv_heads");
+  if (c->head_dim != 64 && c->head_dim != 128) SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "cached attention: head width must be 64 or 128");
+  const int64_t group = c->heads / c->kv_heads;
+  if (c->n_seq > 65535 || c->kv_heads > 65535 || group > 128 || (int64_t)c->tokens * group > (1 << 20) || c->max_seq > (1 << 30))
+    SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "cached attention: shape beyond the kernels' limits");
+  if (!c->q || !c->k || !c->lens) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cached attention: null pointer");
+  const int64_t kv_width = (int64_t)c->kv_heads * c->head_dim, width = (int64_t)c->heads * c->head_dim;
+  a->dtype = c->dtype;
+  a->n_seq = c->n_seq;
+  a->tokens = c->tokens;
+  a->heads = c->heads;
+  a->kv_heads = c->kv_heads;
+  a->group = (int)group;
+  a->dim = c->head_dim;
+  a->max_seq = c->max_seq;
+  if (!(c->scale >= 0.f) || std::isinf(c->scale)) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cached attention: bad scale");
+  a->scale_log2 = 1.4426950408889634f * (c->scale > 0.f ? c->scale : 1.0f / sqrtf((float)c->head_dim));
+  a->q = c->q;
+  a->k = c->k;
+  a->v = c->v;
+  a->k_new = c->k_new;
+  a->v_new = c->v_new;
+  a->q_stride = c->q_stride ? c->q_stride : width;
+  a->kv_stride = c->kv_stride ? c->kv_stride : kv_width;
+  a->seq_stride = c->seq_stride ? c->seq_stride : a->kv_stride * c->max_seq;
+  a->new_stride = c->new_stride ? c->new_stride : kv_width;
+  a->out_stride = c->out_stride ? c->out_stride : width;
+  if (a->q_stride < width || a->kv_stride < kv_width || a->new_stride < kv_width || a->out_stride < width ||
+      (c->n_seq > 1 && a->seq_stride < 1))
+    SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cached attention: a stride is smaller than a row");
+  if ((a->q_stride | a->kv_stride | a->seq_stride | a->new_stride | a->out_stride) % 8)
+    SN_FAIL(SWAPNET_ERR_MISALIGNED, "cached attention: strides must be multiples of 8 elements");
+  if (!aligned16(c->q) || !aligned16(c->k) || !aligned16(c->v) || !aligned16(c->k_new) || !aligned16(c->v_new) || !aligned16(c->out))
+    SN_FAIL(SWAPNET_ERR_MISALIGNED, "cached attention: pointers must be 16-byte aligned");
+  a->lens = c->lens;
+  a->counts = c->counts;
+  a->parents = c->parents;
+  a->rows = c->rows;
+  a->out = c->out;
+  a->lse = c->lse;
+  a->weights_in = c->weights_in;
+  a->weights = c->weights;
+  return SWAPNET_OK;
+}
+
+// The attention call's own rules, on top of fill_args.
+int check_attention(const swapnet_cached_attention* c, CachedArgs* a) {
+  if (int rc = fill_args(c, a)) return rc;
+  if (!c->v || !c->out) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention: null pointer");
+  if (c->rows) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention: a row list is for swapnet_attention_weights");
+  if (!c->k_new != !c->v_new) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention: drafted keys and values come together");
+  if (c->parents && !c->k_new) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention: a tree's nodes are given as k_new and v_new");
+  if (c->k_new && c->tokens > kTreeMax) SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "attention: at most 128 drafted nodes a sequence");
+  if (c->weights && c->k_new)
+    SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention: weights with a draft come from swapnet_attention_weights, once it is accepted");
+  if (c->weights_in && !c->weights) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention: weights_in without weights");
+  if (c->weights && cached_plan(*a).spill == 0 && !c->lse)
+    SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention: weights of more than 32 rows (tokens x heads / kv_heads) need lse");
+  return SWAPNET_OK;
+}
+
+// The device error word of the current device (looked up once per device).
+int error_word(int** out) {
+  static std::atomic<int*> cached[64];
+  const int dev = device_index();
+  if (dev >= 0)
+    if (int* p = cached[dev].load(std::memory_order_acquire)) {
+      *out = p;
+      return SWAPNET_OK;
+    }
+  if (int rc = tc_error_word(out)) return rc;
+  if (dev >= 0) cached[dev].store(*out, std::memory_order_release);
+  return SWAPNET_OK;
+}
+
+}  // namespace
+}  // namespace swapnet
+
+extern "C" {
+
+int swapnet_attention_tree_workspace(const swapnet_cached_attention* c, uint64_t* bytes) {
+  return swapnet::guard_abi([&]() -> int {
+    using namespace swapnet;
+    if (!bytes) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "null output");
+    CachedArgs a;
+    if (int rc = check_attention(c, &a)) return rc;
+    const CachedPlan p = cached_plan(a);
+    *bytes = p.part_bytes + p.ml_bytes + p.score_bytes;
+    return SWAPNET_OK;
+  });
+}
+
+int swapnet_attention_tree(const swapnet_cached_attention* c, void* workspace, uint64_t workspace_bytes, swapnet_stream stream) {
+  return swapnet::guard_abi([&]() -> int {
+    using namespace swapnet;
+    CachedArgs a;
+    if (int rc = check_attention(c, &a)) return rc;
+    const CachedPlan p = cached_plan(a);
+    const uint64_t need = p.part_bytes + p.ml_bytes + p.score_bytes;
+    if (need && !workspace) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention: null workspace");
+    if (workspace_bytes < need) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention: workspace too small");
+    if (need && ((uintptr_t)workspace & (kAlign - 1))) SN_FAIL(SWAPNET_ERR_MISALIGNED, "attention: workspace must be 256-byte aligned");
+    if (int rc = error_word(&a.err)) return rc;
+    char* w = static_cast<char*>(workspace);
+    a.splits = p.splits;
+    a.part = reinterpret_cast<float*>(w);
+    a.ml = reinterpret_cast<float*>(w + p.part_bytes);
+    a.scores = p.spill ? reinterpret_cast<float*>(w + p.part_bytes + p.ml_bytes) : nullptr;
+    a.score_ld = p.score_ld;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    if (int rc = launch_attention_few(a, false, s)) return rc;
+    if (int rc = launch_attention_join(a, s)) return rc;
+    if (a.weights && !p.spill) return launch_weights_few(a, true, s);
+    return SWAPNET_OK;
+  });
+}
+
+int swapnet_attention_weights(const swapnet_cached_attention* c, swapnet_stream stream) {
+  return swapnet::guard_abi([&]() -> int {
+    using namespace swapnet;
+    CachedArgs a;
+    if (int rc = fill_args(c, &a)) return rc;
+    if (!c->lse || !c->weights) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cache weights: null pointer");
+    if (c->k_new || c->v_new || c->parents) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cache weights: the queries are rows of the cache");
+    if (int rc = error_word(&a.err)) return rc;
+    return launch_weights_few(a, false, reinterpret_cast<cudaStream_t>(stream));
+  });
+}
+
+int swapnet_cache_evict(const swapnet_cache_eviction* c, swapnet_stream stream) {
+  return swapnet::guard_abi([&]() -> int {
+    using namespace swapnet;
+    if (!c) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "null arguments");
+    EvictArgs a;
+    std::memset(&a, 0, sizeof(a));
+    if (c->dtype != SWAPNET_F16 && c->dtype != SWAPNET_BF16) SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "eviction: fp16 or bf16 only");
+    if (c->n_seq < 1 || c->kv_heads < 1 || c->head_dim < 1 || c->max_seq < 1 || c->keep < 1)
+      SN_FAIL(SWAPNET_ERR_INVALID_ARG, "eviction: empty shape");
+    if (c->head_dim % 8 || c->head_dim > 512) SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "eviction: head width must be a multiple of 8, at most 512");
+    if (c->n_seq > 65535 || c->kv_heads > 65535 || c->max_seq > (1 << 30))
+      SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "eviction: shape beyond the kernels' limits");
+    if (c->recent < 0 || c->sink < 0 || (int64_t)c->recent + c->sink > c->keep)
+      SN_FAIL(SWAPNET_ERR_INVALID_ARG, "eviction: sink + recent must be within keep");
+    if (!c->k || !c->v || !c->weights || !c->lens || !c->k_out || !c->v_out || !c->weights_out || !c->kept || !c->lens_out)
+      SN_FAIL(SWAPNET_ERR_INVALID_ARG, "eviction: null pointer");
+    const int64_t width = (int64_t)c->kv_heads * c->head_dim;
+    a.dtype = c->dtype;
+    a.n_seq = c->n_seq;
+    a.kv_heads = c->kv_heads;
+    a.dim = c->head_dim;
+    a.max_seq = c->max_seq;
+    a.keep = c->keep;
+    a.recent = c->recent;
+    a.sink = c->sink;
+    a.out_seq = c->out_capacity ? c->out_capacity : c->max_seq;
+    a.kv_stride = c->kv_stride ? c->kv_stride : width;
+    a.seq_stride = c->seq_stride ? c->seq_stride : a.kv_stride * c->max_seq;
+    a.out_stride = c->out_stride ? c->out_stride : width;
+    a.out_seq_stride = c->out_seq_stride ? c->out_seq_stride : a.out_stride * a.out_seq;
+    a.k = c->k;
+    a.v = c->v;
+    a.k_out = c->k_out;
+    a.v_out = c->v_out;
+    a.weights = c->weights;
+    a.weights_out = c->weights_out;
+    a.lens = c->lens;
+    a.kept = c->kept;
+    a.lens_out = c->lens_out;
+    if (a.out_seq < a.keep) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "eviction: out_capacity smaller than keep");
+    if (a.kv_stride < width || a.out_stride < width || (c->n_seq > 1 && (a.seq_stride < 1 || a.out_seq_stride < 1)))
+      SN_FAIL(SWAPNET_ERR_INVALID_ARG, "eviction: a stride is smaller than a row");
+    if ((a.kv_stride | a.seq_stride | a.out_stride | a.out_seq_stride) % 8 || !aligned16(a.k) || !aligned16(a.v) ||
+        !aligned16(a.k_out) || !aligned16(a.v_out))
+      SN_FAIL(SWAPNET_ERR_MISALIGNED, "eviction: caches and strides must be 16-byte aligned");
+    // in place means the same rows: another layout over the same memory would be read after it was written
+    const bool same[3] = {a.k == a.k_out, a.v == a.v_out, a.weights == a.weights_out};
+    if (same[0] != same[1] || same[0] != same[2])
+      SN_FAIL(SWAPNET_ERR_INVALID_ARG, "eviction: keys, values and weights are all moved in place or all to other buffers");
+    if (same[0] && (a.kv_stride != a.out_stride || a.seq_stride != a.out_seq_stride || a.out_seq != a.max_seq))
+      SN_FAIL(SWAPNET_ERR_INVALID_ARG, "eviction: in place the output has the input's layout");
+    if (a.lens == a.lens_out) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "eviction: lens_out must not be lens (every head reads lens)");
+    if (a.k_out == a.v_out) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "eviction: keys and values share an output");
+    if (int rc = error_word(&a.err)) return rc;
+    return launch_cache_evict(a, reinterpret_cast<cudaStream_t>(stream));
+  });
+}
+
+int swapnet_tree_accept(const swapnet_tree_acceptance* c, swapnet_stream stream) {
+  return swapnet::guard_abi([&]() -> int {
+    using namespace swapnet;
+    if (!c) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "null arguments");
+    AcceptArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.es = dtype_size(c->dtype);
+    if (c->dtype != SWAPNET_F16 && c->dtype != SWAPNET_BF16) SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "tree acceptance: fp16 or bf16 only");
+    if (c->n_seq < 1 || c->tokens < 1 || c->width < 1 || c->max_seq < 1 || c->n_caches < 0)
+      SN_FAIL(SWAPNET_ERR_INVALID_ARG, "tree acceptance: empty shape");
+    if (c->tokens > kTreeMax || c->n_caches > kAcceptMaxCaches || c->n_seq > 65535 || c->max_seq > (1 << 30))
+      SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "tree acceptance: at most 128 nodes a sequence and 256 caches");
+    if (c->width % 8) SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "tree acceptance: width must be a multiple of 8");
+    if (!c->ids || !c->targets || !c->lens || !c->path || !c->accepted || !c->next || !c->lens_out || (c->n_caches && (!c->caches || !c->drafts)))
+      SN_FAIL(SWAPNET_ERR_INVALID_ARG, "tree acceptance: null pointer");
+    a.n_seq = c->n_seq;
+    a.tokens = c->tokens;
+    a.width = c->width;
+    a.max_seq = c->max_seq;
+    a.n_caches = c->n_caches;
+    a.cache_stride = c->cache_stride ? c->cache_stride : c->width;
+    a.seq_stride = c->seq_stride ? c->seq_stride : a.cache_stride * c->max_seq;
+    a.new_stride = c->new_stride ? c->new_stride : c->width;
+    if (a.cache_stride < c->width || a.new_stride < c->width || (c->n_seq > 1 && a.seq_stride < 1))
+      SN_FAIL(SWAPNET_ERR_INVALID_ARG, "tree acceptance: a stride is smaller than a row");
+    if ((a.cache_stride | a.seq_stride | a.new_stride) % 8) SN_FAIL(SWAPNET_ERR_MISALIGNED, "tree acceptance: strides must be multiples of 8 elements");
+    for (int i = 0; i < c->n_caches; ++i) {
+      if (!c->caches[i] || !c->drafts[i]) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "tree acceptance: null cache");
+      if (!aligned16(c->caches[i]) || !aligned16(c->drafts[i]))
+        SN_FAIL(SWAPNET_ERR_MISALIGNED, "tree acceptance: caches must be 16-byte aligned");
+      a.caches[i] = c->caches[i];
+      a.drafts[i] = c->drafts[i];
+    }
+    a.ids = c->ids;
+    a.targets = c->targets;
+    a.parents = c->parents;
+    a.counts = c->counts;
+    a.lens = c->lens;
+    a.path = c->path;
+    a.accepted = c->accepted;
+    a.next = c->next;
+    a.lens_out = c->lens_out;
+    if (a.lens == a.lens_out) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "tree acceptance: lens_out must not be lens (every cache reads lens)");
+    if (int rc = error_word(&a.err)) return rc;
+    return launch_tree_accept(a, reinterpret_cast<cudaStream_t>(stream));
+  });
+}
+
+}  // extern "C"

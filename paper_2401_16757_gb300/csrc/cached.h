@@ -1,0 +1,73 @@
+// Internal interface of the cached-attention operators (swapnet_attention_tree,
+// swapnet_attention_weights, swapnet_cache_evict, swapnet_tree_accept): what
+// their kernels get, filled in by the entry points once the arguments have
+// been checked (cached.cpp).
+#pragma once
+#include <cuda_runtime.h>
+#include <cstdint>
+
+namespace swapnet {
+
+constexpr int kTreeMax = 128;  // drafted nodes of a sequence: one tile of keys, 128 ancestor bits
+
+// Row r of a (sequence, key head) is query r / group of the sequence for head
+// r % group of the group.
+struct CachedArgs {
+  int dtype, n_seq, tokens, heads, kv_heads, group, dim, max_seq;
+  float scale_log2;  // log2(e) * scale
+  const void *q, *k, *v, *k_new, *v_new;
+  int64_t q_stride, kv_stride, seq_stride, new_stride, out_stride;  // elements
+  const int *lens, *counts, *parents, *rows;
+  void* out;
+  float* lse;
+  const float* weights_in;
+  float* weights;
+  int* err;
+  // workspace (attention): per (sequence, key head, split, row) the outputs
+  // relative to that split's maximum, the maximum and the sum; with weights
+  // on the few-row kernel the scaled scores [sequence][key head][row][score_ld]
+  int splits;
+  float *part, *ml, *scores;
+  int64_t score_ld;
+};
+
+// How a call runs, from its sizes alone.
+struct CachedPlan {
+  int tc;       // tensor-core kernel (rows in tiles of 128)
+  int splits;   // CTAs that share the keys of a (sequence, key head)
+  int spill;    // weights from stored scores; 0: from a second pass over the keys
+  int64_t score_ld;
+  uint64_t part_bytes, ml_bytes, score_bytes;
+};
+CachedPlan cached_plan(const CachedArgs& a);
+
+int launch_attention_few(const CachedArgs& a, bool early, cudaStream_t s);
+int launch_attention_join(const CachedArgs& a, cudaStream_t s);   // splits -> out, lse (and weights from scores)
+int launch_weights_few(const CachedArgs& a, bool early, cudaStream_t s);
+
+struct EvictArgs {
+  int dtype, n_seq, kv_heads, dim, max_seq, keep, recent, sink, out_seq;
+  int64_t kv_stride, seq_stride, out_stride, out_seq_stride;
+  const void *k, *v;
+  void *k_out, *v_out;
+  const float* weights;
+  float* weights_out;
+  const int* lens;
+  int *kept, *lens_out;
+  int* err;
+};
+int launch_cache_evict(const EvictArgs& a, cudaStream_t s);
+
+constexpr int kAcceptMaxCaches = 256;
+struct AcceptArgs {
+  int es, n_seq, tokens, width, max_seq, n_caches;
+  int64_t cache_stride, seq_stride, new_stride;  // elements
+  const int *ids, *targets, *parents, *counts, *lens;
+  int *path, *accepted, *next, *lens_out;
+  int* err;
+  void* caches[kAcceptMaxCaches];
+  const void* drafts[kAcceptMaxCaches];
+};
+int launch_tree_accept(const AcceptArgs& a, cudaStream_t s);
+
+}  // namespace swapnet

@@ -1,0 +1,658 @@
+// Attention of a few queries over a long key-value cache (decode steps,
+// drafted trees), the join of its splits, and the weights that the cached rows
+// get.  fp16 / bf16 storage, fp32 arithmetic, fixed orders of summation.
+//
+// Rows of a (sequence, key head) are its queries times the heads that share
+// the key head: they read the same keys, so one warp-level product serves up
+// to 16 of them.
+#include <algorithm>
+#include <cstring>
+#include <string>
+#include <type_traits>
+
+#include "cached.cuh"
+#include "internal.h"
+#include "kernels.h"
+
+namespace swapnet {
+
+namespace {
+
+constexpr int kFwWarps = 4, kFwThreads = 32 * kFwWarps;
+constexpr int kGk = 16;      // keys of a group: one step of a warp
+constexpr int kFwStages = 3;
+
+template <int D, int MT> struct FewCfg {
+  static constexpr int kGroup = kGk * D * 2;          // bytes of a group's keys (or values)
+  static constexpr int kWarpRing = kFwStages * 2 * kGroup;
+  static constexpr int kRing = kFwWarps * kWarpRing;
+  static constexpr int kRows = 16 * MT;
+  static constexpr int kQ = kRows * D * 2;
+  static constexpr int kP = kFwWarps * kRows * kGk * 4;
+  static constexpr int kOffQ = kRing;
+  static constexpr int kOffP = kOffQ + kQ;
+  static constexpr int kOffMl = kOffP + kP;
+  static constexpr int kOffAnc = kOffMl + kFwWarps * kRows * 8;
+  static constexpr int kOffPar = kOffAnc + kTreeMax * 16;
+  static constexpr int kSmem = kOffPar + kTreeMax * 4;
+  static_assert(kFwWarps * kRows * D * 4 <= kRing, "the warps' outputs overlay the ring");
+};
+
+// Byte offset of 16-byte chunk `c` of row `r` in a tile of D-element rows:
+// chunks are exchanged within 128 bytes so that the eight rows of an
+// 8 x 8 matrix lie in different banks.
+template <int D> __device__ __forceinline__ uint32_t swz(int r, int c) { return (uint32_t)(r * (D * 2) + ((c ^ (r & 7)) << 4)); }
+
+// The rows' queries into shared memory (zeros behind the last row).
+template <typename T, int D>
+__device__ __forceinline__ void load_queries(const CachedArgs& a, int b, int kvh, int r0, int rows, int cap, uint8_t* dst,
+                                             const int* row_of) {
+  constexpr int C = D / 8;
+  for (int i = threadIdx.x; i < cap * C; i += blockDim.x) {
+    const int rl = i / C, c = i % C, r = r0 + rl;
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (r < rows) {
+      const int t = row_of ? row_of[rl] : r / a.group;
+      if (t >= 0)
+        v = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + ((int64_t)b * a.tokens + t) * a.q_stride +
+                                            (int64_t)(kvh * a.group + r % a.group) * D + c * 8);
+    }
+    *reinterpret_cast<uint4*>(dst + swz<D>(rl, c)) = v;
+  }
+}
+
+// ---------------------------------------------------------- few-row attention
+// One CTA: the keys [split] of a (sequence, key head) for up to 16 MT rows.
+// Its warps take groups of 16 keys in turn and keep a softmax of their own
+// (running maximum m, sum l, output O in registers), so nothing waits for
+// another warp until the end:
+//   S = Q K^T          8 mma.m16n8k16 a 16 rows for 128 dims
+//   p = 2^(S - m)      handed to the next product as two parts p_hi + p_lo of
+//                      the storage type, about 16 bits of p
+//   O = O 2^(m' - m) + p V
+// Keys and values pass through a ring of three groups a warp (cp.async; rows
+// behind the sequence's end arrive as zeros, whatever the cache holds there).
+// The kernel is bound by reading the cache: a group's 8 KB takes 48 products
+// of 16 rows, and the warp-level ones do that at several times DRAM's rate,
+// without the fixed costs (TMEM, barriers, 128-row tiles) of tcgen05.
+template <typename T, int D, int MT, bool SPILL>
+__global__ void __launch_bounds__(kFwThreads, 2) attention_few_kernel(const __grid_constant__ CachedArgs a) {
+  using F = FewCfg<D, MT>;
+  extern __shared__ __align__(128) uint8_t smem[];
+  uint32_t(*anc)[4] = reinterpret_cast<uint32_t(*)[4]>(smem + F::kOffAnc);
+  int* par = reinterpret_cast<int*>(smem + F::kOffPar);
+  float2* mls = reinterpret_cast<float2*>(smem + F::kOffMl);
+  const int split = blockIdx.x % a.splits, r0 = (int)(blockIdx.x / a.splits) * F::kRows;
+  const int kvh = blockIdx.y, b = blockIdx.z;
+  const int warp = warp_index(), lane = threadIdx.x & 31;
+  pdl_wait();
+  pdl_launch_dependents();
+  int len, count;
+  if (!seq_sizes(a, b, &len, &count)) return;
+  const int rows = count * a.group;
+  if (r0 >= rows) return;
+  if (a.k_new && !build_ancestors(a, b, count, anc, par)) return;
+  const int t_last = (min(r0 + F::kRows, rows) - 1) / a.group;
+  const int kmax = visible_limit(a, len, count, t_last), lim_min = visible_limit(a, len, count, r0 / a.group);
+  const int gp = (kmax + kGk - 1) / kGk, groups = gp + (a.k_new ? (count + kGk - 1) / kGk : 0);
+  const int g_begin = (int)((int64_t)groups * split / a.splits), g_end = (int)((int64_t)groups * (split + 1) / a.splits);
+
+  uint8_t* ring = smem + warp * F::kWarpRing;
+  const uint32_t ring_u = smem_u32(ring);
+  auto load = [&](int g, int slot) {
+    if (g < g_end) {
+      const bool nw = g >= gp;
+      const int j0 = (nw ? g - gp : g) * kGk, have = (nw ? count : len) - j0;
+      const int64_t stride = nw ? a.new_stride : a.kv_stride;
+      const int64_t at = (nw ? (int64_t)b * a.tokens * a.new_stride : (int64_t)b * a.seq_stride) + j0 * stride + kvh * D;
+      const T* kb = static_cast<const T*>(nw ? a.k_new : a.k) + at;
+      const T* vb = static_cast<const T*>(nw ? a.v_new : a.v) + at;
+      const uint32_t dst = ring_u + (uint32_t)slot * 2 * F::kGroup;
+      constexpr int C = D / 8;
+#pragma unroll
+      for (int i = 0; i < kGk * C / 32; ++i) {
+        const int r = (lane + 32 * i) / C, c = (lane + 32 * i) % C;
+        const bool ok = r < have;
+        const int64_t off = ok ? r * stride + c * 8 : 0;
+        cp_async_16(dst + swz<D>(r, c), kb + off, ok);
+        cp_async_16(dst + F::kGroup + swz<D>(r, c), vb + off, ok);
+      }
+    }
+    cp_async_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < kFwStages - 1; ++i) load(g_begin + warp + i * kFwWarps, i);
+
+  load_queries<T, D>(a, b, kvh, r0, rows, F::kRows, smem + F::kOffQ, nullptr);
+  __syncthreads();
+  const uint32_t q_u = smem_u32(smem + F::kOffQ);
+  auto query_frag = [&](int mt, int ks, uint32_t(&f)[4]) {
+    ldmatrix_x4(q_u + swz<D>(mt * 16 + (lane & 15), 2 * ks + (lane >> 4)), f);
+  };
+  uint32_t qf[MT == 1 ? D / 16 : 1][4];
+  if (MT == 1) {
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) query_frag(0, ks, qf[MT == 1 ? ks : 0]);
+  }
+  int lim[MT][2], node[MT][2];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = r0 + mt * 16 + 8 * h + (lane >> 2);
+      node[mt][h] = r < rows ? r / a.group : -1;
+      lim[mt][h] = r < rows ? visible_limit(a, len, count, r / a.group) : 0;
+    }
+  float m[MT][2], l[MT][2], o[MT][D / 8][4];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) m[mt][h] = -INFINITY, l[mt][h] = 0.f;
+#pragma unroll
+    for (int n = 0; n < D / 8; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[mt][n][e] = 0.f;
+  }
+  int slot = 0;
+  for (int g = g_begin + warp; g < g_end; g += kFwWarps) {
+    int ahead = slot + kFwStages - 1;
+    if (ahead >= kFwStages) ahead -= kFwStages;
+    load(g + (kFwStages - 1) * kFwWarps, ahead);
+    cp_async_wait<kFwStages - 1>();
+    __syncwarp();
+    const uint32_t ks_u = ring_u + (uint32_t)slot * 2 * F::kGroup, vs_u = ks_u + F::kGroup;
+    const bool nw = g >= gp;
+    const int j0 = (nw ? g - gp : g) * kGk;
+    float s[MT][2][4];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[mt][n][e] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+      uint32_t kf[4];
+      ldmatrix_x4(ks_u + swz<D>((lane & 7) + ((lane >> 4) << 3), 2 * ks + ((lane >> 3) & 1)), kf);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        uint32_t f[4];
+        if (MT == 1) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) f[i] = qf[MT == 1 ? ks : 0][i];
+        } else {
+          query_frag(mt, ks, f);
+        }
+        mma_16816<T>(s[mt][0], f, kf[0], kf[1]);
+        mma_16816<T>(s[mt][1], f, kf[2], kf[3]);
+      }
+    }
+    const bool masked = nw || j0 + kGk > lim_min;  // some of these keys are hidden from some rows
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s[mt][n][e] *= a.scale_log2;
+          if (masked) {
+            const int h = e >> 1, j = j0 + n * 8 + (lane & 3) * 2 + (e & 1);
+            const bool sees = nw ? node[mt][h] >= 0 && (anc[node[mt][h]][j >> 5] >> (j & 31) & 1u) : j < lim[mt][h];
+            if (!sees) s[mt][n][e] = -INFINITY;
+          }
+        }
+    if (SPILL) {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int r = r0 + mt * 16 + 8 * h + (lane >> 2);
+          if (r < rows) {
+            float* to = a.scores + (((int64_t)b * a.kv_heads + kvh) * a.tokens * a.group + r) * a.score_ld + j0 + (lane & 3) * 2;
+#pragma unroll
+            for (int n = 0; n < 2; ++n) *reinterpret_cast<float2*>(to + n * 8) = make_float2(s[mt][n][2 * h], s[mt][n][2 * h + 1]);
+          }
+        }
+    }
+    uint32_t ph[MT][4], pl[MT][4];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      float al[2], base[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float mx = fmaxf(fmaxf(s[mt][0][2 * h], s[mt][0][2 * h + 1]), fmaxf(s[mt][1][2 * h], s[mt][1][2 * h + 1]));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+        const float mn = fmaxf(m[mt][h], mx);
+        base[h] = mn == -INFINITY ? 0.f : mn;  // (nothing seen yet)
+        al[h] = exp2f(m[mt][h] - base[h]);
+        m[mt][h] = mn;
+      }
+      float sum[2] = {0.f, 0.f};
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float p0 = exp2f(s[mt][n][2 * h] - base[h]), p1 = exp2f(s[mt][n][2 * h + 1] - base[h]);
+          sum[h] += p0 + p1;
+          s[mt][n][2 * h] = p0;
+          s[mt][n][2 * h + 1] = p1;
+          const uint32_t hi = pack_pair<T>(p0, p1);
+          const float2 back = unpack_pair<T>(hi);
+          ph[mt][2 * n + h] = hi;
+          pl[mt][2 * n + h] = pack_pair<T>(p0 - back.x, p1 - back.y);
+        }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) l[mt][h] = l[mt][h] * al[h] + sum[h];
+      if (__any_sync(0xffffffffu, al[0] != 1.f || al[1] != 1.f)) {
+#pragma unroll
+        for (int n = 0; n < D / 8; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[mt][n][e] *= al[e >> 1];
+      }
+    }
+    if (masked) {
+      // A hidden value row that is infinite or not a number must not reach
+      // the rows that do not see it (0 x inf): such rows are added by hand,
+      // where they are seen, and zeroed for the product.
+      uint8_t* vs = ring + slot * 2 * F::kGroup + F::kGroup;
+      uint32_t odd = 0;  // bit per value row
+#pragma unroll
+      for (int i = 0; i < kGk * (D / 8) / 32; ++i) {
+        const int r = (lane + 32 * i) / (D / 8), c = (lane + 32 * i) % (D / 8);
+        const uint4 v = *reinterpret_cast<const uint4*>(vs + swz<D>(r, c));
+        if (odd_pair<T>(v.x) || odd_pair<T>(v.y) || odd_pair<T>(v.z) || odd_pair<T>(v.w)) odd |= 1u << r;
+      }
+      odd = __reduce_or_sync(0xffffffffu, odd);
+      if (odd) {
+        float* pb = reinterpret_cast<float*>(smem + F::kOffP) + warp * F::kRows * kGk;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              pb[(mt * 16 + 8 * (e >> 1) + (lane >> 2)) * kGk + n * 8 + (lane & 3) * 2 + (e & 1)] = s[mt][n][e];
+        __syncwarp();
+        while (odd) {
+          const int j = __ffs(odd) - 1;
+          odd &= odd - 1;
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int n = 0; n < D / 8; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float p = pb[(mt * 16 + 8 * (e >> 1) + (lane >> 2)) * kGk + j];
+                const T v = *reinterpret_cast<const T*>(vs + swz<D>(j, n) + ((lane & 3) * 2 + (e & 1)) * 2);
+                if (p != 0.f) o[mt][n][e] = fmaf(p, to_f<T>(v), o[mt][n][e]);
+              }
+          __syncwarp();
+          if (lane < D / 8) *reinterpret_cast<uint4*>(vs + swz<D>(j, lane)) = make_uint4(0u, 0u, 0u, 0u);
+          __syncwarp();
+        }
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < D / 16; ++n) {
+      uint32_t vf[4];
+      ldmatrix_x4_trans(vs_u + swz<D>(lane & 15, 2 * n + (lane >> 4)), vf);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        mma_16816<T>(o[mt][2 * n], ph[mt], vf[0], vf[1]);
+        mma_16816<T>(o[mt][2 * n + 1], ph[mt], vf[2], vf[3]);
+        mma_16816<T>(o[mt][2 * n], pl[mt], vf[0], vf[1]);
+        mma_16816<T>(o[mt][2 * n + 1], pl[mt], vf[2], vf[3]);
+      }
+    }
+    __syncwarp();  // the group has been read before its slot is filled again
+    if (++slot == kFwStages) slot = 0;
+  }
+  // the warps' results meet in shared memory, in warp order
+  cp_async_wait<0>();
+  __syncthreads();
+  float* ow = reinterpret_cast<float*>(smem) + warp * F::kRows * D;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float x = l[mt][h];
+      x += __shfl_xor_sync(0xffffffffu, x, 1);
+      x += __shfl_xor_sync(0xffffffffu, x, 2);
+      const int rl = mt * 16 + 8 * h + (lane >> 2);
+      if ((lane & 3) == 0) mls[warp * F::kRows + rl] = make_float2(m[mt][h], x);
+#pragma unroll
+      for (int n = 0; n < D / 8; ++n)
+        *reinterpret_cast<float2*>(ow + rl * D + n * 8 + (lane & 3) * 2) = make_float2(o[mt][n][2 * h], o[mt][n][2 * h + 1]);
+    }
+  __syncthreads();
+  constexpr int V = D / 4;  // float4 per row
+  for (int i = threadIdx.x; i < F::kRows * V; i += kFwThreads) {
+    const int rl = i / V, c = i % V, r = r0 + rl;
+    if (r >= rows) break;
+    float M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < kFwWarps; ++w) M = fmaxf(M, mls[w * F::kRows + rl].x);
+    const float base = M == -INFINITY ? 0.f : M;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < kFwWarps; ++w) {
+      const float2 ml = mls[w * F::kRows + rl];
+      const float f = exp2f(ml.x - base);
+      const float4 y = reinterpret_cast<const float4*>(smem)[(w * F::kRows + rl) * V + c];
+      L = fmaf(ml.y, f, L);
+      if (f != 0.f) {
+        x.x = fmaf(y.x, f, x.x);
+        x.y = fmaf(y.y, f, x.y);
+        x.z = fmaf(y.z, f, x.z);
+        x.w = fmaf(y.w, f, x.w);
+      }
+    }
+    const int64_t slot_r = (((int64_t)b * a.kv_heads + kvh) * a.splits + split) * a.tokens * a.group + r;
+    if (c == 0 && (a.splits > 1 || SPILL)) reinterpret_cast<float2*>(a.ml)[slot_r] = make_float2(M, L);
+    if (a.splits > 1) {
+      if (M != -INFINITY) reinterpret_cast<float4*>(a.part)[slot_r * V + c] = x;
+      continue;
+    }
+    const int t = r / a.group, hd = kvh * a.group + r % a.group;
+    const float inv = L > 0.f ? 1.0f / L : (L == 0.f ? 0.f : L);  // (a NaN stays one)
+    T* to = static_cast<T*>(a.out) + ((int64_t)b * a.tokens + t) * a.out_stride + (int64_t)hd * D + c * 4;
+    *reinterpret_cast<uint2*>(to) = make_uint2(pack_pair<T>(x.x * inv, x.y * inv), pack_pair<T>(x.z * inv, x.w * inv));
+    if (c == 0 && a.lse) a.lse[((int64_t)b * a.heads + hd) * a.tokens + t] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+  }
+}
+
+// ----------------------------------------------------------------- the join
+// Blocks [0, join_blocks): a warp per row, the splits in order:
+//   M = max m_s, L = sum l_s 2^(m_s - M), out = sum O_s 2^(m_s - M) / L.
+// The blocks behind them: weights_j = weights_in_j + sum over the rows that
+// see row j of 2^(score - log2 L - M), from the stored scores.
+constexpr int kJoinThreads = 256, kJoinKeys = 4 * kJoinThreads;
+
+// log2 of a row's softmax sum, over its splits.
+__device__ __forceinline__ float2 join_stats(const CachedArgs& a, int64_t first, int64_t step) {
+  float M = -INFINITY, L = 0.f;
+  for (int s = 0; s < a.splits; ++s) M = fmaxf(M, reinterpret_cast<const float2*>(a.ml)[first + s * step].x);
+  const float base = M == -INFINITY ? 0.f : M;
+  for (int s = 0; s < a.splits; ++s) {
+    const float2 ml = reinterpret_cast<const float2*>(a.ml)[first + s * step];
+    L = fmaf(ml.y, exp2f(ml.x - base), L);
+  }
+  return make_float2(M, L);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __grid_constant__ CachedArgs a, int join_blocks) {
+  extern __shared__ float lse2[];  // the scores' rows
+  pdl_wait();
+  const int kvh = blockIdx.y, b = blockIdx.z;
+  int len, count;
+  if (!seq_sizes(a, b, &len, &count)) return;
+  const int rows = count * a.group;
+  const int64_t step = (int64_t)a.tokens * a.group;
+  const int64_t first = ((int64_t)b * a.kv_heads + kvh) * a.splits * step;
+  if ((int)blockIdx.x < join_blocks) {
+    if (a.k_new && a.parents) {  // the splits of such a sequence were not computed
+      bool bad = false;
+      for (int t = threadIdx.x; t < count; t += blockDim.x) {
+        const int p = a.parents[(int64_t)b * a.tokens + t];
+        bad = bad || p < -1 || p >= t;
+      }
+      if (__syncthreads_or(bad)) return;
+    }
+    const int r = (int)blockIdx.x * (kJoinThreads / 32) + warp_index(), lane = threadIdx.x & 31;
+    if (r >= rows) return;
+    const float2 st = join_stats(a, first + r, step);
+    const float base = st.x == -INFINITY ? 0.f : st.x;
+    const int t = r / a.group, hd = kvh * a.group + r % a.group;
+    const float inv = st.y > 0.f ? 1.0f / st.y : (st.y == 0.f ? 0.f : st.y);
+    const int V = a.dim / 4;
+    if (lane < V) {
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int s = 0; s < a.splits; ++s) {
+        const float ms = reinterpret_cast<const float2*>(a.ml)[first + s * step + r].x;
+        if (ms == -INFINITY) continue;
+        const float f = exp2f(ms - base);
+        const float4 y = reinterpret_cast<const float4*>(a.part)[(first + s * step + r) * V + lane];
+        x.x = fmaf(y.x, f, x.x);
+        x.y = fmaf(y.y, f, x.y);
+        x.z = fmaf(y.z, f, x.z);
+        x.w = fmaf(y.w, f, x.w);
+      }
+      T* to = static_cast<T*>(a.out) + ((int64_t)b * a.tokens + t) * a.out_stride + (int64_t)hd * a.dim + lane * 4;
+      *reinterpret_cast<uint2*>(to) = make_uint2(pack_pair<T>(x.x * inv, x.y * inv), pack_pair<T>(x.z * inv, x.w * inv));
+    }
+    if (lane == 0 && a.lse)
+      a.lse[((int64_t)b * a.heads + hd) * a.tokens + t] = st.y == 0.f ? -INFINITY : (st.x + log2f(st.y)) * 0.6931471805599453f;
+    return;
+  }
+  const int j0 = ((int)blockIdx.x - join_blocks) * kJoinKeys;
+  if (j0 >= len) return;
+  for (int r = threadIdx.x; r < rows; r += kJoinThreads) {
+    const float2 st = join_stats(a, first + r, step);
+    lse2[r] = st.x + log2f(st.y);
+  }
+  __syncthreads();
+  const int64_t at = ((int64_t)b * a.kv_heads + kvh) * a.max_seq;
+  const float* sc = a.scores + ((int64_t)b * a.kv_heads + kvh) * step * a.score_ld;
+#pragma unroll
+  for (int i = 0; i < kJoinKeys / kJoinThreads; ++i) {
+    const int j = j0 + i * kJoinThreads + threadIdx.x;
+    if (j >= len) break;
+    float w = 0.f;
+    for (int r = 0; r < rows; ++r)
+      if (j < visible_limit(a, len, count, r / a.group)) w += exp2f(sc[(int64_t)r * a.score_ld + j] - lse2[r]);
+    a.weights[at + j] = (a.weights_in ? a.weights_in[at + j] : 0.f) + w;
+  }
+}
+
+// --------------------------------------------------------- few-row weights
+// weights_j = weights_in_j + sum over rows and heads of e^(s_rj - lse_r): one
+// warp per group of 16 keys, S = Q K^T as above, 2^(S - lse) summed over the
+// rows in registers and then over the eight lanes that share a key.  Rows in
+// blocks of 128; a second block reads the keys again and adds to its own sums.
+constexpr int kWfRows = 128, kWfStages = 4;
+template <int D> struct WfCfg {
+  static constexpr int kGroup = kGk * D * 2;
+  static constexpr int kRing = kFwWarps * kWfStages * kGroup;
+  static constexpr int kOffQ = kRing;
+  static constexpr int kOffLse = kOffQ + kWfRows * D * 2;
+  static constexpr int kOffLim = kOffLse + kWfRows * 4;
+  static constexpr int kOffRow = kOffLim + kWfRows * 4;
+  static constexpr int kSmem = kOffRow + kWfRows * 4;
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kFwThreads) weights_few_kernel(const __grid_constant__ CachedArgs a) {
+  using F = WfCfg<D>;
+  extern __shared__ __align__(128) uint8_t smem[];
+  float* lse2 = reinterpret_cast<float*>(smem + F::kOffLse);
+  int* lim = reinterpret_cast<int*>(smem + F::kOffLim);
+  int* row_of = reinterpret_cast<int*>(smem + F::kOffRow);
+  const int split = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z;
+  const int warp = warp_index(), lane = threadIdx.x & 31;
+  pdl_wait();
+  pdl_launch_dependents();
+  int len, count;
+  if (!seq_sizes(a, b, &len, &count)) return;
+  const int rows = count * a.group;
+  const int groups = (len + kGk - 1) / kGk;
+  const int g_begin = (int)((int64_t)groups * split / a.splits), g_end = (int)((int64_t)groups * (split + 1) / a.splits);
+  if (g_begin >= g_end) return;
+  const uint32_t ring_u = smem_u32(smem + warp * kWfStages * F::kGroup), q_u = smem_u32(smem + F::kOffQ);
+  const T* kb = static_cast<const T*>(a.k) + (int64_t)b * a.seq_stride + kvh * D;
+  auto load = [&](int g, int slot) {
+    if (g < g_end) {
+      constexpr int C = D / 8;
+#pragma unroll
+      for (int i = 0; i < kGk * C / 32; ++i) {
+        const int r = (lane + 32 * i) / C, c = (lane + 32 * i) % C, j = g * kGk + r;
+        cp_async_16(ring_u + (uint32_t)slot * F::kGroup + swz<D>(r, c), kb + (j < len ? j * a.kv_stride + c * 8 : 0), j < len);
+      }
+    }
+    cp_async_commit();
+  };
+  const int64_t at = ((int64_t)b * a.kv_heads + kvh) * a.max_seq;
+  const float* from = a.weights_in;
+  for (int r0 = 0; r0 < rows || r0 == 0; r0 += kWfRows) {
+#pragma unroll
+    for (int i = 0; i < kWfStages - 1; ++i) load(g_begin + warp + i * kFwWarps, i);
+    const int here = min(kWfRows, rows - r0), tiles = (here + 15) / 16;
+    for (int i = threadIdx.x; i < kWfRows; i += kFwThreads) {
+      const int r = r0 + i, t = r / a.group;
+      int q = t;
+      if (i < here && a.rows) {
+        q = a.rows[(int64_t)b * a.tokens + t];
+        if (q < 0 || q >= a.tokens) {
+          atomicExch(a.err, kDevErrBounds);
+          q = -1;
+        }
+      }
+      const bool ok = i < here && q >= 0;
+      row_of[i] = ok ? q : -1;
+      lim[i] = ok ? visible_limit(a, len, count, t) : 0;
+      lse2[i] = ok ? a.lse[((int64_t)b * a.heads + kvh * a.group + r % a.group) * a.tokens + q] * 1.4426950408889634f : INFINITY;
+    }
+    __syncthreads();
+    load_queries<T, D>(a, b, kvh, r0, rows, tiles * 16, smem + F::kOffQ, row_of);
+    __syncthreads();
+    const int lim_min = rows ? visible_limit(a, len, count, r0 / a.group) : 0;
+    int slot = 0;
+    for (int g = g_begin + warp; g < g_end; g += kFwWarps) {
+      load(g + (kWfStages - 1) * kFwWarps, (slot + kWfStages - 1) % kWfStages);
+      cp_async_wait<kWfStages - 1>();
+      __syncwarp();
+      const uint32_t ks_u = ring_u + (uint32_t)slot * F::kGroup;
+      const int j0 = g * kGk;
+      uint32_t kf[D / 16][4];
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks)
+        ldmatrix_x4(ks_u + swz<D>((lane & 7) + ((lane >> 4) << 3), 2 * ks + ((lane >> 3) & 1)), kf[ks]);
+      const bool masked = j0 + kGk > lim_min;
+      float w[4] = {0.f, 0.f, 0.f, 0.f};  // this lane's keys: j0 + 8 n + 2 (lane & 3) + u at 2 n + u
+      for (int mt = 0; mt < tiles; ++mt) {
+        float s[2][4];
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+          uint32_t f[4];
+          ldmatrix_x4(q_u + swz<D>(mt * 16 + (lane & 15), 2 * ks + (lane >> 4)), f);
+          mma_16816<T>(s[0], f, kf[ks][0], kf[ks][1]);
+          mma_16816<T>(s[1], f, kf[ks][2], kf[ks][3]);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int rl = mt * 16 + 8 * h + (lane >> 2);
+          const float e2 = lse2[rl];
+          const int lm = lim[rl];
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const float p = exp2f(fmaf(s[n][2 * h + u], a.scale_log2, -e2));
+              if (!masked || j0 + n * 8 + (lane & 3) * 2 + u < lm) w[2 * n + u] += p;
+            }
+        }
+      }
+#pragma unroll
+      for (int off = 4; off < 32; off <<= 1)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] += __shfl_xor_sync(0xffffffffu, w[i], off);
+      if (lane < 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int j = j0 + (i >> 1) * 8 + lane * 2 + (i & 1);
+          if (j < len) a.weights[at + j] = (from ? from[at + j] : 0.f) + w[i];
+        }
+      }
+      __syncwarp();
+      slot = (slot + 1) % kWfStages;
+    }
+    cp_async_wait<0>();
+    __syncthreads();
+    from = a.weights;  // (a key's sums stay with one thread)
+  }
+}
+
+int done(cudaError_t e, const char* what) {
+  if (e == cudaSuccess) e = cudaGetLastError();
+  if (e != cudaSuccess) SN_FAIL(SWAPNET_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
+  return SWAPNET_OK;
+}
+
+template <typename... KArgs, typename... Args>
+cudaError_t launch(void (*kern)(KArgs...), dim3 grid, int threads, size_t smem, bool early, cudaStream_t s, Args... args) {
+  cudaLaunchConfig_t cfg;
+  std::memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = early ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
+}
+
+// Shared memory above 48 KB is allowed per function and device, once.
+template <typename K> int allow_smem(K kern, int bytes, std::atomic<uint64_t>& known) {
+  if (!attr_needed(known)) return SWAPNET_OK;
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e != cudaSuccess) return done(e, "cached attention: shared memory");
+  attr_set(known);
+  return SWAPNET_OK;
+}
+
+template <typename T, int D, int MT, bool SPILL> int few_t(const CachedArgs& a, bool early, cudaStream_t s) {
+  static std::atomic<uint64_t> known{0};
+  using F = FewCfg<D, MT>;
+  if (int rc = allow_smem(attention_few_kernel<T, D, MT, SPILL>, F::kSmem, known)) return rc;
+  const int chunks = (a.tokens * a.group + F::kRows - 1) / F::kRows;
+  return done(launch(attention_few_kernel<T, D, MT, SPILL>, dim3(chunks * a.splits, a.kv_heads, a.n_seq), kFwThreads, F::kSmem,
+                     early, s, a),
+              "cached attention launch");
+}
+template <typename T, int D> int few_d(const CachedArgs& a, bool early, cudaStream_t s) {
+  const bool one = a.tokens * a.group <= 16;
+  if (a.scores) return one ? few_t<T, D, 1, true>(a, early, s) : few_t<T, D, 2, true>(a, early, s);
+  return one ? few_t<T, D, 1, false>(a, early, s) : few_t<T, D, 2, false>(a, early, s);
+}
+template <typename T, int D> int weights_t(const CachedArgs& a, bool early, cudaStream_t s) {
+  static std::atomic<uint64_t> known{0};
+  if (int rc = allow_smem(weights_few_kernel<T, D>, WfCfg<D>::kSmem, known)) return rc;
+  CachedArgs x = a;
+  // about eight CTAs per SM in all, 64 keys a warp at least
+  const int64_t pairs = (int64_t)a.n_seq * a.kv_heads;
+  x.splits = (int)std::max<int64_t>(1, std::min<int64_t>((8 * 152 + pairs - 1) / pairs, (a.max_seq + 255) / 256));
+  return done(launch(weights_few_kernel<T, D>, dim3(x.splits, a.kv_heads, a.n_seq), kFwThreads, WfCfg<D>::kSmem, early, s, x),
+              "cache weights launch");
+}
+
+}  // namespace
+
+#define SN_CACHED_DISPATCH(F, ...)                                                                     \
+  (a.dtype == SWAPNET_BF16 ? (a.dim == 128 ? F<__nv_bfloat16, 128>(__VA_ARGS__) : F<__nv_bfloat16, 64>(__VA_ARGS__)) \
+                           : (a.dim == 128 ? F<__half, 128>(__VA_ARGS__) : F<__half, 64>(__VA_ARGS__)))
+
+int launch_attention_few(const CachedArgs& a, bool early, cudaStream_t s) { return SN_CACHED_DISPATCH(few_d, a, early, s); }
+int launch_weights_few(const CachedArgs& a, bool early, cudaStream_t s) { return SN_CACHED_DISPATCH(weights_t, a, early, s); }
+
+int launch_attention_join(const CachedArgs& a, cudaStream_t s) {
+  const int rows = a.tokens * a.group;
+  const int jb = a.splits > 1 ? (rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32) : 0;
+  const int wb = a.scores ? (a.max_seq + kJoinKeys - 1) / kJoinKeys : 0;
+  if (jb + wb == 0) return SWAPNET_OK;
+  const dim3 grid(jb + wb, a.kv_heads, a.n_seq);
+  const size_t smem = a.scores ? rows * sizeof(float) : 0;
+  return done(a.dtype == SWAPNET_BF16
+                  ? launch(attention_join_kernel<__nv_bfloat16>, grid, kJoinThreads, smem, true, s, a, jb)
+                  : launch(attention_join_kernel<__half>, grid, kJoinThreads, smem, true, s, a, jb),
+              "cached attention join launch");
+}
+
+}  // namespace swapnet

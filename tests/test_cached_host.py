@@ -1,0 +1,116 @@
+"""Refusals and workspace sizes of the cached-attention calls: decided on the
+host, before anything is launched, so they need no GPU."""
+import numpy as np
+import pytest
+
+from paper_2401_16757_gb300 import capi
+
+A = 1 << 20  # an aligned address; nothing is read from it
+
+
+def _attn(**kw):
+    base = dict(dtype="bf16", n_seq=2, tokens=4, heads=8, kv_heads=2, head_dim=128, max_seq=100, q=A, k=A, v=A, lens=A,
+                out=A, lse=A)
+    base.update(kw)
+    return capi.cached_attention(base.pop("dtype"), *[base.pop(x) for x in ("n_seq", "tokens", "heads", "kv_heads", "head_dim",
+                                                                            "max_seq")], **base)
+
+
+def _code(call, *a, **kw):
+    with pytest.raises(capi.SwapnetError) as e:
+        call(*a, **kw)
+    assert str(e.value)
+    return e.value.code
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(dtype="f32"), capi.ERR_UNSUPPORTED), (dict(dtype=9), capi.ERR_UNSUPPORTED),
+    (dict(n_seq=0), capi.ERR_INVALID_ARG), (dict(tokens=0), capi.ERR_INVALID_ARG), (dict(max_seq=0), capi.ERR_INVALID_ARG),
+    (dict(heads=7), capi.ERR_INVALID_ARG), (dict(head_dim=96), capi.ERR_UNSUPPORTED),
+    (dict(n_seq=70000), capi.ERR_UNSUPPORTED), (dict(heads=258, kv_heads=2), capi.ERR_UNSUPPORTED),
+    (dict(q=0), capi.ERR_INVALID_ARG), (dict(k=0), capi.ERR_INVALID_ARG), (dict(v=0), capi.ERR_INVALID_ARG),
+    (dict(lens=0), capi.ERR_INVALID_ARG), (dict(out=0), capi.ERR_INVALID_ARG),
+    (dict(q=A + 8), capi.ERR_MISALIGNED), (dict(k=A + 2), capi.ERR_MISALIGNED), (dict(out=A + 4), capi.ERR_MISALIGNED),
+    (dict(q_stride=1023), capi.ERR_INVALID_ARG), (dict(q_stride=1028), capi.ERR_MISALIGNED),
+    (dict(kv_stride=128), capi.ERR_INVALID_ARG), (dict(out_stride=-8), capi.ERR_INVALID_ARG),
+    (dict(seq_stride=-8), capi.ERR_INVALID_ARG), (dict(seq_stride=12), capi.ERR_MISALIGNED),
+    (dict(scale=-1.0), capi.ERR_INVALID_ARG), (dict(scale=float("nan")), capi.ERR_INVALID_ARG),
+    (dict(scale=float("inf")), capi.ERR_INVALID_ARG),
+    (dict(rows=A), capi.ERR_INVALID_ARG), (dict(k_new=A), capi.ERR_INVALID_ARG), (dict(parents=A), capi.ERR_INVALID_ARG),
+    (dict(k_new=A, v_new=A, tokens=129), capi.ERR_UNSUPPORTED), (dict(k_new=A, v_new=A, weights=A), capi.ERR_INVALID_ARG),
+    (dict(weights_in=A), capi.ERR_INVALID_ARG), (dict(weights=A, lse=0, tokens=9), capi.ERR_INVALID_ARG),
+])
+def test_attention_refuses(change, code):
+    a = _attn(**change)
+    assert _code(capi.attention_tree_workspace, a) == code
+    assert _code(capi.attention_tree, a, A, 1 << 40) == code
+
+
+def test_attention_workspace():
+    """A function of the sizes: nothing for one split, more with splits and stored scores; too little of it is refused."""
+    assert capi.attention_tree_workspace(_attn(max_seq=200)) == 0
+    long = _attn(max_seq=8192)
+    need = capi.attention_tree_workspace(long)
+    assert need > 0 and need == capi.attention_tree_workspace(_attn(max_seq=8192, q=2 * A))
+    assert capi.attention_tree_workspace(_attn(max_seq=8192, tokens=1, weights=A)) > \
+        capi.attention_tree_workspace(_attn(max_seq=8192, tokens=1))
+    assert _code(capi.attention_tree, long, A, need - 1) == capi.ERR_INVALID_ARG
+    assert _code(capi.attention_tree, long, 0, need) == capi.ERR_INVALID_ARG
+    assert _code(capi.attention_tree, long, A + 16, need) == capi.ERR_MISALIGNED
+    assert capi.lib().swapnet_attention_tree_workspace(None, None) == capi.ERR_INVALID_ARG
+    assert capi.lib().swapnet_attention_tree(None, None, 0, None) == capi.ERR_INVALID_ARG
+    assert capi.lib().swapnet_attention_weights(None, None) == capi.ERR_INVALID_ARG
+    assert capi.lib().swapnet_cache_evict(None, None) == capi.ERR_INVALID_ARG
+    assert capi.lib().swapnet_tree_accept(None, None) == capi.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(lse=0), capi.ERR_INVALID_ARG), (dict(weights=0), capi.ERR_INVALID_ARG), (dict(k_new=A, v_new=A), capi.ERR_INVALID_ARG),
+    (dict(parents=A), capi.ERR_INVALID_ARG), (dict(dtype="f32"), capi.ERR_UNSUPPORTED), (dict(q=A + 8), capi.ERR_MISALIGNED),
+])
+def test_weights_refuse(change, code):
+    assert _code(capi.attention_weights, _attn(**{"weights": A, **change})) == code
+
+
+def _evict(**kw):
+    base = dict(dtype="f16", n_seq=2, kv_heads=2, head_dim=64, max_seq=100, keep=50, recent=10, sink=4, k=A, v=2 * A,
+                weights=3 * A, lens=4 * A, k_out=5 * A, v_out=6 * A, weights_out=7 * A, kept=8 * A, lens_out=9 * A)
+    base.update(kw)
+    return capi.cache_evict(**base)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(dtype="f32"), capi.ERR_UNSUPPORTED), (dict(keep=0), capi.ERR_INVALID_ARG), (dict(head_dim=60), capi.ERR_UNSUPPORTED),
+    (dict(recent=47), capi.ERR_INVALID_ARG), (dict(recent=-1), capi.ERR_INVALID_ARG), (dict(sink=-1), capi.ERR_INVALID_ARG),
+    (dict(kept=0), capi.ERR_INVALID_ARG), (dict(weights=0), capi.ERR_INVALID_ARG), (dict(lens_out=4 * A), capi.ERR_INVALID_ARG),
+    (dict(out_capacity=49), capi.ERR_INVALID_ARG), (dict(k_out=A), capi.ERR_INVALID_ARG),
+    (dict(k_out=A, v_out=2 * A, weights_out=3 * A, out_capacity=50), capi.ERR_INVALID_ARG),
+    (dict(v_out=5 * A), capi.ERR_INVALID_ARG), (dict(k=A + 8), capi.ERR_MISALIGNED), (dict(kv_stride=132), capi.ERR_MISALIGNED),
+    (dict(kv_stride=120), capi.ERR_INVALID_ARG), (dict(out_seq_stride=-8), capi.ERR_INVALID_ARG),
+])
+def test_eviction_refuses(change, code):
+    assert _code(_evict, **change) == code
+
+
+def _accept(**kw):
+    base = dict(dtype="f16", n_seq=2, tokens=8, width=64, max_seq=100, ids=A, targets=A, lens=A, caches=np.array([A]),
+                drafts=np.array([A]), path=A, accepted=A, next=A, lens_out=2 * A)
+    base.update(kw)
+    return capi.tree_accept(**base)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(dtype="f32"), capi.ERR_UNSUPPORTED), (dict(tokens=0), capi.ERR_INVALID_ARG), (dict(tokens=129), capi.ERR_UNSUPPORTED),
+    (dict(width=60), capi.ERR_UNSUPPORTED), (dict(ids=0), capi.ERR_INVALID_ARG), (dict(next=0), capi.ERR_INVALID_ARG),
+    (dict(lens_out=A), capi.ERR_INVALID_ARG), (dict(caches=np.array([0])), capi.ERR_INVALID_ARG),
+    (dict(caches=np.array([A + 8])), capi.ERR_MISALIGNED), (dict(cache_stride=32), capi.ERR_INVALID_ARG),
+    (dict(new_stride=68), capi.ERR_MISALIGNED),
+    (dict(caches=np.full(257, A), drafts=np.full(257, A)), capi.ERR_UNSUPPORTED),
+])
+def test_acceptance_refuses(change, code):
+    assert _code(_accept, **change) == code
+
+
+def test_acceptance_needs_a_draft_per_cache():
+    with pytest.raises(ValueError):
+        _accept(caches=np.array([A, A]))
