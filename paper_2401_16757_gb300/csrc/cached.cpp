@@ -12,14 +12,37 @@
 
 namespace swapnet {
 
-// Splits of a (sequence, key head)'s keys: enough CTAs for every SM to hold
-// two of them, twice over where the cache is long enough for 256 keys each.
+// How many CTAs share the keys of a (sequence, key head, row tile): the count
+// whose waves over the SMs take the least time, for the whole cache (how much
+// of it is filled only the device knows).  step / fixed: microseconds of a
+// CTA's tile of keys and of its start and end; more than one also pays the
+// join.
+static int choose_splits(int64_t ctas, int tiles, int per_sm, double step, double fixed) {
+  const int64_t room = 152 * per_sm;
+  int best = 1;
+  double least = 1e30;
+  for (int s = 1; s <= tiles && s <= 128; ++s) {
+    const double waves = std::max(1.0, (double)(ctas * s) / room);  // (many waves even out)
+    const double t = (waves < 4.0 ? std::ceil(waves) : waves) * ((tiles + s - 1) / s * step + fixed) + (s > 1 ? 2.0 + 0.02 * s : 0.0);
+    if (t < least * 0.99) {
+      least = t;
+      best = s;
+    }
+  }
+  return best;
+}
+
 CachedPlan cached_plan(const CachedArgs& a) {
   CachedPlan p;
   std::memset(&p, 0, sizeof(p));
-  const int64_t rows = (int64_t)a.tokens * a.group;
-  const int64_t pairs = (int64_t)a.n_seq * a.kv_heads * ((rows + 31) / 32);
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((4 * 152 + pairs - 1) / pairs, (a.max_seq + 255) / 256));
+  const int64_t rows = (int64_t)a.tokens * a.group, pairs = (int64_t)a.n_seq * a.kv_heads;
+  p.tc = rows > 32;
+  if (p.tc) {
+    const int queries = (rows <= 64 ? 64 : 128) / a.group;
+    p.splits = choose_splits(pairs * ((a.tokens + queries - 1) / queries), (a.max_seq + 127) / 128 + (a.k_new ? 1 : 0), 1, 0.9, 3.0);
+  } else {
+    p.splits = choose_splits(pairs, (a.max_seq + 63) / 64, 2, 0.5, 2.0);
+  }
   p.spill = a.weights && rows <= 32;
   p.score_ld = (a.max_seq + 15) / 16 * 16;
   const uint64_t all = (uint64_t)a.n_seq * a.kv_heads * rows;
@@ -150,7 +173,7 @@ int swapnet_attention_tree(const swapnet_cached_attention* c, void* workspace, u
     a.scores = p.spill ? reinterpret_cast<float*>(w + p.part_bytes + p.ml_bytes) : nullptr;
     a.score_ld = p.score_ld;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    if (int rc = launch_attention_few(a, false, s)) return rc;
+    if (int rc = p.tc ? launch_attention_rows(a, false, s) : launch_attention_few(a, false, s)) return rc;
     if (int rc = launch_attention_join(a, s)) return rc;
     if (a.weights && !p.spill) return launch_weights_few(a, true, s);
     return SWAPNET_OK;

@@ -41,6 +41,7 @@ struct CachedPlan {
 };
 CachedPlan cached_plan(const CachedArgs& a);
 
+int launch_attention_rows(const CachedArgs& a, bool early, cudaStream_t s);  // tcgen05
 int launch_attention_few(const CachedArgs& a, bool early, cudaStream_t s);
 int launch_attention_join(const CachedArgs& a, cudaStream_t s);   // splits -> out, lse (and weights from scores)
 int launch_weights_few(const CachedArgs& a, bool early, cudaStream_t s);

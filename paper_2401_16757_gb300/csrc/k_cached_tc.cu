@@ -1,0 +1,622 @@
+// Attention of many query rows (wide drafted trees, runs of a prompt) over a
+// key-value cache on the tcgen05 tensor cores; fp16 / bf16 storage, fp32
+// arithmetic.
+//
+// Rows of a (sequence, key head) are its queries times the heads that share
+// the key head, query-major: row t * group + h.  One CTA owns up to 128 rows
+// and a share of the key tiles (128 keys each; the drafted nodes are one more
+// tile, the last):
+//   S = Q K^T   tcgen05.mma, M 128 (rows) x N 128 (keys); Q, K and V by TMA
+//               (128-byte swizzle); S in two TMEM buffers, so that the next
+//               tile's S is computed during this tile's softmax
+//   P           warps 2..9, two threads per row: scores from TMEM, masks only
+//               in tiles that a limit crosses, p = 2^(s - m) back to TMEM as
+//               two parts of the storage type p_hi + p_lo (about 16 bits of p)
+//   O += P V    tcgen05.mma with A = P from TMEM, B = V as loaded (MN-major)
+// O stays in TMEM.  The exponent's reference m is the running maximum only
+// where that grew by more than 2^8 since it was last taken (kSlack): until
+// then p and l stay within 2^8 of their usual range, which fp32 sums and both
+// storage types hold without loss, and O is neither read nor rescaled.
+// With at most 64 rows (REP 2) the rows appear twice in the MMA's 128: lanes
+// 0..63 take the first 64 keys of a tile, lanes 64..127 the others, so that
+// all eight warps share the softmax; each half has its own m, l and O (the
+// other half's keys are zeros in its P), joined at the end.
+// K and V tiles pass through one ring in the order they are used.  Every wait
+// is bounded: on timeout the kernel records kDevErrTimeout, drains the loads
+// and MMAs it started, frees TMEM and returns.
+#include <algorithm>
+#include <cstring>
+#include <string>
+#include <type_traits>
+
+#include "cached.cuh"
+#include "internal.h"
+#include "kernels.h"
+
+namespace swapnet {
+
+namespace {
+
+constexpr int kSoftThreads = 256;
+constexpr int kTcThreads = 64 + kSoftThreads;
+constexpr int kKeys = 128;       // keys of a tile
+constexpr float kSlack = 8.0f;   // log2 of what p may exceed 1 by
+constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kTmO = 256, kTmPhi = 384, kTmPlo = 448;  // S: [0, 128) and [128, 256)
+
+template <int D> struct TcCfg {
+  static constexpr int kHalves = D / 64;             // 64-dim boxes of a tile
+  static constexpr int kBox = 128 * 128;             // bytes of a 128-row x 64-element box
+  static constexpr int kTile = kHalves * kBox;
+  static constexpr int kSlots = D == 128 ? 5 : 8;
+  static constexpr int kOffQ = 0;
+  static constexpr int kOffRing = kTile;
+  static constexpr int kOffX = kOffRing + kSlots * kTile;   // exchange [2][2][128] floats
+  static constexpr int kOffPar = kOffX + 2 * 2 * 128 * 4;   // parents
+  static constexpr int kOffOdd = kOffPar + kTreeMax * 4;    // odd value rows [4], p of one key [128]
+  static constexpr int kOffBar = kOffOdd + 16 + 128 * 4;
+  static constexpr int kSmem = kOffBar + 256 + 1024;        // + alignment slack
+  static_assert(kSmem <= 232448, "shared memory of a CTA");
+  static_assert(kSlots * kTile >= 128 * (D + 4) * 4, "the rows' outputs overlay the ring");
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, uint32_t bar, int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+      "l"(tmap), "r"(bar), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem]
+__device__ __forceinline__ void tc_mma_f16_ta(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(tmem_d),
+      "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Descriptor of a B operand stored MN-major with the 128-byte swizzle: 8-row
+// groups 1024 bytes apart, 64-column blocks one box apart.
+__device__ __forceinline__ uint64_t desc_mn(uint32_t addr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((addr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(128 * 128 >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+
+template <typename T, int D, int REP>
+__global__ void __launch_bounds__(kTcThreads, 1)
+    attention_rows_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                          const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmKn,
+                          const __grid_constant__ CUtensorMap tmVn, const __grid_constant__ CachedArgs a, int queries) {
+  using F = TcCfg<D>;
+  constexpr int kRowsMax = 128 / REP;
+  constexpr int NK = 64 / REP;  // keys per thread and tile
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  float* xch = reinterpret_cast<float*>(smem + F::kOffX);
+  int* par = reinterpret_cast<int*>(smem + F::kOffPar);
+  uint32_t* odd_rows = reinterpret_cast<uint32_t*>(smem + F::kOffOdd);
+  float* odd_p = reinterpret_cast<float*>(smem + F::kOffOdd + 16);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + F::kOffBar);
+  auto full = [&](int s) { return smem_u32(bars + s); };
+  auto empty = [&](int s) { return smem_u32(bars + 8 + s); };
+  auto s_full = [&](int i) { return smem_u32(bars + 16 + i); };
+  const uint32_t q_full = smem_u32(bars + 18), p_full = smem_u32(bars + 19), o_full = smem_u32(bars + 20),
+                 done_bar = smem_u32(bars + 21);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 22);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 23);
+
+  const int warp = warp_index(), lane = threadIdx.x & 31;
+  const int split = (int)blockIdx.x % a.splits, t0 = (int)(blockIdx.x / a.splits) * queries;
+  const int kvh = blockIdx.y, b = blockIdx.z;
+  pdl_wait();
+  pdl_launch_dependents();
+  int len, count;
+  if (!seq_sizes(a, b, &len, &count)) return;
+  if (t0 >= count) return;
+  const int nq = min(queries, count - t0), rows = nq * a.group;
+  if (a.k_new && a.parents) {
+    bool bad = false;
+    for (int t = threadIdx.x; t < count; t += kTcThreads) {
+      const int p = a.parents[(int64_t)b * a.tokens + t];
+      par[t] = p;
+      bad = bad || p < -1 || p >= t;
+    }
+    if (__syncthreads_or(bad)) {
+      if (threadIdx.x == 0) atomicExch(a.err, kDevErrBounds);
+      return;
+    }
+  }
+  // this CTA's tiles [i0, i0 + n) of the prefix's np and, behind them, the draft
+  const int kmax = visible_limit(a, len, count, t0 + nq - 1), lim_min = visible_limit(a, len, count, t0);
+  const int np = (kmax + kKeys - 1) / kKeys, tiles = np + (a.k_new ? 1 : 0);
+  const int i0 = (int)((int64_t)tiles * split / a.splits), n = (int)((int64_t)tiles * (split + 1) / a.splits) - i0;
+  const int soft_warps = 2 * (REP == 2 ? 4 : (rows + 31) / 32);  // whose lanes hold rows
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < F::kSlots; ++s) {
+      mbar_init(full(s), 1);
+      mbar_init(empty(s), 1);
+    }
+    mbar_init(s_full(0), 1);
+    mbar_init(s_full(1), 1);
+    mbar_init(q_full, 1);
+    mbar_init(p_full, 32 * soft_warps);
+    mbar_init(o_full, 1);
+    mbar_init(done_bar, 1);
+    *abort_flag = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) odd_rows[w] = 0;
+    fence_barrier_init();
+    prefetch_tmap(&tmQ);
+    prefetch_tmap(&tmK);
+    prefetch_tmap(&tmV);
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(tmem_slot), kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  // tiles in the order of use: K0, K1, V0, K2, V1, ..., V(n-1)
+  auto k_pos = [&](int i) { return i == 0 ? 0 : 2 * i - 1; };
+  auto v_pos = [&](int i) { return i == n - 1 ? 2 * n - 1 : 2 * i + 2; };
+
+  if (warp == 0) {
+    if (n > 0 && elect_one()) {
+      // ---------------- TMA producer
+      const int q_rows = queries * a.group;
+      mbar_arrive_expect_tx(q_full, REP * F::kHalves * q_rows * 128);
+#pragma unroll
+      for (int c = 0; c < REP; ++c)
+#pragma unroll
+        for (int h = 0; h < F::kHalves; ++h)
+          tma_load_3d(smem_u32(smem + F::kOffQ + h * F::kBox + c * (kRowsMax * 128)), &tmQ, q_full, h * 64, kvh * a.group,
+                      b * a.tokens + t0);
+      int pos = 0;
+      auto load = [&](int i, bool keys) -> bool {
+        const int s = pos % F::kSlots;
+        if (pos >= F::kSlots && !mbar_wait_bounded(empty(s), ((pos / F::kSlots) - 1) & 1, abort_flag, a.err)) return false;
+        mbar_arrive_expect_tx(full(s), F::kTile);
+        const bool nw = i0 + i >= np;
+        const CUtensorMap* tm = keys ? (nw ? &tmKn : &tmK) : (nw ? &tmVn : &tmV);
+#pragma unroll
+        for (int h = 0; h < F::kHalves; ++h)
+          tma_load_3d(smem_u32(smem + F::kOffRing + s * F::kTile + h * F::kBox), tm, full(s), kvh * D + h * 64,
+                      nw ? 0 : (i0 + i) * kKeys, b);
+        ++pos;
+        return true;
+      };
+      bool ok = load(0, true) && (n < 2 || load(1, true));
+      for (int i = 0; ok && i < n; ++i) ok = load(i, false) && (i + 2 >= n || load(i + 2, true));
+      // let every load issued land before the CTA can exit
+      volatile int no_abort = 0;
+      mbar_wait_bounded(q_full, 0, &no_abort, nullptr);
+      for (int j = max(0, pos - F::kSlots); j < pos; ++j)
+        mbar_wait_bounded(full(j % F::kSlots), (j / F::kSlots) & 1, &no_abort, nullptr);
+    }
+  } else if (warp == 1) {
+    if (n > 0 && elect_one()) {
+      // ---------------- MMA issuer
+      constexpr int bf = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
+      constexpr uint32_t idesc_s = idesc_f16(bf, 128, kKeys);
+      constexpr uint32_t idesc_pv = idesc_f16(bf, 128, D) | (1u << 16);  // B (values) MN-major
+      const uint64_t qd = smem_desc_sw128(smem_u32(smem + F::kOffQ));
+      const uint64_t kd = smem_desc_sw128(smem_u32(smem + F::kOffRing)), vd = desc_mn(smem_u32(smem + F::kOffRing));
+      auto scores = [&](int i) -> bool {
+        const int pos = k_pos(i), s = pos % F::kSlots;
+        if (!mbar_wait_bounded(full(s), (pos / F::kSlots) & 1, abort_flag, a.err)) return false;
+        tc_fence_after();
+        const uint64_t kt = kd + (uint64_t)(s * (F::kTile >> 4));  // the descriptors' address field counts 16 bytes
+#pragma unroll
+        for (int h = 0; h < F::kHalves; ++h)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            tc_mma_f16(tmem + (uint32_t)(i & 1) * 128u, qd + (uint64_t)(h * (F::kBox >> 4) + 2 * k),
+                       kt + (uint64_t)(h * (F::kBox >> 4) + 2 * k), idesc_s, (h | k) != 0);
+        tc_commit(s_full(i & 1));
+        tc_commit(empty(s));
+        return true;
+      };
+      bool ok = mbar_wait_bounded(q_full, 0, abort_flag, a.err) && scores(0);
+      for (int i = 0; ok && i < n; ++i) {
+        if (i + 1 < n && !scores(i + 1)) break;
+        const int pos = v_pos(i), s = pos % F::kSlots;
+        if (!mbar_wait_bounded(full(s), (pos / F::kSlots) & 1, abort_flag, a.err)) break;
+        if (!mbar_wait_bounded(p_full, i & 1, abort_flag, a.err)) break;
+        tc_fence_after();
+        const uint64_t vt = vd + (uint64_t)(s * (F::kTile >> 4));
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+          for (int ks = 0; ks < 8; ++ks)  // 16 keys a step
+            tc_mma_f16_ta(tmem + kTmO, tmem + (part ? kTmPlo : kTmPhi) + (uint32_t)(ks * 8), vt + (uint64_t)(ks * (2048 >> 4)),
+                          idesc_pv, (uint32_t)(i | part | ks) != 0);
+        tc_commit(o_full);
+        tc_commit(empty(s));
+      }
+      // every MMA issued must have finished before TMEM is freed
+      tc_commit(done_bar);
+      volatile int no_abort = 0;
+      mbar_wait_bounded(done_bar, 0, &no_abort, nullptr);
+    }
+  } else if (REP == 2 || (warp & 3) * 32 < rows) {
+    // ---------------- softmax and output
+    const int q4 = warp & 3, half = (warp - 2) >> 2;
+    const int slot = q4 * 32 + lane, rep = slot / kRowsMax, row = slot % kRowsMax;
+    const int active = 32 * soft_warps, aid = (half * (soft_warps / 2) + q4) * 32 + lane;
+    const int t = t0 + min(row, rows - 1) / a.group;
+    const int lim = visible_limit(a, len, count, t);
+    const int kofs = rep * (128 / REP) + half * NK;
+    const uint32_t lane_off = (uint32_t)(q4 * 32) << 16;
+    // the two warps of a row quarter meet here; both take part in every
+    // tile's exchange, also after a timeout
+    auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory"); };
+    auto all_sync = [&]() { asm volatile("bar.sync 5, %0;" ::"r"(active) : "memory"); };
+    if (REP == 2 && n > 0) {  // the keys of the other half of the lanes stay zeros in P
+      uint32_t z[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) z[i] = 0;
+#pragma unroll
+      for (int c = 0; c < 64; c += 16) tmem_st_x16(tmem + lane_off + (half ? kTmPlo : kTmPhi) + (uint32_t)c, z);
+      tmem_st_wait();
+      pair_sync();
+    }
+    float m = -INFINITY, l = 0.f;  // m: the reference, in log2 units
+    bool ok = true;
+    for (int i = 0; i < n; ++i) {
+      const bool nw = i0 + i >= np;
+      const int k0 = nw ? 0 : (i0 + i) * kKeys;
+      const bool masked = nw || k0 + kKeys > lim_min;  // some of these keys are hidden from some rows
+      ok = ok && mbar_wait_bounded(s_full(i & 1), (i >> 1) & 1, abort_flag, a.err);
+      ok = __all_sync(0xffffffffu, ok);
+      tc_fence_after();
+      uint32_t s[NK];
+      float mx = -INFINITY;
+      if (ok) {
+#pragma unroll
+        for (int c = 0; c < NK; c += 32) {
+          uint32_t(&r)[32] = *reinterpret_cast<uint32_t(*)[32]>(s + c);
+          tmem_ld_32x32b_x32(tmem + (uint32_t)(i & 1) * 128u + lane_off + (uint32_t)(kofs + c), r);
+        }
+        tmem_ld_wait();
+        if (masked) {
+          uint32_t see[NK / 32];
+#pragma unroll
+          for (int w = 0; w < NK / 32; ++w) see[w] = 0;
+          if (nw && a.parents) {
+            for (int j = t; j >= 0; j = par[j]) {
+#pragma unroll
+              for (int w = 0; w < NK / 32; ++w)
+                if ((j - kofs) >> 5 == w) see[w] |= 1u << ((j - kofs) & 31);
+            }
+          } else {
+            const int seen = (nw ? t + 1 : lim - k0) - kofs;
+#pragma unroll
+            for (int w = 0; w < NK / 32; ++w) see[w] = seen >= 32 * w + 32 ? 0xffffffffu : seen > 32 * w ? (1u << (seen - 32 * w)) - 1u : 0u;
+          }
+#pragma unroll
+          for (int k = 0; k < NK; ++k)
+            if (!(see[k >> 5] >> (k & 31) & 1u)) s[k] = 0xff800000u;  // -inf
+        }
+#pragma unroll
+        for (int k = 0; k < NK; ++k) mx = fmaxf(mx, __uint_as_float(s[k]));
+      }
+      float* x = xch + (i & 1) * 256;
+      x[half * 128 + slot] = mx;
+      pair_sync();
+      mx = fmaxf(mx, x[(half ^ 1) * 128 + slot]) * a.scale_log2;
+      const bool grow = mx - m > kSlack;  // (also the first key seen)
+      float alpha = 1.f;
+      if (grow) {
+        alpha = ex2(m - mx);
+        m = mx;
+        l *= alpha;
+      }
+      const float base = m == -INFINITY ? 0.f : m;
+      uint32_t hi[NK / 2], lo[NK / 2];
+      if (ok) {
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < NK / 2; ++k) {
+          const float p0 = ex2(fmaf(__uint_as_float(s[2 * k]), a.scale_log2, -base));
+          const float p1 = ex2(fmaf(__uint_as_float(s[2 * k + 1]), a.scale_log2, -base));
+          sum += p0;
+          sum += p1;
+          hi[k] = pack_pair<T>(p0, p1);
+          const float2 back = unpack_pair<T>(hi[k]);
+          lo[k] = pack_pair<T>(p0 - back.x, p1 - back.y);
+        }
+        l += sum;
+      }
+      if (i > 0) {  // P and O are free once the product of the tile before is done
+        ok = ok && mbar_wait_bounded(o_full, (i - 1) & 1, abort_flag, a.err);
+        ok = __all_sync(0xffffffffu, ok);
+        tc_fence_after();
+        if (ok && __any_sync(0xffffffffu, grow)) {
+#pragma unroll
+          for (int c = 0; c < D / 2; c += 16) {
+            uint32_t r[16];
+            const uint32_t at = tmem + kTmO + lane_off + (uint32_t)(half * (D / 2) + c);
+            tmem_ld_32x32b_x16(at, r);
+            tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * alpha);
+            tmem_st_x16(at, r);
+          }
+        }
+      }
+      uint32_t odd[4] = {0u, 0u, 0u, 0u};
+      uint8_t* vs = smem + F::kOffRing + (v_pos(i) % F::kSlots) * F::kTile;
+      if (masked) {
+        // A value row that some of the rows do not see must not reach them
+        // even if it is infinite or not a number (0 x inf): rows behind the
+        // last key are cleared, others that hold such a value as well, and
+        // added by hand below where they are seen.
+        ok = ok && mbar_wait_bounded(full(v_pos(i) % F::kSlots), (v_pos(i) / F::kSlots) & 1, abort_flag, a.err);
+        ok = __all_sync(0xffffffffu, ok);
+        const int have = min(kKeys, nw ? count : len - k0);
+        auto chunk = [&](int r, int c) {
+          return reinterpret_cast<uint4*>(vs + (c >> 3) * F::kBox + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+        };
+        if (ok) {
+          for (int c = aid; c < kKeys * (D / 8); c += active) {
+            const int r = c / (D / 8);
+            uint4* at = chunk(r, c % (D / 8));
+            if (r >= have) {
+              *at = make_uint4(0u, 0u, 0u, 0u);
+            } else {
+              const uint4 v = *at;
+              if (odd_pair<T>(v.x) || odd_pair<T>(v.y) || odd_pair<T>(v.z) || odd_pair<T>(v.w)) atomicOr(&odd_rows[r >> 5], 1u << (r & 31));
+            }
+          }
+        }
+        all_sync();
+#pragma unroll
+        for (int w = 0; w < 4; ++w) odd[w] = odd_rows[w];
+        if (odd[0] | odd[1] | odd[2] | odd[3]) {
+          for (int c = aid; c < kKeys * (D / 8); c += active) {
+            const int r = c / (D / 8);
+            if (odd_rows[r >> 5] >> (r & 31) & 1u) *chunk(r, c % (D / 8)) = make_uint4(0u, 0u, 0u, 0u);
+          }
+        }
+        fence_proxy_async_smem();  // V is read by the tensor cores (async proxy)
+      }
+      if (ok) {
+#pragma unroll
+        for (int c = 0; c < NK / 2; c += 16) {
+          tmem_st_x16(tmem + kTmPhi + lane_off + (uint32_t)(kofs / 2 + c), hi + c);
+          tmem_st_x16(tmem + kTmPlo + lane_off + (uint32_t)(kofs / 2 + c), lo + c);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(p_full);
+      }
+      if (odd[0] | odd[1] | odd[2] | odd[3]) {
+        ok = ok && mbar_wait_bounded(o_full, i & 1, abort_flag, a.err);
+        ok = __all_sync(0xffffffffu, ok);
+        tc_fence_after();
+        for (int j = 0; j < kKeys; ++j) {
+          if (!(odd_rows[j >> 5] >> (j & 31) & 1u)) continue;
+          const int rel = j - kofs;
+          if (rel >= 0 && rel < NK) {
+            float pj = 0.f;
+#pragma unroll
+            for (int k = 0; k < NK / 2; ++k) {
+              const float2 h2 = unpack_pair<T>(hi[k]), l2 = unpack_pair<T>(lo[k]);
+              if (rel == 2 * k) pj = h2.x + l2.x;
+              if (rel == 2 * k + 1) pj = h2.y + l2.y;
+            }
+            odd_p[slot] = pj;
+          } else if (half == 0 && (REP == 2 && j / kRowsMax != rep)) {
+            odd_p[slot] = 0.f;
+          }
+          pair_sync();
+          const float pj = odd_p[slot];
+          const T* v = nw ? static_cast<const T*>(a.v_new) + ((int64_t)b * a.tokens + j) * a.new_stride
+                          : static_cast<const T*>(a.v) + (int64_t)b * a.seq_stride + (int64_t)(k0 + j) * a.kv_stride;
+          v += kvh * D + half * (D / 2);
+          if (ok) {
+            for (int c = 0; c < D / 2; c += 16) {
+              uint32_t r[16];
+              const uint32_t at = tmem + kTmO + lane_off + (uint32_t)(half * (D / 2) + c);
+              tmem_ld_32x32b_x16(at, r);
+              tmem_ld_wait();
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                if (pj != 0.f) r[e] = __float_as_uint(fmaf(pj, to_f<T>(v[c + e]), __uint_as_float(r[e])));
+              tmem_st_x16(at, r);
+              tmem_st_wait();
+            }
+          }
+          pair_sync();
+        }
+        all_sync();  // everyone has read the odd rows
+        if (aid < 4) odd_rows[aid] = 0;
+        all_sync();
+      }
+    }
+    // ---- the rows' results
+    const int64_t first = (((int64_t)b * a.kv_heads + kvh) * a.splits + split) * a.tokens * a.group + (int64_t)t0 * a.group;
+    auto emit = [&](int r, int c, const float* o, int cols, float L) {  // cols: a multiple of 4
+      if (a.splits > 1) {
+        float4* to = reinterpret_cast<float4*>(a.part + (first + r) * D + c);
+        for (int e = 0; e < cols / 4; ++e) to[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+        return;
+      }
+      const float inv = L > 0.f ? 1.0f / L : (L == 0.f ? 0.f : L);  // (a NaN stays one)
+      T* to = static_cast<T*>(a.out) + ((int64_t)b * a.tokens + t0 + r / a.group) * a.out_stride +
+              (int64_t)(kvh * a.group + r % a.group) * D + c;
+      for (int e = 0; e < cols / 4; ++e)
+        reinterpret_cast<uint2*>(to)[e] =
+            make_uint2(pack_pair<T>(o[4 * e] * inv, o[4 * e + 1] * inv), pack_pair<T>(o[4 * e + 2] * inv, o[4 * e + 3] * inv));
+    };
+    auto emit_stats = [&](int r, float M, float L) {
+      if (a.splits > 1)
+        reinterpret_cast<float2*>(a.ml)[first + r] = make_float2(M, L);
+      else if (a.lse)
+        a.lse[((int64_t)b * a.heads + kvh * a.group + r % a.group) * a.tokens + t0 + r / a.group] =
+            L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+    };
+    if (n > 0) {
+      ok = ok && mbar_wait_bounded(o_full, (n - 1) & 1, abort_flag, a.err);
+      ok = __all_sync(0xffffffffu, ok);
+      tc_fence_after();
+    }
+    float* x = xch + (n & 1) * 256;  // (the other buffer may still be read)
+    x[half * 128 + slot] = l;
+    pair_sync();
+    const float L = x[slot] + x[128 + slot];
+    if (REP == 1) {
+      for (int c = 0; c < D / 2; c += 16) {
+        float o[16];
+        uint32_t r[16];
+        if (n > 0) {
+          tmem_ld_32x32b_x16(tmem + kTmO + lane_off + (uint32_t)(half * (D / 2) + c), r);
+          tmem_ld_wait();
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[e] = n > 0 ? __uint_as_float(r[e]) : 0.f;
+        if (ok && row < rows && (n > 0 || a.splits == 1)) emit(row, half * (D / 2) + c, o, 16, L);
+      }
+      if (ok && half == 0 && row < rows) emit_stats(row, m, L);
+    } else {
+      float* ov = reinterpret_cast<float*>(smem + F::kOffRing);  // [128][D + 4]: every load and product has ended
+      if (n > 0 && ok) {
+        for (int c = 0; c < D / 2; c += 16) {
+          uint32_t r[16];
+          tmem_ld_32x32b_x16(tmem + kTmO + lane_off + (uint32_t)(half * (D / 2) + c), r);
+          tmem_ld_wait();
+          float4* to = reinterpret_cast<float4*>(ov + slot * (D + 4) + half * (D / 2) + c);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            to[e] = make_float4(__uint_as_float(r[4 * e]), __uint_as_float(r[4 * e + 1]), __uint_as_float(r[4 * e + 2]),
+                                __uint_as_float(r[4 * e + 3]));
+        }
+      }
+      float* y = xch + ((n + 1) & 1) * 256;
+      pair_sync();  // (that buffer's last readers have passed)
+      if (half == 0) {
+        y[slot] = m;
+        y[128 + slot] = L;
+      }
+      all_sync();
+      if (ok) {
+        for (int c = aid; c < rows * (D / 4); c += active) {
+          const int r = c / (D / 4), col = c % (D / 4) * 4;
+          const float m0 = y[r], m1 = y[64 + r], M = fmaxf(m0, m1), base = M == -INFINITY ? 0.f : M;
+          const float f0 = ex2(m0 - base), f1 = ex2(m1 - base);
+          const float LL = fmaf(y[128 + r], f0, y[192 + r] * f1);
+          float o[4] = {0.f, 0.f, 0.f, 0.f};
+          if (n > 0) {
+            const float4 u = *reinterpret_cast<const float4*>(ov + r * (D + 4) + col);
+            const float4 w = *reinterpret_cast<const float4*>(ov + (64 + r) * (D + 4) + col);
+            // (a half that saw no key holds zeros, and its factor is zero)
+            o[0] = fmaf(u.x, f0, w.x * f1);
+            o[1] = fmaf(u.y, f0, w.y * f1);
+            o[2] = fmaf(u.z, f0, w.z * f1);
+            o[3] = fmaf(u.w, f0, w.w * f1);
+          }
+          if (n > 0 || a.splits == 1) emit(r, col, o, 4, LL);
+          if (col == 0) emit_stats(r, M, LL);
+        }
+      }
+    }
+    tc_fence_before();
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+int done(cudaError_t e, const char* what) {
+  if (e == cudaSuccess) e = cudaGetLastError();
+  if (e != cudaSuccess) SN_FAIL(SWAPNET_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
+  return SWAPNET_OK;
+}
+
+// Maps of the queries (64 dims x the heads of a group x queries) and of a
+// cache or a draft (64 dims x 128 rows of one sequence).
+int query_map(CUtensorMap* m, const CachedArgs& a, int queries) {
+  const uint64_t dims[3] = {(uint64_t)a.dim, (uint64_t)a.heads, (uint64_t)a.n_seq * a.tokens};
+  const uint64_t strides[2] = {(uint64_t)a.dim * 2, (uint64_t)a.q_stride * 2};
+  const uint32_t box[3] = {64, (uint32_t)a.group, (uint32_t)queries};
+  return make_tmap_3d(m, a.dtype, a.q, dims, strides, box);
+}
+int rows_map(CUtensorMap* m, const CachedArgs& a, const void* base, int64_t rows, int64_t row_stride, int64_t seq_stride) {
+  const uint64_t dims[3] = {(uint64_t)a.kv_heads * a.dim, (uint64_t)rows, (uint64_t)a.n_seq};
+  // (a single sequence's stride is never used, but has to be a valid one)
+  const uint64_t strides[2] = {(uint64_t)row_stride * 2, (uint64_t)(a.n_seq > 1 ? seq_stride : row_stride) * 2};
+  const uint32_t box[3] = {64, kKeys, 1};
+  return make_tmap_3d(m, a.dtype, base, dims, strides, box);
+}
+
+template <typename T, int D, int REP> int rows_t(const CachedArgs& a, bool early, cudaStream_t s) {
+  static std::atomic<uint64_t> known{0};
+  const auto kern = attention_rows_kernel<T, D, REP>;
+  if (attr_needed(known)) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, TcCfg<D>::kSmem);
+    if (e != cudaSuccess) return done(e, "cached attention: shared memory");
+    attr_set(known);
+  }
+  const int queries = std::min(128 / REP / a.group, a.tokens);
+  CUtensorMap q, k, v, kn, vn;
+  int rc = query_map(&q, a, queries);
+  if (!rc) rc = rows_map(&k, a, a.k, a.max_seq, a.kv_stride, a.seq_stride);
+  if (!rc) rc = rows_map(&v, a, a.v, a.max_seq, a.kv_stride, a.seq_stride);
+  kn = k;
+  vn = v;
+  if (a.k_new) {
+    if (!rc) rc = rows_map(&kn, a, a.k_new, a.tokens, a.new_stride, a.new_stride * a.tokens);
+    if (!rc) rc = rows_map(&vn, a, a.v_new, a.tokens, a.new_stride, a.new_stride * a.tokens);
+  }
+  if (rc) return rc;
+  cudaLaunchConfig_t cfg;
+  std::memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = dim3((a.tokens + queries - 1) / queries * a.splits, a.kv_heads, a.n_seq);
+  cfg.blockDim = dim3(kTcThreads);
+  cfg.dynamicSmemBytes = TcCfg<D>::kSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = early ? 1 : 0;
+  return done(cudaLaunchKernelEx(&cfg, kern, q, k, v, kn, vn, a, queries), "cached attention launch");
+}
+template <typename T, int D> int rows_d(const CachedArgs& a, bool early, cudaStream_t s) {
+  return a.tokens * a.group <= 64 ? rows_t<T, D, 2>(a, early, s) : rows_t<T, D, 1>(a, early, s);
+}
+
+}  // namespace
+
+int launch_attention_rows(const CachedArgs& a, bool early, cudaStream_t s) {
+  if (a.dtype == SWAPNET_BF16)
+    return a.dim == 128 ? rows_d<__nv_bfloat16, 128>(a, early, s) : rows_d<__nv_bfloat16, 64>(a, early, s);
+  return a.dim == 128 ? rows_d<__half, 128>(a, early, s) : rows_d<__half, 64>(a, early, s);
+}
+
+}  // namespace swapnet

@@ -203,6 +203,10 @@ int tc_error_word(int** ptr);
 int make_tmap_2d(CUtensorMap* m, int dtype, const void* base, uint64_t inner, uint64_t rows, uint64_t row_stride_bytes,
                  uint32_t box_inner, uint32_t box_rows);
 
+// The same in three dimensions (strides of the second and third).
+int make_tmap_3d(CUtensorMap* m, int dtype, const void* base, const uint64_t (&dims)[3], const uint64_t (&stride_bytes)[2],
+                 const uint32_t (&box)[3]);
+
 // tcgen05 causal attention for query runs (prefill): q [tokens][width]
 // (already rotated), key and value caches [max_seq][width], head width 128,
 // query t at position *pos_ptr + t attends to positions 0..*pos_ptr + t.
