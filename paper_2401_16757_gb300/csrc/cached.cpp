@@ -17,13 +17,13 @@ namespace swapnet {
 // of it is filled only the device knows).  step / fixed: microseconds of a
 // CTA's tile of keys and of its start and end; more than one also pays the
 // join.
-static int choose_splits(int64_t ctas, int tiles, int per_sm, double step, double fixed) {
+static int choose_splits(int64_t ctas, int tiles, int per_sm, double step, double fixed, double join) {
   const int64_t room = 152 * per_sm;
   int best = 1;
   double least = 1e30;
   for (int s = 1; s <= tiles && s <= 128; ++s) {
     const double waves = std::max(1.0, (double)(ctas * s) / room);  // (many waves even out)
-    const double t = (waves < 4.0 ? std::ceil(waves) : waves) * ((tiles + s - 1) / s * step + fixed) + (s > 1 ? 2.0 + 0.02 * s : 0.0);
+    const double t = (waves < 4.0 ? std::ceil(waves) : waves) * ((tiles + s - 1) / s * step + fixed) + (s > 1 ? join + 0.02 * s : 0.0);
     if (t < least * 0.99) {
       least = t;
       best = s;
@@ -39,9 +39,9 @@ CachedPlan cached_plan(const CachedArgs& a) {
   p.tc = rows > 32;
   if (p.tc) {
     const int queries = (rows <= 64 ? 64 : 128) / a.group;
-    p.splits = choose_splits(pairs * ((a.tokens + queries - 1) / queries), (a.max_seq + 127) / 128 + (a.k_new ? 1 : 0), 1, 0.9, 3.0);
+    p.splits = choose_splits(pairs * ((a.tokens + queries - 1) / queries), (a.max_seq + 127) / 128 + (a.k_new ? 1 : 0), 1, 0.9, 3.0, 2.0);
   } else {
-    p.splits = choose_splits(pairs, (a.max_seq + 63) / 64, 2, 0.5, 2.0);
+    p.splits = choose_splits(pairs, (a.max_seq + 63) / 64, 2, 0.5, 2.0, 2.0);
   }
   p.spill = a.weights && rows <= 32;
   p.score_ld = (a.max_seq + 15) / 16 * 16;
@@ -50,6 +50,18 @@ CachedPlan cached_plan(const CachedArgs& a) {
   if (p.splits > 1 || p.spill) p.ml_bytes = align_up(all * p.splits * 8);
   if (p.spill) p.score_bytes = align_up(all * p.score_ld * 4);
   return p;
+}
+
+int launch_weights(const CachedArgs& a, bool early, cudaStream_t s) {
+  const int64_t rows = (int64_t)a.tokens * a.group, pairs = (int64_t)a.n_seq * a.kv_heads;
+  CachedArgs x = a;
+  if (rows > 32) {
+    const int tiles = (int)((rows + 127) / 128);
+    x.splits = choose_splits(pairs, (a.max_seq + 127) / 128, 1, 0.3 + 0.4 * tiles, 2.5, 0.0);
+    return launch_weights_rows(x, early, s);
+  }
+  x.splits = choose_splits(pairs, (a.max_seq + 63) / 64, 2, 0.25, 2.0, 0.0);
+  return launch_weights_few(x, early, s);
 }
 
 namespace {
@@ -175,7 +187,7 @@ int swapnet_attention_tree(const swapnet_cached_attention* c, void* workspace, u
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     if (int rc = p.tc ? launch_attention_rows(a, false, s) : launch_attention_few(a, false, s)) return rc;
     if (int rc = launch_attention_join(a, s)) return rc;
-    if (a.weights && !p.spill) return launch_weights_few(a, true, s);
+    if (a.weights && !p.spill) return launch_weights(a, true, s);
     return SWAPNET_OK;
   });
 }
@@ -188,7 +200,7 @@ int swapnet_attention_weights(const swapnet_cached_attention* c, swapnet_stream 
     if (!c->lse || !c->weights) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cache weights: null pointer");
     if (c->k_new || c->v_new || c->parents) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cache weights: the queries are rows of the cache");
     if (int rc = error_word(&a.err)) return rc;
-    return launch_weights_few(a, false, reinterpret_cast<cudaStream_t>(stream));
+    return launch_weights(a, false, reinterpret_cast<cudaStream_t>(stream));
   });
 }
 

@@ -60,6 +60,13 @@ __device__ __forceinline__ bool build_ancestors(const CachedArgs& a, int b, int 
   return true;
 }
 
+// 2^x to 2 ulp; results below the normal range are 0.
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // ------------------------------------------------------ warp matrix products
 __device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"

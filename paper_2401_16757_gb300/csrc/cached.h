@@ -45,6 +45,9 @@ int launch_attention_rows(const CachedArgs& a, bool early, cudaStream_t s);  // 
 int launch_attention_few(const CachedArgs& a, bool early, cudaStream_t s);
 int launch_attention_join(const CachedArgs& a, cudaStream_t s);   // splits -> out, lse (and weights from scores)
 int launch_weights_few(const CachedArgs& a, bool early, cudaStream_t s);
+int launch_weights_rows(const CachedArgs& a, bool early, cudaStream_t s);  // tcgen05
+// The weights by the kernel and the splits that the sizes call for.
+int launch_weights(const CachedArgs& a, bool early, cudaStream_t s);
 
 struct EvictArgs {
   int dtype, n_seq, kv_heads, dim, max_seq, keep, recent, sink, out_seq;

@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(kFwThreads, 2) attention_few_kernel(const __gr
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
         const float mn = fmaxf(m[mt][h], mx);
         base[h] = mn == -INFINITY ? 0.f : mn;  // (nothing seen yet)
-        al[h] = exp2f(m[mt][h] - base[h]);
+        al[h] = ex2(m[mt][h] - base[h]);
         m[mt][h] = mn;
       }
       float sum[2] = {0.f, 0.f};
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(kFwThreads, 2) attention_few_kernel(const __gr
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float p0 = exp2f(s[mt][n][2 * h] - base[h]), p1 = exp2f(s[mt][n][2 * h + 1] - base[h]);
+          const float p0 = ex2(s[mt][n][2 * h] - base[h]), p1 = ex2(s[mt][n][2 * h + 1] - base[h]);
           sum[h] += p0 + p1;
           s[mt][n][2 * h] = p0;
           s[mt][n][2 * h + 1] = p1;
@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(kFwThreads, 2) attention_few_kernel(const __gr
 #pragma unroll
     for (int w = 0; w < kFwWarps; ++w) {
       const float2 ml = mls[w * F::kRows + rl];
-      const float f = exp2f(ml.x - base);
+      const float f = ex2(ml.x - base);
       const float4 y = reinterpret_cast<const float4*>(smem)[(w * F::kRows + rl) * V + c];
       L = fmaf(ml.y, f, L);
       if (f != 0.f) {
@@ -376,7 +376,7 @@ __device__ __forceinline__ float2 join_stats(const CachedArgs& a, int64_t first,
   const float base = M == -INFINITY ? 0.f : M;
   for (int s = 0; s < a.splits; ++s) {
     const float2 ml = reinterpret_cast<const float2*>(a.ml)[first + s * step];
-    L = fmaf(ml.y, exp2f(ml.x - base), L);
+    L = fmaf(ml.y, ex2(ml.x - base), L);
   }
   return make_float2(M, L);
 }
@@ -412,7 +412,7 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
       for (int s = 0; s < a.splits; ++s) {
         const float ms = reinterpret_cast<const float2*>(a.ml)[first + s * step + r].x;
         if (ms == -INFINITY) continue;
-        const float f = exp2f(ms - base);
+        const float f = ex2(ms - base);
         const float4 y = reinterpret_cast<const float4*>(a.part)[(first + s * step + r) * V + lane];
         x.x = fmaf(y.x, f, x.x);
         x.y = fmaf(y.y, f, x.y);
@@ -441,7 +441,7 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
     if (j >= len) break;
     float w = 0.f;
     for (int r = 0; r < rows; ++r)
-      if (j < visible_limit(a, len, count, r / a.group)) w += exp2f(sc[(int64_t)r * a.score_ld + j] - lse2[r]);
+      if (j < visible_limit(a, len, count, r / a.group)) w += ex2(sc[(int64_t)r * a.score_ld + j] - lse2[r]);
     a.weights[at + j] = (a.weights_in ? a.weights_in[at + j] : 0.f) + w;
   }
 }
@@ -552,7 +552,7 @@ __global__ void __launch_bounds__(kFwThreads) weights_few_kernel(const __grid_co
           for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-              const float p = exp2f(fmaf(s[n][2 * h + u], a.scale_log2, -e2));
+              const float p = ex2(fmaf(s[n][2 * h + u], a.scale_log2, -e2));
               if (!masked || j0 + n * 8 + (lane & 3) * 2 + u < lm) w[2 * n + u] += p;
             }
         }
@@ -625,11 +625,7 @@ template <typename T, int D> int few_d(const CachedArgs& a, bool early, cudaStre
 template <typename T, int D> int weights_t(const CachedArgs& a, bool early, cudaStream_t s) {
   static std::atomic<uint64_t> known{0};
   if (int rc = allow_smem(weights_few_kernel<T, D>, WfCfg<D>::kSmem, known)) return rc;
-  CachedArgs x = a;
-  // about eight CTAs per SM in all, 64 keys a warp at least
-  const int64_t pairs = (int64_t)a.n_seq * a.kv_heads;
-  x.splits = (int)std::max<int64_t>(1, std::min<int64_t>((8 * 152 + pairs - 1) / pairs, (a.max_seq + 255) / 256));
-  return done(launch(weights_few_kernel<T, D>, dim3(x.splits, a.kv_heads, a.n_seq), kFwThreads, WfCfg<D>::kSmem, early, s, x),
+  return done(launch(weights_few_kernel<T, D>, dim3(a.splits, a.kv_heads, a.n_seq), kFwThreads, WfCfg<D>::kSmem, early, s, a),
               "cache weights launch");
 }
 

@@ -60,11 +60,6 @@ template <int D> struct TcCfg {
   static_assert(kSlots * kTile >= 128 * (D + 4) * 4, "the rows' outputs overlay the ring");
 };
 
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, uint32_t bar, int x, int y, int z) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
@@ -552,6 +547,285 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   }
 }
 
+// ------------------------------------------------------------------- weights
+// weights_j = weights_in_j + sum over rows of 2^(s_rj - lse_r): the scores with
+// the keys as the MMA's rows, S^T = K Q^T (M 128 keys x N up to 128 rows), so
+// that a key's sum over the rows stays in one thread.  A CTA takes every
+// splits-th tile of 128 keys of a (sequence, key head) and passes all tiles of
+// rows that see it; K and Q tiles by TMA, S in four TMEM buffers, two threads
+// per key (their sums meet in shared memory).  Rows of a list are fetched one
+// query at a time.
+template <int D> struct WtCfg {
+  static constexpr int kHalves = D / 64;
+  static constexpr int kBox = 128 * 128;
+  static constexpr int kTile = kHalves * kBox;
+  static constexpr int kKSlots = 3, kQSlots = 3;
+  static constexpr int kOffQ = kKSlots * kTile;
+  static constexpr int kOffLse = kOffQ + kQSlots * kTile;  // [2][128] log2 of the rows' sums
+  static constexpr int kOffLim = kOffLse + 2 * 128 * 4;
+  static constexpr int kOffX = kOffLim + 2 * 128 * 4;
+  static constexpr int kOffBar = kOffX + 2 * 128 * 4;
+  static constexpr int kSmem = kOffBar + 256 + 1024;
+  static_assert(kSmem <= 232448, "shared memory of a CTA");
+};
+constexpr int kSBufs = 4;
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kTcThreads, 1)
+    weights_rows_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                        const __grid_constant__ CachedArgs a, int queries) {
+  using F = WtCfg<D>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  float* lse2 = reinterpret_cast<float*>(smem + F::kOffLse);
+  int* lim = reinterpret_cast<int*>(smem + F::kOffLim);
+  float* xch = reinterpret_cast<float*>(smem + F::kOffX);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + F::kOffBar);
+  auto k_full = [&](int s) { return smem_u32(bars + s); };
+  auto k_empty = [&](int s) { return smem_u32(bars + 3 + s); };
+  auto q_full = [&](int s) { return smem_u32(bars + 6 + s); };
+  auto q_empty = [&](int s) { return smem_u32(bars + 9 + s); };
+  auto s_full = [&](int s) { return smem_u32(bars + 12 + s); };
+  auto s_empty = [&](int s) { return smem_u32(bars + 16 + s); };
+  const uint32_t done_bar = smem_u32(bars + 20);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 21);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 22);
+
+  const int warp = warp_index(), lane = threadIdx.x & 31;
+  const int split = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z;
+  pdl_wait();
+  pdl_launch_dependents();
+  int len, count;
+  if (!seq_sizes(a, b, &len, &count)) return;
+  const int ktiles = (len + kKeys - 1) / kKeys, nrt = (count + queries - 1) / queries;
+  if (split >= ktiles) return;
+  // the first tile of rows that sees key k0 (row i sees the keys below len - count + i + 1)
+  auto first_tile = [&](int kt) { return max(0, kt * kKeys - (len - count)) / queries; };
+  const bool keep_q = nrt <= F::kQSlots;  // all queries stay
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < F::kKSlots; ++s) {
+      mbar_init(k_full(s), 1);
+      mbar_init(k_empty(s), 1);
+    }
+    for (int s = 0; s < F::kQSlots; ++s) {
+      mbar_init(q_full(s), 1);
+      mbar_init(q_empty(s), 1);
+    }
+    for (int s = 0; s < kSBufs; ++s) {
+      mbar_init(s_full(s), 1);
+      mbar_init(s_empty(s), kSoftThreads / 32);
+    }
+    mbar_init(done_bar, 1);
+    *abort_flag = 0;
+    fence_barrier_init();
+    prefetch_tmap(&tmQ);
+    prefetch_tmap(&tmK);
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(tmem_slot), kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp == 0) {
+    if (nrt > 0 && elect_one()) {
+      // ---------------- TMA producer
+      auto load_q = [&](int rt, int slot) {
+        const int t0 = rt * queries;
+        const uint32_t dst = smem_u32(smem + F::kOffQ + slot * F::kTile);
+        if (!a.rows) {
+          mbar_arrive_expect_tx(q_full(slot), F::kHalves * queries * a.group * 128);
+#pragma unroll
+          for (int h = 0; h < F::kHalves; ++h)
+            tma_load_3d(dst + h * F::kBox, &tmQ, q_full(slot), h * 64, kvh * a.group, b * a.tokens + t0);
+          return;
+        }
+        const int nq = min(queries, count - t0);
+        mbar_arrive_expect_tx(q_full(slot), F::kHalves * nq * a.group * 128);
+        for (int i = 0; i < nq; ++i) {
+          const int q = min(max(a.rows[(int64_t)b * a.tokens + t0 + i], 0), a.tokens - 1);
+#pragma unroll
+          for (int h = 0; h < F::kHalves; ++h)
+            tma_load_3d(dst + h * F::kBox + i * a.group * 128, &tmQ, q_full(slot), h * 64, kvh * a.group, b * a.tokens + q);
+        }
+      };
+      int it = 0, kp = 0;
+      bool ok = true;
+      for (int kt = split; ok && kt < ktiles; kt += a.splits, ++kp) {
+        const int s = kp % F::kKSlots;
+        if (kp >= F::kKSlots && !mbar_wait_bounded(k_empty(s), ((kp / F::kKSlots) - 1) & 1, abort_flag, a.err)) break;
+        mbar_arrive_expect_tx(k_full(s), F::kTile);
+#pragma unroll
+        for (int h = 0; h < F::kHalves; ++h)
+          tma_load_3d(smem_u32(smem + s * F::kTile + h * F::kBox), &tmK, k_full(s), kvh * D + h * 64, kt * kKeys, b);
+        if (keep_q) {
+          if (kp == 0)
+            for (int rt = 0; rt < nrt; ++rt) load_q(rt, rt);
+          continue;
+        }
+        for (int rt = first_tile(kt); rt < nrt; ++rt, ++it) {
+          const int qs = it % F::kQSlots;
+          if (it >= F::kQSlots && !mbar_wait_bounded(q_empty(qs), ((it / F::kQSlots) - 1) & 1, abort_flag, a.err)) {
+            ok = false;
+            ++kp;  // its keys are on their way
+            break;
+          }
+          load_q(rt, qs);
+        }
+        if (!ok) break;
+      }
+      // let every load issued land before the CTA can exit
+      volatile int no_abort = 0;
+      for (int j = max(0, kp - F::kKSlots); j < kp; ++j)
+        mbar_wait_bounded(k_full(j % F::kKSlots), (j / F::kKSlots) & 1, &no_abort, nullptr);
+      const int nl = keep_q ? nrt : it;
+      for (int j = max(0, nl - F::kQSlots); j < nl; ++j)
+        mbar_wait_bounded(q_full(j % F::kQSlots), (j / F::kQSlots) & 1, &no_abort, nullptr);
+    }
+  } else if (warp == 1) {
+    if (nrt > 0 && elect_one()) {
+      // ---------------- MMA issuer
+      constexpr int bf = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
+      const uint64_t kd = smem_desc_sw128(smem_u32(smem)), qd = smem_desc_sw128(smem_u32(smem + F::kOffQ));
+      int it = 0, kp = 0;
+      bool ok = true;
+      for (int kt = split; ok && kt < ktiles; kt += a.splits, ++kp) {
+        const int s = kp % F::kKSlots;
+        if (!mbar_wait_bounded(k_full(s), (kp / F::kKSlots) & 1, abort_flag, a.err)) break;
+        for (int rt = first_tile(kt); ok && rt < nrt; ++rt, ++it) {
+          const int qs = keep_q ? rt : it % F::kQSlots, sb = it % kSBufs;
+          ok = mbar_wait_bounded(q_full(qs), keep_q ? 0 : (it / F::kQSlots) & 1, abort_flag, a.err) &&
+               (it < kSBufs || mbar_wait_bounded(s_empty(sb), ((it / kSBufs) - 1) & 1, abort_flag, a.err));
+          if (!ok) break;
+          tc_fence_after();
+          const int n = (min(queries, count - rt * queries) * a.group + 15) / 16 * 16;
+          const uint32_t idesc = idesc_f16(bf, 128, n);
+          const uint64_t kk = kd + (uint64_t)(s * (F::kTile >> 4)), qq = qd + (uint64_t)(qs * (F::kTile >> 4));
+#pragma unroll
+          for (int h = 0; h < F::kHalves; ++h)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              tc_mma_f16(tmem + (uint32_t)sb * 128u, kk + (uint64_t)(h * (F::kBox >> 4) + 2 * k),
+                         qq + (uint64_t)(h * (F::kBox >> 4) + 2 * k), idesc, (h | k) != 0);
+          tc_commit(s_full(sb));
+          if (!keep_q) tc_commit(q_empty(qs));
+        }
+        tc_commit(k_empty(s));
+      }
+      tc_commit(done_bar);  // every MMA issued must have finished before TMEM is freed
+      volatile int no_abort = 0;
+      mbar_wait_bounded(done_bar, 0, &no_abort, nullptr);
+    }
+  } else {
+    // ---------------- sums: warps 2..9, a key per thread and half of the rows
+    const int q4 = warp & 3, half = (warp - 2) >> 2, slot = q4 * 32 + lane;
+    const int aid = (warp - 2) * 32 + lane;
+    const uint32_t lane_off = (uint32_t)(q4 * 32) << 16;
+    auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory"); };
+    auto all_sync = [&]() { asm volatile("bar.sync 5, 256;" ::: "memory"); };
+    const int64_t at = ((int64_t)b * a.kv_heads + kvh) * a.max_seq;
+    // what thread aid < 128 brings of row aid of a tile of rows
+    float row_lse = INFINITY;
+    int row_lim = 0;
+    auto fetch = [&](int rt) {
+      const int r = rt * queries * a.group + aid, t = r / a.group;
+      row_lse = INFINITY;
+      row_lim = 0;
+      if (aid < queries * a.group && t < count) {
+        int q = t;
+        if (a.rows) {
+          q = a.rows[(int64_t)b * a.tokens + t];
+          if (q < 0 || q >= a.tokens) {
+            atomicExch(a.err, kDevErrBounds);
+            return;
+          }
+        }
+        row_lse = a.lse[((int64_t)b * a.heads + kvh * a.group + r % a.group) * a.tokens + q] * 1.4426950408889634f;
+        row_lim = visible_limit(a, len, count, t);
+      }
+    };
+    auto store = [&](int buf) {
+      if (aid < 128) {
+        lse2[buf * 128 + aid] = row_lse;
+        lim[buf * 128 + aid] = row_lim;
+      }
+    };
+    const bool one = nrt == 1;  // the rows' limits and sums stay
+    if (nrt > 0) {
+      fetch(first_tile(split));
+      store(0);
+      all_sync();
+    }
+    int it = 0, kp = 0;
+    bool ok = true;
+    for (int kt = split; kt < ktiles; kt += a.splits, ++kp) {
+      const int j = kt * kKeys + slot;
+      const float before = half == 0 && j < len && a.weights_in ? a.weights_in[at + j] : 0.f;
+      float sum = 0.f;
+      for (int rt = first_tile(kt); rt < nrt; ++rt, ++it) {
+        const int sb = it % kSBufs, buf = one ? 0 : it & 1;
+        const bool last = rt + 1 == nrt && kt + a.splits >= ktiles;
+        if (!one && !last) fetch(rt + 1 < nrt ? rt + 1 : first_tile(kt + a.splits));
+        ok = ok && mbar_wait_bounded(s_full(sb), (it / kSBufs) & 1, abort_flag, a.err);
+        ok = __all_sync(0xffffffffu, ok);
+        tc_fence_after();
+        if (ok) {
+          const int rows = min(queries, count - rt * queries) * a.group, nch = (rows + 15) / 16;
+          uint32_t s[4][16];
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (half + 2 * c < nch) tmem_ld_32x32b_x16(tmem + (uint32_t)sb * 128u + lane_off + (uint32_t)((half + 2 * c) * 16), s[c]);
+          tmem_ld_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(s_empty(sb));
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const int c0 = (half + 2 * c) * 16;
+            if (c0 >= rows) break;
+            const float* le = lse2 + buf * 128 + c0;
+            const int* li = lim + buf * 128 + c0;
+            const bool masked = kt * kKeys + kKeys > li[0] || c0 + 16 > rows;
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+              const float4 l4 = *reinterpret_cast<const float4*>(le + e);
+              const float ll[4] = {l4.x, l4.y, l4.z, l4.w};
+              float p[4];
+#pragma unroll
+              for (int u = 0; u < 4; ++u) p[u] = ex2(fmaf(__uint_as_float(s[c][e + u]), a.scale_log2, -ll[u]));
+              if (masked) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                  if (j >= li[e + u]) p[u] = 0.f;
+              }
+              sum += (p[0] + p[1]) + (p[2] + p[3]);
+            }
+          }
+        }
+        if (!one && !last) {
+          store(buf ^ 1);
+          all_sync();
+        }
+      }
+      float* x = xch + (kp & 1) * 128;
+      if (half == 1) x[slot] = sum;
+      pair_sync();
+      if (half == 0 && j < len && ok) a.weights[at + j] = before + (sum + x[slot]);
+    }
+    tc_fence_before();
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
 int done(cudaError_t e, const char* what) {
   if (e == cudaSuccess) e = cudaGetLastError();
   if (e != cudaSuccess) SN_FAIL(SWAPNET_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
@@ -611,7 +885,39 @@ template <typename T, int D> int rows_d(const CachedArgs& a, bool early, cudaStr
   return a.tokens * a.group <= 64 ? rows_t<T, D, 2>(a, early, s) : rows_t<T, D, 1>(a, early, s);
 }
 
+template <typename T, int D> int weights_t(const CachedArgs& a, bool early, cudaStream_t s) {
+  static std::atomic<uint64_t> known{0};
+  const auto kern = weights_rows_kernel<T, D>;
+  if (attr_needed(known)) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, WtCfg<D>::kSmem);
+    if (e != cudaSuccess) return done(e, "cache weights: shared memory");
+    attr_set(known);
+  }
+  const int queries = std::min(128 / a.group, a.tokens);
+  CUtensorMap q, k;
+  int rc = query_map(&q, a, a.rows ? 1 : queries);
+  if (!rc) rc = rows_map(&k, a, a.k, a.max_seq, a.kv_stride, a.seq_stride);
+  if (rc) return rc;
+  cudaLaunchConfig_t cfg;
+  std::memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = dim3(a.splits, a.kv_heads, a.n_seq);
+  cfg.blockDim = dim3(kTcThreads);
+  cfg.dynamicSmemBytes = WtCfg<D>::kSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = early ? 1 : 0;
+  return done(cudaLaunchKernelEx(&cfg, kern, q, k, a, queries), "cache weights launch");
+}
+
 }  // namespace
+
+int launch_weights_rows(const CachedArgs& a, bool early, cudaStream_t s) {
+  if (a.dtype == SWAPNET_BF16) return a.dim == 128 ? weights_t<__nv_bfloat16, 128>(a, early, s) : weights_t<__nv_bfloat16, 64>(a, early, s);
+  return a.dim == 128 ? weights_t<__half, 128>(a, early, s) : weights_t<__half, 64>(a, early, s);
+}
 
 int launch_attention_rows(const CachedArgs& a, bool early, cudaStream_t s) {
   if (a.dtype == SWAPNET_BF16)
