@@ -6,21 +6,24 @@
 // the key head, query-major: row t * group + h.  One CTA owns up to 128 rows
 // and a share of the key tiles (128 keys each; the drafted nodes are one more
 // tile, the last):
-//   S = Q K^T   tcgen05.mma, M 128 (rows) x N 128 (keys); Q, K and V by TMA
-//               (128-byte swizzle); S in two TMEM buffers, so that the next
-//               tile's S is computed during this tile's softmax
-//   P           warps 2..9, two threads per row: scores from TMEM, masks only
-//               in tiles that a limit crosses, p = 2^(s - m) back to TMEM as
-//               two parts of the storage type p_hi + p_lo (about 16 bits of p)
-//   O += P V    tcgen05.mma with A = P from TMEM, B = V as loaded (MN-major)
-// O stays in TMEM.  The exponent's reference m is the running maximum only
-// where that grew by more than 2^8 since it was last taken (kSlack): until
-// then p and l stay within 2^8 of their usual range, which fp32 sums and both
-// storage types hold without loss, and O is neither read nor rescaled.
-// With at most 64 rows (REP 2) the rows appear twice in the MMA's 128: lanes
-// 0..63 take the first 64 keys of a tile, lanes 64..127 the others, so that
-// all eight warps share the softmax; each half has its own m, l and O (the
-// other half's keys are zeros in its P), joined at the end.
+//   S = Q K^T     tcgen05.mma, M 128 (rows) x N 128 (keys); Q, K and V by TMA
+//                 (128-byte swizzle); S in two TMEM buffers, so that the next
+//                 tile's S is computed during this tile's softmax
+//   P             warps 2..9, two threads per row: one takes the first 64 keys
+//                 of every tile, the other the last 64, each with a softmax of
+//                 its own (reference m, sum l, output O_h), so no thread waits
+//                 for another.  Scores from TMEM, masks only in tiles that a
+//                 limit crosses, p = 2^(s - m) back over the scores as two
+//                 parts of the storage type p_hi + p_lo (about 16 bits of p)
+//   O_h += P_h V  tcgen05.mma with A = P from TMEM, B = V as loaded (MN-major)
+// O_0 and O_1 stay in TMEM.  m is the running maximum only where that grew by
+// more than 2^8 since it was last taken (kSlack): until then p and l stay
+// within 2^8 of their usual range, which fp32 sums and both storage types hold
+// without loss, and O is neither read nor rescaled.  At the end the two
+// halves' results are joined in shared memory.
+// With at most 64 rows (REP 2) the rows appear twice in the MMA's 128, and
+// lanes 0..63 and 64..127 share a half's keys, so that all eight warps work
+// (the other 32 keys are zeros in a lane's P).
 // K and V tiles pass through one ring in the order they are used.  Every wait
 // is bounded: on timeout the kernel records kDevErrTimeout, drains the loads
 // and MMAs it started, frees TMEM and returns.
@@ -42,7 +45,9 @@ constexpr int kTcThreads = 64 + kSoftThreads;
 constexpr int kKeys = 128;       // keys of a tile
 constexpr float kSlack = 8.0f;   // log2 of what p may exceed 1 by
 constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kTmO = 256, kTmPhi = 384, kTmPlo = 448;  // S: [0, 128) and [128, 256)
+// TMEM columns: S [0, 128) and [128, 256), each half's P over its scores (hi
+// then lo); O_0 [256, 256 + D), O_1 [384, 384 + D)
+constexpr uint32_t kTmO = 256;
 
 template <int D> struct TcCfg {
   static constexpr int kHalves = D / 64;             // 64-dim boxes of a tile
@@ -51,13 +56,14 @@ template <int D> struct TcCfg {
   static constexpr int kSlots = D == 128 ? 5 : 8;
   static constexpr int kOffQ = 0;
   static constexpr int kOffRing = kTile;
-  static constexpr int kOffX = kOffRing + kSlots * kTile;   // exchange [2][2][128] floats
-  static constexpr int kOffPar = kOffX + 2 * 2 * 128 * 4;   // parents
-  static constexpr int kOffOdd = kOffPar + kTreeMax * 4;    // odd value rows [4], p of one key [128]
-  static constexpr int kOffBar = kOffOdd + 16 + 128 * 4;
+  static constexpr int kOffX = kOffRing + kSlots * kTile;   // (m, l) of every thread
+  static constexpr int kOffPar = kOffX + 256 * 8;           // parents
+  static constexpr int kOffOdd = kOffPar + kTreeMax * 4;    // odd value rows, a bit each
+  static constexpr int kOffBar = kOffOdd + 16;
   static constexpr int kSmem = kOffBar + 256 + 1024;        // + alignment slack
   static_assert(kSmem <= 232448, "shared memory of a CTA");
-  static_assert(kSlots * kTile >= 128 * (D + 4) * 4, "the rows' outputs overlay the ring");
+  static constexpr int kORow = D + 4;                       // floats of a thread's output row
+  static_assert(kSlots * kTile >= 256 * kORow * 4, "the threads' outputs overlay the ring");
 };
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, uint32_t bar, int x, int y, int z) {
@@ -106,18 +112,18 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   constexpr int NK = 64 / REP;  // keys per thread and tile
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  float* xch = reinterpret_cast<float*>(smem + F::kOffX);
+  float2* ml = reinterpret_cast<float2*>(smem + F::kOffX);
   int* par = reinterpret_cast<int*>(smem + F::kOffPar);
   uint32_t* odd_rows = reinterpret_cast<uint32_t*>(smem + F::kOffOdd);
-  float* odd_p = reinterpret_cast<float*>(smem + F::kOffOdd + 16);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + F::kOffBar);
   auto full = [&](int s) { return smem_u32(bars + s); };
   auto empty = [&](int s) { return smem_u32(bars + 8 + s); };
   auto s_full = [&](int i) { return smem_u32(bars + 16 + i); };
-  const uint32_t q_full = smem_u32(bars + 18), p_full = smem_u32(bars + 19), o_full = smem_u32(bars + 20),
-                 done_bar = smem_u32(bars + 21);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 22);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 23);
+  auto p_full = [&](int h) { return smem_u32(bars + 18 + h); };
+  auto o_full = [&](int h) { return smem_u32(bars + 20 + h); };
+  const uint32_t q_full = smem_u32(bars + 22), done_bar = smem_u32(bars + 23);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 24);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 25);
 
   const int warp = warp_index(), lane = threadIdx.x & 31;
   const int split = (int)blockIdx.x % a.splits, t0 = (int)(blockIdx.x / a.splits) * queries;
@@ -154,8 +160,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     mbar_init(s_full(0), 1);
     mbar_init(s_full(1), 1);
     mbar_init(q_full, 1);
-    mbar_init(p_full, 32 * soft_warps);
-    mbar_init(o_full, 1);
+    for (int h = 0; h < 2; ++h) {
+      mbar_init(p_full(h), soft_warps / 2);
+      mbar_init(o_full(h), 1);
+    }
     mbar_init(done_bar, 1);
     *abort_flag = 0;
 #pragma unroll
@@ -238,16 +246,20 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         if (i + 1 < n && !scores(i + 1)) break;
         const int pos = v_pos(i), s = pos % F::kSlots;
         if (!mbar_wait_bounded(full(s), (pos / F::kSlots) & 1, abort_flag, a.err)) break;
-        if (!mbar_wait_bounded(p_full, i & 1, abort_flag, a.err)) break;
-        tc_fence_after();
         const uint64_t vt = vd + (uint64_t)(s * (F::kTile >> 4));
+        for (int h = 0; ok && h < 2; ++h) {
+          ok = mbar_wait_bounded(p_full(h), i & 1, abort_flag, a.err);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t pt = tmem + (uint32_t)(i & 1) * 128u + (uint32_t)h * 64u;
 #pragma unroll
-        for (int part = 0; part < 2; ++part)
+          for (int part = 0; part < 2; ++part)
 #pragma unroll
-          for (int ks = 0; ks < 8; ++ks)  // 16 keys a step
-            tc_mma_f16_ta(tmem + kTmO, tmem + (part ? kTmPlo : kTmPhi) + (uint32_t)(ks * 8), vt + (uint64_t)(ks * (2048 >> 4)),
-                          idesc_pv, (uint32_t)(i | part | ks) != 0);
-        tc_commit(o_full);
+            for (int ks = 0; ks < 4; ++ks)  // 16 keys a step
+              tc_mma_f16_ta(tmem + kTmO + (uint32_t)h * 128u, pt + (uint32_t)(part * 32 + ks * 8),
+                            vt + (uint64_t)((h * 4 + ks) * (2048 >> 4)), idesc_pv, (uint32_t)(i | part | ks) != 0);
+          tc_commit(o_full(h));
+        }
         tc_commit(empty(s));
       }
       // every MMA issued must have finished before TMEM is freed
@@ -262,37 +274,27 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     const int active = 32 * soft_warps, aid = (half * (soft_warps / 2) + q4) * 32 + lane;
     const int t = t0 + min(row, rows - 1) / a.group;
     const int lim = visible_limit(a, len, count, t);
-    const int kofs = rep * (128 / REP) + half * NK;
+    const int kofs = half * 64 + rep * NK;  // this thread's first key of a tile
     const uint32_t lane_off = (uint32_t)(q4 * 32) << 16;
-    // the two warps of a row quarter meet here; both take part in every
-    // tile's exchange, also after a timeout
-    auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory"); };
+    const uint32_t tO = tmem + kTmO + (uint32_t)half * 128u + lane_off;
     auto all_sync = [&]() { asm volatile("bar.sync 5, %0;" ::"r"(active) : "memory"); };
-    if (REP == 2 && n > 0) {  // the keys of the other half of the lanes stay zeros in P
-      uint32_t z[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) z[i] = 0;
-#pragma unroll
-      for (int c = 0; c < 64; c += 16) tmem_st_x16(tmem + lane_off + (half ? kTmPlo : kTmPhi) + (uint32_t)c, z);
-      tmem_st_wait();
-      pair_sync();
-    }
     float m = -INFINITY, l = 0.f;  // m: the reference, in log2 units
     bool ok = true;
     for (int i = 0; i < n; ++i) {
       const bool nw = i0 + i >= np;
       const int k0 = nw ? 0 : (i0 + i) * kKeys;
       const bool masked = nw || k0 + kKeys > lim_min;  // some of these keys are hidden from some rows
+      const uint32_t tS = tmem + (uint32_t)(i & 1) * 128u + lane_off;
       ok = ok && mbar_wait_bounded(s_full(i & 1), (i >> 1) & 1, abort_flag, a.err);
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
-      uint32_t s[NK];
-      float mx = -INFINITY;
+      uint32_t hi[NK / 2], lo[NK / 2];
       if (ok) {
+        uint32_t s[NK];
 #pragma unroll
         for (int c = 0; c < NK; c += 32) {
           uint32_t(&r)[32] = *reinterpret_cast<uint32_t(*)[32]>(s + c);
-          tmem_ld_32x32b_x32(tmem + (uint32_t)(i & 1) * 128u + lane_off + (uint32_t)(kofs + c), r);
+          tmem_ld_32x32b_x32(tS + (uint32_t)(kofs + c), r);
         }
         tmem_ld_wait();
         if (masked) {
@@ -314,61 +316,58 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           for (int k = 0; k < NK; ++k)
             if (!(see[k >> 5] >> (k & 31) & 1u)) s[k] = 0xff800000u;  // -inf
         }
+        float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int k = 0; k < NK; ++k) mx = fmaxf(mx, __uint_as_float(s[k]));
-      }
-      float* x = xch + (i & 1) * 256;
-      x[half * 128 + slot] = mx;
-      pair_sync();
-      mx = fmaxf(mx, x[(half ^ 1) * 128 + slot]) * a.scale_log2;
-      const bool grow = mx - m > kSlack;  // (also the first key seen)
-      float alpha = 1.f;
-      if (grow) {
-        alpha = ex2(m - mx);
-        m = mx;
-        l *= alpha;
-      }
-      const float base = m == -INFINITY ? 0.f : m;
-      uint32_t hi[NK / 2], lo[NK / 2];
-      if (ok) {
-        float sum = 0.f;
+        for (int k = 0; k < NK; ++k) mx4[k & 3] = fmaxf(mx4[k & 3], __uint_as_float(s[k]));
+        const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * a.scale_log2;
+        const bool grow = mx - m > kSlack;  // (also the first key seen)
+        if (__any_sync(0xffffffffu, grow)) {
+          float alpha = 1.f;
+          if (grow) {
+            alpha = ex2(m - mx);
+            m = mx;
+            l *= alpha;
+          }
+          if (i > 0) {  // O is at rest once the product of the tile before is done
+            ok = mbar_wait_bounded(o_full(half), (i - 1) & 1, abort_flag, a.err);
+            ok = __all_sync(0xffffffffu, ok);
+            tc_fence_after();
+            if (ok) {
+#pragma unroll
+              for (int c = 0; c < D; c += 16) {
+                uint32_t r[16];
+                tmem_ld_32x32b_x16(tO + (uint32_t)c, r);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * alpha);
+                tmem_st_x16(tO + (uint32_t)c, r);
+              }
+            }
+          }
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+        float sum4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < NK / 2; ++k) {
           const float p0 = ex2(fmaf(__uint_as_float(s[2 * k]), a.scale_log2, -base));
           const float p1 = ex2(fmaf(__uint_as_float(s[2 * k + 1]), a.scale_log2, -base));
-          sum += p0;
-          sum += p1;
+          sum4[2 * (k & 1)] += p0;
+          sum4[2 * (k & 1) + 1] += p1;
           hi[k] = pack_pair<T>(p0, p1);
           const float2 back = unpack_pair<T>(hi[k]);
           lo[k] = pack_pair<T>(p0 - back.x, p1 - back.y);
         }
-        l += sum;
+        l += (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
       }
-      if (i > 0) {  // P and O are free once the product of the tile before is done
-        ok = ok && mbar_wait_bounded(o_full, (i - 1) & 1, abort_flag, a.err);
-        ok = __all_sync(0xffffffffu, ok);
-        tc_fence_after();
-        if (ok && __any_sync(0xffffffffu, grow)) {
-#pragma unroll
-          for (int c = 0; c < D / 2; c += 16) {
-            uint32_t r[16];
-            const uint32_t at = tmem + kTmO + lane_off + (uint32_t)(half * (D / 2) + c);
-            tmem_ld_32x32b_x16(at, r);
-            tmem_ld_wait();
-#pragma unroll
-            for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * alpha);
-            tmem_st_x16(at, r);
-          }
-        }
-      }
-      uint32_t odd[4] = {0u, 0u, 0u, 0u};
-      uint8_t* vs = smem + F::kOffRing + (v_pos(i) % F::kSlots) * F::kTile;
+      uint32_t odd = 0;
       if (masked) {
         // A value row that some of the rows do not see must not reach them
         // even if it is infinite or not a number (0 x inf): rows behind the
         // last key are cleared, others that hold such a value as well, and
         // added by hand below where they are seen.
-        ok = ok && mbar_wait_bounded(full(v_pos(i) % F::kSlots), (v_pos(i) / F::kSlots) & 1, abort_flag, a.err);
+        const int pos = v_pos(i);
+        uint8_t* vs = smem + F::kOffRing + (pos % F::kSlots) * F::kTile;
+        ok = ok && mbar_wait_bounded(full(pos % F::kSlots), (pos / F::kSlots) & 1, abort_flag, a.err);
         ok = __all_sync(0xffffffffu, ok);
         const int have = min(kKeys, nw ? count : len - k0);
         auto chunk = [&](int r, int c) {
@@ -387,155 +386,138 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           }
         }
         all_sync();
-#pragma unroll
-        for (int w = 0; w < 4; ++w) odd[w] = odd_rows[w];
-        if (odd[0] | odd[1] | odd[2] | odd[3]) {
+        odd = odd_rows[0] | odd_rows[1] | odd_rows[2] | odd_rows[3];
+        if (odd) {
           for (int c = aid; c < kKeys * (D / 8); c += active) {
             const int r = c / (D / 8);
             if (odd_rows[r >> 5] >> (r & 31) & 1u) *chunk(r, c % (D / 8)) = make_uint4(0u, 0u, 0u, 0u);
           }
         }
         fence_proxy_async_smem();  // V is read by the tensor cores (async proxy)
+        all_sync();                // by either half's product
       }
       if (ok) {
+        // over the half's 64 scores: hi parts of its 64 keys, then the lo parts
 #pragma unroll
-        for (int c = 0; c < NK / 2; c += 16) {
-          tmem_st_x16(tmem + kTmPhi + lane_off + (uint32_t)(kofs / 2 + c), hi + c);
-          tmem_st_x16(tmem + kTmPlo + lane_off + (uint32_t)(kofs / 2 + c), lo + c);
+        for (int part = 0; part < 2; ++part) {
+          const uint32_t* x = part ? lo : hi;
+          const uint32_t to = tS + (uint32_t)(half * 64 + part * 32);
+          if (REP == 1) {
+            tmem_st_x16(to, x);
+            tmem_st_x16(to + 16u, x + (NK / 2 - 16));
+          } else {
+            uint32_t z[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) z[e] = 0;
+            tmem_st_x16(to + (uint32_t)rep * 16u, x);
+            tmem_st_x16(to + (uint32_t)(rep ^ 1) * 16u, z);
+          }
         }
         tmem_st_wait();
+        // Not before the product of the tile before is done: the barrier
+        // counts one tile at a time, and the scores of the next one are there
+        // early (a half two tiles ahead of the products would be waited for
+        // in the wrong phase).
+        if (i > 0) {
+          ok = mbar_wait_bounded(o_full(half), (i - 1) & 1, abort_flag, a.err);
+          ok = __all_sync(0xffffffffu, ok);
+        }
         tc_fence_before();
-        mbar_arrive(p_full);
+        __syncwarp();
+        if (lane == 0 && ok) mbar_arrive(p_full(half));
       }
-      if (odd[0] | odd[1] | odd[2] | odd[3]) {
-        ok = ok && mbar_wait_bounded(o_full, i & 1, abort_flag, a.err);
+      if (odd) {
+        ok = ok && mbar_wait_bounded(o_full(half), i & 1, abort_flag, a.err);
         ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
         for (int j = 0; j < kKeys; ++j) {
           if (!(odd_rows[j >> 5] >> (j & 31) & 1u)) continue;
           const int rel = j - kofs;
-          if (rel >= 0 && rel < NK) {
-            float pj = 0.f;
+          if (rel < 0 || rel >= NK || !ok) continue;  // (the same for all lanes of a warp)
+          float pj = 0.f;
 #pragma unroll
-            for (int k = 0; k < NK / 2; ++k) {
-              const float2 h2 = unpack_pair<T>(hi[k]), l2 = unpack_pair<T>(lo[k]);
-              if (rel == 2 * k) pj = h2.x + l2.x;
-              if (rel == 2 * k + 1) pj = h2.y + l2.y;
-            }
-            odd_p[slot] = pj;
-          } else if (half == 0 && (REP == 2 && j / kRowsMax != rep)) {
-            odd_p[slot] = 0.f;
+          for (int k = 0; k < NK / 2; ++k) {
+            const float2 h2 = unpack_pair<T>(hi[k]), l2 = unpack_pair<T>(lo[k]);
+            if (rel == 2 * k) pj = h2.x + l2.x;
+            if (rel == 2 * k + 1) pj = h2.y + l2.y;
           }
-          pair_sync();
-          const float pj = odd_p[slot];
           const T* v = nw ? static_cast<const T*>(a.v_new) + ((int64_t)b * a.tokens + j) * a.new_stride
                           : static_cast<const T*>(a.v) + (int64_t)b * a.seq_stride + (int64_t)(k0 + j) * a.kv_stride;
-          v += kvh * D + half * (D / 2);
-          if (ok) {
-            for (int c = 0; c < D / 2; c += 16) {
-              uint32_t r[16];
-              const uint32_t at = tmem + kTmO + lane_off + (uint32_t)(half * (D / 2) + c);
-              tmem_ld_32x32b_x16(at, r);
-              tmem_ld_wait();
+          v += kvh * D;
+          for (int c = 0; c < D; c += 16) {
+            uint32_t r[16];
+            tmem_ld_32x32b_x16(tO + (uint32_t)c, r);
+            tmem_ld_wait();
 #pragma unroll
-              for (int e = 0; e < 16; ++e)
-                if (pj != 0.f) r[e] = __float_as_uint(fmaf(pj, to_f<T>(v[c + e]), __uint_as_float(r[e])));
-              tmem_st_x16(at, r);
-              tmem_st_wait();
-            }
+            for (int e = 0; e < 16; ++e)
+              if (pj != 0.f) r[e] = __float_as_uint(fmaf(pj, to_f<T>(v[c + e]), __uint_as_float(r[e])));
+            tmem_st_x16(tO + (uint32_t)c, r);
+            tmem_st_wait();
           }
-          pair_sync();
         }
         all_sync();  // everyone has read the odd rows
         if (aid < 4) odd_rows[aid] = 0;
         all_sync();
       }
     }
-    // ---- the rows' results
-    const int64_t first = (((int64_t)b * a.kv_heads + kvh) * a.splits + split) * a.tokens * a.group + (int64_t)t0 * a.group;
-    auto emit = [&](int r, int c, const float* o, int cols, float L) {  // cols: a multiple of 4
-      if (a.splits > 1) {
-        float4* to = reinterpret_cast<float4*>(a.part + (first + r) * D + c);
-        for (int e = 0; e < cols / 4; ++e) to[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
-        return;
-      }
-      const float inv = L > 0.f ? 1.0f / L : (L == 0.f ? 0.f : L);  // (a NaN stays one)
-      T* to = static_cast<T*>(a.out) + ((int64_t)b * a.tokens + t0 + r / a.group) * a.out_stride +
-              (int64_t)(kvh * a.group + r % a.group) * D + c;
-      for (int e = 0; e < cols / 4; ++e)
-        reinterpret_cast<uint2*>(to)[e] =
-            make_uint2(pack_pair<T>(o[4 * e] * inv, o[4 * e + 1] * inv), pack_pair<T>(o[4 * e + 2] * inv, o[4 * e + 3] * inv));
-    };
-    auto emit_stats = [&](int r, float M, float L) {
-      if (a.splits > 1)
-        reinterpret_cast<float2*>(a.ml)[first + r] = make_float2(M, L);
-      else if (a.lse)
-        a.lse[((int64_t)b * a.heads + kvh * a.group + r % a.group) * a.tokens + t0 + r / a.group] =
-            L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
-    };
-    if (n > 0) {
-      ok = ok && mbar_wait_bounded(o_full, (n - 1) & 1, abort_flag, a.err);
+    // ---- the rows' results: the 2 REP softmaxes of a row meet in shared
+    // memory (every load and product of the ring has ended)
+    if (n > 0) {  // (the products before these two are done: the wait above, and their order)
+      for (int h = 0; h < 2; ++h) ok = ok && mbar_wait_bounded(o_full(h), (n - 1) & 1, abort_flag, a.err);
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
     }
-    float* x = xch + (n & 1) * 256;  // (the other buffer may still be read)
-    x[half * 128 + slot] = l;
-    pair_sync();
-    const float L = x[slot] + x[128 + slot];
-    if (REP == 1) {
-      for (int c = 0; c < D / 2; c += 16) {
-        float o[16];
-        uint32_t r[16];
+    float* ov = reinterpret_cast<float*>(smem + F::kOffRing);
+    if (n > 0 && ok) {
+#pragma unroll
+      for (int c = 0; c < D; c += 32) {
+        uint32_t r[32];
+        tmem_ld_32x32b_x32(tO + (uint32_t)c, r);
+        tmem_ld_wait();
+        float4* to = reinterpret_cast<float4*>(ov + (half * 128 + slot) * F::kORow + c);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          to[e] = make_float4(__uint_as_float(r[4 * e]), __uint_as_float(r[4 * e + 1]), __uint_as_float(r[4 * e + 2]),
+                              __uint_as_float(r[4 * e + 3]));
+      }
+    }
+    ml[half * 128 + slot] = make_float2(m, l);
+    all_sync();
+    const int64_t first = (((int64_t)b * a.kv_heads + kvh) * a.splits + split) * a.tokens * a.group + (int64_t)t0 * a.group;
+    for (int c = aid; ok && c < rows * (D / 4); c += active) {
+      const int r = c / (D / 4), col = c % (D / 4) * 4;
+      float2 st[2 * REP];
+      float M = -INFINITY, L = 0.f;
+#pragma unroll
+      for (int u = 0; u < 2 * REP; ++u) {
+        st[u] = ml[u * kRowsMax + r];  // (half-major, then the copies of the rows)
+        M = fmaxf(M, st[u].x);
+      }
+      const float base = M == -INFINITY ? 0.f : M;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int u = 0; u < 2 * REP; ++u) {
+        const float f = ex2(st[u].x - base);  // 0 where no key was seen
+        L = fmaf(st[u].y, f, L);
         if (n > 0) {
-          tmem_ld_32x32b_x16(tmem + kTmO + lane_off + (uint32_t)(half * (D / 2) + c), r);
-          tmem_ld_wait();
-        }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[e] = n > 0 ? __uint_as_float(r[e]) : 0.f;
-        if (ok && row < rows && (n > 0 || a.splits == 1)) emit(row, half * (D / 2) + c, o, 16, L);
-      }
-      if (ok && half == 0 && row < rows) emit_stats(row, m, L);
-    } else {
-      float* ov = reinterpret_cast<float*>(smem + F::kOffRing);  // [128][D + 4]: every load and product has ended
-      if (n > 0 && ok) {
-        for (int c = 0; c < D / 2; c += 16) {
-          uint32_t r[16];
-          tmem_ld_32x32b_x16(tmem + kTmO + lane_off + (uint32_t)(half * (D / 2) + c), r);
-          tmem_ld_wait();
-          float4* to = reinterpret_cast<float4*>(ov + slot * (D + 4) + half * (D / 2) + c);
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            to[e] = make_float4(__uint_as_float(r[4 * e]), __uint_as_float(r[4 * e + 1]), __uint_as_float(r[4 * e + 2]),
-                                __uint_as_float(r[4 * e + 3]));
+          const float4 x = *reinterpret_cast<const float4*>(ov + (u * kRowsMax + r) * F::kORow + col);
+          o.x = fmaf(x.x, f, o.x);
+          o.y = fmaf(x.y, f, o.y);
+          o.z = fmaf(x.z, f, o.z);
+          o.w = fmaf(x.w, f, o.w);
         }
       }
-      float* y = xch + ((n + 1) & 1) * 256;
-      pair_sync();  // (that buffer's last readers have passed)
-      if (half == 0) {
-        y[slot] = m;
-        y[128 + slot] = L;
+      if (a.splits > 1) {
+        if (n > 0) *reinterpret_cast<float4*>(a.part + (first + r) * D + col) = o;
+        if (col == 0) reinterpret_cast<float2*>(a.ml)[first + r] = make_float2(M, L);
+        continue;
       }
-      all_sync();
-      if (ok) {
-        for (int c = aid; c < rows * (D / 4); c += active) {
-          const int r = c / (D / 4), col = c % (D / 4) * 4;
-          const float m0 = y[r], m1 = y[64 + r], M = fmaxf(m0, m1), base = M == -INFINITY ? 0.f : M;
-          const float f0 = ex2(m0 - base), f1 = ex2(m1 - base);
-          const float LL = fmaf(y[128 + r], f0, y[192 + r] * f1);
-          float o[4] = {0.f, 0.f, 0.f, 0.f};
-          if (n > 0) {
-            const float4 u = *reinterpret_cast<const float4*>(ov + r * (D + 4) + col);
-            const float4 w = *reinterpret_cast<const float4*>(ov + (64 + r) * (D + 4) + col);
-            // (a half that saw no key holds zeros, and its factor is zero)
-            o[0] = fmaf(u.x, f0, w.x * f1);
-            o[1] = fmaf(u.y, f0, w.y * f1);
-            o[2] = fmaf(u.z, f0, w.z * f1);
-            o[3] = fmaf(u.w, f0, w.w * f1);
-          }
-          if (n > 0 || a.splits == 1) emit(r, col, o, 4, LL);
-          if (col == 0) emit_stats(r, M, LL);
-        }
-      }
+      const float inv = L > 0.f ? 1.0f / L : (L == 0.f ? 0.f : L);  // (a NaN stays one)
+      const int tq = t0 + r / a.group, hd = kvh * a.group + r % a.group;
+      T* to = static_cast<T*>(a.out) + ((int64_t)b * a.tokens + tq) * a.out_stride + (int64_t)hd * D + col;
+      *reinterpret_cast<uint2*>(to) = make_uint2(pack_pair<T>(o.x * inv, o.y * inv), pack_pair<T>(o.z * inv, o.w * inv));
+      if (col == 0 && a.lse)
+        a.lse[((int64_t)b * a.heads + hd) * a.tokens + tq] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
     }
     tc_fence_before();
   }

@@ -228,6 +228,35 @@ def test_long_cache_is_split(tokens):
     Case("f16", 2, tokens, 8, 2, 128, 9000, [8999, 30], draft=False, weigh=True, seed=9).run().check()
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("tokens", [12, 20])
+def test_many_sequences_with_many_tiles_each(dim, tokens):
+    """Enough sequences that each CTA passes dozens of key tiles, of caches that DRAM has to deliver."""
+    torch = _torch()
+    rng = np.random.default_rng(1)
+    n, cap = 40, 4224
+    lens = rng.integers(3900, cap + 1, size=n)
+    eng = _any_engine()
+    for draft in (True, False):
+        c = Case("bf16", n, tokens, 32, 8, dim, cap, lens, draft=draft, weigh=not draft, seed=5, poison=False).run()
+        eng.sync()  # no wait gave up
+        full, t = c.lens.copy(), tokens
+        for b in (0, 17, n - 1):
+            one = Case.__new__(Case)
+            one.__dict__.update(c.__dict__)
+            one.shape = (1,) + c.shape[1:]
+            one.lens = full[b:b + 1]
+            for x in ("k", "v", "win"):
+                setattr(one, x, None if getattr(c, x) is None else getattr(c, x)[b:b + 1])
+            for x in ("q", "kn", "vn", "out"):
+                setattr(one, x, None if getattr(c, x) is None else getattr(c, x)[b * t:(b + 1) * t])
+            one.par = None if c.par is None else c.par[b:b + 1]
+            one.lse = c.lse[b:b + 1]
+            one.w = None if c.w is None else c.w[b:b + 1]
+            one.check()
+    torch.cuda.synchronize()
+
+
 @pytest.mark.parametrize("draft", [False, True])
 def test_strides_and_streams(draft):
     torch = _torch()
