@@ -84,6 +84,15 @@ typedef enum swapnet_act {
 } swapnet_act;
 
 #define SWAPNET_LAYER_NO_BIAS 1 /* flags: a linear layer without bias tensor */
+/* Flags of ATTENTION layers, the same on every one of a model, whose attention
+ * layers then have one shape (head width 128).  The paper has no counterpart.
+ * TREE: the input tokens are the nodes of a drafted tree (at most 128), each
+ * attending to the cache and its ancestors; their keys and values stay beside
+ * the caches until swapnet_engine_tree_accept.
+ * WEIGHTS: the attention that each cached row gets is added up in the state,
+ * for swapnet_engine_evict. */
+#define SWAPNET_ATTENTION_TREE 2
+#define SWAPNET_ATTENTION_WEIGHTS 4
 
 #define SWAPNET_SRC_INPUT (-1) /* the model input                       */
 #define SWAPNET_SRC_NONE (-2)  /* unused producer / no residual operand */
@@ -102,7 +111,7 @@ typedef struct swapnet_layer {
   int32_t cout;     /* conv: output channels; linear: output features           */
   int32_t kh, kw, stride, pad; /* conv and maxpool window                      */
   int32_t is_output;/* nonzero: a model output, written to the output buffer   */
-  int32_t flags;    /* SWAPNET_LAYER_NO_BIAS                                   */
+  int32_t flags;    /* SWAPNET_LAYER_NO_BIAS, SWAPNET_ATTENTION_*              */
   int64_t t_ex_ns;  /* measured execution delay; 0 = gamma * FLOPs (Sec. 6.1)  */
   int32_t src2;     /* ATTENTION: the values layer                             */
   int32_t heads;    /* ATTENTION: heads (head width = cout / heads)            */
@@ -479,6 +488,47 @@ int swapnet_engine_adapt(swapnet_engine* eng, const swapnet_plan* plan);
  * Must be bound before the first swapnet_infer of such a model. */
 int swapnet_engine_bind_state(swapnet_engine* eng, void* d_state, uint64_t state_bytes);
 
+/* What else a state holds: byte offsets from its start, 0 = not there.  The
+ * header's int32 words: [0] the rows in use (the position above), [1] with
+ * WEIGHTS the rows evicted so far (a token's rotation is that of position
+ * [0] + [1]), [2] scratch, [3] and [4] with TREE results of the last swapnet_engine_tree_accept: accepted nodes and the
+ * model's choice at the last one.
+ * Engines that share a state are built from the same layers with the same
+ * SWAPNET_ATTENTION_WEIGHTS flag; the offsets up to `weights` are the same for
+ * them, what lies behind serves one engine's pass at a time. */
+typedef struct swapnet_state_layout {
+  uint64_t caches;       /* key cache of the first ATTENTION layer              */
+  uint64_t cache_bytes;  /* of one cache: key and value caches follow one another,
+                            layer by layer (0: the layers differ)               */
+  uint64_t weights;      /* WEIGHTS: float [layers][heads][max_seq]             */
+  uint64_t tree_count;   /* TREE: int32 nodes in use                            */
+  uint64_t tree_parents; /* TREE: int32 [tokens], as in swapnet_cached_attention */
+  uint64_t tree_path;    /* TREE: int32 [tokens] the accepted nodes, -1 behind  */
+  uint32_t layers;       /* ATTENTION layers                                    */
+  uint32_t reserved;
+} swapnet_state_layout;
+int swapnet_plan_state_layout(const swapnet_plan* plan, swapnet_state_layout* layout);
+
+/* Greedy decoding with drafted trees (TREE models).  Before each inference the
+ * caller writes the tree (tree_count, tree_parents) into the state, on the same
+ * stream; node 0 is the token the last pass chose and the input holds the
+ * nodes' ids.  The inference does not advance the position.  This call walks
+ * the tree as swapnet_tree_accept does, with d_targets the inference's ARGMAX
+ * output, appends the accepted nodes' rows to every layer's caches, with
+ * WEIGHTS adds their attention to the weights, advances the position by their
+ * number and leaves path, accepted and next in the state.  No room for the
+ * path: nothing is accepted (accepted = 0), reported by swapnet_engine_sync.
+ * Asynchronous on `stream`; no other engine may run on the state in between.
+ * Errors: INVALID_ARG (no TREE model, no state), CUDA. */
+int swapnet_engine_tree_accept(swapnet_engine* eng, const int32_t* d_ids, const int32_t* d_targets, swapnet_stream stream);
+
+/* Eviction in the bound state of a WEIGHTS model: in every layer and head the
+ * cache keeps min(position, keep) rows as swapnet_cache_evict does, the
+ * position becomes that number, and the evicted rows are counted in the header
+ * so that later tokens keep their rotation.  Asynchronous on `stream`.
+ * Errors: INVALID_ARG (no WEIGHTS model, no state, bad numbers), CUDA. */
+int swapnet_engine_evict(swapnet_engine* eng, int32_t keep, int32_t recent, int32_t sink, swapnet_stream stream);
+
 typedef struct swapnet_engine_block {
   int32_t variant;       /* swapnet_swap_variant chosen for the block     */
   int32_t n_segments;    /* contiguous host->arena copies per swap-in     */
@@ -754,8 +804,9 @@ int swapnet_attention_weights(const swapnet_cached_attention* args, swapnet_stre
  * first `sink`, the last `recent` and those of the largest weights (NaN
  * counts as the largest; among equal ones the lower row), in row order.  kept
  * gets the rows kept, k_out / v_out / weights_out their contents in rows
- * 0 .. min(lens, keep) - 1, lens_out their number.  What lies behind is left
- * as it was.  All three may be the inputs themselves (in place, one layout
+ * 0 .. min(lens, keep) - 1, lens_out their number.  weights_out is 0 from there
+ * up to row lens (a row appended later starts from nothing); what else lies
+ * behind is left as it was.  All three may be the inputs themselves (in place, one layout
  * for both); otherwise they must not overlap them.  Keys keep the rotation of
  * the position they were written at.  head_dim: any multiple of 8 up to 512.
  * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA. */

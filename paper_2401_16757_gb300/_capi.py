@@ -23,6 +23,7 @@ OP = {"linear": 1, "conv": 2, "maxpool": 3, "gap": 4, "upsample2x": 5, "concat":
 ACT = {"none": 0, "relu": 1, "leaky": 2, "swiglu": 3}
 DTYPE = {"f32": F32, "f16": F16, "bf16": BF16, "i32": I32}
 LAYER_NO_BIAS = 1
+ATTENTION_TREE, ATTENTION_WEIGHTS = 2, 4
 SWAP_AUTO, SWAP_MEMCPY, SWAP_ZEROCOPY, SWAP_DIRECT, SWAP_PACKED = 0, 1, 2, 3, 4
 SRC_INPUT, SRC_NONE = -1, -2
 
@@ -92,6 +93,11 @@ class EngineBlock(C.Structure):
                 ("zerocopy_us", C.c_float)]
 
 
+class StateLayout(C.Structure):
+    _fields_ = [(n, C.c_uint64) for n in ("caches", "cache_bytes", "weights", "tree_count", "tree_parents", "tree_path")] + \
+        [("layers", C.c_uint32), ("reserved", C.c_uint32)]
+
+
 class CachedAttention(C.Structure):
     """swapnet_cached_attention; pointers are device addresses as integers."""
     _fields_ = [(n, C.c_int32) for n in ("dtype", "n_seq", "tokens", "heads", "kv_heads", "head_dim", "max_seq")] + \
@@ -129,7 +135,8 @@ EXPORTS = ["swapnet_default_options", "swapnet_partition", "swapnet_plan_from_cu
            "swapnet_weights_file_read", "swapnet_weights_file_close", "swapnet_load_file",
            "swapnet_debug_wait_timeout", "swapnet_pack_bf16",
            "swapnet_attention_tree_workspace", "swapnet_attention_tree", "swapnet_attention_weights",
-           "swapnet_cache_evict", "swapnet_tree_accept"]
+           "swapnet_cache_evict", "swapnet_tree_accept", "swapnet_plan_state_layout", "swapnet_engine_tree_accept",
+           "swapnet_engine_evict"]
 
 _lib = None
 
@@ -207,6 +214,9 @@ def lib():
         "swapnet_attention_weights": (C.c_int, [C.POINTER(CachedAttention), P]),
         "swapnet_cache_evict": (C.c_int, [C.POINTER(CacheEviction), P]),
         "swapnet_tree_accept": (C.c_int, [C.POINTER(TreeAcceptance), P]),
+        "swapnet_plan_state_layout": (C.c_int, [P, C.POINTER(StateLayout)]),
+        "swapnet_engine_tree_accept": (C.c_int, [P, P, P, P]),
+        "swapnet_engine_evict": (C.c_int, [P, C.c_int32, C.c_int32, C.c_int32, P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -260,6 +270,7 @@ class Desc:
             elif L["op"] == "attention":
                 c.src0, c.src1, c.src2 = L["src"]
                 c.heads, c.max_seq, c.theta = L["heads"], L["max_seq"], L["theta"]
+                c.flags |= (ATTENTION_TREE if L.get("tree") else 0) | (ATTENTION_WEIGHTS if L.get("weights") else 0)
             if L["op"] == "attention":
                 c.cout = 0  # filled below from the q width
             if L["op"] != "attention":
@@ -330,6 +341,12 @@ class Plan:
         arr = (BlockInfo * max(1, n.value))()
         check(lib().swapnet_plan_blocks(self.h, arr, n.value, None), "swapnet_plan_blocks")
         return [{f: getattr(b, f) for f, _ in BlockInfo._fields_} for b in arr[:n.value]]
+
+    def state_layout(self):
+        """Byte offsets of what a decoder state holds beside the position and the caches (0: not there)."""
+        s = StateLayout()
+        check(lib().swapnet_plan_state_layout(self.h, C.byref(s)), "swapnet_plan_state_layout")
+        return {f: getattr(s, f) for f, _ in StateLayout._fields_ if f != "reserved"}
 
     def output_offsets(self):
         n = C.c_uint32()
@@ -588,6 +605,15 @@ class Engine:
 
     def bind_state(self, d_state, nbytes):
         check(lib().swapnet_engine_bind_state(self.h, C.c_void_p(d_state), nbytes), "swapnet_engine_bind_state")
+
+    def tree_accept(self, d_ids, d_targets, stream=0):
+        """Accept the path of the drafted tree that the last inference verified."""
+        check(lib().swapnet_engine_tree_accept(self.h, d_ids or None, d_targets or None, stream or None),
+              "swapnet_engine_tree_accept")
+
+    def evict(self, keep, recent=0, sink=0, stream=0):
+        """Shrink the bound state's caches to the rows that got the most attention."""
+        check(lib().swapnet_engine_evict(self.h, keep, recent, sink, stream or None), "swapnet_engine_evict")
 
     def infer(self, d_in, d_out, stream=0):
         check(lib().swapnet_infer(self.h, C.c_void_p(d_in), C.c_void_p(d_out), C.c_void_p(stream or None)),

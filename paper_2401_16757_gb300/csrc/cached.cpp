@@ -64,6 +64,59 @@ int launch_weights(const CachedArgs& a, bool early, cudaStream_t s) {
   return launch_weights_few(x, early, s);
 }
 
+int run_cached_attention(CachedArgs a, const CachedPlan& p, void* workspace, bool early, cudaStream_t s) {
+  char* w = static_cast<char*>(workspace);
+  a.splits = p.splits;
+  a.part = reinterpret_cast<float*>(w);
+  a.ml = reinterpret_cast<float*>(w + p.part_bytes);
+  a.scores = p.spill ? reinterpret_cast<float*>(w + p.part_bytes + p.ml_bytes) : nullptr;
+  a.score_ld = p.score_ld;
+  if (int rc = p.tc ? launch_attention_rows(a, early, s) : launch_attention_few(a, early, s)) return rc;
+  if (int rc = launch_attention_join(a, s)) return rc;
+  return a.weights && !p.spill ? launch_weights(a, true, s) : SWAPNET_OK;
+}
+
+void state_attention(const Model& m, char* state, int index, CachedArgs* out) {
+  const StateLayout& s = m.st;
+  CachedArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.dtype = m.dtype;
+  a.n_seq = 1;
+  a.tokens = s.tokens;
+  a.heads = a.kv_heads = s.heads;
+  a.group = 1;
+  a.dim = s.width / s.heads;
+  a.max_seq = s.max_seq;
+  a.scale_log2 = 1.4426950408889634f / sqrtf((float)a.dim);
+  a.q_stride = a.kv_stride = a.new_stride = a.out_stride = s.width;
+  a.seq_stride = (int64_t)(2 * s.cache_bytes) / m.es;  // (layers taken as sequences)
+  a.rows_step = 0;
+  auto at = [&](uint64_t off) { return reinterpret_cast<char*>(reinterpret_cast<uintptr_t>(state) + off); };
+  const uint64_t qkv = (uint64_t)s.tokens * s.width * m.es, stats = (uint64_t)s.heads * s.tokens;
+  a.lens = reinterpret_cast<const int*>(at(0));
+  a.k = at(s.caches + 2 * (uint64_t)index * s.cache_bytes);
+  a.v = at(s.caches + (2 * (uint64_t)index + 1) * s.cache_bytes);
+  a.lse = reinterpret_cast<float*>(at(s.lse));
+  if (s.flags & SWAPNET_ATTENTION_TREE) {
+    a.counts = reinterpret_cast<const int*>(at(s.count));
+    a.parents = reinterpret_cast<const int*>(at(s.parents));
+    a.k_new = at(s.drafts + 2 * (uint64_t)index * s.draft_bytes);
+    a.v_new = at(s.drafts + (2 * (uint64_t)index + 1) * s.draft_bytes);
+    a.q = at(s.queries + index * qkv);
+    a.lse += index * stats;
+  } else {
+    a.len_add = s.tokens;  // the layer's own rows are in the cache, the position is not yet advanced
+    if (s.flags & SWAPNET_ATTENTION_WEIGHTS)
+      a.weights = reinterpret_cast<float*>(at(s.weights)) + (uint64_t)index * s.heads * s.max_seq;
+    a.weights_in = a.weights;
+  }
+  *out = a;
+}
+
+int cached_launches(const CachedArgs& a, const CachedPlan& p) {
+  return 1 + (p.splits > 1 || p.spill ? 1 : 0) + (a.weights && !p.spill ? 1 : 0);
+}
+
 namespace {
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
@@ -113,6 +166,8 @@ int fill_args(const swapnet_cached_attention* c, CachedArgs* a) {
   a->counts = c->counts;
   a->parents = c->parents;
   a->rows = c->rows;
+  a->lens_step = a->counts_step = 1;
+  a->rows_step = c->tokens;
   a->out = c->out;
   a->lse = c->lse;
   a->weights_in = c->weights_in;
@@ -161,8 +216,7 @@ int swapnet_attention_tree_workspace(const swapnet_cached_attention* c, uint64_t
     if (!bytes) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "null output");
     CachedArgs a;
     if (int rc = check_attention(c, &a)) return rc;
-    const CachedPlan p = cached_plan(a);
-    *bytes = p.part_bytes + p.ml_bytes + p.score_bytes;
+    *bytes = plan_bytes(cached_plan(a));
     return SWAPNET_OK;
   });
 }
@@ -173,22 +227,12 @@ int swapnet_attention_tree(const swapnet_cached_attention* c, void* workspace, u
     CachedArgs a;
     if (int rc = check_attention(c, &a)) return rc;
     const CachedPlan p = cached_plan(a);
-    const uint64_t need = p.part_bytes + p.ml_bytes + p.score_bytes;
+    const uint64_t need = plan_bytes(p);
     if (need && !workspace) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention: null workspace");
     if (workspace_bytes < need) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention: workspace too small");
     if (need && ((uintptr_t)workspace & (kAlign - 1))) SN_FAIL(SWAPNET_ERR_MISALIGNED, "attention: workspace must be 256-byte aligned");
     if (int rc = error_word(&a.err)) return rc;
-    char* w = static_cast<char*>(workspace);
-    a.splits = p.splits;
-    a.part = reinterpret_cast<float*>(w);
-    a.ml = reinterpret_cast<float*>(w + p.part_bytes);
-    a.scores = p.spill ? reinterpret_cast<float*>(w + p.part_bytes + p.ml_bytes) : nullptr;
-    a.score_ld = p.score_ld;
-    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    if (int rc = p.tc ? launch_attention_rows(a, false, s) : launch_attention_few(a, false, s)) return rc;
-    if (int rc = launch_attention_join(a, s)) return rc;
-    if (a.weights && !p.spill) return launch_weights(a, true, s);
-    return SWAPNET_OK;
+    return run_cached_attention(a, p, workspace, false, reinterpret_cast<cudaStream_t>(stream));
   });
 }
 
@@ -241,6 +285,7 @@ int swapnet_cache_evict(const swapnet_cache_eviction* c, swapnet_stream stream) 
     a.weights = c->weights;
     a.weights_out = c->weights_out;
     a.lens = c->lens;
+    a.lens_step = 1;
     a.kept = c->kept;
     a.lens_out = c->lens_out;
     if (a.out_seq < a.keep) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "eviction: out_capacity smaller than keep");

@@ -9,7 +9,7 @@ namespace swapnet {
 // Sequence b's cached rows and queries in use; false (and the device error
 // word set) where they are out of range: such a sequence is left alone.
 __device__ __forceinline__ bool seq_sizes(const CachedArgs& a, int b, int* len, int* count) {
-  const int n = a.lens[b], c = a.counts ? a.counts[b] : a.tokens;
+  const int n = a.lens[b * a.lens_step] + a.len_add, c = a.counts ? a.counts[b * a.counts_step] : a.tokens;
   *len = n;
   *count = c;
   if (n < 0 || n > a.max_seq || c < 0 || c > a.tokens) {

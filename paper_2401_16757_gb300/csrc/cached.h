@@ -17,7 +17,11 @@ struct CachedArgs {
   float scale_log2;  // log2(e) * scale
   const void *q, *k, *v, *k_new, *v_new;
   int64_t q_stride, kv_stride, seq_stride, new_stride, out_stride;  // elements
+  // per sequence: lens[b * lens_step] + len_add cached rows, counts[b *
+  // counts_step] queries, a list of queries at rows + b * rows_step (a step of
+  // 0: one value for all)
   const int *lens, *counts, *parents, *rows;
+  int lens_step, counts_step, rows_step, len_add;
   void* out;
   float* lse;
   const float* weights_in;
@@ -40,6 +44,11 @@ struct CachedPlan {
   uint64_t part_bytes, ml_bytes, score_bytes;
 };
 CachedPlan cached_plan(const CachedArgs& a);
+// Attention as that plan says, its workspace at `workspace`; weights too where
+// asked for.  early: the launch may start while the one before it ends.
+int run_cached_attention(CachedArgs a, const CachedPlan& p, void* workspace, bool early, cudaStream_t s);
+inline uint64_t plan_bytes(const CachedPlan& p) { return p.part_bytes + p.ml_bytes + p.score_bytes; }
+int cached_launches(const CachedArgs& a, const CachedPlan& p);
 
 int launch_attention_rows(const CachedArgs& a, bool early, cudaStream_t s);  // tcgen05
 int launch_attention_few(const CachedArgs& a, bool early, cudaStream_t s);
@@ -57,7 +66,8 @@ struct EvictArgs {
   const float* weights;
   float* weights_out;
   const int* lens;
-  int *kept, *lens_out;
+  int lens_step;        // 0: one length for all sequences
+  int *kept, *lens_out; // (lens_out: nullable)
   int* err;
 };
 int launch_cache_evict(const EvictArgs& a, cudaStream_t s);

@@ -15,6 +15,7 @@
 #include <thread>
 #include <utility>
 
+#include "cached.h"
 #include "internal.h"
 #include "kernels.h"
 #include "pack.h"
@@ -1167,6 +1168,29 @@ static int prepare_units(swapnet_engine* e) {
   return SWAPNET_OK;
 }
 
+// An attention layer with flags: rotation (into the caches, or the draft area
+// of a drafted tree), then the cached attention on the state.
+static int run_state_attention(swapnet_engine* e, const Layer& L, const char* q, const char* k, const char* v, char* y,
+                               cudaStream_t s) {
+  const Model& m = e->plan.model;
+  const StateLayout& st = m.st;
+  CachedArgs a;
+  state_attention(m, e->d_state, L.att_index, &a);
+  a.err = e->err_word;
+  a.out = y;
+  const int* evicted = st.flags & SWAPNET_ATTENTION_WEIGHTS ? a.lens + 1 : nullptr;
+  int rc;
+  if (st.flags & SWAPNET_ATTENTION_TREE) {
+    rc = launch_rope_tree(m.dtype, q, k, v, const_cast<void*>(a.q), const_cast<void*>(a.k_new), const_cast<void*>(a.v_new), a.lens,
+                          evicted, a.counts, a.parents, L.n, L.d.heads, L.c, L.d.theta, e->err_word, s);
+  } else {
+    a.q = q;
+    rc = launch_attention(m.dtype, const_cast<char*>(q), k, v, const_cast<void*>(a.k), const_cast<void*>(a.v), a.lens, L.n,
+                          L.d.heads, L.c, L.d.theta, L.d.max_seq, y, e->err_word, s, true, evicted);
+  }
+  return rc ? rc : run_cached_attention(a, cached_plan(a), e->d_state + st.scratch, true, s);
+}
+
 static int run_unit(swapnet_engine* e, int u, const void* din, void* dout, cudaStream_t s) {
   const swapnet_plan& p = e->plan;
   const Model& m = p.model;
@@ -1228,6 +1252,7 @@ static int run_unit(swapnet_engine* e, int u, const void* din, void* dout, cudaS
       if (!e->d_state) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "decoder state not bound (swapnet_engine_bind_state)");
       char* kc = e->d_state + L.state_off;
       char* vc = kc + align_up((uint64_t)L.d.max_seq * L.c * es);
+      if (m.st.flags) return run_state_attention(e, L, x, act_ptr(e, L.d.src1, din, dout), act_ptr(e, L.d.src2, din, dout), y, s);
       return launch_attention(m.dtype, const_cast<char*>(x), act_ptr(e, L.d.src1, din, dout),
                               act_ptr(e, L.d.src2, din, dout), kc, vc, reinterpret_cast<const int*>(e->d_state),
                               L.n, L.d.heads, L.c, L.d.theta, L.d.max_seq, y, e->err_word, s);
@@ -1455,7 +1480,8 @@ int swapnet_engine_adapt(swapnet_engine* e, const swapnet_plan* plan) {
     const Model& a = e->plan.model;
     const Model& b = plan->model;
     bool same = a.L.size() == b.L.size() && a.n_tensors == b.n_tensors && a.dtype == b.dtype &&
-                a.weight_bytes == b.weight_bytes && a.in_bytes == b.in_bytes && a.ws_bytes == b.ws_bytes;
+                a.weight_bytes == b.weight_bytes && a.in_bytes == b.in_bytes && a.ws_bytes == b.ws_bytes &&
+                a.st.flags == b.st.flags && (!a.st.flags || a.state_bytes == b.state_bytes);
     for (size_t i = 0; same && i < a.L.size(); ++i)
       same = std::memcmp(&a.L[i].d, &b.L[i].d, sizeof(swapnet_layer)) == 0 ||
              (a.L[i].d.op == b.L[i].d.op && a.L[i].d.cin == b.L[i].d.cin && a.L[i].d.cout == b.L[i].d.cout &&
@@ -1672,7 +1698,8 @@ static int enqueue(swapnet_engine* e, const void* din, void* dout, cudaStream_t 
   if (p.model.has_attention) {
     if (!e->d_state) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "decoder state not bound (swapnet_engine_bind_state)");
     const Model& m = p.model;
-    int rc = launch_advance(reinterpret_cast<int*>(e->d_state), m.in_n * m.in_h * m.in_w * m.in_c, s);
+    // (a drafted tree's nodes are in no cache yet)
+    int rc = m.st.flags & SWAPNET_ATTENTION_TREE ? SWAPNET_OK : launch_advance(reinterpret_cast<int*>(e->d_state), m.in_n * m.in_h * m.in_w * m.in_c, s);
     if (rc) return rc;
   }
   if (pf) {
@@ -1694,8 +1721,15 @@ static int enqueue(swapnet_engine* e, const void* din, void* dout, cudaStream_t 
 }
 
 static uint64_t launches_per_infer(const swapnet_engine* e) {
-  uint64_t n = e->plan.units.size() + (e->plan.model.has_attention ? 1 : 0);
-  for (int k : e->unit_kind) n += (k == SWAPNET_KERNEL_ATTENTION) ? 1 : 0;
+  const StateLayout& st = e->plan.model.st;
+  uint64_t n = e->plan.units.size() + (e->plan.model.has_attention && !(st.flags & SWAPNET_ATTENTION_TREE) ? 1 : 0);
+  int per_attention = 1;  // beside the rotation
+  if (st.flags) {
+    CachedArgs a;
+    state_attention(e->plan.model, e->d_state, 0, &a);
+    per_attention = cached_launches(a, cached_plan(a));
+  }
+  for (int k : e->unit_kind) n += (k == SWAPNET_KERNEL_ATTENTION) ? per_attention : 0;
   for (char c : e->merged_into) n -= c ? 1 : 0;
   if (!e->plan.resident)
     for (size_t k = 0; k < e->blocks.size(); ++k)
@@ -1925,6 +1959,98 @@ int swapnet_engine_bind_state(swapnet_engine* e, void* d_state, uint64_t bytes) 
     for (auto& kv : e->graphs) cudaGraphExecDestroy(kv.second);  // captured with the old state
     e->graphs.clear();
     return SWAPNET_OK;
+  });
+}
+
+int swapnet_engine_tree_accept(swapnet_engine* e, const int32_t* d_ids, const int32_t* d_targets, swapnet_stream stream) {
+  return swapnet::guard_abi([&]() -> int {
+    if (!e || !d_ids || !d_targets) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "null argument");
+    const Model& m = e->plan.model;
+    const StateLayout& st = m.st;
+    if (!(st.flags & SWAPNET_ATTENTION_TREE)) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "the model's attention takes no drafted tree");
+    if (!e->d_state) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "decoder state not bound (swapnet_engine_bind_state)");
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    CU(cudaSetDevice(e->device), "cudaSetDevice");
+    int* header = reinterpret_cast<int*>(e->d_state);
+    int rc = launch_state_header(header, 0, 0, 0, s);
+    if (rc) return rc;
+    AcceptArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.es = m.es;
+    a.n_seq = 1;
+    a.tokens = st.tokens;
+    a.width = st.width;
+    a.max_seq = st.max_seq;
+    a.n_caches = 2 * st.layers;
+    a.cache_stride = a.new_stride = st.width;
+    a.ids = d_ids;
+    a.targets = d_targets;
+    a.parents = reinterpret_cast<const int*>(e->d_state + st.parents);
+    a.counts = reinterpret_cast<const int*>(e->d_state + st.count);
+    a.lens = header;
+    a.path = reinterpret_cast<int*>(e->d_state + st.path);
+    a.lens_out = header + 2;
+    a.accepted = header + 3;
+    a.next = header + 4;
+    a.err = e->err_word;
+    for (int i = 0; i < a.n_caches; ++i) {
+      a.caches[i] = e->d_state + st.caches + i * st.cache_bytes;
+      a.drafts[i] = e->d_state + st.drafts + i * st.draft_bytes;
+    }
+    rc = launch_tree_accept(a, s);
+    if (!rc && (st.flags & SWAPNET_ATTENTION_WEIGHTS)) {
+      // the accepted nodes are the caches' last rows now; layers as sequences
+      CachedArgs w;
+      state_attention(m, e->d_state, 0, &w);
+      w.n_seq = st.layers;
+      w.lens = header + 2;
+      w.counts = header + 3;
+      w.rows = a.path;
+      w.parents = nullptr;
+      w.k_new = w.v_new = nullptr;
+      w.weights = reinterpret_cast<float*>(e->d_state + st.weights);
+      w.weights_in = w.weights;
+      w.err = e->err_word;
+      rc = launch_weights(w, false, s);
+    }
+    return rc ? rc : launch_state_header(header, 1, 0, 0, s);
+  });
+}
+
+int swapnet_engine_evict(swapnet_engine* e, int32_t keep, int32_t recent, int32_t sink, swapnet_stream stream) {
+  return swapnet::guard_abi([&]() -> int {
+    if (!e) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "null engine");
+    const Model& m = e->plan.model;
+    const StateLayout& st = m.st;
+    if (!(st.flags & SWAPNET_ATTENTION_WEIGHTS)) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "the model keeps no attention weights");
+    if (!e->d_state) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "decoder state not bound (swapnet_engine_bind_state)");
+    if (keep < 1 || keep > st.max_seq || recent < 0 || sink < 0 || (int64_t)recent + sink > keep)
+      SN_FAIL(SWAPNET_ERR_INVALID_ARG, "eviction: sink + recent must be within keep, keep within the cache");
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    CU(cudaSetDevice(e->device), "cudaSetDevice");
+    EvictArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.dtype = m.dtype;
+    a.n_seq = st.layers;
+    a.kv_heads = st.heads;
+    a.dim = st.width / st.heads;
+    a.max_seq = a.out_seq = st.max_seq;
+    a.keep = keep;
+    a.recent = recent;
+    a.sink = sink;
+    a.kv_stride = a.out_stride = st.width;
+    a.seq_stride = a.out_seq_stride = (int64_t)(2 * st.cache_bytes) / m.es;
+    a.k_out = e->d_state + st.caches;
+    a.v_out = e->d_state + st.caches + st.cache_bytes;
+    a.k = a.k_out;
+    a.v = a.v_out;
+    a.weights_out = reinterpret_cast<float*>(e->d_state + st.weights);
+    a.weights = a.weights_out;
+    a.lens = reinterpret_cast<const int*>(e->d_state);
+    a.kept = reinterpret_cast<int*>(e->d_state + st.kept);
+    a.err = e->err_word;
+    const int rc = launch_cache_evict(a, s);
+    return rc ? rc : launch_state_header(reinterpret_cast<int*>(e->d_state), 2, keep, st.max_seq, s);
   });
 }
 

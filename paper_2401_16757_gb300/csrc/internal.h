@@ -69,12 +69,28 @@ struct Layer {
   uint64_t out_bytes;    // raw bytes of the output tensor
   bool host_resident;    // parameters read in host memory, never swapped (EMBED)
   int64_t state_off;     // ATTENTION: offset of its key cache in the decoder state
+  int att_index;         // ATTENTION: which one of the model's
+};
+
+// Where the decoder state of a model whose ATTENTION layers carry flags holds
+// what those need, in bytes from its start; every attention layer has the same
+// shape.  0: not there.
+struct StateLayout {
+  int flags = 0;  // SWAPNET_ATTENTION_*
+  int layers = 0, tokens = 0, heads = 0, width = 0, max_seq = 0;
+  uint64_t caches = 0, cache_bytes = 0;
+  uint64_t weights = 0, kept = 0;                  // fp32, int32 [layers][heads][max_seq]
+  uint64_t count = 0, parents = 0, path = 0;       // int32: 1, [tokens], [tokens]
+  uint64_t drafts = 0, draft_bytes = 0;            // per layer keys and values [tokens][width]
+  uint64_t queries = 0, lse = 0;                   // rotated queries; fp32 [layers][heads][tokens]
+  uint64_t scratch = 0;                            // the attention's workspace
 };
 
 struct Model {
   int dtype = 0, es = 0, in_dtype = 0;
   uint64_t state_bytes = 0;  // decoder state: 256-byte position header + KV caches
   bool has_attention = false;
+  StateLayout st;
   int in_n = 0, in_h = 0, in_w = 0, in_c = 0;
   std::vector<Layer> L;
   int n_tensors = 0;
@@ -142,6 +158,10 @@ struct FileRun {
 int file_read_runs(const swapnet_weights_file* f, const FileRun* runs, size_t n, char* stage);
 
 int analyse_model(const swapnet_model_desc* desc, Model* m);
+// The attention of layer `index` of a model with attention flags, on the state
+// at `state` (its layout alone is used where that is null).
+struct CachedArgs;
+void state_attention(const Model& m, char* state, int index, CachedArgs* a);
 int make_units(const Model& m, const swapnet_options& opt, uint64_t slot, uint64_t region, std::vector<Unit>* out);
 void finalize_blocks(swapnet_plan* p, const std::vector<uint32_t>& cuts);
 int64_t pipeline_ns(const std::vector<Block>& b, int slots, bool prefix = false);

@@ -40,7 +40,7 @@ __global__ void __launch_bounds__(kEvThreads) evict_select_kernel(const __grid_c
   __shared__ uint32_t hist[256];
   __shared__ uint32_t sh_prefix, sh_need, wtot[32];
   const int kvh = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int len = a.lens[b];
+  const int len = a.lens[b * a.lens_step];
   if (len < 0 || len > a.max_seq) {
     if (tid == 0) atomicExch(a.err, kDevErrBounds);
     return;
@@ -50,7 +50,7 @@ __global__ void __launch_bounds__(kEvThreads) evict_select_kernel(const __grid_c
   float* wo = a.weights_out + pair * a.out_seq;
   int* kept = a.kept + pair * a.keep;
   const int keep = min(len, a.keep);
-  if (kvh == 0 && tid == 0) a.lens_out[b] = keep;
+  if (kvh == 0 && tid == 0 && a.lens_out) a.lens_out[b] = keep;
   const int c0 = len > keep ? a.sink : len, c1 = len > keep ? len - a.recent : len;  // candidates [c0, c1)
   uint32_t need = len > keep ? keep - a.sink - a.recent : 0, prefix = 0;
   if (c0 < c1) {
@@ -151,13 +151,15 @@ __global__ void __launch_bounds__(kEvThreads) evict_select_kernel(const __grid_c
     equal += total >> 16;
     __syncthreads();  // wtot is written again
   }
+  // rows appended later start from nothing
+  for (int j = keep + tid; j < min(len, a.out_seq); j += kEvThreads) wo[j] = 0.f;
 }
 
 // Out of place: 16 bytes per thread, rows in any order.
 __global__ void __launch_bounds__(256) evict_copy_kernel(const __grid_constant__ EvictArgs a, int chunks) {
   pdl_wait();
   const int kvh = blockIdx.y, b = blockIdx.z;
-  const int len = a.lens[b];
+  const int len = a.lens[b * a.lens_step];
   if (len < 0 || len > a.max_seq) return;
   const int n = min(len, a.keep) * chunks;
   const int* kept = a.kept + ((int64_t)b * a.kv_heads + kvh) * a.keep;
@@ -179,7 +181,7 @@ constexpr int kEvMove = 4;  // rows per thread and tile
 __global__ void __launch_bounds__(512) evict_move_kernel(const __grid_constant__ EvictArgs a, int slice) {
   pdl_wait();
   const int kvh = blockIdx.y, b = blockIdx.z;
-  const int len = a.lens[b];
+  const int len = a.lens[b * a.lens_step];
   if (len <= a.keep || len > a.max_seq) return;  // (nothing moves)
   const int* kept = a.kept + ((int64_t)b * a.kv_heads + kvh) * a.keep;
   const int parts = gridDim.x / 2;

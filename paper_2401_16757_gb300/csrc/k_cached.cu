@@ -502,7 +502,7 @@ __global__ void __launch_bounds__(kFwThreads) weights_few_kernel(const __grid_co
       const int r = r0 + i, t = r / a.group;
       int q = t;
       if (i < here && a.rows) {
-        q = a.rows[(int64_t)b * a.tokens + t];
+        q = a.rows[(int64_t)b * a.rows_step + t];
         if (q < 0 || q >= a.tokens) {
           atomicExch(a.err, kDevErrBounds);
           q = -1;

@@ -629,7 +629,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         const int nq = min(queries, count - t0);
         mbar_arrive_expect_tx(q_full(slot), F::kHalves * nq * a.group * 128);
         for (int i = 0; i < nq; ++i) {
-          const int q = min(max(a.rows[(int64_t)b * a.tokens + t0 + i], 0), a.tokens - 1);
+          const int q = min(max(a.rows[(int64_t)b * a.rows_step + t0 + i], 0), a.tokens - 1);
 #pragma unroll
           for (int h = 0; h < F::kHalves; ++h)
             tma_load_3d(dst + h * F::kBox + i * a.group * 128, &tmQ, q_full(slot), h * 64, kvh * a.group, b * a.tokens + q);
@@ -720,7 +720,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       if (aid < queries * a.group && t < count) {
         int q = t;
         if (a.rows) {
-          q = a.rows[(int64_t)b * a.tokens + t];
+          q = a.rows[(int64_t)b * a.rows_step + t];
           if (q < 0 || q >= a.tokens) {
             atomicExch(a.err, kDevErrBounds);
             return;

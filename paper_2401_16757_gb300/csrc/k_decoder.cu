@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <cstring>
 
+#include "cached.h"
 #include "device.cuh"
 #include "internal.h"
 #include "kernels.h"
@@ -165,7 +166,8 @@ template <typename T, int HPT, int NP>
 __global__ void __launch_bounds__(128) rope_append_kernel(T* __restrict__ q, const T* k,
                                                           const T* v, T* __restrict__ kc,
                                                           T* __restrict__ vc, const int* pos_ptr,
-                                                          int heads, int dh, float theta, int max_seq, int* err) {
+                                                          int heads, int dh, float theta, int max_seq, int* err,
+                                                          const int* evicted) {
   using Vec = typename RopeVec<NP>::type;
   const int t = blockIdx.y;
   const int chunks = dh / (2 * NP);  // chunks of NP pairs in a head
@@ -186,6 +188,7 @@ __global__ void __launch_bounds__(128) rope_append_kernel(T* __restrict__ q, con
     return;
   }
   const int pos = pos0 + t;
+  const int angle_pos = pos + (evicted ? *evicted : 0);  // rows evicted from the cache still count
   const int width = heads * dh;
   Vec qv[HPT], kv[HPT], vv[HPT];
 #pragma unroll
@@ -199,7 +202,7 @@ __global__ void __launch_bounds__(128) rope_append_kernel(T* __restrict__ q, con
   }
   float sn[NP], cs[NP];
 #pragma unroll
-  for (int u = 0; u < NP; ++u) sincosf((float)pos * inv[u], &sn[u], &cs[u]);
+  for (int u = 0; u < NP; ++u) sincosf((float)angle_pos * inv[u], &sn[u], &cs[u]);
   auto rotate = [&](const Vec& x) {
     Vec y;
     const T* e = reinterpret_cast<const T*>(&x);
@@ -220,6 +223,71 @@ __global__ void __launch_bounds__(128) rope_append_kernel(T* __restrict__ q, con
       *reinterpret_cast<Vec*>(kc + (int64_t)pos * width + col) = rotate(kv[j]);
       *reinterpret_cast<Vec*>(vc + (int64_t)pos * width + col) = vv[j];
     }
+  }
+}
+
+// ------------------------------------------------ RoPE of a drafted tree
+// Node t sits at the position of the cache's end plus its depth below the
+// cached rows.  Rotates q and k and copies v into the state's draft area (the
+// rows that swapnet_engine_tree_accept appends to the caches); thread = a pair
+// of one head of one node, angles as above.
+template <typename T>
+__global__ void __launch_bounds__(128) rope_tree_kernel(const T* q, const T* k, const T* v, T* qo, T* ko, T* vo,
+                                                        const int* header, const int* evicted, const int* count_ptr,
+                                                        const int* parents, int tokens, int heads, int dh, float theta, int* err) {
+  __shared__ int par[kTreeMax];
+  const int t = blockIdx.y;
+  const int id = blockIdx.x * blockDim.x + threadIdx.x, pairs = dh / 2;
+  const int ch = id % pairs, h = id / pairs;
+  const float inv = powf(theta, -2.0f * (float)ch / (float)dh);
+  pdl_wait();
+  pdl_launch_dependents();
+  const int count = *count_ptr;
+  if (count < 1 || count > tokens) {
+    if (id == 0) atomicExch(err, kDevErrBounds);
+    return;
+  }
+  bool bad = false;
+  for (int i = threadIdx.x; i < count; i += blockDim.x) {
+    const int p = parents[i];
+    par[i] = p;
+    bad = bad || p < -1 || p >= i;
+  }
+  if (__syncthreads_or(bad)) {
+    if (id == 0) atomicExch(err, kDevErrBounds);
+    return;
+  }
+  if (t >= count || h >= heads) return;
+  int pos = header[0] + (evicted ? *evicted : 0);
+  for (int i = par[t]; i >= 0; i = par[i]) ++pos;  // (each step goes to a lower node)
+  const int64_t at = (int64_t)t * heads * dh + h * dh + 2 * ch;
+  float sn, cs;
+  sincosf((float)pos * inv, &sn, &cs);
+  auto rotate = [&](const T* from, T* to) {
+    const float a = to_f<T>(from[at]), b = to_f<T>(from[at + 1]);
+    to[at] = from_f<T>(a * cs - b * sn);
+    to[at + 1] = from_f<T>(a * sn + b * cs);
+  };
+  rotate(q, qo);
+  rotate(k, ko);
+  vo[at] = v[at];
+  vo[at + 1] = v[at + 1];
+}
+
+// The header of a state around the calls that change the number of its rows:
+// before an acceptance (word 2: the rows after it), after it, after an
+// eviction.
+enum HeaderStep : int { kHeaderAccept = 0, kHeaderAccepted = 1, kHeaderEvicted = 2 };
+__global__ void state_header_kernel(int* header, int step, int keep, int max_seq) {
+  const int pos = header[0];
+  if (step == kHeaderAccept) {
+    header[2] = pos;
+    header[3] = 0;
+  } else if (step == kHeaderAccepted) {
+    header[0] = header[2];
+  } else if (pos > keep && pos <= max_seq) {
+    header[1] += pos - keep;
+    header[0] = keep;
   }
 }
 
@@ -572,7 +640,7 @@ int launch_rmsnorm(int dtype, const void* x, const void* g, int rows, int d, flo
 
 int launch_attention(int dtype, void* q, const void* k, const void* v, void* kc, void* vc, const int* pos_ptr,
                      int tokens, int heads, int width, float theta, int max_seq, void* out, int* err,
-                     cudaStream_t s) {
+                     cudaStream_t s, bool rotate_only, const int* evicted) {
   if (width % heads || width / heads != kDh) SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "attention: head width must be 128");
   SN_DISPATCH16(dtype, T, {
     if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)kc | (uintptr_t)vc) & 15)
@@ -583,9 +651,9 @@ int launch_attention(int dtype, void* q, const void* k, const void* v, void* kc,
     const dim3 g1((threads + 127) / 128, tokens);
     int rc = done(launch_pdl(many ? rope_append_kernel<T, 4, 4> : rope_append_kernel<T, 1, 1>, g1, dim3(128), 0, s,
                              static_cast<T*>(q), static_cast<const T*>(k), static_cast<const T*>(v),
-                             static_cast<T*>(kc), static_cast<T*>(vc), pos_ptr, heads, kDh, theta, max_seq, err),
+                             static_cast<T*>(kc), static_cast<T*>(vc), pos_ptr, heads, kDh, theta, max_seq, err, evicted),
                   "rope launch");
-    if (rc) return rc;
+    if (rc || rotate_only) return rc;
     if (attention_tc_supported(dtype, tokens, heads, width, max_seq))  // both contractions on the tensor cores
       return launch_attention_tc(dtype, q, kc, vc, pos_ptr, tokens, heads, width, max_seq, out, err, s);
     // decode: the visible keys split over a cluster of CTAs per (query, head)
@@ -624,6 +692,25 @@ int launch_argmax(int dtype, const void* x, int rows, int n, int* out, cudaStrea
   SN_DISPATCH16(dtype, T, return done(launch_pdl(argmax_kernel<T>, dim3(rows), dim3(kArgThreads), 0, s,
                                                  static_cast<const T*>(x), n, out, vec), "argmax launch"));
   return SWAPNET_OK;
+}
+
+int launch_rope_tree(int dtype, const void* q, const void* k, const void* v, void* qo, void* ko, void* vo, const int* header,
+                     const int* evicted, const int* count, const int* parents, int tokens, int heads, int width, float theta, int* err,
+                     cudaStream_t s) {
+  if (width % heads || width / heads != kDh || tokens > kTreeMax)
+    SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "drafted trees: head width 128, at most 128 nodes");
+  const dim3 grid((heads * (kDh / 2) + 127) / 128, tokens);
+  SN_DISPATCH16(dtype, T, return done(launch_pdl(rope_tree_kernel<T>, grid, dim3(128), 0, s, static_cast<const T*>(q),
+                                                 static_cast<const T*>(k), static_cast<const T*>(v), static_cast<T*>(qo),
+                                                 static_cast<T*>(ko), static_cast<T*>(vo), header, evicted, count, parents,
+                                                 tokens, heads, kDh, theta, err),
+                                      "drafted tree rope launch"));
+  return SWAPNET_OK;
+}
+
+int launch_state_header(int* header, int step, int keep, int max_seq, cudaStream_t s) {
+  state_header_kernel<<<1, 1, 0, s>>>(header, step, keep, max_seq);
+  return done(cudaGetLastError(), "state header launch");
 }
 
 int launch_advance(int* pos_ptr, int n, cudaStream_t s) {

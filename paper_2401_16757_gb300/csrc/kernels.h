@@ -95,13 +95,20 @@ int launch_concat(int dtype, const void* a, int ca, const void* b, int cb, int64
 // Decoder kernels (fp16 / bf16).  The embedding table pointer is the device
 // alias of the page-locked host table.  The attention launcher runs the RoPE
 // + cache-append kernel (q rotated in place) and then the attention kernel;
-// pos_ptr is the device-side position of the decoder state.
+// pos_ptr is the device-side position of the decoder state.  evicted (nullable):
+// the rows evicted from the cache so far, which count in the rotation.
 int launch_embed(int dtype, const void* table, const int* ids, int tokens, int vocab, int d, void* out, int* err,
                  cudaStream_t s);
 int launch_rmsnorm(int dtype, const void* x, const void* g, int rows, int d, float eps, void* y, cudaStream_t s);
 int launch_attention(int dtype, void* q, const void* k, const void* v, void* kc, void* vc, const int* pos_ptr,
                      int tokens, int heads, int width, float theta, int max_seq, void* out, int* err,
+                     cudaStream_t s, bool rotate_only = false, const int* evicted = nullptr);
+// The nodes of a drafted tree: rotated q and k, and v, into the state.
+int launch_rope_tree(int dtype, const void* q, const void* k, const void* v, void* qo, void* ko, void* vo, const int* header,
+                     const int* evicted, const int* count, const int* parents, int tokens, int heads, int width, float theta, int* err,
                      cudaStream_t s);
+// The state header before (0) and after (1) an acceptance, after an eviction (2).
+int launch_state_header(int* header, int step, int keep, int max_seq, cudaStream_t s);
 int launch_argmax(int dtype, const void* x, int rows, int n, int* out, cudaStream_t s);
 int launch_advance(int* pos_ptr, int n, cudaStream_t s);
 

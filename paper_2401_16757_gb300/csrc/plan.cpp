@@ -8,6 +8,7 @@
 #include <memory>
 #include <new>
 
+#include "cached.h"
 #include "internal.h"
 
 namespace swapnet {
@@ -27,6 +28,61 @@ static uint64_t mul_div_ceil(uint64_t a, uint64_t b, uint64_t d) {
 }
 
 // ------------------------------------------------------------ model analysis
+// What follows the caches in the state of a model whose attention layers carry
+// flags; *cur: the state's size so far.
+static int lay_out_state(Model* m, uint64_t* cur) {
+  StateLayout& s = m->st;
+  const Layer* first = nullptr;
+  bool same = true;
+  for (const Layer& L : m->L) {
+    if (L.d.op != SWAPNET_OP_ATTENTION) continue;
+    const int flags = L.d.flags & (SWAPNET_ATTENTION_TREE | SWAPNET_ATTENTION_WEIGHTS);
+    if (!first) {
+      first = &L;
+      s.flags = flags;
+    }
+    if (flags != s.flags) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention flags differ between the layers");
+    same = same && L.c == first->c && L.d.heads == first->d.heads && L.d.max_seq == first->d.max_seq && L.n == first->n;
+  }
+  s.caches = (uint64_t)first->state_off;
+  if (same) s.cache_bytes = align_up((uint64_t)first->d.max_seq * first->c * m->es);
+  if (!s.flags) return SWAPNET_OK;
+  if (!same) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention layers with flags must have one shape");
+  if ((m->dtype != SWAPNET_F16 && m->dtype != SWAPNET_BF16) || first->c / first->d.heads != 128)
+    SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "attention flags: fp16 / bf16, head width 128");
+  s.tokens = first->n;
+  s.heads = first->d.heads;
+  s.width = first->c;
+  s.max_seq = first->d.max_seq;
+  if ((s.flags & SWAPNET_ATTENTION_TREE) && s.tokens > kTreeMax)
+    SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "a drafted tree has at most 128 nodes");
+  if ((s.flags & SWAPNET_ATTENTION_TREE) && 2 * s.layers > kAcceptMaxCaches)
+    SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "drafted trees: at most 128 attention layers");
+  auto take = [&](uint64_t bytes) {
+    const uint64_t at = *cur;
+    *cur += align_up(bytes);
+    return at;
+  };
+  const uint64_t rows = (uint64_t)s.layers * s.heads * s.max_seq;
+  if (s.flags & SWAPNET_ATTENTION_WEIGHTS) {
+    s.weights = take(rows * 4);
+    s.kept = take(rows * 4);
+  }
+  if (s.flags & SWAPNET_ATTENTION_TREE) {
+    s.count = take(4);
+    s.parents = take((uint64_t)s.tokens * 4);
+    s.path = take((uint64_t)s.tokens * 4);
+    s.draft_bytes = align_up((uint64_t)s.tokens * s.width * m->es);
+    s.drafts = take(2 * s.layers * s.draft_bytes);
+    s.queries = take((uint64_t)s.layers * s.tokens * s.width * m->es);  // (no gaps: one array for all layers)
+  }
+  s.lse = take((uint64_t)(s.flags & SWAPNET_ATTENTION_TREE ? s.layers : 1) * s.heads * s.tokens * 4);
+  CachedArgs a;
+  state_attention(*m, nullptr, 0, &a);
+  s.scratch = take(plan_bytes(cached_plan(a)));
+  return SWAPNET_OK;
+}
+
 int analyse_model(const swapnet_model_desc* desc, Model* m) {
   if (!desc || !desc->layers || desc->n_layers <= 0) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "empty model descriptor");
   m->dtype = desc->dtype;
@@ -42,6 +98,7 @@ int analyse_model(const swapnet_model_desc* desc, Model* m) {
                 (m->in_dtype == SWAPNET_I32 ? 4 : m->es);
   m->state_bytes = 0;
   m->has_attention = false;
+  m->st = StateLayout{};
   uint64_t state_cur = kAlign;  // position header
   const int nl = desc->n_layers;
   m->L.assign(nl, Layer{});
@@ -147,6 +204,7 @@ int analyse_model(const swapnet_model_desc* desc, Model* m) {
         L.on = L.n; L.oh = 1; L.ow = 1; L.oc = L.c;
         L.flops = 4ull * L.n * (uint64_t)d.max_seq * L.c;
         L.state_off = (int64_t)state_cur;
+        L.att_index = m->st.layers++;
         state_cur += 2 * align_up((uint64_t)d.max_seq * L.c * es);
         m->has_attention = true;
         break;
@@ -183,6 +241,8 @@ int analyse_model(const swapnet_model_desc* desc, Model* m) {
     m->n_tensors += L.n_tensors;
     L.out_bytes = (uint64_t)L.on * L.oh * L.ow * L.oc * (d.op == SWAPNET_OP_ARGMAX ? 4 : es);
   }
+  if (m->has_attention)
+    if (int rc = lay_out_state(m, &state_cur)) return rc;
   m->state_bytes = m->has_attention ? state_cur : 0;
   // liveness: last reader of every output
   for (int i = 0; i < nl; ++i) m->L[i].last_use = i;
@@ -1064,6 +1124,22 @@ int swapnet_plan_blocks(const swapnet_plan* p, swapnet_block_info* b, uint32_t c
       b[i] = swapnet_block_info{(uint32_t)B.u0, (uint32_t)B.u1, (uint32_t)B.slot, (uint32_t)B.depth, B.bytes,
                                 B.t_in, B.t_ex, B.t_out, B.base};
     }
+    return SWAPNET_OK;
+  });
+}
+
+int swapnet_plan_state_layout(const swapnet_plan* p, swapnet_state_layout* out) {
+  return swapnet::guard_abi([&]() -> int {
+    if (!p || !out) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "null argument");
+    const swapnet::StateLayout& s = p->model.st;
+    std::memset(out, 0, sizeof(*out));
+    out->caches = s.caches;
+    out->cache_bytes = s.cache_bytes;
+    out->weights = s.weights;
+    out->tree_count = s.count;
+    out->tree_parents = s.parents;
+    out->tree_path = s.path;
+    out->layers = (uint32_t)s.layers;
     return SWAPNET_OK;
   });
 }

@@ -155,7 +155,7 @@ def yolov3(batch=1, res=416, classes=80):
 
 
 
-def llm(layers=32, d=4096, heads=32, ffn=11008, vocab=32000, tokens=512, max_seq=544):
+def llm(layers=32, d=4096, heads=32, ffn=11008, vocab=32000, tokens=512, max_seq=544, tree=False, weights=False):
     """LLaMA-7B-shaped decoder (pre-norm, RMSNorm eps 1e-6 with gains, RoPE
     theta 10000 on adjacent pairs, causal attention with a KV cache of
     max_seq positions, SwiGLU FFN, untied LM head, no biases), bf16.
@@ -164,6 +164,8 @@ def llm(layers=32, d=4096, heads=32, ffn=11008, vocab=32000, tokens=512, max_seq
     position and their argmax (ties -> lowest index).  Decoder layer i:
       rmsnorm -> q, k, v -> attention -> o (+x) -> rmsnorm -> gate, up
       (silu(gate) * up) -> down (+h)
+    tree: the tokens are the nodes of a drafted tree; weights: the attention
+    that each cached row gets is added up.
     """
     L = [dict(op="embed", src=[-1], vocab=vocab, d=d)]
     x = 0
@@ -174,6 +176,8 @@ def llm(layers=32, d=4096, heads=32, ffn=11008, vocab=32000, tokens=512, max_seq
         k = len(L); L.append(_linear(xn, d, d))
         v = len(L); L.append(_linear(xn, d, d))
         L.append(dict(op="attention", src=[q, k, v], heads=heads, max_seq=max_seq, theta=10000.0))
+        if tree or weights:
+            L[-1].update(tree=tree, weights=weights)
         a = len(L) - 1
         L.append(_linear(a, d, d, res=x))
         h = len(L) - 1

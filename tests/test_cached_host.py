@@ -114,3 +114,54 @@ def test_acceptance_refuses(change, code):
 def test_acceptance_needs_a_draft_per_cache():
     with pytest.raises(ValueError):
         _accept(caches=np.array([A, A]))
+
+
+# --------------------------------------------------- decoders with the flags
+def _llm(**kw):
+    import synth
+    return synth.arch.llm(layers=2, d=256, heads=2, ffn=688, vocab=1000, max_seq=90, **kw)
+
+
+def test_state_layout():
+    """The caches stay where they were; what the flags add lies behind them and nothing overlaps."""
+    base = capi.Plan.resident(capi.Desc(_llm(tokens=4)))
+    tree = capi.Plan.resident(capi.Desc(_llm(tokens=4, tree=True)))
+    both = capi.Plan.resident(capi.Desc(_llm(tokens=4, tree=True, weights=True)))
+    weigh = capi.Plan.resident(capi.Desc(_llm(tokens=9, weights=True)))
+    cache = (90 * 256 * 2 + 255) // 256 * 256
+    assert base.info()["state_bytes"] == 256 + 4 * cache
+    l0, l1, l2, l3 = (p.state_layout() for p in (base, tree, both, weigh))
+    assert l0 == dict(caches=256, cache_bytes=cache, weights=0, tree_count=0, tree_parents=0, tree_path=0, layers=2)
+    for lay, p in ((l1, tree), (l2, both), (l3, weigh)):
+        assert lay["caches"] == 256 and lay["cache_bytes"] == cache and lay["layers"] == 2
+        assert p.info()["state_bytes"] > 256 + 4 * cache
+    assert l1["weights"] == 0 and l2["weights"] == l3["weights"] == 256 + 4 * cache
+    assert l3["tree_count"] == 0 and l2["tree_count"] >= l2["weights"] + 2 * 2 * 2 * 90 * 4
+    assert l1["tree_count"] < l1["tree_parents"] < l1["tree_path"] and (l1["tree_parents"] - l1["tree_count"]) % 256 == 0
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(tokens=129, tree=True), capi.ERR_UNSUPPORTED),
+    (dict(tokens=4, tree=True, heads=4), capi.ERR_UNSUPPORTED),  # head width 64
+    (dict(tokens=4, weights=True, heads=1), capi.ERR_UNSUPPORTED),
+])
+def test_flags_that_no_kernel_takes(change, code):
+    import synth
+    cfg = dict(layers=2, d=256, heads=2, ffn=688, vocab=1000, max_seq=90)
+    cfg.update(change)
+    assert _code(capi.Plan.resident, capi.Desc(synth.arch.llm(**cfg))) == code
+
+
+def test_flags_are_the_same_on_every_layer():
+    m = _llm(tokens=4)
+    att = [L for L in m["layers"] if L["op"] == "attention"]
+    att[0]["weights"] = True
+    assert _code(capi.Plan.resident, capi.Desc(m)) == capi.ERR_INVALID_ARG
+    att[1]["weights"] = True
+    att[1]["max_seq"] = 91
+    assert _code(capi.Plan.resident, capi.Desc(m)) == capi.ERR_INVALID_ARG
+    att[1]["max_seq"] = 90
+    assert capi.Plan.resident(capi.Desc(m)).state_layout()["weights"] > 0
+    assert capi.lib().swapnet_plan_state_layout(None, None) == capi.ERR_INVALID_ARG
+    assert capi.lib().swapnet_engine_tree_accept(None, None, None, None) == capi.ERR_INVALID_ARG
+    assert capi.lib().swapnet_engine_evict(None, 1, 0, 0, None) == capi.ERR_INVALID_ARG

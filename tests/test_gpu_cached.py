@@ -478,8 +478,9 @@ def test_eviction(dtype, kv, dim, keep, recent, sink, in_place):
                 rest = got[b, x:, cols]
                 assert torch.equal(rest, before[name][b, x:, cols]) if in_place else torch.all(rest == SENT)
             assert torch.equal(torch.nan_to_num(gw[b, h, :x], -9), torch.nan_to_num(w[b, h, rows], -9))
-            rest = gw[b, h, x:]
-            assert torch.equal(torch.nan_to_num(rest, -9), torch.nan_to_num(w[b, h, x:], -9)) if in_place else torch.all(rest == SENT)
+            assert torch.all(gw[b, h, x:min(m, ocap)] == 0)  # where later rows start from
+            rest = gw[b, h, min(m, ocap):]
+            assert torch.equal(torch.nan_to_num(rest, -9), torch.nan_to_num(w[b, h, min(m, ocap):], -9)) if in_place else torch.all(rest == SENT)
         assert torch.all(gk[b, :, kv * dim:] == SENT) if not in_place else torch.equal(gk[b, :, kv * dim:], k[b, :, kv * dim:])
 
 
