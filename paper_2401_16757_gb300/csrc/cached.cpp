@@ -12,7 +12,11 @@
 
 namespace swapnet {
 
-// How many CTAs share the keys of a (sequence, key head, row tile): the count
+// Microseconds of the tensor-core kernel: a unit's start and end, a tile of
+// keys, the join of shared units.
+constexpr double kUnitUs = 5.0, kTileUs = 1.0, kJoinUs = 3.0;
+
+// How many CTAs share the keys of a (sequence, key head): the count
 // whose waves over the SMs take the least time, for the whole cache (how much
 // of it is filled only the device knows).  step / fixed: microseconds of a
 // CTA's tile of keys and of its start and end; more than one also pays the
@@ -37,15 +41,25 @@ CachedPlan cached_plan(const CachedArgs& a) {
   std::memset(&p, 0, sizeof(p));
   const int64_t rows = (int64_t)a.tokens * a.group, pairs = (int64_t)a.n_seq * a.kv_heads;
   p.tc = rows > 32;
-  if (p.tc) {
-    const int queries = (rows <= 64 ? 64 : 128) / a.group;
-    p.splits = choose_splits(pairs * ((a.tokens + queries - 1) / queries), (a.max_seq + 127) / 128 + (a.k_new ? 1 : 0), 1, 0.9, 3.0, 2.0);
-  } else {
-    p.splits = choose_splits(pairs, (a.max_seq + 63) / 64, 2, 0.5, 2.0, 2.0);
-  }
   p.spill = a.weights && rows <= 32;
+  if (p.tc) {
+    const int row_tile = rows <= 64 ? 64 : 128, queries = std::min(row_tile / a.group, a.tokens);
+    const int64_t units = pairs * ((a.tokens + queries - 1) / queries);
+    const double tiles = (a.max_seq + 127) / 128 + (a.k_new ? 1 : 0);
+    // a CTA per unit, or equal runs of all tiles and a join
+    const double alone = std::ceil((double)units / kRunCtas) * (kUnitUs + tiles * kTileUs);
+    const double shared = kUnitUs + std::max(2.0, units * tiles / kRunCtas) * kTileUs + (double)units / kRunCtas + kJoinUs;
+    p.splits = alone <= shared && units < (1ll << 31) ? 1 : 0;
+    if (p.splits == 0) {
+      p.part_bytes = align_up((uint64_t)2 * kRunCtas * row_tile * a.dim * 4);
+      p.ml_bytes = align_up((uint64_t)2 * kRunCtas * row_tile * 8);
+      p.unit_bytes = align_up((uint64_t)units * 8);
+    }
+    return p;
+  }
+  p.splits = choose_splits(pairs, (a.max_seq + 63) / 64, 2, 0.5, 2.0, 2.0);
   p.score_ld = (a.max_seq + 15) / 16 * 16;
-  const uint64_t all = (uint64_t)a.n_seq * a.kv_heads * rows;
+  const uint64_t all = (uint64_t)pairs * rows;
   if (p.splits > 1) p.part_bytes = align_up(all * p.splits * a.dim * 4);
   if (p.splits > 1 || p.spill) p.ml_bytes = align_up(all * p.splits * 8);
   if (p.spill) p.score_bytes = align_up(all * p.score_ld * 4);
@@ -71,8 +85,10 @@ int run_cached_attention(CachedArgs a, const CachedPlan& p, void* workspace, boo
   a.ml = reinterpret_cast<float*>(w + p.part_bytes);
   a.scores = p.spill ? reinterpret_cast<float*>(w + p.part_bytes + p.ml_bytes) : nullptr;
   a.score_ld = p.score_ld;
+  a.units = reinterpret_cast<int2*>(w + p.part_bytes + p.ml_bytes + p.score_bytes);
   if (int rc = p.tc ? launch_attention_rows(a, early, s) : launch_attention_few(a, early, s)) return rc;
-  if (int rc = launch_attention_join(a, s)) return rc;
+  if (!p.tc)
+    if (int rc = launch_attention_join(a, s)) return rc;
   return a.weights && !p.spill ? launch_weights(a, true, s) : SWAPNET_OK;
 }
 
@@ -114,7 +130,7 @@ void state_attention(const Model& m, char* state, int index, CachedArgs* out) {
 }
 
 int cached_launches(const CachedArgs& a, const CachedPlan& p) {
-  return 1 + (p.splits > 1 || p.spill ? 1 : 0) + (a.weights && !p.spill ? 1 : 0);
+  return 1 + (p.splits != 1 || p.spill ? 1 : 0) + (a.weights && !p.spill ? 1 : 0);
 }
 
 namespace {

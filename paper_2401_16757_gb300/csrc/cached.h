@@ -33,21 +33,24 @@ struct CachedArgs {
   int splits;
   float *part, *ml, *scores;
   int64_t score_ld;
+  int2* units;  // tensor-core kernel, runs: per unit its first CTA and how many share it
 };
+constexpr int kRunCtas = 152;  // CTAs that share the tiles of all units: one per SM
 
 // How a call runs, from its sizes alone.
 struct CachedPlan {
   int tc;       // tensor-core kernel (rows in tiles of 128)
-  int splits;   // CTAs that share the keys of a (sequence, key head)
+  int splits;   // few rows: CTAs that share the keys of a (sequence, key head);
+                // tensor cores: 1: a CTA per unit, 0: equal runs of all tiles
   int spill;    // weights from stored scores; 0: from a second pass over the keys
   int64_t score_ld;
-  uint64_t part_bytes, ml_bytes, score_bytes;
+  uint64_t part_bytes, ml_bytes, score_bytes, unit_bytes;
 };
 CachedPlan cached_plan(const CachedArgs& a);
 // Attention as that plan says, its workspace at `workspace`; weights too where
 // asked for.  early: the launch may start while the one before it ends.
 int run_cached_attention(CachedArgs a, const CachedPlan& p, void* workspace, bool early, cudaStream_t s);
-inline uint64_t plan_bytes(const CachedPlan& p) { return p.part_bytes + p.ml_bytes + p.score_bytes; }
+inline uint64_t plan_bytes(const CachedPlan& p) { return p.part_bytes + p.ml_bytes + p.score_bytes + p.unit_bytes; }
 int cached_launches(const CachedArgs& a, const CachedPlan& p);
 
 int launch_attention_rows(const CachedArgs& a, bool early, cudaStream_t s);  // tcgen05

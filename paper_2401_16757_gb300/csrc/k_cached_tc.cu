@@ -3,13 +3,14 @@
 // arithmetic.
 //
 // Rows of a (sequence, key head) are its queries times the heads that share
-// the key head, query-major: row t * group + h.  One CTA owns up to 128 rows
-// and a share of the key tiles (128 keys each; the drafted nodes are one more
-// tile, the last):
+// the key head, query-major: row t * group + h.  A unit is up to 128 of them;
+// one CTA per SM takes units, or an equal run of all units' key tiles (128 keys
+// each; the drafted nodes are one more tile, the last), whatever the
+// sequences' lengths.  Per tile:
 //   S = Q K^T     tcgen05.mma, M 128 (rows) x N 128 (keys); Q, K and V by TMA
 //                 (128-byte swizzle); S in two TMEM buffers, so that the next
 //                 tile's S is computed during this tile's softmax
-//   P             warps 2..9, two threads per row: one takes the first 64 keys
+//   P             warps 4..11, two threads per row: one takes the first 64 keys
 //                 of every tile, the other the last 64, each with a softmax of
 //                 its own (reference m, sum l, output O_h), so no thread waits
 //                 for another.  Scores from TMEM, masks only in tiles that a
@@ -19,14 +20,13 @@
 // O_0 and O_1 stay in TMEM.  m is the running maximum only where that grew by
 // more than 2^8 since it was last taken (kSlack): until then p and l stay
 // within 2^8 of their usual range, which fp32 sums and both storage types hold
-// without loss, and O is neither read nor rescaled.  At the end the two
-// halves' results are joined in shared memory.
+// without loss, and O is neither read nor rescaled.
 // With at most 64 rows (REP 2) the rows appear twice in the MMA's 128, and
 // lanes 0..63 and 64..127 share a half's keys, so that all eight warps work
 // (the other 32 keys are zeros in a lane's P).
-// K and V tiles pass through one ring in the order they are used.  Every wait
-// is bounded: on timeout the kernel records kDevErrTimeout, drains the loads
-// and MMAs it started, frees TMEM and returns.
+// K and V tiles pass through one ring in the order they are used, across
+// units.  Every wait is bounded: on timeout the kernel records kDevErrTimeout,
+// drains the loads and MMAs it started, frees TMEM and returns.
 #include <algorithm>
 #include <cstring>
 #include <string>
@@ -42,6 +42,11 @@ namespace {
 
 constexpr int kSoftThreads = 256;
 constexpr int kTcThreads = 64 + kSoftThreads;
+// attention: warps 0 (TMA) and 1 (MMA), two idle ones that complete their
+// warpgroup, the softmax's eight; 384 x 168 registers at launch, of which
+// setmaxnreg leaves 128 x 72 and gives 256 x 216
+constexpr int kAtThreads = 128 + kSoftThreads;
+static_assert(128 * 72 + 256 * 216 <= kAtThreads * 168, "registers of a CTA");
 constexpr int kKeys = 128;       // keys of a tile
 constexpr float kSlack = 8.0f;   // log2 of what p may exceed 1 by
 constexpr uint32_t kTmemCols = 512;
@@ -60,10 +65,9 @@ template <int D> struct TcCfg {
   static constexpr int kOffPar = kOffX + 256 * 8;           // parents
   static constexpr int kOffOdd = kOffPar + kTreeMax * 4;    // odd value rows, a bit each
   static constexpr int kOffBar = kOffOdd + 16;
-  static constexpr int kSmem = kOffBar + 256 + 1024;        // + alignment slack
+  static constexpr int kOffStage = kOffBar + 256;           // REP 2: 32 columns of 2 x 64 rows
+  static constexpr int kSmem = kOffStage + 2 * 64 * 36 * 4 + 1024;  // + alignment slack
   static_assert(kSmem <= 232448, "shared memory of a CTA");
-  static constexpr int kORow = D + 4;                       // floats of a thread's output row
-  static_assert(kSlots * kTile >= 256 * kORow * 4, "the threads' outputs overlay the ring");
 };
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, uint32_t bar, int x, int y, int z) {
@@ -102,11 +106,82 @@ __device__ __forceinline__ uint64_t desc_mn(uint32_t addr) {
   return d;
 }
 
+// ------------------------------------------------------------- who does what
+// A unit is the rows [rt * queries, ...) of a (sequence, key head); pair =
+// b * nrt + rt, unit = pair * kv_heads + key head.  With a.splits == 1 CTA c
+// owns unit c.  Otherwise the units' tiles, in order, are cut into gridDim.x
+// equal runs, one per CTA, whatever the sequences' lengths: a unit may be
+// spread over CTAs that follow one another, whose results meet in the join.
+// Every valid unit has at least one tile.
+constexpr int kRunTiles = 2;  // of a run, where there are too few tiles for all CTAs
+struct PairSize {
+  int len, count, np, tiles;  // np: tiles of the cache, then one of the draft
+};
+__device__ __forceinline__ PairSize pair_size(const CachedArgs& a, int b, int rt, int queries) {
+  PairSize p;
+  p.len = a.lens[b * a.lens_step] + a.len_add;
+  p.count = a.counts ? a.counts[b * a.counts_step] : a.tokens;
+  p.np = p.tiles = 0;
+  if (p.len < 0 || p.len > a.max_seq || p.count < 0 || p.count > a.tokens || rt * queries >= p.count) return p;
+  const int last = min((rt + 1) * queries, p.count) - 1;
+  p.np = (visible_limit(a, p.len, p.count, last) + kKeys - 1) / kKeys;
+  if (!a.k_new && p.np == 0) p.np = 1;  // (nothing to see: zeros are written)
+  p.tiles = p.np + (a.k_new ? 1 : 0);
+  return p;
+}
+
+// A CTA's run of tiles, piece by piece (a piece: its part of one unit).
+struct Cursor {
+  int64_t left;            // tiles of the run from the next piece on
+  int pair, kvh, next;     // unit and first tile of the next piece
+  // the current piece
+  int b, rt, h, i0, n;     // tiles [i0, i0 + n) of the unit
+  PairSize z;
+  __device__ __forceinline__ bool step(const CachedArgs& a, int nrt, int queries) {
+    while (left > 0 && pair < a.n_seq * nrt) {
+      b = pair / nrt;
+      rt = pair % nrt;
+      z = pair_size(a, b, rt, queries);
+      if (z.tiles > next) {
+        h = kvh;
+        i0 = next;
+        n = (int)min((int64_t)(z.tiles - next), left);
+        left -= n;
+        next += n;
+        if (next == z.tiles) {
+          next = 0;
+          if (++kvh == a.kv_heads) kvh = 0, ++pair;
+        }
+        return true;
+      }
+      next = kvh = 0;
+      ++pair;
+    }
+    return false;
+  }
+};
+
+__device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
+  float2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(reinterpret_cast<unsigned long long&>(r))
+      : "l"(reinterpret_cast<unsigned long long&>(x)), "l"(reinterpret_cast<unsigned long long&>(y)),
+        "l"(reinterpret_cast<unsigned long long&>(z)));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 x, float2 y) {
+  float2 r;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<unsigned long long&>(r))
+      : "l"(reinterpret_cast<unsigned long long&>(x)), "l"(reinterpret_cast<unsigned long long&>(y)));
+  return r;
+}
+
 template <typename T, int D, int REP>
-__global__ void __launch_bounds__(kTcThreads, 1)
+__global__ void __launch_bounds__(kAtThreads, 1)
     attention_rows_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                           const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmKn,
-                          const __grid_constant__ CUtensorMap tmVn, const __grid_constant__ CachedArgs a, int queries) {
+                          const __grid_constant__ CUtensorMap tmVn, const __grid_constant__ CachedArgs a, int queries, int nrt) {
   using F = TcCfg<D>;
   constexpr int kRowsMax = 128 / REP;
   constexpr int NK = 64 / REP;  // keys per thread and tile
@@ -118,52 +193,32 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + F::kOffBar);
   auto full = [&](int s) { return smem_u32(bars + s); };
   auto empty = [&](int s) { return smem_u32(bars + 8 + s); };
-  auto s_full = [&](int i) { return smem_u32(bars + 16 + i); };
-  auto p_full = [&](int h) { return smem_u32(bars + 18 + h); };
-  auto o_full = [&](int h) { return smem_u32(bars + 20 + h); };
-  const uint32_t q_full = smem_u32(bars + 22), done_bar = smem_u32(bars + 23);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 24);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 25);
+  auto s_full = [&](int i) { return smem_u32(bars + 16 + (i & 1)); };
+  // one per half and buffer: a half may be two tiles ahead of the products
+  auto p_full = [&](int h, int i) { return smem_u32(bars + 18 + 2 * h + (i & 1)); };
+  auto o_full = [&](int h) { return smem_u32(bars + 22 + h); };
+  const uint32_t q_full = smem_u32(bars + 24), q_free = smem_u32(bars + 25);  // a piece's queries
+  const uint32_t o_done = smem_u32(bars + 26), o_free = smem_u32(bars + 27);  // a piece's outputs
+  const uint32_t done_bar = smem_u32(bars + 28);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 29);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 30);
+  int64_t* sched = reinterpret_cast<int64_t*>(ml);  // (before the first results)
 
   const int warp = warp_index(), lane = threadIdx.x & 31;
-  const int split = (int)blockIdx.x % a.splits, t0 = (int)(blockIdx.x / a.splits) * queries;
-  const int kvh = blockIdx.y, b = blockIdx.z;
-  pdl_wait();
-  pdl_launch_dependents();
-  int len, count;
-  if (!seq_sizes(a, b, &len, &count)) return;
-  if (t0 >= count) return;
-  const int nq = min(queries, count - t0), rows = nq * a.group;
-  if (a.k_new && a.parents) {
-    bool bad = false;
-    for (int t = threadIdx.x; t < count; t += kTcThreads) {
-      const int p = a.parents[(int64_t)b * a.tokens + t];
-      par[t] = p;
-      bad = bad || p < -1 || p >= t;
-    }
-    if (__syncthreads_or(bad)) {
-      if (threadIdx.x == 0) atomicExch(a.err, kDevErrBounds);
-      return;
-    }
-  }
-  // this CTA's tiles [i0, i0 + n) of the prefix's np and, behind them, the draft
-  const int kmax = visible_limit(a, len, count, t0 + nq - 1), lim_min = visible_limit(a, len, count, t0);
-  const int np = (kmax + kKeys - 1) / kKeys, tiles = np + (a.k_new ? 1 : 0);
-  const int i0 = (int)((int64_t)tiles * split / a.splits), n = (int)((int64_t)tiles * (split + 1) / a.splits) - i0;
-  const int soft_warps = 2 * (REP == 2 ? 4 : (rows + 31) / 32);  // whose lanes hold rows
-
   if (threadIdx.x == 0) {
     for (int s = 0; s < F::kSlots; ++s) {
       mbar_init(full(s), 1);
       mbar_init(empty(s), 1);
     }
-    mbar_init(s_full(0), 1);
-    mbar_init(s_full(1), 1);
-    mbar_init(q_full, 1);
-    for (int h = 0; h < 2; ++h) {
-      mbar_init(p_full(h), soft_warps / 2);
-      mbar_init(o_full(h), 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(s_full(i), 1);
+      mbar_init(o_full(i), 1);
+      for (int h = 0; h < 2; ++h) mbar_init(p_full(h, i), 4);
     }
+    mbar_init(q_full, 1);
+    mbar_init(q_free, 1);
+    mbar_init(o_done, 1);
+    mbar_init(o_free, 8);
     mbar_init(done_bar, 1);
     *abort_flag = 0;
 #pragma unroll
@@ -177,347 +232,485 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     tmem_alloc(smem_u32(tmem_slot), kTmemCols);
     tmem_relinquish();
   }
-  tc_fence_before();
-  __syncthreads();
+  pdl_wait();
+  pdl_launch_dependents();
+  Cursor cur;
+  cur.next = 0;
+  int64_t first_tile = 0, total = 0;  // the run's first tile in the order of all; their number
+  int runs = 1;
+  if (a.splits == 1) {
+    cur.pair = blockIdx.x / a.kv_heads;
+    cur.kvh = blockIdx.x % a.kv_heads;
+    const PairSize z = pair_size(a, cur.pair / nrt, cur.pair % nrt, queries);
+    cur.left = z.tiles;
+    if (z.tiles == 0 && threadIdx.x == 0 && cur.kvh == 0) {
+      int len, count;
+      seq_sizes(a, cur.pair / nrt, &len, &count);  // (reports what is out of range)
+    }
+    tc_fence_before();
+    __syncthreads();
+  } else {
+    // every thread adds up a run of pairs, then the threads' sums
+    const int pairs = a.n_seq * nrt, per = (pairs + kAtThreads - 1) / kAtThreads;
+    const int p0 = min((int)threadIdx.x * per, pairs), p1 = min(p0 + per, pairs);
+    int64_t sum = 0;
+    for (int p = p0; p < p1; ++p) {
+      sum += (int64_t)pair_size(a, p / nrt, p % nrt, queries).tiles * a.kv_heads;
+      if (blockIdx.x == 0) {
+        const int b = p / nrt, n = a.lens[b * a.lens_step] + a.len_add, c = a.counts ? a.counts[b * a.counts_step] : a.tokens;
+        if (n < 0 || n > a.max_seq || c < 0 || c > a.tokens) atomicExch(a.err, kDevErrBounds);
+      }
+    }
+    int64_t before = sum;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int64_t o = __shfl_up_sync(0xffffffffu, before, off);
+      if (lane >= off) before += o;
+    }
+    if (lane == 31) sched[warp] = before;
+    before -= sum;
+    tc_fence_before();
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kAtThreads / 32; ++w) {
+      if (w < warp) before += sched[w];
+      total += sched[w];
+    }
+    runs = (int)min((int64_t)gridDim.x, (total + kRunTiles - 1) / kRunTiles);
+    first_tile = (int)blockIdx.x < runs ? total * blockIdx.x / runs : total;
+    cur.left = (int)blockIdx.x < runs ? total * (blockIdx.x + 1) / runs - first_tile : 0;
+    cur.pair = cur.kvh = 0;
+    if (cur.left > 0 && before <= first_tile && first_tile < before + sum) {
+      int64_t at = before;
+      for (int p = p0; p < p1; ++p) {
+        const int tiles = pair_size(a, p / nrt, p % nrt, queries).tiles;
+        if (first_tile < at + (int64_t)tiles * a.kv_heads) {
+          sched[16] = p;
+          sched[17] = first_tile - at;  // in (key head, tile) order
+          sched[18] = tiles;
+          break;
+        }
+        at += (int64_t)tiles * a.kv_heads;
+      }
+    }
+    __syncthreads();
+    if (cur.left > 0) {
+      cur.pair = (int)sched[16];
+      cur.kvh = (int)(sched[17] / sched[18]);
+      cur.next = (int)(sched[17] % sched[18]);
+    }
+    __syncthreads();  // (sched is written again as ml)
+  }
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  // tiles in the order of use: K0, K1, V0, K2, V1, ..., V(n-1)
+  // a piece's tiles in the order of use: K0, K1, V0, K2, V1, ..., V(n-1)
   auto k_pos = [&](int i) { return i == 0 ? 0 : 2 * i - 1; };
-  auto v_pos = [&](int i) { return i == n - 1 ? 2 * n - 1 : 2 * i + 2; };
+  auto v_pos = [&](int i, int n) { return i == n - 1 ? 2 * n - 1 : 2 * i + 2; };
 
-  if (warp == 0) {
-    if (n > 0 && elect_one()) {
+  // the softmax warps take registers that the others leave
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (warp == 0 && elect_one()) {
       // ---------------- TMA producer
-      const int q_rows = queries * a.group;
-      mbar_arrive_expect_tx(q_full, REP * F::kHalves * q_rows * 128);
+      const int q_bytes = REP * F::kHalves * queries * a.group * 128;
+      int pos = 0, piece = 0;
+      bool ok = true;
+      for (; ok && cur.step(a, nrt, queries); ++piece) {
+        auto load = [&](int i, bool keys) -> bool {
+          const int s = pos % F::kSlots;
+          if (pos >= F::kSlots && !mbar_wait_bounded(empty(s), ((pos / F::kSlots) - 1) & 1, abort_flag, a.err)) return false;
+          mbar_arrive_expect_tx(full(s), F::kTile);
+          const bool nw = cur.i0 + i >= cur.z.np;
+          const CUtensorMap* tm = keys ? (nw ? &tmKn : &tmK) : (nw ? &tmVn : &tmV);
 #pragma unroll
-      for (int c = 0; c < REP; ++c)
+          for (int h = 0; h < F::kHalves; ++h)
+            tma_load_3d(smem_u32(smem + F::kOffRing + s * F::kTile + h * F::kBox), tm, full(s), cur.h * D + h * 64,
+                        nw ? 0 : (cur.i0 + i) * kKeys, cur.b);
+          ++pos;
+          return true;
+        };
+        ok = load(0, true) && (cur.n < 2 || load(1, true));
+        if (!ok) break;
+        if (piece > 0 && !mbar_wait_bounded(q_free, (piece - 1) & 1, abort_flag, a.err)) break;
+        mbar_arrive_expect_tx(q_full, q_bytes);
 #pragma unroll
-        for (int h = 0; h < F::kHalves; ++h)
-          tma_load_3d(smem_u32(smem + F::kOffQ + h * F::kBox + c * (kRowsMax * 128)), &tmQ, q_full, h * 64, kvh * a.group,
-                      b * a.tokens + t0);
-      int pos = 0;
-      auto load = [&](int i, bool keys) -> bool {
-        const int s = pos % F::kSlots;
-        if (pos >= F::kSlots && !mbar_wait_bounded(empty(s), ((pos / F::kSlots) - 1) & 1, abort_flag, a.err)) return false;
-        mbar_arrive_expect_tx(full(s), F::kTile);
-        const bool nw = i0 + i >= np;
-        const CUtensorMap* tm = keys ? (nw ? &tmKn : &tmK) : (nw ? &tmVn : &tmV);
+        for (int c = 0; c < REP; ++c)
 #pragma unroll
-        for (int h = 0; h < F::kHalves; ++h)
-          tma_load_3d(smem_u32(smem + F::kOffRing + s * F::kTile + h * F::kBox), tm, full(s), kvh * D + h * 64,
-                      nw ? 0 : (i0 + i) * kKeys, b);
-        ++pos;
-        return true;
-      };
-      bool ok = load(0, true) && (n < 2 || load(1, true));
-      for (int i = 0; ok && i < n; ++i) ok = load(i, false) && (i + 2 >= n || load(i + 2, true));
+          for (int h = 0; h < F::kHalves; ++h)
+            tma_load_3d(smem_u32(smem + F::kOffQ + h * F::kBox + c * (kRowsMax * 128)), &tmQ, q_full, h * 64, cur.h * a.group,
+                        cur.b * a.tokens + cur.rt * queries);
+        for (int i = 0; ok && i < cur.n; ++i) ok = load(i, false) && (i + 2 >= cur.n || load(i + 2, true));
+        if (!ok) {
+          ++piece;  // its queries are on their way
+          break;
+        }
+      }
       // let every load issued land before the CTA can exit
       volatile int no_abort = 0;
-      mbar_wait_bounded(q_full, 0, &no_abort, nullptr);
+      if (piece > 0) mbar_wait_bounded(q_full, (piece - 1) & 1, &no_abort, nullptr);
       for (int j = max(0, pos - F::kSlots); j < pos; ++j)
         mbar_wait_bounded(full(j % F::kSlots), (j / F::kSlots) & 1, &no_abort, nullptr);
     }
-  } else if (warp == 1) {
-    if (n > 0 && elect_one()) {
+    if (warp == 1 && elect_one()) {
       // ---------------- MMA issuer
       constexpr int bf = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
       constexpr uint32_t idesc_s = idesc_f16(bf, 128, kKeys);
       constexpr uint32_t idesc_pv = idesc_f16(bf, 128, D) | (1u << 16);  // B (values) MN-major
       const uint64_t qd = smem_desc_sw128(smem_u32(smem + F::kOffQ));
       const uint64_t kd = smem_desc_sw128(smem_u32(smem + F::kOffRing)), vd = desc_mn(smem_u32(smem + F::kOffRing));
-      auto scores = [&](int i) -> bool {
-        const int pos = k_pos(i), s = pos % F::kSlots;
-        if (!mbar_wait_bounded(full(s), (pos / F::kSlots) & 1, abort_flag, a.err)) return false;
-        tc_fence_after();
-        const uint64_t kt = kd + (uint64_t)(s * (F::kTile >> 4));  // the descriptors' address field counts 16 bytes
-#pragma unroll
-        for (int h = 0; h < F::kHalves; ++h)
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            tc_mma_f16(tmem + (uint32_t)(i & 1) * 128u, qd + (uint64_t)(h * (F::kBox >> 4) + 2 * k),
-                       kt + (uint64_t)(h * (F::kBox >> 4) + 2 * k), idesc_s, (h | k) != 0);
-        tc_commit(s_full(i & 1));
-        tc_commit(empty(s));
-        return true;
-      };
-      bool ok = mbar_wait_bounded(q_full, 0, abort_flag, a.err) && scores(0);
-      for (int i = 0; ok && i < n; ++i) {
-        if (i + 1 < n && !scores(i + 1)) break;
-        const int pos = v_pos(i), s = pos % F::kSlots;
-        if (!mbar_wait_bounded(full(s), (pos / F::kSlots) & 1, abort_flag, a.err)) break;
-        const uint64_t vt = vd + (uint64_t)(s * (F::kTile >> 4));
-        for (int h = 0; ok && h < 2; ++h) {
-          ok = mbar_wait_bounded(p_full(h), i & 1, abort_flag, a.err);
-          if (!ok) break;
+      int pos0 = 0, g0 = 0;  // of the piece: ring position, tiles before
+      bool ok = true;
+      for (int piece = 0; ok && cur.step(a, nrt, queries); ++piece) {
+        const int n = cur.n;
+        auto scores = [&](int i) -> bool {
+          const int pos = pos0 + k_pos(i), s = pos % F::kSlots, g = g0 + i;
+          if (!mbar_wait_bounded(full(s), (pos / F::kSlots) & 1, abort_flag, a.err)) return false;
+          // over the P of two tiles ago, once its product has read it; a
+          // piece's first scores come after all products before (those of tile
+          // g - 1 are on their way: of g - 2 alone could be asked no more)
+          if (i == 0 ? g > 0 : g >= 2)
+            if (!mbar_wait_bounded(o_full(1), (i == 0 ? g - 1 : g) & 1, abort_flag, a.err)) return false;
           tc_fence_after();
-          const uint32_t pt = tmem + (uint32_t)(i & 1) * 128u + (uint32_t)h * 64u;
+          const uint64_t kt = kd + (uint64_t)(s * (F::kTile >> 4));  // the descriptors' address field counts 16 bytes
 #pragma unroll
-          for (int part = 0; part < 2; ++part)
+          for (int h = 0; h < F::kHalves; ++h)
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks)  // 16 keys a step
-              tc_mma_f16_ta(tmem + kTmO + (uint32_t)h * 128u, pt + (uint32_t)(part * 32 + ks * 8),
-                            vt + (uint64_t)((h * 4 + ks) * (2048 >> 4)), idesc_pv, (uint32_t)(i | part | ks) != 0);
-          tc_commit(o_full(h));
+            for (int k = 0; k < 4; ++k)
+              tc_mma_f16(tmem + (uint32_t)(g & 1) * 128u, qd + (uint64_t)(h * (F::kBox >> 4) + 2 * k),
+                         kt + (uint64_t)(h * (F::kBox >> 4) + 2 * k), idesc_s, (h | k) != 0);
+          tc_commit(s_full(g));
+          tc_commit(empty(s));
+          if (i == n - 1) tc_commit(q_free);
+          return true;
+        };
+        ok = mbar_wait_bounded(q_full, piece & 1, abort_flag, a.err) && scores(0);
+        for (int i = 0; ok && i < n; ++i) {
+          if (i + 1 < n && !(ok = scores(i + 1))) break;
+          const int pos = pos0 + v_pos(i, n), s = pos % F::kSlots, g = g0 + i;
+          ok = mbar_wait_bounded(full(s), (pos / F::kSlots) & 1, abort_flag, a.err) &&
+               (i > 0 || piece == 0 || mbar_wait_bounded(o_free, (piece - 1) & 1, abort_flag, a.err));
+          const uint64_t vt = vd + (uint64_t)(s * (F::kTile >> 4));
+          for (int h = 0; ok && h < 2; ++h) {
+            ok = mbar_wait_bounded(p_full(h, g), (g >> 1) & 1, abort_flag, a.err);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t pt = tmem + (uint32_t)(g & 1) * 128u + (uint32_t)h * 64u;
+#pragma unroll
+            for (int part = 0; part < 2; ++part)
+#pragma unroll
+              for (int ks = 0; ks < 4; ++ks)  // 16 keys a step
+                tc_mma_f16_ta(tmem + kTmO + (uint32_t)h * 128u, pt + (uint32_t)(part * 32 + ks * 8),
+                              vt + (uint64_t)((h * 4 + ks) * (2048 >> 4)), idesc_pv, (uint32_t)(i | part | ks) != 0);
+            tc_commit(o_full(h));
+          }
+          if (ok) tc_commit(empty(s));
         }
-        tc_commit(empty(s));
+        if (ok) tc_commit(o_done);
+        pos0 += 2 * n;
+        g0 += n;
       }
       // every MMA issued must have finished before TMEM is freed
       tc_commit(done_bar);
       volatile int no_abort = 0;
       mbar_wait_bounded(done_bar, 0, &no_abort, nullptr);
     }
-  } else if (REP == 2 || (warp & 3) * 32 < rows) {
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     // ---------------- softmax and output
-    const int q4 = warp & 3, half = (warp - 2) >> 2;
+    const int q4 = warp & 3, half = (warp - 4) >> 2;
     const int slot = q4 * 32 + lane, rep = slot / kRowsMax, row = slot % kRowsMax;
-    const int active = 32 * soft_warps, aid = (half * (soft_warps / 2) + q4) * 32 + lane;
-    const int t = t0 + min(row, rows - 1) / a.group;
-    const int lim = visible_limit(a, len, count, t);
+    const int aid = (warp - 4) * 32 + lane;
     const int kofs = half * 64 + rep * NK;  // this thread's first key of a tile
     const uint32_t lane_off = (uint32_t)(q4 * 32) << 16;
     const uint32_t tO = tmem + kTmO + (uint32_t)half * 128u + lane_off;
-    auto all_sync = [&]() { asm volatile("bar.sync 5, %0;" ::"r"(active) : "memory"); };
-    float m = -INFINITY, l = 0.f;  // m: the reference, in log2 units
+    auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory"); };
+    auto all_sync = [&]() { asm volatile("bar.sync 5, 256;" ::: "memory"); };
     bool ok = true;
-    for (int i = 0; i < n; ++i) {
-      const bool nw = i0 + i >= np;
-      const int k0 = nw ? 0 : (i0 + i) * kKeys;
-      const bool masked = nw || k0 + kKeys > lim_min;  // some of these keys are hidden from some rows
-      const uint32_t tS = tmem + (uint32_t)(i & 1) * 128u + lane_off;
-      ok = ok && mbar_wait_bounded(s_full(i & 1), (i >> 1) & 1, abort_flag, a.err);
-      ok = __all_sync(0xffffffffu, ok);
-      tc_fence_after();
-      uint32_t hi[NK / 2], lo[NK / 2];
-      if (ok) {
-        uint32_t s[NK];
+    int pos0 = 0, g0 = 0;
+    for (int piece = 0; cur.step(a, nrt, queries); ++piece) {
+      const int b = cur.b, kvh = cur.h, n = cur.n, np = cur.z.np, len = cur.z.len, count = cur.z.count;
+      const int t0 = cur.rt * queries, rows = min(queries, count - t0) * a.group;
+      const int lim_min = visible_limit(a, len, count, t0);
+      const bool last = cur.i0 + n == cur.z.tiles, whole = cur.i0 == 0 && last;  // a piece up to the unit's end; all of it
+      const bool works = q4 * 32 % kRowsMax < rows;  // the warp's lanes hold rows
+      const int t = t0 + min(row, rows - 1) / a.group;
+      const int lim = visible_limit(a, len, count, t);
+      bool bad = false;  // a parent that is none
+      if (a.parents && last) {
+        all_sync();  // the piece before has read its parents
+        for (int i = aid; i < count; i += kSoftThreads) par[i] = a.parents[(int64_t)b * a.tokens + i];
+        all_sync();
+        for (int i = lane; i < count; i += 32) bad = bad || par[i] < -1 || par[i] >= i;
+        bad = __any_sync(0xffffffffu, bad);
+        if (bad && aid == 0) atomicExch(a.err, kDevErrBounds);
+      }
+      float m = -INFINITY, l = 0.f;  // m: the reference, in log2 units
+      for (int i = 0; i < n; ++i) {
+        const int g = g0 + i;
+        const bool nw = cur.i0 + i >= np;
+        const int k0 = nw ? 0 : (cur.i0 + i) * kKeys;
+        const bool masked = nw || k0 + kKeys > lim_min;  // some of these keys are hidden from some rows
+        const uint32_t tS = tmem + (uint32_t)(g & 1) * 128u + lane_off;
+        ok = ok && mbar_wait_bounded(s_full(g), (g >> 1) & 1, abort_flag, a.err);
+        ok = __all_sync(0xffffffffu, ok);
+        tc_fence_after();
+        uint32_t hi[NK / 2], lo[NK / 2];
+        if (ok && works) {
+          uint32_t s[NK];
 #pragma unroll
-        for (int c = 0; c < NK; c += 32) {
-          uint32_t(&r)[32] = *reinterpret_cast<uint32_t(*)[32]>(s + c);
-          tmem_ld_32x32b_x32(tS + (uint32_t)(kofs + c), r);
-        }
-        tmem_ld_wait();
-        if (masked) {
-          uint32_t see[NK / 32];
+          for (int c = 0; c < NK; c += 32) {
+            uint32_t(&r)[32] = *reinterpret_cast<uint32_t(*)[32]>(s + c);
+            tmem_ld_32x32b_x32(tS + (uint32_t)(kofs + c), r);
+          }
+          tmem_ld_wait();
+          if (masked) {
+            uint32_t see[NK / 32];
 #pragma unroll
-          for (int w = 0; w < NK / 32; ++w) see[w] = 0;
-          if (nw && a.parents) {
-            for (int j = t; j >= 0; j = par[j]) {
+            for (int w = 0; w < NK / 32; ++w) see[w] = 0;
+            if (nw && a.parents) {
+              for (int j = bad ? -1 : t; j >= 0; j = par[j]) {
 #pragma unroll
-              for (int w = 0; w < NK / 32; ++w)
-                if ((j - kofs) >> 5 == w) see[w] |= 1u << ((j - kofs) & 31);
+                for (int w = 0; w < NK / 32; ++w)
+                  if ((j - kofs) >> 5 == w) see[w] |= 1u << ((j - kofs) & 31);
+              }
+            } else {
+              const int seen = (nw ? t + 1 : lim - k0) - kofs;
+#pragma unroll
+              for (int w = 0; w < NK / 32; ++w) see[w] = seen >= 32 * w + 32 ? 0xffffffffu : seen > 32 * w ? (1u << (seen - 32 * w)) - 1u : 0u;
             }
-          } else {
-            const int seen = (nw ? t + 1 : lim - k0) - kofs;
 #pragma unroll
-            for (int w = 0; w < NK / 32; ++w) see[w] = seen >= 32 * w + 32 ? 0xffffffffu : seen > 32 * w ? (1u << (seen - 32 * w)) - 1u : 0u;
+            for (int k = 0; k < NK; ++k)
+              if (!(see[k >> 5] >> (k & 31) & 1u)) s[k] = 0xff800000u;  // -inf
           }
+          float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int k = 0; k < NK; ++k)
-            if (!(see[k >> 5] >> (k & 31) & 1u)) s[k] = 0xff800000u;  // -inf
-        }
-        float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          for (int k = 0; k < NK; ++k) mx4[k & 3] = fmaxf(mx4[k & 3], __uint_as_float(s[k]));
+          const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * a.scale_log2;
+          const bool grow = mx - m > kSlack;  // (also the first key seen)
+          if (__any_sync(0xffffffffu, grow)) {
+            float alpha = 1.f;
+            if (grow) {
+              alpha = ex2(m - mx);
+              m = mx;
+              l *= alpha;
+            }
+            if (i > 0) {  // O is at rest once the product of the tile before is done (the one before that is: these scores came after it)
+              ok = mbar_wait_bounded(o_full(half), (g - 1) & 1, abort_flag, a.err);
+              ok = __all_sync(0xffffffffu, ok);
+              tc_fence_after();
+              if (ok) {
 #pragma unroll
-        for (int k = 0; k < NK; ++k) mx4[k & 3] = fmaxf(mx4[k & 3], __uint_as_float(s[k]));
-        const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * a.scale_log2;
-        const bool grow = mx - m > kSlack;  // (also the first key seen)
-        if (__any_sync(0xffffffffu, grow)) {
-          float alpha = 1.f;
-          if (grow) {
-            alpha = ex2(m - mx);
-            m = mx;
-            l *= alpha;
-          }
-          if (i > 0) {  // O is at rest once the product of the tile before is done
-            ok = mbar_wait_bounded(o_full(half), (i - 1) & 1, abort_flag, a.err);
-            ok = __all_sync(0xffffffffu, ok);
-            tc_fence_after();
-            if (ok) {
+                for (int c = 0; c < D; c += 16) {
+                  uint32_t r[16];
+                  tmem_ld_32x32b_x16(tO + (uint32_t)c, r);
+                  tmem_ld_wait();
 #pragma unroll
-              for (int c = 0; c < D; c += 16) {
-                uint32_t r[16];
-                tmem_ld_32x32b_x16(tO + (uint32_t)c, r);
-                tmem_ld_wait();
-#pragma unroll
-                for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * alpha);
-                tmem_st_x16(tO + (uint32_t)c, r);
+                  for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * alpha);
+                  tmem_st_x16(tO + (uint32_t)c, r);
+                }
               }
             }
           }
-        }
-        const float base = m == -INFINITY ? 0.f : m;
-        float sum4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < NK / 2; ++k) {
-          const float p0 = ex2(fmaf(__uint_as_float(s[2 * k]), a.scale_log2, -base));
-          const float p1 = ex2(fmaf(__uint_as_float(s[2 * k + 1]), a.scale_log2, -base));
-          sum4[2 * (k & 1)] += p0;
-          sum4[2 * (k & 1) + 1] += p1;
-          hi[k] = pack_pair<T>(p0, p1);
-          const float2 back = unpack_pair<T>(hi[k]);
-          lo[k] = pack_pair<T>(p0 - back.x, p1 - back.y);
-        }
-        l += (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
-      }
-      uint32_t odd = 0;
-      if (masked) {
-        // A value row that some of the rows do not see must not reach them
-        // even if it is infinite or not a number (0 x inf): rows behind the
-        // last key are cleared, others that hold such a value as well, and
-        // added by hand below where they are seen.
-        const int pos = v_pos(i);
-        uint8_t* vs = smem + F::kOffRing + (pos % F::kSlots) * F::kTile;
-        ok = ok && mbar_wait_bounded(full(pos % F::kSlots), (pos / F::kSlots) & 1, abort_flag, a.err);
-        ok = __all_sync(0xffffffffu, ok);
-        const int have = min(kKeys, nw ? count : len - k0);
-        auto chunk = [&](int r, int c) {
-          return reinterpret_cast<uint4*>(vs + (c >> 3) * F::kBox + r * 128 + (((c & 7) ^ (r & 7)) << 4));
-        };
-        if (ok) {
-          for (int c = aid; c < kKeys * (D / 8); c += active) {
-            const int r = c / (D / 8);
-            uint4* at = chunk(r, c % (D / 8));
-            if (r >= have) {
-              *at = make_uint4(0u, 0u, 0u, 0u);
-            } else {
-              const uint4 v = *at;
-              if (odd_pair<T>(v.x) || odd_pair<T>(v.y) || odd_pair<T>(v.z) || odd_pair<T>(v.w)) atomicOr(&odd_rows[r >> 5], 1u << (r & 31));
-            }
-          }
-        }
-        all_sync();
-        odd = odd_rows[0] | odd_rows[1] | odd_rows[2] | odd_rows[3];
-        if (odd) {
-          for (int c = aid; c < kKeys * (D / 8); c += active) {
-            const int r = c / (D / 8);
-            if (odd_rows[r >> 5] >> (r & 31) & 1u) *chunk(r, c % (D / 8)) = make_uint4(0u, 0u, 0u, 0u);
-          }
-        }
-        fence_proxy_async_smem();  // V is read by the tensor cores (async proxy)
-        all_sync();                // by either half's product
-      }
-      if (ok) {
-        // over the half's 64 scores: hi parts of its 64 keys, then the lo parts
-#pragma unroll
-        for (int part = 0; part < 2; ++part) {
-          const uint32_t* x = part ? lo : hi;
-          const uint32_t to = tS + (uint32_t)(half * 64 + part * 32);
-          if (REP == 1) {
-            tmem_st_x16(to, x);
-            tmem_st_x16(to + 16u, x + (NK / 2 - 16));
-          } else {
-            uint32_t z[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) z[e] = 0;
-            tmem_st_x16(to + (uint32_t)rep * 16u, x);
-            tmem_st_x16(to + (uint32_t)(rep ^ 1) * 16u, z);
-          }
-        }
-        tmem_st_wait();
-        // Not before the product of the tile before is done: the barrier
-        // counts one tile at a time, and the scores of the next one are there
-        // early (a half two tiles ahead of the products would be waited for
-        // in the wrong phase).
-        if (i > 0) {
-          ok = mbar_wait_bounded(o_full(half), (i - 1) & 1, abort_flag, a.err);
-          ok = __all_sync(0xffffffffu, ok);
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0 && ok) mbar_arrive(p_full(half));
-      }
-      if (odd) {
-        ok = ok && mbar_wait_bounded(o_full(half), i & 1, abort_flag, a.err);
-        ok = __all_sync(0xffffffffu, ok);
-        tc_fence_after();
-        for (int j = 0; j < kKeys; ++j) {
-          if (!(odd_rows[j >> 5] >> (j & 31) & 1u)) continue;
-          const int rel = j - kofs;
-          if (rel < 0 || rel >= NK || !ok) continue;  // (the same for all lanes of a warp)
-          float pj = 0.f;
+          const float base = m == -INFINITY ? 0.f : m;
+          const float2 scale2 = make_float2(a.scale_log2, a.scale_log2), base2 = make_float2(-base, -base), minus = make_float2(-1.f, -1.f);
+          float2 sum2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
           for (int k = 0; k < NK / 2; ++k) {
-            const float2 h2 = unpack_pair<T>(hi[k]), l2 = unpack_pair<T>(lo[k]);
-            if (rel == 2 * k) pj = h2.x + l2.x;
-            if (rel == 2 * k + 1) pj = h2.y + l2.y;
+            const float2 x = fma2(make_float2(__uint_as_float(s[2 * k]), __uint_as_float(s[2 * k + 1])), scale2, base2);
+            const float2 p = make_float2(ex2(x.x), ex2(x.y));
+            sum2[k & 1] = add2(sum2[k & 1], p);
+            hi[k] = pack_pair<T>(p.x, p.y);
+            const float2 rest = fma2(unpack_pair<T>(hi[k]), minus, p);
+            lo[k] = pack_pair<T>(rest.x, rest.y);
           }
-          const T* v = nw ? static_cast<const T*>(a.v_new) + ((int64_t)b * a.tokens + j) * a.new_stride
-                          : static_cast<const T*>(a.v) + (int64_t)b * a.seq_stride + (int64_t)(k0 + j) * a.kv_stride;
-          v += kvh * D;
-          for (int c = 0; c < D; c += 16) {
-            uint32_t r[16];
-            tmem_ld_32x32b_x16(tO + (uint32_t)c, r);
-            tmem_ld_wait();
+          l += (sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y);
+        }
+        uint32_t odd = 0;
+        if (masked) {
+          // A value row that some of the rows do not see must not reach them
+          // even if it is infinite or not a number (0 x inf): rows behind the
+          // last key are cleared, others that hold such a value as well, and
+          // added by hand below where they are seen.
+          const int pos = pos0 + v_pos(i, n);
+          uint8_t* vs = smem + F::kOffRing + (pos % F::kSlots) * F::kTile;
+          ok = ok && mbar_wait_bounded(full(pos % F::kSlots), (pos / F::kSlots) & 1, abort_flag, a.err);
+          ok = __all_sync(0xffffffffu, ok);
+          const int have = min(kKeys, nw ? count : len - k0);
+          auto chunk = [&](int r, int c) {
+            return reinterpret_cast<uint4*>(vs + (c >> 3) * F::kBox + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+          };
+          if (ok) {
+            for (int c = aid; c < kKeys * (D / 8); c += kSoftThreads) {
+              const int r = c / (D / 8);
+              uint4* at = chunk(r, c % (D / 8));
+              if (r >= have) {
+                *at = make_uint4(0u, 0u, 0u, 0u);
+              } else {
+                const uint4 v = *at;
+                if (odd_pair<T>(v.x) || odd_pair<T>(v.y) || odd_pair<T>(v.z) || odd_pair<T>(v.w)) atomicOr(&odd_rows[r >> 5], 1u << (r & 31));
+              }
+            }
+          }
+          all_sync();
+          odd = odd_rows[0] | odd_rows[1] | odd_rows[2] | odd_rows[3];
+          if (odd) {
+            for (int c = aid; c < kKeys * (D / 8); c += kSoftThreads) {
+              const int r = c / (D / 8);
+              if (odd_rows[r >> 5] >> (r & 31) & 1u) *chunk(r, c % (D / 8)) = make_uint4(0u, 0u, 0u, 0u);
+            }
+          }
+          fence_proxy_async_smem();  // V is read by the tensor cores (async proxy)
+          all_sync();                // by either half's product
+        }
+        if (ok) {
+          if (works) {
+            // over the half's 64 scores: hi parts of its 64 keys, then the lo parts
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-              if (pj != 0.f) r[e] = __float_as_uint(fmaf(pj, to_f<T>(v[c + e]), __uint_as_float(r[e])));
-            tmem_st_x16(tO + (uint32_t)c, r);
+            for (int part = 0; part < 2; ++part) {
+              const uint32_t* x = part ? lo : hi;
+              const uint32_t to = tS + (uint32_t)(half * 64 + part * 32);
+              if (REP == 1) {
+                tmem_st_x16(to, x);
+                tmem_st_x16(to + 16u, x + (NK / 2 - 16));
+              } else {
+                uint32_t z[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) z[e] = 0;
+                tmem_st_x16(to + (uint32_t)rep * 16u, x);
+                tmem_st_x16(to + (uint32_t)(rep ^ 1) * 16u, z);
+              }
+            }
             tmem_st_wait();
           }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(p_full(half, g));
         }
-        all_sync();  // everyone has read the odd rows
-        if (aid < 4) odd_rows[aid] = 0;
-        all_sync();
+        if (odd) {
+          ok = ok && mbar_wait_bounded(o_full(half), g & 1, abort_flag, a.err);
+          ok = __all_sync(0xffffffffu, ok);
+          tc_fence_after();
+          for (int j = 0; j < kKeys; ++j) {
+            if (!(odd_rows[j >> 5] >> (j & 31) & 1u)) continue;
+            const int rel = j - kofs;
+            if (rel < 0 || rel >= NK || !ok || !works) continue;  // (the same for all lanes of a warp)
+            float pj = 0.f;
+#pragma unroll
+            for (int k = 0; k < NK / 2; ++k) {
+              const float2 h2 = unpack_pair<T>(hi[k]), l2 = unpack_pair<T>(lo[k]);
+              if (rel == 2 * k) pj = h2.x + l2.x;
+              if (rel == 2 * k + 1) pj = h2.y + l2.y;
+            }
+            const T* v = nw ? static_cast<const T*>(a.v_new) + ((int64_t)b * a.tokens + j) * a.new_stride
+                            : static_cast<const T*>(a.v) + (int64_t)b * a.seq_stride + (int64_t)(k0 + j) * a.kv_stride;
+            v += kvh * D;
+            for (int c = 0; c < D; c += 16) {
+              uint32_t r[16];
+              tmem_ld_32x32b_x16(tO + (uint32_t)c, r);
+              tmem_ld_wait();
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                if (pj != 0.f) r[e] = __float_as_uint(fmaf(pj, to_f<T>(v[c + e]), __uint_as_float(r[e])));
+              tmem_st_x16(tO + (uint32_t)c, r);
+              tmem_st_wait();
+            }
+          }
+          all_sync();  // everyone has read the odd rows
+          if (aid < 4) odd_rows[aid] = 0;
+          all_sync();
+        }
       }
-    }
-    // ---- the rows' results: the 2 REP softmaxes of a row meet in shared
-    // memory (every load and product of the ring has ended)
-    if (n > 0) {  // (the products before these two are done: the wait above, and their order)
-      for (int h = 0; h < 2; ++h) ok = ok && mbar_wait_bounded(o_full(h), (n - 1) & 1, abort_flag, a.err);
+      // ---- the piece's results: a thread joins the two halves of its row in
+      // half of the columns, and with REP 2 the row's two lanes meet in shared
+      // memory
+      ok = ok && mbar_wait_bounded(o_done, piece & 1, abort_flag, a.err);
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
-    }
-    float* ov = reinterpret_cast<float*>(smem + F::kOffRing);
-    if (n > 0 && ok) {
+      ml[half * 128 + slot] = make_float2(m, l);
+      if (REP == 1) pair_sync(); else all_sync();
+      float M = -INFINITY, L = 0.f, f[2];
 #pragma unroll
-      for (int c = 0; c < D; c += 32) {
-        uint32_t r[32];
-        tmem_ld_32x32b_x32(tO + (uint32_t)c, r);
-        tmem_ld_wait();
-        float4* to = reinterpret_cast<float4*>(ov + (half * 128 + slot) * F::kORow + c);
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          to[e] = make_float4(__uint_as_float(r[4 * e]), __uint_as_float(r[4 * e + 1]), __uint_as_float(r[4 * e + 2]),
-                              __uint_as_float(r[4 * e + 3]));
-      }
-    }
-    ml[half * 128 + slot] = make_float2(m, l);
-    all_sync();
-    const int64_t first = (((int64_t)b * a.kv_heads + kvh) * a.splits + split) * a.tokens * a.group + (int64_t)t0 * a.group;
-    for (int c = aid; ok && c < rows * (D / 4); c += active) {
-      const int r = c / (D / 4), col = c % (D / 4) * 4;
-      float2 st[2 * REP];
-      float M = -INFINITY, L = 0.f;
-#pragma unroll
-      for (int u = 0; u < 2 * REP; ++u) {
-        st[u] = ml[u * kRowsMax + r];  // (half-major, then the copies of the rows)
-        M = fmaxf(M, st[u].x);
-      }
+      for (int u = 0; u < 2 * REP; ++u) M = fmaxf(M, ml[u * kRowsMax + row].x);  // (half-major, then the copies of the rows)
       const float base = M == -INFINITY ? 0.f : M;
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int u = 0; u < 2 * REP; ++u) {
-        const float f = ex2(st[u].x - base);  // 0 where no key was seen
-        L = fmaf(st[u].y, f, L);
-        if (n > 0) {
-          const float4 x = *reinterpret_cast<const float4*>(ov + (u * kRowsMax + r) * F::kORow + col);
-          o.x = fmaf(x.x, f, o.x);
-          o.y = fmaf(x.y, f, o.y);
-          o.z = fmaf(x.z, f, o.z);
-          o.w = fmaf(x.w, f, o.w);
+        const float2 x = ml[u * kRowsMax + row];
+        L = fmaf(x.y, ex2(x.x - base), L);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) f[h] = ex2(ml[h * 128 + slot].x - base);  // 0 where no key was seen
+      const float inv = L > 0.f ? 1.0f / L : (L == 0.f ? 0.f : L);  // (a NaN stays one)
+      const bool writes = ok && !bad && row < rows && (REP == 1 || rep == 0);
+      const int tq = t0 + row / a.group, hd = kvh * a.group + row % a.group;
+      T* out = static_cast<T*>(a.out) + ((int64_t)b * a.tokens + tq) * a.out_stride + (int64_t)hd * D;
+      const int64_t part = ((int64_t)2 * blockIdx.x + (cur.i0 == 0 ? 1 : 0)) * kRowsMax + row;
+#pragma unroll
+      for (int c = 0; c < D / 2; c += 32) {
+        float o[32];
+        if (works) {
+          uint32_t r[32];
+          tmem_ld_32x32b_x32(tmem + kTmO + lane_off + (uint32_t)(half * (D / 2) + c), r);
+          tmem_ld_wait();
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(r[e]) * f[0];
+          tmem_ld_32x32b_x32(tmem + kTmO + 128u + lane_off + (uint32_t)(half * (D / 2) + c), r);
+          tmem_ld_wait();
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = fmaf(__uint_as_float(r[e]), f[1], o[e]);
+        }
+        if (REP == 2) {
+          float* stage = reinterpret_cast<float*>(smem + F::kOffStage) + (half * 64 + row) * 36;
+          if (rep == 1) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(stage + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          }
+          all_sync();
+          if (rep == 0) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              const float4 x = *reinterpret_cast<const float4*>(stage + e);
+              o[e] += x.x;
+              o[e + 1] += x.y;
+              o[e + 2] += x.z;
+              o[e + 3] += x.w;
+            }
+          }
+          all_sync();
+        }
+        if (writes) {
+          const int col = half * (D / 2) + c;
+          if (whole) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 8)
+              *reinterpret_cast<uint4*>(out + col + e) =
+                  make_uint4(pack_pair<T>(o[e] * inv, o[e + 1] * inv), pack_pair<T>(o[e + 2] * inv, o[e + 3] * inv),
+                             pack_pair<T>(o[e + 4] * inv, o[e + 5] * inv), pack_pair<T>(o[e + 6] * inv, o[e + 7] * inv));
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4)
+              *reinterpret_cast<float4*>(a.part + part * D + col + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          }
         }
       }
-      if (a.splits > 1) {
-        if (n > 0) *reinterpret_cast<float4*>(a.part + (first + r) * D + col) = o;
-        if (col == 0) reinterpret_cast<float2*>(a.ml)[first + r] = make_float2(M, L);
-        continue;
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0 && ok) mbar_arrive(o_free);
+      if (writes && half == 0) {
+        if (!whole)
+          reinterpret_cast<float2*>(a.ml)[part] = make_float2(M, L);
+        else if (a.lse)
+          a.lse[((int64_t)b * a.heads + hd) * a.tokens + tq] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
       }
-      const float inv = L > 0.f ? 1.0f / L : (L == 0.f ? 0.f : L);  // (a NaN stays one)
-      const int tq = t0 + r / a.group, hd = kvh * a.group + r % a.group;
-      T* to = static_cast<T*>(a.out) + ((int64_t)b * a.tokens + tq) * a.out_stride + (int64_t)hd * D + col;
-      *reinterpret_cast<uint2*>(to) = make_uint2(pack_pair<T>(o.x * inv, o.y * inv), pack_pair<T>(o.z * inv, o.w * inv));
-      if (col == 0 && a.lse)
-        a.lse[((int64_t)b * a.heads + hd) * a.tokens + tq] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+      if (a.splits != 1 && cur.i0 == 0 && aid == 0) {  // the unit's first CTA says how many share it
+        const int64_t end = first_tile + g0 + cur.z.tiles - 1;  // its last tile
+        int c = (int)(end * runs / total);  // whose run that is, up to the rounding
+        while (total * (c + 1) / runs <= end) ++c;
+        while (total * c / runs > end) --c;
+        a.units[((int64_t)b * nrt + cur.rt) * a.kv_heads + kvh] = make_int2((int)blockIdx.x, c - (int)blockIdx.x + 1);
+      }
+      if (REP == 1) pair_sync(); else all_sync();  // ml is written again
+      pos0 += 2 * n;
+      g0 += n;
     }
     tc_fence_before();
   }
@@ -830,6 +1023,61 @@ int rows_map(CUtensorMap* m, const CachedArgs& a, const void* base, int64_t rows
   return make_tmap_3d(m, a.dtype, base, dims, strides, box);
 }
 
+// The join of units that several CTAs shared: a warp per row, the pieces in
+// order.  A CTA holds at most two pieces that are not whole units: the rest of
+// one that began before its run (slot 2 c) and the start of one that goes on
+// behind it (slot 2 c + 1).
+template <typename T>
+__global__ void __launch_bounds__(256) attention_runs_join_kernel(const __grid_constant__ CachedArgs a, int queries, int nrt, int row_tile) {
+  pdl_wait();
+  const int kvh = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 31;
+  int len, count;
+  if (!seq_sizes(a, b, &len, &count)) return;
+  if (a.parents) {  // such a sequence's outputs stay as they were
+    bool bad = false;
+    for (int t = threadIdx.x; t < count; t += blockDim.x) {
+      const int p = a.parents[(int64_t)b * a.tokens + t];
+      bad = bad || p < -1 || p >= t;
+    }
+    if (__syncthreads_or(bad)) return;
+  }
+  const int r = (int)blockIdx.x * 8 + warp_index();
+  if (r >= count * a.group) return;
+  const int t = r / a.group, hd = kvh * a.group + r % a.group, rt = t / queries;
+  const int2 u = a.units[((int64_t)b * nrt + rt) * a.kv_heads + kvh];
+  if (u.y <= 1) return;
+  const int rl = (t - rt * queries) * a.group + r % a.group;
+  auto slot = [&](int p) { return ((int64_t)2 * (u.x + p) + (p == 0 ? 1 : 0)) * row_tile + rl; };
+  const float2* ml = reinterpret_cast<const float2*>(a.ml);
+  float M = -INFINITY, L = 0.f;
+  for (int p = lane; p < u.y; p += 32) M = fmaxf(M, ml[slot(p)].x);
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
+  const float base = M == -INFINITY ? 0.f : M;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int V = a.dim / 4;
+  for (int p = 0; p < u.y; ++p) {
+    const int64_t at = slot(p);
+    const float2 s = ml[at];
+    const float f = ex2(s.x - base);
+    L = fmaf(s.y, f, L);
+    if (lane < V && s.x != -INFINITY) {
+      const float4 y = reinterpret_cast<const float4*>(a.part)[at * V + lane];
+      x.x = fmaf(y.x, f, x.x);
+      x.y = fmaf(y.y, f, x.y);
+      x.z = fmaf(y.z, f, x.z);
+      x.w = fmaf(y.w, f, x.w);
+    }
+  }
+  const float inv = L > 0.f ? 1.0f / L : (L == 0.f ? 0.f : L);
+  if (lane < V) {
+    T* to = static_cast<T*>(a.out) + ((int64_t)b * a.tokens + t) * a.out_stride + (int64_t)hd * a.dim + lane * 4;
+    *reinterpret_cast<uint2*>(to) = make_uint2(pack_pair<T>(x.x * inv, x.y * inv), pack_pair<T>(x.z * inv, x.w * inv));
+  }
+  if (lane == 0 && a.lse)
+    a.lse[((int64_t)b * a.heads + hd) * a.tokens + t] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+}
+
 template <typename T, int D, int REP> int rows_t(const CachedArgs& a, bool early, cudaStream_t s) {
   static std::atomic<uint64_t> known{0};
   const auto kern = attention_rows_kernel<T, D, REP>;
@@ -852,8 +1100,9 @@ template <typename T, int D, int REP> int rows_t(const CachedArgs& a, bool early
   if (rc) return rc;
   cudaLaunchConfig_t cfg;
   std::memset(&cfg, 0, sizeof(cfg));
-  cfg.gridDim = dim3((a.tokens + queries - 1) / queries * a.splits, a.kv_heads, a.n_seq);
-  cfg.blockDim = dim3(kTcThreads);
+  const int nrt = (a.tokens + queries - 1) / queries;
+  cfg.gridDim = dim3(a.splits == 1 ? a.n_seq * nrt * a.kv_heads : kRunCtas);
+  cfg.blockDim = dim3(kAtThreads);
   cfg.dynamicSmemBytes = TcCfg<D>::kSmem;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
@@ -861,7 +1110,13 @@ template <typename T, int D, int REP> int rows_t(const CachedArgs& a, bool early
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = early ? 1 : 0;
-  return done(cudaLaunchKernelEx(&cfg, kern, q, k, v, kn, vn, a, queries), "cached attention launch");
+  rc = done(cudaLaunchKernelEx(&cfg, kern, q, k, v, kn, vn, a, queries, nrt), "cached attention launch");
+  if (rc || a.splits == 1) return rc;
+  cfg.gridDim = dim3((a.tokens * a.group + 7) / 8, a.kv_heads, a.n_seq);
+  cfg.blockDim = dim3(256);
+  cfg.dynamicSmemBytes = 0;
+  cfg.numAttrs = 1;
+  return done(cudaLaunchKernelEx(&cfg, attention_runs_join_kernel<T>, a, queries, nrt, 128 / REP), "cached attention join launch");
 }
 template <typename T, int D> int rows_d(const CachedArgs& a, bool early, cudaStream_t s) {
   return a.tokens * a.group <= 64 ? rows_t<T, D, 2>(a, early, s) : rows_t<T, D, 1>(a, early, s);
