@@ -14,7 +14,7 @@ namespace swapnet {
 
 // Microseconds of the tensor-core kernel: a unit's start and end, a tile of
 // keys, the join of shared units.
-constexpr double kUnitUs = 5.0, kTileUs = 1.0, kJoinUs = 3.0;
+constexpr double kUnitUs = 5.0, kTileUs = 1.0, kJoinUs = 8.0;
 
 // How many CTAs share the keys of a (sequence, key head): the count
 // whose waves over the SMs take the least time, for the whole cache (how much
@@ -46,14 +46,20 @@ CachedPlan cached_plan(const CachedArgs& a) {
     const int row_tile = rows <= 64 ? 64 : 128, queries = std::min(row_tile / a.group, a.tokens);
     const int64_t units = pairs * ((a.tokens + queries - 1) / queries);
     const double tiles = (a.max_seq + 127) / 128 + (a.k_new ? 1 : 0);
-    // a CTA per unit, or equal runs of all tiles and a join
-    const double alone = std::ceil((double)units / kRunCtas) * (kUnitUs + tiles * kTileUs);
-    const double shared = kUnitUs + std::max(2.0, units * tiles / kRunCtas) * kTileUs + (double)units / kRunCtas + kJoinUs;
-    p.splits = alone <= shared && units < (1ll << 31) ? 1 : 0;
+    // A CTA per unit, or equal runs of all tiles and a join.  From two units
+    // per SM on the block scheduler evens out what the runs would (512 units
+    // of up to 33 tiles: 275 against 283 us); below that the join's 8 us decide:
+    // 32 units of 5 tiles 14.9 against 18.4 us, 4 units of 1025 tiles about 1000
+    // against 50.
+    const int ctas = run_ctas(a.kv_heads);
+    const double alone = std::ceil((double)units / kSms) * (kUnitUs + tiles * kTileUs);
+    const double shared = kUnitUs + std::max(2.0, units * tiles / ctas) * kTileUs + (double)units / ctas + kJoinUs;
+    p.splits = units >= 2 * kSms || alone <= shared ? 1 : 0;
+    if (units > 0x7fffffff) p.splits = 0;
     if (p.splits == 0) {
-      p.part_bytes = align_up((uint64_t)2 * kRunCtas * row_tile * a.dim * 4);
-      p.ml_bytes = align_up((uint64_t)2 * kRunCtas * row_tile * 8);
-      p.unit_bytes = align_up((uint64_t)units * 8);
+      p.part_bytes = align_up((uint64_t)2 * ctas * row_tile * a.dim * 4);
+      p.ml_bytes = align_up((uint64_t)2 * ctas * row_tile * 8);
+      p.unit_bytes = align_up((uint64_t)ctas * 16);
     }
     return p;
   }
@@ -85,7 +91,7 @@ int run_cached_attention(CachedArgs a, const CachedPlan& p, void* workspace, boo
   a.ml = reinterpret_cast<float*>(w + p.part_bytes);
   a.scores = p.spill ? reinterpret_cast<float*>(w + p.part_bytes + p.ml_bytes) : nullptr;
   a.score_ld = p.score_ld;
-  a.units = reinterpret_cast<int2*>(w + p.part_bytes + p.ml_bytes + p.score_bytes);
+  a.units = reinterpret_cast<int4*>(w + p.part_bytes + p.ml_bytes + p.score_bytes);
   if (int rc = p.tc ? launch_attention_rows(a, early, s) : launch_attention_few(a, early, s)) return rc;
   if (!p.tc)
     if (int rc = launch_attention_join(a, s)) return rc;

@@ -4,6 +4,7 @@
 // been checked (cached.cpp).
 #pragma once
 #include <cuda_runtime.h>
+#include <algorithm>
 #include <cstdint>
 
 namespace swapnet {
@@ -33,9 +34,14 @@ struct CachedArgs {
   int splits;
   float *part, *ml, *scores;
   int64_t score_ld;
-  int2* units;  // tensor-core kernel, runs: per unit its first CTA and how many share it
+  int4* units;  // tensor-core kernel, runs: per CTA the unit that it begins and others go on with
+                // (sequence, row tile, key head, how many share it; 0: none)
 };
-constexpr int kRunCtas = 152;  // CTAs that share the tiles of all units: one per SM
+// CTAs that share the tiles of all units: as many runs for every key head as
+// find an SM each.
+constexpr int kSms = 152;
+inline int run_ctas(int kv_heads) { return std::max(1, kSms / kv_heads) * kv_heads; }
+
 
 // How a call runs, from its sizes alone.
 struct CachedPlan {

@@ -383,7 +383,7 @@ __device__ __forceinline__ float2 join_stats(const CachedArgs& a, int64_t first,
 
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __grid_constant__ CachedArgs a, int join_blocks) {
-  extern __shared__ float lse2[];  // the scores' rows
+  extern __shared__ float lse2[];  // of the scores' rows, then the keys that they see
   pdl_wait();
   const int kvh = blockIdx.y, b = blockIdx.z;
   int len, count;
@@ -428,21 +428,53 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
   }
   const int j0 = ((int)blockIdx.x - join_blocks) * kJoinKeys;
   if (j0 >= len) return;
+  const int64_t at = ((int64_t)b * a.kv_heads + kvh) * a.max_seq;
+  const float* sc = a.scores + ((int64_t)b * a.kv_heads + kvh) * step * a.score_ld + j0;
+  const bool all = j0 + kJoinKeys <= visible_limit(a, len, count, 0);  // every row sees every key of the block
+  // four keys per thread, the loads of four rows before their arithmetic
+  constexpr int K = kJoinKeys / kJoinThreads;
+  float w[K], x[4][K];
+  auto load = [&](int r0) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int i = 0; i < K; ++i) {
+        const int j = i * kJoinThreads + threadIdx.x;
+        x[u][i] = r0 + u < rows && j0 + j < len ? sc[(int64_t)(r0 + u) * a.score_ld + j] : -INFINITY;
+      }
+  };
+  load(0);
+#pragma unroll
+  for (int i = 0; i < K; ++i) {
+    const int j = j0 + i * kJoinThreads + threadIdx.x;
+    w[i] = j < len && a.weights_in ? a.weights_in[at + j] : 0.f;
+  }
+  int* lim = reinterpret_cast<int*>(lse2 + rows);
   for (int r = threadIdx.x; r < rows; r += kJoinThreads) {
     const float2 st = join_stats(a, first + r, step);
     lse2[r] = st.x + log2f(st.y);
+    lim[r] = visible_limit(a, len, count, r / a.group);
   }
   __syncthreads();
-  const int64_t at = ((int64_t)b * a.kv_heads + kvh) * a.max_seq;
-  const float* sc = a.scores + ((int64_t)b * a.kv_heads + kvh) * step * a.score_ld;
+  float sum[K];
 #pragma unroll
-  for (int i = 0; i < kJoinKeys / kJoinThreads; ++i) {
+  for (int i = 0; i < K; ++i) sum[i] = 0.f;
+  for (int r0 = 0; r0 < rows; r0 += 4) {
+    if (r0 > 0) load(r0);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (r0 + u >= rows) break;
+      const float l2 = lse2[r0 + u];
+      const int lm = lim[r0 + u];
+#pragma unroll
+      for (int i = 0; i < K; ++i)
+        if (all || j0 + i * kJoinThreads + (int)threadIdx.x < lm) sum[i] += ex2(x[u][i] - l2);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < K; ++i) {
     const int j = j0 + i * kJoinThreads + threadIdx.x;
-    if (j >= len) break;
-    float w = 0.f;
-    for (int r = 0; r < rows; ++r)
-      if (j < visible_limit(a, len, count, r / a.group)) w += ex2(sc[(int64_t)r * a.score_ld + j] - lse2[r]);
-    a.weights[at + j] = (a.weights_in ? a.weights_in[at + j] : 0.f) + w;
+    if (j < len) a.weights[at + j] = w[i] + sum[i];
   }
 }
 
@@ -644,7 +676,7 @@ int launch_attention_join(const CachedArgs& a, cudaStream_t s) {
   const int wb = a.scores ? (a.max_seq + kJoinKeys - 1) / kJoinKeys : 0;
   if (jb + wb == 0) return SWAPNET_OK;
   const dim3 grid(jb + wb, a.kv_heads, a.n_seq);
-  const size_t smem = a.scores ? rows * sizeof(float) : 0;
+  const size_t smem = a.scores ? rows * 2 * sizeof(float) : 0;
   return done(a.dtype == SWAPNET_BF16
                   ? launch(attention_join_kernel<__nv_bfloat16>, grid, kJoinThreads, smem, true, s, a, jb)
                   : launch(attention_join_kernel<__half>, grid, kJoinThreads, smem, true, s, a, jb),

@@ -10,20 +10,21 @@
 //   S = Q K^T     tcgen05.mma, M 128 (rows) x N 128 (keys); Q, K and V by TMA
 //                 (128-byte swizzle); S in two TMEM buffers, so that the next
 //                 tile's S is computed during this tile's softmax
-//   P             warps 4..11, two threads per row: one takes the first 64 keys
-//                 of every tile, the other the last 64, each with a softmax of
-//                 its own (reference m, sum l, output O_h), so no thread waits
-//                 for another.  Scores from TMEM, masks only in tiles that a
-//                 limit crosses, p = 2^(s - m) back over the scores as two
-//                 parts of the storage type p_hi + p_lo (about 16 bits of p)
+//   P             warps 4..19, four threads per row, 32 keys each: the first 64
+//                 keys of every tile and the last 64 have a softmax of their
+//                 own (reference m, sum l, output O_h), whose two threads only
+//                 vote on whether m has to grow.  Scores from TMEM, masks only
+//                 in tiles that a limit crosses, p = 2^(s - m) back over the
+//                 scores as two parts of the storage type p_hi + p_lo (about 16
+//                 bits of p)
 //   O_h += P_h V  tcgen05.mma with A = P from TMEM, B = V as loaded (MN-major)
 // O_0 and O_1 stay in TMEM.  m is the running maximum only where that grew by
 // more than 2^8 since it was last taken (kSlack): until then p and l stay
 // within 2^8 of their usual range, which fp32 sums and both storage types hold
 // without loss, and O is neither read nor rescaled.
 // With at most 64 rows (REP 2) the rows appear twice in the MMA's 128, and
-// lanes 0..63 and 64..127 share a half's keys, so that all eight warps work
-// (the other 32 keys are zeros in a lane's P).
+// lanes 0..63 and 64..127 share a thread's keys, so that all warps work (the
+// other 16 keys are zeros in a lane's P).
 // K and V tiles pass through one ring in the order they are used, across
 // units.  Every wait is bounded: on timeout the kernel records kDevErrTimeout,
 // drains the loads and MMAs it started, frees TMEM and returns.
@@ -43,16 +44,20 @@ namespace {
 constexpr int kSoftThreads = 256;
 constexpr int kTcThreads = 64 + kSoftThreads;
 // attention: warps 0 (TMA) and 1 (MMA), two idle ones that complete their
-// warpgroup, the softmax's eight; 384 x 168 registers at launch, of which
+// warpgroup, the softmax's 8 kSub; 384 x 168 registers at launch, of which
 // setmaxnreg leaves 128 x 72 and gives 256 x 216
-constexpr int kAtThreads = 128 + kSoftThreads;
-static_assert(128 * 72 + 256 * 216 <= kAtThreads * 168, "registers of a CTA");
+constexpr int kSub = 1;  // threads per row and half of the keys
+constexpr int kAtSoft = 256 * kSub, kAtThreads = 128 + kAtSoft;
+constexpr int kRegsLow = kSub == 1 ? 72 : 64, kRegsHigh = kSub == 1 ? 216 : 104;
+static_assert(128 * kRegsLow + kAtSoft * kRegsHigh <= kAtThreads * (kSub == 1 ? 168 : 96), "registers of a CTA");
 constexpr int kKeys = 128;       // keys of a tile
 constexpr float kSlack = 8.0f;   // log2 of what p may exceed 1 by
 constexpr uint32_t kTmemCols = 512;
 // TMEM columns: S [0, 128) and [128, 256), each half's P over its scores (hi
 // then lo); O_0 [256, 256 + D), O_1 [384, 384 + D)
 constexpr uint32_t kTmO = 256;
+
+constexpr int kNear = 64;        // sequences whose sizes a CTA keeps
 
 template <int D> struct TcCfg {
   static constexpr int kHalves = D / 64;             // 64-dim boxes of a tile
@@ -62,11 +67,12 @@ template <int D> struct TcCfg {
   static constexpr int kOffQ = 0;
   static constexpr int kOffRing = kTile;
   static constexpr int kOffX = kOffRing + kSlots * kTile;   // (m, l) of every thread
-  static constexpr int kOffPar = kOffX + 256 * 8;           // parents
+  static constexpr int kOffPar = kOffX + kAtSoft * 8;       // parents
   static constexpr int kOffOdd = kOffPar + kTreeMax * 4;    // odd value rows, a bit each
   static constexpr int kOffBar = kOffOdd + 16;
-  static constexpr int kOffStage = kOffBar + 256;           // REP 2: 32 columns of 2 x 64 rows
-  static constexpr int kSmem = kOffStage + 2 * 64 * 36 * 4 + 1024;  // + alignment slack
+  static constexpr int kOffStage = kOffBar + 256;           // REP 2: 32 columns of 2 kSub x 64 rows, and growths' maxima
+  static constexpr int kOffNear = kOffStage + 2 * kSub * 64 * 36 * 4;
+  static constexpr int kSmem = kOffNear + kNear * 8 + 1024;  // + alignment slack
   static_assert(kSmem <= 232448, "shared memory of a CTA");
 };
 
@@ -92,6 +98,18 @@ __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t* r) {
       "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
+__device__ __forceinline__ uint32_t bar_or(int id, int threads, bool v) {  // a named barrier; whether any thread's v is set
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "bar.red.or.pred q, %2, %3, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"((uint32_t)v), "r"(id), "r"(threads)
+      : "memory");
+  return r;
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Descriptor of a B operand stored MN-major with the 128-byte swizzle: 8-row
@@ -108,19 +126,24 @@ __device__ __forceinline__ uint64_t desc_mn(uint32_t addr) {
 
 // ------------------------------------------------------------- who does what
 // A unit is the rows [rt * queries, ...) of a (sequence, key head); pair =
-// b * nrt + rt, unit = pair * kv_heads + key head.  With a.splits == 1 CTA c
-// owns unit c.  Otherwise the units' tiles, in order, are cut into gridDim.x
-// equal runs, one per CTA, whatever the sequences' lengths: a unit may be
-// spread over CTAs that follow one another, whose results meet in the join.
-// Every valid unit has at least one tile.
+// b * nrt + rt.  CTA c works for key head c % kv_heads, so that the CTAs of all
+// heads, which share the cache's rows (a head's part of a row is 128 or 256
+// bytes), pass the same rows at the same time: DRAM pages are opened once.
+// With a.splits == 1 CTA c owns pair c / kv_heads.  Otherwise the tiles of all
+// pairs, in order, are cut into equal runs, one per kv_heads CTAs, whatever the
+// sequences' lengths: a unit may be spread over runs that follow one another,
+// whose results meet in the join.  Every valid unit has at least one tile.
 constexpr int kRunTiles = 2;  // of a run, where there are too few tiles for all CTAs
 struct PairSize {
   int len, count, np, tiles;  // np: tiles of the cache, then one of the draft
 };
-__device__ __forceinline__ PairSize pair_size(const CachedArgs& a, int b, int rt, int queries) {
+__device__ __forceinline__ int2 seq_size(const CachedArgs& a, int b) {
+  return make_int2(a.lens[b * a.lens_step] + a.len_add, a.counts ? a.counts[b * a.counts_step] : a.tokens);
+}
+__device__ __forceinline__ PairSize pair_size(const CachedArgs& a, int2 size, int rt, int queries) {
   PairSize p;
-  p.len = a.lens[b * a.lens_step] + a.len_add;
-  p.count = a.counts ? a.counts[b * a.counts_step] : a.tokens;
+  p.len = size.x;
+  p.count = size.y;
   p.np = p.tiles = 0;
   if (p.len < 0 || p.len > a.max_seq || p.count < 0 || p.count > a.tokens || rt * queries >= p.count) return p;
   const int last = min((rt + 1) * queries, p.count) - 1;
@@ -132,29 +155,32 @@ __device__ __forceinline__ PairSize pair_size(const CachedArgs& a, int b, int rt
 
 // A CTA's run of tiles, piece by piece (a piece: its part of one unit).
 struct Cursor {
-  int64_t left;            // tiles of the run from the next piece on
-  int pair, kvh, next;     // unit and first tile of the next piece
+  int64_t left;       // tiles of the run from the next piece on
+  int pair, next;     // pair and first tile of the next piece
   // the current piece
-  int b, rt, h, i0, n;     // tiles [i0, i0 + n) of the unit
+  int b, rt, i0, n;   // tiles [i0, i0 + n) of the unit
+  // sizes of the sequences from b0 on, in shared memory: a step is on the way
+  // of every warp
+  const int2* near;
+  int b0;
   PairSize z;
   __device__ __forceinline__ bool step(const CachedArgs& a, int nrt, int queries) {
     while (left > 0 && pair < a.n_seq * nrt) {
       b = pair / nrt;
       rt = pair % nrt;
-      z = pair_size(a, b, rt, queries);
+      z = pair_size(a, b - b0 < kNear ? near[b - b0] : seq_size(a, b), rt, queries);
       if (z.tiles > next) {
-        h = kvh;
         i0 = next;
         n = (int)min((int64_t)(z.tiles - next), left);
         left -= n;
         next += n;
         if (next == z.tiles) {
           next = 0;
-          if (++kvh == a.kv_heads) kvh = 0, ++pair;
+          ++pair;
         }
         return true;
       }
-      next = kvh = 0;
+      next = 0;
       ++pair;
     }
     return false;
@@ -177,6 +203,36 @@ __device__ __forceinline__ float2 add2(float2 x, float2 y) {
   return r;
 }
 
+// Every lane's 16 P bytes v, contiguous at `to`, for the lanes with `ok` (a row
+// each): P lanes exchange their pieces (butterflies), so that a store writes
+// 16 P bytes of a row side by side.  Rows written piece by piece, 32 rows a
+// store, took 1850 cycles per 32 rows x 16 columns of eight warps.
+template <int P> __device__ __forceinline__ void store_rows(uint4 (&v)[P], char* to, bool ok) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int st = 1; st < P; st <<= 1)
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+      if (!(i & st)) {
+        const bool up = lane & st;
+        uint4 x = up ? v[i] : v[i | st];
+        x.x = __shfl_xor_sync(0xffffffffu, x.x, st);
+        x.y = __shfl_xor_sync(0xffffffffu, x.y, st);
+        x.z = __shfl_xor_sync(0xffffffffu, x.z, st);
+        x.w = __shfl_xor_sync(0xffffffffu, x.w, st);
+        if (up)
+          v[i] = x;
+        else
+          v[i | st] = x;
+      }
+#pragma unroll
+  for (int i = 0; i < P; ++i) {  // v[i]: piece lane % P of row i of the P lanes' rows
+    const int from = (lane & ~(P - 1)) + i;
+    char* row = reinterpret_cast<char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(to), from));
+    if (__shfl_sync(0xffffffffu, (int)ok, from)) *reinterpret_cast<uint4*>(row + (lane & (P - 1)) * 16) = v[i];
+  }
+}
+
 template <typename T, int D, int REP>
 __global__ void __launch_bounds__(kAtThreads, 1)
     attention_rows_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -184,7 +240,9 @@ __global__ void __launch_bounds__(kAtThreads, 1)
                           const __grid_constant__ CUtensorMap tmVn, const __grid_constant__ CachedArgs a, int queries, int nrt) {
   using F = TcCfg<D>;
   constexpr int kRowsMax = 128 / REP;
-  constexpr int NK = 64 / REP;  // keys per thread and tile
+  constexpr int kPart = 64 / kSub;    // keys of a warp and tile
+  constexpr int NK = kPart / REP;     // of a thread
+  constexpr int kParts = 2 * kSub;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   float2* ml = reinterpret_cast<float2*>(smem + F::kOffX);
@@ -202,6 +260,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
   const uint32_t done_bar = smem_u32(bars + 28);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 29);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 30);
+  int2* near = reinterpret_cast<int2*>(smem + F::kOffNear);
   int64_t* sched = reinterpret_cast<int64_t*>(ml);  // (before the first results)
 
   const int warp = warp_index(), lane = threadIdx.x & 31;
@@ -213,12 +272,12 @@ __global__ void __launch_bounds__(kAtThreads, 1)
     for (int i = 0; i < 2; ++i) {
       mbar_init(s_full(i), 1);
       mbar_init(o_full(i), 1);
-      for (int h = 0; h < 2; ++h) mbar_init(p_full(h, i), 4);
+      for (int h = 0; h < 2; ++h) mbar_init(p_full(h, i), 4 * kSub);
     }
     mbar_init(q_full, 1);
     mbar_init(q_free, 1);
     mbar_init(o_done, 1);
-    mbar_init(o_free, 8);
+    mbar_init(o_free, kAtSoft / 32);
     mbar_init(done_bar, 1);
     *abort_flag = 0;
 #pragma unroll
@@ -236,14 +295,14 @@ __global__ void __launch_bounds__(kAtThreads, 1)
   pdl_launch_dependents();
   Cursor cur;
   cur.next = 0;
+  const int kvh = blockIdx.x % a.kv_heads, run = blockIdx.x / a.kv_heads;
   int64_t first_tile = 0, total = 0;  // the run's first tile in the order of all; their number
   int runs = 1;
   if (a.splits == 1) {
-    cur.pair = blockIdx.x / a.kv_heads;
-    cur.kvh = blockIdx.x % a.kv_heads;
-    const PairSize z = pair_size(a, cur.pair / nrt, cur.pair % nrt, queries);
+    cur.pair = run;
+    const PairSize z = pair_size(a, seq_size(a, cur.pair / nrt), cur.pair % nrt, queries);
     cur.left = z.tiles;
-    if (z.tiles == 0 && threadIdx.x == 0 && cur.kvh == 0) {
+    if (z.tiles == 0 && threadIdx.x == 0 && kvh == 0) {
       int len, count;
       seq_sizes(a, cur.pair / nrt, &len, &count);  // (reports what is out of range)
     }
@@ -255,7 +314,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
     const int p0 = min((int)threadIdx.x * per, pairs), p1 = min(p0 + per, pairs);
     int64_t sum = 0;
     for (int p = p0; p < p1; ++p) {
-      sum += (int64_t)pair_size(a, p / nrt, p % nrt, queries).tiles * a.kv_heads;
+      sum += pair_size(a, seq_size(a, p / nrt), p % nrt, queries).tiles;
       if (blockIdx.x == 0) {
         const int b = p / nrt, n = a.lens[b * a.lens_step] + a.len_add, c = a.counts ? a.counts[b * a.counts_step] : a.tokens;
         if (n < 0 || n > a.max_seq || c < 0 || c > a.tokens) atomicExch(a.err, kDevErrBounds);
@@ -276,31 +335,32 @@ __global__ void __launch_bounds__(kAtThreads, 1)
       if (w < warp) before += sched[w];
       total += sched[w];
     }
-    runs = (int)min((int64_t)gridDim.x, (total + kRunTiles - 1) / kRunTiles);
-    first_tile = (int)blockIdx.x < runs ? total * blockIdx.x / runs : total;
-    cur.left = (int)blockIdx.x < runs ? total * (blockIdx.x + 1) / runs - first_tile : 0;
-    cur.pair = cur.kvh = 0;
+    runs = (int)min((int64_t)(gridDim.x / a.kv_heads), (total + kRunTiles - 1) / kRunTiles);
+    first_tile = run < runs ? total * run / runs : total;
+    cur.left = run < runs ? total * (run + 1) / runs - first_tile : 0;
+    cur.pair = 0;
     if (cur.left > 0 && before <= first_tile && first_tile < before + sum) {
       int64_t at = before;
       for (int p = p0; p < p1; ++p) {
-        const int tiles = pair_size(a, p / nrt, p % nrt, queries).tiles;
-        if (first_tile < at + (int64_t)tiles * a.kv_heads) {
+        const int tiles = pair_size(a, seq_size(a, p / nrt), p % nrt, queries).tiles;
+        if (first_tile < at + tiles) {
           sched[16] = p;
-          sched[17] = first_tile - at;  // in (key head, tile) order
-          sched[18] = tiles;
+          sched[17] = first_tile - at;
           break;
         }
-        at += (int64_t)tiles * a.kv_heads;
+        at += tiles;
       }
     }
     __syncthreads();
     if (cur.left > 0) {
       cur.pair = (int)sched[16];
-      cur.kvh = (int)(sched[17] / sched[18]);
-      cur.next = (int)(sched[17] % sched[18]);
+      cur.next = (int)sched[17];
     }
-    __syncthreads();  // (sched is written again as ml)
   }
+  cur.b0 = cur.pair / nrt;
+  cur.near = near;
+  if (threadIdx.x < kNear && cur.b0 + (int)threadIdx.x < a.n_seq) near[threadIdx.x] = seq_size(a, cur.b0 + threadIdx.x);
+  __syncthreads();  // (and sched is written again, as ml)
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   // a piece's tiles in the order of use: K0, K1, V0, K2, V1, ..., V(n-1)
@@ -309,7 +369,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
 
   // the softmax warps take registers that the others leave
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsLow));
     if (warp == 0 && elect_one()) {
       // ---------------- TMA producer
       const int q_bytes = REP * F::kHalves * queries * a.group * 128;
@@ -324,7 +384,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
           const CUtensorMap* tm = keys ? (nw ? &tmKn : &tmK) : (nw ? &tmVn : &tmV);
 #pragma unroll
           for (int h = 0; h < F::kHalves; ++h)
-            tma_load_3d(smem_u32(smem + F::kOffRing + s * F::kTile + h * F::kBox), tm, full(s), cur.h * D + h * 64,
+            tma_load_3d(smem_u32(smem + F::kOffRing + s * F::kTile + h * F::kBox), tm, full(s), kvh * D + h * 64,
                         nw ? 0 : (cur.i0 + i) * kKeys, cur.b);
           ++pos;
           return true;
@@ -337,7 +397,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
         for (int c = 0; c < REP; ++c)
 #pragma unroll
           for (int h = 0; h < F::kHalves; ++h)
-            tma_load_3d(smem_u32(smem + F::kOffQ + h * F::kBox + c * (kRowsMax * 128)), &tmQ, q_full, h * 64, cur.h * a.group,
+            tma_load_3d(smem_u32(smem + F::kOffQ + h * F::kBox + c * (kRowsMax * 128)), &tmQ, q_full, h * 64, kvh * a.group,
                         cur.b * a.tokens + cur.rt * queries);
         for (int i = 0; ok && i < cur.n; ++i) ok = load(i, false) && (i + 2 >= cur.n || load(i + 2, true));
         if (!ok) {
@@ -360,16 +420,15 @@ __global__ void __launch_bounds__(kAtThreads, 1)
       const uint64_t kd = smem_desc_sw128(smem_u32(smem + F::kOffRing)), vd = desc_mn(smem_u32(smem + F::kOffRing));
       int pos0 = 0, g0 = 0;  // of the piece: ring position, tiles before
       bool ok = true;
+      auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_bounded(bar, parity, abort_flag, a.err); };
       for (int piece = 0; ok && cur.step(a, nrt, queries); ++piece) {
         const int n = cur.n;
         auto scores = [&](int i) -> bool {
           const int pos = pos0 + k_pos(i), s = pos % F::kSlots, g = g0 + i;
-          if (!mbar_wait_bounded(full(s), (pos / F::kSlots) & 1, abort_flag, a.err)) return false;
-          // over the P of two tiles ago, once its product has read it; a
-          // piece's first scores come after all products before (those of tile
-          // g - 1 are on their way: of g - 2 alone could be asked no more)
-          if (i == 0 ? g > 0 : g >= 2)
-            if (!mbar_wait_bounded(o_full(1), (i == 0 ? g - 1 : g) & 1, abort_flag, a.err)) return false;
+          if (!wait(full(s), (pos / F::kSlots) & 1)) return false;
+          // (over the P of two tiles ago: the tensor core runs the MMAs of one
+          // thread in the order of their issue, so its product, issued before,
+          // has read it)
           tc_fence_after();
           const uint64_t kt = kd + (uint64_t)(s * (F::kTile >> 4));  // the descriptors' address field counts 16 bytes
 #pragma unroll
@@ -383,15 +442,14 @@ __global__ void __launch_bounds__(kAtThreads, 1)
           if (i == n - 1) tc_commit(q_free);
           return true;
         };
-        ok = mbar_wait_bounded(q_full, piece & 1, abort_flag, a.err) && scores(0);
+        ok = wait(q_full, piece & 1) && scores(0);
         for (int i = 0; ok && i < n; ++i) {
           if (i + 1 < n && !(ok = scores(i + 1))) break;
           const int pos = pos0 + v_pos(i, n), s = pos % F::kSlots, g = g0 + i;
-          ok = mbar_wait_bounded(full(s), (pos / F::kSlots) & 1, abort_flag, a.err) &&
-               (i > 0 || piece == 0 || mbar_wait_bounded(o_free, (piece - 1) & 1, abort_flag, a.err));
+          ok = wait(full(s), (pos / F::kSlots) & 1) && (i > 0 || piece == 0 || wait(o_free, (piece - 1) & 1));
           const uint64_t vt = vd + (uint64_t)(s * (F::kTile >> 4));
           for (int h = 0; ok && h < 2; ++h) {
-            ok = mbar_wait_bounded(p_full(h, g), (g >> 1) & 1, abort_flag, a.err);
+            ok = wait(p_full(h, g), (g >> 1) & 1);
             if (!ok) break;
             tc_fence_after();
             const uint32_t pt = tmem + (uint32_t)(g & 1) * 128u + (uint32_t)h * 64u;
@@ -399,7 +457,8 @@ __global__ void __launch_bounds__(kAtThreads, 1)
             for (int part = 0; part < 2; ++part)
 #pragma unroll
               for (int ks = 0; ks < 4; ++ks)  // 16 keys a step
-                tc_mma_f16_ta(tmem + kTmO + (uint32_t)h * 128u, pt + (uint32_t)(part * 32 + ks * 8),
+                tc_mma_f16_ta(tmem + kTmO + (uint32_t)h * 128u,
+                              pt + (uint32_t)(ks / (4 / kSub) * kPart + part * (kPart / 2) + ks % (4 / kSub) * 8),
                               vt + (uint64_t)((h * 4 + ks) * (2048 >> 4)), idesc_pv, (uint32_t)(i | part | ks) != 0);
             tc_commit(o_full(h));
           }
@@ -415,20 +474,26 @@ __global__ void __launch_bounds__(kAtThreads, 1)
       mbar_wait_bounded(done_bar, 0, &no_abort, nullptr);
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsHigh));
     // ---------------- softmax and output
-    const int q4 = warp & 3, half = (warp - 4) >> 2;
+    // four threads per row: `half` of a tile's keys (an output and a reference
+    // of its own), `part` = half and half of that
+    const int q4 = warp & 3, part = (warp - 4) >> 2, half = part / kSub;
     const int slot = q4 * 32 + lane, rep = slot / kRowsMax, row = slot % kRowsMax;
     const int aid = (warp - 4) * 32 + lane;
-    const int kofs = half * 64 + rep * NK;  // this thread's first key of a tile
+    const int kofs = part * kPart + rep * NK;  // this thread's first key of a tile
     const uint32_t lane_off = (uint32_t)(q4 * 32) << 16;
     const uint32_t tO = tmem + kTmO + (uint32_t)half * 128u + lane_off;
-    auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory"); };
-    auto all_sync = [&]() { asm volatile("bar.sync 5, 256;" ::: "memory"); };
+    const int pair_id = 1 + 2 * q4 + half;  // the two warps of a half
+    auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(pair_id) : "memory"); };
+    auto row_sync = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(10 + q4), "n"(64 * kSub) : "memory"); };
+    auto all_sync = [&]() { asm volatile("bar.sync 9, %0;" ::"n"(kAtSoft) : "memory"); };
+    float* xch = reinterpret_cast<float*>(smem + F::kOffStage);  // [part][slot]
     bool ok = true;
     int pos0 = 0, g0 = 0;
+    int rest = 0, rest_rows = 0;  // the unit that this CTA begins and others go on with
     for (int piece = 0; cur.step(a, nrt, queries); ++piece) {
-      const int b = cur.b, kvh = cur.h, n = cur.n, np = cur.z.np, len = cur.z.len, count = cur.z.count;
+      const int b = cur.b, n = cur.n, np = cur.z.np, len = cur.z.len, count = cur.z.count;
       const int t0 = cur.rt * queries, rows = min(queries, count - t0) * a.group;
       const int lim_min = visible_limit(a, len, count, t0);
       const bool last = cur.i0 + n == cur.z.tiles, whole = cur.i0 == 0 && last;  // a piece up to the unit's end; all of it
@@ -436,9 +501,9 @@ __global__ void __launch_bounds__(kAtThreads, 1)
       const int t = t0 + min(row, rows - 1) / a.group;
       const int lim = visible_limit(a, len, count, t);
       bool bad = false;  // a parent that is none
-      if (a.parents && last) {
+      if (a.parents && (last || cur.i0 == 0)) {  // (the first piece's CTA speaks for the join)
         all_sync();  // the piece before has read its parents
-        for (int i = aid; i < count; i += kSoftThreads) par[i] = a.parents[(int64_t)b * a.tokens + i];
+        for (int i = aid; i < count; i += kAtSoft) par[i] = a.parents[(int64_t)b * a.tokens + i];
         all_sync();
         for (int i = lane; i < count; i += 32) bad = bad || par[i] < -1 || par[i] >= i;
         bad = __any_sync(0xffffffffu, bad);
@@ -455,75 +520,92 @@ __global__ void __launch_bounds__(kAtThreads, 1)
         ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
         uint32_t hi[NK / 2], lo[NK / 2];
-        if (ok && works) {
+        if (works) {
           uint32_t s[NK];
-#pragma unroll
-          for (int c = 0; c < NK; c += 32) {
-            uint32_t(&r)[32] = *reinterpret_cast<uint32_t(*)[32]>(s + c);
-            tmem_ld_32x32b_x32(tS + (uint32_t)(kofs + c), r);
-          }
-          tmem_ld_wait();
-          if (masked) {
-            uint32_t see[NK / 32];
-#pragma unroll
-            for (int w = 0; w < NK / 32; ++w) see[w] = 0;
-            if (nw && a.parents) {
-              for (int j = bad ? -1 : t; j >= 0; j = par[j]) {
-#pragma unroll
-                for (int w = 0; w < NK / 32; ++w)
-                  if ((j - kofs) >> 5 == w) see[w] |= 1u << ((j - kofs) & 31);
-              }
+          float mx = -INFINITY;
+          if (ok) {
+            if constexpr (NK == 16) {
+              tmem_ld_32x32b_x16(tS + (uint32_t)kofs, s);
             } else {
-              const int seen = (nw ? t + 1 : lim - k0) - kofs;
 #pragma unroll
-              for (int w = 0; w < NK / 32; ++w) see[w] = seen >= 32 * w + 32 ? 0xffffffffu : seen > 32 * w ? (1u << (seen - 32 * w)) - 1u : 0u;
+              for (int c = 0; c < NK; c += 32)
+                tmem_ld_32x32b_x32(tS + (uint32_t)(kofs + c), *reinterpret_cast<uint32_t(*)[32]>(s + c));
             }
+            tmem_ld_wait();
+            if (masked) {
+              uint64_t see = 0;
+              if (nw && a.parents) {
+                for (int j = bad ? -1 : t; j >= 0; j = par[j])
+                  if ((uint32_t)(j - kofs) < (uint32_t)NK) see |= 1ull << (j - kofs);
+              } else {
+                const int seen = (nw ? t + 1 : lim - k0) - kofs;
+                see = seen >= 64 ? ~0ull : seen > 0 ? (1ull << seen) - 1ull : 0ull;
+              }
 #pragma unroll
-            for (int k = 0; k < NK; ++k)
-              if (!(see[k >> 5] >> (k & 31) & 1u)) s[k] = 0xff800000u;  // -inf
+              for (int k = 0; k < NK; ++k)
+                if (!(see >> k & 1u)) s[k] = 0xff800000u;  // -inf
+            }
+            float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int k = 0; k < NK; ++k) mx4[k & 3] = fmaxf(mx4[k & 3], __uint_as_float(s[k]));
+            mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * a.scale_log2;
           }
-          float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-          for (int k = 0; k < NK; ++k) mx4[k & 3] = fmaxf(mx4[k & 3], __uint_as_float(s[k]));
-          const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * a.scale_log2;
+          // the warps of a half vote (with kSub 2, also after a timeout)
           const bool grow = mx - m > kSlack;  // (also the first key seen)
-          if (__any_sync(0xffffffffu, grow)) {
+          if (kSub == 1 ? __any_sync(0xffffffffu, grow) : bar_or(pair_id, 64, grow) != 0) {
+            if (kSub == 2) {
+              xch[part * 128 + slot] = mx;
+              pair_sync();
+              mx = fmaxf(mx, xch[(part ^ 1) * 128 + slot]);
+            }
             float alpha = 1.f;
-            if (grow) {
+            if (mx - m > kSlack) {
               alpha = ex2(m - mx);
               m = mx;
               l *= alpha;
             }
             if (i > 0) {  // O is at rest once the product of the tile before is done (the one before that is: these scores came after it)
-              ok = mbar_wait_bounded(o_full(half), (g - 1) & 1, abort_flag, a.err);
+              ok = ok && mbar_wait_bounded(o_full(half), (g - 1) & 1, abort_flag, a.err);
               ok = __all_sync(0xffffffffu, ok);
               tc_fence_after();
               if (ok) {
 #pragma unroll
-                for (int c = 0; c < D; c += 16) {
+                for (int c = 0; c < D / kSub; c += 16) {  // each warp its share of the columns
                   uint32_t r[16];
-                  tmem_ld_32x32b_x16(tO + (uint32_t)c, r);
+                  const uint32_t at = tO + (uint32_t)(part % kSub * (D / kSub) + c);
+                  tmem_ld_32x32b_x16(at, r);
                   tmem_ld_wait();
 #pragma unroll
                   for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * alpha);
-                  tmem_st_x16(tO + (uint32_t)c, r);
+                  tmem_st_x16(at, r);
                 }
               }
             }
+            if (kSub == 2) pair_sync();  // xch has been read
           }
-          const float base = m == -INFINITY ? 0.f : m;
-          const float2 scale2 = make_float2(a.scale_log2, a.scale_log2), base2 = make_float2(-base, -base), minus = make_float2(-1.f, -1.f);
-          float2 sum2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+          if (ok) {
+            const float base = m == -INFINITY ? 0.f : m;
+            const float2 scale2 = make_float2(a.scale_log2, a.scale_log2), base2 = make_float2(-base, -base), minus = make_float2(-1.f, -1.f);
+            float2 sum2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-          for (int k = 0; k < NK / 2; ++k) {
-            const float2 x = fma2(make_float2(__uint_as_float(s[2 * k]), __uint_as_float(s[2 * k + 1])), scale2, base2);
-            const float2 p = make_float2(ex2(x.x), ex2(x.y));
-            sum2[k & 1] = add2(sum2[k & 1], p);
-            hi[k] = pack_pair<T>(p.x, p.y);
-            const float2 rest = fma2(unpack_pair<T>(hi[k]), minus, p);
-            lo[k] = pack_pair<T>(rest.x, rest.y);
+            for (int k0 = 0; k0 < NK / 2; k0 += 8) {  // (step by step over eight pairs: their latencies overlap)
+              float2 p[8];
+#pragma unroll
+              for (int k = 0; k < 8; ++k)
+                p[k] = fma2(make_float2(__uint_as_float(s[2 * (k0 + k)]), __uint_as_float(s[2 * (k0 + k) + 1])), scale2, base2);
+#pragma unroll
+              for (int k = 0; k < 8; ++k) p[k] = make_float2(ex2(p[k].x), ex2(p[k].y));
+#pragma unroll
+              for (int k = 0; k < 8; ++k) hi[k0 + k] = pack_pair<T>(p[k].x, p[k].y);
+#pragma unroll
+              for (int k = 0; k < 8; ++k) sum2[k & 1] = add2(sum2[k & 1], p[k]);
+#pragma unroll
+              for (int k = 0; k < 8; ++k) p[k] = fma2(unpack_pair<T>(hi[k0 + k]), minus, p[k]);
+#pragma unroll
+              for (int k = 0; k < 8; ++k) lo[k0 + k] = pack_pair<T>(p[k].x, p[k].y);
+            }
+            l += (sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y);
           }
-          l += (sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y);
         }
         uint32_t odd = 0;
         if (masked) {
@@ -540,7 +622,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
             return reinterpret_cast<uint4*>(vs + (c >> 3) * F::kBox + r * 128 + (((c & 7) ^ (r & 7)) << 4));
           };
           if (ok) {
-            for (int c = aid; c < kKeys * (D / 8); c += kSoftThreads) {
+            for (int c = aid; c < kKeys * (D / 8); c += kAtSoft) {
               const int r = c / (D / 8);
               uint4* at = chunk(r, c % (D / 8));
               if (r >= have) {
@@ -554,7 +636,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
           all_sync();
           odd = odd_rows[0] | odd_rows[1] | odd_rows[2] | odd_rows[3];
           if (odd) {
-            for (int c = aid; c < kKeys * (D / 8); c += kSoftThreads) {
+            for (int c = aid; c < kKeys * (D / 8); c += kAtSoft) {
               const int r = c / (D / 8);
               if (odd_rows[r >> 5] >> (r & 31) & 1u) *chunk(r, c % (D / 8)) = make_uint4(0u, 0u, 0u, 0u);
             }
@@ -564,20 +646,16 @@ __global__ void __launch_bounds__(kAtThreads, 1)
         }
         if (ok) {
           if (works) {
-            // over the half's 64 scores: hi parts of its 64 keys, then the lo parts
+            // over the part's scores: hi parts of its keys, then the lo parts
 #pragma unroll
-            for (int part = 0; part < 2; ++part) {
-              const uint32_t* x = part ? lo : hi;
-              const uint32_t to = tS + (uint32_t)(half * 64 + part * 32);
-              if (REP == 1) {
-                tmem_st_x16(to, x);
-                tmem_st_x16(to + 16u, x + (NK / 2 - 16));
-              } else {
-                uint32_t z[16];
+            for (int u = 0; u < 2; ++u) {
+              const uint32_t* x = u ? lo : hi;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) z[e] = 0;
-                tmem_st_x16(to + (uint32_t)rep * 16u, x);
-                tmem_st_x16(to + (uint32_t)(rep ^ 1) * 16u, z);
+              for (int c = 0; c < kPart / 2; c += 16) {
+                uint32_t w[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) w[e] = REP == 1 || (c + e) / (NK / 2) == rep ? x[(c + e) % (NK / 2)] : 0u;
+                tmem_st_x16(tS + (uint32_t)(part * kPart + u * (kPart / 2) + c), w);
               }
             }
             tmem_st_wait();
@@ -590,30 +668,34 @@ __global__ void __launch_bounds__(kAtThreads, 1)
           ok = ok && mbar_wait_bounded(o_full(half), g & 1, abort_flag, a.err);
           ok = __all_sync(0xffffffffu, ok);
           tc_fence_after();
-          for (int j = 0; j < kKeys; ++j) {
+          for (int j = half * 64; j < half * 64 + 64; ++j) {
             if (!(odd_rows[j >> 5] >> (j & 31) & 1u)) continue;
             const int rel = j - kofs;
-            if (rel < 0 || rel >= NK || !ok || !works) continue;  // (the same for all lanes of a warp)
-            float pj = 0.f;
+            if (rel >= 0 && rel < NK && ok && works) {  // (the same for all lanes of a warp)
+              float pj = 0.f;
 #pragma unroll
-            for (int k = 0; k < NK / 2; ++k) {
-              const float2 h2 = unpack_pair<T>(hi[k]), l2 = unpack_pair<T>(lo[k]);
-              if (rel == 2 * k) pj = h2.x + l2.x;
-              if (rel == 2 * k + 1) pj = h2.y + l2.y;
-            }
-            const T* v = nw ? static_cast<const T*>(a.v_new) + ((int64_t)b * a.tokens + j) * a.new_stride
-                            : static_cast<const T*>(a.v) + (int64_t)b * a.seq_stride + (int64_t)(k0 + j) * a.kv_stride;
-            v += kvh * D;
-            for (int c = 0; c < D; c += 16) {
-              uint32_t r[16];
-              tmem_ld_32x32b_x16(tO + (uint32_t)c, r);
-              tmem_ld_wait();
+              for (int k = 0; k < NK / 2; ++k) {
+                const float2 h2 = unpack_pair<T>(hi[k]), l2 = unpack_pair<T>(lo[k]);
+                if (rel == 2 * k) pj = h2.x + l2.x;
+                if (rel == 2 * k + 1) pj = h2.y + l2.y;
+              }
+              const T* v = nw ? static_cast<const T*>(a.v_new) + ((int64_t)b * a.tokens + j) * a.new_stride
+                              : static_cast<const T*>(a.v) + (int64_t)b * a.seq_stride + (int64_t)(k0 + j) * a.kv_stride;
+              v += kvh * D;
+              for (int c = 0; c < D; c += 16) {
+                uint32_t r[16];
+                tmem_ld_32x32b_x16(tO + (uint32_t)c, r);
+                tmem_ld_wait();
 #pragma unroll
-              for (int e = 0; e < 16; ++e)
-                if (pj != 0.f) r[e] = __float_as_uint(fmaf(pj, to_f<T>(v[c + e]), __uint_as_float(r[e])));
-              tmem_st_x16(tO + (uint32_t)c, r);
-              tmem_st_wait();
+                for (int e = 0; e < 16; ++e)
+                  if (pj != 0.f) r[e] = __float_as_uint(fmaf(pj, to_f<T>(v[c + e]), __uint_as_float(r[e])));
+                tmem_st_x16(tO + (uint32_t)c, r);
+                tmem_st_wait();
+              }
+              tc_fence_before();
             }
+            if (kSub == 2) pair_sync();  // the half's other warp adds to the same outputs
+            tc_fence_after();
           }
           all_sync();  // everyone has read the odd rows
           if (aid < 4) odd_rows[aid] = 0;
@@ -621,45 +703,46 @@ __global__ void __launch_bounds__(kAtThreads, 1)
         }
       }
       // ---- the piece's results: a thread joins the two halves of its row in
-      // half of the columns, and with REP 2 the row's two lanes meet in shared
-      // memory
+      // its share of the columns, and with REP 2 the row's two lanes meet in
+      // shared memory
       ok = ok && mbar_wait_bounded(o_done, piece & 1, abort_flag, a.err);
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
-      ml[half * 128 + slot] = make_float2(m, l);
-      if (REP == 1) pair_sync(); else all_sync();
+      ml[part * 128 + slot] = make_float2(m, l);
+      if (REP == 1) row_sync(); else all_sync();
       float M = -INFINITY, L = 0.f, f[2];
 #pragma unroll
-      for (int u = 0; u < 2 * REP; ++u) M = fmaxf(M, ml[u * kRowsMax + row].x);  // (half-major, then the copies of the rows)
+      for (int u = 0; u < kParts * REP; ++u) M = fmaxf(M, ml[u * kRowsMax + row].x);  // (part-major, then the copies of the rows)
       const float base = M == -INFINITY ? 0.f : M;
 #pragma unroll
-      for (int u = 0; u < 2 * REP; ++u) {
+      for (int u = 0; u < kParts * REP; ++u) {
         const float2 x = ml[u * kRowsMax + row];
         L = fmaf(x.y, ex2(x.x - base), L);
       }
 #pragma unroll
-      for (int h = 0; h < 2; ++h) f[h] = ex2(ml[h * 128 + slot].x - base);  // 0 where no key was seen
+      for (int h = 0; h < 2; ++h) f[h] = ex2(ml[kSub * h * 128 + slot].x - base);  // 0 where no key was seen
       const float inv = L > 0.f ? 1.0f / L : (L == 0.f ? 0.f : L);  // (a NaN stays one)
       const bool writes = ok && !bad && row < rows && (REP == 1 || rep == 0);
       const int tq = t0 + row / a.group, hd = kvh * a.group + row % a.group;
       T* out = static_cast<T*>(a.out) + ((int64_t)b * a.tokens + tq) * a.out_stride + (int64_t)hd * D;
-      const int64_t part = ((int64_t)2 * blockIdx.x + (cur.i0 == 0 ? 1 : 0)) * kRowsMax + row;
-#pragma unroll
-      for (int c = 0; c < D / 2; c += 32) {
+      const int64_t at = ((int64_t)2 * blockIdx.x + (cur.i0 == 0 ? 1 : 0)) * kRowsMax + row;
+#pragma unroll 1
+      for (int c = 0; c < D / kParts; c += 32) {
+        const int col = part * (D / kParts) + c;
         float o[32];
         if (works) {
           uint32_t r[32];
-          tmem_ld_32x32b_x32(tmem + kTmO + lane_off + (uint32_t)(half * (D / 2) + c), r);
+          tmem_ld_32x32b_x32(tmem + kTmO + lane_off + (uint32_t)col, r);
           tmem_ld_wait();
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(r[e]) * f[0];
-          tmem_ld_32x32b_x32(tmem + kTmO + 128u + lane_off + (uint32_t)(half * (D / 2) + c), r);
+          tmem_ld_32x32b_x32(tmem + kTmO + 128u + lane_off + (uint32_t)col, r);
           tmem_ld_wait();
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = fmaf(__uint_as_float(r[e]), f[1], o[e]);
         }
         if (REP == 2) {
-          float* stage = reinterpret_cast<float*>(smem + F::kOffStage) + (half * 64 + row) * 36;
+          float* stage = reinterpret_cast<float*>(smem + F::kOffStage) + (part * 64 + row) * 36;
           if (rep == 1) {
 #pragma unroll
             for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(stage + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
@@ -677,40 +760,47 @@ __global__ void __launch_bounds__(kAtThreads, 1)
           }
           all_sync();
         }
-        if (writes) {
-          const int col = half * (D / 2) + c;
-          if (whole) {
+        if (!works || (REP == 2 && rep == 1)) continue;  // (the same for all lanes of a warp)
+        if (whole) {
+          uint4 v[4];
 #pragma unroll
-            for (int e = 0; e < 32; e += 8)
-              *reinterpret_cast<uint4*>(out + col + e) =
-                  make_uint4(pack_pair<T>(o[e] * inv, o[e + 1] * inv), pack_pair<T>(o[e + 2] * inv, o[e + 3] * inv),
-                             pack_pair<T>(o[e + 4] * inv, o[e + 5] * inv), pack_pair<T>(o[e + 6] * inv, o[e + 7] * inv));
-          } else {
+          for (int e = 0; e < 4; ++e)
+            v[e] = make_uint4(pack_pair<T>(o[8 * e] * inv, o[8 * e + 1] * inv), pack_pair<T>(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
+                              pack_pair<T>(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_pair<T>(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
+          store_rows(v, reinterpret_cast<char*>(out + col), writes);
+        } else {
+          uint4 v[8];
 #pragma unroll
-            for (int e = 0; e < 32; e += 4)
-              *reinterpret_cast<float4*>(a.part + part * D + col + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-          }
+          for (int e = 0; e < 8; ++e)
+            v[e] = make_uint4(__float_as_uint(o[4 * e]), __float_as_uint(o[4 * e + 1]), __float_as_uint(o[4 * e + 2]), __float_as_uint(o[4 * e + 3]));
+          store_rows(v, reinterpret_cast<char*>(a.part + at * D + col), writes);
         }
       }
       tc_fence_before();
       __syncwarp();
       if (lane == 0 && ok) mbar_arrive(o_free);
-      if (writes && half == 0) {
+      if (writes && part == 0) {
         if (!whole)
-          reinterpret_cast<float2*>(a.ml)[part] = make_float2(M, L);
+          reinterpret_cast<float2*>(a.ml)[at] = make_float2(M, L);
         else if (a.lse)
           a.lse[((int64_t)b * a.heads + hd) * a.tokens + tq] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
       }
-      if (a.splits != 1 && cur.i0 == 0 && aid == 0) {  // the unit's first CTA says how many share it
-        const int64_t end = first_tile + g0 + cur.z.tiles - 1;  // its last tile
+      rest = cur.i0 == 0 && !whole && !bad ? cur.z.tiles : 0;  // the run ends inside this unit
+      rest_rows = rows;
+      if (REP == 1) row_sync(); else all_sync();  // ml is written again
+      pos0 += 2 * n;
+      g0 += n;
+    }
+    if (a.splits != 1 && aid == 0) {
+      int4 record = make_int4(0, 0, 0, 0);
+      if (rest) {  // how many runs it reaches into
+        const int64_t end = first_tile + (g0 - cur.n) + rest - 1;  // its last tile
         int c = (int)(end * runs / total);  // whose run that is, up to the rounding
         while (total * (c + 1) / runs <= end) ++c;
         while (total * c / runs > end) --c;
-        a.units[((int64_t)b * nrt + cur.rt) * a.kv_heads + kvh] = make_int2((int)blockIdx.x, c - (int)blockIdx.x + 1);
+        record = make_int4(cur.b, cur.rt, kvh | rest_rows << 16, c - run + 1);
       }
-      if (REP == 1) pair_sync(); else all_sync();  // ml is written again
-      pos0 += 2 * n;
-      g0 += n;
+      a.units[blockIdx.x] = record;
     }
     tc_fence_before();
   }
@@ -1023,59 +1113,76 @@ int rows_map(CUtensorMap* m, const CachedArgs& a, const void* base, int64_t rows
   return make_tmap_3d(m, a.dtype, base, dims, strides, box);
 }
 
-// The join of units that several CTAs shared: a warp per row, the pieces in
-// order.  A CTA holds at most two pieces that are not whole units: the rest of
-// one that began before its run (slot 2 c) and the start of one that goes on
-// behind it (slot 2 c + 1).
+// The join of the units that several CTAs shared: blockIdx.y is the CTA that
+// begins one.  A CTA holds at most two pieces that are not whole units: the
+// rest of one that began before its run (slot 2 c) and the start of one that
+// goes on behind it (slot 2 c + 1).  A warp per row, or all eight warps of the
+// block where a unit has many pieces; loads of four pieces at a time.
+constexpr int kRjWarps = 8, kRjBlocks = 16, kRjMany = 8;
 template <typename T>
-__global__ void __launch_bounds__(256) attention_runs_join_kernel(const __grid_constant__ CachedArgs a, int queries, int nrt, int row_tile) {
+__global__ void __launch_bounds__(32 * kRjWarps)
+    attention_runs_join_kernel(const __grid_constant__ CachedArgs a, int queries, int row_tile) {
+  __shared__ float4 so[kRjWarps][32];
+  __shared__ float2 sm[kRjWarps];
   pdl_wait();
-  const int kvh = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 31;
-  int len, count;
-  if (!seq_sizes(a, b, &len, &count)) return;
-  if (a.parents) {  // such a sequence's outputs stay as they were
-    bool bad = false;
-    for (int t = threadIdx.x; t < count; t += blockDim.x) {
-      const int p = a.parents[(int64_t)b * a.tokens + t];
-      bad = bad || p < -1 || p >= t;
-    }
-    if (__syncthreads_or(bad)) return;
-  }
-  const int r = (int)blockIdx.x * 8 + warp_index();
-  if (r >= count * a.group) return;
-  const int t = r / a.group, hd = kvh * a.group + r % a.group, rt = t / queries;
-  const int2 u = a.units[((int64_t)b * nrt + rt) * a.kv_heads + kvh];
-  if (u.y <= 1) return;
-  const int rl = (t - rt * queries) * a.group + r % a.group;
-  auto slot = [&](int p) { return ((int64_t)2 * (u.x + p) + (p == 0 ? 1 : 0)) * row_tile + rl; };
+  const int c = blockIdx.y, lane = threadIdx.x & 31, warp = warp_index();
+  const int4 u = a.units[c];
+  if (u.w == 0) return;
+  const int b = u.x, t0 = u.y * queries, kvh = u.z & 0xffff, rows = u.z >> 16, pieces = u.w;
+  const bool many = pieces > kRjMany;
+  const int V = a.dim / 4, first = many ? warp : 0, step = many ? kRjWarps : 1;
   const float2* ml = reinterpret_cast<const float2*>(a.ml);
-  float M = -INFINITY, L = 0.f;
-  for (int p = lane; p < u.y; p += 32) M = fmaxf(M, ml[slot(p)].x);
+  const float4* part = reinterpret_cast<const float4*>(a.part);
+  for (int r0 = blockIdx.x * (many ? 1 : kRjWarps); r0 < rows; r0 += kRjBlocks * (many ? 1 : kRjWarps)) {
+    const int rl = many ? r0 : r0 + warp;
+    const bool own = rl < rows;
+    auto slot = [&](int p) { return ((int64_t)2 * (c + p * a.kv_heads) + (p == 0 ? 1 : 0)) * row_tile + rl; };
+    float M = -INFINITY, L = 0.f;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto take = [&](float2 s, float4 y) {  // (m = -inf: nothing was seen, and y may be anything)
+      const float m = fmaxf(M, s.x), base = m == -INFINITY ? 0.f : m;
+      const float f = ex2(M - base), g = ex2(s.x - base);
+      M = m;
+      L = fmaf(L, f, s.y * g);
+      if (s.x == -INFINITY) y = make_float4(0.f, 0.f, 0.f, 0.f);
+      x.x = fmaf(x.x, f, y.x * g);
+      x.y = fmaf(x.y, f, y.y * g);
+      x.z = fmaf(x.z, f, y.z * g);
+      x.w = fmaf(x.w, f, y.w * g);
+    };
+    for (int p0 = first; own && p0 < pieces; p0 += 4 * step) {
+      float2 s[4];
+      float4 y[4];
 #pragma unroll
-  for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
-  const float base = M == -INFINITY ? 0.f : M;
-  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-  const int V = a.dim / 4;
-  for (int p = 0; p < u.y; ++p) {
-    const int64_t at = slot(p);
-    const float2 s = ml[at];
-    const float f = ex2(s.x - base);
-    L = fmaf(s.y, f, L);
-    if (lane < V && s.x != -INFINITY) {
-      const float4 y = reinterpret_cast<const float4*>(a.part)[at * V + lane];
-      x.x = fmaf(y.x, f, x.x);
-      x.y = fmaf(y.y, f, x.y);
-      x.z = fmaf(y.z, f, x.z);
-      x.w = fmaf(y.w, f, x.w);
+      for (int i = 0; i < 4; ++i) {
+        const int p = p0 + i * step;
+        s[i] = p < pieces ? ml[slot(p)] : make_float2(-INFINITY, 0.f);
+        y[i] = p < pieces && lane < V ? part[slot(p) * V + lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) take(s[i], y[i]);
+    }
+    if (many) {
+      so[warp][lane] = x;
+      if (lane == 0) sm[warp] = make_float2(M, L);
+      __syncthreads();
+      if (warp == 0) {
+#pragma unroll
+        for (int i = 1; i < kRjWarps; ++i) take(sm[i], so[i][lane]);
+      }
+      __syncthreads();
+    }
+    if (own && (!many || warp == 0)) {
+      const int t = t0 + rl / a.group, hd = kvh * a.group + rl % a.group;
+      const float inv = L > 0.f ? 1.0f / L : (L == 0.f ? 0.f : L);
+      if (lane < V) {
+        T* to = static_cast<T*>(a.out) + ((int64_t)b * a.tokens + t) * a.out_stride + (int64_t)hd * a.dim + lane * 4;
+        *reinterpret_cast<uint2*>(to) = make_uint2(pack_pair<T>(x.x * inv, x.y * inv), pack_pair<T>(x.z * inv, x.w * inv));
+      }
+      if (lane == 0 && a.lse)
+        a.lse[((int64_t)b * a.heads + hd) * a.tokens + t] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
     }
   }
-  const float inv = L > 0.f ? 1.0f / L : (L == 0.f ? 0.f : L);
-  if (lane < V) {
-    T* to = static_cast<T*>(a.out) + ((int64_t)b * a.tokens + t) * a.out_stride + (int64_t)hd * a.dim + lane * 4;
-    *reinterpret_cast<uint2*>(to) = make_uint2(pack_pair<T>(x.x * inv, x.y * inv), pack_pair<T>(x.z * inv, x.w * inv));
-  }
-  if (lane == 0 && a.lse)
-    a.lse[((int64_t)b * a.heads + hd) * a.tokens + t] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
 }
 
 template <typename T, int D, int REP> int rows_t(const CachedArgs& a, bool early, cudaStream_t s) {
@@ -1101,7 +1208,8 @@ template <typename T, int D, int REP> int rows_t(const CachedArgs& a, bool early
   cudaLaunchConfig_t cfg;
   std::memset(&cfg, 0, sizeof(cfg));
   const int nrt = (a.tokens + queries - 1) / queries;
-  cfg.gridDim = dim3(a.splits == 1 ? a.n_seq * nrt * a.kv_heads : kRunCtas);
+  const int ctas = run_ctas(a.kv_heads);
+  cfg.gridDim = dim3(a.splits == 1 ? a.n_seq * nrt * a.kv_heads : ctas);
   cfg.blockDim = dim3(kAtThreads);
   cfg.dynamicSmemBytes = TcCfg<D>::kSmem;
   cfg.stream = s;
@@ -1112,11 +1220,11 @@ template <typename T, int D, int REP> int rows_t(const CachedArgs& a, bool early
   cfg.numAttrs = early ? 1 : 0;
   rc = done(cudaLaunchKernelEx(&cfg, kern, q, k, v, kn, vn, a, queries, nrt), "cached attention launch");
   if (rc || a.splits == 1) return rc;
-  cfg.gridDim = dim3((a.tokens * a.group + 7) / 8, a.kv_heads, a.n_seq);
-  cfg.blockDim = dim3(256);
+  cfg.gridDim = dim3(kRjBlocks, ctas);
+  cfg.blockDim = dim3(32 * kRjWarps);
   cfg.dynamicSmemBytes = 0;
   cfg.numAttrs = 1;
-  return done(cudaLaunchKernelEx(&cfg, attention_runs_join_kernel<T>, a, queries, nrt, 128 / REP), "cached attention join launch");
+  return done(cudaLaunchKernelEx(&cfg, attention_runs_join_kernel<T>, a, queries, 128 / REP), "cached attention join launch");
 }
 template <typename T, int D> int rows_d(const CachedArgs& a, bool early, cudaStream_t s) {
   return a.tokens * a.group <= 64 ? rows_t<T, D, 2>(a, early, s) : rows_t<T, D, 1>(a, early, s);
