@@ -16,18 +16,21 @@ namespace swapnet {
 // keys, the join of shared units.
 constexpr double kUnitUs = 5.0, kTileUs = 1.0, kJoinUs = 8.0;
 
-// How many CTAs share the keys of a (sequence, key head): the count
-// whose waves over the SMs take the least time, for the whole cache (how much
-// of it is filled only the device knows).  step / fixed: microseconds of a
-// CTA's tile of keys and of its start and end; more than one also pays the
-// join.
+// How many CTAs share the keys of a (sequence, key head): the count whose waves
+// over the SMs take the least time for the whole cache (how much of it is
+// filled only the device knows); many waves even out.  step / fixed:
+// microseconds of a CTA's tile of keys and of its start and end; more than one
+// also pays the join, where there is one.
 static int choose_splits(int64_t ctas, int tiles, int per_sm, double step, double fixed, double join) {
-  const int64_t room = 152 * per_sm;
+  const int64_t room = kSms * per_sm;
   int best = 1;
   double least = 1e30;
   for (int s = 1; s <= tiles && s <= 128; ++s) {
-    const double waves = std::max(1.0, (double)(ctas * s) / room);  // (many waves even out)
-    const double t = (waves < 4.0 ? std::ceil(waves) : waves) * ((tiles + s - 1) / s * step + fixed) + (s > 1 ? join + 0.02 * s : 0.0);
+    const double one = (tiles + s - 1) / s * step + fixed, waves = (double)(ctas * s) / room;
+    // without a join: unequal lengths and causal limits leave the SMs uneven by
+    // half a CTA, whatever the waves
+    const double t = join == 0.0 ? std::max(one, ctas * (tiles * step + s * fixed) / room + 0.5 * one)
+                                 : (waves < 4.0 ? std::max(1.0, std::ceil(waves)) : waves) * one + (s > 1 ? join + 0.02 * s : 0.0);
     if (t < least * 0.99) {
       least = t;
       best = s;
@@ -77,7 +80,7 @@ int launch_weights(const CachedArgs& a, bool early, cudaStream_t s) {
   CachedArgs x = a;
   if (rows > 32) {
     const int tiles = (int)((rows + 127) / 128);
-    x.splits = choose_splits(pairs, (a.max_seq + 127) / 128, 1, 0.3 + 0.4 * tiles, 2.5, 0.0);
+    x.splits = choose_splits(pairs, (a.max_seq + 127) / 128, 1, 0.3 + 0.35 * tiles, 1.0, 0.0);
     return launch_weights_rows(x, early, s);
   }
   x.splits = choose_splits(pairs, (a.max_seq + 63) / 64, 2, 0.25, 2.0, 0.0);

@@ -7,9 +7,9 @@
 // one CTA per SM takes units, or an equal run of all units' key tiles (128 keys
 // each; the drafted nodes are one more tile, the last), whatever the
 // sequences' lengths.  Per tile:
-//   S = Q K^T     tcgen05.mma, M 128 (rows) x N 128 (keys); Q, K and V by TMA
-//                 (128-byte swizzle); S in two TMEM buffers, so that the next
-//                 tile's S is computed during this tile's softmax
+//   S = Q K^T     tcgen05.mma, M 128 (rows) x N 64 (keys), twice; Q, K and V by
+//                 TMA (128-byte swizzle); S in two TMEM buffers, so that the
+//                 next tile's S is computed during this tile's softmax
 //   P             warps 4..19, four threads per row, 32 keys each: the first 64
 //                 keys of every tile and the last 64 have a softmax of their
 //                 own (reference m, sum l, output O_h), whose two threads only
@@ -251,15 +251,15 @@ __global__ void __launch_bounds__(kAtThreads, 1)
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + F::kOffBar);
   auto full = [&](int s) { return smem_u32(bars + s); };
   auto empty = [&](int s) { return smem_u32(bars + 8 + s); };
-  auto s_full = [&](int i) { return smem_u32(bars + 16 + (i & 1)); };
   // one per half and buffer: a half may be two tiles ahead of the products
-  auto p_full = [&](int h, int i) { return smem_u32(bars + 18 + 2 * h + (i & 1)); };
-  auto o_full = [&](int h) { return smem_u32(bars + 22 + h); };
-  const uint32_t q_full = smem_u32(bars + 24), q_free = smem_u32(bars + 25);  // a piece's queries
-  const uint32_t o_done = smem_u32(bars + 26), o_free = smem_u32(bars + 27);  // a piece's outputs
-  const uint32_t done_bar = smem_u32(bars + 28);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 29);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 30);
+  auto s_full = [&](int h, int i) { return smem_u32(bars + 16 + 2 * h + (i & 1)); };
+  auto p_full = [&](int h, int i) { return smem_u32(bars + 20 + 2 * h + (i & 1)); };
+  auto o_full = [&](int h) { return smem_u32(bars + 24 + h); };
+  const uint32_t q_full = smem_u32(bars + 26), q_free = smem_u32(bars + 27);  // a piece's queries
+  const uint32_t o_done = smem_u32(bars + 28), o_free = smem_u32(bars + 29);  // a piece's outputs
+  const uint32_t done_bar = smem_u32(bars + 30);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 31);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int2* near = reinterpret_cast<int2*>(smem + F::kOffNear);
   int64_t* sched = reinterpret_cast<int64_t*>(ml);  // (before the first results)
 
@@ -270,9 +270,11 @@ __global__ void __launch_bounds__(kAtThreads, 1)
       mbar_init(empty(s), 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(s_full(i), 1);
       mbar_init(o_full(i), 1);
-      for (int h = 0; h < 2; ++h) mbar_init(p_full(h, i), 4 * kSub);
+      for (int h = 0; h < 2; ++h) {
+        mbar_init(s_full(h, i), 1);
+        mbar_init(p_full(h, i), 4 * kSub);
+      }
     }
     mbar_init(q_full, 1);
     mbar_init(q_free, 1);
@@ -414,7 +416,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
     if (warp == 1 && elect_one()) {
       // ---------------- MMA issuer
       constexpr int bf = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
-      constexpr uint32_t idesc_s = idesc_f16(bf, 128, kKeys);
+      constexpr uint32_t idesc_s = idesc_f16(bf, 128, kKeys / 2);
       constexpr uint32_t idesc_pv = idesc_f16(bf, 128, D) | (1u << 16);  // B (values) MN-major
       const uint64_t qd = smem_desc_sw128(smem_u32(smem + F::kOffQ));
       const uint64_t kd = smem_desc_sw128(smem_u32(smem + F::kOffRing)), vd = desc_mn(smem_u32(smem + F::kOffRing));
@@ -423,33 +425,38 @@ __global__ void __launch_bounds__(kAtThreads, 1)
       auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_bounded(bar, parity, abort_flag, a.err); };
       for (int piece = 0; ok && cur.step(a, nrt, queries); ++piece) {
         const int n = cur.n;
-        auto scores = [&](int i) -> bool {
+        // The halves' scores and products take turns, so that one half's warps
+        // (one of the two on each scheduler) take exponentials while the
+        // other's wait, load and store.
+        auto scores = [&](int i, int h) -> bool {
           const int pos = pos0 + k_pos(i), s = pos % F::kSlots, g = g0 + i;
-          if (!wait(full(s), (pos / F::kSlots) & 1)) return false;
+          if (h == 0 && !wait(full(s), (pos / F::kSlots) & 1)) return false;
           // (over the P of two tiles ago: the tensor core runs the MMAs of one
           // thread in the order of their issue, so its product, issued before,
           // has read it)
           tc_fence_after();
-          const uint64_t kt = kd + (uint64_t)(s * (F::kTile >> 4));  // the descriptors' address field counts 16 bytes
+          const uint64_t kt = kd + (uint64_t)(s * (F::kTile >> 4) + h * (64 * 128 >> 4));  // the descriptors' address field counts 16 bytes
 #pragma unroll
-          for (int h = 0; h < F::kHalves; ++h)
+          for (int c = 0; c < F::kHalves; ++c)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              tc_mma_f16(tmem + (uint32_t)(g & 1) * 128u, qd + (uint64_t)(h * (F::kBox >> 4) + 2 * k),
-                         kt + (uint64_t)(h * (F::kBox >> 4) + 2 * k), idesc_s, (h | k) != 0);
-          tc_commit(s_full(g));
-          tc_commit(empty(s));
-          if (i == n - 1) tc_commit(q_free);
+              tc_mma_f16(tmem + (uint32_t)(g & 1) * 128u + (uint32_t)h * 64u, qd + (uint64_t)(c * (F::kBox >> 4) + 2 * k),
+                         kt + (uint64_t)(c * (F::kBox >> 4) + 2 * k), idesc_s, (c | k) != 0);
+          tc_commit(s_full(h, g));
+          if (h == 1) {
+            tc_commit(empty(s));
+            if (i == n - 1) tc_commit(q_free);
+          }
           return true;
         };
-        ok = wait(q_full, piece & 1) && scores(0);
+        ok = wait(q_full, piece & 1) && scores(0, 0) && scores(0, 1);
         for (int i = 0; ok && i < n; ++i) {
-          if (i + 1 < n && !(ok = scores(i + 1))) break;
           const int pos = pos0 + v_pos(i, n), s = pos % F::kSlots, g = g0 + i;
-          ok = wait(full(s), (pos / F::kSlots) & 1) && (i > 0 || piece == 0 || wait(o_free, (piece - 1) & 1));
           const uint64_t vt = vd + (uint64_t)(s * (F::kTile >> 4));
           for (int h = 0; ok && h < 2; ++h) {
-            ok = wait(p_full(h, g), (g >> 1) & 1);
+            if (i + 1 < n && !(ok = scores(i + 1, h))) break;
+            ok = (h == 1 || (wait(full(s), (pos / F::kSlots) & 1) && (i > 0 || piece == 0 || wait(o_free, (piece - 1) & 1)))) &&
+                 wait(p_full(h, g), (g >> 1) & 1);
             if (!ok) break;
             tc_fence_after();
             const uint32_t pt = tmem + (uint32_t)(g & 1) * 128u + (uint32_t)h * 64u;
@@ -516,7 +523,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
         const int k0 = nw ? 0 : (cur.i0 + i) * kKeys;
         const bool masked = nw || k0 + kKeys > lim_min;  // some of these keys are hidden from some rows
         const uint32_t tS = tmem + (uint32_t)(g & 1) * 128u + lane_off;
-        ok = ok && mbar_wait_bounded(s_full(g), (g >> 1) & 1, abort_flag, a.err);
+        ok = ok && mbar_wait_bounded(s_full(half, g), (g >> 1) & 1, abort_flag, a.err);
         ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
         uint32_t hi[NK / 2], lo[NK / 2];
@@ -817,26 +824,27 @@ __global__ void __launch_bounds__(kAtThreads, 1)
 // the keys as the MMA's rows, S^T = K Q^T (M 128 keys x N up to 128 rows), so
 // that a key's sum over the rows stays in one thread.  A CTA takes every
 // splits-th tile of 128 keys of a (sequence, key head) and passes all tiles of
-// rows that see it; K and Q tiles by TMA, S in four TMEM buffers, two threads
-// per key (their sums meet in shared memory).  Rows of a list are fetched one
-// query at a time.
+// rows that see it; K and Q tiles by TMA, S in two TMEM buffers, two threads
+// per key (their sums meet in shared memory).  Two CTAs share an SM: one's
+// start and waits are the other's time.  Rows of a list are fetched one query
+// at a time.
 template <int D> struct WtCfg {
   static constexpr int kHalves = D / 64;
   static constexpr int kBox = 128 * 128;
   static constexpr int kTile = kHalves * kBox;
-  static constexpr int kKSlots = 3, kQSlots = 3;
-  static constexpr int kOffQ = kKSlots * kTile;
-  static constexpr int kOffLse = kOffQ + kQSlots * kTile;  // [2][128] log2 of the rows' sums
+  static constexpr int kSlots = 3;                         // of keys and queries
+  static constexpr int kOffLse = kSlots * kTile;           // [2][128] log2 of the rows' sums
   static constexpr int kOffLim = kOffLse + 2 * 128 * 4;
   static constexpr int kOffX = kOffLim + 2 * 128 * 4;
   static constexpr int kOffBar = kOffX + 2 * 128 * 4;
   static constexpr int kSmem = kOffBar + 256 + 1024;
-  static_assert(kSmem <= 232448, "shared memory of a CTA");
+  static_assert(2 * (kSmem + 1024) <= 233472, "two CTAs per SM");
 };
-constexpr int kSBufs = 4;
+constexpr int kSBufs = 2;
+constexpr uint32_t kWtTmemCols = 256;  // two CTAs share the SM's 512
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kTcThreads, 1)
+__global__ void __launch_bounds__(kTcThreads, 2)
     weights_rows_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                         const __grid_constant__ CachedArgs a, int queries) {
   using F = WtCfg<D>;
@@ -866,14 +874,16 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   if (split >= ktiles) return;
   // the first tile of rows that sees key k0 (row i sees the keys below len - count + i + 1)
   auto first_tile = [&](int kt) { return max(0, kt * kKeys - (len - count)) / queries; };
-  const bool keep_q = nrt <= F::kQSlots;  // all queries stay
+  // one tile of rows: its queries stay, and two slots take keys in turn; more:
+  // the queries pass through two slots for every tile of keys
+  const bool one = nrt <= 1;
+  const int ks = one ? 2 : 1, qs = one ? 1 : 2;
+  uint8_t* smem_q = smem + ks * F::kTile;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < F::kKSlots; ++s) {
+    for (int s = 0; s < 2; ++s) {
       mbar_init(k_full(s), 1);
       mbar_init(k_empty(s), 1);
-    }
-    for (int s = 0; s < F::kQSlots; ++s) {
       mbar_init(q_full(s), 1);
       mbar_init(q_empty(s), 1);
     }
@@ -888,7 +898,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     prefetch_tmap(&tmK);
   }
   if (warp == 1) {
-    tmem_alloc(smem_u32(tmem_slot), kTmemCols);
+    tmem_alloc(smem_u32(tmem_slot), kWtTmemCols);
     tmem_relinquish();
   }
   tc_fence_before();
@@ -901,7 +911,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       // ---------------- TMA producer
       auto load_q = [&](int rt, int slot) {
         const int t0 = rt * queries;
-        const uint32_t dst = smem_u32(smem + F::kOffQ + slot * F::kTile);
+        const uint32_t dst = smem_u32(smem_q + slot * F::kTile);
         if (!a.rows) {
           mbar_arrive_expect_tx(q_full(slot), F::kHalves * queries * a.group * 128);
 #pragma unroll
@@ -921,55 +931,52 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       int it = 0, kp = 0;
       bool ok = true;
       for (int kt = split; ok && kt < ktiles; kt += a.splits, ++kp) {
-        const int s = kp % F::kKSlots;
-        if (kp >= F::kKSlots && !mbar_wait_bounded(k_empty(s), ((kp / F::kKSlots) - 1) & 1, abort_flag, a.err)) break;
+        const int s = kp % ks;
+        if (kp >= ks && !mbar_wait_bounded(k_empty(s), ((kp / ks) - 1) & 1, abort_flag, a.err)) break;
         mbar_arrive_expect_tx(k_full(s), F::kTile);
 #pragma unroll
         for (int h = 0; h < F::kHalves; ++h)
           tma_load_3d(smem_u32(smem + s * F::kTile + h * F::kBox), &tmK, k_full(s), kvh * D + h * 64, kt * kKeys, b);
-        if (keep_q) {
-          if (kp == 0)
-            for (int rt = 0; rt < nrt; ++rt) load_q(rt, rt);
+        if (one) {
+          if (kp == 0) load_q(0, 0);
           continue;
         }
         for (int rt = first_tile(kt); rt < nrt; ++rt, ++it) {
-          const int qs = it % F::kQSlots;
-          if (it >= F::kQSlots && !mbar_wait_bounded(q_empty(qs), ((it / F::kQSlots) - 1) & 1, abort_flag, a.err)) {
+          const int slot = it % qs;
+          if (it >= qs && !mbar_wait_bounded(q_empty(slot), ((it / qs) - 1) & 1, abort_flag, a.err)) {
             ok = false;
             ++kp;  // its keys are on their way
             break;
           }
-          load_q(rt, qs);
+          load_q(rt, slot);
         }
         if (!ok) break;
       }
       // let every load issued land before the CTA can exit
       volatile int no_abort = 0;
-      for (int j = max(0, kp - F::kKSlots); j < kp; ++j)
-        mbar_wait_bounded(k_full(j % F::kKSlots), (j / F::kKSlots) & 1, &no_abort, nullptr);
-      const int nl = keep_q ? nrt : it;
-      for (int j = max(0, nl - F::kQSlots); j < nl; ++j)
-        mbar_wait_bounded(q_full(j % F::kQSlots), (j / F::kQSlots) & 1, &no_abort, nullptr);
+      for (int j = max(0, kp - ks); j < kp; ++j) mbar_wait_bounded(k_full(j % ks), (j / ks) & 1, &no_abort, nullptr);
+      const int nl = one ? min(kp, 1) : it;
+      for (int j = max(0, nl - qs); j < nl; ++j) mbar_wait_bounded(q_full(j % qs), (j / qs) & 1, &no_abort, nullptr);
     }
   } else if (warp == 1) {
     if (nrt > 0 && elect_one()) {
       // ---------------- MMA issuer
       constexpr int bf = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
-      const uint64_t kd = smem_desc_sw128(smem_u32(smem)), qd = smem_desc_sw128(smem_u32(smem + F::kOffQ));
+      const uint64_t kd = smem_desc_sw128(smem_u32(smem)), qd = smem_desc_sw128(smem_u32(smem_q));
       int it = 0, kp = 0;
       bool ok = true;
       for (int kt = split; ok && kt < ktiles; kt += a.splits, ++kp) {
-        const int s = kp % F::kKSlots;
-        if (!mbar_wait_bounded(k_full(s), (kp / F::kKSlots) & 1, abort_flag, a.err)) break;
+        const int s = kp % ks;
+        if (!mbar_wait_bounded(k_full(s), (kp / ks) & 1, abort_flag, a.err)) break;
         for (int rt = first_tile(kt); ok && rt < nrt; ++rt, ++it) {
-          const int qs = keep_q ? rt : it % F::kQSlots, sb = it % kSBufs;
-          ok = mbar_wait_bounded(q_full(qs), keep_q ? 0 : (it / F::kQSlots) & 1, abort_flag, a.err) &&
+          const int slot = one ? 0 : it % qs, sb = it % kSBufs;
+          ok = mbar_wait_bounded(q_full(slot), one ? 0 : (it / qs) & 1, abort_flag, a.err) &&
                (it < kSBufs || mbar_wait_bounded(s_empty(sb), ((it / kSBufs) - 1) & 1, abort_flag, a.err));
           if (!ok) break;
           tc_fence_after();
           const int n = (min(queries, count - rt * queries) * a.group + 15) / 16 * 16;
           const uint32_t idesc = idesc_f16(bf, 128, n);
-          const uint64_t kk = kd + (uint64_t)(s * (F::kTile >> 4)), qq = qd + (uint64_t)(qs * (F::kTile >> 4));
+          const uint64_t kk = kd + (uint64_t)(s * (F::kTile >> 4)), qq = qd + (uint64_t)(slot * (F::kTile >> 4));
 #pragma unroll
           for (int h = 0; h < F::kHalves; ++h)
 #pragma unroll
@@ -977,7 +984,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
               tc_mma_f16(tmem + (uint32_t)sb * 128u, kk + (uint64_t)(h * (F::kBox >> 4) + 2 * k),
                          qq + (uint64_t)(h * (F::kBox >> 4) + 2 * k), idesc, (h | k) != 0);
           tc_commit(s_full(sb));
-          if (!keep_q) tc_commit(q_empty(qs));
+          if (!one) tc_commit(q_empty(slot));
         }
         tc_commit(k_empty(s));
       }
@@ -1019,7 +1026,6 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         lim[buf * 128 + aid] = row_lim;
       }
     };
-    const bool one = nrt == 1;  // the rows' limits and sums stay
     if (nrt > 0) {
       fetch(first_tile(split));
       store(0);
@@ -1040,34 +1046,40 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         tc_fence_after();
         if (ok) {
           const int rows = min(queries, count - rt * queries) * a.group, nch = (rows + 15) / 16;
-          uint32_t s[4][16];
+          const uint32_t tS = tmem + (uint32_t)sb * 128u + lane_off;
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (half + 2 * c < nch) tmem_ld_32x32b_x16(tmem + (uint32_t)sb * 128u + lane_off + (uint32_t)((half + 2 * c) * 16), s[c]);
-          tmem_ld_wait();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(s_empty(sb));
+          for (int c2 = 0; c2 < 4; c2 += 2) {  // two of the half's chunks of 16 rows at a time
+            uint32_t s[2][16];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const int c0 = (half + 2 * c) * 16;
-            if (c0 >= rows) break;
-            const float* le = lse2 + buf * 128 + c0;
-            const int* li = lim + buf * 128 + c0;
-            const bool masked = kt * kKeys + kKeys > li[0] || c0 + 16 > rows;
+            for (int c = 0; c < 2; ++c)
+              if (half + 2 * (c2 + c) < nch) tmem_ld_32x32b_x16(tS + (uint32_t)((half + 2 * (c2 + c)) * 16), s[c]);
+            tmem_ld_wait();
+            if (c2 == 2) {  // all has been read
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(s_empty(sb));
+            }
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-              const float4 l4 = *reinterpret_cast<const float4*>(le + e);
-              const float ll[4] = {l4.x, l4.y, l4.z, l4.w};
-              float p[4];
+            for (int c = 0; c < 2; ++c) {
+              const int c0 = (half + 2 * (c2 + c)) * 16;
+              if (c0 >= rows) break;
+              const float* le = lse2 + buf * 128 + c0;
+              const int* li = lim + buf * 128 + c0;
+              const bool masked = kt * kKeys + kKeys > li[0] || c0 + 16 > rows;
 #pragma unroll
-              for (int u = 0; u < 4; ++u) p[u] = ex2(fmaf(__uint_as_float(s[c][e + u]), a.scale_log2, -ll[u]));
-              if (masked) {
+              for (int e = 0; e < 16; e += 4) {
+                const float4 l4 = *reinterpret_cast<const float4*>(le + e);
+                const float ll[4] = {l4.x, l4.y, l4.z, l4.w};
+                float p[4];
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-                  if (j >= li[e + u]) p[u] = 0.f;
+                for (int u = 0; u < 4; ++u) p[u] = ex2(fmaf(__uint_as_float(s[c][e + u]), a.scale_log2, -ll[u]));
+                if (masked) {
+#pragma unroll
+                  for (int u = 0; u < 4; ++u)
+                    if (j >= li[e + u]) p[u] = 0.f;
+                }
+                sum += (p[0] + p[1]) + (p[2] + p[3]);
               }
-              sum += (p[0] + p[1]) + (p[2] + p[3]);
             }
           }
         }
@@ -1087,7 +1099,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(tmem, kTmemCols);
+    tmem_dealloc(tmem, kWtTmemCols);
   }
 }
 
@@ -1118,7 +1130,7 @@ int rows_map(CUtensorMap* m, const CachedArgs& a, const void* base, int64_t rows
 // rest of one that began before its run (slot 2 c) and the start of one that
 // goes on behind it (slot 2 c + 1).  A warp per row, or all eight warps of the
 // block where a unit has many pieces; loads of four pieces at a time.
-constexpr int kRjWarps = 8, kRjBlocks = 16, kRjMany = 8;
+constexpr int kRjWarps = 8, kRjMany = 8;
 template <typename T>
 __global__ void __launch_bounds__(32 * kRjWarps)
     attention_runs_join_kernel(const __grid_constant__ CachedArgs a, int queries, int row_tile) {
@@ -1133,7 +1145,7 @@ __global__ void __launch_bounds__(32 * kRjWarps)
   const int V = a.dim / 4, first = many ? warp : 0, step = many ? kRjWarps : 1;
   const float2* ml = reinterpret_cast<const float2*>(a.ml);
   const float4* part = reinterpret_cast<const float4*>(a.part);
-  for (int r0 = blockIdx.x * (many ? 1 : kRjWarps); r0 < rows; r0 += kRjBlocks * (many ? 1 : kRjWarps)) {
+  for (int r0 = blockIdx.x * (many ? 1 : kRjWarps); r0 < rows; r0 += gridDim.x * (many ? 1 : kRjWarps)) {
     const int rl = many ? r0 : r0 + warp;
     const bool own = rl < rows;
     auto slot = [&](int p) { return ((int64_t)2 * (c + p * a.kv_heads) + (p == 0 ? 1 : 0)) * row_tile + rl; };
@@ -1220,7 +1232,9 @@ template <typename T, int D, int REP> int rows_t(const CachedArgs& a, bool early
   cfg.numAttrs = early ? 1 : 0;
   rc = done(cudaLaunchKernelEx(&cfg, kern, q, k, v, kn, vn, a, queries, nrt), "cached attention launch");
   if (rc || a.splits == 1) return rc;
-  cfg.gridDim = dim3(kRjBlocks, ctas);
+  // a row per warp of at most 128; where few units have many pieces, a block per row
+  const int64_t units = (int64_t)a.n_seq * nrt * a.kv_heads;
+  cfg.gridDim = dim3(units <= ctas / kRjMany ? std::min(queries * a.group, 64) : (queries * a.group + kRjWarps - 1) / kRjWarps, ctas);
   cfg.blockDim = dim3(32 * kRjWarps);
   cfg.dynamicSmemBytes = 0;
   cfg.numAttrs = 1;
