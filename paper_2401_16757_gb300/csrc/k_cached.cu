@@ -91,7 +91,6 @@ __global__ void __launch_bounds__(kFwThreads, 2) attention_few_kernel(const __gr
   if (!seq_sizes(a, b, &len, &count)) return;
   const int rows = count * a.group;
   if (r0 >= rows) return;
-  if (a.k_new && !build_ancestors(a, b, count, anc, par)) return;
   const int t_last = (min(r0 + F::kRows, rows) - 1) / a.group;
   const int kmax = visible_limit(a, len, count, t_last), lim_min = visible_limit(a, len, count, r0 / a.group);
   const int gp = (kmax + kGk - 1) / kGk, groups = gp + (a.k_new ? (count + kGk - 1) / kGk : 0);
@@ -124,6 +123,10 @@ __global__ void __launch_bounds__(kFwThreads, 2) attention_few_kernel(const __gr
   for (int i = 0; i < kFwStages - 1; ++i) load(g_begin + warp + i * kFwWarps, i);
 
   load_queries<T, D>(a, b, kvh, r0, rows, F::kRows, smem + F::kOffQ, nullptr);
+  if (a.k_new && !build_ancestors(a, b, count, anc, par)) {  // (while the first groups arrive)
+    cp_async_wait<0>();
+    return;
+  }
   __syncthreads();
   const uint32_t q_u = smem_u32(smem + F::kOffQ);
   auto query_frag = [&](int mt, int ks, uint32_t(&f)[4]) {
