@@ -783,7 +783,7 @@ typedef struct swapnet_cached_attention {
  *     holds its row).  A query that sees no row gives 0 and lse = -inf.
  * With `weights` (no draft): weights[j] = weights_in[j] + the attention that
  * row j got from these queries, summed over the query heads that share its
- * key head; more than 32 rows (tokens x heads / kv_heads) need lse.
+ * key head; more than 16 rows (tokens x heads / kv_heads) need lse.
  * Queries at and behind counts, and weights at and behind lens, are left as
  * they were.  Hidden rows may hold anything.  `workspace` is 256-byte aligned
  * device memory of at least the bytes that _workspace returns (a function of

@@ -16,22 +16,19 @@ namespace swapnet {
 // keys, the join of shared units.
 constexpr double kUnitUs = 5.0, kTileUs = 1.0, kJoinUs = 8.0;
 
-// How many CTAs share the keys of a (sequence, key head): the count whose waves
-// over the SMs take the least time for the whole cache (how much of it is
-// filled only the device knows); many waves even out.  step / fixed:
-// microseconds of a CTA's tile of keys and of its start and end; more than one
-// also pays the join, where there is one.
-static int choose_splits(int64_t ctas, int tiles, int per_sm, double step, double fixed, double join) {
-  const int64_t room = kSms * per_sm;
+// How many CTAs share the keys of a (sequence, key head), for the whole cache
+// (how much of it is filled only the device knows): the count that takes the
+// least time where every SM gets its share of all work, but for half a CTA at
+// the end (lengths and causal limits differ).  In microseconds: a tile of a CTA
+// by itself, a tile of an SM's time when all are busy, a CTA's start and end,
+// and the join where there is one.
+static int choose_splits(int64_t ctas, int tiles, double alone, double busy, double fixed, double join) {
   int best = 1;
   double least = 1e30;
   for (int s = 1; s <= tiles && s <= 128; ++s) {
-    const double one = (tiles + s - 1) / s * step + fixed, waves = (double)(ctas * s) / room;
-    // without a join: unequal lengths and causal limits leave the SMs uneven by
-    // half a CTA, whatever the waves
-    const double t = join == 0.0 ? std::max(one, ctas * (tiles * step + s * fixed) / room + 0.5 * one)
-                                 : (waves < 4.0 ? std::max(1.0, std::ceil(waves)) : waves) * one + (s > 1 ? join + 0.02 * s : 0.0);
-    if (t < least * 0.99) {
+    const double one = (tiles + s - 1) / s * alone + fixed;
+    const double t = std::max(one, ctas * (tiles * busy + s * fixed) / kSms + 0.5 * one) + (s > 1 && join > 0.0 ? join + 0.02 * s : 0.0);
+    if (t < least * 0.995) {
       least = t;
       best = s;
     }
@@ -43,8 +40,12 @@ CachedPlan cached_plan(const CachedArgs& a) {
   CachedPlan p;
   std::memset(&p, 0, sizeof(p));
   const int64_t rows = (int64_t)a.tokens * a.group, pairs = (int64_t)a.n_seq * a.kv_heads;
-  p.tc = rows > 32;
-  p.spill = a.weights && rows <= 32;
+  // Warp products of 16 rows or tensor cores with 128 (us, 8 key heads of 128
+  // unless said otherwise): 16 rows on 8000 keys x 32 sequences 118 / 122, 500 x
+  // 1 10.6 / 15.4, 32000 x 1 36 / 34.5, 32 key heads 500 x 32 61 / 103; 20 rows,
+  // which would take two products, 233 / 123, 13.2 / 15.4, 60 / 34.6.
+  p.tc = rows > kFewAttnRows;
+  p.spill = a.weights && !p.tc;
   if (p.tc) {
     const int row_tile = rows <= 64 ? 64 : 128, queries = std::min(row_tile / a.group, a.tokens);
     const int64_t units = pairs * ((a.tokens + queries - 1) / queries);
@@ -66,7 +67,7 @@ CachedPlan cached_plan(const CachedArgs& a) {
     }
     return p;
   }
-  p.splits = choose_splits(pairs, (a.max_seq + 63) / 64, 2, 0.5, 2.0, 2.0);
+  p.splits = choose_splits(pairs, (a.max_seq + 63) / 64, 0.5, 0.7, 1.5, 2.5);
   p.score_ld = (a.max_seq + 15) / 16 * 16;
   const uint64_t all = (uint64_t)pairs * rows;
   if (p.splits > 1) p.part_bytes = align_up(all * p.splits * a.dim * 4);
@@ -75,16 +76,9 @@ CachedPlan cached_plan(const CachedArgs& a) {
   return p;
 }
 
-int launch_weights(const CachedArgs& a, bool early, cudaStream_t s) {
-  const int64_t rows = (int64_t)a.tokens * a.group, pairs = (int64_t)a.n_seq * a.kv_heads;
-  CachedArgs x = a;
-  if (rows > 32) {
-    const int tiles = (int)((rows + 127) / 128);
-    x.splits = choose_splits(pairs, (a.max_seq + 127) / 128, 1, 0.3 + 0.35 * tiles, 1.0, 0.0);
-    return launch_weights_rows(x, early, s);
-  }
-  x.splits = choose_splits(pairs, (a.max_seq + 63) / 64, 2, 0.25, 2.0, 0.0);
-  return launch_weights_few(x, early, s);
+int weights_splits(const CachedArgs& a) {
+  const int tiles = (int)(((int64_t)a.tokens * a.group + 127) / 128);
+  return choose_splits((int64_t)a.n_seq * a.kv_heads, (a.max_seq + 127) / 128, 0.3 + 0.35 * tiles, 0.3 + 0.35 * tiles, 1.0, 0.0);
 }
 
 int run_cached_attention(CachedArgs a, const CachedPlan& p, void* workspace, bool early, cudaStream_t s) {
@@ -98,7 +92,7 @@ int run_cached_attention(CachedArgs a, const CachedPlan& p, void* workspace, boo
   if (int rc = p.tc ? launch_attention_rows(a, early, s) : launch_attention_few(a, early, s)) return rc;
   if (!p.tc)
     if (int rc = launch_attention_join(a, s)) return rc;
-  return a.weights && !p.spill ? launch_weights(a, true, s) : SWAPNET_OK;
+  return a.weights && !p.spill ? launch_weights(a, weights_splits(a), true, s) : SWAPNET_OK;
 }
 
 void state_attention(const Model& m, char* state, int index, CachedArgs* out) {
@@ -212,7 +206,7 @@ int check_attention(const swapnet_cached_attention* c, CachedArgs* a) {
     SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention: weights with a draft come from swapnet_attention_weights, once it is accepted");
   if (c->weights_in && !c->weights) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention: weights_in without weights");
   if (c->weights && cached_plan(*a).spill == 0 && !c->lse)
-    SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention: weights of more than 32 rows (tokens x heads / kv_heads) need lse");
+    SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention: weights of more than 16 rows (tokens x heads / kv_heads) need lse");
   return SWAPNET_OK;
 }
 
@@ -269,7 +263,7 @@ int swapnet_attention_weights(const swapnet_cached_attention* c, swapnet_stream 
     if (!c->lse || !c->weights) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cache weights: null pointer");
     if (c->k_new || c->v_new || c->parents) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cache weights: the queries are rows of the cache");
     if (int rc = error_word(&a.err)) return rc;
-    return launch_weights(a, false, reinterpret_cast<cudaStream_t>(stream));
+    return launch_weights(a, weights_splits(a), false, reinterpret_cast<cudaStream_t>(stream));
   });
 }
 

@@ -9,6 +9,7 @@
 
 namespace swapnet {
 
+constexpr int kFewAttnRows = 16;   // of a (sequence, key head) that the few-row kernel takes
 constexpr int kTreeMax = 128;  // drafted nodes of a sequence: one tile of keys, 128 ancestor bits
 
 // Row r of a (sequence, key head) is query r / group of the sequence for head
@@ -62,10 +63,8 @@ int cached_launches(const CachedArgs& a, const CachedPlan& p);
 int launch_attention_rows(const CachedArgs& a, bool early, cudaStream_t s);  // tcgen05
 int launch_attention_few(const CachedArgs& a, bool early, cudaStream_t s);
 int launch_attention_join(const CachedArgs& a, cudaStream_t s);   // splits -> out, lse (and weights from scores)
-int launch_weights_few(const CachedArgs& a, bool early, cudaStream_t s);
-int launch_weights_rows(const CachedArgs& a, bool early, cudaStream_t s);  // tcgen05
-// The weights by the kernel and the splits that the sizes call for.
-int launch_weights(const CachedArgs& a, bool early, cudaStream_t s);
+int launch_weights(const CachedArgs& a, int splits, bool early, cudaStream_t s);  // tcgen05
+int weights_splits(const CachedArgs& a);
 
 struct EvictArgs {
   int dtype, n_seq, kv_heads, dim, max_seq, keep, recent, sink, out_seq;

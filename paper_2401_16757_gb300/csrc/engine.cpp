@@ -2011,7 +2011,7 @@ int swapnet_engine_tree_accept(swapnet_engine* e, const int32_t* d_ids, const in
       w.weights = reinterpret_cast<float*>(e->d_state + st.weights);
       w.weights_in = w.weights;
       w.err = e->err_word;
-      rc = launch_weights(w, false, s);
+      rc = launch_weights(w, weights_splits(w), false, s);
     }
     return rc ? rc : launch_state_header(header, 1, 0, 0, s);
   });

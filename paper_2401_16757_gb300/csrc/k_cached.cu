@@ -1,6 +1,6 @@
-// Attention of a few queries over a long key-value cache (decode steps,
-// drafted trees), the join of its splits, and the weights that the cached rows
-// get.  fp16 / bf16 storage, fp32 arithmetic, fixed orders of summation.
+// Attention of a few queries over a long key-value cache (decode steps, small
+// drafted trees), and the join of its splits, with the weights that the cached
+// rows got.  fp16 / bf16 storage, fp32 arithmetic, fixed orders of summation.
 //
 // Rows of a (sequence, key head) are its queries times the heads that share
 // the key head: they read the same keys, so one warp-level product serves up
@@ -22,11 +22,11 @@ constexpr int kFwWarps = 4, kFwThreads = 32 * kFwWarps;
 constexpr int kGk = 16;      // keys of a group: one step of a warp
 constexpr int kFwStages = 3;
 
-template <int D, int MT> struct FewCfg {
+template <int D> struct FewCfg {
   static constexpr int kGroup = kGk * D * 2;          // bytes of a group's keys (or values)
   static constexpr int kWarpRing = kFwStages * 2 * kGroup;
   static constexpr int kRing = kFwWarps * kWarpRing;
-  static constexpr int kRows = 16 * MT;
+  static constexpr int kRows = kFewAttnRows;
   static constexpr int kQ = kRows * D * 2;
   static constexpr int kP = kFwWarps * kRows * kGk * 4;
   static constexpr int kOffQ = kRing;
@@ -45,24 +45,20 @@ template <int D> __device__ __forceinline__ uint32_t swz(int r, int c) { return 
 
 // The rows' queries into shared memory (zeros behind the last row).
 template <typename T, int D>
-__device__ __forceinline__ void load_queries(const CachedArgs& a, int b, int kvh, int r0, int rows, int cap, uint8_t* dst,
-                                             const int* row_of) {
+__device__ __forceinline__ void load_queries(const CachedArgs& a, int b, int kvh, int rows, uint8_t* dst) {
   constexpr int C = D / 8;
-  for (int i = threadIdx.x; i < cap * C; i += blockDim.x) {
-    const int rl = i / C, c = i % C, r = r0 + rl;
+  for (int i = threadIdx.x; i < kFewAttnRows * C; i += kFwThreads) {
+    const int r = i / C, c = i % C;
     uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (r < rows) {
-      const int t = row_of ? row_of[rl] : r / a.group;
-      if (t >= 0)
-        v = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + ((int64_t)b * a.tokens + t) * a.q_stride +
-                                            (int64_t)(kvh * a.group + r % a.group) * D + c * 8);
-    }
-    *reinterpret_cast<uint4*>(dst + swz<D>(rl, c)) = v;
+    if (r < rows)
+      v = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + ((int64_t)b * a.tokens + r / a.group) * a.q_stride +
+                                          (int64_t)(kvh * a.group + r % a.group) * D + c * 8);
+    *reinterpret_cast<uint4*>(dst + swz<D>(r, c)) = v;
   }
 }
 
 // ---------------------------------------------------------- few-row attention
-// One CTA: the keys [split] of a (sequence, key head) for up to 16 MT rows.
+// One CTA: the keys [split] of a (sequence, key head) for up to 16 rows.
 // Its warps take groups of 16 keys in turn and keep a softmax of their own
 // (running maximum m, sum l, output O in registers), so nothing waits for
 // another warp until the end:
@@ -75,14 +71,14 @@ __device__ __forceinline__ void load_queries(const CachedArgs& a, int b, int kvh
 // The kernel is bound by reading the cache: a group's 8 KB takes 48 products
 // of 16 rows, and the warp-level ones do that at several times DRAM's rate,
 // without the fixed costs (TMEM, barriers, 128-row tiles) of tcgen05.
-template <typename T, int D, int MT, bool SPILL>
+template <typename T, int D, bool SPILL>
 __global__ void __launch_bounds__(kFwThreads, 2) attention_few_kernel(const __grid_constant__ CachedArgs a) {
-  using F = FewCfg<D, MT>;
+  using F = FewCfg<D>;
   extern __shared__ __align__(128) uint8_t smem[];
   uint32_t(*anc)[4] = reinterpret_cast<uint32_t(*)[4]>(smem + F::kOffAnc);
   int* par = reinterpret_cast<int*>(smem + F::kOffPar);
   float2* mls = reinterpret_cast<float2*>(smem + F::kOffMl);
-  const int split = blockIdx.x % a.splits, r0 = (int)(blockIdx.x / a.splits) * F::kRows;
+  const int split = blockIdx.x;
   const int kvh = blockIdx.y, b = blockIdx.z;
   const int warp = warp_index(), lane = threadIdx.x & 31;
   pdl_wait();
@@ -90,9 +86,8 @@ __global__ void __launch_bounds__(kFwThreads, 2) attention_few_kernel(const __gr
   int len, count;
   if (!seq_sizes(a, b, &len, &count)) return;
   const int rows = count * a.group;
-  if (r0 >= rows) return;
-  const int t_last = (min(r0 + F::kRows, rows) - 1) / a.group;
-  const int kmax = visible_limit(a, len, count, t_last), lim_min = visible_limit(a, len, count, r0 / a.group);
+  if (rows == 0) return;
+  const int kmax = visible_limit(a, len, count, count - 1), lim_min = visible_limit(a, len, count, 0);
   const int gp = (kmax + kGk - 1) / kGk, groups = gp + (a.k_new ? (count + kGk - 1) / kGk : 0);
   const int g_begin = (int)((int64_t)groups * split / a.splits), g_end = (int)((int64_t)groups * (split + 1) / a.splits);
 
@@ -122,40 +117,29 @@ __global__ void __launch_bounds__(kFwThreads, 2) attention_few_kernel(const __gr
 #pragma unroll
   for (int i = 0; i < kFwStages - 1; ++i) load(g_begin + warp + i * kFwWarps, i);
 
-  load_queries<T, D>(a, b, kvh, r0, rows, F::kRows, smem + F::kOffQ, nullptr);
+  load_queries<T, D>(a, b, kvh, rows, smem + F::kOffQ);
   if (a.k_new && !build_ancestors(a, b, count, anc, par)) {  // (while the first groups arrive)
     cp_async_wait<0>();
     return;
   }
   __syncthreads();
   const uint32_t q_u = smem_u32(smem + F::kOffQ);
-  auto query_frag = [&](int mt, int ks, uint32_t(&f)[4]) {
-    ldmatrix_x4(q_u + swz<D>(mt * 16 + (lane & 15), 2 * ks + (lane >> 4)), f);
-  };
-  uint32_t qf[MT == 1 ? D / 16 : 1][4];
-  if (MT == 1) {
+  uint32_t qf[D / 16][4];
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) query_frag(0, ks, qf[MT == 1 ? ks : 0]);
+  for (int ks = 0; ks < D / 16; ++ks) ldmatrix_x4(q_u + swz<D>(lane & 15, 2 * ks + (lane >> 4)), qf[ks]);
+  // this lane's rows: lane / 4 and 8 behind it
+  int lim[2], node[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = 8 * h + (lane >> 2);
+    node[h] = r < rows ? r / a.group : -1;
+    lim[h] = r < rows ? visible_limit(a, len, count, r / a.group) : 0;
   }
-  int lim[MT][2], node[MT][2];
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[D / 8][4];
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
+  for (int n = 0; n < D / 8; ++n)
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int r = r0 + mt * 16 + 8 * h + (lane >> 2);
-      node[mt][h] = r < rows ? r / a.group : -1;
-      lim[mt][h] = r < rows ? visible_limit(a, len, count, r / a.group) : 0;
-    }
-  float m[MT][2], l[MT][2], o[MT][D / 8][4];
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) m[mt][h] = -INFINITY, l[mt][h] = 0.f;
-#pragma unroll
-    for (int n = 0; n < D / 8; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[mt][n][e] = 0.f;
-  }
+    for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
   int slot = 0;
   for (int g = g_begin + warp; g < g_end; g += kFwWarps) {
     int ahead = slot + kFwStages - 1;
@@ -166,93 +150,74 @@ __global__ void __launch_bounds__(kFwThreads, 2) attention_few_kernel(const __gr
     const uint32_t ks_u = ring_u + (uint32_t)slot * 2 * F::kGroup, vs_u = ks_u + F::kGroup;
     const bool nw = g >= gp;
     const int j0 = (nw ? g - gp : g) * kGk;
-    float s[MT][2][4];
+    float s[2][4];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int n = 0; n < 2; ++n)
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[mt][n][e] = 0.f;
+      for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
       uint32_t kf[4];
       ldmatrix_x4(ks_u + swz<D>((lane & 7) + ((lane >> 4) << 3), 2 * ks + ((lane >> 3) & 1)), kf);
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        uint32_t f[4];
-        if (MT == 1) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) f[i] = qf[MT == 1 ? ks : 0][i];
-        } else {
-          query_frag(mt, ks, f);
-        }
-        mma_16816<T>(s[mt][0], f, kf[0], kf[1]);
-        mma_16816<T>(s[mt][1], f, kf[2], kf[3]);
-      }
+      mma_16816<T>(s[0], qf[ks], kf[0], kf[1]);
+      mma_16816<T>(s[1], qf[ks], kf[2], kf[3]);
     }
     const bool masked = nw || j0 + kGk > lim_min;  // some of these keys are hidden from some rows
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int n = 0; n < 2; ++n)
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s[mt][n][e] *= a.scale_log2;
-          if (masked) {
-            const int h = e >> 1, j = j0 + n * 8 + (lane & 3) * 2 + (e & 1);
-            const bool sees = nw ? node[mt][h] >= 0 && (anc[node[mt][h]][j >> 5] >> (j & 31) & 1u) : j < lim[mt][h];
-            if (!sees) s[mt][n][e] = -INFINITY;
-          }
+      for (int e = 0; e < 4; ++e) {
+        s[n][e] *= a.scale_log2;
+        if (masked) {
+          const int h = e >> 1, j = j0 + n * 8 + (lane & 3) * 2 + (e & 1);
+          const bool sees = nw ? node[h] >= 0 && (anc[node[h]][j >> 5] >> (j & 31) & 1u) : j < lim[h];
+          if (!sees) s[n][e] = -INFINITY;
         }
+      }
     if (SPILL) {
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
+      for (int h = 0; h < 2; ++h) {
+        const int r = 8 * h + (lane >> 2);
+        if (r < rows) {
+          float* to = a.scores + (((int64_t)b * a.kv_heads + kvh) * a.tokens * a.group + r) * a.score_ld + j0 + (lane & 3) * 2;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int r = r0 + mt * 16 + 8 * h + (lane >> 2);
-          if (r < rows) {
-            float* to = a.scores + (((int64_t)b * a.kv_heads + kvh) * a.tokens * a.group + r) * a.score_ld + j0 + (lane & 3) * 2;
-#pragma unroll
-            for (int n = 0; n < 2; ++n) *reinterpret_cast<float2*>(to + n * 8) = make_float2(s[mt][n][2 * h], s[mt][n][2 * h + 1]);
-          }
+          for (int n = 0; n < 2; ++n) *reinterpret_cast<float2*>(to + n * 8) = make_float2(s[n][2 * h], s[n][2 * h + 1]);
         }
+      }
     }
-    uint32_t ph[MT][4], pl[MT][4];
+    uint32_t ph[4], pl[4];
+    float al[2], base[2];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      float al[2], base[2];
+    for (int h = 0; h < 2; ++h) {
+      float mx = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+      const float mn = fmaxf(m[h], mx);
+      base[h] = mn == -INFINITY ? 0.f : mn;  // (nothing seen yet)
+      al[h] = ex2(m[h] - base[h]);
+      m[h] = mn;
+    }
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        float mx = fmaxf(fmaxf(s[mt][0][2 * h], s[mt][0][2 * h + 1]), fmaxf(s[mt][1][2 * h], s[mt][1][2 * h + 1]));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-        const float mn = fmaxf(m[mt][h], mx);
-        base[h] = mn == -INFINITY ? 0.f : mn;  // (nothing seen yet)
-        al[h] = ex2(m[mt][h] - base[h]);
-        m[mt][h] = mn;
+        const float p0 = ex2(s[n][2 * h] - base[h]), p1 = ex2(s[n][2 * h + 1] - base[h]);
+        sum[h] += p0 + p1;
+        s[n][2 * h] = p0;
+        s[n][2 * h + 1] = p1;
+        const uint32_t hi = pack_pair<T>(p0, p1);
+        const float2 back = unpack_pair<T>(hi);
+        ph[2 * n + h] = hi;
+        pl[2 * n + h] = pack_pair<T>(p0 - back.x, p1 - back.y);
       }
-      float sum[2] = {0.f, 0.f};
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+    for (int h = 0; h < 2; ++h) l[h] = l[h] * al[h] + sum[h];
+    if (__any_sync(0xffffffffu, al[0] != 1.f || al[1] != 1.f)) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float p0 = ex2(s[mt][n][2 * h] - base[h]), p1 = ex2(s[mt][n][2 * h + 1] - base[h]);
-          sum[h] += p0 + p1;
-          s[mt][n][2 * h] = p0;
-          s[mt][n][2 * h + 1] = p1;
-          const uint32_t hi = pack_pair<T>(p0, p1);
-          const float2 back = unpack_pair<T>(hi);
-          ph[mt][2 * n + h] = hi;
-          pl[mt][2 * n + h] = pack_pair<T>(p0 - back.x, p1 - back.y);
-        }
+      for (int n = 0; n < D / 8; ++n)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) l[mt][h] = l[mt][h] * al[h] + sum[h];
-      if (__any_sync(0xffffffffu, al[0] != 1.f || al[1] != 1.f)) {
-#pragma unroll
-        for (int n = 0; n < D / 8; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[mt][n][e] *= al[e >> 1];
-      }
+        for (int e = 0; e < 4; ++e) o[n][e] *= al[e >> 1];
     }
     if (masked) {
       // A hidden value row that is infinite or not a number must not reach
@@ -270,26 +235,21 @@ __global__ void __launch_bounds__(kFwThreads, 2) attention_few_kernel(const __gr
       if (odd) {
         float* pb = reinterpret_cast<float*>(smem + F::kOffP) + warp * F::kRows * kGk;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
-          for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              pb[(mt * 16 + 8 * (e >> 1) + (lane >> 2)) * kGk + n * 8 + (lane & 3) * 2 + (e & 1)] = s[mt][n][e];
+          for (int e = 0; e < 4; ++e) pb[(8 * (e >> 1) + (lane >> 2)) * kGk + n * 8 + (lane & 3) * 2 + (e & 1)] = s[n][e];
         __syncwarp();
         while (odd) {
           const int j = __ffs(odd) - 1;
           odd &= odd - 1;
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
+          for (int n = 0; n < D / 8; ++n)
 #pragma unroll
-            for (int n = 0; n < D / 8; ++n)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float p = pb[(mt * 16 + 8 * (e >> 1) + (lane >> 2)) * kGk + j];
-                const T v = *reinterpret_cast<const T*>(vs + swz<D>(j, n) + ((lane & 3) * 2 + (e & 1)) * 2);
-                if (p != 0.f) o[mt][n][e] = fmaf(p, to_f<T>(v), o[mt][n][e]);
-              }
+            for (int e = 0; e < 4; ++e) {
+              const float p = pb[(8 * (e >> 1) + (lane >> 2)) * kGk + j];
+              const T v = *reinterpret_cast<const T*>(vs + swz<D>(j, n) + ((lane & 3) * 2 + (e & 1)) * 2);
+              if (p != 0.f) o[n][e] = fmaf(p, to_f<T>(v), o[n][e]);
+            }
           __syncwarp();
           if (lane < D / 8) *reinterpret_cast<uint4*>(vs + swz<D>(j, lane)) = make_uint4(0u, 0u, 0u, 0u);
           __syncwarp();
@@ -300,13 +260,10 @@ __global__ void __launch_bounds__(kFwThreads, 2) attention_few_kernel(const __gr
     for (int n = 0; n < D / 16; ++n) {
       uint32_t vf[4];
       ldmatrix_x4_trans(vs_u + swz<D>(lane & 15, 2 * n + (lane >> 4)), vf);
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        mma_16816<T>(o[mt][2 * n], ph[mt], vf[0], vf[1]);
-        mma_16816<T>(o[mt][2 * n + 1], ph[mt], vf[2], vf[3]);
-        mma_16816<T>(o[mt][2 * n], pl[mt], vf[0], vf[1]);
-        mma_16816<T>(o[mt][2 * n + 1], pl[mt], vf[2], vf[3]);
-      }
+      mma_16816<T>(o[2 * n], ph, vf[0], vf[1]);
+      mma_16816<T>(o[2 * n + 1], ph, vf[2], vf[3]);
+      mma_16816<T>(o[2 * n], pl, vf[0], vf[1]);
+      mma_16816<T>(o[2 * n + 1], pl, vf[2], vf[3]);
     }
     __syncwarp();  // the group has been read before its slot is filled again
     if (++slot == kFwStages) slot = 0;
@@ -316,33 +273,31 @@ __global__ void __launch_bounds__(kFwThreads, 2) attention_few_kernel(const __gr
   __syncthreads();
   float* ow = reinterpret_cast<float*>(smem) + warp * F::kRows * D;
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
+  for (int h = 0; h < 2; ++h) {
+    float x = l[h];
+    x += __shfl_xor_sync(0xffffffffu, x, 1);
+    x += __shfl_xor_sync(0xffffffffu, x, 2);
+    const int rl = 8 * h + (lane >> 2);
+    if ((lane & 3) == 0) mls[warp * F::kRows + rl] = make_float2(m[h], x);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float x = l[mt][h];
-      x += __shfl_xor_sync(0xffffffffu, x, 1);
-      x += __shfl_xor_sync(0xffffffffu, x, 2);
-      const int rl = mt * 16 + 8 * h + (lane >> 2);
-      if ((lane & 3) == 0) mls[warp * F::kRows + rl] = make_float2(m[mt][h], x);
-#pragma unroll
-      for (int n = 0; n < D / 8; ++n)
-        *reinterpret_cast<float2*>(ow + rl * D + n * 8 + (lane & 3) * 2) = make_float2(o[mt][n][2 * h], o[mt][n][2 * h + 1]);
-    }
+    for (int n = 0; n < D / 8; ++n)
+      *reinterpret_cast<float2*>(ow + rl * D + n * 8 + (lane & 3) * 2) = make_float2(o[n][2 * h], o[n][2 * h + 1]);
+  }
   __syncthreads();
   constexpr int V = D / 4;  // float4 per row
   for (int i = threadIdx.x; i < F::kRows * V; i += kFwThreads) {
-    const int rl = i / V, c = i % V, r = r0 + rl;
+    const int r = i / V, c = i % V;
     if (r >= rows) break;
     float M = -INFINITY, L = 0.f;
 #pragma unroll
-    for (int w = 0; w < kFwWarps; ++w) M = fmaxf(M, mls[w * F::kRows + rl].x);
+    for (int w = 0; w < kFwWarps; ++w) M = fmaxf(M, mls[w * F::kRows + r].x);
     const float base = M == -INFINITY ? 0.f : M;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < kFwWarps; ++w) {
-      const float2 ml = mls[w * F::kRows + rl];
+      const float2 ml = mls[w * F::kRows + r];
       const float f = ex2(ml.x - base);
-      const float4 y = reinterpret_cast<const float4*>(smem)[(w * F::kRows + rl) * V + c];
+      const float4 y = reinterpret_cast<const float4*>(smem)[(w * F::kRows + r) * V + c];
       L = fmaf(ml.y, f, L);
       if (f != 0.f) {
         x.x = fmaf(y.x, f, x.x);
@@ -481,137 +436,6 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
   }
 }
 
-// --------------------------------------------------------- few-row weights
-// weights_j = weights_in_j + sum over rows and heads of e^(s_rj - lse_r): one
-// warp per group of 16 keys, S = Q K^T as above, 2^(S - lse) summed over the
-// rows in registers and then over the eight lanes that share a key.  Rows in
-// blocks of 128; a second block reads the keys again and adds to its own sums.
-constexpr int kWfRows = 128, kWfStages = 4;
-template <int D> struct WfCfg {
-  static constexpr int kGroup = kGk * D * 2;
-  static constexpr int kRing = kFwWarps * kWfStages * kGroup;
-  static constexpr int kOffQ = kRing;
-  static constexpr int kOffLse = kOffQ + kWfRows * D * 2;
-  static constexpr int kOffLim = kOffLse + kWfRows * 4;
-  static constexpr int kOffRow = kOffLim + kWfRows * 4;
-  static constexpr int kSmem = kOffRow + kWfRows * 4;
-};
-
-template <typename T, int D>
-__global__ void __launch_bounds__(kFwThreads) weights_few_kernel(const __grid_constant__ CachedArgs a) {
-  using F = WfCfg<D>;
-  extern __shared__ __align__(128) uint8_t smem[];
-  float* lse2 = reinterpret_cast<float*>(smem + F::kOffLse);
-  int* lim = reinterpret_cast<int*>(smem + F::kOffLim);
-  int* row_of = reinterpret_cast<int*>(smem + F::kOffRow);
-  const int split = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z;
-  const int warp = warp_index(), lane = threadIdx.x & 31;
-  pdl_wait();
-  pdl_launch_dependents();
-  int len, count;
-  if (!seq_sizes(a, b, &len, &count)) return;
-  const int rows = count * a.group;
-  const int groups = (len + kGk - 1) / kGk;
-  const int g_begin = (int)((int64_t)groups * split / a.splits), g_end = (int)((int64_t)groups * (split + 1) / a.splits);
-  if (g_begin >= g_end) return;
-  const uint32_t ring_u = smem_u32(smem + warp * kWfStages * F::kGroup), q_u = smem_u32(smem + F::kOffQ);
-  const T* kb = static_cast<const T*>(a.k) + (int64_t)b * a.seq_stride + kvh * D;
-  auto load = [&](int g, int slot) {
-    if (g < g_end) {
-      constexpr int C = D / 8;
-#pragma unroll
-      for (int i = 0; i < kGk * C / 32; ++i) {
-        const int r = (lane + 32 * i) / C, c = (lane + 32 * i) % C, j = g * kGk + r;
-        cp_async_16(ring_u + (uint32_t)slot * F::kGroup + swz<D>(r, c), kb + (j < len ? j * a.kv_stride + c * 8 : 0), j < len);
-      }
-    }
-    cp_async_commit();
-  };
-  const int64_t at = ((int64_t)b * a.kv_heads + kvh) * a.max_seq;
-  const float* from = a.weights_in;
-  for (int r0 = 0; r0 < rows || r0 == 0; r0 += kWfRows) {
-#pragma unroll
-    for (int i = 0; i < kWfStages - 1; ++i) load(g_begin + warp + i * kFwWarps, i);
-    const int here = min(kWfRows, rows - r0), tiles = (here + 15) / 16;
-    for (int i = threadIdx.x; i < kWfRows; i += kFwThreads) {
-      const int r = r0 + i, t = r / a.group;
-      int q = t;
-      if (i < here && a.rows) {
-        q = a.rows[(int64_t)b * a.rows_step + t];
-        if (q < 0 || q >= a.tokens) {
-          atomicExch(a.err, kDevErrBounds);
-          q = -1;
-        }
-      }
-      const bool ok = i < here && q >= 0;
-      row_of[i] = ok ? q : -1;
-      lim[i] = ok ? visible_limit(a, len, count, t) : 0;
-      lse2[i] = ok ? a.lse[((int64_t)b * a.heads + kvh * a.group + r % a.group) * a.tokens + q] * 1.4426950408889634f : INFINITY;
-    }
-    __syncthreads();
-    load_queries<T, D>(a, b, kvh, r0, rows, tiles * 16, smem + F::kOffQ, row_of);
-    __syncthreads();
-    const int lim_min = rows ? visible_limit(a, len, count, r0 / a.group) : 0;
-    int slot = 0;
-    for (int g = g_begin + warp; g < g_end; g += kFwWarps) {
-      load(g + (kWfStages - 1) * kFwWarps, (slot + kWfStages - 1) % kWfStages);
-      cp_async_wait<kWfStages - 1>();
-      __syncwarp();
-      const uint32_t ks_u = ring_u + (uint32_t)slot * F::kGroup;
-      const int j0 = g * kGk;
-      uint32_t kf[D / 16][4];
-#pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks)
-        ldmatrix_x4(ks_u + swz<D>((lane & 7) + ((lane >> 4) << 3), 2 * ks + ((lane >> 3) & 1)), kf[ks]);
-      const bool masked = j0 + kGk > lim_min;
-      float w[4] = {0.f, 0.f, 0.f, 0.f};  // this lane's keys: j0 + 8 n + 2 (lane & 3) + u at 2 n + u
-      for (int mt = 0; mt < tiles; ++mt) {
-        float s[2][4];
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
-          uint32_t f[4];
-          ldmatrix_x4(q_u + swz<D>(mt * 16 + (lane & 15), 2 * ks + (lane >> 4)), f);
-          mma_16816<T>(s[0], f, kf[ks][0], kf[ks][1]);
-          mma_16816<T>(s[1], f, kf[ks][2], kf[ks][3]);
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int rl = mt * 16 + 8 * h + (lane >> 2);
-          const float e2 = lse2[rl];
-          const int lm = lim[rl];
-#pragma unroll
-          for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const float p = ex2(fmaf(s[n][2 * h + u], a.scale_log2, -e2));
-              if (!masked || j0 + n * 8 + (lane & 3) * 2 + u < lm) w[2 * n + u] += p;
-            }
-        }
-      }
-#pragma unroll
-      for (int off = 4; off < 32; off <<= 1)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] += __shfl_xor_sync(0xffffffffu, w[i], off);
-      if (lane < 4) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int j = j0 + (i >> 1) * 8 + lane * 2 + (i & 1);
-          if (j < len) a.weights[at + j] = (from ? from[at + j] : 0.f) + w[i];
-        }
-      }
-      __syncwarp();
-      slot = (slot + 1) % kWfStages;
-    }
-    cp_async_wait<0>();
-    __syncthreads();
-    from = a.weights;  // (a key's sums stay with one thread)
-  }
-}
-
 int done(cudaError_t e, const char* what) {
   if (e == cudaSuccess) e = cudaGetLastError();
   if (e != cudaSuccess) SN_FAIL(SWAPNET_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
@@ -643,35 +467,22 @@ template <typename K> int allow_smem(K kern, int bytes, std::atomic<uint64_t>& k
   return SWAPNET_OK;
 }
 
-template <typename T, int D, int MT, bool SPILL> int few_t(const CachedArgs& a, bool early, cudaStream_t s) {
+template <typename T, int D, bool SPILL> int few_t(const CachedArgs& a, bool early, cudaStream_t s) {
   static std::atomic<uint64_t> known{0};
-  using F = FewCfg<D, MT>;
-  if (int rc = allow_smem(attention_few_kernel<T, D, MT, SPILL>, F::kSmem, known)) return rc;
-  const int chunks = (a.tokens * a.group + F::kRows - 1) / F::kRows;
-  return done(launch(attention_few_kernel<T, D, MT, SPILL>, dim3(chunks * a.splits, a.kv_heads, a.n_seq), kFwThreads, F::kSmem,
-                     early, s, a),
+  using F = FewCfg<D>;
+  if (int rc = allow_smem(attention_few_kernel<T, D, SPILL>, F::kSmem, known)) return rc;
+  return done(launch(attention_few_kernel<T, D, SPILL>, dim3(a.splits, a.kv_heads, a.n_seq), kFwThreads, F::kSmem, early, s, a),
               "cached attention launch");
 }
 template <typename T, int D> int few_d(const CachedArgs& a, bool early, cudaStream_t s) {
-  const bool one = a.tokens * a.group <= 16;
-  if (a.scores) return one ? few_t<T, D, 1, true>(a, early, s) : few_t<T, D, 2, true>(a, early, s);
-  return one ? few_t<T, D, 1, false>(a, early, s) : few_t<T, D, 2, false>(a, early, s);
+  return a.scores ? few_t<T, D, true>(a, early, s) : few_t<T, D, false>(a, early, s);
 }
-template <typename T, int D> int weights_t(const CachedArgs& a, bool early, cudaStream_t s) {
-  static std::atomic<uint64_t> known{0};
-  if (int rc = allow_smem(weights_few_kernel<T, D>, WfCfg<D>::kSmem, known)) return rc;
-  return done(launch(weights_few_kernel<T, D>, dim3(a.splits, a.kv_heads, a.n_seq), kFwThreads, WfCfg<D>::kSmem, early, s, a),
-              "cache weights launch");
-}
-
 }  // namespace
 
-#define SN_CACHED_DISPATCH(F, ...)                                                                     \
-  (a.dtype == SWAPNET_BF16 ? (a.dim == 128 ? F<__nv_bfloat16, 128>(__VA_ARGS__) : F<__nv_bfloat16, 64>(__VA_ARGS__)) \
-                           : (a.dim == 128 ? F<__half, 128>(__VA_ARGS__) : F<__half, 64>(__VA_ARGS__)))
-
-int launch_attention_few(const CachedArgs& a, bool early, cudaStream_t s) { return SN_CACHED_DISPATCH(few_d, a, early, s); }
-int launch_weights_few(const CachedArgs& a, bool early, cudaStream_t s) { return SN_CACHED_DISPATCH(weights_t, a, early, s); }
+int launch_attention_few(const CachedArgs& a, bool early, cudaStream_t s) {
+  if (a.dtype == SWAPNET_BF16) return a.dim == 128 ? few_d<__nv_bfloat16, 128>(a, early, s) : few_d<__nv_bfloat16, 64>(a, early, s);
+  return a.dim == 128 ? few_d<__half, 128>(a, early, s) : few_d<__half, 64>(a, early, s);
+}
 
 int launch_attention_join(const CachedArgs& a, cudaStream_t s) {
   const int rows = a.tokens * a.group;

@@ -576,7 +576,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
               ok = __all_sync(0xffffffffu, ok);
               tc_fence_after();
               if (ok) {
-#pragma unroll
+#pragma unroll 1  // (seldom run: short code, which the instruction cache has room beside the rest for)
                 for (int c = 0; c < D / kSub; c += 16) {  // each warp its share of the columns
                   uint32_t r[16];
                   const uint32_t at = tO + (uint32_t)(part % kSub * (D / kSub) + c);
@@ -643,6 +643,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
           all_sync();
           odd = odd_rows[0] | odd_rows[1] | odd_rows[2] | odd_rows[3];
           if (odd) {
+#pragma unroll 1
             for (int c = aid; c < kKeys * (D / 8); c += kAtSoft) {
               const int r = c / (D / 8);
               if (odd_rows[r >> 5] >> (r & 31) & 1u) *chunk(r, c % (D / 8)) = make_uint4(0u, 0u, 0u, 0u);
@@ -675,6 +676,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
           ok = ok && mbar_wait_bounded(o_full(half), g & 1, abort_flag, a.err);
           ok = __all_sync(0xffffffffu, ok);
           tc_fence_after();
+#pragma unroll 1
           for (int j = half * 64; j < half * 64 + 64; ++j) {
             if (!(odd_rows[j >> 5] >> (j & 31) & 1u)) continue;
             const int rel = j - kofs;
@@ -689,6 +691,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
               const T* v = nw ? static_cast<const T*>(a.v_new) + ((int64_t)b * a.tokens + j) * a.new_stride
                               : static_cast<const T*>(a.v) + (int64_t)b * a.seq_stride + (int64_t)(k0 + j) * a.kv_stride;
               v += kvh * D;
+#pragma unroll 1
               for (int c = 0; c < D; c += 16) {
                 uint32_t r[16];
                 tmem_ld_32x32b_x16(tO + (uint32_t)c, r);
@@ -930,7 +933,7 @@ __global__ void __launch_bounds__(kTcThreads, 2)
       };
       int it = 0, kp = 0;
       bool ok = true;
-      for (int kt = split; ok && kt < ktiles; kt += a.splits, ++kp) {
+      for (int kt = split; ok && kt < ktiles; kt += (int)gridDim.x, ++kp) {
         const int s = kp % ks;
         if (kp >= ks && !mbar_wait_bounded(k_empty(s), ((kp / ks) - 1) & 1, abort_flag, a.err)) break;
         mbar_arrive_expect_tx(k_full(s), F::kTile);
@@ -965,7 +968,7 @@ __global__ void __launch_bounds__(kTcThreads, 2)
       const uint64_t kd = smem_desc_sw128(smem_u32(smem)), qd = smem_desc_sw128(smem_u32(smem_q));
       int it = 0, kp = 0;
       bool ok = true;
-      for (int kt = split; ok && kt < ktiles; kt += a.splits, ++kp) {
+      for (int kt = split; ok && kt < ktiles; kt += (int)gridDim.x, ++kp) {
         const int s = kp % ks;
         if (!mbar_wait_bounded(k_full(s), (kp / ks) & 1, abort_flag, a.err)) break;
         for (int rt = first_tile(kt); ok && rt < nrt; ++rt, ++it) {
@@ -1033,14 +1036,14 @@ __global__ void __launch_bounds__(kTcThreads, 2)
     }
     int it = 0, kp = 0;
     bool ok = true;
-    for (int kt = split; kt < ktiles; kt += a.splits, ++kp) {
+    for (int kt = split; kt < ktiles; kt += (int)gridDim.x, ++kp) {
       const int j = kt * kKeys + slot;
       const float before = half == 0 && j < len && a.weights_in ? a.weights_in[at + j] : 0.f;
       float sum = 0.f;
       for (int rt = first_tile(kt); rt < nrt; ++rt, ++it) {
         const int sb = it % kSBufs, buf = one ? 0 : it & 1;
-        const bool last = rt + 1 == nrt && kt + a.splits >= ktiles;
-        if (!one && !last) fetch(rt + 1 < nrt ? rt + 1 : first_tile(kt + a.splits));
+        const bool last = rt + 1 == nrt && kt + (int)gridDim.x >= ktiles;
+        if (!one && !last) fetch(rt + 1 < nrt ? rt + 1 : first_tile(kt + (int)gridDim.x));
         ok = ok && mbar_wait_bounded(s_full(sb), (it / kSBufs) & 1, abort_flag, a.err);
         ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
@@ -1244,7 +1247,7 @@ template <typename T, int D> int rows_d(const CachedArgs& a, bool early, cudaStr
   return a.tokens * a.group <= 64 ? rows_t<T, D, 2>(a, early, s) : rows_t<T, D, 1>(a, early, s);
 }
 
-template <typename T, int D> int weights_t(const CachedArgs& a, bool early, cudaStream_t s) {
+template <typename T, int D> int weights_t(const CachedArgs& a, int splits, bool early, cudaStream_t s) {
   static std::atomic<uint64_t> known{0};
   const auto kern = weights_rows_kernel<T, D>;
   if (attr_needed(known)) {
@@ -1259,7 +1262,7 @@ template <typename T, int D> int weights_t(const CachedArgs& a, bool early, cuda
   if (rc) return rc;
   cudaLaunchConfig_t cfg;
   std::memset(&cfg, 0, sizeof(cfg));
-  cfg.gridDim = dim3(a.splits, a.kv_heads, a.n_seq);
+  cfg.gridDim = dim3(splits, a.kv_heads, a.n_seq);
   cfg.blockDim = dim3(kTcThreads);
   cfg.dynamicSmemBytes = WtCfg<D>::kSmem;
   cfg.stream = s;
@@ -1273,9 +1276,10 @@ template <typename T, int D> int weights_t(const CachedArgs& a, bool early, cuda
 
 }  // namespace
 
-int launch_weights_rows(const CachedArgs& a, bool early, cudaStream_t s) {
-  if (a.dtype == SWAPNET_BF16) return a.dim == 128 ? weights_t<__nv_bfloat16, 128>(a, early, s) : weights_t<__nv_bfloat16, 64>(a, early, s);
-  return a.dim == 128 ? weights_t<__half, 128>(a, early, s) : weights_t<__half, 64>(a, early, s);
+int launch_weights(const CachedArgs& a, int splits, bool early, cudaStream_t s) {
+  if (a.dtype == SWAPNET_BF16)
+    return a.dim == 128 ? weights_t<__nv_bfloat16, 128>(a, splits, early, s) : weights_t<__nv_bfloat16, 64>(a, splits, early, s);
+  return a.dim == 128 ? weights_t<__half, 128>(a, splits, early, s) : weights_t<__half, 64>(a, splits, early, s);
 }
 
 int launch_attention_rows(const CachedArgs& a, bool early, cudaStream_t s) {
