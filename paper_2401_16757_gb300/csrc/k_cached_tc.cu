@@ -836,9 +836,8 @@ template <int D> struct WtCfg {
   static constexpr int kBox = 128 * 128;
   static constexpr int kTile = kHalves * kBox;
   static constexpr int kSlots = 3;                         // of keys and queries
-  static constexpr int kOffLse = kSlots * kTile;           // [2][128] log2 of the rows' sums
-  static constexpr int kOffLim = kOffLse + 2 * 128 * 4;
-  static constexpr int kOffX = kOffLim + 2 * 128 * 4;
+  static constexpr int kOffLse = kSlots * kTile;           // [2][128] of the rows
+  static constexpr int kOffX = kOffLse + 2 * 128 * 4;
   static constexpr int kOffBar = kOffX + 2 * 128 * 4;
   static constexpr int kSmem = kOffBar + 256 + 1024;
   static_assert(2 * (kSmem + 1024) <= 233472, "two CTAs per SM");
@@ -853,8 +852,7 @@ __global__ void __launch_bounds__(kTcThreads, 2)
   using F = WtCfg<D>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  float* lse2 = reinterpret_cast<float*>(smem + F::kOffLse);
-  int* lim = reinterpret_cast<int*>(smem + F::kOffLim);
+  float* lse = reinterpret_cast<float*>(smem + F::kOffLse);
   float* xch = reinterpret_cast<float*>(smem + F::kOffX);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + F::kOffBar);
   auto k_full = [&](int s) { return smem_u32(bars + s); };
@@ -1003,52 +1001,52 @@ __global__ void __launch_bounds__(kTcThreads, 2)
     auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory"); };
     auto all_sync = [&]() { asm volatile("bar.sync 5, 256;" ::: "memory"); };
     const int64_t at = ((int64_t)b * a.kv_heads + kvh) * a.max_seq;
-    // what thread aid < 128 brings of row aid of a tile of rows
-    float row_lse = INFINITY;
-    int row_lim = 0;
-    auto fetch = [&](int rt) {
-      const int r = rt * queries * a.group + aid, t = r / a.group;
-      row_lse = INFINITY;
-      row_lim = 0;
-      if (aid < queries * a.group && t < count) {
-        int q = t;
-        if (a.rows) {
-          q = a.rows[(int64_t)b * a.rows_step + t];
-          if (q < 0 || q >= a.tokens) {
-            atomicExch(a.err, kDevErrBounds);
-            return;
-          }
-        }
-        row_lse = a.lse[((int64_t)b * a.heads + kvh * a.group + r % a.group) * a.tokens + q] * 1.4426950408889634f;
-        row_lim = visible_limit(a, len, count, t);
-      }
-    };
-    auto store = [&](int buf) {
+    // thread aid < 128 has row aid of a tile of rows' lse copied to shared memory
+    const int row_q = aid / a.group;
+    const float* row_lse = a.lse + ((int64_t)b * a.heads + kvh * a.group + aid % a.group) * a.tokens;
+    auto fetch = [&](int rt, int buf) {
       if (aid < 128) {
-        lse2[buf * 128 + aid] = row_lse;
-        lim[buf * 128 + aid] = row_lim;
+        const int t = rt * queries + row_q;
+        bool have = row_q < queries && t < count;
+        int q = t;
+        if (have && a.rows) {
+          q = a.rows[(int64_t)b * a.rows_step + t];
+          have = q >= 0 && q < a.tokens;
+          if (!have) atomicExch(a.err, kDevErrBounds);
+        }
+        if (have)
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(lse + buf * 128 + aid)), "l"(row_lse + q) : "memory");
+        else
+          lse[buf * 128 + aid] = INFINITY;  // (adds nothing)
       }
+      cp_async_commit();
     };
     if (nrt > 0) {
-      fetch(first_tile(split));
-      store(0);
+      fetch(first_tile(split), 0);
+      cp_async_wait<0>();
       all_sync();
     }
+    const float2 scale2 = make_float2(a.scale_log2, a.scale_log2), log2e = make_float2(-1.4426950408889634f, -1.4426950408889634f);
+    const float2 zero2 = make_float2(0.f, 0.f);
     int it = 0, kp = 0;
     bool ok = true;
     for (int kt = split; kt < ktiles; kt += (int)gridDim.x, ++kp) {
       const int j = kt * kKeys + slot;
       const float before = half == 0 && j < len && a.weights_in ? a.weights_in[at + j] : 0.f;
-      float sum = 0.f;
+      float2 sum2[2] = {zero2, zero2};
       for (int rt = first_tile(kt); rt < nrt; ++rt, ++it) {
         const int sb = it % kSBufs, buf = one ? 0 : it & 1;
         const bool last = rt + 1 == nrt && kt + (int)gridDim.x >= ktiles;
-        if (!one && !last) fetch(rt + 1 < nrt ? rt + 1 : first_tile(kt + (int)gridDim.x));
+        if (!one && !last) fetch(rt + 1 < nrt ? rt + 1 : first_tile(kt + (int)gridDim.x), buf ^ 1);
         ok = ok && mbar_wait_bounded(s_full(sb), (it / kSBufs) & 1, abort_flag, a.err);
         ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
         if (ok) {
           const int rows = min(queries, count - rt * queries) * a.group, nch = (rows + 15) / 16;
+          // the tile's rows from `low` on see this thread's key; from `low_all`
+          // on, all of the tile's keys
+          const int ahead = kt * kKeys - (len - count) - rt * queries;
+          const int low = (ahead + slot) * a.group, low_all = (ahead + kKeys - 1) * a.group;
           const uint32_t tS = tmem + (uint32_t)sb * 128u + lane_off;
 #pragma unroll
           for (int c2 = 0; c2 < 4; c2 += 2) {  // two of the half's chunks of 16 rows at a time
@@ -1066,31 +1064,35 @@ __global__ void __launch_bounds__(kTcThreads, 2)
             for (int c = 0; c < 2; ++c) {
               const int c0 = (half + 2 * (c2 + c)) * 16;
               if (c0 >= rows) break;
-              const float* le = lse2 + buf * 128 + c0;
-              const int* li = lim + buf * 128 + c0;
-              const bool masked = kt * kKeys + kKeys > li[0] || c0 + 16 > rows;
+              const float* le = lse + buf * 128 + c0;
+              float2 p[8];
 #pragma unroll
-              for (int e = 0; e < 16; e += 4) {
-                const float4 l4 = *reinterpret_cast<const float4*>(le + e);
-                const float ll[4] = {l4.x, l4.y, l4.z, l4.w};
-                float p[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) p[u] = ex2(fmaf(__uint_as_float(s[c][e + u]), a.scale_log2, -ll[u]));
-                if (masked) {
-#pragma unroll
-                  for (int u = 0; u < 4; ++u)
-                    if (j >= li[e + u]) p[u] = 0.f;
-                }
-                sum += (p[0] + p[1]) + (p[2] + p[3]);
+              for (int e = 0; e < 8; e += 2) {
+                const float4 l4 = *reinterpret_cast<const float4*>(le + 2 * e);
+                p[e] = fma2(make_float2(l4.x, l4.y), log2e, fma2(make_float2(__uint_as_float(s[c][2 * e]), __uint_as_float(s[c][2 * e + 1])), scale2, zero2));
+                p[e + 1] = fma2(make_float2(l4.z, l4.w), log2e, fma2(make_float2(__uint_as_float(s[c][2 * e + 2]), __uint_as_float(s[c][2 * e + 3])), scale2, zero2));
               }
+#pragma unroll
+              for (int e = 0; e < 8; ++e) p[e] = make_float2(ex2(p[e].x), ex2(p[e].y));
+              if (c0 < low_all || c0 + 16 > rows) {  // hidden keys, or rows behind the last
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                  const int r = c0 + 2 * e;
+                  if (r < low || r >= rows) p[e].x = 0.f;
+                  if (r + 1 < low || r + 1 >= rows) p[e].y = 0.f;
+                }
+              }
+#pragma unroll
+              for (int e = 0; e < 8; ++e) sum2[e & 1] = add2(sum2[e & 1], p[e]);
             }
           }
         }
         if (!one && !last) {
-          store(buf ^ 1);
+          cp_async_wait<0>();
           all_sync();
         }
       }
+      const float sum = (sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y);
       float* x = xch + (kp & 1) * 128;
       if (half == 1) x[slot] = sum;
       pair_sync();
