@@ -866,7 +866,8 @@ __global__ void __launch_bounds__(kTcThreads, 2)
   volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 22);
 
   const int warp = warp_index(), lane = threadIdx.x & 31;
-  const int split = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z;
+  // (the tiles that most rows see start first)
+  const int kvh = blockIdx.x, b = blockIdx.y, split = blockIdx.z;
   pdl_wait();
   pdl_launch_dependents();
   int len, count;
@@ -931,7 +932,7 @@ __global__ void __launch_bounds__(kTcThreads, 2)
       };
       int it = 0, kp = 0;
       bool ok = true;
-      for (int kt = split; ok && kt < ktiles; kt += (int)gridDim.x, ++kp) {
+      for (int kt = split; ok && kt < ktiles; kt += (int)gridDim.z, ++kp) {
         const int s = kp % ks;
         if (kp >= ks && !mbar_wait_bounded(k_empty(s), ((kp / ks) - 1) & 1, abort_flag, a.err)) break;
         mbar_arrive_expect_tx(k_full(s), F::kTile);
@@ -966,7 +967,7 @@ __global__ void __launch_bounds__(kTcThreads, 2)
       const uint64_t kd = smem_desc_sw128(smem_u32(smem)), qd = smem_desc_sw128(smem_u32(smem_q));
       int it = 0, kp = 0;
       bool ok = true;
-      for (int kt = split; ok && kt < ktiles; kt += (int)gridDim.x, ++kp) {
+      for (int kt = split; ok && kt < ktiles; kt += (int)gridDim.z, ++kp) {
         const int s = kp % ks;
         if (!mbar_wait_bounded(k_full(s), (kp / ks) & 1, abort_flag, a.err)) break;
         for (int rt = first_tile(kt); ok && rt < nrt; ++rt, ++it) {
@@ -1030,14 +1031,14 @@ __global__ void __launch_bounds__(kTcThreads, 2)
     const float2 zero2 = make_float2(0.f, 0.f);
     int it = 0, kp = 0;
     bool ok = true;
-    for (int kt = split; kt < ktiles; kt += (int)gridDim.x, ++kp) {
+    for (int kt = split; kt < ktiles; kt += (int)gridDim.z, ++kp) {
       const int j = kt * kKeys + slot;
       const float before = half == 0 && j < len && a.weights_in ? a.weights_in[at + j] : 0.f;
       float2 sum2[2] = {zero2, zero2};
       for (int rt = first_tile(kt); rt < nrt; ++rt, ++it) {
         const int sb = it % kSBufs, buf = one ? 0 : it & 1;
-        const bool last = rt + 1 == nrt && kt + (int)gridDim.x >= ktiles;
-        if (!one && !last) fetch(rt + 1 < nrt ? rt + 1 : first_tile(kt + (int)gridDim.x), buf ^ 1);
+        const bool last = rt + 1 == nrt && kt + (int)gridDim.z >= ktiles;
+        if (!one && !last) fetch(rt + 1 < nrt ? rt + 1 : first_tile(kt + (int)gridDim.z), buf ^ 1);
         ok = ok && mbar_wait_bounded(s_full(sb), (it / kSBufs) & 1, abort_flag, a.err);
         ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
@@ -1264,7 +1265,7 @@ template <typename T, int D> int weights_t(const CachedArgs& a, int splits, bool
   if (rc) return rc;
   cudaLaunchConfig_t cfg;
   std::memset(&cfg, 0, sizeof(cfg));
-  cfg.gridDim = dim3(splits, a.kv_heads, a.n_seq);
+  cfg.gridDim = dim3(a.kv_heads, a.n_seq, splits);
   cfg.blockDim = dim3(kTcThreads);
   cfg.dynamicSmemBytes = WtCfg<D>::kSmem;
   cfg.stream = s;
