@@ -491,8 +491,11 @@ int swapnet_engine_bind_state(swapnet_engine* eng, void* d_state, uint64_t state
 /* What else a state holds: byte offsets from its start, 0 = not there.  The
  * header's int32 words: [0] the rows in use (the position above), [1] with
  * WEIGHTS the rows evicted so far (a token's rotation is that of position
- * [0] + [1]), [2] scratch, [3] and [4] with TREE results of the last swapnet_engine_tree_accept: accepted nodes and the
- * model's choice at the last one.
+ * [0] + [1]), [2] scratch, [3] and [4] with TREE results of the last
+ * swapnet_engine_tree_accept: accepted nodes and the model's choice at the
+ * last one.  Each run of an ATTENTION unit adds to the weights, also those of
+ * swapnet_engine_measure_units and _calibrate: measure before the state is
+ * used, or zero the weights behind it.
  * Engines that share a state are built from the same layers with the same
  * SWAPNET_ATTENTION_WEIGHTS flag; the offsets up to `weights` are the same for
  * them, what lies behind serves one engine's pass at a time. */
@@ -787,7 +790,8 @@ typedef struct swapnet_cached_attention {
  * Queries at and behind counts, and weights at and behind lens, are left as
  * they were.  Hidden rows may hold anything.  `workspace` is 256-byte aligned
  * device memory of at least the bytes that _workspace returns (a function of
- * the sizes alone), with nothing to keep in it between calls.
+ * the sizes alone), with nothing to keep in it between calls.  Outputs and
+ * workspace overlap none of the inputs (but for weights and weights_in).
  * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA. */
 int swapnet_attention_tree_workspace(const swapnet_cached_attention* args, uint64_t* bytes);
 int swapnet_attention_tree(const swapnet_cached_attention* args, void* workspace, uint64_t workspace_bytes,
@@ -797,7 +801,7 @@ int swapnet_attention_tree(const swapnet_cached_attention* args, void* workspace
  * row rows[b][i] of q and of lse (i < counts[b]) and sits in cache row
  * lens[b] - counts[b] + i; it adds e^(scale q . k_j - lse) to every row j up to
  * its own.  After swapnet_tree_accept: rows = path, counts = accepted,
- * lens = lens_out.  v, out and the workspace are not used. */
+ * lens = lens_out.  v and out are not used. */
 int swapnet_attention_weights(const swapnet_cached_attention* args, swapnet_stream stream);
 
 /* Eviction: per sequence and key head, of lens rows keep min(lens, keep): the
@@ -806,9 +810,10 @@ int swapnet_attention_weights(const swapnet_cached_attention* args, swapnet_stre
  * gets the rows kept, k_out / v_out / weights_out their contents in rows
  * 0 .. min(lens, keep) - 1, lens_out their number.  weights_out is 0 from there
  * up to row lens (a row appended later starts from nothing); what else lies
- * behind is left as it was.  All three may be the inputs themselves (in place, one layout
- * for both); otherwise they must not overlap them.  Keys keep the rotation of
- * the position they were written at.  head_dim: any multiple of 8 up to 512.
+ * behind is left as it was.  k_out, v_out and weights_out may be the inputs
+ * themselves (in place, one layout for both); otherwise they must not overlap
+ * them.  Keys keep the rotation of the position they were written at.
+ * head_dim: any multiple of 8 up to 512.
  * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA. */
 typedef struct swapnet_cache_eviction {
   int32_t dtype, n_seq, kv_heads, head_dim;
@@ -836,7 +841,8 @@ int swapnet_cache_evict(const swapnet_cache_eviction* args, swapnet_stream strea
  * number, next the model's choice at the last one, lens_out = lens + accepted;
  * the accepted rows of every draft are appended to its cache at row lens.  A
  * sequence whose cache has no room for its path, or with counts < 1, is left
- * alone and reported as above.  At most 128 nodes and 256 caches.
+ * alone and reported as above.  At most 128 nodes and 256 caches (distinct
+ * ones); results overlap no input.
  * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA. */
 typedef struct swapnet_tree_acceptance {
   int32_t dtype, n_seq, tokens;

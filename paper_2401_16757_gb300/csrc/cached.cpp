@@ -150,7 +150,8 @@ int fill_args(const swapnet_cached_attention* c, CachedArgs* a) {
   if (c->heads % c->kv_heads) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cached attention: heads must be a multiple of kv_heads");
   if (c->head_dim != 64 && c->head_dim != 128) SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "cached attention: head width must be 64 or 128");
   const int64_t group = c->heads / c->kv_heads;
-  if (c->n_seq > 65535 || c->kv_heads > 65535 || group > 128 || (int64_t)c->tokens * group > (1 << 20) || c->max_seq > (1 << 30))
+  if (c->n_seq > 65535 || c->kv_heads > 65535 || group > 128 || (int64_t)c->tokens * group > (1 << 20) || c->max_seq > (1 << 30) ||
+      (int64_t)c->n_seq * c->tokens > (1 << 30))
     SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "cached attention: shape beyond the kernels' limits");
   if (!c->q || !c->k || !c->lens) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cached attention: null pointer");
   const int64_t kv_width = (int64_t)c->kv_heads * c->head_dim, width = (int64_t)c->heads * c->head_dim;
@@ -277,7 +278,7 @@ int swapnet_cache_evict(const swapnet_cache_eviction* c, swapnet_stream stream) 
     if (c->n_seq < 1 || c->kv_heads < 1 || c->head_dim < 1 || c->max_seq < 1 || c->keep < 1)
       SN_FAIL(SWAPNET_ERR_INVALID_ARG, "eviction: empty shape");
     if (c->head_dim % 8 || c->head_dim > 512) SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "eviction: head width must be a multiple of 8, at most 512");
-    if (c->n_seq > 65535 || c->kv_heads > 65535 || c->max_seq > (1 << 30))
+    if (c->n_seq > 65535 || c->kv_heads > 65535 || c->max_seq > (1 << 30) || (int64_t)c->keep * (c->head_dim / 8) > (1 << 30))
       SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "eviction: shape beyond the kernels' limits");
     if (c->recent < 0 || c->sink < 0 || (int64_t)c->recent + c->sink > c->keep)
       SN_FAIL(SWAPNET_ERR_INVALID_ARG, "eviction: sink + recent must be within keep");
@@ -332,12 +333,12 @@ int swapnet_tree_accept(const swapnet_tree_acceptance* c, swapnet_stream stream)
     if (!c) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "null arguments");
     AcceptArgs a;
     std::memset(&a, 0, sizeof(a));
-    a.es = dtype_size(c->dtype);
     if (c->dtype != SWAPNET_F16 && c->dtype != SWAPNET_BF16) SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "tree acceptance: fp16 or bf16 only");
     if (c->n_seq < 1 || c->tokens < 1 || c->width < 1 || c->max_seq < 1 || c->n_caches < 0)
       SN_FAIL(SWAPNET_ERR_INVALID_ARG, "tree acceptance: empty shape");
     if (c->tokens > kTreeMax || c->n_caches > kAcceptMaxCaches || c->n_seq > 65535 || c->max_seq > (1 << 30))
       SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "tree acceptance: at most 128 nodes a sequence and 256 caches");
+    if (c->width > (1 << 24)) SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "tree acceptance: rows of at most 2^24 elements");
     if (c->width % 8) SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "tree acceptance: width must be a multiple of 8");
     if (!c->ids || !c->targets || !c->lens || !c->path || !c->accepted || !c->next || !c->lens_out || (c->n_caches && (!c->caches || !c->drafts)))
       SN_FAIL(SWAPNET_ERR_INVALID_ARG, "tree acceptance: null pointer");
@@ -368,7 +369,11 @@ int swapnet_tree_accept(const swapnet_tree_acceptance* c, swapnet_stream stream)
     a.accepted = c->accepted;
     a.next = c->next;
     a.lens_out = c->lens_out;
-    if (a.lens == a.lens_out) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "tree acceptance: lens_out must not be lens (every cache reads lens)");
+    // every cache's CTA reads the inputs while the first one writes the results
+    const int *const ins[5] = {a.ids, a.targets, a.parents, a.counts, a.lens}, *const outs[4] = {a.path, a.accepted, a.next, a.lens_out};
+    for (const int* in : ins)
+      for (const int* out : outs)
+        if (in == out) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "tree acceptance: a result must not be an input");
     if (int rc = error_word(&a.err)) return rc;
     return launch_tree_accept(a, reinterpret_cast<cudaStream_t>(stream));
   });

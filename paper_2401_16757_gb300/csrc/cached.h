@@ -82,7 +82,7 @@ int launch_cache_evict(const EvictArgs& a, cudaStream_t s);
 
 constexpr int kAcceptMaxCaches = 256;
 struct AcceptArgs {
-  int es, n_seq, tokens, width, max_seq, n_caches;
+  int n_seq, tokens, width, max_seq, n_caches;
   int64_t cache_stride, seq_stride, new_stride;  // elements
   const int *ids, *targets, *parents, *counts, *lens;
   int *path, *accepted, *next, *lens_out;

@@ -1976,7 +1976,6 @@ int swapnet_engine_tree_accept(swapnet_engine* e, const int32_t* d_ids, const in
     if (rc) return rc;
     AcceptArgs a;
     std::memset(&a, 0, sizeof(a));
-    a.es = m.es;
     a.n_seq = 1;
     a.tokens = st.tokens;
     a.width = st.width;

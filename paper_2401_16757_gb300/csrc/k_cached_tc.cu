@@ -10,13 +10,15 @@
 //   S = Q K^T     tcgen05.mma, M 128 (rows) x N 64 (keys), twice; Q, K and V by
 //                 TMA (128-byte swizzle); S in two TMEM buffers, so that the
 //                 next tile's S is computed during this tile's softmax
-//   P             warps 4..19, four threads per row, 32 keys each: the first 64
-//                 keys of every tile and the last 64 have a softmax of their
-//                 own (reference m, sum l, output O_h), whose two threads only
-//                 vote on whether m has to grow.  Scores from TMEM, masks only
-//                 in tiles that a limit crosses, p = 2^(s - m) back over the
-//                 scores as two parts of the storage type p_hi + p_lo (about 16
-//                 bits of p)
+//   P             warps 4..11, two threads per row: the first 64 keys of every
+//                 tile and the last 64 have a softmax of their own (reference m,
+//                 sum l, output O_h), so that no thread asks another for
+//                 anything.  Scores from TMEM, masks only in tiles that a limit
+//                 crosses, p = 2^(s - m) back over the scores as two parts of
+//                 the storage type, p_hi + p_lo: one part would leave 8 (bf16)
+//                 or 11 (fp16) bits of p, less than the fp32 that the sums keep;
+//                 two leave 16 or more, for a second product with V, whose tensor
+//                 time is hidden behind the exponentials
 //   O_h += P_h V  tcgen05.mma with A = P from TMEM, B = V as loaded (MN-major)
 // O_0 and O_1 stay in TMEM.  m is the running maximum only where that grew by
 // more than 2^8 since it was last taken (kSlack): until then p and l stay
@@ -28,6 +30,9 @@
 // K and V tiles pass through one ring in the order they are used, across
 // units.  Every wait is bounded: on timeout the kernel records kDevErrTimeout,
 // drains the loads and MMAs it started, frees TMEM and returns.
+//
+// What bounds it (GB300, cache out of L2): 12 sequences x 8 key heads (group 4)
+// x 64 nodes on 1100 to 1600 rows each of 128 wide bf16 heads: PERF_TREE_BATCH
 #include <algorithm>
 #include <cstring>
 #include <string>
@@ -42,14 +47,13 @@ namespace swapnet {
 namespace {
 
 constexpr int kSoftThreads = 256;
-constexpr int kTcThreads = 64 + kSoftThreads;
+constexpr int kTcThreads = 64 + kSoftThreads;  // weights: TMA, MMA, sums
 // attention: warps 0 (TMA) and 1 (MMA), two idle ones that complete their
-// warpgroup, the softmax's 8 kSub; 384 x 168 registers at launch, of which
+// warpgroup, the softmax's 8; 384 x 168 registers at launch, of which
 // setmaxnreg leaves 128 x 72 and gives 256 x 216
-constexpr int kSub = 1;  // threads per row and half of the keys
-constexpr int kAtSoft = 256 * kSub, kAtThreads = 128 + kAtSoft;
-constexpr int kRegsLow = kSub == 1 ? 72 : 64, kRegsHigh = kSub == 1 ? 216 : 104;
-static_assert(128 * kRegsLow + kAtSoft * kRegsHigh <= kAtThreads * (kSub == 1 ? 168 : 96), "registers of a CTA");
+constexpr int kAtThreads = 128 + kSoftThreads;
+constexpr int kRegsLow = 72, kRegsHigh = 216;
+static_assert(128 * kRegsLow + kSoftThreads * kRegsHigh <= kAtThreads * 168, "registers of a CTA");
 constexpr int kKeys = 128;       // keys of a tile
 constexpr float kSlack = 8.0f;   // log2 of what p may exceed 1 by
 constexpr uint32_t kTmemCols = 512;
@@ -67,11 +71,11 @@ template <int D> struct TcCfg {
   static constexpr int kOffQ = 0;
   static constexpr int kOffRing = kTile;
   static constexpr int kOffX = kOffRing + kSlots * kTile;   // (m, l) of every thread
-  static constexpr int kOffPar = kOffX + kAtSoft * 8;       // parents
+  static constexpr int kOffPar = kOffX + kSoftThreads * 8;       // parents
   static constexpr int kOffOdd = kOffPar + kTreeMax * 4;    // odd value rows, a bit each
   static constexpr int kOffBar = kOffOdd + 16;
-  static constexpr int kOffStage = kOffBar + 256;           // REP 2: 32 columns of 2 kSub x 64 rows, and growths' maxima
-  static constexpr int kOffNear = kOffStage + 2 * kSub * 64 * 36 * 4;
+  static constexpr int kOffStage = kOffBar + 256;           // REP 2: 32 columns of each half's 64 rows
+  static constexpr int kOffNear = kOffStage + 2 * 64 * 36 * 4;
   static constexpr int kSmem = kOffNear + kNear * 8 + 1024;  // + alignment slack
   static_assert(kSmem <= 232448, "shared memory of a CTA");
 };
@@ -97,18 +101,6 @@ __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t* r) {
       "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
       "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
-}
-__device__ __forceinline__ uint32_t bar_or(int id, int threads, bool v) {  // a named barrier; whether any thread's v is set
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.u32 p, %1, 0;\n\t"
-      "bar.red.or.pred q, %2, %3, p;\n\t"
-      "selp.u32 %0, 1, 0, q;\n\t}"
-      : "=r"(r)
-      : "r"((uint32_t)v), "r"(id), "r"(threads)
-      : "memory");
-  return r;
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -240,9 +232,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
                           const __grid_constant__ CUtensorMap tmVn, const __grid_constant__ CachedArgs a, int queries, int nrt) {
   using F = TcCfg<D>;
   constexpr int kRowsMax = 128 / REP;
-  constexpr int kPart = 64 / kSub;    // keys of a warp and tile
-  constexpr int NK = kPart / REP;     // of a thread
-  constexpr int kParts = 2 * kSub;
+  constexpr int NK = 64 / REP;  // keys of a thread and tile
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   float2* ml = reinterpret_cast<float2*>(smem + F::kOffX);
@@ -273,13 +263,13 @@ __global__ void __launch_bounds__(kAtThreads, 1)
       mbar_init(o_full(i), 1);
       for (int h = 0; h < 2; ++h) {
         mbar_init(s_full(h, i), 1);
-        mbar_init(p_full(h, i), 4 * kSub);
+        mbar_init(p_full(h, i), 4);
       }
     }
     mbar_init(q_full, 1);
     mbar_init(q_free, 1);
     mbar_init(o_done, 1);
-    mbar_init(o_free, kAtSoft / 32);
+    mbar_init(o_free, kSoftThreads / 32);
     mbar_init(done_bar, 1);
     *abort_flag = 0;
 #pragma unroll
@@ -465,7 +455,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
 #pragma unroll
               for (int ks = 0; ks < 4; ++ks)  // 16 keys a step
                 tc_mma_f16_ta(tmem + kTmO + (uint32_t)h * 128u,
-                              pt + (uint32_t)(ks / (4 / kSub) * kPart + part * (kPart / 2) + ks % (4 / kSub) * 8),
+                              pt + (uint32_t)(part * 32 + ks * 8),
                               vt + (uint64_t)((h * 4 + ks) * (2048 >> 4)), idesc_pv, (uint32_t)(i | part | ks) != 0);
             tc_commit(o_full(h));
           }
@@ -483,19 +473,16 @@ __global__ void __launch_bounds__(kAtThreads, 1)
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsHigh));
     // ---------------- softmax and output
-    // four threads per row: `half` of a tile's keys (an output and a reference
-    // of its own), `part` = half and half of that
-    const int q4 = warp & 3, part = (warp - 4) >> 2, half = part / kSub;
+    // two threads per row: `half` of a tile's keys, an output and a reference of
+    // its own
+    const int q4 = warp & 3, half = (warp - 4) >> 2;
     const int slot = q4 * 32 + lane, rep = slot / kRowsMax, row = slot % kRowsMax;
     const int aid = (warp - 4) * 32 + lane;
-    const int kofs = part * kPart + rep * NK;  // this thread's first key of a tile
+    const int kofs = half * 64 + rep * NK;  // this thread's first key of a tile
     const uint32_t lane_off = (uint32_t)(q4 * 32) << 16;
     const uint32_t tO = tmem + kTmO + (uint32_t)half * 128u + lane_off;
-    const int pair_id = 1 + 2 * q4 + half;  // the two warps of a half
-    auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(pair_id) : "memory"); };
-    auto row_sync = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(10 + q4), "n"(64 * kSub) : "memory"); };
-    auto all_sync = [&]() { asm volatile("bar.sync 9, %0;" ::"n"(kAtSoft) : "memory"); };
-    float* xch = reinterpret_cast<float*>(smem + F::kOffStage);  // [part][slot]
+    auto row_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory"); };  // the two warps of the same rows
+    auto all_sync = [&]() { asm volatile("bar.sync 5, %0;" ::"n"(kSoftThreads) : "memory"); };
     bool ok = true;
     int pos0 = 0, g0 = 0;
     int rest = 0, rest_rows = 0;  // the unit that this CTA begins and others go on with
@@ -510,7 +497,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
       bool bad = false;  // a parent that is none
       if (a.parents && (last || cur.i0 == 0)) {  // (the first piece's CTA speaks for the join)
         all_sync();  // the piece before has read its parents
-        for (int i = aid; i < count; i += kAtSoft) par[i] = a.parents[(int64_t)b * a.tokens + i];
+        for (int i = aid; i < count; i += kSoftThreads) par[i] = a.parents[(int64_t)b * a.tokens + i];
         all_sync();
         for (int i = lane; i < count; i += 32) bad = bad || par[i] < -1 || par[i] >= i;
         bad = __any_sync(0xffffffffu, bad);
@@ -531,13 +518,9 @@ __global__ void __launch_bounds__(kAtThreads, 1)
           uint32_t s[NK];
           float mx = -INFINITY;
           if (ok) {
-            if constexpr (NK == 16) {
-              tmem_ld_32x32b_x16(tS + (uint32_t)kofs, s);
-            } else {
 #pragma unroll
-              for (int c = 0; c < NK; c += 32)
-                tmem_ld_32x32b_x32(tS + (uint32_t)(kofs + c), *reinterpret_cast<uint32_t(*)[32]>(s + c));
-            }
+            for (int c = 0; c < NK; c += 32)
+              tmem_ld_32x32b_x32(tS + (uint32_t)(kofs + c), *reinterpret_cast<uint32_t(*)[32]>(s + c));
             tmem_ld_wait();
             if (masked) {
               uint64_t see = 0;
@@ -557,16 +540,10 @@ __global__ void __launch_bounds__(kAtThreads, 1)
             for (int k = 0; k < NK; ++k) mx4[k & 3] = fmaxf(mx4[k & 3], __uint_as_float(s[k]));
             mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * a.scale_log2;
           }
-          // the warps of a half vote (with kSub 2, also after a timeout)
           const bool grow = mx - m > kSlack;  // (also the first key seen)
-          if (kSub == 1 ? __any_sync(0xffffffffu, grow) : bar_or(pair_id, 64, grow) != 0) {
-            if (kSub == 2) {
-              xch[part * 128 + slot] = mx;
-              pair_sync();
-              mx = fmaxf(mx, xch[(part ^ 1) * 128 + slot]);
-            }
+          if (__any_sync(0xffffffffu, grow)) {
             float alpha = 1.f;
-            if (mx - m > kSlack) {
+            if (grow) {
               alpha = ex2(m - mx);
               m = mx;
               l *= alpha;
@@ -577,18 +554,16 @@ __global__ void __launch_bounds__(kAtThreads, 1)
               tc_fence_after();
               if (ok) {
 #pragma unroll 1  // (seldom run: short code, which the instruction cache has room beside the rest for)
-                for (int c = 0; c < D / kSub; c += 16) {  // each warp its share of the columns
+                for (int c = 0; c < D; c += 16) {
                   uint32_t r[16];
-                  const uint32_t at = tO + (uint32_t)(part % kSub * (D / kSub) + c);
-                  tmem_ld_32x32b_x16(at, r);
+                  tmem_ld_32x32b_x16(tO + (uint32_t)c, r);
                   tmem_ld_wait();
 #pragma unroll
                   for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * alpha);
-                  tmem_st_x16(at, r);
+                  tmem_st_x16(tO + (uint32_t)c, r);
                 }
               }
             }
-            if (kSub == 2) pair_sync();  // xch has been read
           }
           if (ok) {
             const float base = m == -INFINITY ? 0.f : m;
@@ -629,7 +604,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
             return reinterpret_cast<uint4*>(vs + (c >> 3) * F::kBox + r * 128 + (((c & 7) ^ (r & 7)) << 4));
           };
           if (ok) {
-            for (int c = aid; c < kKeys * (D / 8); c += kAtSoft) {
+            for (int c = aid; c < kKeys * (D / 8); c += kSoftThreads) {
               const int r = c / (D / 8);
               uint4* at = chunk(r, c % (D / 8));
               if (r >= have) {
@@ -644,7 +619,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
           odd = odd_rows[0] | odd_rows[1] | odd_rows[2] | odd_rows[3];
           if (odd) {
 #pragma unroll 1
-            for (int c = aid; c < kKeys * (D / 8); c += kAtSoft) {
+            for (int c = aid; c < kKeys * (D / 8); c += kSoftThreads) {
               const int r = c / (D / 8);
               if (odd_rows[r >> 5] >> (r & 31) & 1u) *chunk(r, c % (D / 8)) = make_uint4(0u, 0u, 0u, 0u);
             }
@@ -654,16 +629,16 @@ __global__ void __launch_bounds__(kAtThreads, 1)
         }
         if (ok) {
           if (works) {
-            // over the part's scores: hi parts of its keys, then the lo parts
+            // over the half's scores: hi parts of its keys, then the lo parts
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
               const uint32_t* x = u ? lo : hi;
 #pragma unroll
-              for (int c = 0; c < kPart / 2; c += 16) {
+              for (int c = 0; c < 32; c += 16) {
                 uint32_t w[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) w[e] = REP == 1 || (c + e) / (NK / 2) == rep ? x[(c + e) % (NK / 2)] : 0u;
-                tmem_st_x16(tS + (uint32_t)(part * kPart + u * (kPart / 2) + c), w);
+                tmem_st_x16(tS + (uint32_t)(half * 64 + u * 32 + c), w);
               }
             }
             tmem_st_wait();
@@ -704,7 +679,6 @@ __global__ void __launch_bounds__(kAtThreads, 1)
               }
               tc_fence_before();
             }
-            if (kSub == 2) pair_sync();  // the half's other warp adds to the same outputs
             tc_fence_after();
           }
           all_sync();  // everyone has read the odd rows
@@ -718,27 +692,27 @@ __global__ void __launch_bounds__(kAtThreads, 1)
       ok = ok && mbar_wait_bounded(o_done, piece & 1, abort_flag, a.err);
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
-      ml[part * 128 + slot] = make_float2(m, l);
+      ml[half * 128 + slot] = make_float2(m, l);
       if (REP == 1) row_sync(); else all_sync();
       float M = -INFINITY, L = 0.f, f[2];
 #pragma unroll
-      for (int u = 0; u < kParts * REP; ++u) M = fmaxf(M, ml[u * kRowsMax + row].x);  // (part-major, then the copies of the rows)
+      for (int u = 0; u < 2 * REP; ++u) M = fmaxf(M, ml[u * kRowsMax + row].x);  // (half-major, then the copies of the rows)
       const float base = M == -INFINITY ? 0.f : M;
 #pragma unroll
-      for (int u = 0; u < kParts * REP; ++u) {
+      for (int u = 0; u < 2 * REP; ++u) {
         const float2 x = ml[u * kRowsMax + row];
         L = fmaf(x.y, ex2(x.x - base), L);
       }
 #pragma unroll
-      for (int h = 0; h < 2; ++h) f[h] = ex2(ml[kSub * h * 128 + slot].x - base);  // 0 where no key was seen
+      for (int h = 0; h < 2; ++h) f[h] = ex2(ml[h * 128 + slot].x - base);  // 0 where no key was seen
       const float inv = L > 0.f ? 1.0f / L : (L == 0.f ? 0.f : L);  // (a NaN stays one)
       const bool writes = ok && !bad && row < rows && (REP == 1 || rep == 0);
       const int tq = t0 + row / a.group, hd = kvh * a.group + row % a.group;
       T* out = static_cast<T*>(a.out) + ((int64_t)b * a.tokens + tq) * a.out_stride + (int64_t)hd * D;
       const int64_t at = ((int64_t)2 * blockIdx.x + (cur.i0 == 0 ? 1 : 0)) * kRowsMax + row;
 #pragma unroll 1
-      for (int c = 0; c < D / kParts; c += 32) {
-        const int col = part * (D / kParts) + c;
+      for (int c = 0; c < D / 2; c += 32) {
+        const int col = half * (D / 2) + c;
         float o[32];
         if (works) {
           uint32_t r[32];
@@ -752,7 +726,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
           for (int e = 0; e < 32; ++e) o[e] = fmaf(__uint_as_float(r[e]), f[1], o[e]);
         }
         if (REP == 2) {
-          float* stage = reinterpret_cast<float*>(smem + F::kOffStage) + (part * 64 + row) * 36;
+          float* stage = reinterpret_cast<float*>(smem + F::kOffStage) + (half * 64 + row) * 36;
           if (rep == 1) {
 #pragma unroll
             for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(stage + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
@@ -789,7 +763,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
       tc_fence_before();
       __syncwarp();
       if (lane == 0 && ok) mbar_arrive(o_free);
-      if (writes && part == 0) {
+      if (writes && half == 0) {
         if (!whole)
           reinterpret_cast<float2*>(a.ml)[at] = make_float2(M, L);
         else if (a.lse)

@@ -27,7 +27,7 @@ def _code(call, *a, **kw):
     (dict(dtype="f32"), capi.ERR_UNSUPPORTED), (dict(dtype=9), capi.ERR_UNSUPPORTED),
     (dict(n_seq=0), capi.ERR_INVALID_ARG), (dict(tokens=0), capi.ERR_INVALID_ARG), (dict(max_seq=0), capi.ERR_INVALID_ARG),
     (dict(heads=7), capi.ERR_INVALID_ARG), (dict(head_dim=96), capi.ERR_UNSUPPORTED),
-    (dict(n_seq=70000), capi.ERR_UNSUPPORTED), (dict(heads=258, kv_heads=2), capi.ERR_UNSUPPORTED),
+    (dict(n_seq=70000), capi.ERR_UNSUPPORTED), (dict(n_seq=40000, tokens=30000), capi.ERR_UNSUPPORTED), (dict(heads=258, kv_heads=2), capi.ERR_UNSUPPORTED),
     (dict(q=0), capi.ERR_INVALID_ARG), (dict(k=0), capi.ERR_INVALID_ARG), (dict(v=0), capi.ERR_INVALID_ARG),
     (dict(lens=0), capi.ERR_INVALID_ARG), (dict(out=0), capi.ERR_INVALID_ARG),
     (dict(q=A + 8), capi.ERR_MISALIGNED), (dict(k=A + 2), capi.ERR_MISALIGNED), (dict(out=A + 4), capi.ERR_MISALIGNED),
@@ -87,6 +87,7 @@ def _evict(**kw):
     (dict(k_out=A, v_out=2 * A, weights_out=3 * A, out_capacity=50), capi.ERR_INVALID_ARG),
     (dict(v_out=5 * A), capi.ERR_INVALID_ARG), (dict(k=A + 8), capi.ERR_MISALIGNED), (dict(kv_stride=132), capi.ERR_MISALIGNED),
     (dict(kv_stride=120), capi.ERR_INVALID_ARG), (dict(out_seq_stride=-8), capi.ERR_INVALID_ARG),
+    (dict(max_seq=1 << 28, keep=1 << 28), capi.ERR_UNSUPPORTED),
 ])
 def test_eviction_refuses(change, code):
     assert _code(_evict, **change) == code
@@ -102,13 +103,20 @@ def _accept(**kw):
 @pytest.mark.parametrize("change,code", [
     (dict(dtype="f32"), capi.ERR_UNSUPPORTED), (dict(tokens=0), capi.ERR_INVALID_ARG), (dict(tokens=129), capi.ERR_UNSUPPORTED),
     (dict(width=60), capi.ERR_UNSUPPORTED), (dict(ids=0), capi.ERR_INVALID_ARG), (dict(next=0), capi.ERR_INVALID_ARG),
-    (dict(lens_out=A), capi.ERR_INVALID_ARG), (dict(caches=np.array([0])), capi.ERR_INVALID_ARG),
+    (dict(lens_out=A), capi.ERR_INVALID_ARG), (dict(width=1 << 25), capi.ERR_UNSUPPORTED), (dict(caches=np.array([0])), capi.ERR_INVALID_ARG),
     (dict(caches=np.array([A + 8])), capi.ERR_MISALIGNED), (dict(cache_stride=32), capi.ERR_INVALID_ARG),
     (dict(new_stride=68), capi.ERR_MISALIGNED),
     (dict(caches=np.full(257, A), drafts=np.full(257, A)), capi.ERR_UNSUPPORTED),
 ])
 def test_acceptance_refuses(change, code):
     assert _code(_accept, **change) == code
+
+
+@pytest.mark.parametrize("change", [{}, dict(path=2 * A), dict(path=2 * A, accepted=3 * A),
+                                    dict(path=2 * A, accepted=3 * A, next=4 * A, lens_out=5 * A, counts=3 * A),
+                                    dict(path=2 * A, accepted=3 * A, next=4 * A, lens_out=5 * A, parents=2 * A)])
+def test_acceptance_refuses_results_over_inputs(change):
+    assert _code(_accept, **change) == capi.ERR_INVALID_ARG
 
 
 def test_acceptance_needs_a_draft_per_cache():

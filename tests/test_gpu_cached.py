@@ -417,6 +417,170 @@ def test_weights_from_lse(dtype, heads, kv, dim, tokens, pick):
         assert torch.equal(dev[3][b, :, :m], w[b, :, :m]) and torch.equal(dev[3][b, :, m:].cpu(), c.win[b, :, m:])
 
 
+def test_a_query_listed_twice_counts_twice():
+    torch = _torch()
+    c = Case("f16", 1, 6, 4, 2, 64, 90, [70], draft=False, seed=21)
+    rows = torch.tensor([[3, 3, 0, 3]], dtype=torch.int32)
+    z = [torch.einsum("hd,jhd->hj", c.q[r].double().view(4, 64), c.k[0, :67 + i].double().view(-1, 2, 64).repeat_interleave(2, 1)) / 8
+         for i, r in enumerate(rows[0].tolist())]
+    lse = torch.randn(1, 4, 6)
+    lse[0, :, 3], lse[0, :, 0] = z[3].logsumexp(-1).float(), z[2].logsumexp(-1).float()
+    want = torch.zeros(2, 70, dtype=torch.float64)
+    for i, r in enumerate(rows[0].tolist()):
+        want[:, :67 + i] += torch.exp(z[i] - lse[0, :, r, None].double()).view(2, 2, -1).sum(1)
+    dev = [x.cuda() for x in (c.q, c.k, lse, rows, torch.tensor([70], dtype=torch.int32), torch.tensor([4], dtype=torch.int32))]
+    listed = torch.zeros(1, 6, dtype=torch.int32, device="cuda")
+    listed[:, :4] = dev[3]
+    w = torch.full((1, 2, 90), SENT, device="cuda")
+    capi.attention_weights(capi.cached_attention("f16", 1, 6, 4, 2, 64, 90, q=dev[0].data_ptr(), k=dev[1].data_ptr(),
+                                                 lens=dev[4].data_ptr(), counts=dev[5].data_ptr(), rows=listed.data_ptr(),
+                                                 lse=dev[2].data_ptr(), weights=w.data_ptr()),
+                           torch.cuda.current_stream().cuda_stream)
+    # scores of at most about 20 in fp32, 64 products each: 64 2^-23 * 40 of the weight
+    assert torch.all((w[0, :, :70].cpu().double() - want).abs() <= 4e-4 * want + 1e-9) and torch.all(w[..., 70:] == SENT)
+
+
+# ------------------------------------------- layouts, numbers and neighbours
+def _attend(q, k, v, kn, vn, par, lens, n, t, h, kv, d, cap, kv_stride=0, seq_stride=0, weigh=False):
+    """out, lse and weights of a call on device tensors (k, v: addresses)."""
+    torch = _torch()
+    out, lse = torch.full_like(q, SENT), torch.full((n, h, t), SENT, device="cuda")
+    w = torch.full((n, kv, cap), SENT, device="cuda") if weigh else None
+    p = lambda x: 0 if x is None else x.data_ptr()  # noqa: E731
+    a = capi.cached_attention("bf16", n, t, h, kv, d, cap, q=p(q), k=k, v=v, lens=p(lens), k_new=p(kn), v_new=p(vn), parents=p(par),
+                              out=p(out), lse=p(lse), weights=p(w), kv_stride=kv_stride, seq_stride=seq_stride)
+    ws = torch.empty(max(256, capi.attention_tree_workspace(a)), dtype=torch.uint8, device="cuda")
+    capi.attention_tree(a, ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream)
+    return [x for x in (out, lse, w) if x is not None]
+
+
+def test_offsets_past_32_bits_and_interleaved_sequences():
+    """Rows millions of elements apart, the sequences' rows side by side: the same bits as on packed caches, in every call."""
+    torch = _torch()
+    n, h, kv, d, cap, stride = 2, 8, 2, 128, 200, 12_000_000
+    width = kv * d
+    g = torch.Generator().manual_seed(3)
+    k, v = (torch.randn(n, cap, width, generator=g).bfloat16().cuda() for _ in range(2))
+    lens = torch.tensor([200, 190], dtype=torch.int32, device="cuda")
+    big = torch.zeros(cap, stride, dtype=torch.bfloat16, device="cuda")
+    assert (cap - 1) * stride > 2 ** 31
+    wide = big[:, :4 * width].view(cap, n, 2, width)  # row, sequence, keys and values
+
+    def fill():
+        wide[:, :, 0], wide[:, :, 1] = k.transpose(0, 1), v.transpose(0, 1)
+
+    fill()
+    at = dict(k=big.data_ptr(), v=big.data_ptr() + 2 * width, kv_stride=stride, seq_stride=2 * width)
+    for t in (1, 3, 30):
+        q = torch.randn(n * t, h * d, generator=g).bfloat16().cuda()
+        kn, vn = (torch.randn(n * t, width, generator=g).bfloat16().cuda() for _ in range(2))
+        par = torch.from_numpy(_tree(np.random.default_rng(t), n, t)).cuda()
+        for draft in (False, True):
+            x = (kn, vn, par) if draft else (None, None, None)
+            a = _attend(q, k.data_ptr(), v.data_ptr(), *x, lens, n, t, h, kv, d, cap, weigh=not draft)
+            b = _attend(q, at["k"], at["v"], *x, lens, n, t, h, kv, d, cap, stride, 2 * width, weigh=not draft)
+            assert all(torch.equal(y, z) for y, z in zip(a, b)), (t, draft)
+            ws = []
+            for kk, st, sq in ((k.data_ptr(), 0, 0), (at["k"], stride, 2 * width)):
+                w = torch.full((n, kv, cap), SENT, device="cuda")
+                capi.attention_weights(capi.cached_attention("bf16", n, t, h, kv, d, cap, q=q.data_ptr(), k=kk, lens=lens.data_ptr(),
+                                                             lse=a[1].data_ptr(), weights=w.data_ptr(), kv_stride=st, seq_stride=sq),
+                                       torch.cuda.current_stream().cuda_stream)
+                ws.append(w)
+            assert torch.equal(*ws)
+    # acceptance appends at rows behind 2^31 elements
+    t = 8
+    draft = torch.randn(n * t, width, generator=g).bfloat16().cuda()
+    ids = torch.zeros(n, t, dtype=torch.int32, device="cuda")
+    path = torch.empty_like(ids)
+    acc, nxt, lo = (torch.empty(n, dtype=torch.int32, device="cuda") for _ in range(3))
+    few = torch.tensor([185, 181], dtype=torch.int32, device="cuda")
+    capi.tree_accept("bf16", n, t, width, cap, ids=ids.data_ptr(), targets=torch.zeros_like(ids).data_ptr(), lens=few.data_ptr(),
+                     caches=[at["k"], at["v"]], drafts=[draft.data_ptr()] * 2, path=path.data_ptr(), accepted=acc.data_ptr(),
+                     next=nxt.data_ptr(), lens_out=lo.data_ptr(), cache_stride=stride, seq_stride=2 * width,
+                     stream=torch.cuda.current_stream().cuda_stream)
+    assert lo.tolist() == [193, 189]
+    for b, m in enumerate(few.tolist()):
+        for i, old in enumerate((k, v)):
+            want = old[b].clone()
+            want[m:m + t] = draft.view(n, t, width)[b]
+            assert torch.equal(wide[:, b, i], want)
+    # eviction, to another cache and in place
+    w = torch.rand(n, kv, cap, generator=g).cuda()
+    kept, lo = torch.zeros(n, kv, 150, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda")
+    ref = [torch.zeros(n, cap, width, dtype=torch.bfloat16, device="cuda") for _ in range(2)] + [torch.zeros_like(w)]
+    fill()
+    common = dict(lens=lens.data_ptr(), kept=kept.data_ptr(), lens_out=lo.data_ptr(), stream=torch.cuda.current_stream().cuda_stream)
+    capi.cache_evict("bf16", n, kv, d, cap, 150, 9, 2, k=k.data_ptr(), v=v.data_ptr(), weights=w.data_ptr(), k_out=ref[0].data_ptr(),
+                     v_out=ref[1].data_ptr(), weights_out=ref[2].data_ptr(), **common)
+    got = [torch.zeros_like(x) for x in ref]
+    src = dict(k=at["k"], v=at["v"], kv_stride=stride, seq_stride=2 * width)
+    capi.cache_evict("bf16", n, kv, d, cap, 150, 9, 2, weights=w.data_ptr(), k_out=got[0].data_ptr(), v_out=got[1].data_ptr(),
+                     weights_out=got[2].data_ptr(), **src, **common)
+    assert all(torch.equal(x, y) for x, y in zip(ref, got)) and kept.max() > 180
+    capi.cache_evict("bf16", n, kv, d, cap, 150, 9, 2, weights=w.data_ptr(), k_out=at["k"], v_out=at["v"], out_stride=stride,
+                     out_seq_stride=2 * width, weights_out=w.data_ptr(), **src, **common)
+    for b in range(n):
+        for i in range(2):
+            assert torch.equal(wide[:150, b, i], ref[i][b, :150])
+    for b, m in enumerate(lens.tolist()):  # (weights behind the sequence's end stay as they were)
+        assert torch.equal(w[b, :, :m], ref[2][b, :, :m])
+    assert torch.all(big[:, 4 * width:4 * width + 64] == 0)
+
+
+@pytest.mark.parametrize("heads,kv,tokens", [(160, 160, 20), (160, 160, 2), (256, 2, 1), (100, 1, 3)])
+def test_more_heads_than_sms_and_wide_groups(heads, kv, tokens):
+    Case("bf16", 2, tokens, heads, kv, 64, 300, [300, 5 + tokens], draft=True, seed=31).run().check()
+    Case("f16", 2, tokens, heads, kv, 64, 300, [300, 5 + tokens], draft=False, weigh=True, seed=32).run().check()
+
+
+@pytest.mark.parametrize("draft", [False, True])
+def test_runs_over_many_idle_sequences(draft):
+    """A run of key tiles that passes more than a hundred sequences without a query, and ends in others of a tile each."""
+    n = 200
+    lens = [130] * n
+    lens[0], lens[-1] = 4000, 2500
+    counts = [20] * n
+    for b in range(1, 140):
+        counts[b], lens[b] = 0, b
+    Case("bf16", n, 20, 1, 1, 64, 4096, lens, counts, draft=draft, weigh=not draft, seed=33, poison=False).run().check()
+
+
+@pytest.mark.parametrize("tokens", [2, 20])
+def test_replays_follow_the_lengths_and_calls_run_side_by_side(tokens):
+    """A captured call reads the lengths of the moment; calls on two streams at once, with workspaces of their own, give the
+    bits that they give alone."""
+    torch = _torch()
+    n, h, kv, d, cap = 3, 8, 2, 128, 3000
+    g = torch.Generator().manual_seed(8)
+    k, v = (torch.randn(n, cap, kv * d, generator=g).bfloat16().cuda() for _ in range(2))
+    q = torch.randn(n * tokens, h * d, generator=g).bfloat16().cuda()
+    lens = [torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([3000, 20, 777], [64, 2999, 25], [0, 3000, 3000])]
+    alone = [_attend(q, k.data_ptr(), v.data_ptr(), None, None, None, x, n, tokens, h, kv, d, cap, weigh=True) for x in lens]
+    now = lens[0].clone()
+    s = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = _attend(q, k.data_ptr(), v.data_ptr(), None, None, None, now, n, tokens, h, kv, d, cap, weigh=True)
+    for x, want in zip(lens, alone):
+        now.copy_(x)
+        for y in got:
+            y.fill_(SENT)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(y, z) for y, z in zip(got, want))
+    res = [[], []]
+    for _ in range(8):
+        for i in range(2):
+            with torch.cuda.stream(s[i]):
+                res[i].append(_attend(q, k.data_ptr(), v.data_ptr(), None, None, None, lens[i], n, tokens, h, kv, d, cap, weigh=True))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for r in res[i]:
+            assert all(torch.equal(y, z) for y, z in zip(r, alone[i]))
+
+
 # ------------------------------------------------------------------ eviction
 def _keep_rows(w, m, keep, recent, sink):
     if m <= keep:
