@@ -173,3 +173,17 @@ def test_flags_are_the_same_on_every_layer():
     assert capi.lib().swapnet_plan_state_layout(None, None) == capi.ERR_INVALID_ARG
     assert capi.lib().swapnet_engine_tree_accept(None, None, None, None) == capi.ERR_INVALID_ARG
     assert capi.lib().swapnet_engine_evict(None, 1, 0, 0, None) == capi.ERR_INVALID_ARG
+
+
+def test_argument_blocks_have_the_header_layout():
+    """The blocks are packed in one step: every value lands in the field of its name."""
+    import ctypes as C
+
+    from paper_2401_16757_gb300 import _capi
+
+    for form, block in ((_capi._ATTENTION, _capi.CachedAttention), (_capi._EVICTION, _capi.CacheEviction),
+                        (_capi._ACCEPTANCE, _capi.TreeAcceptance)):
+        assert form.size == C.sizeof(block)
+    names = [n for n, _ in _capi.CachedAttention._fields_]
+    a = capi.cached_attention(**{n: i + 1 for i, n in enumerate(names)})
+    assert [getattr(a, n) for n in names] == [i + 1 for i in range(len(names))]
