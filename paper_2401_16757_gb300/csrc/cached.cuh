@@ -112,10 +112,19 @@ template <> __device__ __forceinline__ float2 unpack_pair<__half>(uint32_t u) {
 template <> __device__ __forceinline__ float2 unpack_pair<__nv_bfloat16>(uint32_t u) {
   return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
 }
-// Whether one of a register's two elements is infinite or not a number.
-template <typename T> __device__ __forceinline__ bool odd_pair(uint32_t u) {
-  constexpr uint32_t e = sizeof(T) == 2 && std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u;
-  return (u & e) == e || ((u >> 16) & e) == e;
+// Whether one of eight elements is infinite or not a number: only then is the
+// sum of their products with 0 not 0.
+__device__ __forceinline__ bool odd_sum(__half2 x, __half2 y, __half2 z, __half2 w) {
+  const __half2 o = __float2half2_rn(0.f), s = __hfma2(x, o, __hfma2(y, o, __hfma2(z, o, __hmul2(w, o))));
+  return !__hbeq2(s, o);
+}
+__device__ __forceinline__ bool odd_sum(__nv_bfloat162 x, __nv_bfloat162 y, __nv_bfloat162 z, __nv_bfloat162 w) {
+  const __nv_bfloat162 o = __float2bfloat162_rn(0.f), s = __hfma2(x, o, __hfma2(y, o, __hfma2(z, o, __hmul2(w, o))));
+  return !__hbeq2(s, o);
+}
+template <typename T> __device__ __forceinline__ bool odd_chunk(uint4 v) {
+  using P = typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type;
+  return odd_sum(reinterpret_cast<const P&>(v.x), reinterpret_cast<const P&>(v.y), reinterpret_cast<const P&>(v.z), reinterpret_cast<const P&>(v.w));
 }
 
 }  // namespace swapnet

@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(kFwThreads, 2) attention_few_kernel(const __gr
       for (int i = 0; i < kGk * (D / 8) / 32; ++i) {
         const int r = (lane + 32 * i) / (D / 8), c = (lane + 32 * i) % (D / 8);
         const uint4 v = *reinterpret_cast<const uint4*>(vs + swz<D>(r, c));
-        if (odd_pair<T>(v.x) || odd_pair<T>(v.y) || odd_pair<T>(v.z) || odd_pair<T>(v.w)) odd |= 1u << r;
+        if (odd_chunk<T>(v)) odd |= 1u << r;
       }
       odd = __reduce_or_sync(0xffffffffu, odd);
       if (odd) {

@@ -71,9 +71,9 @@ template <int D> struct TcCfg {
   static constexpr int kOffQ = 0;
   static constexpr int kOffRing = kTile;
   static constexpr int kOffX = kOffRing + kSlots * kTile;   // (m, l) of every thread
-  static constexpr int kOffPar = kOffX + kSoftThreads * 8;       // parents
-  static constexpr int kOffOdd = kOffPar + kTreeMax * 4;    // odd value rows, a bit each
-  static constexpr int kOffBar = kOffOdd + 16;
+  static constexpr int kOffPar = kOffX + kSoftThreads * 8;  // parents, a copy per softmax warp
+  static constexpr int kOffOdd = kOffPar + 8 * kTreeMax * 4;  // odd value rows, a bit each, of two tiles
+  static constexpr int kOffBar = kOffOdd + 32;
   static constexpr int kOffStage = kOffBar + 256;           // REP 2: 32 columns of each half's 64 rows
   static constexpr int kOffNear = kOffStage + 2 * 64 * 36 * 4;
   static constexpr int kSmem = kOffNear + kNear * 8 + 1024;  // + alignment slack
@@ -236,7 +236,6 @@ __global__ void __launch_bounds__(kAtThreads, 1)
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   float2* ml = reinterpret_cast<float2*>(smem + F::kOffX);
-  int* par = reinterpret_cast<int*>(smem + F::kOffPar);
   uint32_t* odd_rows = reinterpret_cast<uint32_t*>(smem + F::kOffOdd);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + F::kOffBar);
   auto full = [&](int s) { return smem_u32(bars + s); };
@@ -273,7 +272,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
     mbar_init(done_bar, 1);
     *abort_flag = 0;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) odd_rows[w] = 0;
+    for (int w = 0; w < 8; ++w) odd_rows[w] = 0;
     fence_barrier_init();
     prefetch_tmap(&tmQ);
     prefetch_tmap(&tmK);
@@ -288,6 +287,13 @@ __global__ void __launch_bounds__(kAtThreads, 1)
   Cursor cur;
   cur.next = 0;
   const int kvh = blockIdx.x % a.kv_heads, run = blockIdx.x / a.kv_heads;
+  // sizes of the sequences from b0 on (with runs and more sequences than that, from the run's first)
+  cur.b0 = a.splits == 1 ? run / nrt : 0;
+  cur.near = near;
+  auto fetch_near = [&]() {
+    if (threadIdx.x < kNear && cur.b0 + (int)threadIdx.x < a.n_seq) near[threadIdx.x] = seq_size(a, cur.b0 + threadIdx.x);
+  };
+  if (a.splits == 1 || a.n_seq <= kNear) fetch_near();
   int64_t first_tile = 0, total = 0;  // the run's first tile in the order of all; their number
   int runs = 1;
   if (a.splits == 1) {
@@ -299,7 +305,6 @@ __global__ void __launch_bounds__(kAtThreads, 1)
       seq_sizes(a, cur.pair / nrt, &len, &count);  // (reports what is out of range)
     }
     tc_fence_before();
-    __syncthreads();
   } else {
     // every thread adds up a run of pairs, then the threads' sums
     const int pairs = a.n_seq * nrt, per = (pairs + kAtThreads - 1) / kAtThreads;
@@ -348,10 +353,11 @@ __global__ void __launch_bounds__(kAtThreads, 1)
       cur.pair = (int)sched[16];
       cur.next = (int)sched[17];
     }
+    if (a.n_seq > kNear) {
+      cur.b0 = cur.pair / nrt;
+      fetch_near();
+    }
   }
-  cur.b0 = cur.pair / nrt;
-  cur.near = near;
-  if (threadIdx.x < kNear && cur.b0 + (int)threadIdx.x < a.n_seq) near[threadIdx.x] = seq_size(a, cur.b0 + threadIdx.x);
   __syncthreads();  // (and sched is written again, as ml)
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
@@ -483,6 +489,9 @@ __global__ void __launch_bounds__(kAtThreads, 1)
     const uint32_t tO = tmem + kTmO + (uint32_t)half * 128u + lane_off;
     auto row_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory"); };  // the two warps of the same rows
     auto all_sync = [&]() { asm volatile("bar.sync 5, %0;" ::"n"(kSoftThreads) : "memory"); };
+    auto half_sync = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(6 + half) : "memory"); };
+    auto copy_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(8 + 2 * (q4 & 1) + half) : "memory"); };  // REP 2: a row's two lanes
+    int* par = reinterpret_cast<int*>(smem + F::kOffPar) + (warp - 4) * kTreeMax;
     bool ok = true;
     int pos0 = 0, g0 = 0;
     int rest = 0, rest_rows = 0;  // the unit that this CTA begins and others go on with
@@ -496,10 +505,12 @@ __global__ void __launch_bounds__(kAtThreads, 1)
       const int lim = visible_limit(a, len, count, t);
       bool bad = false;  // a parent that is none
       if (a.parents && (last || cur.i0 == 0)) {  // (the first piece's CTA speaks for the join)
-        all_sync();  // the piece before has read its parents
-        for (int i = aid; i < count; i += kSoftThreads) par[i] = a.parents[(int64_t)b * a.tokens + i];
-        all_sync();
-        for (int i = lane; i < count; i += 32) bad = bad || par[i] < -1 || par[i] >= i;
+        __syncwarp();  // the piece before has read its parents
+        for (int i = lane; i < count; i += 32) {
+          par[i] = a.parents[(int64_t)b * a.tokens + i];
+          bad = bad || par[i] < -1 || par[i] >= i;
+        }
+        __syncwarp();
         bad = __any_sync(0xffffffffu, bad);
         if (bad && aid == 0) atomicExch(a.err, kDevErrBounds);
       }
@@ -594,38 +605,55 @@ __global__ void __launch_bounds__(kAtThreads, 1)
           // A value row that some of the rows do not see must not reach them
           // even if it is infinite or not a number (0 x inf): rows behind the
           // last key are cleared, others that hold such a value as well, and
-          // added by hand below where they are seen.
+          // added by hand below where they are seen.  Each half looks after
+          // the rows of its own product, so the halves go on taking turns.
           const int pos = pos0 + v_pos(i, n);
           uint8_t* vs = smem + F::kOffRing + (pos % F::kSlots) * F::kTile;
           ok = ok && mbar_wait_bounded(full(pos % F::kSlots), (pos / F::kSlots) & 1, abort_flag, a.err);
           ok = __all_sync(0xffffffffu, ok);
-          const int have = min(kKeys, nw ? count : len - k0);
-          auto chunk = [&](int r, int c) {
-            return reinterpret_cast<uint4*>(vs + (c >> 3) * F::kBox + r * 128 + (((c & 7) ^ (r & 7)) << 4));
-          };
+          const int have = min(kKeys, nw ? count : len - k0), hidden = nw ? 0 : min(have, max(0, lim_min - k0));  // from there on, from some rows
+          // this thread's 16-byte chunks: one column of them, kStep rows apart (a
+          // multiple of the swizzle's eight, so that they lie a constant apart)
+          constexpr int kMine = 64 * (D / 8) / 128, kStep = 128 / (D / 8);
+          const int c0 = aid & 127, r0 = half * 64 + c0 / (D / 8), x0 = c0 % (D / 8);
+          uint8_t* mine = vs + (x0 >> 3) * F::kBox + r0 * 128 + (((x0 & 7) ^ (r0 & 7)) << 4);
+          const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+          // (two buffers: a warp may look through the next tile's rows while
+          // another still reads what was found in this one's; the tile after
+          // that starts once every warp has handed over this one's P)
+          uint32_t* odd_now = odd_rows + 4 * (g & 1);
           if (ok) {
-            for (int c = aid; c < kKeys * (D / 8); c += kSoftThreads) {
-              const int r = c / (D / 8);
-              uint4* at = chunk(r, c % (D / 8));
-              if (r >= have) {
-                *at = make_uint4(0u, 0u, 0u, 0u);
-              } else {
-                const uint4 v = *at;
-                if (odd_pair<T>(v.x) || odd_pair<T>(v.y) || odd_pair<T>(v.z) || odd_pair<T>(v.w)) atomicOr(&odd_rows[r >> 5], 1u << (r & 31));
+            if (hidden < have) {
+              uint4 v[kMine];
+              uint32_t found = 0;
+#pragma unroll
+              for (int u = 0; u < kMine; ++u) v[u] = *reinterpret_cast<const uint4*>(mine + u * kStep * 128);
+#pragma unroll
+              for (int u = 0; u < kMine; ++u) found |= odd_chunk<T>(v[u]) ? 1u << u : 0u;
+              if (found) {
+#pragma unroll 1
+                for (int u = 0; u < kMine; ++u) {
+                  const int r = r0 + u * kStep;
+                  if (found >> u & 1u && r >= hidden && r < have) atomicOr(&odd_now[r >> 5], 1u << (r & 31));
+                }
+              }
+            }
+#pragma unroll
+            for (int u = 0; u < kMine; ++u)
+              if (r0 + u * kStep >= have) *reinterpret_cast<uint4*>(mine + u * kStep * 128) = none;
+          }
+          if (hidden < have) {
+            half_sync();
+            odd = odd_now[2 * half] | odd_now[2 * half + 1];
+            if (odd) {
+#pragma unroll 1
+              for (int u = 0; u < kMine; ++u) {
+                const int r = r0 + u * kStep;
+                if (odd_now[r >> 5] >> (r & 31) & 1u) *reinterpret_cast<uint4*>(mine + u * kStep * 128) = none;
               }
             }
           }
-          all_sync();
-          odd = odd_rows[0] | odd_rows[1] | odd_rows[2] | odd_rows[3];
-          if (odd) {
-#pragma unroll 1
-            for (int c = aid; c < kKeys * (D / 8); c += kSoftThreads) {
-              const int r = c / (D / 8);
-              if (odd_rows[r >> 5] >> (r & 31) & 1u) *chunk(r, c % (D / 8)) = make_uint4(0u, 0u, 0u, 0u);
-            }
-          }
           fence_proxy_async_smem();  // V is read by the tensor cores (async proxy)
-          all_sync();                // by either half's product
         }
         if (ok) {
           if (works) {
@@ -648,12 +676,13 @@ __global__ void __launch_bounds__(kAtThreads, 1)
           if (lane == 0) mbar_arrive(p_full(half, g));
         }
         if (odd) {
+          uint32_t* odd_now = odd_rows + 4 * (g & 1);
           ok = ok && mbar_wait_bounded(o_full(half), g & 1, abort_flag, a.err);
           ok = __all_sync(0xffffffffu, ok);
           tc_fence_after();
 #pragma unroll 1
           for (int j = half * 64; j < half * 64 + 64; ++j) {
-            if (!(odd_rows[j >> 5] >> (j & 31) & 1u)) continue;
+            if (!(odd_now[j >> 5] >> (j & 31) & 1u)) continue;
             const int rel = j - kofs;
             if (rel >= 0 && rel < NK && ok && works) {  // (the same for all lanes of a warp)
               float pj = 0.f;
@@ -681,9 +710,9 @@ __global__ void __launch_bounds__(kAtThreads, 1)
             }
             tc_fence_after();
           }
-          all_sync();  // everyone has read the odd rows
-          if (aid < 4) odd_rows[aid] = 0;
-          all_sync();
+          half_sync();  // everyone has read the odd rows
+          if ((aid & 127) < 2) odd_now[2 * half + (aid & 127)] = 0;
+          half_sync();
         }
       }
       // ---- the piece's results: a thread joins the two halves of its row in
@@ -731,7 +760,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
 #pragma unroll
             for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(stage + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
           }
-          all_sync();
+          copy_sync();
           if (rep == 0) {
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
@@ -742,7 +771,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
               o[e + 3] += x.w;
             }
           }
-          all_sync();
+          copy_sync();
         }
         if (!works || (REP == 2 && rep == 1)) continue;  // (the same for all lanes of a warp)
         if (whole) {
