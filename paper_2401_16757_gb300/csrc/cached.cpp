@@ -53,8 +53,8 @@ CachedPlan cached_plan(const CachedArgs& a) {
     // A CTA per unit, or equal runs of all tiles and a join.  From two units
     // per SM on the block scheduler evens out what the runs would (512 units
     // of up to 33 tiles: 275 against 283 us); below that the join's 8 us decide:
-    // 32 units of 5 tiles 14.9 against 18.4 us, 4 units of 1025 tiles about 1000
-    // against 50.
+    // 32 units of 5 tiles 14.9 against 18.4 us (13.2 now), 4 units of 1025 tiles
+    // about 1000 against 41.
     const int ctas = run_ctas(a.kv_heads);
     const double alone = std::ceil((double)units / kSms) * (kUnitUs + tiles * kTileUs);
     const double shared = kUnitUs + std::max(2.0, units * tiles / ctas) * kTileUs + (double)units / ctas + kJoinUs;

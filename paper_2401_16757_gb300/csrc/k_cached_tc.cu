@@ -31,8 +31,22 @@
 // units.  Every wait is bounded: on timeout the kernel records kDevErrTimeout,
 // drains the loads and MMAs it started, frees TMEM and returns.
 //
-// What bounds it (GB300, cache out of L2): 12 sequences x 8 key heads (group 4)
-// x 64 nodes on 1100 to 1600 rows each of 128 wide bf16 heads: PERF_TREE_BATCH
+// Measured, caches larger than L2: 32 sequences x 8 key heads (group 4) of 128
+// wide bf16 heads on up to 8000 rows (0.72 GB): 16 nodes 121 us, 5.9 TB/s; 24
+// nodes 128, 5.6; 64 nodes 227 and 128 nodes 388, 0.62 and 0.75 PFLOP/s (the
+// second product of P not counted).  1000 queries on 4096 rows, 2 sequences x 32
+// heads, f16: 126 us, 0.71 PFLOP/s.  One sequence of 131001 rows, 4 key heads of
+// 64 wide f16, 52 rows: 41 us, of which the join and a unit's start and end are
+// 15.  32 heads x 64 nodes on 511 rows: 13.2 us.
+// Up to about 100 rows per unit DRAM bounds it, beyond that the softmax warps: a
+// tile of 128 x 128 takes them about 2500 cycles (1265 for exponentials and the
+// two parts of P, 350 for the maximum, 320 to store P, 170 to load S, the rest
+// waits), two warps per scheduler, which issue in 0.43 of the cycles.  Four
+// threads per row (16 warps of 104 registers) were slower: 32 keys per thread
+// leave few independent exponentials, and the two threads of a half have to
+// agree on the maximum.  One softmax for all 128 keys of a row, its two threads
+// exchanging maxima, took 182 us where a softmax per half took 163 (24 nodes, as
+// above, in an earlier form).
 #include <algorithm>
 #include <cstring>
 #include <string>
@@ -67,7 +81,7 @@ template <int D> struct TcCfg {
   static constexpr int kHalves = D / 64;             // 64-dim boxes of a tile
   static constexpr int kBox = 128 * 128;             // bytes of a 128-row x 64-element box
   static constexpr int kTile = kHalves * kBox;
-  static constexpr int kSlots = D == 128 ? 5 : 8;
+  static constexpr int kSlots = D == 128 ? 5 : 8;    // what shared memory holds, up to eight
   static constexpr int kOffQ = 0;
   static constexpr int kOffRing = kTile;
   static constexpr int kOffX = kOffRing + kSlots * kTile;   // (m, l) of every thread
@@ -834,6 +848,13 @@ __global__ void __launch_bounds__(kAtThreads, 1)
 // per key (their sums meet in shared memory).  Two CTAs share an SM: one's
 // start and waits are the other's time.  Rows of a list are fetched one query
 // at a time.
+// Measured: 32 sequences of 8 key heads (group 4), 1 to 8 listed queries on
+// up to 8000 rows (0.37 GB): 66 us, 5.5 TB/s; 1000 queries on 4096 rows, 2 x 32
+// heads, f16: 89 us, 0.50 PFLOP/s; 512 queries x 32 heads on themselves: 8.3 us.
+// Few rows are bound by reading the keys, many by the sum warps: about 1450
+// cycles for 128 x 128 scores on an SM, of which the exponentials' unit is busy
+// for 1024 (16 a cycle).  Warp products (16 rows each) in its place took 119 us
+// for 4 listed rows where this takes 64, so it serves every count of rows.
 template <int D> struct WtCfg {
   static constexpr int kHalves = D / 64;
   static constexpr int kBox = 128 * 128;
