@@ -30,18 +30,22 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 
 constexpr int kEvThreads = 1024;
 constexpr int kEvTile = 4 * kEvThreads;
+constexpr int kEvBins = 2 * kEvThreads;
 
 // One CTA per (sequence, key head): the rows to keep, in row order, into
 // kept; their weights to weights_out.  The candidates (all rows but the first
 // `sink` and the last `recent`) give `need` rows: the need-th largest key by
-// four histogram passes over its bytes, then one pass in row order that takes
-// every larger key and the first of the equal ones.  Bound by the latency of
-// its passes (the weights are in L2 from the second on): 21 us for 256 pairs of
-// up to 8001 rows, 2 CTAs per SM; keys kept in registers between the passes took
-// the same.
+// three histogram passes over 11, 11 and 10 of its bits, then one pass in row
+// order that takes every larger key and the first of the equal ones.  About 20
+// us for 256 pairs of up to 8001 rows, two CTAs per SM: the first round trip (1.7
+// us), three passes of 1 to 2 us with their sums, and 4 us of the last pass's
+// instructions; the weights are read again from L1 and L2, and keeping the keys
+// in registers between the passes took the same, as did four passes over bytes
+// (0.6 us more).
 __global__ void __launch_bounds__(kEvThreads) evict_select_kernel(const __grid_constant__ EvictArgs a) {
-  __shared__ uint32_t hist[256];
+  __shared__ uint32_t hist[kEvBins];
   __shared__ uint32_t sh_prefix, sh_need, wtot[32];
+  pdl_launch_dependents();  // (the rows' kernel may take its place on idle SMs; it waits for this one's end)
   const int kvh = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int len = a.lens[b * a.lens_step];
   if (len < 0 || len > a.max_seq) {
@@ -56,48 +60,45 @@ __global__ void __launch_bounds__(kEvThreads) evict_select_kernel(const __grid_c
   if (kvh == 0 && tid == 0 && a.lens_out) a.lens_out[b] = keep;
   const int c0 = len > keep ? a.sink : len, c1 = len > keep ? len - a.recent : len;  // candidates [c0, c1)
   uint32_t need = len > keep ? keep - a.sink - a.recent : 0, prefix = 0;
-  if (c0 < c1) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < 256; i += kEvThreads) hist[i] = 0;
+  if (need == 0) {
+    prefix = 0xffffffffu;  // nothing but the protected rows
+  } else {
+    for (int shift = 21; shift >= 0; shift = shift == 10 ? 0 : shift - 11) {  // bits 31..21, 20..10, 9..0
+      const uint32_t mask = shift == 0 ? 1023u : kEvBins - 1;
+      const int known = shift == 21 ? 32 : shift == 10 ? 21 : 10;  // bits above are the prefix's
+      hist[tid] = hist[tid + kEvThreads] = 0;
       __syncthreads();
       for (int j = c0 + tid; j < c1; j += kEvThreads) {
         const uint32_t key = weight_key(w[j]);
-        if (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(key >> shift) & 255u], 1u);
+        if (known == 32 || key >> known == prefix >> known) atomicAdd(&hist[(key >> shift) & mask], 1u);
       }
       __syncthreads();
-      if (warp == 0) {  // from the largest byte down: 8 per lane
-        uint32_t h[8], sum = 0;
+      // from the largest bin down, two per thread
+      const uint32_t top = kEvBins - 1 - 2 * tid, h0 = hist[top], h1 = hist[top - 1];
+      uint32_t scan = h0 + h1;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          h[i] = hist[255 - (lane * 8 + i)];
-          sum += h[i];
-        }
-        uint32_t before = sum;
+      for (int off = 1; off < 32; off <<= 1) {
+        const uint32_t o = __shfl_up_sync(0xffffffffu, scan, off);
+        if (lane >= off) scan += o;
+      }
+      if (lane == 31) wtot[warp] = scan;
+      __syncthreads();
+      uint32_t ws = wtot[lane];
+      const uint32_t own = ws;
 #pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-          const uint32_t o = __shfl_up_sync(0xffffffffu, before, off);
-          if (lane >= off) before += o;
-        }
-        before -= sum;
-        if (before < need && need <= before + sum) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            if (before < need && need <= before + h[i]) {
-              sh_prefix = prefix | (uint32_t)(255 - (lane * 8 + i)) << shift;
-              sh_need = need - before;
-            }
-            before += h[i];
-          }
-        }
-        if (need == 0 && lane == 0) {  // nothing but the protected rows
-          sh_prefix = 0xffffffffu;
-          sh_need = 0;
-        }
+      for (int off = 1; off < 32; off <<= 1) {
+        const uint32_t o = __shfl_up_sync(0xffffffffu, ws, off);
+        if (lane >= off) ws += o;
+      }
+      const uint32_t before = __shfl_sync(0xffffffffu, ws - own, warp) + scan - h0 - h1;
+      if (before < need && need <= before + h0 + h1) {
+        const bool second = need > before + h0;
+        sh_prefix = prefix | (second ? top - 1 : top) << shift;
+        sh_need = need - before - (second ? h0 : 0);
       }
       __syncthreads();
       prefix = sh_prefix;
       need = sh_need;
-      if (need == 0) break;
     }
   }
   // keys above `prefix` are taken, and the first `need` equal ones
