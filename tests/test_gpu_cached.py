@@ -308,6 +308,44 @@ def test_later_rows_that_are_not_numbers():
         assert not torch.any(torch.isfinite(c.out[before:]))
 
 
+@pytest.mark.parametrize("draft,tokens,cap", [(False, 300, 700), (False, 300, 5000), (False, 12, 700), (True, 128, 700), (True, 100, 5000)])
+def test_values_that_are_not_numbers_in_many_tiles(draft, tokens, cap):
+    """Several such rows, in both halves of neighbouring key tiles: the elements and the queries that none of them reaches keep
+    their bits or their value, the others are not finite, on every one of many runs."""
+    torch = _torch()
+    n, h, kv, d = 3, 8, 2, 128
+    g = torch.Generator().manual_seed(tokens)
+    lens = [cap - 1, cap // 2, tokens + 3]
+    k, v = (torch.randn(n, cap, kv * d, generator=g).bfloat16().cuda() for _ in range(2))
+    q = torch.randn(n * tokens, h * d, generator=g).bfloat16().cuda()
+    kn, vn = (torch.randn(n * tokens, kv * d, generator=g).bfloat16().cuda() for _ in range(2))
+    par = np.tile(np.arange(-1, tokens - 1, dtype=np.int32), (n, 1))  # a chain, so that what is seen is a range
+    par, dl = torch.from_numpy(par).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda")
+    x = (kn, vn, par) if draft else (None, None, None)
+    clean = _attend(q, k.data_ptr(), v.data_ptr(), *x, dl, n, tokens, h, kv, d, cap)
+    bad = sorted({min(tokens - 1, i) for i in (3, 5, 60, 70, 71, 99, 127, 130, 200, 290)})
+    for b in range(n):
+        for i, at in enumerate(bad):
+            (vn[b * tokens + at] if draft else v[b, lens[b] - tokens + at])[7 + 128 * (i % 2)] = float("nan") if i % 3 else float("inf")
+    first = [min((at for i, at in enumerate(bad) if i % 2 == s), default=tokens) for s in range(2)]
+    want = clean[0].view(n, tokens, kv, h // kv, d)
+    got = None
+    for _ in range(20):
+        run = _attend(q, k.data_ptr(), v.data_ptr(), *x, dl, n, tokens, h, kv, d, cap)
+        assert got is None or all(torch.equal(torch.nan_to_num(a, 77.0), torch.nan_to_num(b, 77.0)) for a, b in zip(run, got))
+        got = run
+    out = got[0].view(n, tokens, kv, h // kv, d)
+    assert torch.equal(got[1], clean[1])  # scores have nothing to do with it
+    assert torch.equal(out[:, :bad[0]], want[:, :bad[0]])
+    for s in range(2):
+        assert not torch.any(torch.isfinite(out[:, first[s]:, s, :, 7])) and torch.all(torch.isfinite(out[:, :first[s], s]))
+    keep = torch.ones(d, dtype=torch.bool, device="cuda")
+    keep[7] = False
+    # a row added by hand in fp32 in place of two products: a rounding of the result to either side, and 2^-13 of values of up to 4
+    a, b = out[..., keep].double(), want[..., keep].double()
+    assert torch.all((a - b).abs() <= 2.0 ** -7 * b.abs() + 2.0 ** -11)
+
+
 def test_sequences_out_of_range_are_left_alone():
     """Bad lengths, counts and parents: that sequence's outputs stay, the others are right, and the next sync reports it."""
     torch = _torch()
