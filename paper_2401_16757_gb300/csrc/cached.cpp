@@ -285,7 +285,6 @@ int swapnet_cache_evict(const swapnet_cache_eviction* c, swapnet_stream stream) 
     if (!c->k || !c->v || !c->weights || !c->lens || !c->k_out || !c->v_out || !c->weights_out || !c->kept || !c->lens_out)
       SN_FAIL(SWAPNET_ERR_INVALID_ARG, "eviction: null pointer");
     const int64_t width = (int64_t)c->kv_heads * c->head_dim;
-    a.dtype = c->dtype;
     a.n_seq = c->n_seq;
     a.kv_heads = c->kv_heads;
     a.dim = c->head_dim;

@@ -67,7 +67,7 @@ int launch_weights(const CachedArgs& a, int splits, bool early, cudaStream_t s);
 int weights_splits(const CachedArgs& a);
 
 struct EvictArgs {
-  int dtype, n_seq, kv_heads, dim, max_seq, keep, recent, sink, out_seq;
+  int n_seq, kv_heads, dim, max_seq, keep, recent, sink, out_seq;
   int64_t kv_stride, seq_stride, out_stride, out_seq_stride;
   const void *k, *v;
   void *k_out, *v_out;

@@ -2029,7 +2029,6 @@ int swapnet_engine_evict(swapnet_engine* e, int32_t keep, int32_t recent, int32_
     CU(cudaSetDevice(e->device), "cudaSetDevice");
     EvictArgs a;
     std::memset(&a, 0, sizeof(a));
-    a.dtype = m.dtype;
     a.n_seq = st.layers;
     a.kv_heads = st.heads;
     a.dim = st.width / st.heads;
