@@ -1159,8 +1159,9 @@ int rows_map(CUtensorMap* m, const CachedArgs& a, const void* base, int64_t rows
 // begins one.  A CTA holds at most two pieces that are not whole units: the
 // rest of one that began before its run (slot 2 c) and the start of one that
 // goes on behind it (slot 2 c + 1).  A warp per row, or all eight warps of the
-// block where a unit has many pieces; loads of four pieces at a time.
-constexpr int kRjWarps = 8, kRjMany = 8;
+// block where that takes fewer rounds of loads, each of four pieces (a unit of
+// hundreds of pieces, or a block per row).
+constexpr int kRjWarps = 8;
 template <typename T>
 __global__ void __launch_bounds__(32 * kRjWarps)
     attention_runs_join_kernel(const __grid_constant__ CachedArgs a, int queries, int row_tile) {
@@ -1171,7 +1172,8 @@ __global__ void __launch_bounds__(32 * kRjWarps)
   const int4 u = a.units[c];
   if (u.w == 0) return;
   const int b = u.x, t0 = u.y * queries, kvh = u.z & 0xffff, rows = u.z >> 16, pieces = u.w;
-  const bool many = pieces > kRjMany;
+  const int blocks = gridDim.x, per_warp = (rows + kRjWarps * blocks - 1) / (kRjWarps * blocks), per_block = (rows + blocks - 1) / blocks;
+  const bool many = per_block * ((pieces + 4 * kRjWarps - 1) / (4 * kRjWarps) + 1) < per_warp * ((pieces + 3) / 4);  // (+ 1: the warps' results meet)
   const int V = a.dim / 4, first = many ? warp : 0, step = many ? kRjWarps : 1;
   const float2* ml = reinterpret_cast<const float2*>(a.ml);
   const float4* part = reinterpret_cast<const float4*>(a.part);
@@ -1262,9 +1264,12 @@ template <typename T, int D, int REP> int rows_t(const CachedArgs& a, bool early
   cfg.numAttrs = early ? 1 : 0;
   rc = done(cudaLaunchKernelEx(&cfg, kern, q, k, v, kn, vn, a, queries, nrt), "cached attention launch");
   if (rc || a.splits == 1) return rc;
-  // a row per warp of at most 128; where few units have many pieces, a block per row
-  const int64_t units = (int64_t)a.n_seq * nrt * a.kv_heads;
-  cfg.gridDim = dim3(units <= ctas / kRjMany ? std::min(queries * a.group, 64) : (queries * a.group + kRjWarps - 1) / kRjWarps, ctas);
+  // eight blocks per SM that find work, but at least a warp and at most a block
+  // for a row (20 units of 28 tiles and 48 rows, up to 9 pieces each: 37.6 us
+  // with 6 blocks for a unit's rows, 25.5 with 48)
+  const int64_t units = std::min<int64_t>((int64_t)a.n_seq * nrt * a.kv_heads, ctas);
+  const int rows = queries * a.group, least = (rows + kRjWarps - 1) / kRjWarps;
+  cfg.gridDim = dim3(std::min(rows, std::max(least, (int)(8 * kSms / units))), ctas);
   cfg.blockDim = dim3(32 * kRjWarps);
   cfg.dynamicSmemBytes = 0;
   cfg.numAttrs = 1;
