@@ -691,7 +691,14 @@ __global__ void __launch_bounds__(kAtThreads, 1)
         }
         if (odd) {
           uint32_t* odd_now = odd_rows + 4 * (g & 1);
-          ok = ok && mbar_wait_bounded(o_full(half), g & 1, abort_flag, a.err);
+          // O is at rest once this tile's product is done.  A parity cannot tell
+          // phase g from phase g - 2, so phase g - 1 has to be known complete
+          // before phase g is waited for: a piece's first tile has it from the
+          // o_done of the piece before; for the others these scores only prove
+          // phase g - 2 (they were issued before the product of g - 1, behind
+          // that of g - 2), which is what makes the wait for g - 1 safe in turn.
+          ok = ok && (i == 0 || mbar_wait_bounded(o_full(half), (g - 1) & 1, abort_flag, a.err)) &&
+               mbar_wait_bounded(o_full(half), g & 1, abort_flag, a.err);
           ok = __all_sync(0xffffffffu, ok);
           tc_fence_after();
 #pragma unroll 1

@@ -41,3 +41,20 @@ def test_rotation_releases_the_attention_after_its_wait():
     launch = text[text.index("int launch_attention("):]
     between = launch[launch.index("rope_append_kernel<T, 1, 1>"):launch.index("attention_split_kernel<T>, static_cast")]
     assert between.count("launch_pdl(") == 0 and between.count("launch_attention_tc(") == 1
+
+
+def _text(name):
+    return re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, name)).read())
+
+
+def test_no_wait_for_a_phase_while_the_one_before_may_be_open():
+    """A parity wait for phase g returns at once while phase g - 1 is still open.  The products of a half complete its
+    o_full phase tile by tile; a softmax warp that did not wait for phase g - 1 waits for it before it waits for phase g."""
+    body = next(body for _, head, body in _kernels() if "attention_rows_kernel" in head)
+    waits = list(re.finditer(r"mbar_wait_bounded\(o_full\(half\), (\(g - 1\) & 1|g & 1)", body))
+    assert waits
+    for i, w in enumerate(waits):
+        if w.group(1) == "g & 1":
+            assert i > 0 and waits[i - 1].group(1) == "(g - 1) & 1"
+            between = body[waits[i - 1].end():w.start()]
+            assert ";" not in between and "{" not in between  # one condition: the first has to hold for the second
