@@ -743,7 +743,9 @@ __global__ void __launch_bounds__(kAtThreads, 1)
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
       ml[half * 128 + slot] = make_float2(m, l);
+      tc_fence_before();  // (values that this half's warps added to its O by hand, which the other half's read below)
       if (REP == 1) row_sync(); else all_sync();
+      tc_fence_after();
       float M = -INFINITY, L = 0.f, f[2];
 #pragma unroll
       for (int u = 0; u < 2 * REP; ++u) M = fmaxf(M, ml[u * kRowsMax + row].x);  // (half-major, then the copies of the rows)

@@ -58,3 +58,13 @@ def test_no_wait_for_a_phase_while_the_one_before_may_be_open():
             assert i > 0 and waits[i - 1].group(1) == "(g - 1) & 1"
             between = body[waits[i - 1].end():w.start()]
             assert ";" not in between and "{" not in between  # one condition: the first has to hold for the second
+
+
+def test_outputs_in_tensor_memory_pass_a_fenced_barrier_between_the_halves():
+    """A softmax warp may have changed its half's outputs in tensor memory by hand; the other half's warps read them behind
+    a barrier, which orders tensor memory only with a fence on either side."""
+    body = next(body for _, head, body in _kernels() if "attention_rows_kernel" in head)
+    at = body.index("ml[half * 128 + slot] = make_float2(m, l);")
+    behind = body[at:body.index("tmem_ld_32x32b_x32", at)]
+    barrier = re.search(r"if \(REP == 1\) row_sync\(\); else all_sync\(\);", behind)
+    assert "tc_fence_before()" in behind[:barrier.start()] and "tc_fence_after()" in behind[barrier.end():]
