@@ -297,7 +297,6 @@ __global__ void __launch_bounds__(kAtThreads, 1)
     tmem_relinquish();
   }
   pdl_wait();
-  pdl_launch_dependents();
   Cursor cur;
   cur.next = 0;
   const int kvh = blockIdx.x % a.kv_heads, run = blockIdx.x / a.kv_heads;
@@ -375,6 +374,9 @@ __global__ void __launch_bounds__(kAtThreads, 1)
   __syncthreads();  // (and sched is written again, as ml)
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  // (not before this CTA has its TMEM: a kernel that starts early may hold some
+  // while it waits for this one's end)
+  pdl_launch_dependents();
   // a piece's tiles in the order of use: K0, K1, V0, K2, V1, ..., V(n-1)
   auto k_pos = [&](int i) { return i == 0 ? 0 : 2 * i - 1; };
   auto v_pos = [&](int i, int n) { return i == n - 1 ? 2 * n - 1 : 2 * i + 2; };
@@ -902,7 +904,6 @@ __global__ void __launch_bounds__(kTcThreads, 2)
   // (the tiles that most rows see start first)
   const int kvh = blockIdx.x, b = blockIdx.y, split = blockIdx.z;
   pdl_wait();
-  pdl_launch_dependents();
   int len, count;
   if (!seq_sizes(a, b, &len, &count)) return;
   const int ktiles = (len + kKeys - 1) / kKeys, nrt = (count + queries - 1) / queries;
@@ -940,6 +941,7 @@ __global__ void __launch_bounds__(kTcThreads, 2)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  pdl_launch_dependents();  // (this CTA has its TMEM, see above)
 
   if (warp == 0) {
     if (nrt > 0 && elect_one()) {

@@ -68,3 +68,18 @@ def test_outputs_in_tensor_memory_pass_a_fenced_barrier_between_the_halves():
     behind = body[at:body.index("tmem_ld_32x32b_x32", at)]
     barrier = re.search(r"if \(REP == 1\) row_sync\(\); else all_sync\(\);", behind)
     assert "tc_fence_before()" in behind[:barrier.start()] and "tc_fence_after()" in behind[barrier.end():]
+
+
+def test_dependents_start_only_once_a_kernel_holds_its_tensor_memory():
+    """Tensor memory is allocated by waiting until an SM has enough of it.  A kernel launched behind another may start as soon
+    as that one's CTAs have released it, and may then hold tensor memory while it waits for that one's end: a CTA that
+    releases it before its own allocation could wait for that memory for ever."""
+    seen = 0
+    for name, head, body in _kernels():
+        if "tmem_alloc(" not in body or "pdl_launch_dependents()" not in body:
+            continue
+        seen += 1
+        assert body.index("tmem_alloc(") < body.index("= *tmem_slot;") < body.index("pdl_launch_dependents()"), (name, head)
+        between = body[body.index("tmem_alloc("):body.index("= *tmem_slot;")]
+        assert "__syncthreads()" in between, (name, head)
+    assert seen >= 6
