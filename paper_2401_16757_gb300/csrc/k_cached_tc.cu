@@ -880,7 +880,7 @@ template <int D> struct WtCfg {
 constexpr int kSBufs = 2;
 constexpr uint32_t kWtTmemCols = 256;  // two CTAs share the SM's 512
 
-template <typename T, int D>
+template <typename T, int D, bool LIST>
 __global__ void __launch_bounds__(kTcThreads, 2)
     weights_rows_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                         const __grid_constant__ CachedArgs a, int queries) {
@@ -899,6 +899,9 @@ __global__ void __launch_bounds__(kTcThreads, 2)
   const uint32_t done_bar = smem_u32(bars + 20);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 21);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 22);
+  // [2][4]: of a tile of listed rows, a bit per row that is none: the scores
+  // there are another query's, which may be unused and hold anything
+  uint32_t* none_rows = reinterpret_cast<uint32_t*>(bars + 24);
 
   const int warp = warp_index(), lane = threadIdx.x & 31;
   // (the tiles that most rows see start first)
@@ -949,7 +952,7 @@ __global__ void __launch_bounds__(kTcThreads, 2)
       auto load_q = [&](int rt, int slot) {
         const int t0 = rt * queries;
         const uint32_t dst = smem_u32(smem_q + slot * F::kTile);
-        if (!a.rows) {
+        if (!LIST) {
           mbar_arrive_expect_tx(q_full(slot), F::kHalves * queries * a.group * 128);
 #pragma unroll
           for (int h = 0; h < F::kHalves; ++h)
@@ -1045,10 +1048,14 @@ __global__ void __launch_bounds__(kTcThreads, 2)
         const int t = rt * queries + row_q;
         bool have = row_q < queries && t < count;
         int q = t;
-        if (have && a.rows) {
+        if (LIST && have) {
           q = a.rows[(int64_t)b * a.rows_step + t];
           have = q >= 0 && q < a.tokens;
           if (!have) atomicExch(a.err, kDevErrBounds);
+        }
+        if (LIST) {
+          const uint32_t none = __ballot_sync(0xffffffffu, !have && row_q < queries && t < count);
+          if (lane == 0) none_rows[buf * 4 + (aid >> 5)] = none;
         }
         if (have)
           asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(lse + buf * 128 + aid)), "l"(row_lse + q) : "memory");
@@ -1084,6 +1091,8 @@ __global__ void __launch_bounds__(kTcThreads, 2)
           const int ahead = kt * kKeys - (len - count) - rt * queries;
           const int low = (ahead + slot) * a.group, low_all = (ahead + kKeys - 1) * a.group;
           const uint32_t tS = tmem + (uint32_t)sb * 128u + lane_off;
+          const uint32_t* none = none_rows + buf * 4;
+          const bool some_none = LIST && (none[0] | none[1] | none[2] | none[3]);
 #pragma unroll
           for (int c2 = 0; c2 < 4; c2 += 2) {  // two of the half's chunks of 16 rows at a time
             uint32_t s[2][16];
@@ -1116,6 +1125,14 @@ __global__ void __launch_bounds__(kTcThreads, 2)
                   const int r = c0 + 2 * e;
                   if (r < low || r >= rows) p[e].x = 0.f;
                   if (r + 1 < low || r + 1 >= rows) p[e].y = 0.f;
+                }
+              }
+              if (some_none) {
+                const uint32_t here = none[c0 >> 5] >> (c0 & 31);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                  if (here >> (2 * e) & 1u) p[e].x = 0.f;
+                  if (here >> (2 * e + 1) & 1u) p[e].y = 0.f;
                 }
               }
 #pragma unroll
@@ -1290,9 +1307,9 @@ template <typename T, int D> int rows_d(const CachedArgs& a, bool early, cudaStr
   return a.tokens * a.group <= 64 ? rows_t<T, D, 2>(a, early, s) : rows_t<T, D, 1>(a, early, s);
 }
 
-template <typename T, int D> int weights_t(const CachedArgs& a, int splits, bool early, cudaStream_t s) {
+template <typename T, int D, bool LIST> int weights_t(const CachedArgs& a, int splits, bool early, cudaStream_t s) {
   static std::atomic<uint64_t> known{0};
-  const auto kern = weights_rows_kernel<T, D>;
+  const auto kern = weights_rows_kernel<T, D, LIST>;
   if (attr_needed(known)) {
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, WtCfg<D>::kSmem);
     if (e != cudaSuccess) return done(e, "cache weights: shared memory");
@@ -1300,7 +1317,7 @@ template <typename T, int D> int weights_t(const CachedArgs& a, int splits, bool
   }
   const int queries = std::min(128 / a.group, a.tokens);
   CUtensorMap q, k;
-  int rc = query_map(&q, a, a.rows ? 1 : queries);
+  int rc = query_map(&q, a, LIST ? 1 : queries);
   if (!rc) rc = rows_map(&k, a, a.k, a.max_seq, a.kv_stride, a.seq_stride);
   if (rc) return rc;
   cudaLaunchConfig_t cfg;
@@ -1316,13 +1333,16 @@ template <typename T, int D> int weights_t(const CachedArgs& a, int splits, bool
   cfg.numAttrs = early ? 1 : 0;
   return done(cudaLaunchKernelEx(&cfg, kern, q, k, a, queries), "cache weights launch");
 }
+template <typename T, int D> int weights_d(const CachedArgs& a, int splits, bool early, cudaStream_t s) {
+  return a.rows ? weights_t<T, D, true>(a, splits, early, s) : weights_t<T, D, false>(a, splits, early, s);
+}
 
 }  // namespace
 
 int launch_weights(const CachedArgs& a, int splits, bool early, cudaStream_t s) {
   if (a.dtype == SWAPNET_BF16)
-    return a.dim == 128 ? weights_t<__nv_bfloat16, 128>(a, splits, early, s) : weights_t<__nv_bfloat16, 64>(a, splits, early, s);
-  return a.dim == 128 ? weights_t<__half, 128>(a, splits, early, s) : weights_t<__half, 64>(a, splits, early, s);
+    return a.dim == 128 ? weights_d<__nv_bfloat16, 128>(a, splits, early, s) : weights_d<__nv_bfloat16, 64>(a, splits, early, s);
+  return a.dim == 128 ? weights_d<__half, 128>(a, splits, early, s) : weights_d<__half, 64>(a, splits, early, s);
 }
 
 int launch_attention_rows(const CachedArgs& a, bool early, cudaStream_t s) {

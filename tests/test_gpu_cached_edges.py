@@ -60,3 +60,59 @@ def test_values_that_are_not_numbers_beside_late_value_tiles(tokens):
         a, b = out[:, bad][..., rest].double(), want[:, bad][..., rest].double()
         assert torch.all((a - b).abs() <= 2.0 ** -7 * b.abs() + 2.0 ** -11)
     _any_engine().sync()  # no wait gave up
+
+
+@pytest.mark.parametrize("heads,kv,dim", [(4, 2, 64), (6, 2, 128), (40, 1, 64)])
+@pytest.mark.parametrize("tokens", [6, 70, 200])
+@pytest.mark.parametrize("unused", [float("nan"), float("inf"), -float("inf"), 1.0])
+def test_listed_rows_out_of_range_add_nothing(heads, kv, dim, tokens, unused):
+    """Entries below 0 and from `tokens` on, among right ones, whatever the first and the last query row hold: the weights are
+    those of the list's other entries at their places, and the entry is reported."""
+    torch = _torch()
+    eng = _any_engine()
+    n, cap, count = 2, 300, tokens - 2
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    q = torch.empty(n, tokens, heads * dim, dtype=torch.float16, device="cuda").normal_(generator=g)
+    k = torch.empty(n, cap, kv * dim, dtype=torch.float16, device="cuda").normal_(generator=g)
+    q[:, 0], q[:, -1] = unused, unused  # in use for no entry
+    lens = torch.tensor([cap, max(tokens, 130)], dtype=torch.int32, device="cuda")
+    counts = torch.full((n,), count, dtype=torch.int32, device="cuda")
+    rows = (torch.arange(tokens, device="cuda") + 1).clamp(max=tokens - 2).int().expand(n, tokens).contiguous()
+    wrong = sorted({1, count // 2, count - 1})
+    for b in range(n):
+        for i, at in enumerate(wrong):
+            rows[b, at] = (-1, tokens, -2 ** 31, 2 ** 31 - 1)[(i + b) % 4]
+    group = heads // kv
+    own = torch.arange(heads, device="cuda") // group
+    lse = torch.full((n, heads, tokens), float("nan"), device="cuda")
+    want = torch.zeros(n, kv, cap, dtype=torch.float64, device="cuda")
+    slack = torch.zeros_like(want)
+    for b in range(n):
+        m = int(lens[b])
+        keys = k[b, :m].double().view(m, kv, dim)[:, own]
+        z0 = torch.einsum("ihd,jhd->hij", q[b, 1:-1].double().view(-1, heads, dim), keys) / dim ** 0.5
+        lse[b, :, 1:-1] = torch.logsumexp(z0, -1).float()
+        for i in range(count):
+            r = int(rows[b, i])
+            if i in wrong:
+                continue
+            z = z0[:, r - 1]
+            seen = torch.arange(m, device="cuda") <= m - count + i
+            p = torch.where(seen, torch.exp(z - lse[b, :, r, None].double()), torch.zeros((), dtype=torch.float64, device="cuda"))
+            # a score's sum of dim products in fp32, a step each, and 2^x of it
+            e = dim * 2.0 ** -23 * torch.einsum("hd,jhd->hj", q[b, r].double().abs().view(heads, dim), keys.abs()) / dim ** 0.5
+            want[b, :, :m] += p.view(kv, group, m).sum(1)
+            slack[b, :, :m] += (p * (e + 2.0 ** -20 * (1 + z.abs()))).view(kv, group, m).sum(1)
+    w = torch.full((n, kv, cap), SENT, device="cuda")
+    capi.attention_weights(capi.cached_attention("f16", n, tokens, heads, kv, dim, cap, q=q.data_ptr(), k=k.data_ptr(),
+                                                 lens=lens.data_ptr(), counts=counts.data_ptr(), rows=rows.data_ptr(),
+                                                 lse=lse.data_ptr(), weights=w.data_ptr()), _stream())
+    with pytest.raises(capi.SwapnetError) as x:
+        eng.sync()
+    assert x.value.code == capi.ERR_INVALID_ARG
+    eng.sync()
+    for b in range(n):
+        m = int(lens[b])
+        err = (w[b, :, :m].double() - want[b, :, :m]).abs()
+        assert torch.all(err <= slack[b, :, :m] + (count * group + 4) * 2.0 ** -24 * want[b, :, :m] + 2.0 ** -126)
+        assert torch.all(w[b, :, m:] == SENT)
