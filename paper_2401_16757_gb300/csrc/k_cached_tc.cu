@@ -1089,7 +1089,8 @@ __global__ void __launch_bounds__(kTcThreads, 2)
           // the tile's rows from `low` on see this thread's key; from `low_all`
           // on, all of the tile's keys
           const int ahead = kt * kKeys - (len - count) - rt * queries;
-          const int low = (ahead + slot) * a.group, low_all = (ahead + kKeys - 1) * a.group;
+          // (clamped first: far behind the queries, rows times heads pass 32 bits)
+          const int low = max(ahead + slot, 0) * a.group, low_all = max(ahead + kKeys - 1, 0) * a.group;
           const uint32_t tS = tmem + (uint32_t)sb * 128u + lane_off;
           const uint32_t* none = none_rows + buf * 4;
           const bool some_none = LIST && (none[0] | none[1] | none[2] | none[3]);

@@ -116,3 +116,37 @@ def test_listed_rows_out_of_range_add_nothing(heads, kv, dim, tokens, unused):
         err = (w[b, :, :m].double() - want[b, :, :m]).abs()
         assert torch.all(err <= slack[b, :, :m] + (count * group + 4) * 2.0 ** -24 * want[b, :, :m] + 2.0 ** -126)
         assert torch.all(w[b, :, m:] == SENT)
+
+
+@pytest.mark.parametrize("tokens,group", [(1, 128), (3, 100)])
+def test_weights_of_a_cache_whose_rows_times_heads_pass_32_bits(tokens, group):
+    """Rows times the heads of a group beyond 2^31: every row gets its attention, from the first to the last."""
+    torch = _torch()
+    dim, length = 64, 2 ** 31 // group + 300_001
+    cap = length + 5
+    g = torch.Generator(device="cuda").manual_seed(group)
+    k = torch.empty(cap, dim, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    q = torch.empty(tokens, group * dim, dtype=torch.bfloat16, device="cuda").normal_(0, 0.5, generator=g)
+    rows = q.double().view(tokens * group, dim)
+    step = 1 << 18
+    last = torch.arange(tokens, device="cuda").repeat_interleave(group) + length - tokens  # a row's own cache row
+
+    def scores(j0):
+        z = rows @ k[j0:min(j0 + step, length)].double().T / dim ** 0.5
+        return z.masked_fill(torch.arange(j0, j0 + z.shape[1], device="cuda") > last[:, None], -float("inf"))
+
+    parts = torch.stack([torch.logsumexp(scores(j0), -1) for j0 in range(0, length, step)])
+    lse = torch.logsumexp(parts, 0).float()  # [query, head]
+    lens = torch.tensor([length], dtype=torch.int32, device="cuda")
+    stats = lse.view(tokens, group).T.contiguous()
+    w = torch.full((cap,), SENT, device="cuda")
+    capi.attention_weights(capi.cached_attention("bf16", 1, tokens, group, 1, dim, cap, q=q.data_ptr(), k=k.data_ptr(),
+                                                 lens=lens.data_ptr(), lse=stats.data_ptr(), weights=w.data_ptr()), _stream())
+    assert torch.all(w[length:] == SENT)
+    norm = float(rows.abs().sum(1).max()) * float(k.abs().max()) / dim ** 0.5  # of any score's products
+    for j0 in range(0, length, step):
+        p = torch.exp(scores(j0) - lse[:, None].double())
+        want = p.sum(0)
+        # a score's sum of dim products in fp32, a step each; 2^x of numbers of up to 64; the sum over the rows
+        e = dim * 2.0 ** -23 * norm + 2.0 ** -16 + tokens * group * 2.0 ** -24
+        assert torch.all((w[j0:j0 + p.shape[1]].double() - want).abs() <= e * want), j0
