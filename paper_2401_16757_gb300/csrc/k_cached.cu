@@ -21,6 +21,11 @@ namespace {
 constexpr int kFwWarps = 4, kFwThreads = 32 * kFwWarps;
 constexpr int kGk = 16;      // keys of a group: one step of a warp
 constexpr int kFwStages = 3;
+// log2 of the largest p: fp16 has no step below 2^-24, so that its two parts of
+// p <= 1 would lose the keys below 2^-25 of the largest; with p <= 2^15 a key is
+// off by at most 2^-40.  bf16 has fp32's exponents.  (Part of the reference m, so
+// that it costs one subtraction per row and group.)
+template <typename T> constexpr float kPTop = std::is_same<T, __half>::value ? 15.0f : 0.0f;
 
 template <int D> struct FewCfg {
   static constexpr int kGroup = kGk * D * 2;          // bytes of a group's keys (or values)
@@ -64,7 +69,7 @@ __device__ __forceinline__ void load_queries(const CachedArgs& a, int b, int kvh
 // another warp until the end:
 //   S = Q K^T          8 mma.m16n8k16 a 16 rows for 128 dims
 //   p = 2^(S - m)      handed to the next product as two parts p_hi + p_lo of
-//                      the storage type, about 16 bits of p
+//                      the storage type: 17 bits of p (bf16) or 22 (fp16)
 //   O = O 2^(m' - m) + p V
 // Keys and values pass through a ring of three groups a warp (cp.async; rows
 // behind the sequence's end arrive as zeros, whatever the cache holds there).
@@ -199,7 +204,7 @@ __global__ void __launch_bounds__(kFwThreads, 2) attention_few_kernel(const __gr
     for (int h = 0; h < 2; ++h) {
       float mx = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2)) - kPTop<T>;
       const float mn = fmaxf(m[h], mx);
       base[h] = mn == -INFINITY ? 0.f : mn;  // (nothing seen yet)
       al[h] = ex2(m[h] - base[h]);

@@ -17,13 +17,15 @@
 //                 crosses, p = 2^(s - m) back over the scores as two parts of
 //                 the storage type, p_hi + p_lo: one part would leave 8 (bf16)
 //                 or 11 (fp16) bits of p, less than the fp32 that the sums keep;
-//                 two leave 16 or more, for a second product with V, whose tensor
-//                 time is hidden behind the exponentials
+//                 two leave 17 (bf16) or 22 (fp16, down to its least step, see
+//                 PRange), for a second product with V, whose tensor time is
+//                 hidden behind the exponentials.  A third part has no room:
+//                 TMEM is full with two tiles' scores and both outputs
 //   O_h += P_h V  tcgen05.mma with A = P from TMEM, B = V as loaded (MN-major)
-// O_0 and O_1 stay in TMEM.  m is the running maximum only where that grew by
-// more than 2^8 since it was last taken (kSlack): until then p and l stay
-// within 2^8 of their usual range, which fp32 sums and both storage types hold
-// without loss, and O is neither read nor rescaled.
+// O_0 and O_1 stay in TMEM.  m, the running maximum less a constant, is taken
+// again only where p would pass 2^8 (bf16) or 2^15 (fp16): until then O is
+// neither read nor rescaled, and fp32 holds the sums without loss (PRange: what
+// the parts of p hold).
 // With at most 64 rows (REP 2) the rows appear twice in the MMA's 128, and
 // lanes 0..63 and 64..127 share a thread's keys, so that all warps work (the
 // other 16 keys are zeros in a lane's P).
@@ -69,7 +71,25 @@ constexpr int kAtThreads = 128 + kSoftThreads;
 constexpr int kRegsLow = 72, kRegsHigh = 216;
 static_assert(128 * kRegsLow + kSoftThreads * kRegsHigh <= kAtThreads * 168, "registers of a CTA");
 constexpr int kKeys = 128;       // keys of a tile
-constexpr float kSlack = 8.0f;   // log2 of what p may exceed 1 by
+// Where p lies, in log2: at most kMost (then m is taken again), at first kWide
+// for the largest score so far, from a long piece's tile kTightAt on kTight.
+// bf16 has fp32's exponents.  fp16 has no step below 2^-24, so its p ends at
+// 2^15, and a key is off by at most 2^-32 of the largest p in the wide range,
+// 2^-37 in the tight one: 2^-20 of the values for 4000 keys, the most that stay
+// in the wide range, as for 131072 in the tight one.  The wide range is for the
+// first tiles, whose maxima grow by a few powers of two (us, caches larger
+// than L2, fp16 without shift / 7, 12 from tile 16 on / 13 always: 24 nodes on
+// 32 x 8000 rows 133.9 / 132.7 / 144.2; 1000 queries on 4096 rows, with weights,
+// 212 / 210 / 244; 13 nodes on 131001 rows, 64 wide, 41.1 / 42.7 / 42.8; 200
+// queries on 16 x 9000 rows, 64 wide, 193 / 201 / 224).
+template <typename T> struct PRange {
+  static constexpr float kMost = 8.0f, kWide = 0.0f, kTight = 0.0f;
+  static constexpr int kTightAt = 0;  // (never)
+};
+template <> struct PRange<__half> {
+  static constexpr float kMost = 15.0f, kWide = 7.0f, kTight = 12.0f;
+  static constexpr int kTightAt = 16;
+};
 constexpr uint32_t kTmemCols = 512;
 // TMEM columns: S [0, 128) and [128, 256), each half's P over its scores (hi
 // then lo); O_0 [256, 256 + D), O_1 [384, 384 + D)
@@ -530,7 +550,10 @@ __global__ void __launch_bounds__(kAtThreads, 1)
         bad = __any_sync(0xffffffffu, bad);
         if (bad && aid == 0) atomicExch(a.err, kDevErrBounds);
       }
+      using R = PRange<T>;
       float m = -INFINITY, l = 0.f;  // m: the reference, in log2 units
+      float top = -INFINITY;         // the largest scaled score so far
+      const bool tighten = R::kTightAt > 0 && n >= 2 * R::kTightAt;
       for (int i = 0; i < n; ++i) {
         const int g = g0 + i;
         const bool nw = cur.i0 + i >= np;
@@ -567,12 +590,14 @@ __global__ void __launch_bounds__(kAtThreads, 1)
             for (int k = 0; k < NK; ++k) mx4[k & 3] = fmaxf(mx4[k & 3], __uint_as_float(s[k]));
             mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * a.scale_log2;
           }
-          const bool grow = mx - m > kSlack;  // (also the first key seen)
+          top = fmaxf(top, mx);
+          const bool grow = mx - m > R::kMost || (tighten && i == R::kTightAt && top != -INFINITY);  // (also the first key seen)
           if (__any_sync(0xffffffffu, grow)) {
             float alpha = 1.f;
             if (grow) {
-              alpha = ex2(m - mx);
-              m = mx;
+              const float ref = (R::kTightAt ? top : mx) - (tighten && i >= R::kTightAt ? R::kTight : R::kWide);
+              alpha = ex2(m - ref);
+              m = ref;
               l *= alpha;
             }
             if (i > 0) {  // O is at rest once the product of the tile before is done (the one before that is: these scores came after it)

@@ -150,3 +150,60 @@ def test_weights_of_a_cache_whose_rows_times_heads_pass_32_bits(tokens, group):
         # a score's sum of dim products in fp32, a step each; 2^x of numbers of up to 64; the sum over the rows
         e = dim * 2.0 ** -23 * norm + 2.0 ** -16 + tokens * group * 2.0 ** -24
         assert torch.all((w[j0:j0 + p.shape[1]].double() - want).abs() <= e * want), j0
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("tokens,kv,dim,length,draft", [
+    (1, 8, 128, 300, False), (1, 8, 128, 8000, False), (1, 1, 64, 131000, False), (16, 2, 64, 5000, True), (7, 8, 128, 100, True),
+    (24, 8, 128, 700, True), (20, 2, 64, 3900, False), (64, 4, 64, 131000, True), (100, 2, 128, 9000, True), (128, 8, 128, 9000, False)])
+@pytest.mark.parametrize("below", [12, 20, 24, 26, 28, 30])
+@pytest.mark.parametrize("first", [True, False])
+def test_a_dominant_key_without_a_value_leaves_the_rest(dtype, tokens, kv, dim, length, draft, below, first):
+    """One key takes all but 2^-below of a row's attention per other key, and its values are 0: the output is the other keys',
+    to the type's rounding, whether the dominant key comes first or among the last."""
+    torch = _torch()
+    n, h, cap = 1, kv, length + 9
+    g = torch.Generator(device="cuda").manual_seed(length + below)
+    dt = {"f16": torch.float16, "bf16": torch.bfloat16}[dtype]
+    # scores: the first element's product alone
+    q, k = torch.zeros(tokens, h, dim, dtype=dt, device="cuda"), torch.zeros(n, cap, kv, dim, dtype=dt, device="cuda")
+    q[..., 0] = 1.0
+    k[..., 0] = torch.empty(n, cap, kv, device="cuda").uniform_(-0.5, 0.5, generator=g).to(dt)
+    at = 0 if first else length - tokens - 1
+    k[:, at, :, 0] = below * np.log(2.0)
+    v = torch.empty(n, cap, kv, dim, device="cuda").uniform_(0.5, 1.5, generator=g).to(dt)
+    v[:, at] = 0
+    kn = torch.zeros(tokens, kv, dim, dtype=dt, device="cuda")
+    vn = torch.empty(tokens, kv, dim, device="cuda").uniform_(0.5, 1.5, generator=g).to(dt)
+    a = dict(k_new=kn, v_new=vn) if draft else {}
+    lens = torch.tensor([length], dtype=torch.int32, device="cuda")
+    out = torch.empty(tokens, h, dim, dtype=dt, device="cuda")
+    lse = torch.empty(1, h, tokens, device="cuda")
+    c = capi.cached_attention(dtype, n, tokens, h, kv, dim, cap, q=q.data_ptr(), k=k.data_ptr(), v=v.data_ptr(), lens=lens.data_ptr(),
+                              out=out.data_ptr(), lse=lse.data_ptr(), scale=1.0, **{x: y.data_ptr() for x, y in a.items()})
+    ws = torch.empty(max(256, capi.attention_tree_workspace(c)), dtype=torch.uint8, device="cuda")
+    capi.attention_tree(c, ws.data_ptr(), ws.numel(), _stream())
+    z = k[0, :length, :, 0].double()  # [row, head]
+    e = torch.exp(z)
+    sums, vals = torch.cumsum(e, 0), torch.cumsum(e[..., None] * v[0, :length].double(), 0)
+    if draft:  # a chain
+        sums, vals = sums[-1:].expand(tokens, -1), vals[-1:].expand(tokens, -1, -1)
+        sums = sums + torch.cumsum(torch.ones(tokens, kv, dtype=torch.float64, device="cuda"), 0)
+        vals = vals + torch.cumsum(vn.double(), 0)
+    else:
+        sums, vals = sums[length - tokens:], vals[length - tokens:]
+    ref = vals / sums[..., None]
+    # 2^x of numbers of up to 31 (fp32 scores: exact products of a single element); the sums over the keys, as they
+    # are added in tiles of 16 and more; the parts of p; a rounding of the output, half a step at least
+    keys = length + tokens
+    half = torch.finfo(dt).eps / 2
+    rel = 2 * (32 * 2.0 ** -23 + 2.0 ** -21) + 2 * (keys / 16 + 40) * 2.0 ** -23 + 2.0 ** -17
+    tol = (half + rel) * ref
+    if dtype == "f16":
+        few = tokens * h // kv <= 16
+        # half of fp16's least step for every key's p, which ends at 2^15, 2^7 or 2^12; values of up to 1.5
+        lost = keys * 2.0 ** -40 if few else min(keys, 31 * 128 + 128) * 2.0 ** -32 + keys * 2.0 ** -37
+        tol = tol + 1.5 * lost + 2.0 ** -25
+    err = (out.double() - ref).abs()
+    assert torch.all(err <= tol), float((err / tol).max())
+    assert torch.all((lse[0].T.double() - torch.log(sums)).abs() <= rel + 2.0 ** -23 * torch.log(sums).abs())
