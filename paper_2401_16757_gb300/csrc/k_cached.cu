@@ -68,13 +68,14 @@ __device__ __forceinline__ void load_queries(const CachedArgs& a, int b, int kvh
 // (running maximum m, sum l, output O in registers), so nothing waits for
 // another warp until the end:
 //   S = Q K^T          8 mma.m16n8k16 a 16 rows for 128 dims
-//   p = 2^(S - m)      handed to the next product as two parts p_hi + p_lo of
-//                      the storage type: 17 bits of p (bf16) or 22 (fp16)
+//   p = 2^(S - m)      handed to the next product as parts of the storage type:
+//                      three of bf16, all 24 bits of p, two of fp16, 22 bits
 //   O = O 2^(m' - m) + p V
 // Keys and values pass through a ring of three groups a warp (cp.async; rows
 // behind the sequence's end arrive as zeros, whatever the cache holds there).
-// The two parts cost a second product, which is free here; one part would
-// leave 8 (bf16) or 11 (fp16) bits of p, less than the fp32 that the sums keep.
+// The parts cost a second and a third product, which are free here; one part
+// would leave 8 (bf16) or 11 (fp16) bits of p, less than the fp32 that the sums
+// keep, two of bf16 17.
 // The kernel is bound by reading the cache: a group's 8 KB takes 48 products
 // of 16 rows, and the warp-level ones do that at several times DRAM's rate,
 // without the fixed costs (TMEM, barriers, 128-row tiles) of tcgen05.
@@ -198,7 +199,8 @@ __global__ void __launch_bounds__(kFwThreads, 2) attention_few_kernel(const __gr
         }
       }
     }
-    uint32_t ph[4], pl[4];
+    constexpr int kParts = std::is_same<T, __half>::value ? 2 : 3;
+    uint32_t pp[kParts][4];
     float al[2], base[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -219,10 +221,13 @@ __global__ void __launch_bounds__(kFwThreads, 2) attention_few_kernel(const __gr
         sum[h] += p0 + p1;
         s[n][2 * h] = p0;
         s[n][2 * h + 1] = p1;
-        const uint32_t hi = pack_pair<T>(p0, p1);
-        const float2 back = unpack_pair<T>(hi);
-        ph[2 * n + h] = hi;
-        pl[2 * n + h] = pack_pair<T>(p0 - back.x, p1 - back.y);
+        float2 left = make_float2(p0, p1);
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) {
+          const uint32_t part = pp[i][2 * n + h] = pack_pair<T>(left.x, left.y);
+          const float2 back = unpack_pair<T>(part);
+          left = make_float2(left.x - back.x, left.y - back.y);
+        }
       }
 #pragma unroll
     for (int h = 0; h < 2; ++h) l[h] = l[h] * al[h] + sum[h];
@@ -273,10 +278,11 @@ __global__ void __launch_bounds__(kFwThreads, 2) attention_few_kernel(const __gr
     for (int n = 0; n < D / 16; ++n) {
       uint32_t vf[4];
       ldmatrix_x4_trans(vs_u + swz<D>(lane & 15, 2 * n + (lane >> 4)), vf);
-      mma_16816<T>(o[2 * n], ph, vf[0], vf[1]);
-      mma_16816<T>(o[2 * n + 1], ph, vf[2], vf[3]);
-      mma_16816<T>(o[2 * n], pl, vf[0], vf[1]);
-      mma_16816<T>(o[2 * n + 1], pl, vf[2], vf[3]);
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) {
+        mma_16816<T>(o[2 * n], pp[i], vf[0], vf[1]);
+        mma_16816<T>(o[2 * n + 1], pp[i], vf[2], vf[3]);
+      }
     }
     __syncwarp();  // the group has been read before its slot is filled again
     if (++slot == kFwStages) slot = 0;

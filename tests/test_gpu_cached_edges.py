@@ -207,3 +207,40 @@ def test_a_dominant_key_without_a_value_leaves_the_rest(dtype, tokens, kv, dim, 
     err = (out.double() - ref).abs()
     assert torch.all(err <= tol), float((err / tol).max())
     assert torch.all((lse[0].T.double() - torch.log(sums)).abs() <= rel + 2.0 ** -23 * torch.log(sums).abs())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("tokens,length,dim", [(1, 16, 128), (1, 300, 64), (1, 9000, 128), (16, 300, 64), (5, 9000, 64)])
+def test_probabilities_of_few_rows_keep_their_bits(dtype, tokens, length, dim):
+    """Two keys whose probabilities differ by 2^-12 and whose values cancel: the difference is right to fp32's steps."""
+    torch = _torch()
+    h, cap = 64, length + 16
+    g = torch.Generator(device="cuda").manual_seed(length + tokens)
+    dt = {"f16": torch.float16, "bf16": torch.bfloat16}[dtype]
+    q, k = torch.zeros(tokens, h, dim, dtype=dt, device="cuda"), torch.zeros(1, cap, h, dim, dtype=dt, device="cuda")
+    v = torch.zeros(1, cap, h, dim, dtype=dt, device="cuda")
+    q[..., 0], q[..., 1], q[..., 2] = 1.0, 2.0 ** -12, 1.0
+    k[:, :, :, 2] = -64.0  # nothing
+    k[:, 0, :, 2] = 0.0    # the largest score, 0
+    a, b = (3, 9) if length == 16 else (3, length - tokens - 2)
+    c = -torch.empty(h, device="cuda").uniform_(0.3, 0.9, generator=g).to(dt)
+    for at, more, value in ((a, 0.0, 1.0), (b, 1.0, -1.0)):
+        k[0, at, :, 0], k[0, at, :, 1], k[0, at, :, 2] = c, more, 0.0
+        v[0, at] = value
+    v[0, a, :, 1::2] = -v[0, a, :, 1::2]
+    v[0, b, :, 1::2] = -v[0, b, :, 1::2]
+    lens = torch.tensor([length], dtype=torch.int32, device="cuda")
+    out = torch.empty(tokens, h, dim, dtype=dt, device="cuda")
+    args = capi.cached_attention(dtype, 1, tokens, h, h, dim, cap, q=q.data_ptr(), k=k.data_ptr(), v=v.data_ptr(),
+                                 lens=lens.data_ptr(), out=out.data_ptr(), scale=1.0)
+    ws = torch.empty(max(256, capi.attention_tree_workspace(args)), dtype=torch.uint8, device="cuda")
+    capi.attention_tree(args, ws.data_ptr(), ws.numel(), _stream())
+    pa, pb = torch.exp(c.double()), torch.exp(c.double() + 2.0 ** -12)
+    ref = ((pa - pb) / (1 + pa + pb))[None, :, None] * torch.tensor([1.0, -1.0], dtype=torch.float64, device="cuda").repeat(dim // 2)
+    # 2^x to 2^-22 and its argument to 2^-24 of at most 1.3; eight steps of the sums of products; the quotient; the rounding
+    half = torch.finfo(dt).eps / 2
+    tol = half * ref.abs() + (((pa + pb) * (2.0 ** -22 + 1.3 * 2.0 ** -24) + 8 * 2.0 ** -23 * pb) / (1 + pa + pb))[None, :, None]
+    if dtype == "f16":  # 22 bits of each p, and half of the type's least step
+        tol = tol + ((pa + pb) * 2.0 ** -23 / (1 + pa + pb))[None, :, None] + 2.0 ** -25
+    err = (out.double() - ref).abs()
+    assert torch.all(err <= tol), float((err / tol).max())
