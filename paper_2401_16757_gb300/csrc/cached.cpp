@@ -165,6 +165,7 @@ int fill_args(const swapnet_cached_attention* c, CachedArgs* a) {
   a->max_seq = c->max_seq;
   if (!(c->scale >= 0.f) || std::isinf(c->scale)) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cached attention: bad scale");
   a->scale_log2 = 1.4426950408889634f * (c->scale > 0.f ? c->scale : 1.0f / sqrtf((float)c->head_dim));
+  if (std::isinf(a->scale_log2)) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cached attention: bad scale");
   a->q = c->q;
   a->k = c->k;
   a->v = c->v;

@@ -187,3 +187,11 @@ def test_argument_blocks_have_the_header_layout():
     names = [n for n, _ in _capi.CachedAttention._fields_]
     a = capi.cached_attention(**{n: i + 1 for i, n in enumerate(names)})
     assert [getattr(a, n) for n in names] == [i + 1 for i in range(len(names))]
+
+
+@pytest.mark.parametrize("scale", [2.5e38, 3.4e38])
+def test_a_scale_beyond_the_base_two_scores_is_refused(scale):
+    """The kernels scale by log2(e) times as much: beyond fp32 a score of 0 would become NaN."""
+    assert _code(capi.attention_tree, _attn(scale=scale), A, 1 << 40) == capi.ERR_INVALID_ARG
+    assert _code(capi.attention_weights, _attn(scale=scale, weights=A)) == capi.ERR_INVALID_ARG
+    assert capi.attention_tree_workspace(_attn(scale=2.3e38)) == 0
