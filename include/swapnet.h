@@ -718,11 +718,18 @@ void swapnet_engine_free(swapnet_engine* eng);
  * are not returned by this call, which does not wait for its kernel: if a
  * bounded wait inside the kernel gives up (one second), Y is incomplete and
  * the timeout is recorded in the library's device error word, which the
- * next swapnet_engine_sync (of any engine on the device) reports as
- * SWAPNET_ERR_TIMEOUT and clears. */
+ * next swapnet_engine_sync (of any engine on the device) or
+ * swapnet_device_sync reports as SWAPNET_ERR_TIMEOUT and clears. */
 #define SWAPNET_NOALLOC_SCRATCH_BYTES (4u << 20)
 int swapnet_gemm_noalloc(int32_t dtype, const void* A, const void* W, const void* bias, void* Y, int32_t M,
                          int32_t N, int32_t K, int32_t act, swapnet_stream stream);
+
+/* Waits for the current device's work and reports what kernels recorded there
+ * since the last report, as swapnet_engine_sync does, for programs that make
+ * the calls above and below without an engine: TIMEOUT (a bounded wait gave up,
+ * outputs are incomplete), INVALID_ARG (a value in device memory was out of
+ * range), CUDA. */
+int swapnet_device_sync(void);
 
 /* ------------------------------------------------- cached attention
  * The attention of a decoder over its key-value cache as calls of their own,
@@ -742,8 +749,10 @@ int swapnet_gemm_noalloc(int32_t dtype, const void* A, const void* W, const void
  * same time.  Sizes are checked on the host; what lies in device memory
  * (lens, counts, parents, rows) is checked there: a sequence with a value out
  * of range is left alone (a row list's entry out of range adds nothing) and
- * the next swapnet_engine_sync on the device reports
- * SWAPNET_ERR_INVALID_ARG.
+ * swapnet_device_sync reports SWAPNET_ERR_INVALID_ARG.  A device has one record
+ * of such errors, which every report clears: the next swapnet_engine_sync
+ * reports it as well, so a program that also runs engines calls
+ * swapnet_device_sync before an inference whose report it wants by itself.
  *
  * Layout: element type F16 or BF16; a cache row holds the kv_heads heads of
  * one position, head h at element h * head_dim; sequence b's row j is at

@@ -137,7 +137,7 @@ EXPORTS = ["swapnet_default_options", "swapnet_partition", "swapnet_plan_from_cu
            "swapnet_debug_wait_timeout", "swapnet_pack_bf16",
            "swapnet_attention_tree_workspace", "swapnet_attention_tree", "swapnet_attention_weights",
            "swapnet_cache_evict", "swapnet_tree_accept", "swapnet_plan_state_layout", "swapnet_engine_tree_accept",
-           "swapnet_engine_evict"]
+           "swapnet_engine_evict", "swapnet_device_sync"]
 
 _lib = None
 
@@ -218,6 +218,7 @@ def lib():
         "swapnet_plan_state_layout": (C.c_int, [P, C.POINTER(StateLayout)]),
         "swapnet_engine_tree_accept": (C.c_int, [P, P, P, P]),
         "swapnet_engine_evict": (C.c_int, [P, C.c_int32, C.c_int32, C.c_int32, P]),
+        "swapnet_device_sync": (C.c_int, []),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -410,6 +411,11 @@ def gemm_noalloc(dtype, a_ptr, w_ptr, bias_ptr, y_ptr, M, N, K, act=0, stream=0)
     check(lib().swapnet_gemm_noalloc(dtype, C.c_void_p(a_ptr), C.c_void_p(w_ptr), C.c_void_p(bias_ptr),
                                      C.c_void_p(y_ptr), M, N, K, act, C.c_void_p(stream or None)),
           "swapnet_gemm_noalloc")
+
+
+def device_sync():
+    """Wait for the current device and raise what kernels recorded on it since the last report."""
+    check(lib().swapnet_device_sync(), "swapnet_device_sync")
 
 
 # -------------------------------------------------------- cached attention

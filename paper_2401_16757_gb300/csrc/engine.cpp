@@ -1720,6 +1720,17 @@ static int enqueue(swapnet_engine* e, const void* din, void* dout, cudaStream_t 
   return SWAPNET_OK;
 }
 
+// What kernels of the current device recorded since the last report; cleared.
+static int take_device_error(int* word) {
+  int w = 0;
+  CU(cudaMemcpy(&w, word, sizeof(int), cudaMemcpyDeviceToHost), "error word");
+  if (!w) return SWAPNET_OK;
+  const int zero = 0;
+  cudaMemcpy(word, &zero, sizeof(int), cudaMemcpyHostToDevice);
+  if (w == 2) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "a token id, a cache position, a length, a count or a parent was out of range");
+  SN_FAIL(SWAPNET_ERR_TIMEOUT, "a device-side wait gave up");
+}
+
 static uint64_t launches_per_infer(const swapnet_engine* e) {
   const StateLayout& st = e->plan.model.st;
   uint64_t n = e->plan.units.size() + (e->plan.model.has_attention && !(st.flags & SWAPNET_ATTENTION_TREE) ? 1 : 0);
@@ -1826,6 +1837,15 @@ int swapnet_infer_host(swapnet_engine* e, const void* hin, void* hout, swapnet_s
   });
 }
 
+int swapnet_device_sync(void) {
+  return swapnet::guard_abi([&]() -> int {
+    int* word = nullptr;
+    if (int rc = tc_error_word(&word)) return rc;
+    CU(cudaDeviceSynchronize(), "device synchronize");
+    return take_device_error(word);
+  });
+}
+
 int swapnet_engine_sync(swapnet_engine* e) {
   return swapnet::guard_abi([&]() -> int {
     if (!e) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "null engine");
@@ -1835,15 +1855,7 @@ int swapnet_engine_sync(swapnet_engine* e) {
     CU(cudaDeviceSynchronize(), "device synchronize");
     if (const int io = e->io_errno.exchange(0))
       SN_FAIL(SWAPNET_ERR_IO, std::string("weights file read during an inference: ") + std::strerror(io));
-    int w = 0;
-    CU(cudaMemcpy(&w, e->err_word, sizeof(int), cudaMemcpyDeviceToHost), "error word");
-    if (w) {
-      const int zero = 0;
-      cudaMemcpy(e->err_word, &zero, sizeof(int), cudaMemcpyHostToDevice);
-      if (w == 2) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "a token id or a cache position was out of range");
-      SN_FAIL(SWAPNET_ERR_TIMEOUT, "a device-side wait gave up");
-    }
-    return SWAPNET_OK;
+    return take_device_error(e->err_word);
   });
 }
 

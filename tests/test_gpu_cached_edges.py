@@ -244,3 +244,37 @@ def test_probabilities_of_few_rows_keep_their_bits(dtype, tokens, length, dim):
         tol = tol + ((pa + pb) * 2.0 ** -23 / (1 + pa + pb))[None, :, None] + 2.0 ** -25
     err = (out.double() - ref).abs()
     assert torch.all(err <= tol), float((err / tol).max())
+
+
+def test_errors_are_reported_without_an_engine():
+    """Each call's value out of range is reported once by the device, without an engine; an engine's next sync is clean."""
+    torch = _torch()
+    capi.device_sync()
+    n, t, h, d, cap = 2, 3, 2, 64, 20
+    q, k = torch.zeros(n * t, h * d, dtype=torch.float16, device="cuda"), torch.zeros(n, cap, h * d, dtype=torch.float16, device="cuda")
+    out, lse, w = torch.zeros_like(q), torch.zeros(n, h, t, device="cuda"), torch.zeros(n, h, cap, device="cuda")
+    bad = torch.tensor([5, cap + 1], dtype=torch.int32, device="cuda")
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")  # noqa: E731
+    ids, tgt, path, acc, nxt, lo, kept = i32(n, t), i32(n, t), i32(n, t), i32(n), i32(n), i32(n), i32(n, h, 4)
+    args = capi.cached_attention("f16", n, t, h, h, d, cap, q=q.data_ptr(), k=k.data_ptr(), v=k.data_ptr(), lens=bad.data_ptr(),
+                                 out=out.data_ptr(), lse=lse.data_ptr(), weights=w.data_ptr())
+    ws = torch.empty(max(256, capi.attention_tree_workspace(args)), dtype=torch.uint8, device="cuda")
+    to = [torch.zeros(n, cap, h * d, dtype=torch.float16, device="cuda") for _ in range(2)] + [torch.zeros_like(w)]
+    calls = [
+        lambda: capi.attention_tree(args, ws.data_ptr(), ws.numel(), _stream()),
+        lambda: capi.attention_weights(args, _stream()),
+        lambda: capi.tree_accept("f16", n, t, h * d, cap, ids=ids.data_ptr(), targets=tgt.data_ptr(), lens=bad.data_ptr(),
+                                 caches=[to[0].data_ptr()], drafts=[q.data_ptr()], path=path.data_ptr(), accepted=acc.data_ptr(),
+                                 next=nxt.data_ptr(), lens_out=lo.data_ptr(), stream=_stream()),
+        lambda: capi.cache_evict("f16", n, h, d, cap, 4, 1, 1, k=k.data_ptr(), v=k.data_ptr(), weights=w.data_ptr(), lens=bad.data_ptr(),
+                                 k_out=to[0].data_ptr(), v_out=to[1].data_ptr(), weights_out=to[2].data_ptr(), kept=kept.data_ptr(),
+                                 lens_out=lo.data_ptr(), stream=_stream()),
+    ]
+    eng = _any_engine()
+    for call in calls:
+        call()
+        with pytest.raises(capi.SwapnetError) as x:
+            capi.device_sync()
+        assert x.value.code == capi.ERR_INVALID_ARG and "length" in str(x.value)
+        capi.device_sync()
+        eng.sync()
