@@ -278,3 +278,47 @@ def test_errors_are_reported_without_an_engine():
         assert x.value.code == capi.ERR_INVALID_ARG and "length" in str(x.value)
         capi.device_sync()
         eng.sync()
+
+
+@pytest.mark.parametrize("weights", [False, True])
+def test_a_decoder_accepts_what_the_cache_has_room_for(weights):
+    """Two rows free: a child that the model chose is accepted behind its parent. One row free: the same path changes
+    nothing and is reported, a path of one node is accepted."""
+    import synth
+    from test_gpu_decode_cache import CFG, Engines
+    e = Engines({"prefill": (30, False), "tree": (4, True)}, weights=weights)
+    e.run("prefill", synth.gen.model_input(synth.arch.llm(tokens=30, **CFG)).reshape(-1))
+    rows, parents = CFG["max_seq"], [-1, 0, 0, 0]
+
+    def choice():
+        """The model's choice at node 0, which sees the cache and itself."""
+        return int(e.run("tree", [1, 2, 3, 4], parents)[1][0])
+
+    def state():
+        return e.caches("tree").copy(), e.weights("tree").copy() if weights else np.zeros(0)
+
+    e.header[0] = rows - 2
+    t = choice()
+    child = 5 if t != 5 else 6
+    _, tok = e.run("tree", [1, child, t, 7], parents)
+    assert int(tok[0]) == t
+    before = state()
+    path, n, nxt = e.accept("tree")
+    assert path == [0, 2] and n == 2 and nxt == int(tok[2]) and int(e.header[0]) == rows
+    after = state()
+    assert np.array_equal(after[0][:, :, :rows - 2], before[0][:, :, :rows - 2]) and not np.array_equal(after[0], before[0])
+    if weights:  # two queries' attention in every layer and head
+        assert np.all(np.abs(after[1].sum(-1) - before[1].sum(-1) - 2) <= 1e-3)
+    e.header[0] = rows - 1
+    t = choice()
+    e.run("tree", [1, child if child != t else 9, t, 7], parents)
+    before = state()
+    with pytest.raises(capi.SwapnetError) as x:
+        e.accept("tree")
+    assert x.value.code == capi.ERR_INVALID_ARG
+    assert int(e.header[0]) == rows - 1 and int(e.header[3]) == 0
+    assert all(np.array_equal(a, b) for a, b in zip(state(), before))
+    others = [i for i in range(20, 30) if i != t][:3]
+    _, tok = e.run("tree", [1] + others, parents)
+    path, n, nxt = e.accept("tree")
+    assert path == [0] and n == 1 and nxt == t == int(tok[0]) and int(e.header[0]) == rows
