@@ -522,7 +522,7 @@ int swapnet_plan_state_layout(const swapnet_plan* plan, swapnet_state_layout* la
  * number and leaves path, accepted and next in the state.  No room for the
  * path: nothing is accepted (accepted = 0), reported by swapnet_engine_sync.
  * Asynchronous on `stream`; no other engine may run on the state in between.
- * Errors: INVALID_ARG (no TREE model, no state), CUDA. */
+ * Errors: INVALID_ARG (no TREE model, no state), MISALIGNED, CUDA. */
 int swapnet_engine_tree_accept(swapnet_engine* eng, const int32_t* d_ids, const int32_t* d_targets, swapnet_stream stream);
 
 /* Eviction in the bound state of a WEIGHTS model: in every layer and head the
@@ -758,8 +758,8 @@ int swapnet_device_sync(void);
  * one position, head h at element h * head_dim; sequence b's row j is at
  * element b * seq_stride + j * kv_stride of k and v.  Query t of sequence b is
  * row b * tokens + t of q (heads * head_dim elements, stride q_stride).
- * Strides are in elements, 0 = packed; pointers are 16-byte aligned and
- * strides multiples of 8.  head_dim is 64 or 128; heads is a multiple of
+ * Strides are in elements, 0 = packed; queries, keys, values and outputs are
+ * 16-byte aligned, int32 and float arrays 4-byte, strides multiples of 8.  head_dim is 64 or 128; heads is a multiple of
  * kv_heads (query head h reads key head h / (heads / kv_heads)). */
 typedef struct swapnet_cached_attention {
   int32_t dtype;      /* SWAPNET_F16 or SWAPNET_BF16                          */

@@ -139,6 +139,8 @@ int cached_launches(const CachedArgs& a, const CachedPlan& p) {
 namespace {
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+// int32 and float arrays: single elements are read and written
+template <typename... P> bool aligned4(const P*... p) { return ((... | (uintptr_t)p) & 3) == 0; }
 
 // What both attention entry points require of their arguments.
 int fill_args(const swapnet_cached_attention* c, CachedArgs* a) {
@@ -183,6 +185,8 @@ int fill_args(const swapnet_cached_attention* c, CachedArgs* a) {
     SN_FAIL(SWAPNET_ERR_MISALIGNED, "cached attention: strides must be multiples of 8 elements");
   if (!aligned16(c->q) || !aligned16(c->k) || !aligned16(c->v) || !aligned16(c->k_new) || !aligned16(c->v_new) || !aligned16(c->out))
     SN_FAIL(SWAPNET_ERR_MISALIGNED, "cached attention: pointers must be 16-byte aligned");
+  if (!aligned4(c->lens, c->counts, c->parents, c->rows, c->lse, c->weights_in, c->weights))
+    SN_FAIL(SWAPNET_ERR_MISALIGNED, "cached attention: int32 and float arrays must be 4-byte aligned");
   a->lens = c->lens;
   a->counts = c->counts;
   a->parents = c->parents;
@@ -314,6 +318,8 @@ int swapnet_cache_evict(const swapnet_cache_eviction* c, swapnet_stream stream) 
     if ((a.kv_stride | a.seq_stride | a.out_stride | a.out_seq_stride) % 8 || !aligned16(a.k) || !aligned16(a.v) ||
         !aligned16(a.k_out) || !aligned16(a.v_out))
       SN_FAIL(SWAPNET_ERR_MISALIGNED, "eviction: caches and strides must be 16-byte aligned");
+    if (!aligned4(a.weights, a.weights_out, a.lens, a.kept, a.lens_out))
+      SN_FAIL(SWAPNET_ERR_MISALIGNED, "eviction: int32 and float arrays must be 4-byte aligned");
     // in place means the same rows: another layout over the same memory would be read after it was written
     const bool same[3] = {a.k == a.k_out, a.v == a.v_out, a.weights == a.weights_out};
     if (same[0] != same[1] || same[0] != same[2])
@@ -369,6 +375,8 @@ int swapnet_tree_accept(const swapnet_tree_acceptance* c, swapnet_stream stream)
     a.accepted = c->accepted;
     a.next = c->next;
     a.lens_out = c->lens_out;
+    if (!aligned4(a.ids, a.targets, a.parents, a.counts, a.lens, a.path, a.accepted, a.next, a.lens_out))
+      SN_FAIL(SWAPNET_ERR_MISALIGNED, "tree acceptance: int32 arrays must be 4-byte aligned");
     // every cache's CTA reads the inputs while the first one writes the results
     const int *const ins[5] = {a.ids, a.targets, a.parents, a.counts, a.lens}, *const outs[4] = {a.path, a.accepted, a.next, a.lens_out};
     for (const int* in : ins)

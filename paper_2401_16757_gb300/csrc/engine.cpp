@@ -1977,6 +1977,7 @@ int swapnet_engine_bind_state(swapnet_engine* e, void* d_state, uint64_t bytes) 
 int swapnet_engine_tree_accept(swapnet_engine* e, const int32_t* d_ids, const int32_t* d_targets, swapnet_stream stream) {
   return swapnet::guard_abi([&]() -> int {
     if (!e || !d_ids || !d_targets) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "null argument");
+    if (((uintptr_t)d_ids | (uintptr_t)d_targets) & 3) SN_FAIL(SWAPNET_ERR_MISALIGNED, "token ids must be 4-byte aligned");
     const Model& m = e->plan.model;
     const StateLayout& st = m.st;
     if (!(st.flags & SWAPNET_ATTENTION_TREE)) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "the model's attention takes no drafted tree");

@@ -195,3 +195,20 @@ def test_a_scale_beyond_the_base_two_scores_is_refused(scale):
     assert _code(capi.attention_tree, _attn(scale=scale), A, 1 << 40) == capi.ERR_INVALID_ARG
     assert _code(capi.attention_weights, _attn(scale=scale, weights=A)) == capi.ERR_INVALID_ARG
     assert capi.attention_tree_workspace(_attn(scale=2.3e38)) == 0
+
+
+@pytest.mark.parametrize("off", [1, 2, 3])
+def test_index_and_float_arrays_off_their_four_bytes_are_refused(off):
+    """Single elements of them are loaded: an address between two would fault on the device."""
+    for name in ("lens", "counts", "lse"):
+        assert _code(capi.attention_tree, _attn(**{name: A + off}), A, 1 << 40) == capi.ERR_MISALIGNED, name
+    assert _code(capi.attention_tree, _attn(k_new=A, v_new=A, parents=A + off), A, 1 << 40) == capi.ERR_MISALIGNED
+    for name in ("weights", "weights_in"):
+        assert _code(capi.attention_tree, _attn(**{"weights": A, name: A + off}), A, 1 << 40) == capi.ERR_MISALIGNED, name
+    for name in ("lens", "counts", "lse", "rows", "weights", "weights_in"):
+        assert _code(capi.attention_weights, _attn(**{"weights": A, name: A + off})) == capi.ERR_MISALIGNED, name
+    for name in ("weights", "lens", "weights_out", "kept", "lens_out"):
+        assert _code(_evict, **{name: 16 * A + off}) == capi.ERR_MISALIGNED, name
+    good = dict(path=2 * A, accepted=3 * A, next=4 * A, lens_out=5 * A)
+    for name in ("ids", "targets", "lens", "parents", "counts", "path", "accepted", "next", "lens_out"):
+        assert _code(_accept, **{**good, name: 16 * A + off}) == capi.ERR_MISALIGNED, name

@@ -322,3 +322,12 @@ def test_a_decoder_accepts_what_the_cache_has_room_for(weights):
     _, tok = e.run("tree", [1] + others, parents)
     path, n, nxt = e.accept("tree")
     assert path == [0] and n == 1 and nxt == t == int(tok[0]) and int(e.header[0]) == rows
+
+
+def test_token_ids_off_their_four_bytes_are_refused():
+    from test_gpu_decode_cache import Engines
+    eng = Engines({"tree": (4, True)}).e["tree"][2]
+    for ids, targets in ((18, 16), (16, 17)):
+        with pytest.raises(capi.SwapnetError) as x:
+            eng.tree_accept(ids, targets)
+        assert x.value.code == capi.ERR_MISALIGNED
