@@ -5,6 +5,7 @@
 #include <atomic>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 
 #include "cached.h"
 #include "internal.h"
@@ -142,6 +143,19 @@ bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 // int32 and float arrays: single elements are read and written
 template <typename... P> bool aligned4(const P*... p) { return ((... | (uintptr_t)p) & 3) == 0; }
 
+// Whether a result is one of the inputs, or another result, by its address
+// (null ones are not there); ranges are the caller's: caches may be interleaved.
+bool shares(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins) {
+  for (const void* const* o = outs.begin(); o != outs.end(); ++o) {
+    if (!*o) continue;
+    for (const void* in : ins)
+      if (*o == in) return true;
+    for (const void* const* p = outs.begin(); p != o; ++p)
+      if (*o == *p) return true;
+  }
+  return false;
+}
+
 // What both attention entry points require of their arguments.
 int fill_args(const swapnet_cached_attention* c, CachedArgs* a) {
   if (!c) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "null arguments");
@@ -256,6 +270,11 @@ int swapnet_attention_tree(const swapnet_cached_attention* c, void* workspace, u
     if (need && !workspace) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention: null workspace");
     if (workspace_bytes < need) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention: workspace too small");
     if (need && ((uintptr_t)workspace & (kAlign - 1))) SN_FAIL(SWAPNET_ERR_MISALIGNED, "attention: workspace must be 256-byte aligned");
+    // (weights may be weights_in)
+    if (shares({c->out, c->lse, c->weights, need ? workspace : nullptr},
+               {c->q, c->k, c->v, c->k_new, c->v_new, c->lens, c->counts, c->parents}) ||
+        shares({c->out, c->lse, need ? workspace : nullptr}, {c->weights_in}))
+      SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention: a result must not be an input or another result");
     if (int rc = error_word(&a.err)) return rc;
     return run_cached_attention(a, p, workspace, false, reinterpret_cast<cudaStream_t>(stream));
   });
@@ -268,6 +287,8 @@ int swapnet_attention_weights(const swapnet_cached_attention* c, swapnet_stream 
     if (int rc = fill_args(c, &a)) return rc;
     if (!c->lse || !c->weights) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cache weights: null pointer");
     if (c->k_new || c->v_new || c->parents) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cache weights: the queries are rows of the cache");
+    if (shares({c->weights}, {c->q, c->k, c->lens, c->counts, c->rows, c->lse}))
+      SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cache weights: the result must not be an input");
     if (int rc = error_word(&a.err)) return rc;
     return launch_weights(a, weights_splits(a), false, reinterpret_cast<cudaStream_t>(stream));
   });
@@ -327,7 +348,9 @@ int swapnet_cache_evict(const swapnet_cache_eviction* c, swapnet_stream stream) 
     if (same[0] && (a.kv_stride != a.out_stride || a.seq_stride != a.out_seq_stride || a.out_seq != a.max_seq))
       SN_FAIL(SWAPNET_ERR_INVALID_ARG, "eviction: in place the output has the input's layout");
     if (a.lens == a.lens_out) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "eviction: lens_out must not be lens (every head reads lens)");
-    if (a.k_out == a.v_out) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "eviction: keys and values share an output");
+    if (shares({a.k_out, a.v_out, a.weights_out, a.kept, a.lens_out}, {a.lens}) || shares({a.k_out}, {a.v, a.weights}) ||
+        shares({a.v_out}, {a.k, a.weights}) || shares({a.weights_out}, {a.k, a.v}) || shares({a.kept, a.lens_out}, {a.k, a.v, a.weights}))
+      SN_FAIL(SWAPNET_ERR_INVALID_ARG, "eviction: a result must not be another input or result");
     if (int rc = error_word(&a.err)) return rc;
     return launch_cache_evict(a, reinterpret_cast<cudaStream_t>(stream));
   });
@@ -378,10 +401,8 @@ int swapnet_tree_accept(const swapnet_tree_acceptance* c, swapnet_stream stream)
     if (!aligned4(a.ids, a.targets, a.parents, a.counts, a.lens, a.path, a.accepted, a.next, a.lens_out))
       SN_FAIL(SWAPNET_ERR_MISALIGNED, "tree acceptance: int32 arrays must be 4-byte aligned");
     // every cache's CTA reads the inputs while the first one writes the results
-    const int *const ins[5] = {a.ids, a.targets, a.parents, a.counts, a.lens}, *const outs[4] = {a.path, a.accepted, a.next, a.lens_out};
-    for (const int* in : ins)
-      for (const int* out : outs)
-        if (in == out) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "tree acceptance: a result must not be an input");
+    if (shares({a.path, a.accepted, a.next, a.lens_out}, {a.ids, a.targets, a.parents, a.counts, a.lens}))
+      SN_FAIL(SWAPNET_ERR_INVALID_ARG, "tree acceptance: a result must not be an input or another result");
     if (int rc = error_word(&a.err)) return rc;
     return launch_tree_accept(a, reinterpret_cast<cudaStream_t>(stream));
   });

@@ -212,3 +212,41 @@ def test_index_and_float_arrays_off_their_four_bytes_are_refused(off):
     good = dict(path=2 * A, accepted=3 * A, next=4 * A, lens_out=5 * A)
     for name in ("ids", "targets", "lens", "parents", "counts", "path", "accepted", "next", "lens_out"):
         assert _code(_accept, **{**good, name: 16 * A + off}) == capi.ERR_MISALIGNED, name
+
+
+def _apart(**kw):
+    """An attention call whose operands all lie apart."""
+    base = dict(q=1 * A, k=2 * A, v=3 * A, lens=4 * A, out=5 * A, lse=6 * A, max_seq=200)
+    base.update(kw)
+    return _attn(**base)
+
+
+@pytest.mark.parametrize("change", [dict(out=1 * A), dict(out=2 * A), dict(out=3 * A), dict(out=4 * A), dict(lse=1 * A), dict(lse=5 * A),
+                                    dict(k_new=5 * A, v_new=8 * A), dict(k_new=8 * A, v_new=9 * A, parents=6 * A), dict(counts=5 * A),
+                                    dict(weights=1 * A), dict(weights=6 * A), dict(weights=8 * A, weights_in=5 * A)])
+def test_attention_refuses_results_over_inputs(change):
+    """CTAs read the inputs while others write the results."""
+    assert _code(capi.attention_tree, _apart(**change), 20 * A, 1 << 40) == capi.ERR_INVALID_ARG
+
+
+def test_attention_refuses_a_workspace_that_is_an_operand():
+    long = dict(max_seq=8192)
+    assert capi.attention_tree_workspace(_apart(**long)) > 0
+    for at in (1, 2, 3, 4, 5, 6):
+        assert _code(capi.attention_tree, _apart(**long), at * A, 1 << 40) == capi.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("at", [1, 2, 4, 6, 8])
+def test_weights_refuse_results_over_inputs(at):
+    assert _code(capi.attention_weights, _apart(weights=at * A, rows=8 * A)) == capi.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("change", [dict(k_out=2 * A), dict(v_out=1 * A), dict(k_out=3 * A), dict(weights_out=1 * A), dict(kept=4 * A),
+                                    dict(kept=9 * A), dict(kept=3 * A), dict(lens_out=5 * A), dict(kept=7 * A)])
+def test_eviction_refuses_results_over_other_operands(change):
+    assert _code(_evict, **change) == capi.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("change", [dict(path=3 * A), dict(accepted=4 * A), dict(next=5 * A), dict(lens_out=2 * A)])
+def test_acceptance_refuses_results_over_results(change):
+    assert _code(_accept, **{**dict(path=2 * A, accepted=3 * A, next=4 * A, lens_out=5 * A), **change}) == capi.ERR_INVALID_ARG
