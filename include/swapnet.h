@@ -495,7 +495,8 @@ int swapnet_engine_bind_state(swapnet_engine* eng, void* d_state, uint64_t state
  * swapnet_engine_tree_accept: accepted nodes and the model's choice at the
  * last one.  Each run of an ATTENTION unit adds to the weights, also those of
  * swapnet_engine_measure_units and _calibrate: measure before the state is
- * used, or zero the weights behind it.
+ * used, or zero the weights behind it.  With TREE write a tree first: an empty
+ * one is out of range.
  * Engines that share a state are built from the same layers with the same
  * SWAPNET_ATTENTION_WEIGHTS flag; the offsets up to `weights` are the same for
  * them, what lies behind serves one engine's pass at a time. */
@@ -515,7 +516,8 @@ int swapnet_plan_state_layout(const swapnet_plan* plan, swapnet_state_layout* la
 /* Greedy decoding with drafted trees (TREE models).  Before each inference the
  * caller writes the tree (tree_count, tree_parents) into the state, on the same
  * stream; node 0 is the token the last pass chose and the input holds the
- * nodes' ids.  The inference does not advance the position.  This call walks
+ * nodes' ids, any valid ones behind tree_count; what the outputs hold for those
+ * is undefined.  The inference does not advance the position.  This call walks
  * the tree as swapnet_tree_accept does, with d_targets the inference's ARGMAX
  * output, appends the accepted nodes' rows to every layer's caches, with
  * WEIGHTS adds their attention to the weights, advances the position by their
@@ -787,7 +789,7 @@ typedef struct swapnet_cached_attention {
   int64_t q_stride, kv_stride, seq_stride, new_stride, out_stride;
 } swapnet_cached_attention;
 
-/* out[t] = sum_j softmax_j(scale q_t . k_j) v_j, exact in fp32 over
+/* out[t] = sum_j softmax_j(scale q_t . k_j) v_j, rounded once, over
  *   - with a draft (k_new): every cached row (j < lens) and, of the drafted
  *     nodes, the query's own and its ancestors; at most 128 nodes;
  *   - without: the queries are the cache's last `counts` rows, each sees the
@@ -797,9 +799,18 @@ typedef struct swapnet_cached_attention {
  * row j got from these queries, summed over the query heads that share its
  * key head; more than 16 rows (tokens x heads / kv_heads) need lse.
  * Queries at and behind counts, and weights at and behind lens, are left as
- * they were.  Hidden rows may hold anything.  `workspace` is 256-byte aligned
- * device memory of at least the bytes that _workspace returns (a function of
- * the sizes alone), with nothing to keep in it between calls.  Outputs and
+ * they were.  Hidden rows may hold anything.
+ * Scores, statistics and sums are fp32.  The probabilities enter their product
+ * with the values as parts of the storage type: up to 16 rows 24 bits of them
+ * (BF16) or 22 (F16), more rows 17 or 22.  F16 has no step below 2^-24, so a
+ * row's part of the largest probability is off by at most 2^-40 up to 16 rows;
+ * beyond, by at most 2^-32 in caches of up to 4000 rows and in the first 2048
+ * rows that a CTA takes of a longer one, 2^-37 in the rest.
+ * `workspace` is 256-byte aligned device memory of at least the bytes that
+ * _workspace returns, a function of the sizes and of whether k_new and weights
+ * are given, with nothing to keep in it between calls.  How many CTAs share a
+ * cache goes by max_seq as well, since lens are on the device: a large cache
+ * with few rows in use pays for a join that it does not need.  Outputs and
  * workspace overlap none of the inputs (but for weights and weights_in).
  * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA. */
 int swapnet_attention_tree_workspace(const swapnet_cached_attention* args, uint64_t* bytes);
