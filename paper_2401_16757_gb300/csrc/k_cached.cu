@@ -80,9 +80,9 @@ __device__ __forceinline__ void load_queries(const CachedArgs& a, int b, int kvh
 // of 16 rows, and the warp-level ones do that at several times DRAM's rate,
 // without the fixed costs (TMEM, barriers, 128-row tiles) of tcgen05.
 // Measured: one token of 64 sequences, 8 key heads (group 4) of 128 wide bf16
-// heads, up to 16384 rows (3.2 GB): 451 us, 7.0 TB/s; with the weights (SPILL: the
-// scaled scores are stored for the join, 0.13 GB written and read) 530, 6.1
-// TB/s; 7 nodes of 8 heads on 100 rows: 7.3 us, all of it latency (two launches,
+// heads, up to 16384 rows (3.2 GB): 452 us, 7.0 TB/s; with the weights (SPILL: the
+// scaled scores are stored for the join, 0.13 GB written and read) 531, 6.1
+// TB/s; 7 nodes of 8 heads on 100 rows: 7.2 us, all of it latency (two launches,
 // lengths, a tile's round trip, the join).  The second pass over the keys that
 // stored scores replace would read 1.6 GB again.
 template <typename T, int D, bool SPILL>
@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(kFwThreads, 2) attention_few_kernel(const __gr
 //   M = max m_s, L = sum l_s 2^(m_s - M), out = sum O_s 2^(m_s - M) / L.
 // The blocks behind them: weights_j = weights_in_j + sum over the rows that
 // see row j of 2^(score - log2 L - M), from the stored scores.  The scores of
-// the 530 us call above take it 33 us, 6 TB/s of scores and weights.
+// the 531 us call above take it 33 us, 6 TB/s of scores and weights.
 constexpr int kJoinThreads = 256, kJoinKeys = 4 * kJoinThreads;
 
 // log2 of a row's softmax sum, over its splits.

@@ -34,12 +34,12 @@
 // drains the loads and MMAs it started, frees TMEM and returns.
 //
 // Measured, caches larger than L2: 32 sequences x 8 key heads (group 4) of 128
-// wide bf16 heads on up to 8000 rows (0.72 GB): 16 nodes 121 us, 5.9 TB/s; 24
-// nodes 128, 5.6; 64 nodes 227 and 128 nodes 388, 0.62 and 0.75 PFLOP/s (the
+// wide bf16 heads on up to 8000 rows (0.72 GB): 16 nodes 122 us, 5.9 TB/s; 24
+// nodes 129, 5.6; 64 nodes 228 and 128 nodes 390, 0.62 and 0.75 PFLOP/s (the
 // second product of P not counted).  1000 queries on 4096 rows, 2 sequences x 32
-// heads, f16: 126 us, 0.71 PFLOP/s.  One sequence of 131001 rows, 4 key heads of
-// 64 wide f16, 52 rows: 41 us, of which the join and a unit's start and end are
-// 15.  32 heads x 64 nodes on 511 rows: 13.2 us.
+// heads, f16: 124 us, 0.72 PFLOP/s.  One sequence of 131001 rows, 4 key heads of
+// 64 wide f16, 52 rows: 42 us, of which the join and a unit's start and end are
+// 15.  32 heads x 64 nodes on 511 rows: 13.0 us.
 // Up to about 100 rows per unit DRAM bounds it, beyond that the softmax warps: a
 // tile of 128 x 128 takes them about 2500 cycles (1265 for exponentials and the
 // two parts of P, 350 for the maximum, 320 to store P, 170 to load S, the rest
@@ -885,12 +885,15 @@ __global__ void __launch_bounds__(kAtThreads, 1)
 // start and waits are the other's time.  Rows of a list are fetched one query
 // at a time.
 // Measured: 32 sequences of 8 key heads (group 4), 1 to 8 listed queries on
-// up to 8000 rows (0.37 GB): 66 us, 5.5 TB/s; 1000 queries on 4096 rows, 2 x 32
-// heads, f16: 89 us, 0.50 PFLOP/s; 512 queries x 32 heads on themselves: 8.3 us.
+// up to 8000 rows (0.37 GB): 68.5 us, 5.3 TB/s; 1000 queries on 4096 rows, 2 x 32
+// heads, f16: 87 us, 0.51 PFLOP/s; 512 queries x 32 heads on themselves: 8.2 us.
 // Few rows are bound by reading the keys, many by the sum warps: about 1450
 // cycles for 128 x 128 scores on an SM, of which the exponentials' unit is busy
 // for 1024 (16 a cycle).  Warp products (16 rows each) in its place took 119 us
-// for 4 listed rows where this takes 64, so it serves every count of rows.
+// for 4 listed rows where this took 64, so it serves every count of rows.
+// LIST: rows of a list, in an instance of its own, since looking for entries out
+// of range in the loop of the others took 4 % of theirs (211 us with the
+// attention, 220 so) and 2.5 % of the list's.
 template <int D> struct WtCfg {
   static constexpr int kHalves = D / 64;
   static constexpr int kBox = 128 * 128;
