@@ -331,3 +331,73 @@ def test_token_ids_off_their_four_bytes_are_refused():
         with pytest.raises(capi.SwapnetError) as x:
             eng.tree_accept(ids, targets)
         assert x.value.code == capi.ERR_MISALIGNED
+
+
+@pytest.mark.parametrize("dtype,tokens,heads,kv,dim", [("bf16", 6, 8, 2, 128), ("f16", 40, 8, 8, 64), ("bf16", 100, 4, 2, 128)])
+def test_a_captured_chain_of_the_calls_follows_its_inputs(dtype, tokens, heads, kv, dim):
+    """Verification, acceptance, weighing and eviction captured into one graph: replays on other lengths, trees and tokens give
+    the bits of the same calls made one by one."""
+    torch = _torch()
+    dt = {"f16": torch.float16, "bf16": torch.bfloat16}[dtype]
+    n, cap, keep = 5, 700, 150
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    rng = np.random.default_rng(tokens)
+
+    def normal(*shape):
+        return torch.empty(shape, dtype=dt, device="cuda").normal_(generator=g)
+
+    def inputs():
+        par = np.full((n, tokens), -1, dtype=np.int32)
+        for i in range(1, tokens):
+            par[:, i] = rng.integers(max(0, i - 4), i, size=n)
+        i32 = lambda x: torch.from_numpy(np.ascontiguousarray(x, dtype=np.int32)).cuda()  # noqa: E731
+        return dict(k=normal(n, cap, kv * dim), v=normal(n, cap, kv * dim), q=normal(n * tokens, heads * dim),
+                    kn=normal(n * tokens, kv * dim), vn=normal(n * tokens, kv * dim),
+                    w=torch.empty(n, kv, cap, device="cuda").uniform_(0, 2, generator=g), par=i32(par),
+                    lens=i32(rng.integers(0, cap - tokens, size=n)), counts=i32(rng.integers(1, tokens + 1, size=n)),
+                    ids=i32(rng.integers(0, 3, size=(n, tokens))), tgt=i32(rng.integers(0, 3, size=(n, tokens))))
+
+    sets = [inputs() for _ in range(3)]
+    s = {x: y.clone() for x, y in sets[0].items()}  # the buffers that the calls use
+    out, lse = torch.empty(n * tokens, heads * dim, dtype=dt, device="cuda"), torch.empty(n, heads, tokens, device="cuda")
+    i32 = lambda *shape: torch.empty(*shape, dtype=torch.int32, device="cuda")  # noqa: E731
+    path, acc, nxt, lens2, lens3, kept = i32(n, tokens), i32(n), i32(n), i32(n), i32(n), i32(n, kv, keep)
+    p = {x: y.data_ptr() for x, y in s.items()}
+    a = capi.cached_attention(dtype, n, tokens, heads, kv, dim, cap, q=p["q"], k=p["k"], v=p["v"], lens=p["lens"], counts=p["counts"],
+                              parents=p["par"], k_new=p["kn"], v_new=p["vn"], out=out.data_ptr(), lse=lse.data_ptr())
+    w = capi.cached_attention(dtype, n, tokens, heads, kv, dim, cap, q=p["q"], k=p["k"], lens=lens2.data_ptr(), counts=acc.data_ptr(),
+                              rows=path.data_ptr(), lse=lse.data_ptr(), weights_in=p["w"], weights=p["w"])
+    ws = torch.empty(max(256, capi.attention_tree_workspace(a)), dtype=torch.uint8, device="cuda")
+    results = [out, lse, path, acc, nxt, lens2, lens3, kept, s["k"], s["v"], s["w"]]
+
+    def chain():
+        capi.attention_tree(a, ws.data_ptr(), ws.numel(), _stream())
+        capi.tree_accept(dtype, n, tokens, kv * dim, cap, ids=p["ids"], targets=p["tgt"], parents=p["par"], counts=p["counts"],
+                         lens=p["lens"], caches=[p["k"], p["v"]], drafts=[p["kn"], p["vn"]], path=path.data_ptr(),
+                         accepted=acc.data_ptr(), next=nxt.data_ptr(), lens_out=lens2.data_ptr(), stream=_stream())
+        capi.attention_weights(w, _stream())
+        capi.cache_evict(dtype, n, kv, dim, cap, keep, 20, 2, k=p["k"], v=p["v"], weights=p["w"], lens=lens2.data_ptr(), k_out=p["k"],
+                         v_out=p["v"], weights_out=p["w"], kept=kept.data_ptr(), lens_out=lens3.data_ptr(), stream=_stream())
+
+    def reset(i):
+        for x, y in sets[i].items():
+            s[x].copy_(y)
+        for x in results[:8]:
+            x.fill_(7)
+
+    alone = []
+    for i in range(3):
+        reset(i)
+        chain()
+        alone.append([x.clone() for x in results])
+    graph = torch.cuda.CUDAGraph()
+    reset(0)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        chain()
+    for i in (2, 0, 1, 2):
+        reset(i)
+        graph.replay()
+        assert all(torch.equal(x, y) for x, y in zip(results, alone[i])), i
+    capi.device_sync()
+    assert max(int(x[3].max()) for x in alone) > 1 and min(int(x[6].min()) for x in alone) < keep
