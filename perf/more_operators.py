@@ -237,10 +237,11 @@ def _plain_append(s):
     first, end = lens // b, lens + counts  # the blocks from the one that is open on
     nb = (t + 2 * b - 2) // b
     row = first[:, None] * b + torch.arange(nb * b, device="cuda")  # [n, rows]
-    valid = (row < end[:, None]) & (counts > 0)[:, None]
+    held = row < end[:, None]
+    valid = held & (counts > 0)[:, None]
     old = row < lens[:, None]
     tail = (end // b)[:, None]  # the block that stays open
-    staged = valid & (row // b == tail)
+    staged = held & (row // b == tail)
     for rows, cache, scales, opened, opened_out in (
             (new[0], s["k"], s["k_scale"], s["k_open"], s["k_open_out"]),
             (new[1], s["v"], s["v_scale"], s["v_open"], s["v_open_out"])):
@@ -333,7 +334,7 @@ def work(case):
     if not b:
         return dict(bytes=byte + new * 4 * kv * d, flops=0)
     opened = sum(y % b for x, y in zip(counts, lens) if x)  # rows of the open blocks, read again
-    left = sum((x + y) % b for x, y in zip(counts, lens) if x)
+    left = sum((x + y) % b for x, y in zip(counts, lens))
     touched = sum(-(-(x + y) // b) - y // b for x, y in zip(counts, lens) if x)
     return dict(bytes=byte + 2 * kv * d * (2 * opened + new + opened + 2 * left) + 8 * kv * touched, flops=0)
 
@@ -406,7 +407,9 @@ def _exact_append(c, s):
     opened = [s["k_open_out"].double(), s["v_open_out"].double()]
     for cache, scale, left, rows, before in zip(caches, scales, opened, new, (s["k_open"], s["v_open"])):
         for i, m in enumerate(counts):
+            rest = int(ends[i]) % b
             if m == 0:
+                left[i, :rest] = before[i, :rest].double()
                 continue
             first = lens[i] // b
             x = torch.cat([before[i, :lens[i] % b].double(), rows(i, m)])
@@ -425,7 +428,6 @@ def _exact_append(c, s):
                 code = torch.round(code)
             cache[i, first * b:first * b + x.shape[0]] = code.view(nb * b, kv, d)[:x.shape[0]]
             scale[i, :, first:first + nb] = step.T
-            rest = int(ends[i]) % b
             if rest:
                 left[i, :rest] = x[x.shape[0] - rest:]
     if c["cache"] == "i8":
