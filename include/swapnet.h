@@ -54,7 +54,9 @@ typedef enum swapnet_dtype {
   SWAPNET_F32 = 0,
   SWAPNET_F16 = 1,
   SWAPNET_BF16 = 2,
-  SWAPNET_I32 = 3 /* model input only: token ids */
+  SWAPNET_I32 = 3, /* model input only: token ids */
+  SWAPNET_I8 = 4,  /* codes of a quantised key-value cache only: -127 .. 127    */
+  SWAPNET_E4M3 = 5 /* the same, 8-bit floats (1-4-3, largest 448, no infinity)  */
 } swapnet_dtype;
 
 typedef enum swapnet_op {
@@ -883,6 +885,123 @@ typedef struct swapnet_tree_acceptance {
   int64_t cache_stride, seq_stride, new_stride;
 } swapnet_tree_acceptance;
 int swapnet_tree_accept(const swapnet_tree_acceptance* args, swapnet_stream stream);
+
+/* ------------------------------------------------- quantised caches
+ * A key-value cache held in 8 bits, with a scale for each block of rows and key
+ * head: half the bytes beside the arena, and half the bytes for every decode
+ * step to read.  swapnet_cache_append prepares a step's queries and puts its
+ * rows into the cache; swapnet_attention_quantized reads it.  What is said of
+ * the cached-attention calls above (streams, captures, workspaces, errors found
+ * on the device, the current device) holds for these as well.  The paper has no
+ * counterpart.
+ *
+ * Layout: codes k, v of cache_dtype, [n_seq][max_seq][kv_heads][head_dim] with
+ * kv_stride and seq_stride as above (in codes, multiples of 16; 0 = packed);
+ * scales [n_seq][kv_heads][ceil(max_seq / block)] fp32.  The scale of block i
+ * is that of rows i * block .. i * block + block - 1 of one head; a value is
+ * code * scale.  block: 16, 32, 64 or 128.  The rows of a sequence's last
+ * block, as long as it is not full, are kept in 16 bits as well: k_open, v_open,
+ * [n_seq][block][kv_heads][head_dim], row j of the cache at j % block.  A row is
+ * rounded to 8 bits from its 16-bit value whatever the calls that append it,
+ * and the cache is a function of the rows alone:
+ *   E4M3  scale = the least power of two >= m / 448
+ *   I8    scale = m / 127
+ * with m the block's largest magnitude so far (scale at least 2^-100), code =
+ * value / scale rounded to the nearest (ties to even).  A block with a value
+ * that is infinite or not a number has a scale that is not a number (codes of
+ * I8: 0), and so has the attention of every query that sees one of its rows. */
+
+/* Appends the rows of up to `tokens` new tokens per sequence to a cache, and
+ * prepares their queries:
+ *   q, k: x / sqrt(mean(x^2) + eps) * gain for each head (with a gain), then the
+ *   rotation (with theta): pair i of the first rope_dim elements turned by
+ *   position * theta^(-2 i / rope_dim); pairs are (2i, 2i + 1), with `halves`
+ *   (i, i + rope_dim / 2).  Rounded once, to dtype.  v as it is.
+ * With `sections` the pairs follow up to three position axes (e.g. time, height,
+ * width): the first sections[0] pairs axis 0, the next sections[1] axis 1, the
+ * rest axis 2.
+ * k and v rows t < counts[b] go to rows lens[b] + t; lens_out = lens + counts.
+ * cache_dtype = dtype: a 16-bit cache, rows as they are (block 0, no scales).
+ * I8, E4M3: as above; k_open_out and v_open_out receive the rows of the block
+ * that is open afterwards (NULL: in place; other buffers: the call may be
+ * repeated).  Rows at and behind counts of q_out, rows at and behind lens_out
+ * of the cache and of the open block, and scales of blocks without new rows are
+ * left as they were.  A sequence whose rows do not fit its cache, or with a
+ * length or count out of range, is left alone and reported by
+ * swapnet_device_sync; a position that is negative or not below 2^24 counts as
+ * 0 and is reported.
+ * heads = 0, q and q_out NULL: no queries (a 16-bit cache put into 8 bits).
+ * q_out may be q (one stride); no other result may be an input.  head_dim 64 or
+ * 128.
+ * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA. */
+typedef struct swapnet_cache_rows {
+  int32_t dtype;        /* F16 or BF16: queries, new rows, gains, open rows      */
+  int32_t cache_dtype;  /* dtype, SWAPNET_I8 or SWAPNET_E4M3                     */
+  int32_t n_seq, tokens, heads, kv_heads, head_dim;
+  int32_t max_seq;      /* rows of a sequence's cache, at most 2^24              */
+  int32_t block;        /* rows of a scale; 0 for a 16-bit cache                 */
+  int32_t rope_dim;     /* a multiple of 16 up to head_dim; 0 = head_dim         */
+  int32_t halves;       /* which elements make a pair                            */
+  int32_t sections[3];  /* pairs of each axis, rope_dim / 2 in all; all 0: one axis */
+  float theta;          /* 0: no rotation                                        */
+  float eps;            /* of the norms                                          */
+  const void* q;        /* [n_seq * tokens][heads * head_dim], stride q_stride   */
+  const void* k_new;    /* [n_seq * tokens][kv_heads * head_dim], stride new_stride */
+  const void* v_new;
+  const void* q_gain;   /* [head_dim], NULL = no norm of the queries             */
+  const void* k_gain;   /* the same for the keys                                 */
+  const int32_t* lens;  /* [n_seq] rows of the cache in use before               */
+  const int32_t* counts;    /* [n_seq] new rows, NULL = tokens                   */
+  const int32_t* positions; /* [axes][n_seq][tokens], axes = 1 without sections,
+                               else 3; NULL = lens + t on every axis             */
+  void* q_out;          /* [n_seq * tokens][heads * head_dim], stride out_stride */
+  void* k;              /* the cache                                             */
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  const void* k_open;   /* the open blocks' rows                                 */
+  const void* v_open;
+  void* k_open_out;     /* NULL = k_open, v_open                                 */
+  void* v_open_out;
+  int32_t* lens_out;    /* [n_seq], not lens itself; nullable                    */
+  int64_t q_stride, new_stride, out_stride, kv_stride, seq_stride; /* elements, 0 = packed */
+} swapnet_cache_rows;
+int swapnet_cache_append(const swapnet_cache_rows* args, swapnet_stream stream);
+
+/* out[t] = sum_j softmax_j(scale q_t . k_j) v_j over a quantised cache, rounded
+ * once: the queries are the cache's last `counts` rows, each sees the rows up to
+ * its own (one token: a decode step whose row swapnet_cache_append has put into
+ * the cache).  A query that sees no row gives 0 and lse = -inf.  Queries at and
+ * behind counts are left as they were; codes and scales behind lens may hold
+ * anything.
+ * Scores, statistics and sums are fp32.  Keys and values enter the products as
+ * fp16 numbers that hold their codes exactly, queries as fp16 (BF16 ones scaled
+ * by a power of two per query, which loses what is below 2^-39 of its largest
+ * element), probabilities times their value scales as two fp16 parts (22 bits;
+ * off by at most 2^-32 of a query's largest such product).  A value scale below
+ * 2^-100 counts as 2^-100; scales are not negative.
+ * `workspace` as for swapnet_attention_tree.  Results and workspace overlap
+ * none of the inputs.  Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA. */
+typedef struct swapnet_quantized_attention {
+  int32_t dtype;        /* F16 or BF16: queries and outputs                      */
+  int32_t cache_dtype;  /* SWAPNET_I8 or SWAPNET_E4M3                            */
+  int32_t n_seq, tokens, heads, kv_heads, head_dim;
+  int32_t max_seq, block;
+  float scale;          /* of q . k; 0 = 1 / sqrt(head_dim)                      */
+  const void* q;        /* rotated queries [n_seq * tokens], stride q_stride     */
+  const void* k;
+  const void* v;
+  const float* k_scale;
+  const float* v_scale;
+  const int32_t* lens;   /* [n_seq] rows of the cache in use                     */
+  const int32_t* counts; /* [n_seq] queries in use, NULL = tokens                */
+  void* out;             /* [n_seq * tokens][heads * head_dim], stride out_stride */
+  float* lse;            /* [n_seq][heads][tokens], nullable                     */
+  int64_t q_stride, kv_stride, seq_stride, out_stride;
+} swapnet_quantized_attention;
+int swapnet_attention_quantized_workspace(const swapnet_quantized_attention* args, uint64_t* bytes);
+int swapnet_attention_quantized(const swapnet_quantized_attention* args, void* workspace, uint64_t workspace_bytes,
+                                swapnet_stream stream);
 
 /* --------------------------------------------------------- host weights */
 /* Page-locked, device-mapped host memory for weight storage (the pinned

@@ -18,11 +18,11 @@ LIB_PATH = os.path.join(_PKG, "libswapnet.so")
 OK, ERR_INVALID_ARG, ERR_INFEASIBLE, ERR_OOM, ERR_CUDA, ERR_TIMEOUT, ERR_MISALIGNED, ERR_UNSUPPORTED, ERR_IO, \
     ERR_INTERNAL = 0, -1, -2, -3, -4, -5, -6, -7, -8, -9
 F32, F16, BF16 = 0, 1, 2
-I32 = 3
+I32, I8, E4M3 = 3, 4, 5
 OP = {"linear": 1, "conv": 2, "maxpool": 3, "gap": 4, "upsample2x": 5, "concat": 6, "embed": 7, "rmsnorm": 8,
       "attention": 9, "argmax": 10}
 ACT = {"none": 0, "relu": 1, "leaky": 2, "swiglu": 3}
-DTYPE = {"f32": F32, "f16": F16, "bf16": BF16, "i32": I32}
+DTYPE = {"f32": F32, "f16": F16, "bf16": BF16, "i32": I32, "i8": I8, "e4m3": E4M3}
 LAYER_NO_BIAS = 1
 ATTENTION_TREE, ATTENTION_WEIGHTS = 2, 4
 SWAP_AUTO, SWAP_MEMCPY, SWAP_ZEROCOPY, SWAP_DIRECT, SWAP_PACKED = 0, 1, 2, 3, 4
@@ -122,6 +122,25 @@ class TreeAcceptance(C.Structure):
         [(n, C.c_int64) for n in ("cache_stride", "seq_stride", "new_stride")]
 
 
+class CacheRows(C.Structure):
+    """swapnet_cache_rows; pointers are device addresses as integers."""
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "cache_dtype", "n_seq", "tokens", "heads", "kv_heads", "head_dim", "max_seq",
+                                         "block", "rope_dim", "halves")] + \
+        [("sections", C.c_int32 * 3), ("theta", C.c_float), ("eps", C.c_float)] + \
+        [(n, C.c_void_p) for n in ("q", "k_new", "v_new", "q_gain", "k_gain", "lens", "counts", "positions", "q_out", "k", "v",
+                                   "k_scale", "v_scale", "k_open", "v_open", "k_open_out", "v_open_out", "lens_out")] + \
+        [(n, C.c_int64) for n in ("q_stride", "new_stride", "out_stride", "kv_stride", "seq_stride")]
+
+
+class QuantizedAttention(C.Structure):
+    """swapnet_quantized_attention; pointers are device addresses as integers."""
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "cache_dtype", "n_seq", "tokens", "heads", "kv_heads", "head_dim", "max_seq",
+                                         "block")] + \
+        [("scale", C.c_float)] + \
+        [(n, C.c_void_p) for n in ("q", "k", "v", "k_scale", "v_scale", "lens", "counts", "out", "lse")] + \
+        [(n, C.c_int64) for n in ("q_stride", "kv_stride", "seq_stride", "out_stride")]
+
+
 EXPORTS = ["swapnet_default_options", "swapnet_partition", "swapnet_plan_from_cuts", "swapnet_plan_resident",
            "swapnet_plan_info_get", "swapnet_plan_cuts", "swapnet_plan_units", "swapnet_plan_blocks",
            "swapnet_plan_output_offsets", "swapnet_plan_free", "swapnet_schedule", "swapnet_load",
@@ -137,7 +156,8 @@ EXPORTS = ["swapnet_default_options", "swapnet_partition", "swapnet_plan_from_cu
            "swapnet_debug_wait_timeout", "swapnet_pack_bf16",
            "swapnet_attention_tree_workspace", "swapnet_attention_tree", "swapnet_attention_weights",
            "swapnet_cache_evict", "swapnet_tree_accept", "swapnet_plan_state_layout", "swapnet_engine_tree_accept",
-           "swapnet_engine_evict", "swapnet_device_sync"]
+           "swapnet_engine_evict", "swapnet_device_sync", "swapnet_cache_append", "swapnet_attention_quantized_workspace",
+           "swapnet_attention_quantized"]
 
 _lib = None
 
@@ -219,6 +239,9 @@ def lib():
         "swapnet_engine_tree_accept": (C.c_int, [P, P, P, P]),
         "swapnet_engine_evict": (C.c_int, [P, C.c_int32, C.c_int32, C.c_int32, P]),
         "swapnet_device_sync": (C.c_int, []),
+        "swapnet_cache_append": (C.c_int, [C.POINTER(CacheRows), P]),
+        "swapnet_attention_quantized_workspace": (C.c_int, [C.POINTER(QuantizedAttention), C.POINTER(C.c_uint64)]),
+        "swapnet_attention_quantized": (C.c_int, [C.POINTER(QuantizedAttention), P, C.c_uint64, P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -473,6 +496,45 @@ def tree_accept(dtype, n_seq, tokens, width, max_seq, ids, targets, lens, caches
         DTYPE.get(dtype, dtype), n_seq, tokens, width, max_seq, caches.size, ids, targets, parents, counts, lens,
         caches.ctypes.data, drafts.ctypes.data, path, accepted, next, lens_out, cache_stride, seq_stride, new_stride))
     check(lib().swapnet_tree_accept(C.byref(a), stream or None), "swapnet_tree_accept")
+
+
+# -------------------------------------------------------- quantised caches
+_ROWS, _QUANTIZED = struct.Struct("14i2f18P5q"), struct.Struct("9if9P4q")
+
+
+def cache_append(dtype, cache_dtype, n_seq, tokens, heads, kv_heads, head_dim, max_seq, k_new, v_new, lens, k, v, q=0, q_out=0,
+                 counts=0, positions=0, q_gain=0, k_gain=0, k_scale=0, v_scale=0, k_open=0, v_open=0, k_open_out=0,
+                 v_open_out=0, lens_out=0, block=0, rope_dim=0, theta=0.0, halves=False, sections=(0, 0, 0), eps=0.0,
+                 q_stride=0, new_stride=0, out_stride=0, kv_stride=0, seq_stride=0, stream=0):
+    """Norms and rotation of new queries and keys, and their rows put into a cache of 16 bits, "i8" or "e4m3":
+    sizes, device addresses (0: none), then options and strides in elements (0: packed)."""
+    a = CacheRows.from_buffer_copy(_ROWS.pack(
+        DTYPE.get(dtype, dtype), DTYPE.get(cache_dtype, cache_dtype), n_seq, tokens, heads, kv_heads, head_dim, max_seq, block,
+        rope_dim, bool(halves), *sections, theta, eps, q, k_new, v_new, q_gain, k_gain, lens, counts, positions, q_out, k, v,
+        k_scale, v_scale, k_open, v_open, k_open_out, v_open_out, lens_out, q_stride, new_stride, out_stride, kv_stride,
+        seq_stride))
+    check(lib().swapnet_cache_append(C.byref(a), stream or None), "swapnet_cache_append")
+
+
+def quantized_attention(dtype, cache_dtype, n_seq, tokens, heads, kv_heads, head_dim, max_seq, block, q, k, v, k_scale, v_scale,
+                        lens, out, lse=0, counts=0, scale=0.0, q_stride=0, kv_stride=0, seq_stride=0, out_stride=0):
+    """The arguments of attention_quantized: sizes, device addresses (0: none), strides in elements (0: packed)."""
+    return QuantizedAttention.from_buffer_copy(_QUANTIZED.pack(
+        DTYPE.get(dtype, dtype), DTYPE.get(cache_dtype, cache_dtype), n_seq, tokens, heads, kv_heads, head_dim, max_seq, block,
+        scale, q, k, v, k_scale, v_scale, lens, counts, out, lse, q_stride, kv_stride, seq_stride, out_stride))
+
+
+def attention_quantized_workspace(args):
+    """Bytes of device memory that attention_quantized needs beside its operands."""
+    n = C.c_uint64()
+    check(lib().swapnet_attention_quantized_workspace(C.byref(args), C.byref(n)), "swapnet_attention_quantized_workspace")
+    return n.value
+
+
+def attention_quantized(args, workspace=0, workspace_bytes=0, stream=0):
+    """Attention of the cache's last rows over a cache held in 8 bits."""
+    check(lib().swapnet_attention_quantized(C.byref(args), workspace or None, workspace_bytes, stream or None),
+          "swapnet_attention_quantized")
 
 
 # ------------------------------------------------------------ host weights

@@ -23,7 +23,7 @@ constexpr double kUnitUs = 5.0, kTileUs = 1.0, kJoinUs = 8.0;
 // the end (lengths and causal limits differ).  In microseconds: a tile of a CTA
 // by itself, a tile of an SM's time when all are busy, a CTA's start and end,
 // and the join where there is one.
-static int choose_splits(int64_t ctas, int tiles, double alone, double busy, double fixed, double join) {
+int choose_splits(int64_t ctas, int tiles, double alone, double busy, double fixed, double join) {
   int best = 1;
   double least = 1e30;
   for (int s = 1; s <= tiles && s <= 128; ++s) {
@@ -133,28 +133,24 @@ void state_attention(const Model& m, char* state, int index, CachedArgs* out) {
   *out = a;
 }
 
+int error_word(int** out) {
+  static std::atomic<int*> cached[64];
+  const int dev = device_index();
+  if (dev >= 0)
+    if (int* p = cached[dev].load(std::memory_order_acquire)) {
+      *out = p;
+      return SWAPNET_OK;
+    }
+  if (int rc = tc_error_word(out)) return rc;
+  if (dev >= 0) cached[dev].store(*out, std::memory_order_release);
+  return SWAPNET_OK;
+}
+
 int cached_launches(const CachedArgs& a, const CachedPlan& p) {
   return 1 + (p.splits != 1 || p.spill ? 1 : 0) + (a.weights && !p.spill ? 1 : 0);
 }
 
 namespace {
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-// int32 and float arrays: single elements are read and written
-template <typename... P> bool aligned4(const P*... p) { return ((... | (uintptr_t)p) & 3) == 0; }
-
-// Whether a result is one of the inputs, or another result, by its address
-// (null ones are not there); ranges are the caller's: caches may be interleaved.
-bool shares(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins) {
-  for (const void* const* o = outs.begin(); o != outs.end(); ++o) {
-    if (!*o) continue;
-    for (const void* in : ins)
-      if (*o == in) return true;
-    for (const void* const* p = outs.begin(); p != o; ++p)
-      if (*o == *p) return true;
-  }
-  return false;
-}
 
 // What both attention entry points require of their arguments.
 int fill_args(const swapnet_cached_attention* c, CachedArgs* a) {
@@ -227,20 +223,6 @@ int check_attention(const swapnet_cached_attention* c, CachedArgs* a) {
   if (c->weights_in && !c->weights) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention: weights_in without weights");
   if (c->weights && cached_plan(*a).spill == 0 && !c->lse)
     SN_FAIL(SWAPNET_ERR_INVALID_ARG, "attention: weights of more than 16 rows (tokens x heads / kv_heads) need lse");
-  return SWAPNET_OK;
-}
-
-// The device error word of the current device (looked up once per device).
-int error_word(int** out) {
-  static std::atomic<int*> cached[64];
-  const int dev = device_index();
-  if (dev >= 0)
-    if (int* p = cached[dev].load(std::memory_order_acquire)) {
-      *out = p;
-      return SWAPNET_OK;
-    }
-  if (int rc = tc_error_word(out)) return rc;
-  if (dev >= 0) cached[dev].store(*out, std::memory_order_release);
   return SWAPNET_OK;
 }
 

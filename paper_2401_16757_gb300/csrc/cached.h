@@ -6,6 +6,7 @@
 #include <cuda_runtime.h>
 #include <algorithm>
 #include <cstdint>
+#include <initializer_list>
 
 namespace swapnet {
 
@@ -59,6 +60,29 @@ CachedPlan cached_plan(const CachedArgs& a);
 int run_cached_attention(CachedArgs a, const CachedPlan& p, void* workspace, bool early, cudaStream_t s);
 inline uint64_t plan_bytes(const CachedPlan& p) { return p.part_bytes + p.ml_bytes + p.score_bytes + p.unit_bytes; }
 int cached_launches(const CachedArgs& a, const CachedPlan& p);
+
+// How many CTAs share the keys of one of `ctas` units (cached.cpp).
+int choose_splits(int64_t ctas, int tiles, double alone, double busy, double fixed, double join);
+// The device error word of the current device (looked up once per device).
+int error_word(int** out);
+
+// What the entry points check of their pointers.
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+// int32 and float arrays: single elements are read and written
+template <typename... P> inline bool aligned4(const P*... p) { return ((... | (uintptr_t)p) & 3) == 0; }
+
+// Whether a result is one of the inputs, or another result, by its address
+// (null ones are not there); ranges are the caller's: caches may be interleaved.
+inline bool shares(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins) {
+  for (const void* const* o = outs.begin(); o != outs.end(); ++o) {
+    if (!*o) continue;
+    for (const void* in : ins)
+      if (*o == in) return true;
+    for (const void* const* p = outs.begin(); p != o; ++p)
+      if (*o == *p) return true;
+  }
+  return false;
+}
 
 int launch_attention_rows(const CachedArgs& a, bool early, cudaStream_t s);  // tcgen05
 int launch_attention_few(const CachedArgs& a, bool early, cudaStream_t s);

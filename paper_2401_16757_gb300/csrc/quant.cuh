@@ -1,0 +1,102 @@
+// Device-side pieces of the attention over a cache of 8-bit codes: codes to
+// fp16, queries to fp16, scales.
+#pragma once
+#include "cached.cuh"
+#include "quant.h"
+
+namespace swapnet {
+
+// Byte offset of 16-byte chunk `c` of row `r` in a tile of D-byte rows: chunks
+// are exchanged so that the eight rows of an 8 x 8 matrix lie in different
+// banks.
+template <int D> __device__ __forceinline__ uint32_t swz8(uint32_t r, uint32_t c) {
+  if (D == 128) return r * 128 + ((c ^ (r & 7)) << 4);
+  return r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
+}
+__device__ __forceinline__ void cp_async_4(uint32_t dst, const void* src, bool valid) {
+  const int n = valid ? 4 : 0;  // 0: write zeros, read nothing
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+// An 8 x 8 matrix of 16-bit elements, transposed across the warp.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+// Two codes as fp16 numbers: bytes of x that `sel` (a byte permutation with a
+// second word of 0x64 or 0) brings into place.
+// I8: 1024 + (code + 128) as the byte below an exponent, less 1152: exact.
+// E4M3: sign, exponent and fraction moved into fp16's places, which gives
+// code * 2^-8, subnormal ones included (the two codes that are no numbers give
+// a finite one: the block's scale says what they are).
+__device__ __forceinline__ uint32_t i8_pair(uint32_t flipped, uint32_t sel) {
+  const uint32_t u = __byte_perm(flipped, 0x64646464u, sel);
+  const __half2 r = __hsub2(reinterpret_cast<const __half2&>(u), __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480)));
+  return reinterpret_cast<const uint32_t&>(r);
+}
+__device__ __forceinline__ uint32_t e4m3_pair(uint32_t x, uint32_t sel) {
+  const uint32_t z = __byte_perm(x, 0u, sel);  // the codes in the upper bytes
+  return (z & 0x80008000u) | ((z >> 1) & 0x3f803f80u);
+}
+// bytes (0, 1) and (2, 3)
+template <int CODE> __device__ __forceinline__ uint2 pairs_near(uint32_t x) {
+  if (CODE == kCodeI8) {
+    const uint32_t f = x ^ 0x80808080u;
+    return make_uint2(i8_pair(f, 0x4140), i8_pair(f, 0x4342));
+  }
+  return make_uint2(e4m3_pair(x, 0x1404), e4m3_pair(x, 0x3424));
+}
+// bytes (0, 2) and (1, 3)
+template <int CODE> __device__ __forceinline__ uint2 pairs_apart(uint32_t x) {
+  if (CODE == kCodeI8) {
+    const uint32_t f = x ^ 0x80808080u;
+    return make_uint2(i8_pair(f, 0x4240), i8_pair(f, 0x4341));
+  }
+  return make_uint2(e4m3_pair(x, 0x2404), e4m3_pair(x, 0x3414));
+}
+// What a code's fp16 form is to be multiplied by.
+template <int CODE> __device__ __forceinline__ float code_unit() { return CODE == kCodeE4M3 ? 256.0f : 1.0f; }
+
+// scale = 2^e * f with f in [1, 2) and inv = 2^-e; scales below 2^-100 count as
+// that, those that are no number or infinite keep f so.
+__device__ __forceinline__ void split_scale(float scale, float* e, float* f, float* inv) {
+  scale = scale < kLeastScale ? kLeastScale : scale;
+  const int x = min((int)(__float_as_uint(scale) >> 23 & 0xffu), 253);
+  *inv = __uint_as_float((uint32_t)(254 - x) << 23);
+  *f = scale * *inv;
+  *e = (float)(x - 127);
+}
+
+// A query's C x 4 elements of this lane (four lanes of a row) as fp16 pairs,
+// and the power of two that they were divided by: fp16 as it is, bf16 with the
+// largest element of the row in [2^14, 2^15), so that what fp16 loses is below
+// 2^-39 of it.
+template <typename T, int C> __device__ __forceinline__ float query_fp16(const uint2 (&raw)[C], uint32_t (&out)[C][2]) {
+  if (std::is_same<T, __half>::value) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      out[c][0] = raw[c].x;
+      out[c][1] = raw[c].y;
+    }
+    return 1.0f;
+  }
+  uint32_t most = 0u;
+#pragma unroll
+  for (int c = 0; c < C; ++c) most = __vmaxu2(__vmaxu2(most, raw[c].x & 0x7fff7fffu), raw[c].y & 0x7fff7fffu);
+  most = max(most & 0xffffu, most >> 16);
+  most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+  most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+  // exponent field of the largest: 2^(x - 127) <= it < 2^(x - 126); infinities keep theirs
+  const int x = min(max((int)(most >> 7), 28), 254);
+  const float by = __uint_as_float((uint32_t)(127 + 14 - (x - 127)) << 23);
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const float2 u = unpack_pair<__nv_bfloat16>(raw[c].x), w = unpack_pair<__nv_bfloat16>(raw[c].y);
+    out[c][0] = pack_pair<__half>(u.x * by, u.y * by);
+    out[c][1] = pack_pair<__half>(w.x * by, w.y * by);
+  }
+  return __uint_as_float((uint32_t)(127 + (x - 127) - 14) << 23);
+}
+
+}  // namespace swapnet
