@@ -24,7 +24,7 @@ struct AppendArgs {
   int* lens_out;
   int64_t q_stride, new_stride, out_stride, kv_stride, seq_stride;  // elements
   int* err;
-  int row_ctas, block_ctas;  // of a sequence: for rows in 16 bits, for blocks
+  int q_ctas, kv_ctas, row_ctas, block_ctas;  // of a sequence: for queries, for 16-bit keys (and as many for values), all these; for blocks
   float2 turns[64];          // a pair's turns per position, as the sum of two numbers
 };
 int launch_cache_append(AppendArgs a, cudaStream_t s);

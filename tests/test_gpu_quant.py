@@ -315,6 +315,34 @@ def test_append_of_values_that_are_no_numbers(fmt):
         assert (a == b).all()
 
 
+@pytest.mark.parametrize("dtype,bits", [("f16", 10), ("bf16", 7)])
+def test_i8_codes_are_the_rounded_quotients(dtype, bits):
+    """Every fraction of a largest magnitude against every fraction of a value, at each distance of their exponents that a
+    code tells apart: the code is the quotient by the scale as fp32 rounds it, rounded to the nearest, ties to even."""
+    torch = _torch()
+    n, dt = 1 << bits, _dt(dtype)
+    most = torch.arange(n, 2 * n, device="cuda", dtype=torch.float32)  # a head each
+    x = most[None].repeat(n, 1)
+    for shift in range(9):
+        y = (x * 2.0 ** -shift).clamp(max=most[:, None]).to(dt)
+        rows = torch.zeros(n, 1024, dtype=dt, device="cuda")  # 16 rows of 64 elements a head
+        rows[:, :n] = y
+        rows[:, 0] = most
+        rows[:, 1::2] *= -1
+        k = rows.view(n, 16, 64).transpose(0, 1).contiguous().view(1, 16, n * 64)
+        codes, scale = torch.zeros(2, 16, n * 64, dtype=torch.int8, device="cuda"), torch.zeros(2, n, device="cuda")
+        room, lens = torch.zeros_like(k), torch.zeros(1, dtype=torch.int32, device="cuda")
+        capi.cache_append(dtype, "i8", 1, 16, 0, n, 64, 16, k_new=k.data_ptr(), v_new=k.data_ptr(), lens=lens.data_ptr(),
+                          k=codes[0].data_ptr(), v=codes[1].data_ptr(), k_scale=scale[0].data_ptr(), v_scale=scale[1].data_ptr(),
+                          k_open=room.data_ptr(), v_open=room.data_ptr() + 32 * n, block=16, stream=_stream())
+        capi.device_sync()
+        want = most.cpu().numpy() / np.float32(127)
+        assert (scale[0].cpu().numpy() == want).all() and (scale[1].cpu().numpy() == want).all()
+        want = np.rint(rows.float().cpu().numpy() / want[:, None])
+        for c in codes:
+            assert (c.view(16, n, 64).transpose(0, 1).reshape(n, 1024).cpu().numpy() == want).all()
+
+
 def test_queries_in_place_on_a_stream_of_their_own_and_in_a_graph():
     torch = _torch()
     kw = dict(dtype="bf16", fmt="e4m3", n_seq=3, tokens=2, heads=8, kv_heads=2, dim=128, max_seq=64, block=16, lens=[15, 3, 40], norm=True)
