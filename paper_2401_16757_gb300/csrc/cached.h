@@ -86,6 +86,8 @@ inline bool shares(std::initializer_list<const void*> outs, std::initializer_lis
 
 int launch_attention_rows(const CachedArgs& a, bool early, cudaStream_t s);  // tcgen05
 int launch_attention_few(const CachedArgs& a, bool early, cudaStream_t s);
+// The units that several CTAs of a tensor-core attention shared (row_tile rows a slot).
+int launch_runs_join(const CachedArgs& a, int queries, int row_tile, int nrt, cudaStream_t s);
 int launch_attention_join(const CachedArgs& a, cudaStream_t s);   // splits -> out, lse (and weights from scores)
 int launch_weights(const CachedArgs& a, int splits, bool early, cudaStream_t s);  // tcgen05
 int weights_splits(const CachedArgs& a);

@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kQfWarps = 4, kQfThreads = 32 * kQfWarps;
 constexpr int kStep = 32;     // keys of a warp's step
-constexpr int kQfStages = 3;
+constexpr int kQfStages = 2;
 constexpr float kTop = 14.0f; // log2 of the largest p: times its scale's fraction below 2 it stays within fp16
 
 template <int D, int NR> struct QfCfg {
@@ -56,7 +56,7 @@ template <int D, int NR> struct QfCfg {
 // m grows only where a score passes the largest so far; until then nothing is
 // rescaled and no lane asks another.
 template <typename T, int D, int CODE, int NR>
-__global__ void __launch_bounds__(kQfThreads, 2) attention_quant_few_kernel(const __grid_constant__ QuantArgs a, int row_tiles) {
+__global__ void __launch_bounds__(kQfThreads, NR == 1 ? 3 : 2) attention_quant_few_kernel(const __grid_constant__ QuantArgs a, int row_tiles) {
   using F = QfCfg<D, NR>;
   extern __shared__ __align__(128) uint8_t smem[];
   float2* mls = reinterpret_cast<float2*>(smem + F::kOffMl);
@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(kQfThreads, 2) attention_quant_few_kernel(cons
     for (int c = 0; c < C; ++c) raw[c] = on ? *reinterpret_cast<const uint2*>(q + c * 16) : make_uint2(0u, 0u);
     const float s = query_fp16<T, C>(raw, qf[n]);
 #pragma unroll
-    for (int e = 0; e < 2; ++e) qs[n][e] = __shfl_sync(0xffffffffu, s, ((lane & 3) * 2 + e) * 4) * a.scale_log2 * code_unit<CODE>();
+    for (int e = 0; e < 2; ++e) qs[n][e] = __shfl_sync(0xffffffffu, s, ((lane & 3) * 2 + e) * 4) * a.scale_log2;
   }
   int lim[NR][2];
 #pragma unroll
@@ -209,6 +209,18 @@ __global__ void __launch_bounds__(kQfThreads, 2) attention_quant_few_kernel(cons
           for (int e = 0; e < 4; ++e) o[d][n][e] *= al[e & 1];
       }
     }
+    if (CODE == kCodeE4M3 && masked) {
+      // a hidden value row must not reach the rows that do not see it: its
+      // codes may be no numbers (0 x NaN); a seen one's scale says so
+      uint8_t* vs = ring + slot * F::kSlot + F::kTile;
+#pragma unroll
+      for (int i = 0; i < kStep * C / 32; ++i) {
+        uint4* at = reinterpret_cast<uint4*>(vs + (lane + i * 32) * 16);
+        const uint4 v = *at;
+        *at = make_uint4(numbers_only(v.x), numbers_only(v.y), numbers_only(v.z), numbers_only(v.w));
+      }
+      __syncwarp();
+    }
     uint32_t pt[2][NR][2][2];  // P^T: [part of the keys][rows][hi, lo][keys 0..7, 8..15]
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
@@ -267,7 +279,7 @@ __global__ void __launch_bounds__(kQfThreads, 2) attention_quant_few_kernel(cons
 #pragma unroll
       for (int d = 0; d < D / 16; ++d)
         *reinterpret_cast<float2*>(ow + r * D + d * 16 + (lane >> 2) * 2) =
-            make_float2(o[d][n][e] * code_unit<CODE>(), o[d][n][e + 2] * code_unit<CODE>());
+            make_float2(o[d][n][e], o[d][n][e + 2]);
     }
   __syncthreads();
   constexpr int V = D / 4;  // float4 per row

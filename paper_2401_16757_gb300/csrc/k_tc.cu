@@ -468,7 +468,7 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   return fn;
 }
 
-// A tiled map of 16-bit elements with zero fill.  The CUDA driver's call needs a
+// A tiled map of 16-bit elements (I8: of bytes) with zero fill.  The CUDA driver's call needs a
 // current context, which a thread whose first CUDA call leads here does not
 // have yet (the runtime binds one at its own calls): bind that of the thread's
 // device and ask again.
@@ -477,7 +477,7 @@ CUresult encode_tiled(CUtensorMap* m, int dtype, int rank, const void* base, con
   auto fn = encode_fn();
   if (!fn) return CUDA_ERROR_NOT_FOUND;
   auto encode = [&] {
-    return fn(m, dtype == SWAPNET_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)rank,
+    return fn(m, dtype == SWAPNET_I8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : dtype == SWAPNET_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)rank,
               const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   };
@@ -951,6 +951,16 @@ int make_tmap_3d(CUtensorMap* m, int dtype, const void* base, const uint64_t (&d
   const cuuint64_t d[3] = {dims[0], dims[1], dims[2]}, st[2] = {stride_bytes[0], stride_bytes[1]};
   const cuuint32_t b[3] = {box[0], box[1], box[2]}, estr[3] = {1, 1, 1};
   const CUresult r = encode_tiled(m, dtype, 3, base, d, st, b, estr, CU_TENSOR_MAP_SWIZZLE_128B);
+  if (r != CUDA_SUCCESS) SN_FAIL(SWAPNET_ERR_CUDA, "cuTensorMapEncodeTiled failed (" + std::to_string((int)r) + ")");
+  return SWAPNET_OK;
+}
+
+int make_tmap_codes(CUtensorMap* m, const void* base, const uint64_t (&dims)[3], const uint64_t (&stride_bytes)[2], const uint32_t (&box)[3]) {
+  if (((uintptr_t)base & 15) || ((stride_bytes[0] | stride_bytes[1]) & 15) || box[0] % 16)
+    SN_FAIL(SWAPNET_ERR_MISALIGNED, "TMA operand must be 16-byte aligned with 16-byte multiple strides");
+  const cuuint64_t d[3] = {dims[0], dims[1], dims[2]}, st[2] = {stride_bytes[0], stride_bytes[1]};
+  const cuuint32_t b[3] = {box[0], box[1], box[2]}, estr[3] = {1, 1, 1};
+  const CUresult r = encode_tiled(m, SWAPNET_I8, 3, base, d, st, b, estr, CU_TENSOR_MAP_SWIZZLE_NONE);
   if (r != CUDA_SUCCESS) SN_FAIL(SWAPNET_ERR_CUDA, "cuTensorMapEncodeTiled failed (" + std::to_string((int)r) + ")");
   return SWAPNET_OK;
 }

@@ -11,12 +11,33 @@
 
 namespace swapnet {
 
+// Microseconds of the tensor-core kernel: a unit's start and end, a tile of
+// keys, the join of shared units.
+constexpr double kUnitUs = 5.0, kTileUs = 1.0, kJoinUs = 8.0;
+
 CachedPlan quant_plan(const QuantArgs& a) {
   CachedPlan p;
   std::memset(&p, 0, sizeof(p));
   const int64_t rows = (int64_t)a.tokens * a.group, pairs = (int64_t)a.n_seq * a.kv_heads;
-  const int64_t tiles = (rows + kFewAttnRows - 1) / kFewAttnRows;
-  p.splits = choose_splits(pairs * tiles, (a.max_seq + 127) / 128, 0.5, 0.7, 1.5, 2.5);
+  p.tc = rows > kFewAttnRows;
+  if (p.tc) {
+    const int row_tile = rows <= 64 ? 64 : 128, queries = std::min(row_tile / a.group, a.tokens);
+    const int64_t units = pairs * ((a.tokens + queries - 1) / queries);
+    // a CTA per unit, or equal runs of all tiles and a join (see cached_plan)
+    const double tiles = (a.max_seq + 127) / 128;
+    const int ctas = run_ctas(a.kv_heads);
+    const double alone = std::ceil((double)units / kSms) * (kUnitUs + tiles * kTileUs);
+    const double shared = kUnitUs + std::max(2.0, units * tiles / ctas) * kTileUs + (double)units / ctas + kJoinUs;
+    p.splits = units >= 2 * kSms || alone <= shared ? 1 : 0;
+    if (units > 0x7fffffff) p.splits = 0;
+    if (p.splits == 0) {
+      p.part_bytes = align_up((uint64_t)2 * ctas * row_tile * a.dim * 4);
+      p.ml_bytes = align_up((uint64_t)2 * ctas * row_tile * 8);
+      p.unit_bytes = align_up((uint64_t)ctas * 16);
+    }
+    return p;
+  }
+  p.splits = choose_splits(pairs, (a.max_seq + 127) / 128, 0.5, 0.7, 1.5, 2.5);
   if (p.splits > 1) {
     p.part_bytes = align_up((uint64_t)pairs * rows * p.splits * a.dim * 4);
     p.ml_bytes = align_up((uint64_t)pairs * rows * p.splits * 8);
@@ -29,6 +50,8 @@ int run_quant_attention(QuantArgs a, const CachedPlan& p, void* workspace, cudaS
   a.splits = p.splits;
   a.part = reinterpret_cast<float*>(w);
   a.ml = reinterpret_cast<float*>(w + p.part_bytes);
+  a.units = reinterpret_cast<int4*>(w + p.part_bytes + p.ml_bytes);
+  if (p.tc) return launch_quant_rows(a, s);
   if (int rc = launch_quant_few(a, s)) return rc;
   return launch_attention_join(a, s);
 }

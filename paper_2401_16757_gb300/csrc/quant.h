@@ -38,6 +38,7 @@ struct QuantArgs : CachedArgs {
 // How a call runs, from its sizes alone.
 CachedPlan quant_plan(const QuantArgs& a);
 int run_quant_attention(QuantArgs a, const CachedPlan& p, void* workspace, cudaStream_t s);
-int launch_quant_few(const QuantArgs& a, cudaStream_t s);
+int launch_quant_few(const QuantArgs& a, cudaStream_t s);   // up to 16 rows a (sequence, key head)
+int launch_quant_rows(const QuantArgs& a, cudaStream_t s);  // tcgen05, with the join
 
 }  // namespace swapnet
