@@ -23,7 +23,6 @@
 #include <string>
 #include <type_traits>
 
-#include "cached_tc.cuh"
 #include "internal.h"
 #include "kernels.h"
 #include "quant.cuh"
@@ -49,7 +48,8 @@ template <int D> struct QtCfg {
   static constexpr int kBox = 128 * 128;              // bytes of a 128-row x 64-element fp16 box
   static constexpr int kTile = kHalves * kBox;
   static constexpr int kRaw = 128 * D;                // bytes of a tile's codes
-  static constexpr int kSlots = 4, kRawSlots = D == 128 ? 3 : 6;
+  static constexpr int kSlots = 4;  // two pairs
+  static constexpr int kRawSlots = D == 128 ? 3 : 6;
   static constexpr int kOffQ = 0;
   static constexpr int kOffRing = kTile;
   static constexpr int kOffRaw = kOffRing + kSlots * kTile;
@@ -62,25 +62,24 @@ template <int D> struct QtCfg {
 };
 
 // The power of two that a BF16 query row is divided by: its largest element
-// comes to lie in [2^14, 2^15).  Exponent field of the largest magnitude, kept
-// where both factors are normal numbers.
-template <typename T, int D> __device__ __forceinline__ int query_exponent(const T* q) {
-  if (std::is_same<T, __half>::value) return 127 + 14;  // (as it is)
-  uint32_t most = 0u;
-  for (int c = 0; c < D / 8; c += 4) {
-    uint4 v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = reinterpret_cast<const uint4*>(q)[c + i];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      most = __vmaxu2(__vmaxu2(__vmaxu2(__vmaxu2(most, v[i].x & 0x7fff7fffu), v[i].y & 0x7fff7fffu), v[i].z & 0x7fff7fffu), v[i].w & 0x7fff7fffu);
-  }
-  return min(max((int)(max(most & 0xffffu, most >> 16) >> 7), 28), 254);
+// comes to lie in [2^14, 2^15).  From the bits of the largest magnitude its
+// exponent field, kept where both factors are normal numbers.
+__device__ __forceinline__ uint32_t largest_bits(const uint4& v) {
+  const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+  return max(m & 0xffffu, m >> 16);
 }
-template <typename T> __device__ __forceinline__ uint32_t query_pair(uint32_t x, float by) {
-  if (std::is_same<T, __half>::value) return x;
+__device__ __forceinline__ int query_exponent(uint32_t most) { return min(max((int)(most >> 7), 28), 254); }
+__device__ __forceinline__ uint32_t query_pair(uint32_t x, float by) {
   const float2 u = unpack_pair<__nv_bfloat16>(x);
   return pack_pair<__half>(u.x * by, u.y * by);
+}
+// What a row's queries have been divided by.
+template <typename T, int D> __device__ __forceinline__ float query_scale(const T* q) {
+  if (std::is_same<T, __half>::value) return 1.0f;  // (as they are)
+  uint32_t most = 0u;
+#pragma unroll
+  for (int c = 0; c < D / 8; ++c) most = max(most, largest_bits(reinterpret_cast<const uint4*>(q)[c]));
+  return __uint_as_float((uint32_t)(query_exponent(most) - 14) << 23);
 }
 
 __device__ __forceinline__ float2 mul2(float2 x, float2 y) {
@@ -99,16 +98,17 @@ __global__ void __launch_bounds__(kQtThreads, 1)
   constexpr int kRowsMax = 128 / REP;
   constexpr int NK = 64 / REP;  // keys of a thread and tile
   constexpr int NG = NK / 16;   // parts of them
+  constexpr int kParts = 2;  // of a probability
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   float2* ml = reinterpret_cast<float2*>(smem + F::kOffX);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + F::kOffBar);
-  auto full = [&](int s) { return smem_u32(bars + s); };            // an fp16 tile
-  auto empty = [&](int s) { return smem_u32(bars + 4 + s); };
-  auto raw_full = [&](int s) { return smem_u32(bars + 8 + s); };    // its codes
+  auto full = [&](int j) { return smem_u32(bars + (j & 1)); };      // a pair of fp16 tiles
+  auto empty = [&](int j) { return smem_u32(bars + 4 + (j & 1)); };
+  auto raw_full = [&](int s) { return smem_u32(bars + 8 + s); };    // a tile's codes
   auto raw_empty = [&](int s) { return smem_u32(bars + 14 + s); };
-  // one per half and buffer: a half may be two tiles ahead of the products
-  auto s_full = [&](int h, int i) { return smem_u32(bars + 20 + 2 * h + (i & 1)); };
+  // (P: one per half and buffer, a half may be two tiles ahead of the products)
+  auto s_full = [&](int i) { return smem_u32(bars + 20 + (i & 1)); };
   auto p_full = [&](int h, int i) { return smem_u32(bars + 24 + 2 * h + (i & 1)); };
   auto o_full = [&](int h) { return smem_u32(bars + 28 + h); };
   const uint32_t q_full = smem_u32(bars + 30), q_free = smem_u32(bars + 31);  // a piece's queries
@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(kQtThreads, 1)
 
   const int warp = warp_index(), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < F::kSlots; ++s) {
+    for (int s = 0; s < 2; ++s) {
       mbar_init(full(s), kConvThreads / 32);
       mbar_init(empty(s), 1);
     }
@@ -131,10 +131,8 @@ __global__ void __launch_bounds__(kQtThreads, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(o_full(i), 1);
-      for (int h = 0; h < 2; ++h) {
-        mbar_init(s_full(h, i), 1);
-        mbar_init(p_full(h, i), 4);
-      }
+      mbar_init(s_full(i), 1);
+      for (int h = 0; h < 2; ++h) mbar_init(p_full(h, i), 4);
     }
     mbar_init(q_full, kConvThreads / 32);
     mbar_init(q_free, 1);
@@ -152,167 +150,125 @@ __global__ void __launch_bounds__(kQtThreads, 1)
   }
   pdl_wait();
   Cursor cur;
-  cur.next = 0;
-  const int kvh = blockIdx.x % a.kv_heads, run = blockIdx.x / a.kv_heads;
-  // sizes of the sequences from b0 on (with runs and more sequences than that, from the run's first)
-  cur.b0 = a.splits == 1 ? run / nrt : 0;
-  cur.near = near;
-  auto fetch_near = [&]() {
-    if (threadIdx.x < kNear && cur.b0 + (int)threadIdx.x < a.n_seq) near[threadIdx.x] = seq_size(a, cur.b0 + threadIdx.x);
-  };
-  if (a.splits == 1 || a.n_seq <= kNear) fetch_near();
-  int64_t first_tile = 0, total = 0;  // the run's first tile in the order of all; their number
-  int runs = 1;
-  if (a.splits == 1) {
-    cur.pair = run;
-    const PairSize z = pair_size(a, seq_size(a, cur.pair / nrt), cur.pair % nrt, queries);
-    cur.left = z.tiles;
-    if (z.tiles == 0 && threadIdx.x == 0 && kvh == 0) {
-      int len, count;
-      seq_sizes(a, cur.pair / nrt, &len, &count);  // (reports what is out of range)
-    }
-    tc_fence_before();
-  } else {
-    // every thread adds up a run of pairs, then the threads' sums
-    const int pairs = a.n_seq * nrt, per = (pairs + kQtThreads - 1) / kQtThreads;
-    const int p0 = min((int)threadIdx.x * per, pairs), p1 = min(p0 + per, pairs);
-    int64_t sum = 0;
-    for (int p = p0; p < p1; ++p) {
-      const int2 size = seq_size(a, p / nrt);
-      sum += pair_size(a, size, p % nrt, queries).tiles;
-      if (blockIdx.x == 0 && (size.x < 0 || size.x > a.max_seq || size.y < 0 || size.y > a.tokens)) atomicExch(a.err, kDevErrBounds);
-    }
-    int64_t before = sum;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const int64_t o = __shfl_up_sync(0xffffffffu, before, off);
-      if (lane >= off) before += o;
-    }
-    if (lane == 31) sched[warp] = before;
-    before -= sum;
-    tc_fence_before();
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kQtThreads / 32; ++w) {
-      if (w < warp) before += sched[w];
-      total += sched[w];
-    }
-    runs = (int)min((int64_t)(gridDim.x / a.kv_heads), (total + kRunTiles - 1) / kRunTiles);
-    first_tile = run < runs ? total * run / runs : total;
-    cur.left = run < runs ? total * (run + 1) / runs - first_tile : 0;
-    cur.pair = 0;
-    if (cur.left > 0 && before <= first_tile && first_tile < before + sum) {
-      int64_t at = before;
-      for (int p = p0; p < p1; ++p) {
-        const int tiles = pair_size(a, seq_size(a, p / nrt), p % nrt, queries).tiles;
-        if (first_tile < at + tiles) {
-          sched[20] = p;
-          sched[21] = first_tile - at;
-          break;
-        }
-        at += tiles;
-      }
-    }
-    __syncthreads();
-    if (cur.left > 0) {
-      cur.pair = (int)sched[20];
-      cur.next = (int)sched[21];
-    }
-    if (a.n_seq > kNear) {
-      cur.b0 = cur.pair / nrt;
-      fetch_near();
-    }
-  }
+  tc_fence_before();
+  const Run r_ = start_run(a, cur, near, sched, queries, nrt);
+  const int kvh = r_.kvh;
   __syncthreads();  // (and sched is written again, as ml)
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   // (not before this CTA has its TMEM: a kernel that starts early may hold some
   // while it waits for this one's end)
   pdl_launch_dependents();
-  // a piece's tiles in the order of use: K0, K1, V0, K2, V1, ..., V(n-1)
-  auto k_pos = [&](int i) { return i == 0 ? 0 : 2 * i - 1; };
-  auto v_pos = [&](int i, int n) { return i == n - 1 ? 2 * n - 1 : 2 * i + 2; };
+  // The run's tiles are taken in pairs: the keys of tile j with the values of tile
+  // j - 1, across pieces; the last pair has values alone.  Tiles(j) yields them,
+  // for every role in one loop (one place in the code for what it does: the CTA's
+  // warps run five programs, whose instructions share the caches).
+  struct Pair {
+    bool keys, values, first, last;    // what there is; the keys' tile is its piece's first, last
+    bool v_first, v_last;              // the same of the values' tile
+    int b, tile, v_b, v_tile, piece, v_piece;
+  };
+  Pair pr;
+  pr.keys = false;
+  pr.piece = -1;
+  int at = 0, of = 0;  // tile of the piece, its tiles
+  auto next_pair = [&](int j) -> bool {  // j = 0, 1, 2, ...
+    pr.values = j > 0;
+    pr.v_first = pr.first;
+    pr.v_last = pr.last;
+    pr.v_b = pr.b;
+    pr.v_tile = pr.tile;
+    pr.v_piece = pr.piece;
+    if (j > 0 && !pr.keys) return false;  // (the last pair has been)
+    if (at == of) {
+      pr.keys = cur.step(a, nrt, queries);
+      at = 0;
+      of = pr.keys ? cur.n : 0;
+      if (pr.keys) ++pr.piece;
+    }
+    if (!pr.keys) return j > 0;
+    pr.first = at == 0;
+    pr.last = at == of - 1;
+    pr.b = cur.b;
+    pr.tile = cur.i0 + at;
+    ++at;
+    return true;
+  };
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
     if (warp == 0 && elect_one()) {
-      // ---------------- TMA producer: a tile's codes
+      // ---------------- TMA producer: the tiles' codes
       int pos = 0;
       bool ok = true;
-      while (ok && cur.step(a, nrt, queries)) {
-        auto load = [&](int i, bool keys) -> bool {
+      for (int j = 0; ok && next_pair(j); ++j) {
+#pragma unroll 1
+        for (int part = 0; part < 2; ++part) {
+          if (!(part ? pr.values : pr.keys)) continue;
           const int s = pos % F::kRawSlots;
-          if (pos >= F::kRawSlots && !mbar_wait_bounded(raw_empty(s), ((pos / F::kRawSlots) - 1) & 1, abort_flag, a.err)) return false;
+          if (pos >= F::kRawSlots && !(ok = mbar_wait_bounded(raw_empty(s), ((pos / F::kRawSlots) - 1) & 1, abort_flag, a.err))) break;
           mbar_arrive_expect_tx(raw_full(s), F::kRaw);
-          tma_load_3d(smem_u32(smem + F::kOffRaw + s * F::kRaw), keys ? &tmK : &tmV, raw_full(s), kvh * D, (cur.i0 + i) * kKeys, cur.b);
+          tma_load_3d(smem_u32(smem + F::kOffRaw + s * F::kRaw), part ? &tmV : &tmK, raw_full(s), kvh * D,
+                      (part ? pr.v_tile : pr.tile) * kKeys, part ? pr.v_b : pr.b);
           ++pos;
-          return true;
-        };
-        ok = load(0, true) && (cur.n < 2 || load(1, true));
-        for (int i = 0; ok && i < cur.n; ++i) ok = load(i, false) && (i + 2 >= cur.n || load(i + 2, true));
+        }
       }
       // let every load issued land before the CTA can exit
       volatile int no_abort = 0;
-      for (int j = max(0, pos - F::kRawSlots); j < pos; ++j)
-        mbar_wait_bounded(raw_full(j % F::kRawSlots), (j / F::kRawSlots) & 1, &no_abort, nullptr);
+      for (int p = max(0, pos - F::kRawSlots); p < pos; ++p)
+        mbar_wait_bounded(raw_full(p % F::kRawSlots), (p / F::kRawSlots) & 1, &no_abort, nullptr);
     }
     if (warp == 1 && elect_one()) {
       // ---------------- MMA issuer
-      constexpr uint32_t idesc_s = idesc_f16(0, 128, kKeys / 2);
+      constexpr uint32_t idesc_s = idesc_f16(0, 128, kKeys);
       constexpr uint32_t idesc_pv = idesc_f16(0, 128, D) | (1u << 16);  // B (values) MN-major
       const uint64_t qd = smem_desc_sw128(smem_u32(smem + F::kOffQ));
-      const uint64_t kd = smem_desc_sw128(smem_u32(smem + F::kOffRing)), vd = desc_mn(smem_u32(smem + F::kOffRing));
-      int pos0 = 0, g0 = 0;  // of the piece: ring position, tiles before
+      const uint64_t kd = smem_desc_sw128(smem_u32(smem + F::kOffRing)), vd = desc_mn(smem_u32(smem + F::kOffRing + F::kTile));
       bool ok = true;
-      auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_bounded(bar, parity, abort_flag, a.err); };
-      for (int piece = 0; ok && cur.step(a, nrt, queries); ++piece) {
-        const int n = cur.n;
-        // (the halves take turns, as in the 16-bit caches' attention)
-        auto scores = [&](int i, int h) -> bool {
-          const int pos = pos0 + k_pos(i), s = pos % F::kSlots, g = g0 + i;
-          if (h == 0 && !wait(full(s), (pos / F::kSlots) & 1)) return false;
-          // (over the P of two tiles ago: the tensor core runs the MMAs of one
-          // thread in the order of their issue, so its product, issued before,
-          // has read it)
-          tc_fence_after();
-          const uint64_t kt = kd + (uint64_t)(s * (F::kTile >> 4) + h * (64 * 128 >> 4));  // the descriptors' address field counts 16 bytes
+      auto wait = [&](uint32_t bar, uint32_t parity) { return ok = ok && mbar_wait_bounded(bar, parity, abort_flag, a.err); };
+      for (int j = 0; ok && next_pair(j); ++j) {
+        wait(full(j), (j >> 1) & 1);
+        const uint64_t kt = kd + (uint64_t)((j & 1) * (2 * F::kTile >> 4)), vt = vd + (uint64_t)((j & 1) * (2 * F::kTile >> 4));  // the descriptors' address field counts 16 bytes
+        // The next scores ahead of this tile's products, but for a new piece's,
+        // whose queries may not be there yet.
+#pragma unroll 1
+        for (int turn = 0; ok && turn < 2; ++turn) {
+          if ((turn == 1) == pr.first) {
+            if (!pr.keys || (pr.first && !wait(q_full, pr.piece & 1))) continue;
+            // (over the P of two tiles ago: the tensor core runs the MMAs of one
+            // thread in the order of their issue, so its product, issued before,
+            // has read it)
+            tc_fence_after();
 #pragma unroll
-          for (int c = 0; c < F::kHalves; ++c)
+            for (int c = 0; c < F::kHalves; ++c)
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              tc_mma_f16(tmem + (uint32_t)(g & 1) * 128u + (uint32_t)h * 64u, qd + (uint64_t)(c * (F::kBox >> 4) + 2 * k),
-                         kt + (uint64_t)(c * (F::kBox >> 4) + 2 * k), idesc_s, (c | k) != 0);
-          tc_commit(s_full(h, g));
-          if (h == 1) {
-            tc_commit(empty(s));
-            if (i == n - 1) tc_commit(q_free);
+              for (int k = 0; k < 4; ++k)
+                tc_mma_f16(tmem + (uint32_t)(j & 1) * 128u, qd + (uint64_t)(c * (F::kBox >> 4) + 2 * k),
+                           kt + (uint64_t)(c * (F::kBox >> 4) + 2 * k), idesc_s, (c | k) != 0);
+            tc_commit(s_full(j));
+            if (pr.last) tc_commit(q_free);
+            continue;
           }
-          return true;
-        };
-        ok = wait(q_full, piece & 1) && scores(0, 0) && scores(0, 1);
-        for (int i = 0; ok && i < n; ++i) {
-          const int pos = pos0 + v_pos(i, n), s = pos % F::kSlots, g = g0 + i;
-          const uint64_t vt = vd + (uint64_t)(s * (F::kTile >> 4));
-          for (int h = 0; ok && h < 2; ++h) {
-            if (i + 1 < n && !(ok = scores(i + 1, h))) break;
-            ok = (h == 1 || (wait(full(s), (pos / F::kSlots) & 1) && (i > 0 || piece == 0 || wait(o_free, (piece - 1) & 1)))) &&
-                 wait(p_full(h, g), (g >> 1) & 1);
-            if (!ok) break;
+          if (!pr.values) continue;
+          const int g = j - 1;
+          if (pr.v_first && pr.v_piece > 0) wait(o_free, (pr.v_piece - 1) & 1);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (!wait(p_full(h, g), (g >> 1) & 1)) break;
             tc_fence_after();
             const uint32_t pt = tmem + (uint32_t)(g & 1) * 128u + (uint32_t)h * 64u;
 #pragma unroll
-            for (int part = 0; part < 2; ++part)
+            for (int part = 0; part < kParts; ++part)
 #pragma unroll
               for (int ks = 0; ks < 4; ++ks)  // 16 keys a step
                 tc_mma_f16_ta(tmem + kTmO + (uint32_t)h * 128u, pt + (uint32_t)(part * 32 + ks * 8),
-                              vt + (uint64_t)((h * 4 + ks) * (2048 >> 4)), idesc_pv, (uint32_t)(i | part | ks) != 0);
+                              vt + (uint64_t)((h * 4 + ks) * (2048 >> 4)), idesc_pv, (uint32_t)(!pr.v_first || (part | ks) != 0));
             tc_commit(o_full(h));
           }
-          if (ok) tc_commit(empty(s));
         }
-        if (ok) tc_commit(o_done);
-        pos0 += 2 * n;
-        g0 += n;
+        if (!ok) break;
+        tc_commit(empty(j));
+        if (pr.values && pr.v_last) tc_commit(o_done);
       }
       // every MMA issued must have finished before TMEM is freed
       tc_commit(done_bar);
@@ -323,72 +279,101 @@ __global__ void __launch_bounds__(kQtThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsConv));
     // ---------------- codes and queries to fp16
     const int ct = threadIdx.x - 128;
-    int pos = 0;
-    bool ok = true;
-    for (int piece = 0; ok && cur.step(a, nrt, queries); ++piece) {
-      const int lim_min = visible_limit(a, cur.z.len, cur.z.count, cur.rt * queries);
-      auto convert = [&](int i, bool keys) {
-        const int rs = pos % F::kRawSlots, s = pos % F::kSlots;
-        ok = ok && mbar_wait_bounded(raw_full(rs), (pos / F::kRawSlots) & 1, abort_flag, a.err) &&
-             (pos < F::kSlots || mbar_wait_bounded(empty(s), ((pos / F::kSlots) - 1) & 1, abort_flag, a.err));
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) return;
-        const uint8_t* raw = smem + F::kOffRaw + rs * F::kRaw;
-        uint8_t* tile = smem + F::kOffRing + s * F::kTile;
-        const bool clear = CODE == kCodeE4M3 && !keys && (cur.i0 + i + 1) * kKeys > lim_min;  // some rows are hidden from some queries
-        // 16 codes a time: four lanes read 64 bytes of a row, their neighbours
-        // the other 64 of the next, so that neither the reads nor the swizzled
-        // stores meet in a bank
-        const int r0 = ct >> 2, l4 = ct & 3;
+    // 16 codes a time: four lanes read 64 bytes of a row, their neighbours the
+    // other 64 of the next, so that neither the reads nor the swizzled stores
+    // meet in a bank
+    const int r0 = ct >> 2;
+    uint32_t from[F::kHalves], to[F::kHalves][2];  // of this thread's first chunks: in the codes, in the fp16 tile
 #pragma unroll
-        for (int u = 0; u < 4 * F::kHalves; ++u) {
-          const int r = (u / F::kHalves) * 32 + r0;
-          const int c = F::kHalves == 2 ? l4 + 4 * ((r0 & 1) ^ (u & 1)) : l4;
-          uint4 v = *reinterpret_cast<const uint4*>(raw + r * D + c * 16);
-          if (clear) v = make_uint4(numbers_only(v.x), numbers_only(v.y), numbers_only(v.z), numbers_only(v.w));
-          const uint2 x = pairs_near<CODE>(v.x), y = pairs_near<CODE>(v.y), z = pairs_near<CODE>(v.z), w = pairs_near<CODE>(v.w);
-          uint8_t* to = tile + (c >> 2) * F::kBox + r * 128;
-          const int cc = (c & 3) * 2;
-          *reinterpret_cast<uint4*>(to + ((cc ^ (r & 7)) << 4)) = make_uint4(x.x, x.y, y.x, y.y);
-          *reinterpret_cast<uint4*>(to + (((cc | 1) ^ (r & 7)) << 4)) = make_uint4(z.x, z.y, w.x, w.y);
+    for (int u = 0; u < F::kHalves; ++u) {
+      const int c = (ct & 3) + (F::kHalves == 2 ? 4 * ((r0 & 1) ^ u) : 0);
+      from[u] = r0 * D + c * 16;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) to[u][e] = (c >> 2) * F::kBox + r0 * 128 + ((((c & 3) * 2 + e) ^ (r0 & 7)) << 4);
+    }
+    int pos = 0, lim_min = 0, v_lim_min = 0;
+    bool ok = true;
+    for (int j = 0; ok && next_pair(j); ++j) {
+      v_lim_min = lim_min;
+      if (pr.keys && pr.first) lim_min = visible_limit(a, cur.z.len, cur.z.count, cur.rt * queries);
+      ok = j < 2 || mbar_wait_bounded(empty(j), ((j >> 1) - 1) & 1, abort_flag, a.err);
+#pragma unroll 1
+      for (int part = 0; part < 2; ++part) {
+        if (!(part ? pr.values : pr.keys)) continue;
+        const int rs = pos % F::kRawSlots;
+        ok = ok && mbar_wait_bounded(raw_full(rs), (pos / F::kRawSlots) & 1, abort_flag, a.err);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        const uint8_t* raw = smem + F::kOffRaw + rs * F::kRaw;
+        uint8_t* tile = smem + F::kOffRing + ((j & 1) * 2 + part) * F::kTile;
+        uint4 v[4][F::kHalves];  // (all read before the first store, which might be to the same memory for what the compiler knows)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int u = 0; u < F::kHalves; ++u) v[r][u] = *reinterpret_cast<const uint4*>(raw + r * 32 * D + from[u]);
+        if (CODE == kCodeE4M3 && part && (pr.v_tile + 1) * kKeys > v_lim_min) {  // some rows are hidden from some queries
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int u = 0; u < F::kHalves; ++u)
+              v[r][u] = make_uint4(numbers_only(v[r][u].x), numbers_only(v[r][u].y), numbers_only(v[r][u].z), numbers_only(v[r][u].w));
         }
-        fence_proxy_async_smem();  // the tile is read by the tensor cores (async proxy)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int u = 0; u < F::kHalves; ++u) {
+            const uint2 x = pairs_near<CODE>(v[r][u].x), y = pairs_near<CODE>(v[r][u].y), z = pairs_near<CODE>(v[r][u].z),
+                        w = pairs_near<CODE>(v[r][u].w);
+            *reinterpret_cast<uint4*>(tile + r * 32 * 128 + to[u][0]) = make_uint4(x.x, x.y, y.x, y.y);
+            *reinterpret_cast<uint4*>(tile + r * 32 * 128 + to[u][1]) = make_uint4(z.x, z.y, w.x, w.y);
+          }
         __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(full(s));
-          mbar_arrive(raw_empty(rs));
-        }
+        if (lane == 0) mbar_arrive(raw_empty(rs));
         ++pos;
-      };
-      convert(0, true);
-      if (ok && cur.n > 1) convert(1, true);
+      }
       if (!ok) break;
-      // the piece's queries, a row per thread (REP 2: every row twice)
-      ok = piece == 0 || mbar_wait_bounded(q_free, (piece - 1) & 1, abort_flag, a.err);
+      fence_proxy_async_smem();  // the tiles are read by the tensor cores (async proxy)
+      __syncwarp();
+      if (lane == 0) mbar_arrive(full(j));
+      if (!(pr.keys && pr.first)) continue;
+      // a piece's queries: D / 8 lanes a row (REP 2: every row twice)
+      ok = pr.piece == 0 || mbar_wait_bounded(q_free, (pr.piece - 1) & 1, abort_flag, a.err);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      {
-        const int row = ct % kRowsMax, t0 = cur.rt * queries, rows = min(queries, cur.z.count - t0) * a.group;
-        if (row < rows) {
-          const T* q = static_cast<const T*>(a.q) + ((int64_t)cur.b * a.tokens + t0 + row / a.group) * a.q_stride +
-                       (int64_t)(kvh * a.group + row % a.group) * D;
-          const float by = __uint_as_float((uint32_t)(127 + 14 - (query_exponent<T, D>(q) - 127)) << 23);
-          uint8_t* to = smem + F::kOffQ + ct * 128;
-#pragma unroll 4
-          for (int c = 0; c < D / 8; ++c) {
-            const uint4 v = reinterpret_cast<const uint4*>(q)[c];
-            *reinterpret_cast<uint4*>(to + (c >> 3) * F::kBox + (((c & 7) ^ (ct & 7)) << 4)) =
-                make_uint4(query_pair<T>(v.x, by), query_pair<T>(v.y, by), query_pair<T>(v.z, by), query_pair<T>(v.w, by));
+      constexpr int L = D / 8, kPass = kConvThreads / L, kBatch = 8;  // rows of a pass, passes whose loads are on the way together
+      const int t0 = cur.rt * queries, rows = min(queries, cur.z.count - t0) * a.group, c = ct % L;
+#pragma unroll 1
+      for (int p0 = 0; p0 < rows; p0 += kBatch * kPass) {
+        uint4 v[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          const int row = p0 + u * kPass + ct / L;
+          v[u] = make_uint4(0u, 0u, 0u, 0u);
+          if (row < rows)
+            v[u] = reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + ((int64_t)cur.b * a.tokens + t0 + row / a.group) * a.q_stride +
+                                                  (int64_t)(kvh * a.group + row % a.group) * D)[c];
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          const int row = p0 + u * kPass + ct / L;
+          if (p0 + u * kPass >= kRowsMax) break;
+          if (!std::is_same<T, __half>::value) {
+            uint32_t most = largest_bits(v[u]);
+#pragma unroll
+            for (int off = L / 2; off > 0; off >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, off));
+            const float by = __uint_as_float((uint32_t)(127 + 14 - (query_exponent(most) - 127)) << 23);
+            v[u] = make_uint4(query_pair(v[u].x, by), query_pair(v[u].y, by), query_pair(v[u].z, by), query_pair(v[u].w, by));
+          }
+#pragma unroll
+          for (int e = 0; e < REP; ++e) {
+            const int r = row + e * kRowsMax;
+            *reinterpret_cast<uint4*>(smem + F::kOffQ + (c >> 3) * F::kBox + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v[u];
           }
         }
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(q_full);
       }
-      for (int i = 0; ok && i < cur.n; ++i) {
-        convert(i, false);
-        if (ok && i + 2 < cur.n) convert(i + 2, true);
-      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_full);
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoft));
@@ -406,7 +391,7 @@ __global__ void __launch_bounds__(kQtThreads, 1)
     auto copy_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(8 + 2 * (q4 & 1) + half) : "memory"); };  // REP 2: a row's two lanes
     bool ok = true;
     int g0 = 0;
-    int rest = 0, rest_rows = 0;  // the unit that this CTA begins and others go on with
+    int64_t at_tile = r_.first;
     for (int piece = 0; cur.step(a, nrt, queries); ++piece) {
       const int b = cur.b, n = cur.n, len = cur.z.len, count = cur.z.count;
       const int t0 = cur.rt * queries, rows = min(queries, count - t0) * a.group;
@@ -417,13 +402,15 @@ __global__ void __launch_bounds__(kQtThreads, 1)
       const int lim = visible_limit(a, len, count, t);
       // lane e < 4: the key scale of this warp's part e of 16 keys, lane 4 + e: the value scale
       const float* scale_from = (lane & 4 ? a.v_scale : a.k_scale) + ((int64_t)b * a.kv_heads + kvh) * a.blocks;
+      const int scale_key = half * 64 + (q4 * 32 / kRowsMax) * NK + (lane & 3) * 16;
       auto fetch = [&](int i) {
-        const int j = (cur.i0 + i) * kKeys + half * 64 + (q4 * 32 / kRowsMax) * NK + (lane & 3) * 16;
-        return i < n && lane < 8 && (lane & 3) < NG && j < len ? scale_from[j / a.block] : 1.0f;
+        const int j = (cur.i0 + i) * kKeys + scale_key;
+        return i < n && lane < 8 && (lane & 3) < NG && j < len ? scale_from[j >> a.block_log2] : 1.0f;
       };
       float scales = fetch(0);
       const T* q = static_cast<const T*>(a.q) + ((int64_t)b * a.tokens + t) * a.q_stride + (int64_t)(kvh * a.group + mine % a.group) * D;
-      const float row_scale = a.scale_log2 * __uint_as_float((uint32_t)(query_exponent<T, D>(q) - 14) << 23);
+      const float row_scale = a.scale_log2 * query_scale<T, D>(q);
+      const bool one_scale = a.block >= NK;  // for all of a thread's keys of a tile
       float m = -INFINITY, l = 0.f;  // m: the reference, in log2 units
       float top = -INFINITY;         // the largest y so far
       const bool tighten = n >= 2 * kTightAt;
@@ -437,13 +424,17 @@ __global__ void __launch_bounds__(kQtThreads, 1)
         float fk[NG], ve[NG], vf[NG], vi[NG];
 #pragma unroll
         for (int e = 0; e < NG; ++e) {
+          if (e > 0 && one_scale) {
+            fk[e] = fk[0], ve[e] = ve[0], vf[e] = vf[0], vi[e] = vi[0];
+            continue;
+          }
           fk[e] = __shfl_sync(0xffffffffu, now, e) * row_scale;
           split_scale(__shfl_sync(0xffffffffu, now, 4 + e), &ve[e], &vf[e], &vi[e]);
         }
-        ok = ok && mbar_wait_bounded(s_full(half, g), (g >> 1) & 1, abort_flag, a.err);
+        ok = ok && mbar_wait_bounded(s_full(g), (g >> 1) & 1, abort_flag, a.err);
         ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
-        uint32_t hi[NK / 2], lo[NK / 2];
+        uint32_t hi[NK / 2], lo[kParts > 1 ? NK / 2 : 1];
         if (works) {
           float2 y[NK / 2];
           float mx = -INFINITY;
@@ -522,10 +513,12 @@ __global__ void __launch_bounds__(kQtThreads, 1)
               for (int k = 0; k < 8; ++k) p[k] = mul2(p[k], frac);
 #pragma unroll
               for (int k = 0; k < 8; ++k) hi[k0 + k] = pack_pair<__half>(p[k].x, p[k].y);
+              if (kParts > 1) {
 #pragma unroll
-              for (int k = 0; k < 8; ++k) p[k] = fma2(unpack_pair<__half>(hi[k0 + k]), minus, p[k]);
+                for (int k = 0; k < 8; ++k) p[k] = fma2(unpack_pair<__half>(hi[k0 + k]), minus, p[k]);
 #pragma unroll
-              for (int k = 0; k < 8; ++k) lo[k0 + k] = pack_pair<__half>(p[k].x, p[k].y);
+                for (int k = 0; k < 8; ++k) lo[k0 + k] = pack_pair<__half>(p[k].x, p[k].y);
+              }
             }
             l += (sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y);
           }
@@ -534,7 +527,7 @@ __global__ void __launch_bounds__(kQtThreads, 1)
           if (works) {
             // over the half's scores: hi parts of its keys, then the lo parts
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
+            for (int u = 0; u < kParts; ++u) {
               const uint32_t* x = u ? lo : hi;
 #pragma unroll
               for (int c = 0; c < 32; c += 16) {
@@ -640,21 +633,10 @@ __global__ void __launch_bounds__(kQtThreads, 1)
         else if (a.lse)
           a.lse[((int64_t)b * a.heads + hd) * a.tokens + tq] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
       }
-      rest = cur.i0 == 0 && !whole ? cur.z.tiles : 0;  // the run ends inside this unit
-      rest_rows = rows;
+      if (a.splits != 1 && cur.i0 == 0 && aid == 0) record_unit(a, r_, cur, nrt, at_tile);
+      at_tile += n;
       if (REP == 1) row_sync(); else all_sync();  // ml is written again
       g0 += n;
-    }
-    if (a.splits != 1 && aid == 0) {
-      int4 record = make_int4(0, 0, 0, 0);
-      if (rest) {  // how many runs it reaches into
-        const int64_t end = first_tile + (g0 - cur.n) + rest - 1;  // its last tile
-        int c = (int)(end * runs / total);  // whose run that is, up to the rounding
-        while (total * (c + 1) / runs <= end) ++c;
-        while (total * c / runs > end) --c;
-        record = make_int4(cur.b, cur.rt, kvh | rest_rows << 16, c - run + 1);
-      }
-      a.units[blockIdx.x] = record;
     }
     tc_fence_before();
   }
@@ -672,7 +654,7 @@ int fail(cudaError_t e, const char* what) {
   return SWAPNET_OK;
 }
 
-template <typename T, int D, int CODE, int REP> int rows_t(const QuantArgs& a, cudaStream_t s) {
+template <typename T, int D, int CODE, int REP> int rows_t(const QuantArgs& a, int ctas, cudaStream_t s) {
   static std::atomic<uint64_t> known{0};
   const auto kern = attention_quant_rows_kernel<T, D, CODE, REP>;
   if (attr_needed(known)) {
@@ -689,24 +671,23 @@ template <typename T, int D, int CODE, int REP> int rows_t(const QuantArgs& a, c
   int rc = make_tmap_codes(&k, a.k, dims, strides, box);
   if (!rc) rc = make_tmap_codes(&v, a.v, dims, strides, box);
   if (rc) return rc;
-  const int ctas = a.splits == 1 ? a.n_seq * nrt * a.kv_heads : run_ctas(a.kv_heads);
   kern<<<ctas, kQtThreads, QtCfg<D>::kSmem, s>>>(k, v, a, queries, nrt);
   rc = fail(cudaSuccess, "quantised attention launch");
   if (rc || a.splits == 1) return rc;
-  return launch_runs_join(a, queries, 128 / REP, nrt, s);
+  return launch_quant_join(a, queries, 128 / REP, nrt, s);
 }
-template <typename T, int D, int CODE> int rows_r(const QuantArgs& a, cudaStream_t s) {
-  return a.tokens * a.group <= 64 ? rows_t<T, D, CODE, 2>(a, s) : rows_t<T, D, CODE, 1>(a, s);
+template <typename T, int D, int CODE> int rows_r(const QuantArgs& a, int ctas, cudaStream_t s) {
+  return a.tokens * a.group <= 64 ? rows_t<T, D, CODE, 2>(a, ctas, s) : rows_t<T, D, CODE, 1>(a, ctas, s);
 }
-template <typename T, int D> int rows_c(const QuantArgs& a, cudaStream_t s) {
-  return a.code == kCodeI8 ? rows_r<T, D, kCodeI8>(a, s) : rows_r<T, D, kCodeE4M3>(a, s);
+template <typename T, int D> int rows_c(const QuantArgs& a, int ctas, cudaStream_t s) {
+  return a.code == kCodeI8 ? rows_r<T, D, kCodeI8>(a, ctas, s) : rows_r<T, D, kCodeE4M3>(a, ctas, s);
 }
 
 }  // namespace
 
-int launch_quant_rows(const QuantArgs& a, cudaStream_t s) {
-  if (a.dtype == SWAPNET_BF16) return a.dim == 128 ? rows_c<__nv_bfloat16, 128>(a, s) : rows_c<__nv_bfloat16, 64>(a, s);
-  return a.dim == 128 ? rows_c<__half, 128>(a, s) : rows_c<__half, 64>(a, s);
+int launch_quant_rows(const QuantArgs& a, int ctas, cudaStream_t s) {
+  if (a.dtype == SWAPNET_BF16) return a.dim == 128 ? rows_c<__nv_bfloat16, 128>(a, ctas, s) : rows_c<__nv_bfloat16, 64>(a, ctas, s);
+  return a.dim == 128 ? rows_c<__half, 128>(a, ctas, s) : rows_c<__half, 64>(a, ctas, s);
 }
 
 }  // namespace swapnet

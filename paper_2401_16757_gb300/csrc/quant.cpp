@@ -11,49 +11,57 @@
 
 namespace swapnet {
 
-// Microseconds of the tensor-core kernel: a unit's start and end, a tile of
-// keys, the join of shared units.
-constexpr double kUnitUs = 5.0, kTileUs = 1.0, kJoinUs = 8.0;
+// Microseconds: a unit's start and end, a tile of 128 keys by itself and its
+// share of a busy SM's time, the join of shared units; warp products of up to
+// 16 and 32 rows, the tensor cores.
+struct Costs {
+  double unit, tile, busy, join;
+};
+constexpr Costs kFewCosts = {3.0, 0.9, 0.8, 4.0}, kMoreCosts = {3.0, 1.2, 0.95, 4.0}, kTcCosts = {5.0, 1.5, 1.5, 12.0};
+// CTAs that share the tiles of all units: as many as are resident, or up to
+// four times that where their runs are long: the memory does not serve all SMs
+// alike, and CTAs that start later even that out (one token of 64 sequences, up
+// to 16384 rows: 274 us with 456 runs, whose times lie between 174 and 279, 250
+// with four times as many).
+constexpr int kRunLeast = 24;  // tiles of such a run
 
-CachedPlan quant_plan(const QuantArgs& a) {
+CachedPlan quant_plan(const QuantArgs& a, int* ctas) {
   CachedPlan p;
   std::memset(&p, 0, sizeof(p));
   const int64_t rows = (int64_t)a.tokens * a.group, pairs = (int64_t)a.n_seq * a.kv_heads;
-  p.tc = rows > kFewAttnRows;
-  if (p.tc) {
-    const int row_tile = rows <= 64 ? 64 : 128, queries = std::min(row_tile / a.group, a.tokens);
-    const int64_t units = pairs * ((a.tokens + queries - 1) / queries);
-    // a CTA per unit, or equal runs of all tiles and a join (see cached_plan)
-    const double tiles = (a.max_seq + 127) / 128;
-    const int ctas = run_ctas(a.kv_heads);
-    const double alone = std::ceil((double)units / kSms) * (kUnitUs + tiles * kTileUs);
-    const double shared = kUnitUs + std::max(2.0, units * tiles / ctas) * kTileUs + (double)units / ctas + kJoinUs;
-    p.splits = units >= 2 * kSms || alone <= shared ? 1 : 0;
-    if (units > 0x7fffffff) p.splits = 0;
-    if (p.splits == 0) {
-      p.part_bytes = align_up((uint64_t)2 * ctas * row_tile * a.dim * 4);
-      p.ml_bytes = align_up((uint64_t)2 * ctas * row_tile * 8);
-      p.unit_bytes = align_up((uint64_t)ctas * 16);
-    }
-    return p;
+  p.tc = rows > kQuantFewRows;
+  const Costs c = p.tc ? kTcCosts : rows > 16 ? kMoreCosts : kFewCosts;
+  const int row_tile = p.tc ? (rows <= 64 ? 64 : 128) : rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
+  const int resident = p.tc ? 1 : quant_few_resident((int)rows, a.dim);
+  const int queries = std::min(row_tile / a.group, a.tokens);
+  const int64_t units = pairs * ((a.tokens + queries - 1) / queries);
+  // A CTA per unit, or equal runs of all tiles and a join.  Where units queue for
+  // the SMs, part of one waits for the last at the end (lengths and causal
+  // limits differ).
+  const double tiles = (a.max_seq + 127) / 128, slots = (double)kSms * resident;
+  int runs = std::max(1, kSms * resident / a.kv_heads) * a.kv_heads;
+  auto per_tile = [&](double on_sm) { return std::max(c.tile, c.busy * std::min((double)resident, std::ceil(on_sm))); };
+  const double alone = (c.unit + per_tile((double)units / kSms) * tiles) * (units <= slots ? 1.0 : units / slots + 0.25);
+  const double mine = std::max(2.0, units * tiles / runs);  // tiles of a run
+  const double shared = c.unit * (1.0 + (double)units / runs) + per_tile(units * tiles / mine / kSms) * mine + c.join;
+  p.splits = alone <= shared || units > 65535 ? 1 : 0;
+  if (!p.tc) runs *= (int)std::min(4.0, std::max(1.0, mine / kRunLeast));
+  if (p.splits == 0) {
+    p.part_bytes = align_up((uint64_t)2 * runs * row_tile * a.dim * 4);
+    p.ml_bytes = align_up((uint64_t)2 * runs * row_tile * 8);
+    p.unit_bytes = align_up((uint64_t)units * 8);
   }
-  p.splits = choose_splits(pairs, (a.max_seq + 127) / 128, 0.5, 0.7, 1.5, 2.5);
-  if (p.splits > 1) {
-    p.part_bytes = align_up((uint64_t)pairs * rows * p.splits * a.dim * 4);
-    p.ml_bytes = align_up((uint64_t)pairs * rows * p.splits * 8);
-  }
+  *ctas = p.splits == 0 ? runs : (int)units;
   return p;
 }
 
-int run_quant_attention(QuantArgs a, const CachedPlan& p, void* workspace, cudaStream_t s) {
+int run_quant_attention(QuantArgs a, const CachedPlan& p, int ctas, void* workspace, cudaStream_t s) {
   char* w = static_cast<char*>(workspace);
   a.splits = p.splits;
   a.part = reinterpret_cast<float*>(w);
   a.ml = reinterpret_cast<float*>(w + p.part_bytes);
   a.units = reinterpret_cast<int4*>(w + p.part_bytes + p.ml_bytes);
-  if (p.tc) return launch_quant_rows(a, s);
-  if (int rc = launch_quant_few(a, s)) return rc;
-  return launch_attention_join(a, s);
+  return p.tc ? launch_quant_rows(a, ctas, s) : launch_quant_few(a, ctas, s);
 }
 
 namespace {
@@ -183,7 +191,7 @@ int check_quant(const swapnet_quantized_attention* c, QuantArgs* a) {
   if (!valid_block(c->block)) SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "quantised attention: block must be 16, 32, 64 or 128 rows");
   const int64_t group = c->heads / c->kv_heads;
   if (c->n_seq > 65535 || c->kv_heads > 65535 || group > 128 || (int64_t)c->tokens * group > (1 << 20) || c->max_seq > (1 << 30) ||
-      (int64_t)c->n_seq * c->tokens > (1 << 30))
+      (int64_t)c->n_seq * c->tokens > (1 << 30) || (int64_t)c->n_seq * c->tokens * c->kv_heads > 0x7fffffff)
     SN_FAIL(SWAPNET_ERR_UNSUPPORTED, "quantised attention: shape beyond the kernels' limits");
   if (!c->q || !c->k || !c->v || !c->k_scale || !c->v_scale || !c->lens || !c->out)
     SN_FAIL(SWAPNET_ERR_INVALID_ARG, "quantised attention: null pointer");
@@ -200,6 +208,7 @@ int check_quant(const swapnet_quantized_attention* c, QuantArgs* a) {
   a->dim = c->head_dim;
   a->max_seq = c->max_seq;
   a->block = c->block;
+  a->block_log2 = c->block == 16 ? 4 : c->block == 32 ? 5 : c->block == 64 ? 6 : 7;
   a->blocks = (c->max_seq + c->block - 1) / c->block;
   a->q = c->q;
   a->k = c->k;
@@ -247,7 +256,8 @@ int swapnet_attention_quantized_workspace(const swapnet_quantized_attention* c, 
     if (!bytes) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "null output");
     QuantArgs a;
     if (int rc = check_quant(c, &a)) return rc;
-    *bytes = plan_bytes(quant_plan(a));
+    int ctas;
+    *bytes = plan_bytes(quant_plan(a, &ctas));
     return SWAPNET_OK;
   });
 }
@@ -257,7 +267,8 @@ int swapnet_attention_quantized(const swapnet_quantized_attention* c, void* work
     using namespace swapnet;
     QuantArgs a;
     if (int rc = check_quant(c, &a)) return rc;
-    const CachedPlan p = quant_plan(a);
+    int ctas;
+    const CachedPlan p = quant_plan(a, &ctas);
     const uint64_t need = plan_bytes(p);
     if (need && !workspace) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "quantised attention: null workspace");
     if (workspace_bytes < need) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "quantised attention: workspace too small");
@@ -265,7 +276,7 @@ int swapnet_attention_quantized(const swapnet_quantized_attention* c, void* work
     if (shares({c->out, c->lse, need ? workspace : nullptr}, {c->q, c->k, c->v, c->k_scale, c->v_scale, c->lens, c->counts}))
       SN_FAIL(SWAPNET_ERR_INVALID_ARG, "quantised attention: a result must not be an input or another result");
     if (int rc = error_word(&a.err)) return rc;
-    return run_quant_attention(a, p, workspace, reinterpret_cast<cudaStream_t>(stream));
+    return run_quant_attention(a, p, ctas, workspace, reinterpret_cast<cudaStream_t>(stream));
   });
 }
 

@@ -1,7 +1,7 @@
 // Device-side pieces of the attention over a cache of 8-bit codes: codes to
 // fp16, queries to fp16, scales.
 #pragma once
-#include "cached.cuh"
+#include "cached_tc.cuh"
 #include "quant.h"
 
 namespace swapnet {
@@ -105,6 +105,101 @@ template <typename T, int C> __device__ __forceinline__ float query_fp16(const u
     out[c][1] = pack_pair<__half>(w.x * by, w.y * by);
   }
   return __uint_as_float((uint32_t)(127 + (x - 127) - 14) << 23);
+}
+
+// ------------------------------------------------------------------ runs
+// Which tiles a CTA of an attention launch takes: with a.splits == 1 unit
+// blockIdx / kv_heads of its key head, otherwise an equal run of all the head's
+// tiles (see Cursor).  near: sizes of sequences, sched: scratch of at least
+// blockDim / 32 + 2 words, both in shared memory.  All threads of the block.
+struct Run {
+  int kvh, run, runs;      // the run's number and how many there are
+  int64_t first, total;    // its first tile in the order of all; their number
+};
+__device__ __forceinline__ Run start_run(const CachedArgs& a, Cursor& cur, int2* near, int64_t* sched, int queries, int nrt) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x / 32;
+  Run r;
+  r.kvh = blockIdx.x % a.kv_heads;
+  r.run = blockIdx.x / a.kv_heads;
+  r.runs = 1;
+  r.first = r.total = 0;
+  cur.next = 0;
+  cur.near = near;
+  const bool all_near = a.splits != 1 && a.n_seq <= kNear;
+  cur.b0 = a.splits == 1 ? r.run / nrt : 0;
+  if ((a.splits == 1 || all_near) && threadIdx.x < kNear && cur.b0 + (int)threadIdx.x < a.n_seq) near[threadIdx.x] = seq_size(a, cur.b0 + threadIdx.x);
+  __syncthreads();
+  if (a.splits == 1) {
+    cur.pair = r.run;
+    cur.left = pair_size(a, near[0], r.run % nrt, queries).tiles;
+    if (cur.left == 0 && r.kvh == 0) {
+      int len, count;
+      seq_sizes(a, r.run / nrt, &len, &count);  // (reports what is out of range)
+    }
+    return r;
+  }
+  // every thread adds up some pairs, then the threads' sums
+  auto size_of = [&](int b) { return all_near ? near[b] : seq_size(a, b); };
+  const int pairs = a.n_seq * nrt, per = (pairs + blockDim.x - 1) / blockDim.x;
+  const int p0 = min((int)threadIdx.x * per, pairs), p1 = min(p0 + per, pairs);
+  int64_t sum = 0;
+  for (int p = p0; p < p1; ++p) {
+    const int2 size = size_of(p / nrt);
+    sum += pair_size(a, size, p % nrt, queries).tiles;
+    if (blockIdx.x == 0 && (size.x < 0 || size.x > a.max_seq || size.y < 0 || size.y > a.tokens)) atomicExch(a.err, kDevErrBounds);
+  }
+  int64_t before = sum;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const int64_t o = __shfl_up_sync(0xffffffffu, before, off);
+    if (lane >= off) before += o;
+  }
+  if (lane == 31) sched[warp] = before;
+  before -= sum;
+  __syncthreads();
+  for (int w = 0; w < warps; ++w) {
+    if (w < warp) before += sched[w];
+    r.total += sched[w];
+  }
+  r.runs = (int)min((int64_t)(gridDim.x / a.kv_heads), (r.total + kRunTiles - 1) / kRunTiles);
+  r.first = r.run < r.runs ? r.total * r.run / r.runs : r.total;
+  cur.left = r.run < r.runs ? r.total * (r.run + 1) / r.runs - r.first : 0;
+  cur.pair = 0;
+  if (cur.left > 0 && before <= r.first && r.first < before + sum) {
+    int64_t at = before;
+    for (int p = p0; p < p1; ++p) {
+      const int tiles = pair_size(a, size_of(p / nrt), p % nrt, queries).tiles;
+      if (r.first < at + tiles) {
+        sched[warps] = p;
+        sched[warps + 1] = r.first - at;
+        break;
+      }
+      at += tiles;
+    }
+  }
+  __syncthreads();
+  if (cur.left > 0) {
+    cur.pair = (int)sched[warps];
+    cur.next = (int)sched[warps + 1];
+  }
+  if (!all_near) {
+    cur.b0 = cur.pair / nrt;
+    if (threadIdx.x < kNear && cur.b0 + (int)threadIdx.x < a.n_seq) near[threadIdx.x] = seq_size(a, cur.b0 + threadIdx.x);
+  }
+  return r;
+}
+// One thread, for a unit whose first piece this CTA has had (tile `at` of the
+// run's order on): the CTA, and how many runs share the unit (0: it is whole).
+__device__ __forceinline__ void record_unit(const CachedArgs& a, const Run& r, const Cursor& cur, int nrt, int64_t at) {
+  int pieces = 0;
+  if (cur.n < cur.z.tiles) {
+    const int64_t end = at + cur.z.tiles - 1;  // its last tile
+    int c = (int)(end * r.runs / r.total);  // whose run that is, up to the rounding
+    while (r.total * (c + 1) / r.runs <= end) ++c;
+    while (r.total * c / r.runs > end) --c;
+    pieces = c - r.run + 1;
+  }
+  reinterpret_cast<int2*>(a.units)[((int64_t)cur.b * nrt + cur.rt) * a.kv_heads + r.kvh] = make_int2(blockIdx.x, pieces);
 }
 
 }  // namespace swapnet

@@ -32,13 +32,17 @@ int launch_cache_append(AppendArgs a, cudaStream_t s);
 // The attention's arguments; of those of the 16-bit caches there are no draft
 // and no weights, k and v are codes and kv_stride and seq_stride count them.
 struct QuantArgs : CachedArgs {
-  int code, block, blocks;
+  int code, block, block_log2, blocks;
   const float *k_scale, *v_scale;
 };
-// How a call runs, from its sizes alone.
-CachedPlan quant_plan(const QuantArgs& a);
-int run_quant_attention(QuantArgs a, const CachedPlan& p, void* workspace, cudaStream_t s);
-int launch_quant_few(const QuantArgs& a, cudaStream_t s);   // up to 16 rows a (sequence, key head)
-int launch_quant_rows(const QuantArgs& a, cudaStream_t s);  // tcgen05, with the join
+// How a call runs, from its sizes alone; ctas: of its attention launch.
+CachedPlan quant_plan(const QuantArgs& a, int* ctas);
+int run_quant_attention(QuantArgs a, const CachedPlan& p, int ctas, void* workspace, cudaStream_t s);
+constexpr int kQuantFewRows = 32;  // of a (sequence, key head) that the warp products take
+// Their CTAs that an SM holds, by registers and shared memory.
+constexpr int quant_few_resident(int rows, int dim) { return rows <= 8 ? (dim == 64 ? 4 : 3) : rows <= 16 && dim == 64 ? 3 : 2; }
+int launch_quant_join(const QuantArgs& a, int queries, int row_tile, int nrt, cudaStream_t s);  // the units that runs shared
+int launch_quant_few(const QuantArgs& a, int ctas, cudaStream_t s);   // warp products, with the join
+int launch_quant_rows(const QuantArgs& a, int ctas, cudaStream_t s);  // tcgen05, with the join
 
 }  // namespace swapnet
