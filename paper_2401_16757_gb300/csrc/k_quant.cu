@@ -303,15 +303,19 @@ __global__ void __launch_bounds__(32 * W, QfCfg<D, NR, W>::kResident)
         for (int c = 0; c < C; c += 2) {
           uint32_t vr[4];
           ldmatrix_x4_trans(vs_u + swz8<D>(u * 16 + lrow, c + lchunk), vr);
+          uint32_t af[2][4];
 #pragma unroll
           for (int w = 0; w < 2; ++w) {
             const uint2 lo = pairs_apart<CODE>(vr[2 * w]), hi = pairs_apart<CODE>(vr[2 * w + 1]);
-            const uint32_t af[4] = {lo.x, lo.y, hi.x, hi.y};
-#pragma unroll
-            for (int n = 0; n < NR; ++n)
-#pragma unroll
-              for (int i = 0; i < 2; ++i) mma_16816<__half>(o[c + w][n], af, pt[u][n][i][0], pt[u][n][i][1]);
+            af[w][0] = lo.x, af[w][1] = lo.y, af[w][2] = hi.x, af[w][3] = hi.y;
           }
+          // (the parts apart: a product waits for the one before it of the same sums)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int w = 0; w < 2; ++w)
+#pragma unroll
+              for (int n = 0; n < NR; ++n) mma_16816<__half>(o[c + w][n], af[w], pt[u][n][i][0], pt[u][n][i][1]);
         }
       __syncwarp();  // and the values before theirs
       load(g + kQfStages * W, slot, false);

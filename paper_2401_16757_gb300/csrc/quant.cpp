@@ -18,11 +18,12 @@ struct Costs {
   double unit, tile, busy, join;
 };
 constexpr Costs kFewCosts = {3.0, 0.9, 0.8, 4.0}, kMoreCosts = {3.0, 1.2, 0.95, 4.0}, kTcCosts = {5.0, 1.5, 1.5, 12.0};
-// CTAs that share the tiles of all units: as many as are resident, or up to
-// four times that where their runs are long: the memory does not serve all SMs
-// alike, and CTAs that start later even that out (one token of 64 sequences, up
-// to 16384 rows: 274 us with 456 runs, whose times lie between 174 and 279, 250
-// with four times as many).
+// CTAs that share the tiles of all units: as many as are resident, or for up to
+// 16 rows, which the memory bounds, up to six times that where their runs are
+// long: the memory does not serve all SMs alike, and CTAs that start later even
+// that out (one token of 64 sequences, up to 16384 rows: 269 us with 456 runs,
+// whose times lie between 174 and 279, 254 with six times as many; 32 rows pay
+// more for a run's end: 127 us with 304 runs, 141 with twice as many).
 constexpr int kRunLeast = 24;  // tiles of such a run
 
 CachedPlan quant_plan(const QuantArgs& a, int* ctas) {
@@ -45,7 +46,7 @@ CachedPlan quant_plan(const QuantArgs& a, int* ctas) {
   const double mine = std::max(2.0, units * tiles / runs);  // tiles of a run
   const double shared = c.unit * (1.0 + (double)units / runs) + per_tile(units * tiles / mine / kSms) * mine + c.join;
   p.splits = alone <= shared || units > 65535 ? 1 : 0;
-  if (!p.tc) runs *= (int)std::min(4.0, std::max(1.0, mine / kRunLeast));
+  if (rows <= 16) runs *= (int)std::min(6.0, std::max(1.0, mine / kRunLeast));
   if (p.splits == 0) {
     p.part_bytes = align_up((uint64_t)2 * runs * row_tile * a.dim * 4);
     p.ml_bytes = align_up((uint64_t)2 * runs * row_tile * 8);
