@@ -445,7 +445,7 @@ __device__ __forceinline__ void append_blocks(const AppendArgs& a, const float2*
 // row_ctas for rows in 16 bits, which take less time; CTA by CTA of all
 // sequences.
 template <typename T, int D, int CODE, int kHeads, int P>
-__global__ void __launch_bounds__(kMaxThreads, P >= 8 ? 3 : 4) cache_append_kernel(const __grid_constant__ AppendArgs a) {
+__global__ void __launch_bounds__(kMaxThreads, 4) cache_append_kernel(const __grid_constant__ AppendArgs a) {
   const int cta = blockIdx.x / a.n_seq, b = blockIdx.x % a.n_seq;
   __shared__ __align__(16) float2 turns_of[64];  // (lanes that read different kernel arguments wait for one another)
   if (a.rope_dim && threadIdx.x < a.rope_dim / 2) turns_of[threadIdx.x] = a.turns[threadIdx.x];

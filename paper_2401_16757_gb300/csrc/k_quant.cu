@@ -384,9 +384,9 @@ __global__ void __launch_bounds__(32 * W, QfCfg<D, NR, W>::kResident)
 // CTA that began it, each with m, l and O relative to its m.  A CTA holds at
 // most two pieces that are not whole units: the rest of one that began before
 // its run (slot 2 c) and the start of one that goes on behind it (slot 2 c + 1).
-// A warp per row, or all eight warps of the block where that takes fewer rounds
-// of loads, each of four pieces.
-constexpr int kQjWarps = 8;
+// A warp per row, or all warps of the block where that takes fewer rounds of
+// loads, each of eight pieces.
+constexpr int kQjWarps = 16, kQjAhead = 8;
 template <typename T>
 __global__ void __launch_bounds__(32 * kQjWarps)
     attention_quant_join_kernel(const __grid_constant__ QuantArgs a, int queries, int row_tile, int nrt) {
@@ -399,7 +399,7 @@ __global__ void __launch_bounds__(32 * kQjWarps)
   if (pair_size(a, size, rt, queries).tiles == 0 || u.y == 0) return;  // (an empty unit has no record)
   const int t0 = rt * queries, rows = min(queries, size.y - t0) * a.group, pieces = u.y;
   const int blocks = gridDim.x, per_warp = (rows + kQjWarps * blocks - 1) / (kQjWarps * blocks), per_block = (rows + blocks - 1) / blocks;
-  const bool many = per_block * ((pieces + 4 * kQjWarps - 1) / (4 * kQjWarps) + 1) < per_warp * ((pieces + 3) / 4);  // (+ 1: the warps' results meet)
+  const bool many = per_block * ((pieces + kQjAhead * kQjWarps - 1) / (kQjAhead * kQjWarps) + 1) < per_warp * ((pieces + kQjAhead - 1) / kQjAhead);  // (+ 1: the warps' results meet)
   const int V = a.dim / 4, first = many ? warp : 0, step = many ? kQjWarps : 1;
   const float2* ml = reinterpret_cast<const float2*>(a.ml);
   const float4* part = reinterpret_cast<const float4*>(a.part);
@@ -420,17 +420,17 @@ __global__ void __launch_bounds__(32 * kQjWarps)
       x.z = fmaf(x.z, f, y.z * g);
       x.w = fmaf(x.w, f, y.w * g);
     };
-    for (int p0 = first; own && p0 < pieces; p0 += 4 * step) {
-      float2 s[4];
-      float4 y[4];
+    for (int p0 = first; own && p0 < pieces; p0 += kQjAhead * step) {
+      float2 s[kQjAhead];
+      float4 y[kQjAhead];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < kQjAhead; ++i) {
         const int p = p0 + i * step;
         s[i] = p < pieces ? ml[slot(p)] : make_float2(-INFINITY, 0.f);
         y[i] = p < pieces && lane < V ? part[slot(p) * V + lane] : make_float4(0.f, 0.f, 0.f, 0.f);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) take(s[i], y[i]);
+      for (int i = 0; i < kQjAhead; ++i) take(s[i], y[i]);
     }
     if (many) {
       so[warp][lane] = x;
@@ -481,12 +481,12 @@ template <typename T, int D> int few_c(const QuantArgs& a, int ctas, cudaStream_
 }  // namespace
 
 int launch_quant_join(const QuantArgs& a, int queries, int row_tile, int nrt, cudaStream_t s) {
-  // about eight blocks per SM, but at least a warp and at most a block for a row
+  // about four blocks per SM, but at least a warp and at most a block for a row
   const int64_t units = (int64_t)a.n_seq * nrt * a.kv_heads;
   const int rows = queries * a.group, least = (rows + kQjWarps - 1) / kQjWarps;
   cudaLaunchConfig_t cfg;
   std::memset(&cfg, 0, sizeof(cfg));
-  cfg.gridDim = dim3(std::min(rows, std::max(least, (int)(8 * kSms / units))), (unsigned)units);
+  cfg.gridDim = dim3(std::min(rows, std::max(least, (int)(4 * kSms / units))), (unsigned)units);
   cfg.blockDim = dim3(32 * kQjWarps);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];

@@ -112,8 +112,12 @@ int check_append(const swapnet_cache_rows* c, AppendArgs* a) {
       a->axis1 = (int)n0;
       a->axis2 = (int)(n0 + n1);
     }
+    // theta^(-2 i / rope), i = 8 j + k: from 8 powers each (64 of them took 0.6 us of a call)
+    double fine[8], coarse = 1.0;
+    for (int k = 0; k < 8; ++k) fine[k] = std::pow((double)c->theta, -2.0 * k / rope) / kTurn;
     for (int i = 0; i < rope / 2; ++i) {
-      const double turns = std::pow((double)c->theta, -2.0 * i / rope) / kTurn;
+      if (i % 8 == 0) coarse = std::pow((double)c->theta, -2.0 * i / rope);
+      const double turns = coarse * fine[i % 8];
       a->turns[i].x = (float)turns;
       a->turns[i].y = (float)(turns - (double)a->turns[i].x);
       if (!(turns <= 1e6)) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cache append: bad theta or eps");
