@@ -903,13 +903,15 @@ int swapnet_tree_accept(const swapnet_tree_acceptance* args, swapnet_stream stre
  * block, as long as it is not full, are kept in 16 bits as well: k_open, v_open,
  * [n_seq][block][kv_heads][head_dim], row j of the cache at j % block.  A row is
  * rounded to 8 bits from its 16-bit value whatever the calls that append it,
- * and the cache is a function of the rows alone:
+ * and the cache is a function of the rows alone (a sequence's last rows can be
+ * taken back by a smaller length, as far as the start of its open block):
  *   E4M3  scale = the least power of two >= m / 448
  *   I8    scale = m / 127
  * with m the block's largest magnitude so far (scale at least 2^-100), code =
  * value / scale rounded to the nearest (ties to even).  A block with a value
  * that is infinite or not a number has a scale that is not a number (codes of
- * I8: 0), and so has the attention of every query that sees one of its rows. */
+ * I8: 0; E4M3: not a number), and so is the attention of every query that sees
+ * one of its rows. */
 
 /* Appends the rows of up to `tokens` new tokens per sequence to a cache, and
  * prepares their queries:
@@ -977,10 +979,13 @@ int swapnet_cache_append(const swapnet_cache_rows* args, swapnet_stream stream);
  * Scores, statistics and sums are fp32.  Keys and values enter the products as
  * fp16 numbers that hold their codes exactly, queries as fp16 (BF16 ones scaled
  * by a power of two per query, which loses what is below 2^-39 of its largest
- * element), probabilities times their value scales as two fp16 parts (22 bits;
- * off by at most 2^-32 of a query's largest such product).  A value scale below
- * 2^-100 counts as 2^-100; scales are not negative.
- * `workspace` as for swapnet_attention_tree.  Results and workspace overlap
+ * element), probabilities times their value scales as two fp16 parts: 22 bits,
+ * off by at most 2^-39 of a query's largest such product up to 32 rows (tokens x
+ * heads / kv_heads), beyond by 2^-32 in short caches and in the first 2048 rows
+ * that a CTA takes of a long one, 2^-37 in the rest.  A value scale below 2^-100
+ * counts as 2^-100; scales are not negative.
+ * `workspace` as for swapnet_attention_tree: a function of the sizes; how many
+ * CTAs share a cache goes by max_seq.  Results and workspace overlap
  * none of the inputs.  Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA. */
 typedef struct swapnet_quantized_attention {
   int32_t dtype;        /* F16 or BF16: queries and outputs                      */

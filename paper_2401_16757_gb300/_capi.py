@@ -239,7 +239,7 @@ def lib():
         "swapnet_engine_tree_accept": (C.c_int, [P, P, P, P]),
         "swapnet_engine_evict": (C.c_int, [P, C.c_int32, C.c_int32, C.c_int32, P]),
         "swapnet_device_sync": (C.c_int, []),
-        "swapnet_cache_append": (C.c_int, [C.POINTER(CacheRows), P]),
+        "swapnet_cache_append": (C.c_int, [P, P]),  # (the packed block as it is)
         "swapnet_attention_quantized_workspace": (C.c_int, [C.POINTER(QuantizedAttention), C.POINTER(C.c_uint64)]),
         "swapnet_attention_quantized": (C.c_int, [C.POINTER(QuantizedAttention), P, C.c_uint64, P]),
     }
@@ -508,12 +508,11 @@ def cache_append(dtype, cache_dtype, n_seq, tokens, heads, kv_heads, head_dim, m
                  q_stride=0, new_stride=0, out_stride=0, kv_stride=0, seq_stride=0, stream=0):
     """Norms and rotation of new queries and keys, and their rows put into a cache of 16 bits, "i8" or "e4m3":
     sizes, device addresses (0: none), then options and strides in elements (0: packed)."""
-    a = CacheRows.from_buffer_copy(_ROWS.pack(
+    a = _ROWS.pack(
         DTYPE.get(dtype, dtype), DTYPE.get(cache_dtype, cache_dtype), n_seq, tokens, heads, kv_heads, head_dim, max_seq, block,
         rope_dim, bool(halves), *sections, theta, eps, q, k_new, v_new, q_gain, k_gain, lens, counts, positions, q_out, k, v,
-        k_scale, v_scale, k_open, v_open, k_open_out, v_open_out, lens_out, q_stride, new_stride, out_stride, kv_stride,
-        seq_stride))
-    check(lib().swapnet_cache_append(C.byref(a), stream or None), "swapnet_cache_append")
+        k_scale, v_scale, k_open, v_open, k_open_out, v_open_out, lens_out, q_stride, new_stride, out_stride, kv_stride, seq_stride)
+    check(lib().swapnet_cache_append(a, stream or None), "swapnet_cache_append")
 
 
 def quantized_attention(dtype, cache_dtype, n_seq, tokens, heads, kv_heads, head_dim, max_seq, block, q, k, v, k_scale, v_scale,

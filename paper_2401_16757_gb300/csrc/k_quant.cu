@@ -470,12 +470,11 @@ template <typename T, int D, int CODE, int NR, int W> int few_t(const QuantArgs&
   if (e != cudaSuccess) SN_FAIL(SWAPNET_ERR_CUDA, std::string("quantised attention launch: ") + cudaGetErrorString(e));
   return a.splits == 1 ? SWAPNET_OK : launch_quant_join(a, queries, F::kRows, nrt, s);
 }
-template <typename T, int D, int CODE> int few_r(const QuantArgs& a, int ctas, cudaStream_t s) {
-  const int rows = a.tokens * a.group;
-  return rows <= 8 ? few_t<T, D, CODE, 1, 4>(a, ctas, s) : rows <= 16 ? few_t<T, D, CODE, 2, 4>(a, ctas, s) : few_t<T, D, CODE, 4, 4>(a, ctas, s);
+template <typename T, int D, int CODE> int few_r(const QuantArgs& a, int ctas, int row_tile, cudaStream_t s) {
+  return row_tile == 8 ? few_t<T, D, CODE, 1, 4>(a, ctas, s) : row_tile == 16 ? few_t<T, D, CODE, 2, 4>(a, ctas, s) : few_t<T, D, CODE, 4, 4>(a, ctas, s);
 }
-template <typename T, int D> int few_c(const QuantArgs& a, int ctas, cudaStream_t s) {
-  return a.code == kCodeI8 ? few_r<T, D, kCodeI8>(a, ctas, s) : few_r<T, D, kCodeE4M3>(a, ctas, s);
+template <typename T, int D> int few_c(const QuantArgs& a, int ctas, int row_tile, cudaStream_t s) {
+  return a.code == kCodeI8 ? few_r<T, D, kCodeI8>(a, ctas, row_tile, s) : few_r<T, D, kCodeE4M3>(a, ctas, row_tile, s);
 }
 
 }  // namespace
@@ -501,9 +500,9 @@ int launch_quant_join(const QuantArgs& a, int queries, int row_tile, int nrt, cu
   return SWAPNET_OK;
 }
 
-int launch_quant_few(const QuantArgs& a, int ctas, cudaStream_t s) {
-  if (a.dtype == SWAPNET_BF16) return a.dim == 128 ? few_c<__nv_bfloat16, 128>(a, ctas, s) : few_c<__nv_bfloat16, 64>(a, ctas, s);
-  return a.dim == 128 ? few_c<__half, 128>(a, ctas, s) : few_c<__half, 64>(a, ctas, s);
+int launch_quant_few(const QuantArgs& a, int ctas, int row_tile, cudaStream_t s) {
+  if (a.dtype == SWAPNET_BF16) return a.dim == 128 ? few_c<__nv_bfloat16, 128>(a, ctas, row_tile, s) : few_c<__nv_bfloat16, 64>(a, ctas, row_tile, s);
+  return a.dim == 128 ? few_c<__half, 128>(a, ctas, row_tile, s) : few_c<__half, 64>(a, ctas, row_tile, s);
 }
 
 }  // namespace swapnet

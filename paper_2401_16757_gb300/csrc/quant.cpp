@@ -13,11 +13,12 @@ namespace swapnet {
 
 // Microseconds: a unit's start and end, a tile of 128 keys by itself and its
 // share of a busy SM's time, the join of shared units; warp products of up to
-// 16 and 32 rows, the tensor cores.
+// 16 and 32 rows, the tensor cores' 64 and 128.
 struct Costs {
   double unit, tile, busy, join;
 };
-constexpr Costs kFewCosts = {3.0, 0.9, 0.8, 4.0}, kMoreCosts = {3.0, 1.2, 0.95, 4.0}, kTcCosts = {5.0, 1.5, 1.5, 12.0};
+constexpr Costs kFewCosts = {3.0, 0.9, 0.8, 5.0}, kMoreCosts = {6.0, 1.3, 1.05, 6.0}, kTc64Costs = {8.0, 1.8, 1.8, 10.0},
+                kTc128Costs = {8.0, 2.3, 2.3, 10.0};
 // CTAs that share the tiles of all units: as many as are resident, or for up to
 // 16 rows, which the memory bounds, up to six times that where their runs are
 // long: the memory does not serve all SMs alike, and CTAs that start later even
@@ -26,43 +27,69 @@ constexpr Costs kFewCosts = {3.0, 0.9, 0.8, 4.0}, kMoreCosts = {3.0, 1.2, 0.95, 
 // more for a run's end: 127 us with 304 runs, 141 with twice as many).
 constexpr int kRunLeast = 24;  // tiles of such a run
 
-CachedPlan quant_plan(const QuantArgs& a, int* ctas) {
-  CachedPlan p;
-  std::memset(&p, 0, sizeof(p));
-  const int64_t rows = (int64_t)a.tokens * a.group, pairs = (int64_t)a.n_seq * a.kv_heads;
-  p.tc = rows > kQuantFewRows;
-  const Costs c = p.tc ? kTcCosts : rows > 16 ? kMoreCosts : kFewCosts;
-  const int row_tile = p.tc ? (rows <= 64 ? 64 : 128) : rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
-  const int resident = p.tc ? 1 : quant_few_resident((int)rows, a.dim);
+// A way to run a call: rows of a unit, how its tiles are shared, its cost.
+struct Way {
+  int row_tile, splits, ctas;
+  int64_t units;
+  double us;
+};
+static Way way(const QuantArgs& a, const Costs& c, int row_tile, int resident) {
+  Way w;
   const int queries = std::min(row_tile / a.group, a.tokens);
-  const int64_t units = pairs * ((a.tokens + queries - 1) / queries);
+  w.row_tile = row_tile;
+  w.units = (int64_t)a.n_seq * a.kv_heads * ((a.tokens + queries - 1) / queries);
   // A CTA per unit, or equal runs of all tiles and a join.  Where units queue for
   // the SMs, part of one waits for the last at the end (lengths and causal
   // limits differ).
   const double tiles = (a.max_seq + 127) / 128, slots = (double)kSms * resident;
   int runs = std::max(1, kSms * resident / a.kv_heads) * a.kv_heads;
   auto per_tile = [&](double on_sm) { return std::max(c.tile, c.busy * std::min((double)resident, std::ceil(on_sm))); };
-  const double alone = (c.unit + per_tile((double)units / kSms) * tiles) * (units <= slots ? 1.0 : units / slots + 0.25);
-  const double mine = std::max(2.0, units * tiles / runs);  // tiles of a run
-  const double shared = c.unit * (1.0 + (double)units / runs) + per_tile(units * tiles / mine / kSms) * mine + c.join;
-  p.splits = alone <= shared || units > 65535 ? 1 : 0;
-  if (rows <= 16) runs *= (int)std::min(6.0, std::max(1.0, mine / kRunLeast));
-  if (p.splits == 0) {
-    p.part_bytes = align_up((uint64_t)2 * runs * row_tile * a.dim * 4);
-    p.ml_bytes = align_up((uint64_t)2 * runs * row_tile * 8);
-    p.unit_bytes = align_up((uint64_t)units * 8);
+  const double alone = (c.unit + per_tile((double)w.units / kSms) * tiles) * (w.units <= slots ? 1.0 : w.units / slots + 0.1);
+  const double mine = std::max(2.0, w.units * tiles / runs);  // tiles of a run
+  const double shared = c.unit * (1.0 + (double)w.units / runs) + per_tile(w.units * tiles / mine / kSms) * mine + c.join;
+  if (row_tile <= 16) runs *= (int)std::min(6.0, std::max(1.0, mine / kRunLeast));
+  // (tensor cores with two units per SM: 512 units of up to 33 tiles 178 us, in runs 219)
+  w.splits = alone <= shared || w.units > 65535 || (resident == 1 && w.units >= 2 * kSms) ? 1 : 0;
+  w.ctas = w.splits ? (int)w.units : runs;
+  w.us = w.splits ? alone : shared;
+  return w;
+}
+
+CachedPlan quant_plan(const QuantArgs& a, int* ctas, int* row_tile) {
+  CachedPlan p;
+  std::memset(&p, 0, sizeof(p));
+  const int64_t rows = (int64_t)a.tokens * a.group;
+  const int tile = rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
+  Way w;
+  w.us = 1e30;
+  if (a.group <= tile) w = way(a, rows <= 16 ? kFewCosts : kMoreCosts, tile, quant_few_resident(tile, a.dim));
+  if (rows > kQuantFewRows) {
+    // (two or more tiles of warp products for a small call: they start and end
+    // sooner; 78 rows of 10 sequences on 2052 rows: 33 us on the tensor cores)
+    const Way t = rows <= 64 ? way(a, kTc64Costs, 64, 1) : way(a, kTc128Costs, 128, 1);
+    if (t.us <= w.us) {
+      w = t;
+      p.tc = 1;
+    }
   }
-  *ctas = p.splits == 0 ? runs : (int)units;
+  p.splits = w.splits;
+  if (p.splits == 0) {
+    p.part_bytes = align_up((uint64_t)2 * w.ctas * w.row_tile * a.dim * 4);
+    p.ml_bytes = align_up((uint64_t)2 * w.ctas * w.row_tile * 8);
+    p.unit_bytes = align_up((uint64_t)w.units * 8);
+  }
+  *ctas = w.ctas;
+  *row_tile = w.row_tile;
   return p;
 }
 
-int run_quant_attention(QuantArgs a, const CachedPlan& p, int ctas, void* workspace, cudaStream_t s) {
+int run_quant_attention(QuantArgs a, const CachedPlan& p, int ctas, int row_tile, void* workspace, cudaStream_t s) {
   char* w = static_cast<char*>(workspace);
   a.splits = p.splits;
   a.part = reinterpret_cast<float*>(w);
   a.ml = reinterpret_cast<float*>(w + p.part_bytes);
   a.units = reinterpret_cast<int4*>(w + p.part_bytes + p.ml_bytes);
-  return p.tc ? launch_quant_rows(a, ctas, s) : launch_quant_few(a, ctas, s);
+  return p.tc ? launch_quant_rows(a, ctas, s) : launch_quant_few(a, ctas, row_tile, s);
 }
 
 namespace {
@@ -261,8 +288,8 @@ int swapnet_attention_quantized_workspace(const swapnet_quantized_attention* c, 
     if (!bytes) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "null output");
     QuantArgs a;
     if (int rc = check_quant(c, &a)) return rc;
-    int ctas;
-    *bytes = plan_bytes(quant_plan(a, &ctas));
+    int ctas, row_tile;
+    *bytes = plan_bytes(quant_plan(a, &ctas, &row_tile));
     return SWAPNET_OK;
   });
 }
@@ -272,8 +299,8 @@ int swapnet_attention_quantized(const swapnet_quantized_attention* c, void* work
     using namespace swapnet;
     QuantArgs a;
     if (int rc = check_quant(c, &a)) return rc;
-    int ctas;
-    const CachedPlan p = quant_plan(a, &ctas);
+    int ctas, row_tile;
+    const CachedPlan p = quant_plan(a, &ctas, &row_tile);
     const uint64_t need = plan_bytes(p);
     if (need && !workspace) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "quantised attention: null workspace");
     if (workspace_bytes < need) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "quantised attention: workspace too small");
@@ -281,7 +308,7 @@ int swapnet_attention_quantized(const swapnet_quantized_attention* c, void* work
     if (shares({c->out, c->lse, need ? workspace : nullptr}, {c->q, c->k, c->v, c->k_scale, c->v_scale, c->lens, c->counts}))
       SN_FAIL(SWAPNET_ERR_INVALID_ARG, "quantised attention: a result must not be an input or another result");
     if (int rc = error_word(&a.err)) return rc;
-    return run_quant_attention(a, p, ctas, workspace, reinterpret_cast<cudaStream_t>(stream));
+    return run_quant_attention(a, p, ctas, row_tile, workspace, reinterpret_cast<cudaStream_t>(stream));
   });
 }
 

@@ -35,14 +35,15 @@ struct QuantArgs : CachedArgs {
   int code, block, block_log2, blocks;
   const float *k_scale, *v_scale;
 };
-// How a call runs, from its sizes alone; ctas: of its attention launch.
-CachedPlan quant_plan(const QuantArgs& a, int* ctas);
-int run_quant_attention(QuantArgs a, const CachedPlan& p, int ctas, void* workspace, cudaStream_t s);
-constexpr int kQuantFewRows = 32;  // of a (sequence, key head) that the warp products take
+// How a call runs, from its sizes alone; ctas: of its attention launch,
+// row_tile: rows of a unit.
+CachedPlan quant_plan(const QuantArgs& a, int* ctas, int* row_tile);
+int run_quant_attention(QuantArgs a, const CachedPlan& p, int ctas, int row_tile, void* workspace, cudaStream_t s);
+constexpr int kQuantFewRows = 32;  // of a unit, at most, on warp products
 // Their CTAs that an SM holds, by registers and shared memory.
 constexpr int quant_few_resident(int rows, int dim) { return rows <= 8 ? (dim == 64 ? 4 : 3) : rows <= 16 && dim == 64 ? 3 : 2; }
 int launch_quant_join(const QuantArgs& a, int queries, int row_tile, int nrt, cudaStream_t s);  // the units that runs shared
-int launch_quant_few(const QuantArgs& a, int ctas, cudaStream_t s);   // warp products, with the join
+int launch_quant_few(const QuantArgs& a, int ctas, int row_tile, cudaStream_t s);  // warp products, with the join
 int launch_quant_rows(const QuantArgs& a, int ctas, cudaStream_t s);  // tcgen05, with the join
 
 }  // namespace swapnet

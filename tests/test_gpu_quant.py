@@ -224,6 +224,11 @@ class Append:
     dict(dtype="bf16", fmt="bf16", n_seq=2, tokens=600, heads=14, kv_heads=6, dim=128, max_seq=700, block=0, lens=[100, 0], counts=[600, 599],
          halves=True, rope_dim=16),
     dict(dtype="bf16", fmt="bf16", n_seq=1, tokens=4, heads=0, kv_heads=3, dim=128, max_seq=4, block=0, lens=[0], norm=True, theta=500000.0, far=1 << 24),
+    # many rows, eight heads of a token in the same lanes (the last ones fewer)
+    dict(dtype="f16", fmt="e4m3", n_seq=1, tokens=1100, heads=19, kv_heads=2, dim=128, max_seq=1200, block=128, lens=[77], norm=True, halves=True,
+         sections=(24, 20, 20), far=100000, pad=8),
+    dict(dtype="bf16", fmt="i8", n_seq=2, tokens=1030, heads=9, kv_heads=1, dim=64, max_seq=1030, block=64, lens=[0, 0], counts=[1030, 1001],
+         rope_dim=48),
 ])
 def test_append_against_the_definition(kw):
     c = Append(seed=3, **kw)
@@ -280,6 +285,26 @@ def test_append_leaves_a_sequence_without_room_alone():
             # the others are done
             assert c.lens_out.tolist()[1:] == [16, 14] and not (c.q_out[1:] == SENT).all()
     capi.device_sync()
+
+
+def test_rows_taken_back():
+    """A sequence whose last rows are taken back, within the open block: what is appended then is as if they had never been."""
+    torch = _torch()
+    kw = dict(dtype="bf16", fmt="i8", n_seq=1, heads=2, kv_heads=2, dim=64, max_seq=64, block=32, norm=True)
+    a, b = (Append(tokens=10, lens=[0], seed=1, **kw) for _ in range(2))
+    a.call(in_place=True), b.call(in_place=True)
+    gone = Append(tokens=9, lens=[10], seed=2, std=50.0, **kw)  # larger values: other scales and codes
+    last = Append(tokens=5, lens=[10], seed=3, **kw)
+    again = Append(tokens=5, lens=[10], seed=3, **kw)
+    for x, of in ((gone, a), (last, a), (again, b)):
+        for name in ("k", "v", "ks", "vs", "ko", "vo"):
+            setattr(x, name, getattr(of, name))
+        x.gains = a.gains
+        x.call(in_place=True)
+    capi.device_sync()
+    for name in ("k", "v", "ko", "vo"):
+        assert torch.equal(getattr(a, name)[:, :15], getattr(b, name)[:, :15])
+    assert torch.equal(a.ks[:, :, :1], b.ks[:, :, :1]) and torch.equal(a.vs[:, :, :1], b.vs[:, :, :1])
 
 
 def test_append_reports_positions_out_of_range():
@@ -488,6 +513,17 @@ class Attend:
     dict(dtype="f16", fmt="e4m3", n_seq=2, tokens=70, heads=4, kv_heads=2, dim=128, max_seq=600, block=16, lens=[600, 64], spread=20.0),
     dict(dtype="bf16", fmt="e4m3", n_seq=2, tokens=1, heads=4, kv_heads=1, dim=128, max_seq=300, block=32, lens=[300, 299], std=1e-30),
     dict(dtype="bf16", fmt="i8", n_seq=2, tokens=33, heads=4, kv_heads=1, dim=128, max_seq=300, block=32, lens=[300, 299], std=1e4, scale=1e-5),
+    # rows of other strides on the tensor cores, one and two rows a lane
+    dict(dtype="f16", fmt="i8", n_seq=2, tokens=50, heads=4, kv_heads=2, dim=64, max_seq=400, block=16, lens=[399, 50], pad=24),
+    dict(dtype="bf16", fmt="e4m3", n_seq=2, tokens=11, heads=8, kv_heads=2, dim=128, max_seq=400, block=128, lens=[399, 250], pad=8),
+    # runs of tiles over more sequences than a CTA keeps sizes of, some of them empty
+    dict(dtype="bf16", fmt="i8", n_seq=70, tokens=2, heads=2, kv_heads=1, dim=64, max_seq=9000, block=64,
+         lens=[(i * 1237) % 3000 * (i % 5 > 0) for i in range(69)] + [9000], counts=[2 - i % 3 % 2 for i in range(70)]),
+    dict(dtype="f16", fmt="e4m3", n_seq=66, tokens=40, heads=1, kv_heads=1, dim=64, max_seq=6000, block=16,
+         lens=[(i * 1237) % 1000 * (i % 4 > 0) for i in range(65)] + [6000], counts=[40 - i % 41 for i in range(66)]),
+    # a unit over many runs: tails of one tile, rows that see nothing of them
+    dict(dtype="f16", fmt="i8", n_seq=1, tokens=30, heads=1, kv_heads=1, dim=128, max_seq=20000, block=32, lens=[19970]),
+    dict(dtype="bf16", fmt="e4m3", n_seq=1, tokens=300, heads=1, kv_heads=1, dim=128, max_seq=9000, block=64, lens=[8833]),
 ])
 def test_attention_against_the_definition(kw):
     c = Attend(seed=6, **kw)
@@ -496,10 +532,11 @@ def test_attention_against_the_definition(kw):
     c.check()
 
 
-@pytest.mark.parametrize("tokens,heads", [(1, 4), (6, 4), (50, 4), (150, 2)])
-def test_attention_leaves_bad_sequences_alone(tokens, heads):
-    for lens, counts in (([301, 300], None), ([-1, 300], None), ([200, 300], [tokens + 1, tokens]), ([200, 300], [-1, tokens])):
-        c = Attend("bf16", "i8", 2, tokens, heads, 2, 128, 300, 32, lens, counts, seed=2)
+@pytest.mark.parametrize("tokens,heads,max_seq", [(1, 4, 300), (6, 4, 300), (50, 4, 300), (150, 2, 300), (1, 4, 9000), (12, 4, 9000), (50, 2, 9000)])
+def test_attention_leaves_bad_sequences_alone(tokens, heads, max_seq):
+    """A CTA per unit (short caches) or equal runs (long ones)."""
+    for lens, counts in (([max_seq + 1, 300], None), ([-1, 300], None), ([200, 300], [tokens + 1, tokens]), ([200, 300], [-1, tokens])):
+        c = Attend("bf16", "i8", 2, tokens, heads, 2, 128, max_seq, 32, lens, counts, seed=2)
         c.call()
         with pytest.raises(capi.SwapnetError) as e:
             capi.device_sync()
