@@ -982,8 +982,9 @@ int swapnet_cache_append(const swapnet_cache_rows* args, swapnet_stream stream);
  * element), probabilities times their value scales as two fp16 parts: 22 bits,
  * off by at most 2^-39 of a query's largest such product up to 32 rows (tokens x
  * heads / kv_heads), beyond by 2^-32 in short caches and in the first 2048 rows
- * that a CTA takes of a long one, 2^-37 in the rest.  A value scale below 2^-100
- * counts as 2^-100; scales are not negative.
+ * that a CTA takes of a long one, 2^-37 in the rest.  All that holds for value
+ * scales from 2^-48 to 2^64 beside one another; the values of smaller ones lose
+ * bits, and from 2^-79 on may count as 0.  Scales are not negative.
  * `workspace` as for swapnet_attention_tree: a function of the sizes; how many
  * CTAs share a cache goes by max_seq.  Results and workspace overlap
  * none of the inputs.  Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA. */

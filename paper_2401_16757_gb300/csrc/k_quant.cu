@@ -20,7 +20,6 @@ namespace {
 
 constexpr int kStep = 32;     // keys of a warp's step
 constexpr int kQfStages = 2;
-constexpr float kTop = 14.0f; // log2 of the largest p: times its scale's fraction below 2 it stays within fp16
 
 // W warps; up to 8 NR rows.
 template <int D, int NR, int W> struct QfCfg {

@@ -25,7 +25,7 @@
 // Measured: 1000 queries on 4096 rows, 2 sequences x 32 heads, f16, I8: 181 us,
 // 0.49 PFLOP/s (the second product of P not counted; the 16-bit caches' 124); 64
 // rows of 32 x 8 units on up to 8000 rows about 135.  No pipe is full: a tile of
-// 128 x 128 takes about 3500 cycles, of which the tensor pipe is busy for 1600,
+// 128 x 128 takes about 4300 cycles, of which the tensor pipe is busy for 1540,
 // the softmax warps for 2500 (64 rows: 1700), the conversion for 1550 (E4M3
 // 1000); shared memory moves by count 260 KB of the 450 that it could, half of it
 // codes and their fp16 form; instructions wait for their cache.  Slower: the
@@ -50,9 +50,8 @@ constexpr int kSoftThreads = 256, kConvThreads = 128;
 constexpr int kQtThreads = 128 + kConvThreads + kSoftThreads;
 constexpr int kRegsIssue = 56, kRegsConv = 88, kRegsSoft = 184;
 static_assert(128 * kRegsIssue + kConvThreads * kRegsConv + kSoftThreads * kRegsSoft <= kQtThreads * 128, "registers of a CTA");
-// Where p lies, in log2 (see the 16-bit caches' PRange): times f below 2 it ends
-// at 2^15.
-constexpr float kMost = 14.0f, kWide = 7.0f, kTight = 12.0f;
+// Where p lies, in log2 (see the 16-bit caches' PRange, and split_scale).
+constexpr float kMost = kTop, kWide = kTop - 7.0f, kTight = kTop - 2.0f;
 constexpr int kTightAt = 16;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kTmO = 256;  // columns of O_0, O_1 behind it; S and P as there
@@ -112,7 +111,6 @@ __global__ void __launch_bounds__(kQtThreads, 1)
   constexpr int kRowsMax = 128 / REP;
   constexpr int NK = 64 / REP;  // keys of a thread and tile
   constexpr int NG = NK / 16;   // parts of them
-  constexpr int kParts = 2;  // of a probability
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   float2* ml = reinterpret_cast<float2*>(smem + F::kOffX);
@@ -272,7 +270,7 @@ __global__ void __launch_bounds__(kQtThreads, 1)
             tc_fence_after();
             const uint32_t pt = tmem + (uint32_t)(g & 1) * 128u + (uint32_t)h * 64u;
 #pragma unroll
-            for (int part = 0; part < kParts; ++part)
+            for (int part = 0; part < 2; ++part)  // of the probabilities
 #pragma unroll
               for (int ks = 0; ks < 4; ++ks)  // 16 keys a step
                 tc_mma_f16_ta(tmem + kTmO + (uint32_t)h * 128u, pt + (uint32_t)(part * 32 + ks * 8),
@@ -448,7 +446,7 @@ __global__ void __launch_bounds__(kQtThreads, 1)
         ok = ok && mbar_wait_bounded(s_full(g), (g >> 1) & 1, abort_flag, a.err);
         ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
-        uint32_t hi[NK / 2], lo[kParts > 1 ? NK / 2 : 1];
+        uint32_t hi[NK / 2], lo[NK / 2];
         if (works) {
           float2 y[NK / 2];
           float mx = -INFINITY;
@@ -527,12 +525,10 @@ __global__ void __launch_bounds__(kQtThreads, 1)
               for (int k = 0; k < 8; ++k) p[k] = mul2(p[k], frac);
 #pragma unroll
               for (int k = 0; k < 8; ++k) hi[k0 + k] = pack_pair<__half>(p[k].x, p[k].y);
-              if (kParts > 1) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) p[k] = fma2(unpack_pair<__half>(hi[k0 + k]), minus, p[k]);
+              for (int k = 0; k < 8; ++k) p[k] = fma2(unpack_pair<__half>(hi[k0 + k]), minus, p[k]);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) lo[k0 + k] = pack_pair<__half>(p[k].x, p[k].y);
-              }
+              for (int k = 0; k < 8; ++k) lo[k0 + k] = pack_pair<__half>(p[k].x, p[k].y);
             }
             l += (sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y);
           }
@@ -541,7 +537,7 @@ __global__ void __launch_bounds__(kQtThreads, 1)
           if (works) {
             // over the half's scores: hi parts of its keys, then the lo parts
 #pragma unroll
-            for (int u = 0; u < kParts; ++u) {
+            for (int u = 0; u < 2; ++u) {
               const uint32_t* x = u ? lo : hi;
 #pragma unroll
               for (int c = 0; c < 32; c += 16) {

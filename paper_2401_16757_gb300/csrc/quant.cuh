@@ -66,11 +66,16 @@ __device__ __forceinline__ uint32_t numbers_only(uint32_t x) {
   return x & ~(none | (none - (none >> 7)));
 }
 
-// scale = 2^e * f with f in [1, 2) and inv = 2^-e; scales below 2^-100 count as
-// that, those that are no number or infinite keep f so.
+// A value scale = 2^e * f with f in [1, 2), and inv = 2^-e; scales below 2^-48
+// have e = -48 and smaller f, those that are no number or infinite keep f so.
+// The softmax takes p = 2^(score + e - m) with p <= 2^14, adds p inv to its sum
+// and gives p f, at most 2^15, to the products.  A key loses its weight only
+// where p falls below 2^-126: one of a block of zeros beside value scales of
+// 2^64 where it is below 2^-28 of the largest (a least e of -100 left nothing of
+// zeros beside scales of 2^40).
+constexpr float kTop = 14.0f;  // log2 of the largest p
 __device__ __forceinline__ void split_scale(float scale, float* e, float* f, float* inv) {
-  scale = scale < kLeastScale ? kLeastScale : scale;
-  const int x = min((int)(__float_as_uint(scale) >> 23 & 0xffu), 253);
+  const int x = min(max((int)(__float_as_uint(scale) >> 23 & 0xffu), 127 - 48), 253);
   *inv = __uint_as_float((uint32_t)(254 - x) << 23);
   *f = scale * *inv;
   *e = (float)(x - 127);

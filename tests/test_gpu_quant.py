@@ -591,6 +591,46 @@ def test_a_dominant_key_hides_nothing(tokens):
     assert ((got - want[:, None]).abs() <= want[:, None] * (2.0 ** -11 + 2.0 ** -10 * 2.0 ** -3)).all()
 
 
+@pytest.mark.parametrize("tokens,max_seq", [(1, 900), (1, 9000), (40, 900), (150, 900)])
+@pytest.mark.parametrize("least", [2.0 ** -100, 2.0 ** -48])
+def test_zeros_beside_large_values_keep_their_weights(tokens, max_seq, least):
+    """All scores equal; every other block of 16 rows has small values, the others large ones: the mean of what is seen."""
+    torch = _torch()
+    for large in (1.0, 2.0 ** 40, 2.0 ** 64):
+        c = Attend("bf16", "i8", 1, tokens, 2, 1, 128, max_seq, 16, [max_seq], seed=5)
+        c.q.zero_(), c.v.fill_(64)
+        c.vs[0, 0, 0::2], c.vs[0, 0, 1::2] = least, large
+        if least < 2.0 ** -48:
+            for i in range(0, max_seq, 32):
+                c.v[0, i:i + 16] = 0
+        c.call()
+        capi.device_sync()
+        n = max_seq - tokens + torch.arange(1, tokens + 1)
+        big = n // 32 * 16 + (n % 32 - 16).clamp(min=0)
+        want = (64 * large * big + (64 * least if least == 2.0 ** -48 else 0.0) * (n - big)).double() / n
+        got = c.out.double().cpu()[0]
+        # half a step of bf16; sums of n equal terms, two parts of p and the division: (n / 16 + 40) 2^-23
+        tol = want * (2.0 ** -8 + (max_seq / 16 + 40) * 2.0 ** -23)
+        assert ((got - want[:, None]).abs() <= tol[:, None]).all(), (large, ((got / want[:, None]) - 1).abs().max().item())
+        lse = c.lse.double().cpu()[0]
+        assert ((lse - torch.log(n.double())).abs() <= (max_seq / 16 + 40) * 2.0 ** -22).all()
+
+
+def test_values_below_the_least_exponent():
+    """Scales under 2^-48 lose bits from below: 2^-39 of 2^-48, whatever the scale."""
+    torch = _torch()
+    for tokens in (1, 40, 150):
+        for small in (2.0 ** -60, 2.0 ** -70):
+            c = Attend("bf16", "e4m3", 1, tokens, 2, 1, 64, 700, 32, [700], seed=7)
+            c.q.zero_(), c.v.fill_(64), c.vs.fill_(small)
+            c.call()
+            capi.device_sync()
+            want = torch.full((tokens, 128), 64 * small, dtype=torch.float64)
+            # p is at least 2^7 (more rows: where the first keys put it), so that half of 2^-24 is 2^-32 of 2^-48 / scale
+            tol = want * (2.0 ** -8 + (700 / 16 + 40) * 2.0 ** -23 + 2.0 ** -32 * 2.0 ** -48 / small)
+            assert ((c.out.double().cpu()[0] - want).abs() <= tol).all(), (tokens, small)
+
+
 def test_large_offsets():
     """Rows of a cache beyond 2^32 bytes."""
     torch = _torch()
