@@ -980,9 +980,9 @@ int swapnet_cache_append(const swapnet_cache_rows* args, swapnet_stream stream);
  * fp16 numbers that hold their codes exactly, queries as fp16 (BF16 ones scaled
  * by a power of two per query, which loses what is below 2^-39 of its largest
  * element), probabilities times their value scales as two fp16 parts: 22 bits,
- * off by at most 2^-39 of a query's largest such product up to 32 rows (tokens x
- * heads / kv_heads), beyond by 2^-32 in short caches and in the first 2048 rows
- * that a CTA takes of a long one, 2^-37 in the rest.  All that holds for value
+ * off by at most 2^-39 of a query's largest such product up to 16 rows (tokens x
+ * heads / kv_heads; 32 with a head_dim of 64), beyond by 2^-32 (2^-37 where more
+ * than 32 rows are behind the first 2048 that a CTA takes of a long cache).  All that holds for value
  * scales from 2^-48 to 2^64 beside one another; the values of smaller ones lose
  * bits, and from 2^-79 on may count as 0.  Scales are not negative.
  * `workspace` as for swapnet_attention_tree: a function of the sizes; how many

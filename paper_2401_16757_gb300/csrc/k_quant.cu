@@ -70,8 +70,9 @@ template <int D, int NR, int W> struct QfCfg {
 // any product take 252, a copy of as many bytes 238, so that DRAM bounds it.  12
 // rows of 4 key heads of 64, E4M3, on 131001 rows: 26.6 us, of which start, end
 // and join are 11.  32 rows of 32 x 8 (sequence, head)s on up to 8000 rows (0.34
-// GB): 130 us: two warps a scheduler (255 registers), whose products fill the
-// pipe to 0.46 and whose instructions issue in 0.41 of the cycles.  One row of 32
+// GB): 131 us: two warps a scheduler (255 registers), whose products fill the
+// pipe to 0.46 and whose instructions issue in 0.41 of the cycles
+// (k_quant_keys.cu takes that call: 112).  One row of 32
 // heads on 543 rows: 9.2 us, five tiles of 1.2 us and the launch; one row of 8 heads on
 // 100 rows 5.0, all of it latency.  Consecutive products of the same sums are kept
 // apart (decode 274 to 262 us, in the same form).

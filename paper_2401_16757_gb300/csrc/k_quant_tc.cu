@@ -74,18 +74,6 @@ template <int D> struct QtCfg {
   static_assert(kSmem <= 232448, "shared memory of a CTA");
 };
 
-// The power of two that a BF16 query row is divided by: its largest element
-// comes to lie in [2^14, 2^15).  From the bits of the largest magnitude its
-// exponent field, kept where both factors are normal numbers.
-__device__ __forceinline__ uint32_t largest_bits(const uint4& v) {
-  const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
-  return max(m & 0xffffu, m >> 16);
-}
-__device__ __forceinline__ int query_exponent(uint32_t most) { return min(max((int)(most >> 7), 28), 254); }
-__device__ __forceinline__ uint32_t query_pair(uint32_t x, float by) {
-  const float2 u = unpack_pair<__nv_bfloat16>(x);
-  return pack_pair<__half>(u.x * by, u.y * by);
-}
 // What a row's queries have been divided by.
 template <typename T, int D> __device__ __forceinline__ float query_scale(const T* q) {
   if (std::is_same<T, __half>::value) return 1.0f;  // (as they are)
@@ -93,14 +81,6 @@ template <typename T, int D> __device__ __forceinline__ float query_scale(const 
 #pragma unroll
   for (int c = 0; c < D / 8; ++c) most = max(most, largest_bits(reinterpret_cast<const uint4*>(q)[c]));
   return __uint_as_float((uint32_t)(query_exponent(most) - 14) << 23);
-}
-
-__device__ __forceinline__ float2 mul2(float2 x, float2 y) {
-  float2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;"
-      : "=l"(reinterpret_cast<unsigned long long&>(r))
-      : "l"(reinterpret_cast<unsigned long long&>(x)), "l"(reinterpret_cast<unsigned long long&>(y)));
-  return r;
 }
 
 template <typename T, int D, int CODE, int REP>
@@ -673,13 +653,8 @@ template <typename T, int D, int CODE, int REP> int rows_t(const QuantArgs& a, i
     attr_set(known);
   }
   const int queries = std::min(128 / REP / a.group, a.tokens), nrt = (a.tokens + queries - 1) / queries;
-  const uint64_t dims[3] = {(uint64_t)a.kv_heads * a.dim, (uint64_t)a.max_seq, (uint64_t)a.n_seq};
-  // (a single sequence's stride is never used, but has to be a valid one)
-  const uint64_t strides[2] = {(uint64_t)a.kv_stride, (uint64_t)(a.n_seq > 1 ? a.seq_stride : a.kv_stride)};
-  const uint32_t box[3] = {(uint32_t)D, kKeys, 1};
   CUtensorMap k, v;
-  int rc = make_tmap_codes(&k, a.k, dims, strides, box);
-  if (!rc) rc = make_tmap_codes(&v, a.v, dims, strides, box);
+  int rc = quant_maps(a, &k, &v, false);
   if (rc) return rc;
   kern<<<ctas, kQtThreads, QtCfg<D>::kSmem, s>>>(k, v, a, queries, nrt);
   rc = fail(cudaSuccess, "quantised attention launch");

@@ -955,12 +955,13 @@ int make_tmap_3d(CUtensorMap* m, int dtype, const void* base, const uint64_t (&d
   return SWAPNET_OK;
 }
 
-int make_tmap_codes(CUtensorMap* m, const void* base, const uint64_t (&dims)[3], const uint64_t (&stride_bytes)[2], const uint32_t (&box)[3]) {
+int make_tmap_codes(CUtensorMap* m, const void* base, const uint64_t (&dims)[3], const uint64_t (&stride_bytes)[2], const uint32_t (&box)[3],
+                    bool swizzled) {
   if (((uintptr_t)base & 15) || ((stride_bytes[0] | stride_bytes[1]) & 15) || box[0] % 16)
     SN_FAIL(SWAPNET_ERR_MISALIGNED, "TMA operand must be 16-byte aligned with 16-byte multiple strides");
   const cuuint64_t d[3] = {dims[0], dims[1], dims[2]}, st[2] = {stride_bytes[0], stride_bytes[1]};
   const cuuint32_t b[3] = {box[0], box[1], box[2]}, estr[3] = {1, 1, 1};
-  const CUresult r = encode_tiled(m, SWAPNET_I8, 3, base, d, st, b, estr, CU_TENSOR_MAP_SWIZZLE_NONE);
+  const CUresult r = encode_tiled(m, SWAPNET_I8, 3, base, d, st, b, estr, swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE);
   if (r != CUDA_SUCCESS) SN_FAIL(SWAPNET_ERR_CUDA, "cuTensorMapEncodeTiled failed (" + std::to_string((int)r) + ")");
   return SWAPNET_OK;
 }

@@ -214,8 +214,9 @@ int make_tmap_2d(CUtensorMap* m, int dtype, const void* base, uint64_t inner, ui
 int make_tmap_3d(CUtensorMap* m, int dtype, const void* base, const uint64_t (&dims)[3], const uint64_t (&stride_bytes)[2],
                  const uint32_t (&box)[3]);
 
-// The same of bytes, as they are (no swizzle).
-int make_tmap_codes(CUtensorMap* m, const void* base, const uint64_t (&dims)[3], const uint64_t (&stride_bytes)[2], const uint32_t (&box)[3]);
+// The same of bytes, as they are or (boxes 128 bytes wide) with the 128-byte swizzle.
+int make_tmap_codes(CUtensorMap* m, const void* base, const uint64_t (&dims)[3], const uint64_t (&stride_bytes)[2], const uint32_t (&box)[3],
+                    bool swizzled);
 
 // tcgen05 causal attention for query runs (prefill): q [tokens][width]
 // (already rotated), key and value caches [max_seq][width], head width 128,

@@ -12,13 +12,14 @@
 namespace swapnet {
 
 // Microseconds: a unit's start and end, a tile of 128 keys by itself and its
-// share of a busy SM's time, the join of shared units; warp products of up to
-// 16 and 32 rows, the tensor cores' 64 and 128.
+// share of a busy SM's time, the join of shared units, rounds of more units than
+// fit at once, at least; warp products of up to 16 and 32 rows, the tensor cores
+// with keys as rows (32), with rows of 64 and 128.
 struct Costs {
-  double unit, tile, busy, join;
+  double unit, tile, busy, join, rounds;
 };
-constexpr Costs kFewCosts = {3.0, 0.9, 0.8, 5.0}, kMoreCosts = {6.0, 1.3, 1.05, 6.0}, kTc64Costs = {8.0, 1.8, 1.8, 10.0},
-                kTc128Costs = {8.0, 2.3, 2.3, 10.0};
+constexpr Costs kFewCosts = {3.0, 0.9, 0.8, 5.0, 1.0}, kMoreCosts = {6.0, 1.3, 1.05, 6.0, 1.0}, kKeyCosts = {7.0, 0.8, 0.8, 8.0, 2.0},
+                kTc64Costs = {8.0, 1.8, 1.8, 10.0, 1.0}, kTc128Costs = {8.0, 2.3, 2.3, 10.0, 1.0};
 // CTAs that share the tiles of all units: as many as are resident, or for up to
 // 16 rows, which the memory bounds, up to six times that where their runs are
 // long: the memory does not serve all SMs alike, and CTAs that start later even
@@ -44,7 +45,7 @@ static Way way(const QuantArgs& a, const Costs& c, int row_tile, int resident) {
   const double tiles = (a.max_seq + 127) / 128, slots = (double)kSms * resident;
   int runs = std::max(1, kSms * resident / a.kv_heads) * a.kv_heads;
   auto per_tile = [&](double on_sm) { return std::max(c.tile, c.busy * std::min((double)resident, std::ceil(on_sm))); };
-  const double alone = (c.unit + per_tile((double)w.units / kSms) * tiles) * (w.units <= slots ? 1.0 : w.units / slots + 0.1);
+  const double alone = (c.unit + per_tile((double)w.units / kSms) * tiles) * (w.units <= slots ? 1.0 : std::max(c.rounds, w.units / slots + 0.1));
   const double mine = std::max(2.0, w.units * tiles / runs);  // tiles of a run
   const double shared = c.unit * (1.0 + (double)w.units / runs) + per_tile(w.units * tiles / mine / kSms) * mine + c.join;
   if (row_tile <= 16) runs *= (int)std::min(6.0, std::max(1.0, mine / kRunLeast));
@@ -63,6 +64,16 @@ CachedPlan quant_plan(const QuantArgs& a, int* ctas, int* row_tile) {
   Way w;
   w.us = 1e30;
   if (a.group <= tile) w = way(a, rows <= 16 ? kFewCosts : kMoreCosts, tile, quant_few_resident(tile, a.dim));
+  if (rows > 16 && rows <= kQuantFewRows && a.dim == 128) {
+    // (32 sequences, 8 key heads of 32 rows, up to 8000 keys 112 us, on warp
+    // products 131; 4 of up to 500 keys 12.5 and 18.3; 64 rows as two units 208,
+    // with rows as rows 161)
+    const Way t = way(a, kKeyCosts, kQuantFewRows, 1);
+    if (t.us <= w.us) {
+      w = t;
+      p.tc = 2;
+    }
+  }
   if (rows > kQuantFewRows) {
     // (two or more tiles of warp products for a small call: they start and end
     // sooner; 78 rows of 10 sequences on 2052 rows: 33 us on the tensor cores)
@@ -89,6 +100,7 @@ int run_quant_attention(QuantArgs a, const CachedPlan& p, int ctas, int row_tile
   a.part = reinterpret_cast<float*>(w);
   a.ml = reinterpret_cast<float*>(w + p.part_bytes);
   a.units = reinterpret_cast<int4*>(w + p.part_bytes + p.ml_bytes);
+  if (p.tc == 2) return launch_quant_keys(a, ctas, s);
   return p.tc ? launch_quant_rows(a, ctas, s) : launch_quant_few(a, ctas, row_tile, s);
 }
 

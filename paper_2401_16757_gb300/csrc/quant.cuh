@@ -2,6 +2,7 @@
 // fp16, queries to fp16, scales.
 #pragma once
 #include "cached_tc.cuh"
+#include "kernels.h"
 #include "quant.h"
 
 namespace swapnet {
@@ -112,6 +113,26 @@ template <typename T, int C> __device__ __forceinline__ float query_fp16(const u
   return __uint_as_float((uint32_t)(127 + (x - 127) - 14) << 23);
 }
 
+// The power of two that a BF16 query row is divided by: its largest element
+// comes to lie in [2^14, 2^15).  From the bits of the largest magnitude its
+// exponent field, kept where both factors are normal numbers.
+__device__ __forceinline__ uint32_t largest_bits(const uint4& v) {
+  const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+  return max(m & 0xffffu, m >> 16);
+}
+__device__ __forceinline__ int query_exponent(uint32_t most) { return min(max((int)(most >> 7), 28), 254); }
+__device__ __forceinline__ uint32_t query_pair(uint32_t x, float by) {
+  const float2 u = unpack_pair<__nv_bfloat16>(x);
+  return pack_pair<__half>(u.x * by, u.y * by);
+}
+__device__ __forceinline__ float2 mul2(float2 x, float2 y) {
+  float2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<unsigned long long&>(r))
+      : "l"(reinterpret_cast<unsigned long long&>(x)), "l"(reinterpret_cast<unsigned long long&>(y)));
+  return r;
+}
+
 // ------------------------------------------------------------------ runs
 // Which tiles a CTA of an attention launch takes: with a.splits == 1 unit
 // blockIdx / kv_heads of its key head, otherwise an equal run of all the head's
@@ -205,6 +226,17 @@ __device__ __forceinline__ void record_unit(const CachedArgs& a, const Run& r, c
     pieces = c - r.run + 1;
   }
   reinterpret_cast<int2*>(a.units)[((int64_t)cur.b * nrt + cur.rt) * a.kv_heads + r.kvh] = make_int2(blockIdx.x, pieces);
+}
+
+// Tensor maps of a call's codes, in tiles of kKeys rows of a head; swizzled: the
+// keys' 16-byte chunks by the 128-byte pattern (rows of 128 codes).
+inline int quant_maps(const QuantArgs& a, CUtensorMap* k, CUtensorMap* v, bool swizzled) {
+  const uint64_t dims[3] = {(uint64_t)a.kv_heads * a.dim, (uint64_t)a.max_seq, (uint64_t)a.n_seq};
+  // (a single sequence's stride is never used, but has to be a valid one)
+  const uint64_t strides[2] = {(uint64_t)a.kv_stride, (uint64_t)(a.n_seq > 1 ? a.seq_stride : a.kv_stride)};
+  const uint32_t box[3] = {(uint32_t)a.dim, kKeys, 1};
+  if (int rc = make_tmap_codes(k, a.k, dims, strides, box, swizzled)) return rc;
+  return make_tmap_codes(v, a.v, dims, strides, box, false);
 }
 
 }  // namespace swapnet

@@ -35,8 +35,9 @@ struct QuantArgs : CachedArgs {
   int code, block, block_log2, blocks;
   const float *k_scale, *v_scale;
 };
-// How a call runs, from its sizes alone; ctas: of its attention launch,
-// row_tile: rows of a unit.
+// How a call runs, from its sizes alone; tc: 0 warp products, on the tensor cores
+// 1 rows as rows, 2 keys as rows; ctas: of its attention launch, row_tile: rows
+// of a unit.
 CachedPlan quant_plan(const QuantArgs& a, int* ctas, int* row_tile);
 int run_quant_attention(QuantArgs a, const CachedPlan& p, int ctas, int row_tile, void* workspace, cudaStream_t s);
 constexpr int kQuantFewRows = 32;  // of a unit, at most, on warp products
@@ -44,6 +45,7 @@ constexpr int kQuantFewRows = 32;  // of a unit, at most, on warp products
 constexpr int quant_few_resident(int rows, int dim) { return rows <= 8 ? (dim == 64 ? 4 : 3) : rows <= 16 && dim == 64 ? 3 : 2; }
 int launch_quant_join(const QuantArgs& a, int queries, int row_tile, int nrt, cudaStream_t s);  // the units that runs shared
 int launch_quant_few(const QuantArgs& a, int ctas, int row_tile, cudaStream_t s);  // warp products, with the join
+int launch_quant_keys(const QuantArgs& a, int ctas, cudaStream_t s);  // tcgen05, keys as rows: up to 32 rows 128 wide, with the join
 int launch_quant_rows(const QuantArgs& a, int ctas, cudaStream_t s);  // tcgen05, with the join
 
 }  // namespace swapnet

@@ -480,9 +480,12 @@ class Attend:
                 lse = (m + torch.log(l))[..., 0]
                 p = p / torch.where(l > 0, l, torch.ones_like(l))
                 want, size = p @ v, p @ v.abs()
-                part = (p[..., None, :] * v.abs().T[None, None]).amax(-1) if ln * c * grp * d <= 1 << 26 else size  # of the largest p |v|
+                # p times a value scale, 2^7 or more where it is largest, is off by up to half of fp16's least step, 2^-25:
+                # by 2^-32 of the largest, times the row's code
+                vs = self.vs[b, e][row // B].double()
+                part = (p * vs).amax(-1)[..., None] * self.v[b, :ln, e * d:(e + 1) * d].double().abs().sum(0)
                 rel = 2 * off + 2.0 ** -21 + (ln / 16 + 40) * 2.0 ** -23 + 2.0 ** -22
-                tol = eps * want.abs() + rel[..., None] * size + ln * 2.0 ** -32 * part
+                tol = eps * want.abs() + rel[..., None] * size + 2.0 ** -32 * part
                 got = self.out[b, :c, e * grp * d:(e + 1) * grp * d].double().view(c, grp, d).transpose(0, 1)
                 ok = (got - want).abs() <= tol * (1 + 2.0 ** -10)
                 if self.dtype == "f16":  # from half a step behind its largest number on, 65520, the nearest fp16 is infinite
@@ -524,6 +527,17 @@ class Attend:
     # a unit over many runs: tails of one tile, rows that see nothing of them
     dict(dtype="f16", fmt="i8", n_seq=1, tokens=30, heads=1, kv_heads=1, dim=128, max_seq=20000, block=32, lens=[19970]),
     dict(dtype="bf16", fmt="e4m3", n_seq=1, tokens=300, heads=1, kv_heads=1, dim=128, max_seq=9000, block=64, lens=[8833]),
+    # 17 to 32 rows of 128 per key head
+    dict(dtype="f16", fmt="i8", n_seq=1, tokens=17, heads=1, kv_heads=1, dim=128, max_seq=128, block=16, lens=[128]),
+    dict(dtype="bf16", fmt="e4m3", n_seq=5, tokens=8, heads=16, kv_heads=4, dim=128, max_seq=700, block=64, lens=[0, 3, 128, 129, 700],
+         counts=[8, 5, 8, 0, 7], pad=16),
+    dict(dtype="bf16", fmt="i8", n_seq=3, tokens=3, heads=20, kv_heads=2, dim=128, max_seq=400, block=16, lens=[1, 257, 400], pad=8),
+    dict(dtype="f16", fmt="e4m3", n_seq=2, tokens=1, heads=31, kv_heads=1, dim=128, max_seq=3000, block=128, lens=[2999, 640]),
+    dict(dtype="f16", fmt="i8", n_seq=70, tokens=25, heads=2, kv_heads=2, dim=128, max_seq=1500, block=32,
+         lens=[(i * 1237) % 1400 * (i % 4 > 0) for i in range(69)] + [1500], counts=[25 - i % 26 for i in range(70)]),
+    dict(dtype="bf16", fmt="e4m3", n_seq=2, tokens=8, heads=8, kv_heads=2, dim=128, max_seq=40000, block=16, lens=[39999, 9], spread=20.0),
+    dict(dtype="bf16", fmt="i8", n_seq=40, tokens=4, heads=32, kv_heads=4, dim=128, max_seq=600, block=32,
+         lens=[(i * 731) % 600 + 1 for i in range(40)], std=4.0),
 ])
 def test_attention_against_the_definition(kw):
     c = Attend(seed=6, **kw)
@@ -532,7 +546,7 @@ def test_attention_against_the_definition(kw):
     c.check()
 
 
-@pytest.mark.parametrize("tokens,heads,max_seq", [(1, 4, 300), (6, 4, 300), (50, 4, 300), (150, 2, 300), (1, 4, 9000), (12, 4, 9000), (50, 2, 9000)])
+@pytest.mark.parametrize("tokens,heads,max_seq", [(1, 4, 300), (6, 4, 300), (12, 4, 300), (50, 4, 300), (150, 2, 300), (1, 4, 9000), (12, 4, 9000), (50, 2, 9000)])
 def test_attention_leaves_bad_sequences_alone(tokens, heads, max_seq):
     """A CTA per unit (short caches) or equal runs (long ones)."""
     for lens, counts in (([max_seq + 1, 300], None), ([-1, 300], None), ([200, 300], [tokens + 1, tokens]), ([200, 300], [-1, tokens])):
@@ -591,7 +605,7 @@ def test_a_dominant_key_hides_nothing(tokens):
     assert ((got - want[:, None]).abs() <= want[:, None] * (2.0 ** -11 + 2.0 ** -10 * 2.0 ** -3)).all()
 
 
-@pytest.mark.parametrize("tokens,max_seq", [(1, 900), (1, 9000), (40, 900), (150, 900)])
+@pytest.mark.parametrize("tokens,max_seq", [(1, 900), (1, 9000), (12, 900), (40, 900), (150, 900)])
 @pytest.mark.parametrize("least", [2.0 ** -100, 2.0 ** -48])
 def test_zeros_beside_large_values_keep_their_weights(tokens, max_seq, least):
     """All scores equal; every other block of 16 rows has small values, the others large ones: the mean of what is seen."""
@@ -631,6 +645,32 @@ def test_values_below_the_least_exponent():
             assert ((c.out.double().cpu()[0] - want).abs() <= tol).all(), (tokens, small)
 
 
+@pytest.mark.parametrize("tokens", [1, 12, 40, 150])
+@pytest.mark.parametrize("score", [-3000.0, 3000.0])
+def test_scores_far_from_zero(tokens, score):
+    """All scores equal and far from what exponentials hold: the mean of the values seen; then one key above all others."""
+    torch = _torch()
+    ln = 1400
+    c = Attend("f16", "i8", 1, tokens, 2, 1, 128, ln, 32, [ln], seed=13)
+    c.k.fill_(64 if score > 0 else -64), c.ks.fill_(1.0), c.vs.fill_(2.0 ** -6)
+    c.q.fill_(4.0)
+    c.scale = 3000 / (4 * 64 * 128.0)
+    c.v.zero_()
+    c.v[0, ::2] = 64
+    c.call()
+    capi.device_sync()
+    n = ln - tokens + torch.arange(1, tokens + 1)
+    want = ((n + 1) // 2).double() / n
+    got, lse = c.out.double().cpu()[0], c.lse.double().cpu()[0]
+    # half a step of fp16; the scores are exact (powers of two and 3000 / 2^15, one rounding each: 2^-22 of 3000 / ln 2 bits, for all the same)
+    assert ((got - want[:, None]).abs() <= want[:, None] * (2.0 ** -11 + (ln / 16 + 40) * 2.0 ** -23)).all()
+    assert ((lse - score - torch.log(n.double())).abs() <= 3000 * 2.0 ** -21 + (ln / 16 + 40) * 2.0 ** -22).all()
+    c.k[0, ln - tokens - 30] = 127 if score > 0 else -1
+    c.call()
+    capi.device_sync()
+    assert (c.out[0] == (1.0 if (ln - tokens - 30) % 2 == 0 else 0.0)).all()
+
+
 def test_large_offsets():
     """Rows of a cache beyond 2^32 bytes."""
     torch = _torch()
@@ -656,7 +696,7 @@ def test_large_offsets():
     del kv
 
 
-@pytest.mark.parametrize("tokens", [1, 9, 150])
+@pytest.mark.parametrize("tokens", [1, 7, 9, 150])
 def test_attention_in_graphs_and_on_streams(tokens):
     """Captured and replayed on other inputs; two calls at once with workspaces of their own; the same bits every time."""
     torch = _torch()
