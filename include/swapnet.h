@@ -981,8 +981,7 @@ int swapnet_cache_append(const swapnet_cache_rows* args, swapnet_stream stream);
  * by a power of two per query, which loses what is below 2^-39 of its largest
  * element), probabilities times their value scales as two fp16 parts: 22 bits,
  * off by at most 2^-39 of a query's largest such product up to 16 rows (tokens x
- * heads / kv_heads; 32 with a head_dim of 64), beyond by 2^-32 (2^-37 where more
- * than 32 rows are behind the first 2048 that a CTA takes of a long cache).  All that holds for value
+ * heads / kv_heads; 32 with a head_dim of 64), 2^-32 beyond.  All that for value
  * scales from 2^-48 to 2^64 beside one another; the values of smaller ones lose
  * bits, and from 2^-79 on may count as 0.  Scales are not negative.
  * `workspace` as for swapnet_attention_tree: a function of the sizes; how many

@@ -1,5 +1,5 @@
-// Attention of up to 32 query rows per key head (short drafted runs, decode
-// steps of wide groups) over a cache held in 8 bits, on the tcgen05 tensor cores
+// Attention of units of up to 32 query rows per key head (short drafted runs,
+// decode steps of wide groups, small calls) over a cache held in 8 bits, on the tcgen05 tensor cores
 // with the keys as the rows of their products; fp32 arithmetic, fixed orders of
 // summation.
 //

@@ -64,12 +64,14 @@ CachedPlan quant_plan(const QuantArgs& a, int* ctas, int* row_tile) {
   Way w;
   w.us = 1e30;
   if (a.group <= tile) w = way(a, rows <= 16 ? kFewCosts : kMoreCosts, tile, quant_few_resident(tile, a.dim));
-  if (rows > 16 && rows <= kQuantFewRows && a.dim == 128) {
-    // (32 sequences, 8 key heads of 32 rows, up to 8000 keys 112 us, on warp
-    // products 131; 4 of up to 500 keys 12.5 and 18.3; 64 rows as two units 208,
-    // with rows as rows 161)
+  if (rows > 16 && a.group <= kQuantFewRows && a.dim == 128) {
+    // 32 sequences, 8 key heads of 32 rows, up to 8000 keys 112 us, on warp
+    // products 131; 4 of up to 500 keys 12.5 and 18.3.  More rows are units that
+    // convert the same keys, which pays while every unit has an SM: 8 x 8 of 64
+    // rows, 2000 keys 26.6 us, with rows as the products' rows 42.1; 32 x 8 of
+    // them, up to 8000 keys 208 and 161.
     const Way t = way(a, kKeyCosts, kQuantFewRows, 1);
-    if (t.us <= w.us) {
+    if (t.us <= w.us && (rows <= kQuantFewRows || (t.splits == 1 && t.units <= kSms))) {
       w = t;
       p.tc = 2;
     }

@@ -45,7 +45,7 @@ constexpr int kQuantFewRows = 32;  // of a unit, at most, on warp products
 constexpr int quant_few_resident(int rows, int dim) { return rows <= 8 ? (dim == 64 ? 4 : 3) : rows <= 16 && dim == 64 ? 3 : 2; }
 int launch_quant_join(const QuantArgs& a, int queries, int row_tile, int nrt, cudaStream_t s);  // the units that runs shared
 int launch_quant_few(const QuantArgs& a, int ctas, int row_tile, cudaStream_t s);  // warp products, with the join
-int launch_quant_keys(const QuantArgs& a, int ctas, cudaStream_t s);  // tcgen05, keys as rows: up to 32 rows 128 wide, with the join
+int launch_quant_keys(const QuantArgs& a, int ctas, cudaStream_t s);  // tcgen05, keys as rows: units of 32 rows 128 wide, with the join
 int launch_quant_rows(const QuantArgs& a, int ctas, cudaStream_t s);  // tcgen05, with the join
 
 }  // namespace swapnet
