@@ -23,7 +23,7 @@ constexpr double kUnitUs = 5.0, kTileUs = 1.0, kJoinUs = 8.0;
 // the end (lengths and causal limits differ).  In microseconds: a tile of a CTA
 // by itself, a tile of an SM's time when all are busy, a CTA's start and end,
 // and the join where there is one.
-int choose_splits(int64_t ctas, int tiles, double alone, double busy, double fixed, double join) {
+static int choose_splits(int64_t ctas, int tiles, double alone, double busy, double fixed, double join) {
   int best = 1;
   double least = 1e30;
   for (int s = 1; s <= tiles && s <= 128; ++s) {

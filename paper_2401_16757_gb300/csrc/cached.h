@@ -61,8 +61,6 @@ int run_cached_attention(CachedArgs a, const CachedPlan& p, void* workspace, boo
 inline uint64_t plan_bytes(const CachedPlan& p) { return p.part_bytes + p.ml_bytes + p.score_bytes + p.unit_bytes; }
 int cached_launches(const CachedArgs& a, const CachedPlan& p);
 
-// How many CTAs share the keys of one of `ctas` units (cached.cpp).
-int choose_splits(int64_t ctas, int tiles, double alone, double busy, double fixed, double join);
 // The device error word of the current device (looked up once per device).
 int error_word(int** out);
 
@@ -86,8 +84,6 @@ inline bool shares(std::initializer_list<const void*> outs, std::initializer_lis
 
 int launch_attention_rows(const CachedArgs& a, bool early, cudaStream_t s);  // tcgen05
 int launch_attention_few(const CachedArgs& a, bool early, cudaStream_t s);
-// The units that several CTAs of a tensor-core attention shared (row_tile rows a slot).
-int launch_runs_join(const CachedArgs& a, int queries, int row_tile, int nrt, cudaStream_t s);
 int launch_attention_join(const CachedArgs& a, cudaStream_t s);   // splits -> out, lse (and weights from scores)
 int launch_weights(const CachedArgs& a, int splits, bool early, cudaStream_t s);  // tcgen05
 int weights_splits(const CachedArgs& a);

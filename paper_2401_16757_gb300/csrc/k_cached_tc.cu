@@ -1138,31 +1138,6 @@ __global__ void __launch_bounds__(32 * kRjWarps)
   }
 }
 
-}  // namespace
-
-int launch_runs_join(const CachedArgs& a, int queries, int row_tile, int nrt, cudaStream_t s) {
-  // eight blocks per SM that find work, but at least a warp and at most a block
-  // for a row (20 units of 28 tiles and 48 rows, up to 9 pieces each: 37.6 us
-  // with 6 blocks for a unit's rows, 25.5 with 48)
-  const int ctas = run_ctas(a.kv_heads);
-  const int64_t units = std::min<int64_t>((int64_t)a.n_seq * nrt * a.kv_heads, ctas);
-  const int rows = queries * a.group, least = (rows + kRjWarps - 1) / kRjWarps;
-  cudaLaunchConfig_t cfg;
-  std::memset(&cfg, 0, sizeof(cfg));
-  cfg.gridDim = dim3(std::min(rows, std::max(least, (int)(8 * kSms / units))), ctas);
-  cfg.blockDim = dim3(32 * kRjWarps);
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  const auto kern = a.dtype == SWAPNET_BF16 ? attention_runs_join_kernel<__nv_bfloat16> : attention_runs_join_kernel<__half>;
-  return done(cudaLaunchKernelEx(&cfg, kern, a, queries, row_tile), "cached attention join launch");
-}
-
-namespace {
-
 template <typename T, int D, int REP> int rows_t(const CachedArgs& a, bool early, cudaStream_t s) {
   static std::atomic<uint64_t> known{0};
   const auto kern = attention_rows_kernel<T, D, REP>;
@@ -1198,7 +1173,16 @@ template <typename T, int D, int REP> int rows_t(const CachedArgs& a, bool early
   cfg.numAttrs = early ? 1 : 0;
   rc = done(cudaLaunchKernelEx(&cfg, kern, q, k, v, kn, vn, a, queries, nrt), "cached attention launch");
   if (rc || a.splits == 1) return rc;
-  return launch_runs_join(a, queries, 128 / REP, nrt, s);
+  // eight blocks per SM that find work, but at least a warp and at most a block
+  // for a row (20 units of 28 tiles and 48 rows, up to 9 pieces each: 37.6 us
+  // with 6 blocks for a unit's rows, 25.5 with 48)
+  const int64_t units = std::min<int64_t>((int64_t)a.n_seq * nrt * a.kv_heads, ctas);
+  const int rows = queries * a.group, least = (rows + kRjWarps - 1) / kRjWarps;
+  cfg.gridDim = dim3(std::min(rows, std::max(least, (int)(8 * kSms / units))), ctas);
+  cfg.blockDim = dim3(32 * kRjWarps);
+  cfg.dynamicSmemBytes = 0;
+  cfg.numAttrs = 1;
+  return done(cudaLaunchKernelEx(&cfg, attention_runs_join_kernel<T>, a, queries, 128 / REP), "cached attention join launch");
 }
 template <typename T, int D> int rows_d(const CachedArgs& a, bool early, cudaStream_t s) {
   return a.tokens * a.group <= 64 ? rows_t<T, D, 2>(a, early, s) : rows_t<T, D, 1>(a, early, s);

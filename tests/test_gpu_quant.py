@@ -527,7 +527,12 @@ class Attend:
     # a unit over many runs: tails of one tile, rows that see nothing of them
     dict(dtype="f16", fmt="i8", n_seq=1, tokens=30, heads=1, kv_heads=1, dim=128, max_seq=20000, block=32, lens=[19970]),
     dict(dtype="bf16", fmt="e4m3", n_seq=1, tokens=300, heads=1, kv_heads=1, dim=128, max_seq=9000, block=64, lens=[8833]),
-    # 17 to 32 rows of 128 per key head
+    # many units of more rows
+    dict(dtype="bf16", fmt="i8", n_seq=20, tokens=100, heads=8, kv_heads=8, dim=128, max_seq=300, block=16,
+         lens=[(i * 97) % 201 + 100 for i in range(20)], counts=[100 - i * 5 for i in range(20)]),
+    dict(dtype="f16", fmt="e4m3", n_seq=30, tokens=50, heads=8, kv_heads=8, dim=128, max_seq=2000, block=64,
+         lens=[(i * 1237) % 2001 for i in range(30)], counts=[min(50 - i, (i * 1237) % 2001) for i in range(30)]),
+    # units of 17 to 32 rows of 128
     dict(dtype="f16", fmt="i8", n_seq=1, tokens=17, heads=1, kv_heads=1, dim=128, max_seq=128, block=16, lens=[128]),
     dict(dtype="bf16", fmt="e4m3", n_seq=5, tokens=8, heads=16, kv_heads=4, dim=128, max_seq=700, block=64, lens=[0, 3, 128, 129, 700],
          counts=[8, 5, 8, 0, 7], pad=16),
@@ -559,26 +564,26 @@ def test_attention_leaves_bad_sequences_alone(tokens, heads, max_seq):
     capi.device_sync()
 
 
-@pytest.mark.parametrize("tokens", [2, 12, 70, 200])
+@pytest.mark.parametrize("dim,tokens", [(128, 2), (128, 12), (128, 70), (128, 200), (64, 12), (64, 70), (64, 200)])
 @pytest.mark.parametrize("fmt", ["i8", "e4m3"])
-def test_scales_that_are_no_numbers_reach_only_the_queries_that_see_them(tokens, fmt):
+def test_scales_that_are_no_numbers_reach_only_the_queries_that_see_them(dim, tokens, fmt):
     """A block whose scale is no number: queries that see one of its rows get no number, the others are untouched by it,
     also where they share a tile with the block's rows; codes there may be any bytes."""
     torch = _torch()
     ln, B = 300, 16
-    good = Attend("bf16", fmt, 1, tokens, 4, 2, 128, 320, B, [ln], seed=11)
+    good = Attend("bf16", fmt, 1, tokens, 4, 2, dim, 320, B, [ln], seed=11)
     good.call()
     capi.device_sync()
     for which, value in (("ks", math.nan), ("vs", math.nan), ("vs", math.inf)):
-        c = Attend("bf16", fmt, 1, tokens, 4, 2, 128, 320, B, [ln], seed=11)
+        c = Attend("bf16", fmt, 1, tokens, 4, 2, dim, 320, B, [ln], seed=11)
         block = (ln - 2) // B  # the last rows but one, seen by the last queries
         getattr(c, which)[0, 1, block] = value
         for x in (c.k, c.v):
-            x.view(torch.uint8)[0, block * B:(block + 1) * B, 128:256] = 0x7f
+            x.view(torch.uint8)[0, block * B:(block + 1) * B, dim:2 * dim] = 0x7f
         c.call()
         capi.device_sync()
         first = max(0, block * B - (ln - tokens))  # the first query that sees the block
-        out, ref = c.out.view(1, tokens, 4, 128), good.out.view(1, tokens, 4, 128)
+        out, ref = c.out.view(1, tokens, 4, dim), good.out.view(1, tokens, 4, dim)
         assert torch.equal(out[:, :, :2], ref[:, :, :2])  # the other key head
         assert torch.equal(out[:, :first], ref[:, :first])
         if value == math.inf:
@@ -605,13 +610,13 @@ def test_a_dominant_key_hides_nothing(tokens):
     assert ((got - want[:, None]).abs() <= want[:, None] * (2.0 ** -11 + 2.0 ** -10 * 2.0 ** -3)).all()
 
 
-@pytest.mark.parametrize("tokens,max_seq", [(1, 900), (1, 9000), (12, 900), (40, 900), (150, 900)])
+@pytest.mark.parametrize("dim,tokens,max_seq", [(128, 1, 900), (128, 1, 9000), (128, 12, 900), (128, 40, 900), (64, 40, 900), (64, 150, 900)])
 @pytest.mark.parametrize("least", [2.0 ** -100, 2.0 ** -48])
-def test_zeros_beside_large_values_keep_their_weights(tokens, max_seq, least):
+def test_zeros_beside_large_values_keep_their_weights(dim, tokens, max_seq, least):
     """All scores equal; every other block of 16 rows has small values, the others large ones: the mean of what is seen."""
     torch = _torch()
     for large in (1.0, 2.0 ** 40, 2.0 ** 64):
-        c = Attend("bf16", "i8", 1, tokens, 2, 1, 128, max_seq, 16, [max_seq], seed=5)
+        c = Attend("bf16", "i8", 1, tokens, 2, 1, dim, max_seq, 16, [max_seq], seed=5)
         c.q.zero_(), c.v.fill_(64)
         c.vs[0, 0, 0::2], c.vs[0, 0, 1::2] = least, large
         if least < 2.0 ** -48:
@@ -645,16 +650,16 @@ def test_values_below_the_least_exponent():
             assert ((c.out.double().cpu()[0] - want).abs() <= tol).all(), (tokens, small)
 
 
-@pytest.mark.parametrize("tokens", [1, 12, 40, 150])
+@pytest.mark.parametrize("dim,tokens", [(128, 1), (128, 12), (128, 40), (64, 12), (64, 40), (64, 150)])
 @pytest.mark.parametrize("score", [-3000.0, 3000.0])
-def test_scores_far_from_zero(tokens, score):
+def test_scores_far_from_zero(dim, tokens, score):
     """All scores equal and far from what exponentials hold: the mean of the values seen; then one key above all others."""
     torch = _torch()
     ln = 1400
-    c = Attend("f16", "i8", 1, tokens, 2, 1, 128, ln, 32, [ln], seed=13)
+    c = Attend("f16", "i8", 1, tokens, 2, 1, dim, ln, 32, [ln], seed=13)
     c.k.fill_(64 if score > 0 else -64), c.ks.fill_(1.0), c.vs.fill_(2.0 ** -6)
     c.q.fill_(4.0)
-    c.scale = 3000 / (4 * 64 * 128.0)
+    c.scale = 3000 / (4.0 * 64 * dim)
     c.v.zero_()
     c.v[0, ::2] = 64
     c.call()
