@@ -66,7 +66,8 @@ CachedPlan quant_plan(const QuantArgs& a, int* ctas, int* row_tile) {
   if (a.group <= tile) w = way(a, rows <= 16 ? kFewCosts : kMoreCosts, tile, quant_few_resident(tile, a.dim));
   if (rows > 16 && a.group <= kQuantFewRows && a.dim == 128) {
     // 32 sequences, 8 key heads of 32 rows, up to 8000 keys 112 us, on warp
-    // products 131; 4 of up to 500 keys 12.5 and 18.3.  More rows are units that
+    // products 131 (16 rows 107 and 97, 8 x 8 of them on 2000 keys 24.5 and 22.6); 4
+    // of up to 500 keys 12.5 and 18.3.  More rows are units that
     // convert the same keys, which pays while every unit has an SM: 8 x 8 of 64
     // rows, 2000 keys 26.6 us, with rows as the products' rows 42.1; 32 x 8 of
     // them, up to 8000 keys 208 and 161.
