@@ -562,11 +562,16 @@ __global__ void __launch_bounds__(kQkThreads, 1)
         for (int k = 0; k < 16; ++k) x[2 * k] = l2[k].x, x[2 * k + 1] = l2[k].y;
         sums[(set * 4 + q4) * kRows + lane] = reduce32(x, [](float u, float v) { return u + v; });
       }
-      const int last = g0 + n - 1;
-      ok = ok && mbar_wait_bounded(pv_done(last), (last >> 1) & 1, abort_flag, a.err);
+      // a set waits for its own products alone (a wait for a phase of the other
+      // set's barrier would return at once while the phase before is open) and
+      // learns of the other's at the barrier, with a fence on either side
+      const int done = g0 + n - 1 - ((n - 1 - first) & 1);  // the set's last tile, if it has one
+      if (done >= g0 + first) ok = ok && mbar_wait_bounded(pv_done(done), (done >> 1) & 1, abort_flag, a.err);
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
+      tc_fence_before();
       asm volatile("bar.sync 3, 256;" ::: "memory");
+      tc_fence_after();
       float f[2], own[2], M = -INFINITY, L = 0.f;
       const float* minus_m = reinterpret_cast<const float*>(smem + kOffM) + (piece & 1) * 2 * kRows + lane;
 #pragma unroll

@@ -83,3 +83,47 @@ def test_dependents_start_only_once_a_kernel_holds_its_tensor_memory():
         between = body[body.index("tmem_alloc("):body.index("= *tmem_slot;")]
         assert "__syncthreads()" in between, (name, head)
     assert seen >= 6
+
+
+def _quant_keys_body():
+    return next(body for _, head, body in _kernels() if "attention_quant_keys_kernel" in head)
+
+
+def test_a_softmax_set_waits_for_every_phase_of_its_products():
+    """The two softmax sets of the attention with keys as rows take a run's tiles in turn, and the products of each
+    complete phases of a barrier of its own.  A set that skipped one would get the next wait's answer a phase early.  The
+    waits of the source, gone through for runs of pieces of all lengths."""
+    body = _quant_keys_body()
+    first = re.search(r"const int first = ([^;]+);", body).group(1)
+    assert re.search(r"for \(int i = first; i < n; i \+= 2\) \{\s*const int g = g0 \+ i,", body)
+    assert re.search(r"if \(i != first\) \{\s*ok = ok && mbar_wait_bounded\(pv_done\(g\), \(\(g >> 1\) - 1\) & 1,", body)
+    end = re.search(r"const int (\w+) = ([^;]+);\s*(?:if \(([^)]+)\) )?ok = ok && mbar_wait_bounded\(pv_done\(\1\), \(\1 >> 1\) & 1,", body)
+    assert end
+    for lengths in ([1] * 9, [2, 1, 3, 1, 1, 4, 2, 5, 1], [3, 3, 3], [7, 2, 1, 6], [5], [4, 1, 4]):
+        for s in range(2):
+            phases, g0 = {0: -1, 1: -1}, 0  # the last phase that the set knows to be over, of either barrier
+
+            def wait(tile):
+                assert phases[tile & 1] + 1 >= tile >> 1, (lengths, s, tile)
+                phases[tile & 1] = max(phases[tile & 1], tile >> 1)
+
+            for n in lengths:
+                names = {"g0": g0, "n": n, "set": s}
+                names["first"] = at = eval(first, {}, names)
+                for i in range(at + 2, n, 2):
+                    wait(g0 + i - 2)
+                names[end.group(1)] = tile = eval(end.group(2), {}, names)
+                if end.group(3) is None or eval(end.group(3), {}, names):
+                    wait(tile)
+                g0 += n
+                assert all(phases[t & 1] >= t >> 1 for t in range(g0) if t & 1 == s)  # all of its own
+
+
+def test_outputs_of_both_softmax_sets_pass_a_fenced_barrier():
+    """A piece's outputs of both sets are read from tensor memory behind a barrier of the two, each of which has waited for
+    its own products: a fence on either side orders them."""
+    body = _quant_keys_body()
+    at = body.rindex("pv_done(", 0, body.index("tmem_ld_x8("))
+    behind = body[at:body.index("tmem_ld_x8(", at)]
+    barrier = re.search(r'"bar\.sync 3, 256;"', behind)
+    assert "tc_fence_before()" in behind[:barrier.start()] and "tc_fence_after()" in behind[barrier.end():]
