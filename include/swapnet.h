@@ -1008,6 +1008,16 @@ int swapnet_attention_quantized_workspace(const swapnet_quantized_attention* arg
 int swapnet_attention_quantized(const swapnet_quantized_attention* args, void* workspace, uint64_t workspace_bytes,
                                 swapnet_stream stream);
 
+/* How the call would run, which goes by the sizes alone (diagnostics, and tests
+ * of a kernel's edges). */
+typedef struct swapnet_quantized_tiling {
+  int32_t kernel; /* 0 warp products; on the tensor cores 1 rows as rows, 2 keys as rows */
+  int32_t rows;   /* of a unit: queries x heads that share a key head            */
+  int32_t shared; /* 0 a CTA per unit; 1 equal runs of all units' tiles and a join */
+  int32_t ctas;
+} swapnet_quantized_tiling;
+int swapnet_attention_quantized_tiling(const swapnet_quantized_attention* args, swapnet_quantized_tiling* tiling);
+
 /* --------------------------------------------------------- host weights */
 /* Page-locked, device-mapped host memory for weight storage (the pinned
  * host copy that Sec. 4.2's swap-in reads): allocated by the CUDA driver in

@@ -141,6 +141,10 @@ class QuantizedAttention(C.Structure):
         [(n, C.c_int64) for n in ("q_stride", "kv_stride", "seq_stride", "out_stride")]
 
 
+class QuantizedTiling(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("kernel", "rows", "shared", "ctas")]
+
+
 EXPORTS = ["swapnet_default_options", "swapnet_partition", "swapnet_plan_from_cuts", "swapnet_plan_resident",
            "swapnet_plan_info_get", "swapnet_plan_cuts", "swapnet_plan_units", "swapnet_plan_blocks",
            "swapnet_plan_output_offsets", "swapnet_plan_free", "swapnet_schedule", "swapnet_load",
@@ -157,7 +161,7 @@ EXPORTS = ["swapnet_default_options", "swapnet_partition", "swapnet_plan_from_cu
            "swapnet_attention_tree_workspace", "swapnet_attention_tree", "swapnet_attention_weights",
            "swapnet_cache_evict", "swapnet_tree_accept", "swapnet_plan_state_layout", "swapnet_engine_tree_accept",
            "swapnet_engine_evict", "swapnet_device_sync", "swapnet_cache_append", "swapnet_attention_quantized_workspace",
-           "swapnet_attention_quantized"]
+           "swapnet_attention_quantized", "swapnet_attention_quantized_tiling"]
 
 _lib = None
 
@@ -242,6 +246,7 @@ def lib():
         "swapnet_cache_append": (C.c_int, [P, P]),  # (the packed block as it is)
         "swapnet_attention_quantized_workspace": (C.c_int, [C.POINTER(QuantizedAttention), C.POINTER(C.c_uint64)]),
         "swapnet_attention_quantized": (C.c_int, [C.POINTER(QuantizedAttention), P, C.c_uint64, P]),
+        "swapnet_attention_quantized_tiling": (C.c_int, [C.POINTER(QuantizedAttention), C.POINTER(QuantizedTiling)]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -528,6 +533,14 @@ def attention_quantized_workspace(args):
     n = C.c_uint64()
     check(lib().swapnet_attention_quantized_workspace(C.byref(args), C.byref(n)), "swapnet_attention_quantized_workspace")
     return n.value
+
+
+def attention_quantized_tiling(args):
+    """How attention_quantized would run: its kernel ("warp", "rows", "keys"), rows of a unit, whether units are shared by
+    runs of tiles, CTAs."""
+    t = QuantizedTiling()
+    check(lib().swapnet_attention_quantized_tiling(C.byref(args), C.byref(t)), "swapnet_attention_quantized_tiling")
+    return dict(kernel=("warp", "rows", "keys")[t.kernel], rows=t.rows, shared=bool(t.shared), ctas=t.ctas)
 
 
 def attention_quantized(args, workspace=0, workspace_bytes=0, stream=0):

@@ -309,6 +309,19 @@ int swapnet_attention_quantized_workspace(const swapnet_quantized_attention* c, 
   });
 }
 
+int swapnet_attention_quantized_tiling(const swapnet_quantized_attention* c, swapnet_quantized_tiling* t) {
+  return swapnet::guard_abi([&]() -> int {
+    using namespace swapnet;
+    if (!t) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "null output");
+    QuantArgs a;
+    if (int rc = check_quant(c, &a)) return rc;
+    int ctas, row_tile;
+    const CachedPlan p = quant_plan(a, &ctas, &row_tile);
+    *t = swapnet_quantized_tiling{p.tc, row_tile, p.splits != 1, ctas};
+    return SWAPNET_OK;
+  });
+}
+
 int swapnet_attention_quantized(const swapnet_quantized_attention* c, void* workspace, uint64_t workspace_bytes, swapnet_stream stream) {
   return swapnet::guard_abi([&]() -> int {
     using namespace swapnet;

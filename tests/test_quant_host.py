@@ -6,6 +6,8 @@ import pytest
 
 from paper_2401_16757_gb300 import capi
 
+from quant_ways import WAYS, tiling
+
 A = 1 << 20  # an aligned address; nothing is read from it
 
 
@@ -118,3 +120,21 @@ def test_argument_blocks_are_the_structs():
     assert C.sizeof(capi.CacheRows) == capi._ROWS.size and C.sizeof(capi.QuantizedAttention) == capi._QUANTIZED.size
     a = _attn(scale=0.5, out_stride=2048)
     assert (a.cache_dtype, a.block, a.scale, a.lse, a.out_stride) == (capi.I8, 32, 0.5, _at(8), 2048)
+
+
+@pytest.mark.parametrize("way", sorted(WAYS))
+@pytest.mark.parametrize("dtype,fmt,block", [("bf16", "i8", 16), ("f16", "e4m3", 128)])
+def test_sizes_that_run_each_kernel(way, dtype, fmt, block):
+    """What the tests of the kernels' edges rely on: a changed choice shows here."""
+    (n, t, h, kv, d, cap), want = WAYS[way]
+    a = _attn(dtype=dtype, cache_dtype=fmt, n_seq=n, tokens=t, heads=h, kv_heads=kv, head_dim=d, max_seq=cap, block=block)
+    assert tiling(a) == want
+    assert (capi.attention_quantized_workspace(a) > 0) == want[2]
+    assert capi.attention_quantized_tiling(a)["ctas"] >= 1
+
+
+def test_tiling_refuses():
+    lib, t = capi.lib(), capi.QuantizedTiling()
+    assert lib.swapnet_attention_quantized_tiling(None, C.byref(t)) == INVALID
+    assert lib.swapnet_attention_quantized_tiling(C.byref(_attn()), None) == INVALID
+    assert _code(capi.attention_quantized_tiling, _attn(block=24)) == UNSUPPORTED
