@@ -918,7 +918,8 @@ int swapnet_tree_accept(const swapnet_tree_acceptance* args, swapnet_stream stre
  *   q, k: x / sqrt(mean(x^2) + eps) * gain for each head (with a gain), then the
  *   rotation (with theta): pair i of the first rope_dim elements turned by
  *   position * theta^(-2 i / rope_dim); pairs are (2i, 2i + 1), with `halves`
- *   (i, i + rope_dim / 2).  Rounded once, to dtype.  v as it is.
+ *   (i, i + rope_dim / 2).  Rounded once, to dtype.  v as it is.  An angle is off
+ *   by at most 2^-21 and 2^-49 of position * theta^(-2 i / rope_dim).
  * With `sections` the pairs follow up to three position axes (e.g. time, height,
  * width): the first sections[0] pairs axis 0, the next sections[1] axis 1, the
  * rest axis 2.

@@ -141,9 +141,13 @@ template <int D> __device__ __forceinline__ void norm(Pairs& x, const Pairs& gai
 }
 
 // cos and sin of the angles of this lane's pairs at a token's position.  The
-// angle in turns is position * (hi + lo): the product with hi is split into
-// what it rounds to and the rest (fma), whole turns are taken off, and only
-// then is it an angle; far positions keep an error below 2^-23.  Less the
+// angle in turns is position * (hi + lo), |hi| at most 1/2: the product with hi
+// is split into what it rounds to (below 2^23) and the rest (fma, at most 1/4),
+// whole turns are taken off, and only then is it an angle.  Off by: the last sum
+// of turns, up to 3/4, 2^-25; the one before it, up to 1/4, 2^-26; lo's rounding
+// times the position 2^-26; 2 pi and the product with it 2^-24 in all: below
+// 2^-21 (2^-22 for positions below 4096), beside 2^-49 of position * frequency
+// that the frequency in 64 bits is off by.  Less the
 // nearest quarter turn it is at most pi / 4, where Taylor's series for sine
 // (to x^9) and cosine (to x^8) are within 2^-25; the quarters exchange and
 // negate the two.  Two pairs at a time: sincosf's share of the rows of 12000

@@ -159,10 +159,11 @@ int check_append(const swapnet_cache_rows* c, AppendArgs* a) {
     for (int k = 0; k < 8; ++k) fine[k] = std::pow((double)c->theta, -2.0 * k / rope) / kTurn;
     for (int i = 0; i < rope / 2; ++i) {
       if (i % 8 == 0) coarse = std::pow((double)c->theta, -2.0 * i / rope);
-      const double turns = coarse * fine[i % 8];
+      double turns = coarse * fine[i % 8];
+      if (!(turns <= 1e6)) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cache append: bad theta or eps");
+      turns = std::remainder(turns, 1.0);  // (positions are whole numbers; theta below 1: more than a turn each)
       a->turns[i].x = (float)turns;
       a->turns[i].y = (float)(turns - (double)a->turns[i].x);
-      if (!(turns <= 1e6)) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cache append: bad theta or eps");
     }
   } else if (c->positions) {
     SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cache append: positions without a rotation");

@@ -1,0 +1,68 @@
+"""swapnet_cache_append where its users' calls go beyond the sizes of
+test_gpu_quant.py."""
+import decimal
+
+import numpy as np
+import pytest
+
+from paper_2401_16757_gb300 import capi
+
+from test_gpu_quant import _stream, _torch
+
+pytestmark = pytest.mark.gpu
+
+
+def _angles(theta, rope, positions):
+    """position * theta^(-2 i / rope) less whole turns, as exact as float64 holds it, and the angles as they are: [t][pairs]."""
+    decimal.getcontext().prec = 60
+    D = decimal.Decimal
+    pi = D("3.14159265358979323846264338327950288419716939937510582097494459")
+    log = D(float(np.float32(theta))).ln()
+    freq = [(log * (-2 * i) / rope).exp() for i in range(rope // 2)]
+    rest = np.empty((len(positions), rope // 2))
+    for t, p in enumerate(positions):
+        for i, f in enumerate(freq):
+            x = int(p) * f
+            rest[t, i] = float(x - (x / (2 * pi)).to_integral_value() * 2 * pi)
+    return rest, np.outer(positions, [float(f) for f in freq])
+
+
+@pytest.mark.parametrize("theta,rope", [(10000.0, 128), (1e6, 48), (1.0, 128), (0.5, 128), (0.01, 128), (1e-4, 48), (1e-6, 128)])
+def test_angles_of_far_positions(theta, rope):
+    """Pairs (a, b) of large numbers chosen for each angle x so that a cos x - b sin x nearly vanishes: what is left shows the
+    angle's error, |(a, b)| times it.
+
+    Promised: 2^-21, and 2^-49 of position * frequency.  Sine and cosine as functions of the angle: 2^-23 (series 2^-25, their last step
+    2^-24).  The product b sin x: 2^-24 of itself; the sum and the result: half a step of fp16."""
+    torch = _torch()
+    rng = np.random.default_rng(int(theta * 8) + rope)
+    pos = np.concatenate([[0, 1, 2, 4095, (1 << 24) - 1, (1 << 23) + 1], rng.integers(1 << 22, 1 << 24, 26)])
+    rest, full = _angles(theta, rope, pos)
+    c, s = np.cos(rest), np.sin(rest)
+    n, pairs = rest.shape
+    # of the larger of cos and sin the partner is the quotient, rounded; the best of many
+    swap = np.abs(s) < np.abs(c)
+    big, small = np.where(swap, c, s), np.where(swap, s, c)
+    tries = rng.uniform(20000, 60000, (400, n, pairs)).astype(np.float16).astype(np.float64)
+    other = (tries * small / big).astype(np.float16).astype(np.float64)
+    best = np.abs(other * big - tries * small).argmin(0)[None]
+    lead, follow = (np.take_along_axis(x, best, 0)[0] for x in (tries, other))
+    a, b = np.where(swap, follow, lead), np.where(swap, lead, follow)
+    q = np.zeros((n, 2, 128))
+    q[:, 0, 0:rope:2], q[:, 0, 1:rope:2] = a, b          # u = a cos - b sin is small
+    q[:, 1, 0:rope:2], q[:, 1, 1:rope:2] = b, -a         # v = -a cos + b sin is small
+    dev = lambda x, t: torch.from_numpy(np.ascontiguousarray(x)).to(t).cuda()  # noqa: E731
+    q, rows = dev(q, torch.float16), torch.zeros(n, 128, dtype=torch.float16, device="cuda")
+    out, k, v = torch.zeros_like(q), torch.zeros_like(rows), torch.zeros_like(rows)
+    lens, at = dev(np.zeros(1), torch.int32), dev(pos, torch.int32)
+    capi.cache_append("f16", "f16", 1, n, 2, 1, 128, n, k_new=rows.data_ptr(), v_new=rows.data_ptr(), lens=lens.data_ptr(), k=k.data_ptr(),
+                      v=v.data_ptr(), q=q.data_ptr(), q_out=out.data_ptr(), positions=at.data_ptr(), theta=theta, rope_dim=rope, stream=_stream())
+    capi.device_sync()
+    got = out.double().cpu().numpy()
+    want = a * c - b * s
+    size = np.hypot(a, b)
+    tol = size * (2.0 ** -21 + 2.0 ** -49 * full) + (np.abs(a) + np.abs(b)) * 2.0 ** -23 + np.abs(b) * 2.0 ** -24 + 2.0 ** -11 * np.abs(want) + 2.0 ** -25
+    assert 2.0 ** -11 * np.abs(want).max() < 2.0 ** -3 * (size * 2.0 ** -21).max()  # (what fp16's step hides)
+    for x in (got[:, 0, 0:rope:2] - want, got[:, 1, 1:rope:2] + want):
+        worst = np.abs(x) / tol
+        assert (worst <= 1).all(), (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
