@@ -7,7 +7,7 @@ import pytest
 
 from paper_2401_16757_gb300 import capi
 
-from test_gpu_quant import _stream, _torch
+from test_gpu_quant import Append, _stream, _torch
 
 pytestmark = pytest.mark.gpu
 
@@ -66,3 +66,41 @@ def test_angles_of_far_positions(theta, rope):
     for x in (got[:, 0, 0:rope:2] - want, got[:, 1, 1:rope:2] + want):
         worst = np.abs(x) / tol
         assert (worst <= 1).all(), (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+
+
+def _bytes(x):
+    return x.contiguous().view(_torch().uint8)
+
+
+@pytest.mark.parametrize("fmt,dtype,dim", [("i8", "bf16", 128), ("e4m3", "f16", 64), ("bf16", "bf16", 128)])
+@pytest.mark.parametrize("tokens,lens,counts", [(5, [30, 0, 65], [5, 0, 4]), (150, [31, 32, 1], [150, 97, 130])])
+def test_sequence_strides(fmt, dtype, dim, tokens, lens, counts):
+    """A sequence's rows a padded number of elements apart, and rows of all sequences in turn: the rows of the packed call, bit
+    for bit, and nothing written beside them."""
+    torch = _torch()
+    n, kv, cap, block = 3, 2, 200, 32 if fmt in ("i8", "e4m3") else 0
+    kw = dict(dtype=dtype, fmt=fmt, n_seq=n, tokens=tokens, heads=4, kv_heads=kv, dim=dim, max_seq=cap, block=block, lens=lens, counts=counts,
+              norm=True, halves=True, seed=31)
+    want = Append(**kw)
+    want.call()
+    capi.device_sync()
+    kd = kv * dim
+    for kv_stride, seq_stride in ((kd, kd * cap + 48), (kd + 16, (kd + 16) * cap + 16), (n * kd, kd), (n * kd + 32, kd)):
+        total = (n - 1) * seq_stride + (cap - 1) * kv_stride + kd
+        c = Append(**kw)
+        k, v = (torch.full((total,), 7.0, device="cuda").to(want.k.dtype) for _ in range(2))
+        c.call(k=k.data_ptr(), v=v.data_ptr(), kv_stride=kv_stride, seq_stride=seq_stride)
+        capi.device_sync()
+        for flat, ref, scales, ref_scales in ((k, want.k, c.ks, want.ks), (v, want.v, c.vs, want.vs)):
+            left = _bytes(flat).clone().view(total, -1)
+            for b in range(n):
+                rows = torch.as_strided(flat, (cap, kd), (kv_stride, 1), b * seq_stride)
+                assert torch.equal(_bytes(rows), _bytes(ref[b]))
+                at = (b * seq_stride + torch.arange(cap, device="cuda")[:, None] * kv_stride + torch.arange(kd, device="cuda")).flatten()
+                left[at] = _bytes(torch.full((1,), 7.0, device="cuda").to(flat.dtype))
+            assert (left == left[:1]).all()
+            if block:
+                assert torch.equal(scales, ref_scales)
+        assert torch.equal(c.q_out, want.q_out)
+        if block:
+            assert torch.equal(c.ko2, want.ko2) and torch.equal(c.vo2, want.vo2)

@@ -318,3 +318,24 @@ def test_a_dominant_key_hides_nothing(way):
     # key up to 2^-39 or 2^-32 of the largest product
     tol = want * (2.0 ** -11 + 2.0 ** -13) + 2.0 ** -25 + n.double() * c.lost()
     assert ((c.out.double() - want[:, None]).abs() <= tol[:, None]).all()
+
+
+@way_of_call
+@pytest.mark.parametrize("dtype,fmt,block", [("bf16", "e4m3", 64), ("f16", "i8", 16)])
+def test_sequence_strides(way, dtype, fmt, block):
+    """A sequence's rows a padded number of codes apart, no multiple of a row's, and the sequences' rows in turn: the bits of the
+    packed call, whatever lies between."""
+    torch = _torch()
+    c = Wide(way, dtype, fmt, block, seed=26)
+    c.call()
+    capi.device_sync()
+    want, (n, cap, kd) = _bits(c.out, c.lse), c.k.shape
+    for kv_stride, seq_stride in ((kd, kd * cap + 48), (kd + 16, (kd + 16) * cap + 16), (n * kd, kd), (n * kd + 16, kd)):
+        total = (n - 1) * seq_stride + (cap - 1) * kv_stride + kd
+        flat = [torch.full((total,), 0x7f, dtype=torch.uint8, device="cuda") for _ in range(2)]
+        for x, of in zip(flat, (c.k, c.v)):
+            torch.as_strided(x, (n, cap, kd), (seq_stride, kv_stride, 1)).copy_(of.view(torch.uint8))
+        c.out.fill_(SENT), c.lse.fill_(SENT)
+        c.call(k=flat[0].data_ptr(), v=flat[1].data_ptr(), kv_stride=kv_stride, seq_stride=seq_stride)
+        capi.device_sync()
+        assert all(torch.equal(x, y) for x, y in zip(want, _bits(c.out, c.lse))), (kv_stride, seq_stride)
