@@ -104,3 +104,17 @@ def test_sequence_strides(fmt, dtype, dim, tokens, lens, counts):
         assert torch.equal(c.q_out, want.q_out)
         if block:
             assert torch.equal(c.ko2, want.ko2) and torch.equal(c.vo2, want.vo2)
+
+
+@pytest.mark.parametrize("fmt,dtype", [("i8", "bf16"), ("e4m3", "f16")])
+@pytest.mark.parametrize("tokens,lens,counts", [(5, [30, 7, 65, 31, 64, 0], [5, 0, 5, 0, 0, 0]), (1, [127, 33], [0, 0]), (40, [1, 95, 32], [0, 0, 40])])
+def test_requests_that_bring_nothing(fmt, dtype, tokens, lens, counts):
+    """Open rows elsewhere: those of a sequence without new tokens are passed on, its codes and scales left as they were."""
+    c = Append(dtype, fmt, len(lens), tokens, 4, 2, 64, 150, 32, lens, counts, norm=True, halves=True, seed=32)
+    c.call()
+    capi.device_sync()
+    c.check()
+    for b, (ln, count) in enumerate(zip(lens, counts)):
+        if count == 0:
+            assert (_bytes(c.ko2[b, :ln % 32]) == _bytes(c.ko[b, :ln % 32])).all() and (_bytes(c.vo2[b, :ln % 32]) == _bytes(c.vo[b, :ln % 32])).all()
+            assert (c.ks[b] == 7.0).all() and (c.k[b].double() == 7.0).all() and (c.vs[b] == 7.0).all() and (c.v[b].double() == 7.0).all()
