@@ -903,15 +903,24 @@ int swapnet_tree_accept(const swapnet_tree_acceptance* args, swapnet_stream stre
  * block, as long as it is not full, are kept in 16 bits as well: k_open, v_open,
  * [n_seq][block][kv_heads][head_dim], row j of the cache at j % block.  A row is
  * rounded to 8 bits from its 16-bit value whatever the calls that append it,
- * and the cache is a function of the rows alone (a sequence's last rows can be
- * taken back by a smaller length, as far as the start of its open block):
+ * and the cache is a function of the rows alone:
  *   E4M3  scale = the least power of two >= m / 448
  *   I8    scale = m / 127
  * with m the block's largest magnitude so far (scale at least 2^-100), code =
  * value / scale rounded to the nearest (ties to even).  A block with a value
  * that is infinite or not a number has a scale that is not a number (codes of
  * I8: 0; E4M3: not a number), and so is the attention of every query that sees
- * one of its rows. */
+ * one of its rows.
+ *
+ * A sequence's last rows can be taken back by a smaller length as far as the
+ * start of its open block, no further: the 16-bit rows of the block before are
+ * gone, and nothing would notice that those of another stand in their place.
+ * The open block's codes and scale stay as the rows taken back left them until
+ * the next append that brings the sequence a row.  To take back any number of a
+ * call's rows (a drafted run, part of which is accepted): append the run with
+ * other buffers for the open rows (and for the queries); once the counts are
+ * known, append it again, with those counts, from the same lens and open rows,
+ * which may now be updated in place. */
 
 /* Appends the rows of up to `tokens` new tokens per sequence to a cache, and
  * prepares their queries:

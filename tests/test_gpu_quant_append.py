@@ -118,3 +118,45 @@ def test_requests_that_bring_nothing(fmt, dtype, tokens, lens, counts):
         if count == 0:
             assert (_bytes(c.ko2[b, :ln % 32]) == _bytes(c.ko[b, :ln % 32])).all() and (_bytes(c.vo2[b, :ln % 32]) == _bytes(c.vo[b, :ln % 32])).all()
             assert (c.ks[b] == 7.0).all() and (c.k[b].double() == 7.0).all() and (c.vs[b] == 7.0).all() and (c.v[b].double() == 7.0).all()
+
+
+@pytest.mark.parametrize("fmt,dtype,block", [("i8", "bf16", 16), ("e4m3", "bf16", 32), ("e4m3", "f16", 64)])
+def test_a_draft_taken_back_across_a_block(fmt, dtype, block):
+    """A drafted run appended with its open rows elsewhere, then appended again from the open rows of before with the counts
+    that were accepted: the cache of those rows alone, bit for bit, whatever blocks the draft had begun."""
+    torch = _torch()
+    n, tokens, cap, dim = 5, 24, 160, 64
+    lens = [block - 3, block - 3, 2 * block - 1, block, 5]
+    accepted = [2, 9, 1, 24, 0]
+    kw = dict(dtype=dtype, fmt=fmt, n_seq=n, heads=4, kv_heads=2, dim=dim, max_seq=cap, block=block, norm=True, halves=True)
+
+    def prompt():
+        a = Append(tokens=max(lens), lens=[0] * n, counts=lens, seed=41, **kw)
+        a.call(in_place=True)
+        return a
+
+    def then(a, counts, **call):
+        c = Append(tokens=tokens, lens=lens, counts=counts, seed=42, **kw)
+        for name in ("k", "v", "ks", "vs", "ko", "vo"):
+            setattr(c, name, getattr(a, name))
+        c.gains = a.gains
+        c.v_new[:, 3:] *= 30  # (rejected rows that would enlarge the scales)
+        c.call(**call)
+        return c
+
+    a, b = prompt(), prompt()
+    then(a, [tokens] * n)                 # the draft: its open rows go elsewhere
+    x = then(a, accepted, in_place=True)  # what was accepted, from the state of before
+    y = then(b, accepted, in_place=True)  # as if there had been no draft
+    capi.device_sync()
+    assert x.lens_out.tolist() == y.lens_out.tolist() == [u + v for u, v in zip(lens, accepted)]
+    for s in range(n):
+        end = lens[s] + accepted[s]
+        for name in ("ko", "vo"):
+            assert torch.equal(_bytes(getattr(x, name)[s, :end % block]), _bytes(getattr(y, name)[s, :end % block]))
+        if accepted[s] == 0:
+            continue
+        for name in ("k", "v"):
+            assert torch.equal(_bytes(getattr(x, name)[s, :end]), _bytes(getattr(y, name)[s, :end]))
+        for name in ("ks", "vs"):
+            assert torch.equal(getattr(x, name)[s, :, :-(-end // block)], getattr(y, name)[s, :, :-(-end // block)])
