@@ -339,3 +339,36 @@ def test_sequence_strides(way, dtype, fmt, block):
         c.call(k=flat[0].data_ptr(), v=flat[1].data_ptr(), kv_stride=kv_stride, seq_stride=seq_stride)
         capi.device_sync()
         assert all(torch.equal(x, y) for x, y in zip(want, _bits(c.out, c.lse))), (kv_stride, seq_stride)
+
+
+@way_of_call
+def test_small_products_beside_large_ones(way):
+    """One key in 32 has nearly all of the weight and the value 0 in every dim but the first; the others' products are 2^-30 of
+    its own, or 2^-36 where a call promises 2^-39 of the largest: what they add up to is the output of the other dims."""
+    torch = _torch()
+    c, n = _full(way, "bf16", "i8", 16)
+    exact = c.lost() == 2.0 ** -39
+    below = 35.63 if exact else 29.63  # bits, no whole number of them: a lost low part shows
+    c.k.zero_(), c.ks.fill_(1.0), c.vs.fill_(2.0 ** 20)
+    c.q.fill_(0.5)
+    heavy = torch.arange(c.max_seq, device="cuda") % 32 == 9
+    c.k[:, heavy] = 4
+    c.scale = below * math.log(2) / (0.5 * 4 * c.d)  # of the heavy keys' scores
+    c.v.fill_(64)
+    first = torch.arange(c.kv, device="cuda") * c.d
+    c.v[:, heavy] = 0
+    for e in first.tolist():
+        c.v[:, heavy, e] = 64
+    c.call()
+    capi.device_sync()
+    many = ((n - 1 - 9) // 32 + 1).clamp(min=0).double()  # heavy keys seen
+    light, w = n.double() - many, 2.0 ** -below
+    want = light * w / (many + light * w) * 64 * 2.0 ** 20
+    # a score of up to 36 bits, rounded three times by 2^-24: 36 2^-22 of p; sums; half a step of bf16; what is promised of
+    # every light key's product, as a share of the heavy keys' sum
+    tol = want * (2.0 ** -8 + 36 * 2.0 ** -22 + (c.max_seq / 16 + 40) * 2.0 ** -23) + light / many * c.lost() * 64 * 2.0 ** 20
+    assert (tol < want / 3).all()
+    got = c.out.double().view(c.n, c.t, c.h, c.d)
+    assert ((got[..., 1:] - want[:, None, None]).abs() <= tol[:, None, None] * (1 + 2.0 ** -10)).all(), ((got[..., 1:] / want[:, None, None] - 1).abs().max().item())
+    near = 64 * 2.0 ** 20
+    assert ((got[..., 0] - near).abs() <= near * (2.0 ** -8 + 2.0 ** -12)).all()
