@@ -993,7 +993,11 @@ int swapnet_cache_append(const swapnet_cache_rows* args, swapnet_stream stream);
  * off by at most 2^-39 of a query's largest such product up to 16 rows (tokens x
  * heads / kv_heads; 32 with a head_dim of 64), 2^-32 beyond.  All that for value
  * scales from 2^-48 to 2^64 beside one another; the values of smaller ones lose
- * bits, and from 2^-79 on may count as 0.  Scales are not negative.
+ * bits, and from 2^-79 on may count as 0.  A key whose value scale is 2^112 below
+ * the largest (blocks of zeros count as 2^-48) may count for nothing in the sum of
+ * weights where its own is below 2^-28 of the largest (2^-21 where products are
+ * kept to 2^-32); nearer scales move that down bit by bit.  Scales are not
+ * negative.
  * `workspace` as for swapnet_attention_tree: a function of the sizes; how many
  * CTAs share a cache goes by max_seq.  Results and workspace overlap
  * none of the inputs.  Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA. */

@@ -72,8 +72,9 @@ __device__ __forceinline__ uint32_t numbers_only(uint32_t x) {
 // The softmax takes p = 2^(score + e - m) with p <= 2^14, adds p inv to its sum
 // and gives p f, at most 2^15, to the products.  A key loses its weight only
 // where p falls below 2^-126: one of a block of zeros beside value scales of
-// 2^64 where it is below 2^-28 of the largest (a least e of -100 left nothing of
-// zeros beside scales of 2^40).
+// 2^64 where it is below 2^-28 of the largest on warp products, whose m leaves
+// the largest p at 2^14, and 2^-21 on the tensor cores, where it may be 2^7 (a
+// least e of -100 left nothing of zeros beside scales of 2^40).
 constexpr float kTop = 14.0f;  // log2 of the largest p
 __device__ __forceinline__ void split_scale(float scale, float* e, float* f, float* inv) {
   const int x = min(max((int)(__float_as_uint(scale) >> 23 & 0xffu), 127 - 48), 253);

@@ -372,3 +372,29 @@ def test_small_products_beside_large_ones(way):
     assert ((got[..., 1:] - want[:, None, None]).abs() <= tol[:, None, None] * (1 + 2.0 ** -10)).all(), ((got[..., 1:] / want[:, None, None] - 1).abs().max().item())
     near = 64 * 2.0 ** 20
     assert ((got[..., 0] - near).abs() <= near * (2.0 ** -8 + 2.0 ** -12)).all()
+
+
+@way_of_call
+def test_weights_of_zeros_far_below(way):
+    """One key above all others, whose weights are 2^-20 of its own; every other block of 16 rows holds zeros beside value scales
+    of 2^64.  Their keys' weights still count, in lse and in what is divided by the sum."""
+    torch = _torch()
+    c, n = _full(way, "bf16", "i8", 16)
+    c.k.zero_(), c.ks.fill_(1.0), c.q.fill_(0.5)
+    c.k[:, 19] = 4
+    c.scale = 20 * math.log(2) / (0.5 * 4 * c.d)
+    c.v.fill_(64)
+    c.v[:, torch.arange(c.max_seq, device="cuda") % 32 < 16] = 0
+    c.vs[:, :, 0::2], c.vs[:, :, 1::2] = 2.0 ** -100, 2.0 ** 64
+    c.call()
+    capi.device_sync()
+    n, top = n.double(), 2.0 ** 20
+    lse = torch.log(top + n - 1)
+    big = (n // 32 * 16 + (n % 32 - 16).clamp(min=0))
+    want = 64 * 2.0 ** 64 * (top + big - 1) / (top + n - 1)
+    # a score of 20 bits, whose factors round by 2^-24 twice, with the scale's exponent 84: 2^-24 of all that; sums of n terms.
+    # What n / 2 lost weights would change is more
+    rel = 128 * 2.0 ** -24 + (c.max_seq / 16 + 40) * 2.0 ** -23
+    assert rel < (n / 4 / top).min()
+    assert ((c.lse.double() - lse).abs() <= rel + 2.0 ** -22 * lse).all()
+    assert ((c.out.double() - want[:, None]).abs() <= (want * (2.0 ** -8 + rel))[:, None]).all()
