@@ -161,7 +161,7 @@ int check_append(const swapnet_cache_rows* c, AppendArgs* a) {
       if (i % 8 == 0) coarse = std::pow((double)c->theta, -2.0 * i / rope);
       double turns = coarse * fine[i % 8];
       if (!(turns <= 1e6)) SN_FAIL(SWAPNET_ERR_INVALID_ARG, "cache append: bad theta or eps");
-      turns = std::remainder(turns, 1.0);  // (positions are whole numbers; theta below 1: more than a turn each)
+      if (turns > 0.5) turns -= std::rint(turns);  // (exact; positions are whole numbers, only theta below 1 has such)
       a->turns[i].x = (float)turns;
       a->turns[i].y = (float)(turns - (double)a->turns[i].x);
     }
