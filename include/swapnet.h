@@ -888,8 +888,9 @@ int swapnet_tree_accept(const swapnet_tree_acceptance* args, swapnet_stream stre
 
 /* ------------------------------------------------- quantised caches
  * A key-value cache held in 8 bits, with a scale for each block of rows and key
- * head: half the bytes beside the arena, and half the bytes for every decode
- * step to read.  swapnet_cache_append prepares a step's queries and puts its
+ * head: half the bytes to hold, and for every decode step to read.  For programs
+ * that keep their caches themselves: a decoder engine's, and those of the calls
+ * above, have 16 bits.  swapnet_cache_append prepares a step's queries and puts its
  * rows into the cache; swapnet_attention_quantized reads it.  What is said of
  * the cached-attention calls above (streams, captures, workspaces, errors found
  * on the device, the current device) holds for these as well.  The paper has no

@@ -295,7 +295,7 @@ template <> __device__ __forceinline__ uint32_t larger2<__nv_bfloat16>(uint32_t 
 // 8 codes of x / scale, to nearest even; inv = 1 / scale.
 // E4M3: the product with the reciprocal of a power of two is the quotient.  I8:
 // the product's rest x - q scale, times the reciprocal, makes it the quotient as
-// a division rounds it (for every pair of 16-bit x and largest magnitude), at a
+// a division rounds it (Markstein's correction; for every pair of 16-bit x and largest magnitude), at a
 // third of a division's instructions; adding 1.5 * 2^23 rounds it to a whole
 // number in the low bits.
 template <typename T, int CODE> __device__ __forceinline__ uint2 codes8(const uint4& w, float scale, float inv) {

@@ -66,7 +66,7 @@ template <int D, int NR, int W> struct QfCfg {
 // rescaled and no lane asks another.  With NR 4 the outputs fill half of the
 // registers, and the queries stay in shared memory.
 // Measured: one token of 64 sequences, 8 key heads (group 4) of 128, I8, up to
-// 16384 rows (1.57 GB): 254 to 268 us, 5.8 to 6.2 TB/s; the same loads without
+// 16384 rows (1.57 GB): 254 to 268 us by the card, 5.8 to 6.2 TB/s; the same loads without
 // any product take 252, a copy of as many bytes 238, so that DRAM bounds it.  12
 // rows of 4 key heads of 64, E4M3, on 131001 rows: 26.6 us, of which start, end
 // and join are 11.  32 rows of 32 x 8 (sequence, head)s on up to 8000 rows (0.34

@@ -24,7 +24,7 @@
 // issued, as a pair: half of the waits of a tile at a time.
 // Measured: 1000 queries on 4096 rows, 2 sequences x 32 heads, f16, I8: 181 us,
 // 0.49 PFLOP/s (the second product of P not counted; the 16-bit caches' 124); 64
-// rows of 32 x 8 units on up to 8000 rows about 135.  No pipe is full: a tile of
+// rows of 32 x 8 units on up to 8000 rows, bf16, E4M3: 161.  No pipe is full: a tile of
 // 128 x 128 takes about 4300 cycles, of which the tensor pipe is busy for 1540,
 // the softmax warps for 2500 (64 rows: 1700), the conversion for 1550 (E4M3
 // 1000); shared memory moves by count 260 KB of the 450 that it could, half of it

@@ -23,9 +23,10 @@ constexpr Costs kFewCosts = {3.0, 0.9, 0.8, 5.0, 1.0}, kMoreCosts = {6.0, 1.3, 1
 // CTAs that share the tiles of all units: as many as are resident, or for up to
 // 16 rows, which the memory bounds, up to six times that where their runs are
 // long: the memory does not serve all SMs alike, and CTAs that start later even
-// that out (one token of 64 sequences, up to 16384 rows: 269 us with 456 runs,
-// whose times lie between 174 and 279, 254 with six times as many; 32 rows pay
-// more for a run's end: 127 us with 304 runs, 141 with twice as many).
+// that out (one token of 64 sequences, up to 16384 rows: 273 us with 456 runs,
+// whose times lie between 174 and 279, 268 with three times, 259 with six times
+// as many; 32 rows pay more for a run's end: 127 us with 304 runs, 141 with
+// twice as many).
 constexpr int kRunLeast = 24;  // tiles of such a run
 
 // A way to run a call: rows of a unit, how its tiles are shared, its cost.
